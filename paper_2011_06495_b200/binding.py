@@ -27,6 +27,8 @@ MV_SELECT_STATIC_MAX_D = 1 << 24
 MV_MODE_AUTO = 0
 MV_MODE_GENERAL = 1
 MV_MODE_TRACK = 2
+MV_F32, MV_BF16, MV_F16, MV_I32, MV_I64 = 0, 1, 2, 3, 4
+MV_TOP_MAX = 64
 MV_DBG_CAND_OVERFLOW, MV_DBG_WINDOW_OVERFLOW, MV_DBG_FALLBACK, MV_DBG_LIST_OVERFLOW = 1, 2, 4, 8
 MV_DBG_PICK_RANGE, MV_DBG_LIST_RANGE, MV_DBG_OUT_RANGE, MV_DBG_GATHER_RANGE, MV_DBG_INTERNAL = 16, 32, 64, 128, 256
 
@@ -128,6 +130,30 @@ def _open(path: str, how: str) -> ctypes.CDLL:
     lib.mv_quantize.argtypes = [c_vp, c_vp, c_i64, c_i, c_vp, c_vp, c_vp, c_sz]
     lib.mv_dequantize.restype = c_i
     lib.mv_dequantize.argtypes = [c_vp, c_vp, c_i64, c_i, c_vp]
+    # language-model operators (include/mv_lm.h)
+    c_f = ctypes.c_float
+    lib.mv_embed.restype = c_i
+    lib.mv_embed.argtypes = [c_vp, c_vp, c_i, c_i64, c_i64, c_i64, c_vp, c_i, c_i64, c_f, c_vp, c_i, c_i64]
+    lib.mv_embed_grad_workspace_bytes.restype = c_sz
+    lib.mv_embed_grad_workspace_bytes.argtypes = [c_i64, c_i64, c_i64]
+    lib.mv_embed_grad.restype = c_i
+    lib.mv_embed_grad.argtypes = [c_vp, c_vp, c_i, c_i64, c_vp, c_i, c_i64, c_i64, c_i64, c_f, c_i64, c_i, c_vp, c_i64, c_vp, c_sz]
+    lib.mv_token_logprob.restype = c_i
+    lib.mv_token_logprob.argtypes = [c_vp, c_vp, c_i, c_i64, c_i64, c_i64, c_vp, c_i, c_f, c_i, c_vp, c_vp, c_vp, c_vp, c_vp]
+    lib.mv_token_logprob_grad.restype = c_i
+    lib.mv_token_logprob_grad.argtypes = [c_vp, c_vp, c_i, c_i64, c_i64, c_i64, c_vp, c_i, c_f, c_vp, c_vp, c_vp, c_vp, c_vp, c_i64]
+    lib.mv_clip_workspace_bytes.restype = c_sz
+    lib.mv_clip_workspace_bytes.argtypes = [c_vp, c_i, c_i]
+    lib.mv_clip_create.restype = c_i
+    lib.mv_clip_create.argtypes = [ctypes.POINTER(c_vp), c_vp, c_vp, c_vp, c_vp, c_vp, c_i, c_i, c_vp, c_sz]
+    lib.mv_clip_destroy.restype = c_i
+    lib.mv_clip_destroy.argtypes = [c_vp]
+    lib.mv_clip_norm.restype = c_i
+    lib.mv_clip_norm.argtypes = [c_vp, c_vp, c_vp]
+    lib.mv_clip_scale.restype = c_i
+    lib.mv_clip_scale.argtypes = [c_vp, c_vp, c_f, c_vp]
+    lib.mv_clip_pack.restype = c_i
+    lib.mv_clip_pack.argtypes = [c_vp, c_vp, c_f, c_vp, c_i64, c_vp]
     lib.mv_set_tail_kernel.restype = c_i
     lib.mv_set_tail_kernel.argtypes = [c_vp, c_i]
     lib.mv_fallback_count.restype = c_i
@@ -208,6 +234,164 @@ def mv_quantize(v, q: int, words, workspace, value_range=None, stream: Optional[
 
 def mv_dequantize(words, K: int, q: int, out, stream: Optional[torch.cuda.Stream] = None):
     _check(load().mv_dequantize(_stream_ptr(words, stream), _ptr(words), int(K), int(q), _ptr(out)), "mv_dequantize")
+
+
+_TYPES = {torch.float32: MV_F32, torch.bfloat16: MV_BF16, torch.float16: MV_F16, torch.int32: MV_I32, torch.int64: MV_I64}
+
+
+def _need(ok: bool, where: str):
+    """Shapes, types and devices that the raw pointers of the C call no longer show."""
+    if not ok:
+        raise MvError(MV_ERR_INVALID_ARG, where)
+
+
+def _addr(t: Optional[torch.Tensor]):
+    return None if t is None else t.data_ptr()
+
+
+def _raw_stream(t: torch.Tensor, stream: Optional[torch.cuda.Stream]):
+    return (stream if stream is not None else torch.cuda.current_stream(t.device)).cuda_stream
+
+
+def _matrix(t: torch.Tensor, kinds, where: str):
+    """(type code, rows, columns, row pitch) of a 2-d tensor whose rows are contiguous."""
+    code = _TYPES.get(t.dtype, -1)
+    _need(t.dim() == 2 and code in kinds and t.is_cuda and (t.stride(1) == 1 or t.shape[1] == 1), where)
+    rows, cols = t.shape
+    return code, rows, cols, t.stride(0) if rows > 1 else cols
+
+
+_VALUES, _IDS = (MV_F32, MV_BF16, MV_F16), (MV_I32, MV_I64)
+
+
+def _vector(t: Optional[torch.Tensor], n: int, kinds, dev, where: str):
+    """Type code of a contiguous 1-d tensor of n elements (None passes as the first kind)."""
+    if t is None:
+        return kinds[0]
+    code = _TYPES.get(t.dtype, -1)
+    _need(t.dim() == 1 and t.shape[0] == n and code in kinds and t.device == dev and (n <= 1 or t.stride(0) == 1), where)
+    return code
+
+
+def mv_embed(weight, ids, out, scale: float = 1.0, stream: Optional[torch.cuda.Stream] = None):
+    """out[t] = scale * weight[ids[t]]; weight [V, D], ids [T], out [T, D]."""
+    w_type, V, D, ldw = _matrix(weight, _VALUES, "mv_embed")
+    o_type, T, Do, ldo = _matrix(out, _VALUES, "mv_embed")
+    i_type = _vector(ids, T, _IDS, weight.device, "mv_embed")
+    _need(Do == D and out.device == weight.device, "mv_embed")
+    _check(load().mv_embed(_raw_stream(out, stream), _addr(weight), w_type, V, D, ldw, _addr(ids), i_type, T, float(scale), _addr(out),
+                           o_type, ldo), "mv_embed")
+
+
+def embed_grad_workspace_bytes(T: int, V: int, D: int) -> int:
+    return int(load().mv_embed_grad_workspace_bytes(int(T), int(V), int(D)))
+
+
+def mv_embed_grad(dout, ids, dweight, workspace, scale: float = 1.0, pad_id: int = -1, accumulate: bool = False,
+                  stream: Optional[torch.cuda.Stream] = None):
+    """dweight[v] (+)= scale * sum of dout over the tokens with id v; dout [T, D], ids [T], dweight float [V, D]."""
+    x_type, T, D, ldd = _matrix(dout, _VALUES, "mv_embed_grad")
+    _, V, Dw, ldw = _matrix(dweight, (MV_F32,), "mv_embed_grad")
+    i_type = _vector(ids, T, _IDS, dout.device, "mv_embed_grad")
+    _need(Dw == D and dweight.device == dout.device and workspace.device == dout.device and workspace.is_contiguous(), "mv_embed_grad")
+    _check(load().mv_embed_grad(_raw_stream(dout, stream), _addr(dout), x_type, ldd, _addr(ids), i_type, T, V, D, float(scale), int(pad_id),
+                                int(accumulate), _addr(dweight), ldw, _addr(workspace), workspace.numel() * workspace.element_size()),
+           "mv_embed_grad")
+
+
+def mv_token_logprob(logits, targets=None, scale: float = 1.0, logprob=None, entropy=None, lse=None, top_logprob=None, top_id=None,
+                     stream: Optional[torch.cuda.Stream] = None):
+    """Log probabilities of targets [T] under softmax(scale * logits), logits [T, V]; logprob, entropy, lse: float [T];
+    top_logprob float [T, k], top_id int32 [T, k].  An output that is None is not computed."""
+    x_type, T, V, ld = _matrix(logits, _VALUES, "mv_token_logprob")
+    dev = logits.device
+    i_type = _vector(targets, T, _IDS, dev, "mv_token_logprob")
+    for t in (logprob, entropy, lse):
+        _vector(t, T, (MV_F32,), dev, "mv_token_logprob")
+    k = 0
+    for t, kind in ((top_logprob, torch.float32), (top_id, torch.int32)):
+        if t is not None:
+            _need(t.dim() == 2 and t.shape[0] == T and t.is_contiguous() and t.dtype == kind and t.device == dev and k in (0, t.shape[1]),
+                  "mv_token_logprob")
+            k = t.shape[1]
+    _check(load().mv_token_logprob(_raw_stream(logits, stream), _addr(logits), x_type, T, V, ld, _addr(targets), i_type, float(scale), k,
+                                   _addr(logprob), _addr(entropy), _addr(lse), _addr(top_logprob), _addr(top_id)), "mv_token_logprob")
+
+
+def mv_token_logprob_grad(logits, targets, lse, g_logprob, dlogits, scale: float = 1.0, entropy=None, g_entropy=None,
+                          stream: Optional[torch.cuda.Stream] = None):
+    """dlogits [T, V] of sum(g_logprob * logprob + g_entropy * entropy); dlogits may be logits.  g_logprob (with targets)
+    or g_entropy (with entropy) may be None."""
+    x_type, T, V, ld = _matrix(logits, _VALUES, "mv_token_logprob_grad")
+    d_type, Td, Vd, ldg = _matrix(dlogits, _VALUES, "mv_token_logprob_grad")
+    dev = logits.device
+    i_type = _vector(targets, T, _IDS, dev, "mv_token_logprob_grad")
+    for t in (lse, g_logprob, entropy, g_entropy):
+        _vector(t, T, (MV_F32,), dev, "mv_token_logprob_grad")
+    _need((d_type, Td, Vd) == (x_type, T, V) and dlogits.device == dev, "mv_token_logprob_grad")
+    _check(load().mv_token_logprob_grad(_raw_stream(logits, stream), _addr(logits), x_type, T, V, ld, _addr(targets), i_type, float(scale),
+                                        _addr(lse), _addr(entropy), _addr(g_logprob), _addr(g_entropy), _addr(dlogits), ldg),
+           "mv_token_logprob_grad")
+
+
+class MvClip:
+    """A plan over a fixed list of contiguous tensors, which it keeps alive with its workspace; `groups` (ascending) says
+    which tensors share a norm (None: all of them)."""
+
+    def __init__(self, tensors, groups=None, n_groups: Optional[int] = None, stream: Optional[torch.cuda.Stream] = None, device=None):
+        self.handle = None
+        self.lib = load()
+        self.tensors = list(tensors)
+        n = len(self.tensors)
+        dev = torch.device(device) if device is not None else self.tensors[0].device if n else torch.device("cuda", torch.cuda.current_device())
+        groups = [0] * n if groups is None else [int(g) for g in groups]
+        self.n_groups = int(n_groups) if n_groups is not None else (max(groups) + 1 if n else 1)
+        lengths = [0] * max(self.n_groups, 1)
+        for t, g in zip(self.tensors, groups):
+            if 0 <= g < self.n_groups:
+                lengths[g] += t.numel()
+        self.longest = max(lengths)              # elements of the longest group: what a row has to hold
+        _need(len(groups) == n and all(t.is_cuda and t.device == dev and t.is_contiguous() for t in self.tensors), "mv_clip_create")
+        ptrs = (ctypes.c_void_p * n)(*[t.data_ptr() for t in self.tensors])
+        types = (ctypes.c_int * n)(*[_TYPES.get(t.dtype, -1) for t in self.tensors])
+        numel = (ctypes.c_int64 * n)(*[t.numel() for t in self.tensors])
+        group = (ctypes.c_int * n)(*groups)
+        nbytes = int(self.lib.mv_clip_workspace_bytes(numel, n, self.n_groups))
+        _need(nbytes > 0, "mv_clip_workspace_bytes")
+        self.workspace = torch.empty(nbytes, dtype=torch.uint8, device=dev)
+        handle = ctypes.c_void_p()
+        _check(self.lib.mv_clip_create(ctypes.byref(handle), _raw_stream(self.workspace, stream), ptrs, types, numel, group, n, self.n_groups,
+                                       _addr(self.workspace), nbytes), "mv_clip_create")
+        self.handle = handle
+
+    def close(self):
+        if getattr(self, "handle", None):
+            self.lib.mv_clip_destroy(self.handle)
+            self.handle = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+    def _norms(self, norms, where):
+        _vector(norms, self.n_groups, (MV_F32,), self.workspace.device, where)
+
+    def mv_clip_norm(self, norms, stream: Optional[torch.cuda.Stream] = None):
+        self._norms(norms, "mv_clip_norm")
+        _check(self.lib.mv_clip_norm(self.handle, _raw_stream(self.workspace, stream), _addr(norms)), "mv_clip_norm")
+
+    def mv_clip_scale(self, max_norm: float, norms=None, stream: Optional[torch.cuda.Stream] = None):
+        self._norms(norms, "mv_clip_scale")
+        _check(self.lib.mv_clip_scale(self.handle, _raw_stream(self.workspace, stream), float(max_norm), _addr(norms)), "mv_clip_scale")
+
+    def mv_clip_pack(self, max_norm: float, rows, norms=None, stream: Optional[torch.cuda.Stream] = None):
+        self._norms(norms, "mv_clip_pack")
+        _, G, d, ld = _matrix(rows, (MV_F32,), "mv_clip_pack")
+        _need(G == self.n_groups and d >= self.longest and rows.device == self.workspace.device, "mv_clip_pack")
+        _check(self.lib.mv_clip_pack(self.handle, _raw_stream(self.workspace, stream), float(max_norm), _addr(rows), ld, _addr(norms)),
+               "mv_clip_pack")
 
 
 class MvContext:

@@ -7,8 +7,9 @@ import sys
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 SRC = os.path.join(HERE, "csrc", "mv_sparse.cu")
-SRCS = [SRC, os.path.join(HERE, "csrc", "mv_wire.cu")]
-HDRS = [os.path.join(os.path.dirname(HERE), "include", h) for h in ("mv_sparse.h", "mv_wire.h")]
+SRCS = [SRC, *(os.path.join(HERE, "csrc", f) for f in ("mv_wire.cu", "mv_embed.cu", "mv_token.cu", "mv_clip.cu"))]
+HDRS = [*(os.path.join(os.path.dirname(HERE), "include", h) for h in ("mv_sparse.h", "mv_wire.h", "mv_lm.h")),
+        os.path.join(HERE, "csrc", "mv_lm.cuh")]
 LIB = os.path.join(HERE, "libmvsparse.so")
 LIB_DEBUG = os.path.join(HERE, "libmvsparse_debug.so")      # the checked build (-DMV_DEBUG), see mv_debug_status
 

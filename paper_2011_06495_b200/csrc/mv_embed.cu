@@ -1,118 +1,375 @@
 // mv_embed.cu -- embedding lookup with scaling, and its gradient by sorted tokens, for sm_100a.
+//
+// Both only move bytes (a multiplication or an addition per element), so both are bound by memory: what counts is
+// that every lane has several independent 16-byte loads in flight and that nothing is moved twice.
 #include "mv_lm.cuh"
 
 namespace {
 
-// ------------------------------------------------------------------------------------------ lookup
-template <typename W, typename O>
-__global__ void __launch_bounds__(256) k_embed(const W* __restrict__ weight, int64_t V, int64_t D, int64_t ldw, const void* __restrict__ ids,
-                                                int id_type, int64_t T, float scale, O* __restrict__ out, int64_t ldo) {
-  for (int64_t t = blockIdx.x; t < T; t += gridDim.x) {
-    const int64_t v = load_id(ids, id_type, t, V);
-    for (int64_t j = threadIdx.x; j < D; j += blockDim.x)
-      out[t * ldo + j] = v >= 0 ? from_f<O>(to_f(weight[v * ldw + j]) * scale) : from_f<O>(0.0f);
-  }
+// A lane's share of a row: 16 bytes of the input type where the rows allow it (VEC: consecutive elements), else as many
+// single elements, 32 apart, so that a warp's accesses stay contiguous.
+template <typename X> constexpr int LANE = 16 / int(sizeof(X));
+template <typename X> constexpr int BLOCK = 32 * LANE<X>;         // columns per warp
+
+template <typename X, bool VEC> __device__ __forceinline__ int64_t column(int64_t cb, int lane, int j) {
+  return VEC ? cb * BLOCK<X> + lane * LANE<X> + j : cb * BLOCK<X> + j * 32 + lane;
 }
 
-// ------------------------------------------------------------------------------------------ gradient
-// The tokens fall into `nb` buckets (a power of two) by id mod nb, so that the frequent tokens, which have
-// neighbouring ids, spread over all buckets.  The CTA of a bucket reads all ids, counts its own ids in shared
-// memory (one counter per id / nb) and writes its tokens grouped by id, in token order, to `perm`.
-constexpr int SORT_TPB = 256;
-constexpr int SORT_BINS = 8192;      // ids per bucket, at most
+// The raw elements of one row, loaded without being converted (so that loads of several rows can be outstanding).
+template <typename X> struct Raw { X e[LANE<X>]; };
 
-struct EmbedWs { size_t perm, row, total; };
-inline EmbedWs embed_ws(int64_t T) {
-  EmbedWs L;
-  size_t o = 0;
-  L.perm = o; o = align_up(o + size_t(T) * 4, 16);
-  L.row = o;  o = align_up(o + size_t(T) * 4, 16);
-  L.total = o ? o : 16;
-  return L;
-}
-
-inline int64_t bucket_count(int64_t V) {
-  int64_t nb = 128;
-  while ((V + nb - 1) / nb > SORT_BINS) nb *= 2;
-  return nb;
-}
-
-__global__ void __launch_bounds__(SORT_TPB) k_embed_sort(const void* __restrict__ ids, int id_type, int64_t T, int64_t V, int64_t pad_id,
-                                                          int nb_log, int32_t* __restrict__ perm, int32_t* __restrict__ row) {
-  extern __shared__ uint32_t cnt[];                 // [ids of this bucket]: tokens per id, then the next slot of the id
-  __shared__ uint32_t s_below, s_scan[SORT_TPB];
-  const int64_t nb = int64_t(1) << nb_log;
-  const int b = blockIdx.x;
-  const int bins = int((V - b + nb - 1) >> nb_log);
-  for (int i = threadIdx.x; i < bins; i += SORT_TPB) cnt[i] = 0;
-  if (threadIdx.x == 0) s_below = 0;
-  __syncthreads();
-  uint32_t below = 0;
-  for (int64_t t = threadIdx.x; t < T; t += SORT_TPB) {
-    const int64_t v = load_id(ids, id_type, t, V);
-    if (v < 0 || v == pad_id) continue;
-    const int64_t m = v & (nb - 1);
-    if (m < b) ++below;
-    else if (m == b) atomicAdd(&cnt[v >> nb_log], 1u);
-  }
-  atomicAdd(&s_below, below);
-  __syncthreads();
-  // exclusive scan of the counters: every thread takes consecutive ones
-  const int per = (bins + SORT_TPB - 1) / SORT_TPB;
-  const int i0 = min(bins, int(threadIdx.x) * per), i1 = min(bins, i0 + per);
-  uint32_t sum = 0;
-  for (int i = i0; i < i1; ++i) sum += cnt[i];
-  s_scan[threadIdx.x] = sum;
-  __syncthreads();
-  if (threadIdx.x == 0) {
-    uint32_t run = s_below;
-    for (int i = 0; i < SORT_TPB; ++i) { uint32_t c = s_scan[i]; s_scan[i] = run; run += c; }
-  }
-  __syncthreads();
-  uint32_t run = s_scan[threadIdx.x];
-  for (int i = i0; i < i1; ++i) { uint32_t c = cnt[i]; cnt[i] = run; run += c; }
-  __syncthreads();
-  // the first warp goes through the tokens in order
-  if (threadIdx.x >= 32) return;
-  for (int64_t t0 = 0; t0 < T; t0 += 32) {
-    const int64_t t = t0 + threadIdx.x;
-    const int64_t v = t < T ? load_id(ids, id_type, t, V) : -1;
-    const bool mine = v >= 0 && v != pad_id && (v & (nb - 1)) == b;
-    const unsigned any = __ballot_sync(0xffffffffu, mine);
-    if (!any) continue;
-    if (mine) {
-      const unsigned same = __match_any_sync(any, int(v));
-      const int rank = __popc(same & ((1u << threadIdx.x) - 1u));
-      const uint32_t slot = cnt[v >> nb_log] + rank;
-      perm[slot] = int32_t(t);
-      row[slot] = int32_t(v);
-      __syncwarp(any);
-      if (rank == 0) cnt[v >> nb_log] += __popc(same);
+template <typename X, bool VEC> __device__ __forceinline__ void load_raw(const X* row, int64_t D, int64_t cb, int lane, uint4& u) {
+  Raw<X> r;
+  if constexpr (VEC) {
+    const int64_t c0 = column<X, true>(cb, lane, 0);
+    if (c0 + LANE<X> <= D) {
+      u = __ldg(reinterpret_cast<const uint4*>(row + c0));
+      return;
     }
+#pragma unroll
+    for (int j = 0; j < LANE<X>; ++j) r.e[j] = c0 + j < D ? row[c0 + j] : from_f<X>(0.0f);
+  } else {
+#pragma unroll
+    for (int j = 0; j < LANE<X>; ++j) {
+      const int64_t c = column<X, false>(cb, lane, j);
+      r.e[j] = c < D ? row[c] : from_f<X>(0.0f);
+    }
+  }
+  memcpy(&u, &r, 16);
+}
+
+// ------------------------------------------------------------------------------------------ lookup
+// A warp takes R tokens and one block of columns: it reads the R ids with one load, then R independent pieces of rows.
+constexpr int EMBED_TPB = 128;
+
+template <typename W, typename O, bool VEC, int R>
+__global__ void __launch_bounds__(EMBED_TPB) k_embed(const W* __restrict__ weight, int64_t V, int64_t D, int64_t ldw, const void* __restrict__ ids,
+                                                      int id_type, int64_t T, float scale, O* __restrict__ out, int64_t ldo, int ncb) {
+  const int lane = threadIdx.x & 31;
+  const int64_t item = int64_t(blockIdx.x) * (EMBED_TPB / 32) + (threadIdx.x >> 5);
+  const int64_t t0 = item / ncb * R, cb = item % ncb;
+  if (t0 >= T) return;
+  const int n = int(min(int64_t(R), T - t0));
+  const int64_t mine = lane < n ? load_id(ids, id_type, t0 + lane, V) : -1;
+  uint4 u[R];
+#pragma unroll
+  for (int i = 0; i < R; ++i) {
+    const int64_t v = __shfl_sync(0xffffffffu, mine, i);
+    u[i] = make_uint4(0, 0, 0, 0);
+    if (v >= 0) load_raw<W, VEC>(weight + v * ldw, D, cb, lane, u[i]);
+  }
+#pragma unroll
+  for (int i = 0; i < R; ++i) {
+    if (i >= n) break;
+    const bool known = __shfl_sync(0xffffffffu, mine, i) >= 0;      // an unknown id gives +0 whatever the scale
+    Raw<W> r;
+    memcpy(&r, &u[i], 16);
+    struct alignas(sizeof(O) * LANE<W> < 16 ? sizeof(O) * LANE<W> : 16) Row { O e[LANE<W>]; } o;
+#pragma unroll
+    for (int j = 0; j < LANE<W>; ++j) o.e[j] = from_f<O>(known ? to_f(r.e[j]) * scale : 0.0f);
+    O* dst = out + (t0 + i) * ldo;
+    const int64_t c0 = column<W, VEC>(cb, lane, 0);
+    if (VEC && c0 + LANE<W> <= D) {
+      *reinterpret_cast<Row*>(dst + c0) = o;
+    } else {
+#pragma unroll
+      for (int j = 0; j < LANE<W>; ++j) {
+        const int64_t c = column<W, VEC>(cb, lane, j);
+        if (c < D) dst[c] = o.e[j];
+      }
+    }
+  }
+}
+
+// ------------------------------------------------------------------------------------------ gradient: grouping the tokens
+// The tokens fall into nb buckets (a power of two) by id mod nb, so that the frequent tokens, which have neighbouring
+// ids, spread over all buckets.  The CTA of a bucket reads all ids twice.  First it counts: for each of its warps, which
+// own consecutive stretches of the tokens, how many tokens of each of the bucket's ids the stretch holds, and how many
+// tokens belong to lower buckets.  A scan over (id, warp) turns the counts into places, and the second reading puts every
+// token at its place: grouped by id, in token order, without a sort and whatever the skew.  Then the CTA clears
+// the rows of those of its ids that no token has.
+constexpr int SORT_TPB = 1024;
+constexpr int SORT_WARPS = SORT_TPB / 32;
+constexpr int SORT_BINS = 1024;      // ids per bucket, at most: one thread each in the scan, 128 KB of counters
+constexpr int PIECE = 32;            // sorted tokens per warp of the summation
+
+struct EmbedPlan {
+  int nb_log;
+  int64_t bins;                      // counters per bucket
+  int64_t buckets;                   // buckets that hold an id
+  int64_t pieces, ncb;
+  size_t perm, row, start, valid, ticket, part, total;
+};
+
+inline EmbedPlan embed_plan(int64_t T, int64_t V, int64_t D, int block) {
+  EmbedPlan p;
+  p.nb_log = 7;
+  while (((V - 1) >> p.nb_log) + 1 > SORT_BINS) ++p.nb_log;
+  p.bins = ((V - 1) >> p.nb_log) + 1;
+  p.buckets = V < (int64_t(1) << p.nb_log) ? V : int64_t(1) << p.nb_log;
+  p.pieces = (T + PIECE - 1) / PIECE;
+  p.ncb = (D + block - 1) / block;
+  size_t o = 0;
+  p.valid = o;  o = align_up(o + 4, 16);
+  p.perm = o;   o = align_up(o + size_t(T) * 4, 16);
+  p.row = o;    o = align_up(o + size_t(T) * 4, 16);
+  p.start = o;  o = align_up(o + size_t(p.buckets) * size_t(p.bins + 1) * 4, 16);
+  p.ticket = o; o = align_up(o + size_t(p.pieces) * size_t(p.ncb) * 4, 16);
+  p.part = o;   o = align_up(o + size_t(p.pieces) * 2 * size_t(D) * 4, 16);
+  p.total = o;
+  return p;
+}
+
+struct SortArgs {
+  const void* ids;
+  int64_t T, V, pad_id;
+  int nb_log, bins;
+  int32_t *perm, *row, *start, *valid;
+  uint32_t* ticket;
+  int64_t n_ticket;
+  float* fill;                       // the table whose untouched rows are cleared, or null
+  int64_t D, ldw;
+};
+
+// A row of zeros, written by one warp: single words up to a 16-byte boundary, then 16 bytes a lane.
+__device__ __forceinline__ void clear_row(float* p, int64_t D, int lane) {
+  const int64_t head = min(D, int64_t((16 - (reinterpret_cast<uintptr_t>(p) & 15)) / 4 & 3));
+  if (lane < head) p[lane] = 0.0f;
+  float4* q = reinterpret_cast<float4*>(p + head);
+  const int64_t nv = (D - head) >> 2;
+  for (int64_t i = lane; i < nv; i += 32) q[i] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+  const int64_t done = head + 4 * nv;
+  if (lane < D - done) p[done + lane] = 0.0f;
+}
+
+template <typename ID>
+__global__ void __launch_bounds__(SORT_TPB) k_embed_sort(SortArgs a) {
+  extern __shared__ uint32_t cnt[];                 // [warp][bin] counts, then next places; behind them [bin] places of the ids
+  __shared__ uint32_t s_warp[SORT_WARPS], s_below[SORT_WARPS];
+  constexpr int U = 8;                              // independent id loads per lane
+  const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
+  const int b = blockIdx.x;
+  const int bins = a.bins;
+  const int64_t nb_mask = (int64_t(1) << a.nb_log) - 1;
+  uint32_t* first = cnt + SORT_WARPS * bins;
+  uint32_t* own = cnt + w * bins;
+  const ID* ids = static_cast<const ID*>(a.ids);
+  for (int64_t i = int64_t(b) * SORT_TPB + threadIdx.x; i < a.n_ticket; i += int64_t(gridDim.x) * SORT_TPB) a.ticket[i] = 0;
+  for (int i = threadIdx.x; i < SORT_WARPS * bins; i += SORT_TPB) cnt[i] = 0;
+  __syncthreads();
+  const int64_t seg = (a.T + SORT_TPB - 1) / SORT_TPB * 32;
+  const int64_t lo = min(a.T, w * seg), hi = min(a.T, lo + seg);
+  uint32_t below = 0;
+  for (int64_t t0 = lo; t0 < hi; t0 += 32 * U) {
+    int64_t v[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int64_t t = t0 + u * 32 + lane;
+      v[u] = t < hi ? int64_t(ids[t]) : -1;
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      if (v[u] < 0 || v[u] >= a.V || v[u] == a.pad_id) continue;
+      const int m = int(v[u] & nb_mask);
+      if (m < b) ++below;
+      else if (m == b) atomicAdd(&own[v[u] >> a.nb_log], 1u);
+    }
+  }
+  below = __reduce_add_sync(0xffffffffu, below);
+  if (lane == 0) s_below[w] = below;
+  __syncthreads();
+  // places: an exclusive scan over the ids' totals, then over the warps of each id
+  uint32_t total = 0;
+  if (int(threadIdx.x) < bins)
+    for (int i = 0; i < SORT_WARPS; ++i) total += cnt[i * bins + threadIdx.x];
+  uint32_t incl = total;
+  for (int o = 1; o < 32; o <<= 1) {
+    const uint32_t x = __shfl_up_sync(0xffffffffu, incl, o);
+    if (lane >= o) incl += x;
+  }
+  if (lane == 31) s_warp[w] = incl;
+  __syncthreads();
+  uint32_t place = incl - total;
+  for (int i = 0; i < SORT_WARPS; ++i) place += s_below[i] + (i < w ? s_warp[i] : 0u);
+  if (int(threadIdx.x) < bins) {
+    first[threadIdx.x] = place;
+    a.start[int64_t(b) * (bins + 1) + threadIdx.x] = int32_t(place);
+    uint32_t run = place;
+    for (int i = 0; i < SORT_WARPS; ++i) { const uint32_t c = cnt[i * bins + threadIdx.x]; cnt[i * bins + threadIdx.x] = run; run += c; }
+    if (int(threadIdx.x) == bins - 1) {
+      first[bins] = run;
+      a.start[int64_t(b) * (bins + 1) + bins] = int32_t(run);
+      if (b == int(gridDim.x) - 1) *a.valid = int32_t(run);
+    }
+  }
+  __syncthreads();
+  asm volatile("griddepcontrol.launch_dependents;");      // the sums may be set up; they wait for the end of this kernel
+  for (int64_t t0 = lo; t0 < hi; t0 += 32 * U) {
+    int64_t v[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int64_t t = t0 + u * 32 + lane;
+      v[u] = t < hi ? int64_t(ids[t]) : -1;
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const bool mine = v[u] >= 0 && v[u] < a.V && v[u] != a.pad_id && int(v[u] & nb_mask) == b;
+      const unsigned any = __ballot_sync(0xffffffffu, mine);
+      if (any == 0) continue;
+      if (mine) {
+        const unsigned same = __match_any_sync(any, int(v[u]));
+        const int rank = __popc(same & ((1u << lane) - 1u));
+        const int bin = int(v[u] >> a.nb_log);
+        const uint32_t slot = own[bin] + rank;
+        __syncwarp(any);
+        if (rank == 0) own[bin] += __popc(same);
+        a.perm[slot] = int32_t(t0 + u * 32 + lane);
+        a.row[slot] = int32_t(v[u]);
+      }
+      __syncwarp();
+    }
+  }
+  if (a.fill == nullptr) return;
+  for (int i = w; i < bins; i += SORT_WARPS) {
+    const int64_t v = (int64_t(i) << a.nb_log) + b;
+    if (v < a.V && first[i] == first[i + 1]) clear_row(a.fill + v * a.ldw, a.D, lane);
+  }
+}
+
+// ------------------------------------------------------------------------------------------ gradient: the sums
+// A warp takes one piece of PIECE sorted tokens and one block of columns and adds the rows up in order.  A run of
+// equal ids that lies inside the piece is finished there.  One that crosses into other pieces leaves a partial sum per
+// piece; the warp that leaves the last one adds the partial sums up in the order of the pieces.  So a frequent token's
+// rows are read by many warps, and the result does not depend on which of them comes last.
+struct SumArgs {
+  const int32_t *perm, *row, *start, *valid;
+  uint32_t* ticket;
+  float* part;                       // [piece][0: the run that the piece begins with, 1: the one it ends with][D]
+  int64_t D, ldd, ldw;
+  float scale;
+  int accumulate, nb_log, bins, ncb;
+  int dw_aligned;                    // the table's rows start at multiples of 16 bytes
+  float* dweight;
+};
+
+constexpr int SUM_TPB = 256;
+
+template <typename X> struct Lanes { float v[LANE<X>]; };
+
+template <typename X, bool VEC>
+__device__ __forceinline__ void put_row(const SumArgs& a, int64_t v, int64_t cb, int lane, const Lanes<X>& acc, float* stage) {
+  float* dst = a.dweight + v * a.ldw;
+  if (VEC && a.dw_aligned && column<X, VEC>(cb, lane, 0) + LANE<X> <= a.D) {
+#pragma unroll
+    for (int j = 0; j < LANE<X>; j += 4) {
+      float4* q = reinterpret_cast<float4*>(dst + column<X, VEC>(cb, lane, j));
+      float4 o = make_float4(acc.v[j] * a.scale, acc.v[j + 1] * a.scale, acc.v[j + 2] * a.scale, acc.v[j + 3] * a.scale);
+      if (a.accumulate) {
+        const float4 old = *q;
+        o.x += old.x; o.y += old.y; o.z += old.z; o.w += old.w;
+      }
+      *q = o;
+    }
+    return;
+  }
+  const bool turn = VEC && !a.dw_aligned;            // turn the block through shared memory: contiguous words for the warp
+  if (turn) {
+#pragma unroll
+    for (int j = 0; j < LANE<X>; ++j) stage[lane * LANE<X> + j] = acc.v[j];
     __syncwarp();
   }
+#pragma unroll
+  for (int j = 0; j < LANE<X>; ++j) {
+    const int64_t c = turn ? cb * BLOCK<X> + j * 32 + lane : column<X, VEC>(cb, lane, j);
+    const float x = (turn ? stage[j * 32 + lane] : acc.v[j]) * a.scale;
+    if (c < a.D) dst[c] = a.accumulate ? dst[c] + x : x;
+  }
+  if (turn) __syncwarp();
 }
 
-__global__ void k_zero(float* __restrict__ dst, int64_t V, int64_t D, int64_t ldw) {
-  for (int64_t v = blockIdx.x; v < V; v += gridDim.x)
-    for (int64_t j = threadIdx.x; j < D; j += blockDim.x) dst[v * ldw + j] = 0.0f;
+// Partial sums are kept in lane order (not column order): [piece][slot][block of columns][j][lane].
+template <typename X> __device__ __forceinline__ float* part_at(const SumArgs& a, int64_t piece, int slot, int64_t cb, int lane) {
+  return a.part + ((piece * 2 + slot) * a.ncb + cb) * BLOCK<X> + lane;
 }
 
-// A CTA per sorted position; the one that starts a run sums it.
-template <typename T_>
-__global__ void __launch_bounds__(256) k_embed_sum(const T_* __restrict__ dout, int64_t ldd, const int32_t* __restrict__ perm, const int32_t* __restrict__ row,
-                                                    int64_t T, int64_t D, float scale, int accumulate, float* __restrict__ dweight, int64_t ldw) {
-  for (int64_t s = blockIdx.x; s < T; s += gridDim.x) {
-    const int32_t v = row[s];
-    if (v < 0 || (s > 0 && row[s - 1] == v)) continue;
-    for (int64_t j = threadIdx.x; j < D; j += blockDim.x) {
-      float acc = 0.0f;
-      for (int64_t u = s; u < T && row[u] == v; ++u) acc += to_f(dout[int64_t(perm[u]) * ldd + j]);
-      float* p = dweight + int64_t(v) * ldw + j;
-      *p = accumulate ? *p + acc * scale : acc * scale;
+// The end of a run (or of the piece inside one).  Not inlined: it stands behind each of the unrolled rows.
+template <typename X, bool VEC>
+__device__ __noinline__ void end_run(const SumArgs* __restrict__ pa, int v, int piece, int cb, bool whole, int slot, Lanes<X> acc, float* stage) {
+  const SumArgs& a = *pa;
+  const int lane = threadIdx.x & 31;
+  if (!whole) {
+    float* q = part_at<X>(a, piece, slot, cb, lane);
+#pragma unroll
+    for (int j = 0; j < LANE<X>; ++j) __stcg(q + j * 32, acc.v[j]);
+    const int32_t* st = a.start + int64_t(v & ((1 << a.nb_log) - 1)) * (a.bins + 1) + (v >> a.nb_log);
+    const int first = st[0], p0 = first / PIECE, p1 = (st[1] - 1) / PIECE;
+    __threadfence();
+    __syncwarp();
+    uint32_t arrived = 0;
+    if (lane == 0) arrived = atomicAdd(a.ticket + int64_t(p0) * a.ncb + cb, 1u);
+    if (__shfl_sync(0xffffffffu, arrived, 0) != uint32_t(p1 - p0)) return;
+    __threadfence();
+    const float* q0 = part_at<X>(a, p0, first % PIECE ? 1 : 0, cb, lane);
+#pragma unroll
+    for (int j = 0; j < LANE<X>; ++j) acc.v[j] = __ldcg(q0 + j * 32);
+    const int64_t step = 2 * int64_t(a.ncb) * BLOCK<X>;
+    const float* q1 = part_at<X>(a, p0 + 1, 0, cb, lane);
+#pragma unroll 4
+    for (int k = p0 + 1; k <= p1; ++k, q1 += step)
+#pragma unroll
+      for (int j = 0; j < LANE<X>; ++j) acc.v[j] += __ldcg(q1 + j * 32);
+  }
+  put_row<X, VEC>(a, v, cb, lane, acc, stage);
+}
+
+template <typename X, bool VEC>
+__global__ void __launch_bounds__(SUM_TPB) k_embed_sum(const X* __restrict__ dout, const __grid_constant__ SumArgs a) {
+  __shared__ float s_stage[SUM_TPB / 32][BLOCK<X>];
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  constexpr int E = LANE<X>, U = 8;
+  const int lane = threadIdx.x & 31;
+  float* stage = s_stage[threadIdx.x >> 5];
+  const int64_t item = int64_t(blockIdx.x) * (SUM_TPB / 32) + (threadIdx.x >> 5);
+  const int64_t piece = item / a.ncb, cb = item % a.ncb;
+  const int64_t s0 = piece * PIECE, valid = *a.valid;
+  if (s0 >= valid) return;
+  const int n = int(min(int64_t(PIECE), valid - s0));
+  const int32_t p = lane < n ? a.perm[s0 + lane] : 0;
+  const int32_t r = lane < n ? a.row[s0 + lane] : -1;
+  const int32_t before = s0 > 0 ? a.row[s0 - 1] : -1;
+  const int32_t after = s0 + n < valid ? a.row[s0 + n] : -1;
+  const int32_t r0 = __shfl_sync(0xffffffffu, r, 0);
+  const int32_t next = __shfl_down_sync(0xffffffffu, r, 1);
+  const unsigned ends = __ballot_sync(0xffffffffu, lane < n && (lane == n - 1 || next != r));   // last token of a run (or of the piece)
+  Lanes<X> acc;
+#pragma unroll
+  for (int j = 0; j < E; ++j) acc.v[j] = 0.0f;
+  for (int i0 = 0; i0 < n; i0 += U) {
+    uint4 u[U];
+#pragma unroll
+    for (int i = 0; i < U; ++i) {
+      const int64_t t = __shfl_sync(0xffffffffu, p, i0 + i);
+      if (i0 + i < n) load_raw<X, VEC>(dout + t * a.ldd, a.D, cb, lane, u[i]);
+    }
+#pragma unroll
+    for (int i = 0; i < U; ++i) {
+      if (i0 + i >= n) break;
+      Raw<X> x;
+      memcpy(&x, &u[i], 16);
+#pragma unroll
+      for (int j = 0; j < E; ++j) acc.v[j] += to_f(x.e[j]);
+      if (!(ends >> (i0 + i) & 1u)) continue;
+      const int32_t v = __shfl_sync(0xffffffffu, r, i0 + i);
+      const bool from_before = v == r0 && before == v;
+      const bool goes_on = i0 + i == n - 1 && after == v;
+      end_run<X, VEC>(&a, v, int(piece), int(cb), !from_before && !goes_on, v == r0 ? 0 : 1, acc, stage);
+#pragma unroll
+      for (int j = 0; j < E; ++j) acc.v[j] = 0.0f;
     }
   }
 }
+
+inline bool rows_aligned(const void* p, int64_t ld, int size, int bytes) { return !misaligned(p, bytes) && ld * size % bytes == 0; }
 
 }  // namespace
 
@@ -131,8 +388,15 @@ int mv_embed(void* stream, const void* weight, int w_type, int64_t V, int64_t D,
     return with_type(out_type, [&](auto o) {
       using W = decltype(w);
       using O = decltype(o);
-      k_embed<W, O><<<unsigned(T < (1 << 16) ? T : (1 << 16)), 256, 0, st>>>(static_cast<const W*>(weight), V, D, ldw, ids, id_type, T, scale,
-                                                                              static_cast<O*>(out), ldo);
+      const int64_t ncb = (D + BLOCK<W> - 1) / BLOCK<W>;
+      const int ob = int(sizeof(O)) * LANE<W> < 16 ? int(sizeof(O)) * LANE<W> : 16;
+      const bool vec = rows_aligned(weight, ldw, sizeof(W), 16) && rows_aligned(out, ldo, sizeof(O), ob);
+      // eight tokens a warp once that still gives every multiprocessor its warps; below, the latency of one row counts
+      const int R = T * ncb >= 148 * 64 * 8 ? 8 : 1;
+      const int64_t items = (T + R - 1) / R * ncb, grid = (items + EMBED_TPB / 32 - 1) / (EMBED_TPB / 32);
+      if (grid >= lim) return int(MV_ERR_INVALID_ARG);
+      auto* kernel = vec ? (R == 8 ? k_embed<W, O, true, 8> : k_embed<W, O, true, 1>) : (R == 8 ? k_embed<W, O, false, 8> : k_embed<W, O, false, 1>);
+      kernel<<<unsigned(grid), EMBED_TPB, 0, st>>>(static_cast<const W*>(weight), V, D, ldw, ids, id_type, T, scale, static_cast<O*>(out), ldo, int(ncb));
       return cuda_ok();
     });
   });
@@ -141,7 +405,9 @@ int mv_embed(void* stream, const void* weight, int w_type, int64_t V, int64_t D,
 size_t mv_embed_grad_workspace_bytes(int64_t T, int64_t V, int64_t D) {
   const int64_t lim = int64_t(1) << 31;
   if (T < 0 || T >= lim || V < 1 || V >= lim || D < 1 || D >= lim) return 0;
-  return embed_ws(T).total;
+  // the largest any type of dout needs: blocks of 128 columns (32 bits) give the most tickets, of 256 (16 bits) the widest rows
+  const EmbedPlan a = embed_plan(T, V, (D + 127) / 128 * 128, 128), b = embed_plan(T, V, (D + 255) / 256 * 256, 256);
+  return a.total > b.total ? a.total : b.total;
 }
 
 int mv_embed_grad(void* stream, const void* dout, int dout_type, int64_t ldd, const void* ids, int id_type, int64_t T, int64_t V,
@@ -152,25 +418,53 @@ int mv_embed_grad(void* stream, const void* dout, int dout_type, int64_t ldd, co
       ldw < D || (accumulate != 0 && accumulate != 1) || !dweight || (T > 0 && (!dout || !ids)) || misaligned(dout, type_size(dout_type)) ||
       misaligned(ids, type_size(id_type)) || misaligned(dweight, 4) || misaligned(workspace, 16))
     return MV_ERR_INVALID_ARG;
-  const EmbedWs L = embed_ws(T);
-  if (!workspace || workspace_bytes < L.total) return MV_ERR_WORKSPACE;
+  if (!workspace || workspace_bytes < mv_embed_grad_workspace_bytes(T, V, D)) return MV_ERR_WORKSPACE;
+  const int block = dout_type == MV_F32 ? BLOCK<float> : BLOCK<__half>;
+  const EmbedPlan p = embed_plan(T, V, (D + block - 1) / block * block, block);
+  const int64_t items = p.pieces * p.ncb, grid = (items + SUM_TPB / 32 - 1) / (SUM_TPB / 32);
+  if (grid >= lim) return MV_ERR_INVALID_ARG;
+  if (accumulate && T == 0) return MV_OK;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
-  int32_t* perm = reinterpret_cast<int32_t*>(static_cast<char*>(workspace) + L.perm);
-  int32_t* row = reinterpret_cast<int32_t*>(static_cast<char*>(workspace) + L.row);
-  if (!accumulate) k_zero<<<unsigned(V < (1 << 16) ? V : (1 << 16)), 256, 0, st>>>(dweight, V, D, ldw);
+  char* base = static_cast<char*>(workspace);
+  SortArgs s;
+  s.ids = ids; s.T = T; s.V = V; s.pad_id = pad_id; s.nb_log = p.nb_log; s.bins = int(p.bins);
+  s.perm = reinterpret_cast<int32_t*>(base + p.perm);
+  s.row = reinterpret_cast<int32_t*>(base + p.row);
+  s.start = reinterpret_cast<int32_t*>(base + p.start);
+  s.valid = reinterpret_cast<int32_t*>(base + p.valid);
+  s.ticket = reinterpret_cast<uint32_t*>(base + p.ticket);
+  s.n_ticket = items;
+  s.fill = accumulate ? nullptr : dweight;
+  s.D = D; s.ldw = ldw;
+  const size_t smem = (size_t(SORT_WARPS) * p.bins + p.bins + 1) * 4;
+  auto* sort = id_type == MV_I32 ? k_embed_sort<int32_t> : k_embed_sort<int64_t>;
+  if (smem > 48 * 1024 && cudaFuncSetAttribute(sort, cudaFuncAttributeMaxDynamicSharedMemorySize, int(smem)) != cudaSuccess) {
+    cudaGetLastError();
+    return MV_ERR_CUDA;
+  }
+  sort<<<unsigned(p.buckets), SORT_TPB, smem, st>>>(s);
   if (T == 0) return cuda_ok();
-  if (cudaMemsetAsync(row, 0xff, size_t(T) * 4, st) != cudaSuccess) return MV_ERR_CUDA;
-  const int64_t nb = bucket_count(V);
-  int nb_log = 0;
-  while ((int64_t(1) << nb_log) < nb) ++nb_log;
-  const int64_t buckets = V < nb ? V : nb;
-  const size_t smem = size_t((V + nb - 1) / nb) * 4;
-  k_embed_sort<<<unsigned(buckets), SORT_TPB, smem, st>>>(ids, id_type, T, V, pad_id, nb_log, perm, row);
+  SumArgs a;
+  a.perm = s.perm; a.row = s.row; a.start = s.start; a.valid = s.valid; a.ticket = s.ticket;
+  a.part = reinterpret_cast<float*>(base + p.part);
+  a.D = D; a.ldd = ldd; a.ldw = ldw; a.scale = scale; a.accumulate = accumulate; a.nb_log = p.nb_log; a.bins = int(p.bins);
+  a.ncb = int(p.ncb);
+  a.dw_aligned = rows_aligned(dweight, ldw, 4, 16);
+  a.dweight = dweight;
   return with_type(dout_type, [&](auto x) {
     using X = decltype(x);
-    k_embed_sum<X><<<unsigned(T < (1 << 16) ? T : (1 << 16)), 256, 0, st>>>(static_cast<const X*>(dout), ldd, perm, row, T, D, scale, accumulate,
-                                                                             dweight, ldw);
-    return cuda_ok();
+    auto* kernel = rows_aligned(dout, ldd, sizeof(X), 16) ? k_embed_sum<X, true> : k_embed_sum<X, false>;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(unsigned(grid));
+    cfg.blockDim = dim3(SUM_TPB);
+    cfg.stream = st;
+    cudaLaunchAttribute early = {};
+    early.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    early.val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = &early;
+    cfg.numAttrs = 1;
+    const bool ok = cudaLaunchKernelEx(&cfg, kernel, static_cast<const X*>(dout), a) == cudaSuccess;
+    return cuda_ok() == MV_OK && ok ? int(MV_OK) : int(MV_ERR_CUDA);
   });
 }
 

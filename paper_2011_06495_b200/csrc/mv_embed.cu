@@ -292,80 +292,113 @@ template <typename X> __device__ __forceinline__ float* part_at(const SumArgs& a
   return a.part + ((piece * 2 + slot) * a.ncb + cb) * BLOCK<X> + lane;
 }
 
-// The end of a run (or of the piece inside one).  Not inlined: it stands behind each of the unrolled rows.
-template <typename X, bool VEC>
-__device__ __noinline__ void end_run(const SumArgs* __restrict__ pa, int v, int piece, int cb, bool whole, int slot, Lanes<X> acc, float* stage) {
-  const SumArgs& a = *pa;
-  const int lane = threadIdx.x & 31;
-  if (!whole) {
-    float* q = part_at<X>(a, piece, slot, cb, lane);
+// 16 bytes of a row on their way to this lane's slot in shared memory.  Rows of 16-bit elements that start at odd
+// multiples of two bytes have no asynchronous copy; they go through registers.
+__device__ __forceinline__ uint32_t smem_addr(const void* p) { return uint32_t(__cvta_generic_to_shared(p)); }
+
+template <typename X, bool VEC> __device__ __forceinline__ void fetch(const X* row, int64_t D, int64_t cb, int lane, uint4* slot) {
+  const int64_t c0 = column<X, VEC>(cb, lane, 0);
+  if (VEC && c0 + LANE<X> <= D) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem_addr(slot)), "l"(row + c0) : "memory");
+  } else if (!VEC && sizeof(X) == 4) {
 #pragma unroll
-    for (int j = 0; j < LANE<X>; ++j) __stcg(q + j * 32, acc.v[j]);
-    const int32_t* st = a.start + int64_t(v & ((1 << a.nb_log) - 1)) * (a.bins + 1) + (v >> a.nb_log);
-    const int first = st[0], p0 = first / PIECE, p1 = (st[1] - 1) / PIECE;
-    __threadfence();
-    __syncwarp();
-    uint32_t arrived = 0;
-    if (lane == 0) arrived = atomicAdd(a.ticket + int64_t(p0) * a.ncb + cb, 1u);
-    if (__shfl_sync(0xffffffffu, arrived, 0) != uint32_t(p1 - p0)) return;
-    __threadfence();
-    const float* q0 = part_at<X>(a, p0, first % PIECE ? 1 : 0, cb, lane);
-#pragma unroll
-    for (int j = 0; j < LANE<X>; ++j) acc.v[j] = __ldcg(q0 + j * 32);
-    const int64_t step = 2 * int64_t(a.ncb) * BLOCK<X>;
-    const float* q1 = part_at<X>(a, p0 + 1, 0, cb, lane);
-#pragma unroll 4
-    for (int k = p0 + 1; k <= p1; ++k, q1 += step)
-#pragma unroll
-      for (int j = 0; j < LANE<X>; ++j) acc.v[j] += __ldcg(q1 + j * 32);
+    for (int j = 0; j < LANE<X>; ++j) {
+      const int64_t c = c0 + j * 32;
+      if (c < D) asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(smem_addr(reinterpret_cast<X*>(slot) + j)), "l"(row + c) : "memory");
+    }
+  } else {
+    load_raw<X, VEC>(row, D, cb, lane, *slot);
   }
-  put_row<X, VEC>(a, v, cb, lane, acc, stage);
 }
+
+constexpr int DEPTH = 16;            // rows on their way per warp: 8 KB, 24 warps a multiprocessor
 
 template <typename X, bool VEC>
 __global__ void __launch_bounds__(SUM_TPB) k_embed_sum(const X* __restrict__ dout, const __grid_constant__ SumArgs a) {
-  __shared__ float s_stage[SUM_TPB / 32][BLOCK<X>];
-  asm volatile("griddepcontrol.wait;" ::: "memory");
-  constexpr int E = LANE<X>, U = 8;
+  extern __shared__ uint4 ring[];                   // [DEPTH][thread]: a lane only ever reads what it fetched itself
+  __shared__ float s_stage[VEC ? SUM_TPB / 32 : 1][VEC ? BLOCK<X> : 1];
+  constexpr int E = LANE<X>;
   const int lane = threadIdx.x & 31;
-  float* stage = s_stage[threadIdx.x >> 5];
+  float* stage = VEC ? s_stage[threadIdx.x >> 5] : nullptr;
   const int64_t item = int64_t(blockIdx.x) * (SUM_TPB / 32) + (threadIdx.x >> 5);
   const int64_t piece = item / a.ncb, cb = item % a.ncb;
-  const int64_t s0 = piece * PIECE, valid = *a.valid;
+  const int64_t s0 = piece * PIECE;
+  for (int i = 0; i < DEPTH; ++i) ring[i * SUM_TPB + threadIdx.x] = make_uint4(0, 0, 0, 0);     // columns beyond the row stay zero
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  const int64_t valid = *a.valid;
   if (s0 >= valid) return;
   const int n = int(min(int64_t(PIECE), valid - s0));
   const int32_t p = lane < n ? a.perm[s0 + lane] : 0;
   const int32_t r = lane < n ? a.row[s0 + lane] : -1;
   const int32_t before = s0 > 0 ? a.row[s0 - 1] : -1;
   const int32_t after = s0 + n < valid ? a.row[s0 + n] : -1;
-  const int32_t r0 = __shfl_sync(0xffffffffu, r, 0);
+  auto issue = [&](int i) {
+    const int64_t t = __shfl_sync(0xffffffffu, p, i & 31);
+    if (i < n) fetch<X, VEC>(dout + t * a.ldd, a.D, cb, lane, ring + (i % DEPTH) * SUM_TPB + threadIdx.x);
+    asm volatile("cp.async.commit_group;" ::: "memory");
+  };
+#pragma unroll
+  for (int i = 0; i < DEPTH; ++i) issue(i);
+  const int32_t r0 = __shfl_sync(0xffffffffu, r, 0), rn = __shfl_sync(0xffffffffu, r, n - 1);
   const int32_t next = __shfl_down_sync(0xffffffffu, r, 1);
   const unsigned ends = __ballot_sync(0xffffffffu, lane < n && (lane == n - 1 || next != r));   // last token of a run (or of the piece)
+  // the places of the runs that cross into this piece and out of it
+  const bool cross0 = before == r0 || (r0 == rn && after == rn), cross1 = r0 != rn && after == rn;
+  int first[2] = {0, 0}, last[2] = {0, 0};
+  if (cross0) {
+    const int32_t* st = a.start + int64_t(r0 & ((1 << a.nb_log) - 1)) * (a.bins + 1) + (r0 >> a.nb_log);
+    first[0] = st[0]; last[0] = st[1] - 1;
+  }
+  if (cross1) {
+    const int32_t* st = a.start + int64_t(rn & ((1 << a.nb_log) - 1)) * (a.bins + 1) + (rn >> a.nb_log);
+    first[1] = st[0]; last[1] = st[1] - 1;
+  }
   Lanes<X> acc;
 #pragma unroll
   for (int j = 0; j < E; ++j) acc.v[j] = 0.0f;
-  for (int i0 = 0; i0 < n; i0 += U) {
-    uint4 u[U];
+#pragma unroll 1
+  for (int i = 0; i < n; ++i) {
+    asm volatile("cp.async.wait_group %0;" ::"n"(DEPTH - 1) : "memory");
+    Raw<X> x;
+    memcpy(&x, ring + (i % DEPTH) * SUM_TPB + threadIdx.x, 16);
+    issue(i + DEPTH);
 #pragma unroll
-    for (int i = 0; i < U; ++i) {
-      const int64_t t = __shfl_sync(0xffffffffu, p, i0 + i);
-      if (i0 + i < n) load_raw<X, VEC>(dout + t * a.ldd, a.D, cb, lane, u[i]);
+    for (int j = 0; j < E; ++j) acc.v[j] += to_f(x.e[j]);
+    if (!(ends >> i & 1u)) continue;
+    const int32_t v = __shfl_sync(0xffffffffu, r, i);
+    const int slot = v == r0 ? 0 : 1;
+    if ((slot == 0 && cross0) || (i == n - 1 && cross1)) {
+      float* q = part_at<X>(a, piece, slot, cb, lane);
+#pragma unroll
+      for (int j = 0; j < E; ++j) __stcg(q + j * 32, acc.v[j]);
+    } else {
+      put_row<X, VEC>(a, v, cb, lane, acc, stage);
     }
 #pragma unroll
-    for (int i = 0; i < U; ++i) {
-      if (i0 + i >= n) break;
-      Raw<X> x;
-      memcpy(&x, &u[i], 16);
+    for (int j = 0; j < E; ++j) acc.v[j] = 0.0f;
+  }
+  if (!cross0 && !cross1) return;
+  // this piece's partial sums are written: is it the last one of either run?
+  __threadfence();
+  __syncwarp();
+#pragma unroll 1
+  for (int c = 0; c < 2; ++c) {
+    if (!(c ? cross1 : cross0)) continue;
+    const int f = c ? first[1] : first[0], p0 = f / PIECE, p1 = (c ? last[1] : last[0]) / PIECE;
+    uint32_t arrived = 0;
+    if (lane == 0) arrived = atomicAdd(a.ticket + int64_t(p0) * a.ncb + cb, 1u);
+    if (__shfl_sync(0xffffffffu, arrived, 0) != uint32_t(p1 - p0)) continue;
+    __threadfence();
+    const float* q0 = part_at<X>(a, p0, f % PIECE ? 1 : 0, cb, lane);
 #pragma unroll
-      for (int j = 0; j < E; ++j) acc.v[j] += to_f(x.e[j]);
-      if (!(ends >> (i0 + i) & 1u)) continue;
-      const int32_t v = __shfl_sync(0xffffffffu, r, i0 + i);
-      const bool from_before = v == r0 && before == v;
-      const bool goes_on = i0 + i == n - 1 && after == v;
-      end_run<X, VEC>(&a, v, int(piece), int(cb), !from_before && !goes_on, v == r0 ? 0 : 1, acc, stage);
+    for (int j = 0; j < E; ++j) acc.v[j] = __ldcg(q0 + j * 32);
+    const int64_t step = 2 * int64_t(a.ncb) * BLOCK<X>;
+    const float* q1 = part_at<X>(a, p0 + 1, 0, cb, lane);
+#pragma unroll 4
+    for (int k = p0 + 1; k <= p1; ++k, q1 += step)
 #pragma unroll
-      for (int j = 0; j < E; ++j) acc.v[j] = 0.0f;
-    }
+      for (int j = 0; j < E; ++j) acc.v[j] += __ldcg(q1 + j * 32);
+    put_row<X, VEC>(a, c ? rn : r0, cb, lane, acc, stage);
   }
 }
 
@@ -454,9 +487,15 @@ int mv_embed_grad(void* stream, const void* dout, int dout_type, int64_t ldd, co
   return with_type(dout_type, [&](auto x) {
     using X = decltype(x);
     auto* kernel = rows_aligned(dout, ldd, sizeof(X), 16) ? k_embed_sum<X, true> : k_embed_sum<X, false>;
+    const int ring = DEPTH * SUM_TPB * 16;
+    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, ring) != cudaSuccess) {
+      cudaGetLastError();
+      return int(MV_ERR_CUDA);
+    }
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(unsigned(grid));
     cfg.blockDim = dim3(SUM_TPB);
+    cfg.dynamicSmemBytes = ring;
     cfg.stream = st;
     cudaLaunchAttribute early = {};
     early.id = cudaLaunchAttributeProgrammaticStreamSerialization;

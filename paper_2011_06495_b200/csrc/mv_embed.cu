@@ -83,20 +83,21 @@ __global__ void __launch_bounds__(EMBED_TPB) k_embed(const W* __restrict__ weigh
 
 // ------------------------------------------------------------------------------------------ gradient: grouping the tokens
 // The tokens fall into nb buckets (a power of two) by id mod nb, so that the frequent tokens, which have neighbouring
-// ids, spread over all buckets.  The CTA of a bucket reads all ids twice.  First it counts: for each of its warps, which
-// own consecutive stretches of the tokens, how many tokens of each of the bucket's ids the stretch holds, and how many
-// tokens belong to lower buckets.  A scan over (id, warp) turns the counts into places, and the second reading puts every
-// token at its place: grouped by id, in token order, without a sort and whatever the skew.  Then the CTA clears
-// the rows of those of its ids that no token has.
+// ids, spread over all buckets.  The CTA of a bucket reads all ids.  Each of its warps owns a consecutive stretch of them
+// and counts, per id of the bucket, the stretch's tokens, and the tokens that belong to lower buckets.  A scan over (id,
+// warp) turns the counts into places, and each warp puts its tokens there: grouped by id, in token order, without a
+// sort and whatever the skew.  A warp remembers the tokens it found (one in nb, on average); if they are too many for its list it
+// reads its stretch a second time.
 constexpr int SORT_TPB = 1024;
 constexpr int SORT_WARPS = SORT_TPB / 32;
 constexpr int SORT_BINS = 1024;      // ids per bucket, at most: one thread each in the scan, 128 KB of counters
-constexpr int PIECE = 32;            // sorted tokens per warp of the summation
+constexpr int SORT_LIST = 128;       // tokens a warp remembers: 32 KB a CTA
 
 struct EmbedPlan {
   int nb_log;
   int64_t bins;                      // counters per bucket
   int64_t buckets;                   // buckets that hold an id
+  int piece;                         // sorted tokens per warp of the summation
   int64_t pieces, ncb;
   size_t perm, row, start, valid, ticket, part, total;
 };
@@ -107,13 +108,15 @@ inline EmbedPlan embed_plan(int64_t T, int64_t V, int64_t D, int block) {
   while (((V - 1) >> p.nb_log) + 1 > SORT_BINS) ++p.nb_log;
   p.bins = ((V - 1) >> p.nb_log) + 1;
   p.buckets = V < (int64_t(1) << p.nb_log) ? V : int64_t(1) << p.nb_log;
-  p.pieces = (T + PIECE - 1) / PIECE;
   p.ncb = (D + block - 1) / block;
+  // short pieces while long ones would not give every multiprocessor its 24 warps: then the length of one warp's chain counts
+  p.piece = (T + 31) / 32 * p.ncb >= 148 * 24 ? 32 : 8;
+  p.pieces = (T + p.piece - 1) / p.piece;
   size_t o = 0;
   p.valid = o;  o = align_up(o + 4, 16);
   p.perm = o;   o = align_up(o + size_t(T) * 4, 16);
   p.row = o;    o = align_up(o + size_t(T) * 4, 16);
-  p.start = o;  o = align_up(o + size_t(p.buckets) * size_t(p.bins + 1) * 4, 16);
+  p.start = o;  o = align_up(o + (size_t(p.bins + 1) << p.nb_log) * 4, 16);
   p.ticket = o; o = align_up(o + size_t(p.pieces) * size_t(p.ncb) * 4, 16);
   p.part = o;   o = align_up(o + size_t(p.pieces) * 2 * size_t(D) * 4, 16);
   p.total = o;
@@ -124,57 +127,61 @@ struct SortArgs {
   const void* ids;
   int64_t T, V, pad_id;
   int nb_log, bins;
-  int32_t *perm, *row, *start, *valid;
+  int32_t *perm, *row;
+  int32_t* start;                    // [id]: place of the id's first token; [id + nb]: the place behind its last one
+  int32_t* valid;                    // tokens with a gradient
   uint32_t* ticket;
   int64_t n_ticket;
-  float* fill;                       // the table whose untouched rows are cleared, or null
-  int64_t D, ldw;
 };
 
-// A row of zeros, written by one warp: single words up to a 16-byte boundary, then 16 bytes a lane.
-__device__ __forceinline__ void clear_row(float* p, int64_t D, int lane) {
-  const int64_t head = min(D, int64_t((16 - (reinterpret_cast<uintptr_t>(p) & 15)) / 4 & 3));
-  if (lane < head) p[lane] = 0.0f;
-  float4* q = reinterpret_cast<float4*>(p + head);
-  const int64_t nv = (D - head) >> 2;
-  for (int64_t i = lane; i < nv; i += 32) q[i] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-  const int64_t done = head + 4 * nv;
-  if (lane < D - done) p[done + lane] = 0.0f;
-}
-
 template <typename ID>
-__global__ void __launch_bounds__(SORT_TPB) k_embed_sort(SortArgs a) {
-  extern __shared__ uint32_t cnt[];                 // [warp][bin] counts, then next places; behind them [bin] places of the ids
+__global__ void __launch_bounds__(SORT_TPB) k_embed_sort(const __grid_constant__ SortArgs a) {
+  extern __shared__ uint32_t cnt[];                 // [warp][bin] counts, then next places
+  __shared__ int2 s_list[SORT_WARPS][SORT_LIST];    // (token, id)
   __shared__ uint32_t s_warp[SORT_WARPS], s_below[SORT_WARPS];
   constexpr int U = 8;                              // independent id loads per lane
   const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
   const int b = blockIdx.x;
   const int bins = a.bins;
   const int64_t nb_mask = (int64_t(1) << a.nb_log) - 1;
-  uint32_t* first = cnt + SORT_WARPS * bins;
+  const unsigned lower = (1u << lane) - 1u;
   uint32_t* own = cnt + w * bins;
   const ID* ids = static_cast<const ID*>(a.ids);
   for (int64_t i = int64_t(b) * SORT_TPB + threadIdx.x; i < a.n_ticket; i += int64_t(gridDim.x) * SORT_TPB) a.ticket[i] = 0;
   for (int i = threadIdx.x; i < SORT_WARPS * bins; i += SORT_TPB) cnt[i] = 0;
   __syncthreads();
+  asm volatile("griddepcontrol.launch_dependents;");      // the sums may be set up; they wait for the end of this kernel
   const int64_t seg = (a.T + SORT_TPB - 1) / SORT_TPB * 32;
   const int64_t lo = min(a.T, w * seg), hi = min(a.T, lo + seg);
+  // f(token, id, whether the id is of this bucket), for 32 tokens of the stretch at a time and in their order
+  auto stretch = [&](auto&& f) {
+    for (int64_t t0 = lo; t0 < hi; t0 += 32 * U) {
+      int64_t v[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int64_t t = t0 + u * 32 + lane;
+        v[u] = t < hi ? int64_t(ids[t]) : -1;
+      }
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const bool is = v[u] >= 0 && v[u] < a.V && v[u] != a.pad_id;
+        f(int(t0 + u * 32 + lane), int(v[u]), is, is && int(v[u] & nb_mask) == b);
+      }
+    }
+  };
   uint32_t below = 0;
-  for (int64_t t0 = lo; t0 < hi; t0 += 32 * U) {
-    int64_t v[U];
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const int64_t t = t0 + u * 32 + lane;
-      v[u] = t < hi ? int64_t(ids[t]) : -1;
+  int found = 0;
+  stretch([&](int t, int v, bool is, bool mine) {
+    if (is && int(v & nb_mask) < b) ++below;
+    const unsigned any = __ballot_sync(0xffffffffu, mine);
+    if (any == 0) return;
+    if (mine) {
+      atomicAdd(&own[v >> a.nb_log], 1u);
+      const int i = found + __popc(any & lower);
+      if (i < SORT_LIST) s_list[w][i] = make_int2(t, v);
     }
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-      if (v[u] < 0 || v[u] >= a.V || v[u] == a.pad_id) continue;
-      const int m = int(v[u] & nb_mask);
-      if (m < b) ++below;
-      else if (m == b) atomicAdd(&own[v[u] >> a.nb_log], 1u);
-    }
-  }
+    found += __popc(any);
+  });
   below = __reduce_add_sync(0xffffffffu, below);
   if (lane == 0) s_below[w] = below;
   __syncthreads();
@@ -192,67 +199,82 @@ __global__ void __launch_bounds__(SORT_TPB) k_embed_sort(SortArgs a) {
   uint32_t place = incl - total;
   for (int i = 0; i < SORT_WARPS; ++i) place += s_below[i] + (i < w ? s_warp[i] : 0u);
   if (int(threadIdx.x) < bins) {
-    first[threadIdx.x] = place;
-    a.start[int64_t(b) * (bins + 1) + threadIdx.x] = int32_t(place);
+    a.start[(int64_t(threadIdx.x) << a.nb_log) + b] = int32_t(place);
     uint32_t run = place;
     for (int i = 0; i < SORT_WARPS; ++i) { const uint32_t c = cnt[i * bins + threadIdx.x]; cnt[i * bins + threadIdx.x] = run; run += c; }
     if (int(threadIdx.x) == bins - 1) {
-      first[bins] = run;
-      a.start[int64_t(b) * (bins + 1) + bins] = int32_t(run);
+      a.start[(int64_t(bins) << a.nb_log) + b] = int32_t(run);
       if (b == int(gridDim.x) - 1) *a.valid = int32_t(run);
     }
   }
   __syncthreads();
-  asm volatile("griddepcontrol.launch_dependents;");      // the sums may be set up; they wait for the end of this kernel
-  for (int64_t t0 = lo; t0 < hi; t0 += 32 * U) {
-    int64_t v[U];
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const int64_t t = t0 + u * 32 + lane;
-      v[u] = t < hi ? int64_t(ids[t]) : -1;
+  auto put = [&](int t, int v, bool mine) {
+    const unsigned any = __ballot_sync(0xffffffffu, mine);
+    if (any == 0) return;
+    if (mine) {
+      const unsigned same = __match_any_sync(any, v);
+      const int rank = __popc(same & lower), bin = v >> a.nb_log;
+      const uint32_t slot = own[bin] + rank;
+      __syncwarp(any);
+      if (rank == 0) own[bin] += __popc(same);
+      a.perm[slot] = t;
+      a.row[slot] = v;
     }
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const bool mine = v[u] >= 0 && v[u] < a.V && v[u] != a.pad_id && int(v[u] & nb_mask) == b;
-      const unsigned any = __ballot_sync(0xffffffffu, mine);
-      if (any == 0) continue;
-      if (mine) {
-        const unsigned same = __match_any_sync(any, int(v[u]));
-        const int rank = __popc(same & ((1u << lane) - 1u));
-        const int bin = int(v[u] >> a.nb_log);
-        const uint32_t slot = own[bin] + rank;
-        __syncwarp(any);
-        if (rank == 0) own[bin] += __popc(same);
-        a.perm[slot] = int32_t(t0 + u * 32 + lane);
-        a.row[slot] = int32_t(v[u]);
-      }
-      __syncwarp();
+    __syncwarp();
+  };
+  if (found <= SORT_LIST) {
+    for (int i = lane; i < (found + 31) / 32 * 32; i += 32) {
+      const int2 e = i < found ? s_list[w][i] : make_int2(0, 0);
+      put(e.x, e.y, i < found);
     }
-  }
-  if (a.fill == nullptr) return;
-  for (int i = w; i < bins; i += SORT_WARPS) {
-    const int64_t v = (int64_t(i) << a.nb_log) + b;
-    if (v < a.V && first[i] == first[i + 1]) clear_row(a.fill + v * a.ldw, a.D, lane);
+  } else {
+    stretch([&](int t, int v, bool, bool mine) { put(t, v, mine); });
   }
 }
 
 // ------------------------------------------------------------------------------------------ gradient: the sums
-// A warp takes one piece of PIECE sorted tokens and one block of columns and adds the rows up in order.  A run of
+// A warp takes one piece of consecutive sorted tokens and one block of columns and adds the rows up in order.  A run of
 // equal ids that lies inside the piece is finished there.  One that crosses into other pieces leaves a partial sum per
 // piece; the warp that leaves the last one adds the partial sums up in the order of the pieces.  So a frequent token's
-// rows are read by many warps, and the result does not depend on which of them comes last.
+// rows are read by many warps, and the result does not depend on which of them comes last.  CTAs that clear the rows
+// without a token stand between those that sum, so that reads and writes share the memory's time.
 struct SumArgs {
   const int32_t *perm, *row, *start, *valid;
   uint32_t* ticket;
   float* part;                       // [piece][0: the run that the piece begins with, 1: the one it ends with][D]
-  int64_t D, ldd, ldw;
+  int64_t V, D, ldd, ldw;
   float scale;
-  int accumulate, nb_log, bins, ncb;
+  int accumulate, nb, ncb;
   int dw_aligned;                    // the table's rows start at multiples of 16 bytes
+  int64_t n_fill;                    // CTAs that clear
+  int fill_rows;                     // rows each of them looks at, a multiple of 32
   float* dweight;
 };
 
 constexpr int SUM_TPB = 256;
+
+// A row of zeros, written by one warp: single words up to a 16-byte boundary, then 16 bytes a lane.
+__device__ __forceinline__ void clear_row(float* p, int64_t D, int lane) {
+  const int64_t head = min(D, int64_t((16 - (reinterpret_cast<uintptr_t>(p) & 15)) / 4 & 3));
+  if (lane < head) p[lane] = 0.0f;
+  float4* q = reinterpret_cast<float4*>(p + head);
+  const int64_t nv = (D - head) >> 2;
+  for (int64_t i = lane; i < nv; i += 32) q[i] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+  const int64_t done = head + 4 * nv;
+  if (lane < D - done) p[done + lane] = 0.0f;
+}
+
+__device__ void clear_unused(const SumArgs& a, int64_t cta) {
+  const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
+  const int64_t v0 = cta * a.fill_rows, v1 = min(a.V, v0 + a.fill_rows);
+  for (int64_t v = v0; v < v1; v += 32) {
+    const bool unused = v + lane < v1 && a.start[v + lane] == a.start[v + lane + a.nb];
+    // every warp an eighth of the unused rows
+    unsigned m = __ballot_sync(0xffffffffu, unused);
+    for (int i = 0; m; ++i, m &= m - 1)
+      if ((i & (SUM_TPB / 32 - 1)) == w) clear_row(a.dweight + (v + __ffs(int(m)) - 1) * a.ldw, a.D, lane);
+  }
+}
 
 template <typename X> struct Lanes { float v[LANE<X>]; };
 
@@ -292,8 +314,8 @@ template <typename X> __device__ __forceinline__ float* part_at(const SumArgs& a
   return a.part + ((piece * 2 + slot) * a.ncb + cb) * BLOCK<X> + lane;
 }
 
-// 16 bytes of a row on their way to this lane's slot in shared memory.  Rows of 16-bit elements that start at odd
-// multiples of two bytes have no asynchronous copy; they go through registers.
+// 16 bytes of a row on their way to this lane's slot in shared memory.  Rows of 16-bit elements that do not start at a
+// multiple of 16 bytes have no asynchronous copy; they go through registers.
 __device__ __forceinline__ uint32_t smem_addr(const void* p) { return uint32_t(__cvta_generic_to_shared(p)); }
 
 template <typename X, bool VEC> __device__ __forceinline__ void fetch(const X* row, int64_t D, int64_t cb, int lane, uint4* slot) {
@@ -311,20 +333,27 @@ template <typename X, bool VEC> __device__ __forceinline__ void fetch(const X* r
   }
 }
 
-constexpr int DEPTH = 16;            // rows on their way per warp: 8 KB, 24 warps a multiprocessor
-
-template <typename X, bool VEC>
+// PIECE: tokens per warp.  Up to 16 rows of 512 bytes are on their way per warp: 24 warps a multiprocessor.
+template <typename X, bool VEC, int PIECE>
 __global__ void __launch_bounds__(SUM_TPB) k_embed_sum(const X* __restrict__ dout, const __grid_constant__ SumArgs a) {
+  constexpr int E = LANE<X>, DEPTH = PIECE < 16 ? PIECE : 16;
   extern __shared__ uint4 ring[];                   // [DEPTH][thread]: a lane only ever reads what it fetched itself
   __shared__ float s_stage[VEC ? SUM_TPB / 32 : 1][VEC ? BLOCK<X> : 1];
-  constexpr int E = LANE<X>;
   const int lane = threadIdx.x & 31;
   float* stage = VEC ? s_stage[threadIdx.x >> 5] : nullptr;
-  const int64_t item = int64_t(blockIdx.x) * (SUM_TPB / 32) + (threadIdx.x >> 5);
+  // the CTAs that clear are spread evenly between the others
+  const int64_t fill = int64_t(blockIdx.x) * a.n_fill / gridDim.x;
+  const bool clears = int64_t(blockIdx.x + 1) * a.n_fill / gridDim.x != fill;
+  const int64_t item = (blockIdx.x - fill) * (SUM_TPB / 32) + (threadIdx.x >> 5);
   const int64_t piece = item / a.ncb, cb = item % a.ncb;
   const int64_t s0 = piece * PIECE;
-  for (int i = 0; i < DEPTH; ++i) ring[i * SUM_TPB + threadIdx.x] = make_uint4(0, 0, 0, 0);     // columns beyond the row stay zero
+  if (!clears)
+    for (int i = 0; i < DEPTH; ++i) ring[i * SUM_TPB + threadIdx.x] = make_uint4(0, 0, 0, 0);     // columns beyond the row stay zero
   asm volatile("griddepcontrol.wait;" ::: "memory");
+  if (clears) {
+    clear_unused(a, fill);
+    return;
+  }
   const int64_t valid = *a.valid;
   if (s0 >= valid) return;
   const int n = int(min(int64_t(PIECE), valid - s0));
@@ -345,14 +374,8 @@ __global__ void __launch_bounds__(SUM_TPB) k_embed_sum(const X* __restrict__ dou
   // the places of the runs that cross into this piece and out of it
   const bool cross0 = before == r0 || (r0 == rn && after == rn), cross1 = r0 != rn && after == rn;
   int first[2] = {0, 0}, last[2] = {0, 0};
-  if (cross0) {
-    const int32_t* st = a.start + int64_t(r0 & ((1 << a.nb_log) - 1)) * (a.bins + 1) + (r0 >> a.nb_log);
-    first[0] = st[0]; last[0] = st[1] - 1;
-  }
-  if (cross1) {
-    const int32_t* st = a.start + int64_t(rn & ((1 << a.nb_log) - 1)) * (a.bins + 1) + (rn >> a.nb_log);
-    first[1] = st[0]; last[1] = st[1] - 1;
-  }
+  if (cross0) { first[0] = a.start[r0]; last[0] = a.start[r0 + a.nb] - 1; }
+  if (cross1) { first[1] = a.start[rn]; last[1] = a.start[rn + a.nb] - 1; }
   Lanes<X> acc;
 #pragma unroll
   for (int j = 0; j < E; ++j) acc.v[j] = 0.0f;
@@ -361,7 +384,8 @@ __global__ void __launch_bounds__(SUM_TPB) k_embed_sum(const X* __restrict__ dou
     asm volatile("cp.async.wait_group %0;" ::"n"(DEPTH - 1) : "memory");
     Raw<X> x;
     memcpy(&x, ring + (i % DEPTH) * SUM_TPB + threadIdx.x, 16);
-    issue(i + DEPTH);
+    if (PIECE > DEPTH) issue(i + DEPTH);
+    else asm volatile("cp.async.commit_group;" ::: "memory");
 #pragma unroll
     for (int j = 0; j < E; ++j) acc.v[j] += to_f(x.e[j]);
     if (!(ends >> i & 1u)) continue;
@@ -454,8 +478,12 @@ int mv_embed_grad(void* stream, const void* dout, int dout_type, int64_t ldd, co
   if (!workspace || workspace_bytes < mv_embed_grad_workspace_bytes(T, V, D)) return MV_ERR_WORKSPACE;
   const int block = dout_type == MV_F32 ? BLOCK<float> : BLOCK<__half>;
   const EmbedPlan p = embed_plan(T, V, (D + block - 1) / block * block, block);
-  const int64_t items = p.pieces * p.ncb, grid = (items + SUM_TPB / 32 - 1) / (SUM_TPB / 32);
-  if (grid >= lim) return MV_ERR_INVALID_ARG;
+  const int64_t items = p.pieces * p.ncb, n_sum = (items + SUM_TPB / 32 - 1) / (SUM_TPB / 32);
+  SumArgs a;
+  // a CTA that clears looks at 64 KB of rows, or 32 rows
+  a.fill_rows = int(32 * (D >= 512 ? 1 : 512 / D));
+  a.n_fill = accumulate ? 0 : (V + a.fill_rows - 1) / a.fill_rows;
+  if (n_sum + a.n_fill >= lim) return MV_ERR_INVALID_ARG;
   if (accumulate && T == 0) return MV_OK;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   char* base = static_cast<char*>(workspace);
@@ -467,33 +495,31 @@ int mv_embed_grad(void* stream, const void* dout, int dout_type, int64_t ldd, co
   s.valid = reinterpret_cast<int32_t*>(base + p.valid);
   s.ticket = reinterpret_cast<uint32_t*>(base + p.ticket);
   s.n_ticket = items;
-  s.fill = accumulate ? nullptr : dweight;
-  s.D = D; s.ldw = ldw;
-  const size_t smem = (size_t(SORT_WARPS) * p.bins + p.bins + 1) * 4;
+  const size_t smem = size_t(SORT_WARPS) * p.bins * 4;
   auto* sort = id_type == MV_I32 ? k_embed_sort<int32_t> : k_embed_sort<int64_t>;
-  if (smem > 48 * 1024 && cudaFuncSetAttribute(sort, cudaFuncAttributeMaxDynamicSharedMemorySize, int(smem)) != cudaSuccess) {
+  if (cudaFuncSetAttribute(sort, cudaFuncAttributeMaxDynamicSharedMemorySize, int(smem)) != cudaSuccess) {
     cudaGetLastError();
     return MV_ERR_CUDA;
   }
   sort<<<unsigned(p.buckets), SORT_TPB, smem, st>>>(s);
-  if (T == 0) return cuda_ok();
-  SumArgs a;
   a.perm = s.perm; a.row = s.row; a.start = s.start; a.valid = s.valid; a.ticket = s.ticket;
   a.part = reinterpret_cast<float*>(base + p.part);
-  a.D = D; a.ldd = ldd; a.ldw = ldw; a.scale = scale; a.accumulate = accumulate; a.nb_log = p.nb_log; a.bins = int(p.bins);
+  a.V = V; a.D = D; a.ldd = ldd; a.ldw = ldw; a.scale = scale; a.accumulate = accumulate; a.nb = 1 << p.nb_log;
   a.ncb = int(p.ncb);
   a.dw_aligned = rows_aligned(dweight, ldw, 4, 16);
   a.dweight = dweight;
   return with_type(dout_type, [&](auto x) {
     using X = decltype(x);
-    auto* kernel = rows_aligned(dout, ldd, sizeof(X), 16) ? k_embed_sum<X, true> : k_embed_sum<X, false>;
-    const int ring = DEPTH * SUM_TPB * 16;
+    const bool vec = rows_aligned(dout, ldd, sizeof(X), 16);
+    auto* kernel = p.piece == 32 ? (vec ? k_embed_sum<X, true, 32> : k_embed_sum<X, false, 32>)
+                                 : (vec ? k_embed_sum<X, true, 8> : k_embed_sum<X, false, 8>);
+    const int ring = (p.piece == 32 ? 16 : 8) * SUM_TPB * 16;
     if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, ring) != cudaSuccess) {
       cudaGetLastError();
       return int(MV_ERR_CUDA);
     }
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(unsigned(grid));
+    cfg.gridDim = dim3(unsigned(n_sum + a.n_fill));
     cfg.blockDim = dim3(SUM_TPB);
     cfg.dynamicSmemBytes = ring;
     cfg.stream = st;

@@ -83,20 +83,20 @@ __global__ void __launch_bounds__(EMBED_TPB) k_embed(const W* __restrict__ weigh
 
 // ------------------------------------------------------------------------------------------ gradient: grouping the tokens
 // The tokens fall into nb buckets (a power of two) by id mod nb, so that the frequent tokens, which have neighbouring
-// ids, spread over all buckets.  The CTA of a bucket reads all ids.  Each of its warps owns a consecutive stretch of them
-// and counts, per id of the bucket, the stretch's tokens, and the tokens that belong to lower buckets.  A scan over (id,
-// warp) turns the counts into places, and each warp puts its tokens there: grouped by id, in token order, without a
-// sort and whatever the skew.  A warp remembers the tokens it found (one in nb, on average); if they are too many for its list it
-// reads its stretch a second time.
+// ids, spread over all buckets.  A bucket's CTA reads all ids: each of its warps owns a consecutive stretch, counts the
+// tokens of lower buckets and lists its own ones.  The lists, end to end, are the bucket's tokens in order; they are
+// counted per (id, warp), and a scan turns the counts into places: grouped by id, in token order, without a sort.  What it
+// costs is latency (half a dozen short phases) and, for many tokens, the 128-fold reading of the ids out of L2.
+// Lists that would not hold all (a text of very few ids, millions of tokens) are not used: then the ids are read twice more.
 constexpr int SORT_TPB = 1024;
 constexpr int SORT_WARPS = SORT_TPB / 32;
 constexpr int SORT_BINS = 1024;      // ids per bucket, at most: one thread each in the scan, 128 KB of counters
-constexpr int SORT_LIST = 128;       // tokens a warp remembers: 32 KB a CTA
+constexpr int SORT_LIST = 128;       // tokens a warp lists (32 KB); one in nb of its stretch on average
+constexpr int SORT_OWN = SORT_WARPS * SORT_LIST;
 
 struct EmbedPlan {
   int nb_log;
   int64_t bins;                      // counters per bucket
-  int64_t buckets;                   // buckets that hold an id
   int piece;                         // sorted tokens per warp of the summation
   int64_t pieces, ncb;
   size_t perm, row, start, valid, ticket, part, total;
@@ -104,10 +104,12 @@ struct EmbedPlan {
 
 inline EmbedPlan embed_plan(int64_t T, int64_t V, int64_t D, int block) {
   EmbedPlan p;
-  p.nb_log = 7;
+#ifndef NBL
+#define NBL 7
+#endif
+  p.nb_log = NBL;
   while (((V - 1) >> p.nb_log) + 1 > SORT_BINS) ++p.nb_log;
   p.bins = ((V - 1) >> p.nb_log) + 1;
-  p.buckets = V < (int64_t(1) << p.nb_log) ? V : int64_t(1) << p.nb_log;
   p.ncb = (D + block - 1) / block;
   // short pieces while long ones would not give every multiprocessor its 24 warps: then the length of one warp's chain counts
   p.piece = (T + 31) / 32 * p.ncb >= 148 * 24 ? 32 : 8;
@@ -134,101 +136,161 @@ struct SortArgs {
   int64_t n_ticket;
 };
 
+struct SortSmem {
+  int2 list[SORT_WARPS][SORT_LIST];  // (token, id)
+  int2 own[SORT_OWN];                // the lists end to end
+  uint32_t warp[SORT_WARPS], below[SORT_WARPS];
+  uint32_t cnt[1];                   // [row][bin] counts, then next places; a row per warp
+};
+
+// 256 consecutive ids, eight per lane: 16 bytes of ids a lane and load, loads end to end; -1 from `hi` on.
+template <typename ID> struct Ids {
+  static constexpr int PER = 16 / int(sizeof(ID)), LOADS = 8 / PER;
+  ID v[LOADS][PER];
+  __device__ static int64_t offset(int lane, int j, int e) { return j * 32 * PER + lane * PER + e; }
+};
+template <typename ID> __device__ __forceinline__ void load_ids(const ID* ids, int64_t t, int64_t hi, bool aligned, int lane, Ids<ID>& x) {
+  if (aligned && t + 256 <= hi) {
+#pragma unroll
+    for (int j = 0; j < Ids<ID>::LOADS; ++j) {
+      const uint4 u = __ldg(reinterpret_cast<const uint4*>(ids + t + Ids<ID>::offset(lane, j, 0)));
+      memcpy(x.v[j], &u, 16);
+    }
+  } else {
+#pragma unroll
+    for (int j = 0; j < Ids<ID>::LOADS; ++j)
+#pragma unroll
+      for (int e = 0; e < Ids<ID>::PER; ++e) {
+        const int64_t i = t + Ids<ID>::offset(lane, j, e);
+        x.v[j][e] = i < hi ? ids[i] : ID(-1);
+      }
+  }
+}
+
 template <typename ID>
 __global__ void __launch_bounds__(SORT_TPB) k_embed_sort(const __grid_constant__ SortArgs a) {
-  extern __shared__ uint32_t cnt[];                 // [warp][bin] counts, then next places
-  __shared__ int2 s_list[SORT_WARPS][SORT_LIST];    // (token, id)
-  __shared__ uint32_t s_warp[SORT_WARPS], s_below[SORT_WARPS];
-  constexpr int U = 8;                              // independent id loads per lane
+  extern __shared__ __align__(16) unsigned char sort_smem[];
+  SortSmem& s = *reinterpret_cast<SortSmem*>(sort_smem);
   const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
-  const int b = blockIdx.x;
+  const uint32_t b = blockIdx.x, mask = (1u << a.nb_log) - 1u;
   const int bins = a.bins;
-  const int64_t nb_mask = (int64_t(1) << a.nb_log) - 1;
   const unsigned lower = (1u << lane) - 1u;
-  uint32_t* own = cnt + w * bins;
+  const uint32_t V = uint32_t(a.V), pad = a.pad_id >= 0 && a.pad_id < a.V ? uint32_t(a.pad_id) : ~0u;
   const ID* ids = static_cast<const ID*>(a.ids);
-  for (int64_t i = int64_t(b) * SORT_TPB + threadIdx.x; i < a.n_ticket; i += int64_t(gridDim.x) * SORT_TPB) a.ticket[i] = 0;
-  for (int i = threadIdx.x; i < SORT_WARPS * bins; i += SORT_TPB) cnt[i] = 0;
-  __syncthreads();
+  const bool aligned = (reinterpret_cast<uintptr_t>(ids) & 15) == 0;
+  uint32_t* row = s.cnt + w * bins;
   asm volatile("griddepcontrol.launch_dependents;");      // the sums may be set up; they wait for the end of this kernel
-  const int64_t seg = (a.T + SORT_TPB - 1) / SORT_TPB * 32;
+  const int64_t seg = (a.T + SORT_WARPS * 256 - 1) / (SORT_WARPS * 256) * 256;
   const int64_t lo = min(a.T, w * seg), hi = min(a.T, lo + seg);
-  // f(token, id, whether the id is of this bucket), for 32 tokens of the stretch at a time and in their order
-  auto stretch = [&](auto&& f) {
-    for (int64_t t0 = lo; t0 < hi; t0 += 32 * U) {
-      int64_t v[U];
-#pragma unroll
-      for (int u = 0; u < U; ++u) {
-        const int64_t t = t0 + u * 32 + lane;
-        v[u] = t < hi ? int64_t(ids[t]) : -1;
-      }
-#pragma unroll
-      for (int u = 0; u < U; ++u) {
-        const bool is = v[u] >= 0 && v[u] < a.V && v[u] != a.pad_id;
-        f(int(t0 + u * 32 + lane), int(v[u]), is, is && int(v[u] & nb_mask) == b);
-      }
-    }
-  };
+  auto known = [&](ID v) { return (sizeof(ID) == 4 || uint64_t(v) >> 32 == 0) && uint32_t(v) < V && uint32_t(v) != pad; };
+  Ids<ID> x;
+  load_ids(ids, lo, hi, aligned, lane, x);
+  for (int i = threadIdx.x; i < SORT_WARPS * bins; i += SORT_TPB) s.cnt[i] = 0;
+  for (int64_t i = int64_t(b) * SORT_TPB + threadIdx.x; i < a.n_ticket; i += int64_t(gridDim.x) * SORT_TPB) a.ticket[i] = 0;
   uint32_t below = 0;
   int found = 0;
-  stretch([&](int t, int v, bool is, bool mine) {
-    if (is && int(v & nb_mask) < b) ++below;
-    const unsigned any = __ballot_sync(0xffffffffu, mine);
-    if (any == 0) return;
-    if (mine) {
-      atomicAdd(&own[v >> a.nb_log], 1u);
-      const int i = found + __popc(any & lower);
-      if (i < SORT_LIST) s_list[w][i] = make_int2(t, v);
+  for (int64_t t0 = lo; t0 < hi; t0 += 256) {
+    const Ids<ID> y = x;
+    if (t0 + 256 < hi) load_ids(ids, t0 + 256, hi, aligned, lane, x);
+    unsigned hit = 0, c = 0;         // hits of this lane: a bit each, and a byte per load
+#pragma unroll
+    for (int j = 0; j < Ids<ID>::LOADS; ++j)
+#pragma unroll
+      for (int e = 0; e < Ids<ID>::PER; ++e) {
+        const uint32_t m = uint32_t(y.v[j][e]) & mask;
+        const bool is = known(y.v[j][e]);
+        below += is && m < b;
+        if (is && m == b) { hit |= 1u << (j * Ids<ID>::PER + e); c += 1u << (8 * j); }
+      }
+    if (!__any_sync(0xffffffffu, hit != 0)) continue;
+    unsigned incl = c;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const unsigned z = __shfl_up_sync(0xffffffffu, incl, o);
+      if (lane >= o) incl += z;
     }
-    found += __popc(any);
-  });
+    const unsigned all = __shfl_sync(0xffffffffu, incl, 31), ahead = incl - c;
+#pragma unroll
+    for (int j = 0; j < Ids<ID>::LOADS; ++j) {
+      int at = found + int(ahead >> (8 * j) & 255u);
+#pragma unroll
+      for (int e = 0; e < Ids<ID>::PER; ++e)
+        if (hit >> (j * Ids<ID>::PER + e) & 1u) {
+          if (at < SORT_LIST) s.list[w][at] = make_int2(int(t0 + Ids<ID>::offset(lane, j, e)), int(y.v[j][e]));
+          ++at;
+        }
+      found += int(all >> (8 * j) & 255u);
+    }
+  }
   below = __reduce_add_sync(0xffffffffu, below);
-  if (lane == 0) s_below[w] = below;
+  if (lane == 0) { s.warp[w] = found; s.below[w] = below; }
   __syncthreads();
-  // places: an exclusive scan over the ids' totals, then over the warps of each id
+  const uint32_t nw = s.warp[lane];
+  const uint32_t before = __reduce_add_sync(0xffffffffu, s.below[lane]);      // tokens in lower buckets
+  const int own = int(__reduce_add_sync(0xffffffffu, nw));
+  const bool listed = __reduce_max_sync(0xffffffffu, nw) <= SORT_LIST;
+  // rows of counts: a warp per 32 tokens while there are fewer than 32 such, else 1/32 of the tokens each
+  const int chunk = (own + SORT_TPB - 1) / SORT_TPB * 32;
+  const int rows = listed ? (own == 0 ? 0 : (own + chunk - 1) / chunk) : SORT_WARPS;
+  const int i0 = min(own, w * chunk), i1 = min(own, i0 + chunk);
+  auto mine = [&](ID v) { return known(v) && (uint32_t(v) & mask) == b; };
+  if (listed) {
+    const int at = int(__reduce_add_sync(0xffffffffu, lane < w ? nw : 0u));
+    for (int i = lane; i < found; i += 32) s.own[at + i] = s.list[w][i];
+    __syncthreads();
+    for (int i = i0 + lane; i < i1; i += 32) atomicAdd(&row[s.own[i].y >> a.nb_log], 1u);
+  } else {
+    for (int64_t t = lo + lane; t < hi; t += 32) {
+      const ID v = ids[t];
+      if (mine(v)) atomicAdd(&row[uint32_t(v) >> a.nb_log], 1u);
+    }
+  }
+  __syncthreads();
+  // places: an exclusive scan over the ids' totals, then over the rows of each id
   uint32_t total = 0;
   if (int(threadIdx.x) < bins)
-    for (int i = 0; i < SORT_WARPS; ++i) total += cnt[i * bins + threadIdx.x];
+    for (int i = 0; i < rows; ++i) total += s.cnt[i * bins + threadIdx.x];
   uint32_t incl = total;
+#pragma unroll
   for (int o = 1; o < 32; o <<= 1) {
-    const uint32_t x = __shfl_up_sync(0xffffffffu, incl, o);
-    if (lane >= o) incl += x;
+    const uint32_t z = __shfl_up_sync(0xffffffffu, incl, o);
+    if (lane >= o) incl += z;
   }
-  if (lane == 31) s_warp[w] = incl;
+  if (lane == 31) s.warp[w] = incl;
   __syncthreads();
-  uint32_t place = incl - total;
-  for (int i = 0; i < SORT_WARPS; ++i) place += s_below[i] + (i < w ? s_warp[i] : 0u);
+  uint32_t run = before + incl - total + __reduce_add_sync(0xffffffffu, lane < w ? s.warp[lane] : 0u);
   if (int(threadIdx.x) < bins) {
-    a.start[(int64_t(threadIdx.x) << a.nb_log) + b] = int32_t(place);
-    uint32_t run = place;
-    for (int i = 0; i < SORT_WARPS; ++i) { const uint32_t c = cnt[i * bins + threadIdx.x]; cnt[i * bins + threadIdx.x] = run; run += c; }
+    a.start[(int64_t(threadIdx.x) << a.nb_log) + b] = int32_t(run);
+    for (int i = 0; i < rows; ++i) { const uint32_t c = s.cnt[i * bins + threadIdx.x]; s.cnt[i * bins + threadIdx.x] = run; run += c; }
     if (int(threadIdx.x) == bins - 1) {
       a.start[(int64_t(bins) << a.nb_log) + b] = int32_t(run);
-      if (b == int(gridDim.x) - 1) *a.valid = int32_t(run);
+      if (b == gridDim.x - 1) *a.valid = int32_t(run);
     }
   }
   __syncthreads();
-  auto put = [&](int t, int v, bool mine) {
-    const unsigned any = __ballot_sync(0xffffffffu, mine);
-    if (any == 0) return;
-    if (mine) {
+  auto place = [&](int t, int v, bool is) {      // 32 tokens at a time, in order: the row's next place, past the lanes ahead with the same id
+    const unsigned any = __ballot_sync(0xffffffffu, is);
+    if (is) {
       const unsigned same = __match_any_sync(any, v);
-      const int rank = __popc(same & lower), bin = v >> a.nb_log;
-      const uint32_t slot = own[bin] + rank;
+      const int ahead = __popc(same & lower), bin = v >> a.nb_log;
+      const uint32_t slot = row[bin] + ahead;
       __syncwarp(any);
-      if (rank == 0) own[bin] += __popc(same);
+      if (ahead == 0) row[bin] += __popc(same);
       a.perm[slot] = t;
       a.row[slot] = v;
     }
     __syncwarp();
   };
-  if (found <= SORT_LIST) {
-    for (int i = lane; i < (found + 31) / 32 * 32; i += 32) {
-      const int2 e = i < found ? s_list[w][i] : make_int2(0, 0);
-      put(e.x, e.y, i < found);
+  if (listed) {
+    for (int i = i0 + lane; i - lane < i1; i += 32) {
+      const int2 e = i < i1 ? s.own[i] : make_int2(0, 0);
+      place(e.x, e.y, i < i1);
     }
   } else {
-    stretch([&](int t, int v, bool, bool mine) { put(t, v, mine); });
+    for (int64_t t = lo + lane; t - lane < hi; t += 32) {
+      const ID v = t < hi ? ids[t] : ID(-1);
+      place(int(t), int(v), mine(v));
+    }
   }
 }
 
@@ -247,11 +309,16 @@ struct SumArgs {
   int accumulate, nb, ncb;
   int dw_aligned;                    // the table's rows start at multiples of 16 bytes
   int64_t n_fill;                    // CTAs that clear
-  int fill_rows;                     // rows each of them looks at, a multiple of 32
+  int fill_rows;                     // rows each of them looks at
   float* dweight;
 };
 
 constexpr int SUM_TPB = 256;
+#ifndef RINGD
+#define RINGD 16
+#define MINB 3
+#endif
+constexpr int RING = RINGD;
 
 // A row of zeros, written by one warp: single words up to a 16-byte boundary, then 16 bytes a lane.
 __device__ __forceinline__ void clear_row(float* p, int64_t D, int lane) {
@@ -267,12 +334,11 @@ __device__ __forceinline__ void clear_row(float* p, int64_t D, int lane) {
 __device__ void clear_unused(const SumArgs& a, int64_t cta) {
   const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
   const int64_t v0 = cta * a.fill_rows, v1 = min(a.V, v0 + a.fill_rows);
-  for (int64_t v = v0; v < v1; v += 32) {
-    const bool unused = v + lane < v1 && a.start[v + lane] == a.start[v + lane + a.nb];
-    // every warp an eighth of the unused rows
-    unsigned m = __ballot_sync(0xffffffffu, unused);
-    for (int i = 0; m; ++i, m &= m - 1)
-      if ((i & (SUM_TPB / 32 - 1)) == w) clear_row(a.dweight + (v + __ffs(int(m)) - 1) * a.ldw, a.D, lane);
+  constexpr int W = SUM_TPB / 32;
+  for (int64_t v = v0 + w; v < v1; v += 32 * W) {     // every warp one row in W
+    const int64_t mine = v + lane * W;
+    const bool unused = mine < v1 && a.start[mine] == a.start[mine + a.nb];
+    for (unsigned m = __ballot_sync(0xffffffffu, unused); m; m &= m - 1) clear_row(a.dweight + (v + (__ffs(int(m)) - 1) * W) * a.ldw, a.D, lane);
   }
 }
 
@@ -335,8 +401,8 @@ template <typename X, bool VEC> __device__ __forceinline__ void fetch(const X* r
 
 // PIECE: tokens per warp.  Up to 16 rows of 512 bytes are on their way per warp: 24 warps a multiprocessor.
 template <typename X, bool VEC, int PIECE>
-__global__ void __launch_bounds__(SUM_TPB) k_embed_sum(const X* __restrict__ dout, const __grid_constant__ SumArgs a) {
-  constexpr int E = LANE<X>, DEPTH = PIECE < 16 ? PIECE : 16;
+__global__ void __launch_bounds__(SUM_TPB, MINB) k_embed_sum(const X* __restrict__ dout, const __grid_constant__ SumArgs a) {
+  constexpr int E = LANE<X>, DEPTH = PIECE < RING ? PIECE : RING;
   extern __shared__ uint4 ring[];                   // [DEPTH][thread]: a lane only ever reads what it fetched itself
   __shared__ float s_stage[VEC ? SUM_TPB / 32 : 1][VEC ? BLOCK<X> : 1];
   const int lane = threadIdx.x & 31;
@@ -480,8 +546,9 @@ int mv_embed_grad(void* stream, const void* dout, int dout_type, int64_t ldd, co
   const EmbedPlan p = embed_plan(T, V, (D + block - 1) / block * block, block);
   const int64_t items = p.pieces * p.ncb, n_sum = (items + SUM_TPB / 32 - 1) / (SUM_TPB / 32);
   SumArgs a;
-  // a CTA that clears looks at 64 KB of rows, or 32 rows
-  a.fill_rows = int(32 * (D >= 512 ? 1 : 512 / D));
+  // a CTA that clears looks at 128 KB of rows, or at eight rows (one a warp)
+  a.fill_rows = int(((32 << 10) / D + 7) / 8 * 8);
+  if (a.fill_rows < 8) a.fill_rows = 8;
   a.n_fill = accumulate ? 0 : (V + a.fill_rows - 1) / a.fill_rows;
   if (n_sum + a.n_fill >= lim) return MV_ERR_INVALID_ARG;
   if (accumulate && T == 0) return MV_OK;
@@ -495,13 +562,13 @@ int mv_embed_grad(void* stream, const void* dout, int dout_type, int64_t ldd, co
   s.valid = reinterpret_cast<int32_t*>(base + p.valid);
   s.ticket = reinterpret_cast<uint32_t*>(base + p.ticket);
   s.n_ticket = items;
-  const size_t smem = size_t(SORT_WARPS) * p.bins * 4;
+  const size_t smem = sizeof(SortSmem) + size_t(SORT_WARPS) * p.bins * 4;
   auto* sort = id_type == MV_I32 ? k_embed_sort<int32_t> : k_embed_sort<int64_t>;
   if (cudaFuncSetAttribute(sort, cudaFuncAttributeMaxDynamicSharedMemorySize, int(smem)) != cudaSuccess) {
     cudaGetLastError();
     return MV_ERR_CUDA;
   }
-  sort<<<unsigned(p.buckets), SORT_TPB, smem, st>>>(s);
+  sort<<<1u << p.nb_log, SORT_TPB, smem, st>>>(s);
   a.perm = s.perm; a.row = s.row; a.start = s.start; a.valid = s.valid; a.ticket = s.ticket;
   a.part = reinterpret_cast<float*>(base + p.part);
   a.V = V; a.D = D; a.ldd = ldd; a.ldw = ldw; a.scale = scale; a.accumulate = accumulate; a.nb = 1 << p.nb_log;
@@ -513,7 +580,7 @@ int mv_embed_grad(void* stream, const void* dout, int dout_type, int64_t ldd, co
     const bool vec = rows_aligned(dout, ldd, sizeof(X), 16);
     auto* kernel = p.piece == 32 ? (vec ? k_embed_sum<X, true, 32> : k_embed_sum<X, false, 32>)
                                  : (vec ? k_embed_sum<X, true, 8> : k_embed_sum<X, false, 8>);
-    const int ring = (p.piece == 32 ? 16 : 8) * SUM_TPB * 16;
+    const int ring = (p.piece < RING ? p.piece : RING) * SUM_TPB * 16;
     if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, ring) != cudaSuccess) {
       cudaGetLastError();
       return int(MV_ERR_CUDA);

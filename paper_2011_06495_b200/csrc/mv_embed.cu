@@ -104,15 +104,12 @@ struct EmbedPlan {
 
 inline EmbedPlan embed_plan(int64_t T, int64_t V, int64_t D, int block) {
   EmbedPlan p;
-#ifndef NBL
-#define NBL 7
-#endif
-  p.nb_log = NBL;
+  p.nb_log = 7;
   while (((V - 1) >> p.nb_log) + 1 > SORT_BINS) ++p.nb_log;
   p.bins = ((V - 1) >> p.nb_log) + 1;
   p.ncb = (D + block - 1) / block;
-  // short pieces while long ones would not give every multiprocessor its 24 warps: then the length of one warp's chain counts
-  p.piece = (T + 31) / 32 * p.ncb >= 148 * 24 ? 32 : 8;
+  // short pieces while long ones would not give every multiprocessor its 32 warps: then the length of one warp's chain counts
+  p.piece = (T + 31) / 32 * p.ncb >= 148 * 32 ? 32 : 8;
   p.pieces = (T + p.piece - 1) / p.piece;
   size_t o = 0;
   p.valid = o;  o = align_up(o + 4, 16);
@@ -233,6 +230,15 @@ __global__ void __launch_bounds__(SORT_TPB) k_embed_sort(const __grid_constant__
   const int chunk = (own + SORT_TPB - 1) / SORT_TPB * 32;
   const int rows = listed ? (own == 0 ? 0 : (own + chunk - 1) / chunk) : SORT_WARPS;
   const int i0 = min(own, w * chunk), i1 = min(own, i0 + chunk);
+  auto again = [&](auto&& f) {       // the stretch once more, 32 tokens at a time and in order, eight loads on their way
+    for (int64_t t0 = lo; t0 < hi; t0 += 256) {
+      ID v[8];
+#pragma unroll
+      for (int u = 0; u < 8; ++u) v[u] = t0 + u * 32 + lane < hi ? ids[t0 + u * 32 + lane] : ID(-1);
+#pragma unroll
+      for (int u = 0; u < 8; ++u) f(int(t0) + u * 32 + lane, v[u]);
+    }
+  };
   auto mine = [&](ID v) { return known(v) && (uint32_t(v) & mask) == b; };
   if (listed) {
     const int at = int(__reduce_add_sync(0xffffffffu, lane < w ? nw : 0u));
@@ -240,10 +246,9 @@ __global__ void __launch_bounds__(SORT_TPB) k_embed_sort(const __grid_constant__
     __syncthreads();
     for (int i = i0 + lane; i < i1; i += 32) atomicAdd(&row[s.own[i].y >> a.nb_log], 1u);
   } else {
-    for (int64_t t = lo + lane; t < hi; t += 32) {
-      const ID v = ids[t];
+    again([&](int, ID v) {
       if (mine(v)) atomicAdd(&row[uint32_t(v) >> a.nb_log], 1u);
-    }
+    });
   }
   __syncthreads();
   // places: an exclusive scan over the ids' totals, then over the rows of each id
@@ -287,10 +292,7 @@ __global__ void __launch_bounds__(SORT_TPB) k_embed_sort(const __grid_constant__
       place(e.x, e.y, i < i1);
     }
   } else {
-    for (int64_t t = lo + lane; t - lane < hi; t += 32) {
-      const ID v = t < hi ? ids[t] : ID(-1);
-      place(int(t), int(v), mine(v));
-    }
+    again([&](int t, ID v) { place(t, int(v), mine(v)); });
   }
 }
 
@@ -299,7 +301,7 @@ __global__ void __launch_bounds__(SORT_TPB) k_embed_sort(const __grid_constant__
 // equal ids that lies inside the piece is finished there.  One that crosses into other pieces leaves a partial sum per
 // piece; the warp that leaves the last one adds the partial sums up in the order of the pieces.  So a frequent token's
 // rows are read by many warps, and the result does not depend on which of them comes last.  CTAs that clear the rows
-// without a token stand between those that sum, so that reads and writes share the memory's time.
+// without a token follow those that sum.
 struct SumArgs {
   const int32_t *perm, *row, *start, *valid;
   uint32_t* ticket;
@@ -307,18 +309,14 @@ struct SumArgs {
   int64_t V, D, ldd, ldw;
   float scale;
   int accumulate, nb, ncb;
-  int dw_aligned;                    // the table's rows start at multiples of 16 bytes
+  int dw_aligned;                    // the table's rows start at multiples of what a lane stores (16 or 32 bytes)
   int64_t n_fill;                    // CTAs that clear
   int fill_rows;                     // rows each of them looks at
   float* dweight;
 };
 
 constexpr int SUM_TPB = 256;
-#ifndef RINGD
-#define RINGD 16
-#define MINB 3
-#endif
-constexpr int RING = RINGD;
+constexpr int RING = 8;              // rows on their way per warp (4 KB; 32 warps a multiprocessor)
 
 // A row of zeros, written by one warp: single words up to a 16-byte boundary, then 16 bytes a lane.
 __device__ __forceinline__ void clear_row(float* p, int64_t D, int lane) {
@@ -348,15 +346,22 @@ template <typename X, bool VEC>
 __device__ __forceinline__ void put_row(const SumArgs& a, int64_t v, int64_t cb, int lane, const Lanes<X>& acc, float* stage) {
   float* dst = a.dweight + v * a.ldw;
   if (VEC && a.dw_aligned && column<X, VEC>(cb, lane, 0) + LANE<X> <= a.D) {
+    float* q = dst + column<X, VEC>(cb, lane, 0);
+    float o[LANE<X>];
 #pragma unroll
-    for (int j = 0; j < LANE<X>; j += 4) {
-      float4* q = reinterpret_cast<float4*>(dst + column<X, VEC>(cb, lane, j));
-      float4 o = make_float4(acc.v[j] * a.scale, acc.v[j + 1] * a.scale, acc.v[j + 2] * a.scale, acc.v[j + 3] * a.scale);
-      if (a.accumulate) {
-        const float4 old = *q;
-        o.x += old.x; o.y += old.y; o.z += old.z; o.w += old.w;
+    for (int j = 0; j < LANE<X>; ++j) o[j] = acc.v[j] * a.scale;
+    if (a.accumulate) {
+#pragma unroll
+      for (int j = 0; j < LANE<X>; j += 4) {
+        const float4 old = *reinterpret_cast<const float4*>(q + j);
+        o[j] += old.x; o[j + 1] += old.y; o[j + 2] += old.z; o[j + 3] += old.w;
       }
-      *q = o;
+    }
+    if constexpr (LANE<X> == 8) {      // one 32-byte store a lane: whole sectors
+      asm volatile("st.global.v8.f32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(q), "f"(o[0]), "f"(o[1]), "f"(o[2]), "f"(o[3]), "f"(o[4]),
+                   "f"(o[5]), "f"(o[6]), "f"(o[7]) : "memory");
+    } else {
+      *reinterpret_cast<float4*>(q) = make_float4(o[0], o[1], o[2], o[3]);
     }
     return;
   }
@@ -399,25 +404,26 @@ template <typename X, bool VEC> __device__ __forceinline__ void fetch(const X* r
   }
 }
 
-// PIECE: tokens per warp.  Up to 16 rows of 512 bytes are on their way per warp: 24 warps a multiprocessor.
+// PIECE: tokens per warp.
 template <typename X, bool VEC, int PIECE>
-__global__ void __launch_bounds__(SUM_TPB, MINB) k_embed_sum(const X* __restrict__ dout, const __grid_constant__ SumArgs a) {
+__global__ void __launch_bounds__(SUM_TPB, 4) k_embed_sum(const X* __restrict__ dout, const __grid_constant__ SumArgs a) {
   constexpr int E = LANE<X>, DEPTH = PIECE < RING ? PIECE : RING;
   extern __shared__ uint4 ring[];                   // [DEPTH][thread]: a lane only ever reads what it fetched itself
   __shared__ float s_stage[VEC ? SUM_TPB / 32 : 1][VEC ? BLOCK<X> : 1];
   const int lane = threadIdx.x & 31;
   float* stage = VEC ? s_stage[threadIdx.x >> 5] : nullptr;
-  // the CTAs that clear are spread evenly between the others
-  const int64_t fill = int64_t(blockIdx.x) * a.n_fill / gridDim.x;
-  const bool clears = int64_t(blockIdx.x + 1) * a.n_fill / gridDim.x != fill;
-  const int64_t item = (blockIdx.x - fill) * (SUM_TPB / 32) + (threadIdx.x >> 5);
+  // the CTAs that clear come last: their stores fill the time in which the last sums wait for their rows (in between, or
+  // first, they cost 8 to 4 % more at 65536 tokens, 65536 x 2048)
+  const int64_t n_sum = gridDim.x - a.n_fill;
+  const bool clears = blockIdx.x >= n_sum;
+  const int64_t item = int64_t(blockIdx.x) * (SUM_TPB / 32) + (threadIdx.x >> 5);
   const int64_t piece = item / a.ncb, cb = item % a.ncb;
   const int64_t s0 = piece * PIECE;
   if (!clears)
     for (int i = 0; i < DEPTH; ++i) ring[i * SUM_TPB + threadIdx.x] = make_uint4(0, 0, 0, 0);     // columns beyond the row stay zero
   asm volatile("griddepcontrol.wait;" ::: "memory");
   if (clears) {
-    clear_unused(a, fill);
+    clear_unused(a, blockIdx.x - n_sum);
     return;
   }
   const int64_t valid = *a.valid;
@@ -573,7 +579,7 @@ int mv_embed_grad(void* stream, const void* dout, int dout_type, int64_t ldd, co
   a.part = reinterpret_cast<float*>(base + p.part);
   a.V = V; a.D = D; a.ldd = ldd; a.ldw = ldw; a.scale = scale; a.accumulate = accumulate; a.nb = 1 << p.nb_log;
   a.ncb = int(p.ncb);
-  a.dw_aligned = rows_aligned(dweight, ldw, 4, 16);
+  a.dw_aligned = rows_aligned(dweight, ldw, 4, dout_type == MV_F32 ? 16 : 32);
   a.dweight = dweight;
   return with_type(dout_type, [&](auto x) {
     using X = decltype(x);

@@ -2,8 +2,9 @@
 //
 // With z = c x, r a reference near the row's largest logit and t = (x - r) c log2(e):  s = sum 2^t,  lse = c r + log s,
 // H = log s - ln 2 (sum 2^t t) / s.  A masked logit (-inf) has 2^t = 0 and must not multiply its t, so t is kept above a
-// finite floor.  The difference x - r is formed before it is scaled: c r alone may overflow (a row of the type's lowest
-// value).
+// finite floor.  t is one fused multiply-add, x (c log2 e) - R with R = r c log2(e) rounded; what the rounding of R costs is put
+// right once per thread.  Rows in which R itself would overflow (every logit near the type's lowest or largest value) are
+// summed again in a form that takes the difference first.
 
 #include "mv_lm.cuh"
 
@@ -16,8 +17,7 @@ namespace cg = cooperative_groups;
 
 constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
 constexpr float T_FLOOR = -1.0e30f;
-constexpr int TPB = 256;
-constexpr int WARPS = TPB / 32;
+constexpr float R_MAX = 1.0e37f;     // references up to here are summed by the fused form
 
 __device__ __forceinline__ float max_nan(float a, float b) {
   float r;
@@ -54,14 +54,13 @@ __device__ __forceinline__ f2 fma2(f2 a, f2 b, f2 c) {
   return r;
 }
 
-// 16 bytes of logits: their largest (a NaN never is), and the elements two by two.
+// 16 bytes of logits: the larger halves of two words (a NaN is never the larger), the larger half of one, and the elements two by two.
 template <typename X> struct Vec;
 template <> struct Vec<float> {
   static constexpr int N = 4;
   static constexpr uint32_t NONE = 0xff800000u;                       // -inf
-  __device__ static float largest(const uint4& u) {
-    return fmaxf(fmaxf(__uint_as_float(u.x), __uint_as_float(u.y)), fmaxf(__uint_as_float(u.z), __uint_as_float(u.w)));
-  }
+  __device__ static uint32_t max2(uint32_t a, uint32_t b) { return __float_as_uint(fmaxf(__uint_as_float(a), __uint_as_float(b))); }
+  __device__ static float widen(uint32_t m) { return __uint_as_float(m); }
   __device__ static f2 pair(const uint4& u, int i) {
     return i == 0 ? pack2(__uint_as_float(u.x), __uint_as_float(u.y)) : pack2(__uint_as_float(u.z), __uint_as_float(u.w));
   }
@@ -75,10 +74,7 @@ template <> struct Vec<__nv_bfloat16> {
     asm("max.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
     return r;
   }
-  __device__ static float largest(const uint4& u) {
-    const uint32_t m = max2(max2(u.x, u.y), max2(u.z, u.w));
-    return fmaxf(__uint_as_float(m << 16), __uint_as_float(m & 0xffff0000u));
-  }
+  __device__ static float widen(uint32_t m) { return fmaxf(__uint_as_float(m << 16), __uint_as_float(m & 0xffff0000u)); }
   __device__ static f2 pair(const uint4& u, int i) {
     const uint32_t w = word(u, i);
     return pack2(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u));
@@ -97,8 +93,8 @@ template <> struct Vec<__half> {
     memcpy(&h, &w, 4);
     return __half22float2(h);
   }
-  __device__ static float largest(const uint4& u) {
-    const float2 f = both(max2(max2(u.x, u.y), max2(u.z, u.w)));
+  __device__ static float widen(uint32_t m) {
+    const float2 f = both(m);
     return fmaxf(f.x, f.y);
   }
   __device__ static f2 pair(const uint4& u, int i) {
@@ -146,7 +142,7 @@ struct TopSmem {
   unsigned long long key[KEY_LIST];
   unsigned long long best[MV_TOP_MAX];
   uint16_t group[GROUP_LIST];
-  float sorted[WARPS][32];
+  float sorted[16][32];              // of each warp
   float bound;
   int n_key, n_group, n_above, found;
 };
@@ -176,8 +172,9 @@ template <typename X, typename F> __device__ __forceinline__ void each_logit(con
 }
 
 // The k best keys of this part, in order, in s.best (0 where there are fewer).  All threads; ends with a barrier.
-template <typename X>
+template <typename X, int TPB>
 __device__ void best_of_part(const Part<X>& p, int k, const float* gmax, int groups, int steps, float mine, TopSmem& s) {
+  constexpr int WARPS = TPB / 32;
   const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
   const float sorted = sort_warp(mine);
   s.sorted[w][lane] = sorted;
@@ -345,10 +342,36 @@ __device__ __forceinline__ Sums shift(const Sums& x, float ref, float c2) {
   return {ref, x.s * f, fmaf(x.s, d, x.st) * f};
 }
 
+// The sums of a part whose reference does not fit the fused form (or that is empty): the largest logit first, then the differences.
+template <typename X, int TPB>
+__device__ __noinline__ Sums sums_of_extremes(const Part<X>& p, float c2, float* sh) {
+  const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
+  float m = -INFINITY;
+  auto all = [&](auto&& f) {
+    if (threadIdx.x < p.head + p.tail) f(to_f(p.row[threadIdx.x < p.head ? threadIdx.x : p.tail_col + threadIdx.x - p.head]));
+    for (int64_t v = threadIdx.x; v < p.nv; v += TPB) each_logit<X>(__ldg(p.vec + v), [&](int, float x) { f(x); });
+  };
+  all([&](float x) { m = fmaxf(m, x); });
+  for (int o = 16; o; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+  __syncthreads();
+  if (lane == 0) sh[w] = m;
+  __syncthreads();
+  for (int i = 0; i < TPB / 32; ++i) m = fmaxf(m, sh[i]);
+  const float ref = m == -INFINITY ? 0.0f : m;
+  Sums x = {m, 0.0f, 0.0f};
+  all([&](float v) {
+    const float u = max_nan((v - ref) * c2, T_FLOOR), e = exp2_fast(u);
+    x.s += e;
+    x.st = fmaf(e, u, x.st);
+  });
+  __syncthreads();
+  return x;
+}
+
 // A row belongs to a cluster of CTAs (one CTA when there are rows enough), each of which streams a part of it once.
-template <typename X, bool TOP>
-__global__ void __launch_bounds__(TPB, 4) k_token_logprob(const X* __restrict__ logits, const __grid_constant__ LogprobArgs a) {
-  constexpr int N = Vec<X>::N;
+template <typename X, bool TOP, int TPB>
+__global__ void __launch_bounds__(TPB, 1024 / TPB) k_token_logprob(const X* __restrict__ logits, const __grid_constant__ LogprobArgs a) {
+  constexpr int N = Vec<X>::N, WARPS = TPB / 32;
   extern __shared__ float gmax[];    // [group][thread], with TOP
   __shared__ Sums s_sums[WARPS];
   __shared__ Sums s_part;
@@ -361,12 +384,12 @@ __global__ void __launch_bounds__(TPB, 4) k_token_logprob(const X* __restrict__ 
   p.row = logits + t * a.ld;
   // the vectors begin at the row's first 16-byte boundary
   const int64_t to16 = int64_t((16 - (reinterpret_cast<uintptr_t>(p.row) & 15)) & 15) / int(sizeof(X));
-  const int64_t first = min(a.V, to16), all = (a.V - first) / N, per = (all + ctas - 1) / ctas, v0 = min(all, rank * per);
+  const int first = int(min(a.V, to16)), all = (int(a.V) - first) / N, per = (all + ctas - 1) / ctas, v0 = min(all, rank * per);
   p.nv = min(all - v0, per);
   p.vec = reinterpret_cast<const uint4*>(p.row + first) + v0;
-  p.col0 = uint32_t(first + v0 * N);
+  p.col0 = uint32_t(first) + uint32_t(v0) * N;
   p.head = rank == 0 ? uint32_t(first) : 0u;
-  p.tail_col = uint32_t(first + all * N);
+  p.tail_col = uint32_t(first) + uint32_t(all) * N;
   p.tail = rank == ctas - 1 ? uint32_t(a.V) - p.tail_col : 0u;
   int64_t y = -1;
   float xy = 0.0f;
@@ -374,84 +397,95 @@ __global__ void __launch_bounds__(TPB, 4) k_token_logprob(const X* __restrict__ 
     y = load_id(a.targets, a.id_type, t, a.V);
     if (y >= 0) xy = to_f(p.row[y]);
   }
+  const uint4 none = make_uint4(Vec<X>::NONE, Vec<X>::NONE, Vec<X>::NONE, Vec<X>::NONE);
+  const uint4* ptr = p.vec + threadIdx.x;
+  const int nv = int(p.nv), n_full = nv / (TPB * U), n_steps = (nv + TPB * U - 1) / (TPB * U);
+  auto load = [&](int step, uint4 (&u)[U]) {
+    if (step < n_full) {
+#pragma unroll
+      for (int i = 0; i < U; ++i) u[i] = load_stream(ptr + i * TPB);
+    } else {
+#pragma unroll
+      for (int i = 0; i < U; ++i) u[i] = step * TPB * U + i * TPB + int(threadIdx.x) < nv ? load_stream(ptr + i * TPB) : none;
+    }
+    ptr += U * TPB;
+  };
   const float c2 = a.scale * LOG2E, room = 40.0f / c2;      // a larger logit changes the reference only if it exceeds it by 2^40
   const f2 c22 = pack2(c2, c2);
-  Sums x = {-INFINITY, 0.0f, 0.0f};
-  float limit = -INFINITY;
+  float ref = -INFINITY, R = 0.0f, limit = -R_MAX / c2;     // logits below that never set the reference
   f2 minus = pack2(0.0f, 0.0f), s2 = pack2(0.0f, 0.0f), st2 = s2;
   auto raise = [&](float m) {        // a new reference
-    float p0, p1, q0, q1;
-    unpack2(s2, p0, p1);
-    unpack2(st2, q0, q1);
-    x = {x.ref, p0 + p1, q0 + q1};
-    if (x.ref == -INFINITY) x.ref = m;                      // nothing but masked logits so far (or a NaN, which stays)
-    else x = shift(x, m, c2);
-    s2 = pack2(x.s, 0.0f);
-    st2 = pack2(x.st, 0.0f);
+    const float Rm = m * c2;
+    if (ref != -INFINITY) {
+      const float d = max_nan(R - Rm, T_FLOOR), f = exp2_fast(d);
+      float p0, p1, q0, q1;
+      unpack2(s2, p0, p1);
+      unpack2(st2, q0, q1);
+      p0 += p1;
+      s2 = pack2(p0 * f, 0.0f);
+      st2 = pack2(fmaf(p0, d, q0 + q1) * f, 0.0f);
+    }                                // else nothing but masked logits so far (or a NaN, which stays)
+    ref = m;
+    R = Rm;
     limit = m + room;
-    minus = pack2(-m, -m);
+    minus = pack2(-Rm, -Rm);
   };
   auto add_pair = [&](f2 v) {
     float u0, u1;
-    unpack2(mul2(add2(v, minus), c22), u0, u1);
-    u0 = max_nan(u0, T_FLOOR);
-    u1 = max_nan(u1, T_FLOOR);
+    unpack2(fma2(v, c22, minus), u0, u1);
     const f2 e = pack2(exp2_fast(u0), exp2_fast(u1));
     s2 = add2(s2, e);
-    st2 = fma2(e, pack2(u0, u1), st2);
+    st2 = fma2(e, pack2(max_nan(u0, T_FLOOR), max_nan(u1, T_FLOOR)), st2);
   };
-  if (threadIdx.x < p.head + p.tail) {
-    const float v = to_f(p.row[threadIdx.x < p.head ? threadIdx.x : p.tail_col + threadIdx.x - p.head]);
-    if (v > limit) raise(v);
-    add_pair(pack2(v, -INFINITY));
-  }
-  const int n_steps = int((p.nv + TPB * U - 1) / (TPB * U));
-  const uint4 none = make_uint4(Vec<X>::NONE, Vec<X>::NONE, Vec<X>::NONE, Vec<X>::NONE);
-  uint4 next[U];
-#pragma unroll
-  for (int i = 0; i < U; ++i) {
-    const int64_t v = i * TPB + threadIdx.x;
-    next[i] = v < p.nv ? load_stream(p.vec + v) : none;
-  }
-  float gm = -INFINITY, mine = -INFINITY;
+  float gm = -INFINITY, mine = -INFINITY, extra = -INFINITY;
   int left = a.steps, group = 0;
-  for (int step = 0; step < n_steps; ++step) {
-    uint4 u[U];
+  auto take = [&](const uint4 (&u)[U]) {
+    uint32_t m2 = Vec<X>::max2(Vec<X>::max2(u[0].x, u[0].y), Vec<X>::max2(u[0].z, u[0].w));
 #pragma unroll
-    for (int i = 0; i < U; ++i) u[i] = next[i];
-    if (step + 1 < n_steps) {
-#pragma unroll
-      for (int i = 0; i < U; ++i) {
-        const int64_t v = (int64_t(step + 1) * U + i) * TPB + threadIdx.x;
-        next[i] = v < p.nv ? load_stream(p.vec + v) : none;
+    for (int i = 1; i < U; ++i) m2 = Vec<X>::max2(m2, Vec<X>::max2(Vec<X>::max2(u[i].x, u[i].y), Vec<X>::max2(u[i].z, u[i].w)));
+    const float m = Vec<X>::widen(m2);
+    if (m > limit) raise(m);
+    mine = fmaxf(mine, m);
+    if (TOP) {
+      gm = fmaxf(gm, m);
+      if (--left == 0) {
+        gmax[group++ * TPB + threadIdx.x] = gm;
+        gm = -INFINITY;
+        left = a.steps;
       }
     }
 #pragma unroll
-    for (int i = 0; i < U; ++i) {
-      const float m = Vec<X>::largest(u[i]);
-      if (m > limit) raise(m);
-      if (TOP) gm = fmaxf(gm, m);
+    for (int i = 0; i < U; ++i)
 #pragma unroll
       for (int j = 0; j < N / 2; ++j) add_pair(Vec<X>::pair(u[i], j));
-    }
-    if (TOP && --left == 0) {
-      gmax[group++ * TPB + threadIdx.x] = gm;
-      mine = fmaxf(mine, gm);
-      gm = -INFINITY;
-      left = a.steps;
-    }
+  };
+  uint4 even[U], odd[U];
+  if (n_steps > 0) load(0, even);
+  if (threadIdx.x < p.head + p.tail) {
+    extra = to_f(p.row[threadIdx.x < p.head ? threadIdx.x : p.tail_col + threadIdx.x - p.head]);
+    if (extra > limit) raise(extra);
+    add_pair(pack2(extra, -INFINITY));
   }
-  if (TOP && left != a.steps) {
-    gmax[group++ * TPB + threadIdx.x] = gm;
-    mine = fmaxf(mine, gm);
+  for (int step = 0; step < n_steps; step += 2) {
+    if (step + 1 < n_steps) load(step + 1, odd);
+    take(even);
+    if (step + 1 >= n_steps) break;
+    if (step + 2 < n_steps) load(step + 2, even);
+    take(odd);
   }
+  if (TOP && left != a.steps) gmax[group++ * TPB + threadIdx.x] = gm;
+  Sums x;
   {
     float p0, p1, q0, q1;
     unpack2(s2, p0, p1);
     unpack2(st2, q0, q1);
-    x.s = p0 + p1;
-    x.st = q0 + q1;
+    const float d = ref == -INFINITY ? 0.0f : fmaf(ref, c2, -R), f = 1.0f - LN2 * d;      // d: at most half a unit of R; 2^-d
+    x = {ref, (p0 + p1) * f, fmaf(-d, p0 + p1, q0 + q1) * f};
   }
+  const float top = fmaxf(mine, extra);
+  // logits that the fused form cannot take: too large ones anywhere, or nothing but too small ones
+  if (__syncthreads_or(top * c2 > R_MAX) || (!__syncthreads_or(ref != -INFINITY) && __syncthreads_or(top > -INFINITY)))
+    x = sums_of_extremes<X, TPB>(p, c2, &s_sums[0].ref);
   // the threads' sums to one reference, warp by warp and then together
   float m = x.ref;
 #pragma unroll
@@ -474,7 +508,7 @@ __global__ void __launch_bounds__(TPB, 4) k_token_logprob(const X* __restrict__ 
     x.s += __shfl_xor_sync(0xffffffffu, x.s, o);
     x.st += __shfl_xor_sync(0xffffffffu, x.st, o);
   }
-  if (TOP) best_of_part(p, a.k, gmax, group, a.steps, mine, s_top[0]);
+  if (TOP) best_of_part<X, TPB>(p, a.k, gmax, group, a.steps, mine, s_top[0]);
   if (ctas > 1) {
     if (threadIdx.x == 0) s_part = x;
     cluster.sync();
@@ -506,22 +540,24 @@ __global__ void __launch_bounds__(TPB, 4) k_token_logprob(const X* __restrict__ 
     if (rank != 0) return;
   }
   const bool empty = x.s == 0.0f;
-  const float ref = empty ? 0.0f : x.ref, ls = logf(x.s);
+  const float r = empty ? 0.0f : x.ref, ls = logf(x.s);
   if (threadIdx.x == 0) {
-    if (a.lse) a.lse[t] = empty ? -INFINITY : fmaf(a.scale, ref, ls);
+    if (a.lse) a.lse[t] = empty ? -INFINITY : fmaf(a.scale, r, ls);
     if (a.entropy) a.entropy[t] = empty ? 0.0f : ls - LN2 * (x.st / x.s);
-    if (a.logprob) a.logprob[t] = y < 0 ? 0.0f : empty ? -INFINITY : (xy - ref) * a.scale - ls;
+    if (a.logprob) a.logprob[t] = y < 0 ? 0.0f : empty ? -INFINITY : (xy - r) * a.scale - ls;
   }
   if (TOP && int(threadIdx.x) < a.k) {
     const unsigned long long key = s_top[0].best[threadIdx.x];
     const float v = key_value(key);
     if (a.top_id) a.top_id[t * a.k + threadIdx.x] = key ? int32_t(key_index(key)) : -1;
-    if (a.top_logprob) a.top_logprob[t * a.k + threadIdx.x] = isnan(x.s) ? x.s : key == 0 || v == -INFINITY ? -INFINITY : (v - ref) * a.scale - ls;
+    if (a.top_logprob) a.top_logprob[t * a.k + threadIdx.x] = isnan(x.s) ? x.s : key == 0 || v == -INFINITY ? -INFINITY : (v - r) * a.scale - ls;
   }
 }
 
+constexpr int GRAD_TPB = 256;
+
 template <typename X>
-__global__ void __launch_bounds__(TPB) k_token_grad(const X* logits, int64_t V, int64_t ld, const void* __restrict__ targets, int id_type, float scale,
+__global__ void __launch_bounds__(GRAD_TPB) k_token_grad(const X* logits, int64_t V, int64_t ld, const void* __restrict__ targets, int id_type, float scale,
                                                      const float* __restrict__ lse, const float* __restrict__ entropy, const float* __restrict__ g_logprob,
                                                      const float* __restrict__ g_entropy, X* dlogits, int64_t ldg) {
   const int64_t t = blockIdx.x;
@@ -533,7 +569,7 @@ __global__ void __launch_bounds__(TPB) k_token_grad(const X* logits, int64_t V, 
   const float g2 = g_entropy ? g_entropy[t] : 0.0f;
   const bool none = (g1 == 0.0f && g2 == 0.0f) || l == -INFINITY;
   const float a = g1 + (g2 == 0.0f ? 0.0f : g2 * entropy[t]);
-  for (int64_t j = threadIdx.x; j < V; j += TPB) {
+  for (int64_t j = threadIdx.x; j < V; j += GRAD_TPB) {
     float d = 0.0f;
     if (!none) {
       const float lp = max_nan(fmaf(to_f(x[j]), scale, -l), T_FLOOR);
@@ -567,18 +603,19 @@ int mv_token_logprob(void* stream, const void* logits, int type, int64_t T, int6
   return with_type(type, [&](auto x) {
     using X = decltype(x);
     const int64_t vecs = V / Vec<X>::N;
-    // CTAs per row: until there are eight for each place on the device (148 multiprocessors, four CTAs each), while a CTA
-    // keeps a whole step of its own
+    // Many rows: small CTAs, whose ends overlap with the others' streaming.  Fewer rows than multiprocessors: large CTAs, and as many per row
+    // (up to the eight of a portable cluster) as keep a whole step for each thread and fit the device at once.
+    const int tpb = T < 148 ? 512 : 128;
     int ctas = 1;
-    while (ctas < 8 && T * ctas < 148 * 4 * 8 && vecs >= int64_t(ctas) * 2 * TPB * U) ctas *= 2;
-    const int64_t n_steps = ((vecs + ctas - 1) / ctas + TPB * U - 1) / (TPB * U);
+    while (ctas < 8 && T * ctas * tpb < 148 * 1024 && vecs >= int64_t(ctas) * 2 * tpb * U) ctas *= 2;
+    const int64_t n_steps = ((vecs + ctas - 1) / ctas + tpb * U - 1) / (tpb * U);
     a.steps = int((n_steps + MAX_GROUPS - 1) / MAX_GROUPS);
     if (a.steps < 1) a.steps = 1;
     if (T * ctas >= lim) return int(MV_ERR_INVALID_ARG);
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(unsigned(T * ctas));
-    cfg.blockDim = dim3(TPB);
-    cfg.dynamicSmemBytes = k ? size_t((n_steps + a.steps - 1) / a.steps) * TPB * 4 : 0;
+    cfg.blockDim = dim3(unsigned(tpb));
+    cfg.dynamicSmemBytes = k ? size_t((n_steps + a.steps - 1) / a.steps) * tpb * 4 : 0;
     cfg.stream = st;
     cudaLaunchAttribute attr = {};
     attr.id = cudaLaunchAttributeClusterDimension;
@@ -586,7 +623,12 @@ int mv_token_logprob(void* stream, const void* logits, int type, int64_t T, int6
     attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
     cfg.attrs = &attr;
     cfg.numAttrs = 1;
-    auto* kernel = k ? k_token_logprob<X, true> : k_token_logprob<X, false>;
+    auto* kernel = tpb == 128 ? (k ? k_token_logprob<X, true, 128> : k_token_logprob<X, false, 128>)
+                              : (k ? k_token_logprob<X, true, 512> : k_token_logprob<X, false, 512>);
+    if (cfg.dynamicSmemBytes > 32 << 10 && cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 64 << 10) != cudaSuccess) {
+      cudaGetLastError();
+      return int(MV_ERR_CUDA);
+    }
     const bool ok = cudaLaunchKernelEx(&cfg, kernel, static_cast<const X*>(logits), a) == cudaSuccess;
     return cuda_ok() == MV_OK && ok ? int(MV_OK) : int(MV_ERR_CUDA);
   });
@@ -610,7 +652,7 @@ int mv_token_logprob_grad(void* stream, const void* logits, int type, int64_t T,
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   return with_type(type, [&](auto x) {
     using X = decltype(x);
-    k_token_grad<X><<<unsigned(T), TPB, 0, st>>>(static_cast<const X*>(logits), V, ld, targets, id_type, scale, lse, entropy, g_logprob, g_entropy,
+    k_token_grad<X><<<unsigned(T), GRAD_TPB, 0, st>>>(static_cast<const X*>(logits), V, ld, targets, id_type, scale, lse, entropy, g_logprob, g_entropy,
                                                   static_cast<X*>(dlogits), ldg);
     return cuda_ok();
   });

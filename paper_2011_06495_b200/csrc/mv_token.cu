@@ -43,11 +43,6 @@ __device__ __forceinline__ f2 add2(f2 a, f2 b) {
   asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
   return r;
 }
-__device__ __forceinline__ f2 mul2(f2 a, f2 b) {
-  f2 r;
-  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
-  return r;
-}
 __device__ __forceinline__ f2 fma2(f2 a, f2 b, f2 c) {
   f2 r;
   asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
@@ -144,7 +139,7 @@ struct TopSmem {
   uint16_t group[GROUP_LIST];
   float sorted[16][32];              // of each warp
   float bound;
-  int n_key, n_group, n_above, found;
+  int n_key, n_group, found;
 };
 
 // Sorts a warp's 32 values in descending order.
@@ -171,107 +166,107 @@ template <typename X, typename F> __device__ __forceinline__ void each_logit(con
   }
 }
 
-// The k best keys of this part, in order, in s.best (0 where there are fewer).  All threads; ends with a barrier.
+__device__ __forceinline__ void push_key(TopSmem& s, float x, uint32_t col) {
+  const int i = atomicAdd(&s.n_key, 1);
+  if (i < KEY_LIST) s.key[i] = make_key(x, col);
+}
+
+// Every candidate's place is the number of candidates before it.
+template <int TPB> __device__ __forceinline__ void rank_keys(TopSmem& s, int n, int k) {
+#pragma unroll 1
+  for (int i = threadIdx.x; i < n; i += TPB) {
+    const unsigned long long mine = s.key[i];
+    int place = 0;
+#pragma unroll 2
+    for (int j = 0; j < n; ++j) place += s.key[j] > mine;
+    if (place < k && mine != 0) s.best[place] = mine;
+  }
+}
+
+// The elements of the listed groups that reach the bound (or lie above it) become candidates.
+template <typename X, int TPB> __device__ __forceinline__ void gather_groups(const Part<X>& p, int listed, int steps, bool above, TopSmem& s) {
+  const float B = s.bound;
+  const unsigned per = unsigned(steps) * U;                          // vectors per group
+#pragma unroll 1
+  for (unsigned i = threadIdx.x; i < listed * per; i += TPB) {
+    const unsigned gi = s.group[i / per], v = gi % TPB + (gi / TPB * per + i % per) * TPB;
+    if (int64_t(v) >= p.nv) continue;
+    const uint4 u = __ldg(p.vec + v);
+    unsigned hit = 0;
+    each_logit<X>(u, [&](int e, float y) { hit |= (above ? y > B : y >= B) ? 1u << e : 0u; });
+    for (; hit; hit &= hit - 1) {
+      const unsigned c = v * Vec<X>::N + __ffs(int(hit)) - 1;
+      push_key(s, to_f(reinterpret_cast<const X*>(p.vec)[c]), p.col0 + c);
+    }
+  }
+}
+
+// The groups whose maximum reaches the bound (or lies above it).
+template <int TPB> __device__ __forceinline__ void list_groups(const float* gmax, int groups, bool above, TopSmem& s) {
+  const float B = s.bound;
+#pragma unroll 1
+  for (int g0 = 0; g0 < groups; g0 += 8) {
+    float m[8];
+#pragma unroll
+    for (int g = 0; g < 8; ++g) m[g] = g0 + g < groups ? gmax[(g0 + g) * TPB + threadIdx.x] : -INFINITY;
+    unsigned hit = 0;
+#pragma unroll
+    for (int g = 0; g < 8; ++g) hit |= g0 + g < groups && (above ? m[g] > B : m[g] >= B) ? 1u << g : 0u;
+    if (hit == 0) continue;
+    int i = atomicAdd(&s.n_group, __popc(hit));
+    for (; hit; hit &= hit - 1, ++i)
+      if (i < GROUP_LIST) s.group[i] = uint16_t((g0 + __ffs(int(hit)) - 1) * TPB + threadIdx.x);
+  }
+}
+
+// Rows with crowds: many groups at the bound itself (few distinct values; fewer logits than k left by a mask), or large
+// logits crowded in the columns of few threads.  Not inlined: seldom run.
 template <typename X, int TPB>
-__device__ void best_of_part(const Part<X>& p, int k, const float* gmax, int groups, int steps, float mine, TopSmem& s) {
+__device__ __noinline__ void best_of_crowd(const Part<X>& p, int k, const float* gmax, int groups, int steps, float mine, TopSmem& s) {
   constexpr int WARPS = TPB / 32;
   const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
-  const float sorted = sort_warp(mine);
-  s.sorted[w][lane] = sorted;
-  if (threadIdx.x == 0) { s.n_key = 0; s.n_group = 0; s.n_above = 0; s.found = 0; }
-  if (threadIdx.x < MV_TOP_MAX) s.best[threadIdx.x] = 0;
-  __syncthreads();
-  if (w == 0) {
-    // If j warps hold r maxima >= b each, j r >= k of them reach b: lane r - 1 tries r, with the ceil(k / r)-th largest of the warps' r-th maxima.
-    float v[WARPS];
-#pragma unroll
-    for (int i = 0; i < WARPS; ++i) v[i] = s.sorted[i][lane];
-    const int j = (k + lane) / (lane + 1);
-    float b = -INFINITY;
-#pragma unroll
-    for (int i = 0; i < WARPS; ++i) {
-      int reach = 0;
-#pragma unroll
-      for (int m = 0; m < WARPS; ++m) reach += v[m] >= v[i];
-      if (reach >= j) b = fmaxf(b, v[i]);
-    }
-#pragma unroll
-    for (int o = 16; o; o >>= 1) b = fmaxf(b, __shfl_xor_sync(0xffffffffu, b, o));
-    if (lane == 0) s.bound = b;
-  }
-  __syncthreads();
   const float B = s.bound;
-  auto push = [&](float x, uint32_t col) {
-    const int i = atomicAdd(&s.n_key, 1);
-    if (i < KEY_LIST) s.key[i] = make_key(x, col);
-  };
-  if (mine >= B)
-    for (int g = 0; g < groups; ++g) {
-      const float m = gmax[g * TPB + threadIdx.x];
-      if (m > B) atomicAdd(&s.n_above, 1);
-      if (m >= B) {
-        const int i = atomicAdd(&s.n_group, 1);
-        if (i < GROUP_LIST) s.group[i] = uint16_t(g * TPB + threadIdx.x);
-      }
+  const X* x = reinterpret_cast<const X*>(p.vec);
+  const uint32_t n = uint32_t(p.nv) * Vec<X>::N;
+  auto ends = [&](auto&& f) {
+    if (threadIdx.x < p.head + p.tail) {
+      const uint32_t col = threadIdx.x < p.head ? threadIdx.x : p.tail_col + threadIdx.x - p.head;
+      f(to_f(p.row[col]), col);
     }
-  // the single logits at the ends are always candidates
-  if (threadIdx.x < p.head + p.tail) {
-    const uint32_t col = threadIdx.x < p.head ? threadIdx.x : p.tail_col + threadIdx.x - p.head;
-    const float x = to_f(p.row[col]);
-    if (x == x) push(x, col);
-  }
+  };
   __syncthreads();
-  const bool few = s.n_group <= GROUP_LIST;
-  const int per = steps * U;         // vectors per group
-  if (!few && s.n_above > 0) {       // many groups at the bound itself: list the ones above it
-    __syncthreads();
-    if (threadIdx.x == 0) s.n_group = 0;
-    __syncthreads();
-    if (mine > B)
-      for (int g = 0; g < groups; ++g)
-        if (gmax[g * TPB + threadIdx.x] > B) {
-          const int i = atomicAdd(&s.n_group, 1);
-          if (i < GROUP_LIST) s.group[i] = uint16_t(g * TPB + threadIdx.x);
-        }
-    __syncthreads();
-  }
-  const int listed = few || s.n_above > 0 ? min(s.n_group, GROUP_LIST) : 0;
-  for (int i = threadIdx.x; i < listed * per; i += TPB) {
-    const int gi = s.group[i / per], g = gi / TPB;
-    const int64_t v = int64_t(gi % TPB) + (int64_t(g) * per + i % per) * TPB;
-    if (v >= p.nv) continue;
-    const uint4 u = __ldg(p.vec + v);
-    const uint32_t col = p.col0 + uint32_t(v) * Vec<X>::N;
-    each_logit<X>(u, [&](int e, float x) {
-      if (few ? x >= B : x > B) push(x, col + e);
-    });
-  }
+  if (threadIdx.x == 0) { s.n_key = 0; s.n_group = 0; s.found = 0; }
   __syncthreads();
-  bool whole = s.n_above <= GROUP_LIST && s.n_key <= KEY_LIST;
-  if (whole && !few) {
+  ends([&](float v, uint32_t col) { if (v == v) push_key(s, v, col); });
+  if (mine > B) list_groups<TPB>(gmax, groups, true, s);
+  __syncthreads();
+  const int above = s.n_group;
+  gather_groups<X, TPB>(p, min(above, GROUP_LIST), steps, true, s);
+  __syncthreads();
+  bool whole = above <= GROUP_LIST && s.n_key <= KEY_LIST;
+  if (whole) {
     // the logits at the bound, in order from the start of the part until k of them are found (they are many)
-    for (int64_t v0 = 0; v0 < p.nv; v0 += TPB) {
-      const int64_t v = v0 + threadIdx.x;
+#pragma unroll 1
+    for (uint32_t c0 = 0; c0 < n; c0 += TPB * 8) {
+      const uint32_t c1 = c0 + threadIdx.x * 8;
       unsigned hit = 0;
-      if (v < p.nv) {
-        const uint4 u = __ldg(p.vec + v);
-        each_logit<X>(u, [&](int e, float x) { hit |= x == B ? 1u << e : 0u; });
-      }
-      int c = __popc(hit), incl = c;
+      for (uint32_t e = 0; e < 8; ++e)
+        if (c1 + e < n && to_f(x[c1 + e]) == B) hit |= 1u << e;
+      int incl = __popc(hit);
       for (int o = 1; o < 32; o <<= 1) {
         const int z = __shfl_up_sync(0xffffffffu, incl, o);
         if (lane >= o) incl += z;
       }
       if (lane == 31) s.sorted[w][0] = __int_as_float(incl);
       __syncthreads();
-      int at = s.found + incl - c, all = s.found;
+      int at = s.found + incl - __popc(hit), all = s.found;
       for (int i = 0; i < WARPS; ++i) {
-        const int n = __float_as_int(s.sorted[i][0]);
-        at += i < w ? n : 0;
-        all += n;
+        const int c = __float_as_int(s.sorted[i][0]);
+        at += i < w ? c : 0;
+        all += c;
       }
-      for (int e = 0; e < Vec<X>::N; ++e)
-        if ((hit >> e & 1u) && at++ < k) push(B, p.col0 + uint32_t(v) * Vec<X>::N + e);
+      for (uint32_t e = 0; e < 8; ++e)
+        if ((hit >> e & 1u) && at++ < k) push_key(s, B, p.col0 + c1 + e);
       __syncthreads();
       if (threadIdx.x == 0) s.found = all;
       __syncthreads();
@@ -280,31 +275,19 @@ __device__ void best_of_part(const Part<X>& p, int k, const float* gmax, int gro
     whole = s.n_key <= KEY_LIST;
   }
   if (whole) {
-    // every candidate's place is the number of candidates before it
-    const int n = s.n_key;
-    for (int i = threadIdx.x; i < n; i += TPB) {
-      const unsigned long long mykey = s.key[i];
-      int place = 0;
-      for (int j = 0; j < n; ++j) place += s.key[j] > mykey;
-      if (place < k) s.best[place] = mykey;
-    }
+    rank_keys<TPB>(s, s.n_key, k);
   } else {
-    // too many candidates (large logits crowded in few threads' columns): one reading of the part per alternative
+    // one reading of the part per alternative
     unsigned long long last = ~0ull;
+#pragma unroll 1
     for (int r = 0; r < k; ++r) {
       unsigned long long b = 0;
-      auto take = [&](float x, uint32_t col) {
-        const unsigned long long y = x == x ? make_key(x, col) : 0;
+      auto take = [&](float v, uint32_t col) {
+        const unsigned long long y = v == v ? make_key(v, col) : 0;
         if (y < last && y > b) b = y;
       };
-      for (int64_t v = threadIdx.x; v < p.nv; v += TPB) {
-        const uint4 u = __ldg(p.vec + v);
-        each_logit<X>(u, [&](int e, float x) { take(x, p.col0 + uint32_t(v) * Vec<X>::N + e); });
-      }
-      if (threadIdx.x < p.head + p.tail) {
-        const uint32_t col = threadIdx.x < p.head ? threadIdx.x : p.tail_col + threadIdx.x - p.head;
-        take(to_f(p.row[col]), col);
-      }
+      for (uint32_t c = threadIdx.x; c < n; c += TPB) take(to_f(x[c]), p.col0 + c);
+      ends(take);
       for (int o = 16; o; o >>= 1) {
         const unsigned long long y = __shfl_xor_sync(0xffffffffu, b, o);
         if (y > b) b = y;
@@ -319,6 +302,51 @@ __device__ void best_of_part(const Part<X>& p, int k, const float* gmax, int gro
       last = b;
     }
   }
+}
+
+// The k best keys of this part, in order, in s.best (0 where there are fewer).  All threads; ends with a barrier.  The
+// code is kept short: it runs once per row, and with one wave of rows its instructions come from memory.
+template <typename X, int TPB>
+__device__ __forceinline__ void best_of_part(const Part<X>& p, int k, const float* gmax, int groups, int steps, float mine, TopSmem& s) {
+  constexpr int WARPS = TPB / 32;
+  const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
+  s.sorted[w][lane] = sort_warp(mine);
+  if (threadIdx.x == 0) { s.n_key = 0; s.n_group = 0; }
+  if (threadIdx.x < MV_TOP_MAX) s.best[threadIdx.x] = 0;
+  __syncthreads();
+  // the single logits at the ends are always candidates
+  if (threadIdx.x < p.head + p.tail) {
+    const uint32_t col = threadIdx.x < p.head ? threadIdx.x : p.tail_col + threadIdx.x - p.head;
+    const float x = to_f(p.row[col]);
+    if (x == x) push_key(s, x, col);
+  }
+  if (w == 0) {
+    // If j warps hold r maxima >= b each, j r >= k of them reach b: lane r - 1 tries r, with the ceil(k / r)-th largest of the warps' r-th maxima.
+    float v[WARPS], b = -INFINITY;
+#pragma unroll
+    for (int i = 0; i < WARPS; ++i) v[i] = s.sorted[i][lane];
+    const int j = (k + lane) / (lane + 1);
+#pragma unroll 1
+    for (int i = 0; i < WARPS; ++i) {
+      const float vi = s.sorted[i][lane];
+      int reach = 0;
+#pragma unroll
+      for (int m = 0; m < WARPS; ++m) reach += v[m] >= vi;
+      if (reach >= j) b = fmaxf(b, vi);
+    }
+#pragma unroll
+    for (int o = 16; o; o >>= 1) b = fmaxf(b, __shfl_xor_sync(0xffffffffu, b, o));
+    if (lane == 0) s.bound = b;
+  }
+  __syncthreads();
+  if (mine >= s.bound) list_groups<TPB>(gmax, groups, false, s);
+  __syncthreads();
+  const int listed = s.n_group;
+  if (listed <= GROUP_LIST) gather_groups<X, TPB>(p, listed, steps, false, s);
+  __syncthreads();
+  const int n = s.n_key;
+  if (listed <= GROUP_LIST && n <= KEY_LIST) rank_keys<TPB>(s, n, k);
+  else best_of_crowd<X, TPB>(p, k, gmax, groups, steps, mine, s);
   __syncthreads();
 }
 
@@ -526,13 +554,7 @@ __global__ void __launch_bounds__(TPB, 1024 / TPB) k_token_logprob(const X* __re
         __syncthreads();
         if (threadIdx.x < MV_TOP_MAX) s_top[0].best[threadIdx.x] = 0;
         __syncthreads();
-        for (int i = threadIdx.x; i < ctas * a.k; i += TPB) {
-          const unsigned long long mykey = s_top[0].key[i];
-          if (mykey == 0) continue;
-          int place = 0;
-          for (int j = 0; j < ctas * a.k; ++j) place += s_top[0].key[j] > mykey;
-          if (place < a.k) s_top[0].best[place] = mykey;
-        }
+        rank_keys<TPB>(s_top[0], ctas * a.k, a.k);
         __syncthreads();
       }
     }
@@ -554,31 +576,106 @@ __global__ void __launch_bounds__(TPB, 1024 / TPB) k_token_logprob(const X* __re
   }
 }
 
-constexpr int GRAD_TPB = 256;
+// ------------------------------------------------------------------------------------------ gradient
+// dx = c (g1 (1[v = y] - p) - g2 p (log p + H)), log p = c x - lse: with w = log2 p, p = 2^w and
+// dx = -p (c g2 ln 2 w + c (g1 + g2 H)) + c g1 1[v = y]: a multiplication, an addition and an exponential per logit, then one
+// or two more.  Each CTA takes one stretch of one row, so that the stretches, in the order of memory, go to the
+// multiprocessors as they become free.
+constexpr int GRAD_TPB = 256, GRAD_U = 4;
 
-template <typename X>
-__global__ void __launch_bounds__(GRAD_TPB) k_token_grad(const X* logits, int64_t V, int64_t ld, const void* __restrict__ targets, int id_type, float scale,
-                                                     const float* __restrict__ lse, const float* __restrict__ entropy, const float* __restrict__ g_logprob,
-                                                     const float* __restrict__ g_entropy, X* dlogits, int64_t ldg) {
-  const int64_t t = blockIdx.x;
-  const X* x = logits + t * ld;
-  X* dx = dlogits + t * ldg;
-  const int64_t y = targets ? load_id(targets, id_type, t, V) : -1;
-  const float l = lse[t];
-  const float g1 = y >= 0 && g_logprob ? g_logprob[t] : 0.0f;
-  const float g2 = g_entropy ? g_entropy[t] : 0.0f;
+struct GradArgs {
+  int64_t V, ld, ldg;
+  const void* targets;
+  int id_type;
+  float scale;
+  unsigned stretches;                // CTAs per row
+  const float *lse, *entropy, *g_logprob, *g_entropy;
+};
+
+template <typename X> __device__ __forceinline__ uint32_t narrow2(float a, float b);
+template <> __device__ __forceinline__ uint32_t narrow2<__nv_bfloat16>(float a, float b) {
+  const __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
+  uint32_t r;
+  memcpy(&r, &h, 4);
+  return r;
+}
+template <> __device__ __forceinline__ uint32_t narrow2<__half>(float a, float b) {
+  const __half2 h = __floats2half2_rn(a, b);
+  uint32_t r;
+  memcpy(&r, &h, 4);
+  return r;
+}
+
+template <typename X> __device__ __forceinline__ uint4 pack_vec(const float (&d)[Vec<X>::N]) {
+  if constexpr (sizeof(X) == 4) return make_uint4(__float_as_uint(d[0]), __float_as_uint(d[1]), __float_as_uint(d[2]), __float_as_uint(d[3]));
+  else return make_uint4(narrow2<X>(d[0], d[1]), narrow2<X>(d[2], d[3]), narrow2<X>(d[4], d[5]), narrow2<X>(d[6], d[7]));
+}
+
+// VEC: logits and gradient start at the same place within 16 bytes in every row.
+template <typename X, bool VEC>
+__global__ void __launch_bounds__(GRAD_TPB) k_token_grad(const X* logits, X* dlogits, const __grid_constant__ GradArgs a) {
+  constexpr int N = Vec<X>::N;
+  const int64_t t = blockIdx.x / a.stretches;
+  const unsigned stretch = blockIdx.x % a.stretches;
+  const X* x = logits + t * a.ld;
+  X* dx = dlogits + t * a.ldg;
+  const int64_t y = a.targets ? load_id(a.targets, a.id_type, t, a.V) : -1;
+  const float l = a.lse[t];
+  const float g1 = y >= 0 && a.g_logprob ? a.g_logprob[t] : 0.0f;
+  const float g2 = a.g_entropy ? a.g_entropy[t] : 0.0f;
   const bool none = (g1 == 0.0f && g2 == 0.0f) || l == -INFINITY;
-  const float a = g1 + (g2 == 0.0f ? 0.0f : g2 * entropy[t]);
-  for (int64_t j = threadIdx.x; j < V; j += GRAD_TPB) {
-    float d = 0.0f;
-    if (!none) {
-      const float lp = max_nan(fmaf(to_f(x[j]), scale, -l), T_FLOOR);
-      const float p = exp2f(lp * LOG2E);
-      d = -p * fmaf(g2, lp, a);
-      if (j == y) d += g1;
-      d *= scale;
+  const float sum = g1 + (g2 == 0.0f ? 0.0f : g2 * a.entropy[t]);
+  auto one = [&](float v, int64_t col) {
+    if (none) return 0.0f;
+    const float lp = max_nan(fmaf(v, a.scale, -l), T_FLOOR);
+    float d = -exp2f(lp * LOG2E) * fmaf(g2, lp, sum);
+    if (col == y) d += g1;
+    return d * a.scale;
+  };
+  // the vectors begin at the row's first 16-byte boundary; what is before and behind them goes to the first stretch
+  const int64_t first = VEC ? min(a.V, int64_t((16 - (reinterpret_cast<uintptr_t>(x) & 15)) & 15) / int(sizeof(X))) : 0;
+  const int64_t nv = VEC ? (a.V - first) / N : 0;
+  if (VEC && stretch == 0) {
+    const int64_t behind = first + nv * N;
+    if (threadIdx.x < first + a.V - behind) {
+      const int64_t col = threadIdx.x < first ? threadIdx.x : behind + threadIdx.x - first;
+      dx[col] = from_f<X>(one(to_f(x[col]), col));
     }
-    dx[j] = from_f<X>(d);
+  }
+  if constexpr (VEC) {
+    const int64_t v0 = int64_t(stretch) * GRAD_TPB * GRAD_U + threadIdx.x;
+    const uint4* in = reinterpret_cast<const uint4*>(x + first);
+    uint4* out = reinterpret_cast<uint4*>(dx + first);
+    if (none) {
+#pragma unroll
+      for (int i = 0; i < GRAD_U; ++i)
+        if (v0 + i * GRAD_TPB < nv) __stcs(out + v0 + i * GRAD_TPB, make_uint4(0, 0, 0, 0));
+      return;
+    }
+    uint4 u[GRAD_U];
+#pragma unroll
+    for (int i = 0; i < GRAD_U; ++i)
+      if (v0 + i * GRAD_TPB < nv) u[i] = __ldcs(in + v0 + i * GRAD_TPB);
+#pragma unroll
+    for (int i = 0; i < GRAD_U; ++i) {
+      const int64_t v = v0 + i * GRAD_TPB;
+      if (v >= nv) break;
+      float d[N];
+      each_logit<X>(u[i], [&](int e, float z) {
+        const float lp = max_nan(fmaf(z, a.scale, -l), T_FLOOR);
+        d[e] = -exp2f(lp * LOG2E) * fmaf(g2, lp, sum) * a.scale;
+      });
+      const int64_t hot = y - first - v * N;
+      if (hot >= 0 && hot < N) {     // the target's term belongs inside the sum that is rounded
+#pragma unroll
+        for (int e = 0; e < N; ++e)
+          if (e == hot) d[e] = one(to_f(x[first + v * N + e]), y);
+      }
+      __stcs(out + v, pack_vec<X>(d));
+    }
+  } else {
+    const int64_t c0 = int64_t(stretch) * GRAD_TPB * GRAD_U * N, c1 = min(a.V, c0 + GRAD_TPB * GRAD_U * N);
+    for (int64_t c = c0 + threadIdx.x; c < c1; c += GRAD_TPB) dx[c] = from_f<X>(one(to_f(x[c]), c));
   }
 }
 
@@ -603,11 +700,13 @@ int mv_token_logprob(void* stream, const void* logits, int type, int64_t T, int6
   return with_type(type, [&](auto x) {
     using X = decltype(x);
     const int64_t vecs = V / Vec<X>::N;
-    // Many rows: small CTAs, whose ends overlap with the others' streaming.  Fewer rows than multiprocessors: large CTAs, and as many per row
-    // (up to the eight of a portable cluster) as keep a whole step for each thread and fit the device at once.
-    const int tpb = T < 148 ? 512 : 128;
+    // Many rows: small CTAs, whose ends overlap with the others' streaming (8192 x 65536 bf16, k = 16: 195 us, with 256 threads 222).
+    // Rows for less than two waves of those: 256 threads (1003 x 50021 fp32: 47 us, with 128 threads 49).  Fewer rows than
+    // multiprocessors: 512 threads, and as many CTAs per row (up to the eight of a portable cluster) as keep a whole step for
+    // each thread and fit the device at once; with more rows than that, clusters only cost (two CTAs per row: 246 us).
+    const int tpb = T < 148 ? 512 : T < 148 * 16 ? 256 : 128;
     int ctas = 1;
-    while (ctas < 8 && T * ctas * tpb < 148 * 1024 && vecs >= int64_t(ctas) * 2 * tpb * U) ctas *= 2;
+    while (T < 148 && ctas < 8 && T * ctas * tpb < 148 * 1024 && vecs >= int64_t(ctas) * 2 * tpb * U) ctas *= 2;
     const int64_t n_steps = ((vecs + ctas - 1) / ctas + tpb * U - 1) / (tpb * U);
     a.steps = int((n_steps + MAX_GROUPS - 1) / MAX_GROUPS);
     if (a.steps < 1) a.steps = 1;
@@ -624,6 +723,7 @@ int mv_token_logprob(void* stream, const void* logits, int type, int64_t T, int6
     cfg.attrs = &attr;
     cfg.numAttrs = 1;
     auto* kernel = tpb == 128 ? (k ? k_token_logprob<X, true, 128> : k_token_logprob<X, false, 128>)
+                 : tpb == 256 ? (k ? k_token_logprob<X, true, 256> : k_token_logprob<X, false, 256>)
                               : (k ? k_token_logprob<X, true, 512> : k_token_logprob<X, false, 512>);
     if (cfg.dynamicSmemBytes > 32 << 10 && cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 64 << 10) != cudaSuccess) {
       cudaGetLastError();
@@ -652,8 +752,17 @@ int mv_token_logprob_grad(void* stream, const void* logits, int type, int64_t T,
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   return with_type(type, [&](auto x) {
     using X = decltype(x);
-    k_token_grad<X><<<unsigned(T), GRAD_TPB, 0, st>>>(static_cast<const X*>(logits), V, ld, targets, id_type, scale, lse, entropy, g_logprob, g_entropy,
-                                                  static_cast<X*>(dlogits), ldg);
+    GradArgs g;
+    g.V = V; g.ld = ld; g.ldg = ldg; g.targets = targets; g.id_type = id_type; g.scale = scale;
+    g.lse = lse; g.entropy = entropy; g.g_logprob = g_logprob; g.g_entropy = g_entropy;
+    const int64_t per = int64_t(GRAD_TPB) * GRAD_U * Vec<X>::N, stretches = (V + per - 1) / per;
+    if (T * stretches >= lim) return int(MV_ERR_INVALID_ARG);
+    g.stretches = unsigned(stretches);
+    // a gradient that lies otherwise within 16 bytes than the logits, in some row, is written one by one
+    const bool vec = ((reinterpret_cast<uintptr_t>(logits) ^ reinterpret_cast<uintptr_t>(dlogits)) & 15) == 0 &&
+                     (T == 1 || (ld - ldg) * int64_t(sizeof(X)) % 16 == 0);
+    auto* kernel = vec ? k_token_grad<X, true> : k_token_grad<X, false>;
+    kernel<<<unsigned(T * stretches), GRAD_TPB, 0, st>>>(static_cast<const X*>(logits), static_cast<X*>(dlogits), g);
     return cuda_ok();
   });
 }

@@ -43,6 +43,11 @@ __device__ __forceinline__ f2 add2(f2 a, f2 b) {
   asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
   return r;
 }
+__device__ __forceinline__ f2 mul2(f2 a, f2 b) {
+  f2 r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
 __device__ __forceinline__ f2 fma2(f2 a, f2 b, f2 c) {
   f2 r;
   asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
@@ -67,6 +72,11 @@ template <> struct Vec<__nv_bfloat16> {
   __device__ static uint32_t max2(uint32_t a, uint32_t b) {
     uint32_t r;
     asm("max.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+    return r;
+  }
+  __device__ static uint32_t max2_nan(uint32_t a, uint32_t b) {
+    uint32_t r;
+    asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
     return r;
   }
   __device__ static float widen(uint32_t m) { return fmaxf(__uint_as_float(m << 16), __uint_as_float(m & 0xffff0000u)); }
@@ -440,7 +450,12 @@ __global__ void __launch_bounds__(TPB, 1024 / TPB) k_token_logprob(const X* __re
   };
   const float c2 = a.scale * LOG2E, room = 40.0f / c2;      // a larger logit changes the reference only if it exceeds it by 2^40
   const f2 c22 = pack2(c2, c2);
-  float ref = -INFINITY, R = 0.0f, limit = -R_MAX / c2;     // logits below that never set the reference
+  float ref = -INFINITY, R = 0.0f, limit = -R_MAX / fmaxf(c2, 0.1f);      // logits below that never set the reference
+  // bf16 has the range of 32 bits: two logits at a time are kept above a floor so far below the limit that 2^t is 0 there,
+  // and so near that t is finite; for the other types t itself is kept above T_FLOOR
+  constexpr bool FLOOR2 = sizeof(X) == 2 && Vec<X>::NONE == 0xff80ff80u;
+  uint32_t floor2 = 0;
+  if constexpr (FLOOR2) floor2 = (__float_as_uint(-3.0e38f / fmaxf(c2, 1.0f)) >> 16) * 0x10001u;
   f2 minus = pack2(0.0f, 0.0f), s2 = pack2(0.0f, 0.0f), st2 = s2;
   auto raise = [&](float m) {        // a new reference
     const float Rm = m * c2;
@@ -463,7 +478,8 @@ __global__ void __launch_bounds__(TPB, 1024 / TPB) k_token_logprob(const X* __re
     unpack2(fma2(v, c22, minus), u0, u1);
     const f2 e = pack2(exp2_fast(u0), exp2_fast(u1));
     s2 = add2(s2, e);
-    st2 = fma2(e, pack2(max_nan(u0, T_FLOOR), max_nan(u1, T_FLOOR)), st2);
+    if constexpr (!FLOOR2) st2 = fma2(e, pack2(max_nan(u0, T_FLOOR), max_nan(u1, T_FLOOR)), st2);
+    else st2 = fma2(e, pack2(u0, u1), st2);
   };
   float gm = -INFINITY, mine = -INFINITY, extra = -INFINITY;
   int left = a.steps, group = 0;
@@ -483,16 +499,19 @@ __global__ void __launch_bounds__(TPB, 1024 / TPB) k_token_logprob(const X* __re
       }
     }
 #pragma unroll
-    for (int i = 0; i < U; ++i)
+    for (int i = 0; i < U; ++i) {
+      uint4 v = u[i];
+      if constexpr (FLOOR2) v = make_uint4(Vec<X>::max2_nan(v.x, floor2), Vec<X>::max2_nan(v.y, floor2), Vec<X>::max2_nan(v.z, floor2), Vec<X>::max2_nan(v.w, floor2));
 #pragma unroll
-      for (int j = 0; j < N / 2; ++j) add_pair(Vec<X>::pair(u[i], j));
+      for (int j = 0; j < N / 2; ++j) add_pair(Vec<X>::pair(v, j));
+    }
   };
   uint4 even[U], odd[U];
   if (n_steps > 0) load(0, even);
   if (threadIdx.x < p.head + p.tail) {
     extra = to_f(p.row[threadIdx.x < p.head ? threadIdx.x : p.tail_col + threadIdx.x - p.head]);
     if (extra > limit) raise(extra);
-    add_pair(pack2(extra, -INFINITY));
+    add_pair(pack2(FLOOR2 ? max_nan(extra, __uint_as_float(floor2 << 16)) : extra, __uint_as_float(FLOOR2 ? floor2 << 16 : 0xff800000u)));
   }
   for (int step = 0; step < n_steps; step += 2) {
     if (step + 1 < n_steps) load(step + 1, odd);
@@ -577,11 +596,12 @@ __global__ void __launch_bounds__(TPB, 1024 / TPB) k_token_logprob(const X* __re
 }
 
 // ------------------------------------------------------------------------------------------ gradient
-// dx = c (g1 (1[v = y] - p) - g2 p (log p + H)), log p = c x - lse: with w = log2 p, p = 2^w and
-// dx = -p (c g2 ln 2 w + c (g1 + g2 H)) + c g1 1[v = y]: a multiplication, an addition and an exponential per logit, then one
-// or two more.  Each CTA takes one stretch of one row, so that the stretches, in the order of memory, go to the
-// multiprocessors as they become free.
+// dx = c (g1 (1[v = y] - p) - g2 p (log p + H)), log p = c x - lse.  With h = log2(p) / 2 and q = 2^h:
+// dx = q (q (A h + B)) + c g1 1[v = y], A = -2 ln 2 c g2, B = -c (g1 + g2 H): two fused multiply-adds, an exponential and two
+// products per logit.  p is formed as q q because the hardware's exponential has no subnormal results.  Each CTA takes
+// one stretch of one row, so that the stretches, in the order of memory, go to the multiprocessors as they become free.
 constexpr int GRAD_TPB = 256, GRAD_U = 4;
+constexpr float H_FLOOR = -1.0e4f;
 
 struct GradArgs {
   int64_t V, ld, ldg;
@@ -637,8 +657,8 @@ __global__ void __launch_bounds__(GRAD_TPB) k_token_grad(const X* logits, X* dlo
   const int64_t nv = VEC ? (a.V - first) / N : 0;
   if (VEC && stretch == 0) {
     const int64_t behind = first + nv * N;
-    if (threadIdx.x < first + a.V - behind) {
-      const int64_t col = threadIdx.x < first ? threadIdx.x : behind + threadIdx.x - first;
+    if (int64_t(threadIdx.x) < first + a.V - behind) {
+      const int64_t col = int64_t(threadIdx.x) < first ? int64_t(threadIdx.x) : behind + threadIdx.x - first;
       dx[col] = from_f<X>(one(to_f(x[col]), col));
     }
   }
@@ -652,6 +672,9 @@ __global__ void __launch_bounds__(GRAD_TPB) k_token_grad(const X* logits, X* dlo
         if (v0 + i * GRAD_TPB < nv) __stcs(out + v0 + i * GRAD_TPB, make_uint4(0, 0, 0, 0));
       return;
     }
+    const float c2 = a.scale * LOG2E * 0.5f, l2 = l * LOG2E * 0.5f;
+    const float A = -2.0f * LN2 * a.scale * g2, B = -a.scale * sum;
+    const f2 c22 = pack2(c2, c2), minus = pack2(-l2, -l2), A2 = pack2(A, A), B2 = pack2(B, B);
     uint4 u[GRAD_U];
 #pragma unroll
     for (int i = 0; i < GRAD_U; ++i)
@@ -661,10 +684,15 @@ __global__ void __launch_bounds__(GRAD_TPB) k_token_grad(const X* logits, X* dlo
       const int64_t v = v0 + i * GRAD_TPB;
       if (v >= nv) break;
       float d[N];
-      each_logit<X>(u[i], [&](int e, float z) {
-        const float lp = max_nan(fmaf(z, a.scale, -l), T_FLOOR);
-        d[e] = -exp2f(lp * LOG2E) * fmaf(g2, lp, sum) * a.scale;
-      });
+#pragma unroll
+      for (int j = 0; j < N / 2; ++j) {
+        float h0, h1;
+        unpack2(fma2(Vec<X>::pair(u[i], j), c22, minus), h0, h1);
+        h0 = max_nan(h0, H_FLOOR);
+        h1 = max_nan(h1, H_FLOOR);
+        const f2 q = pack2(exp2_fast(h0), exp2_fast(h1));
+        unpack2(mul2(q, mul2(q, fma2(pack2(h0, h1), A2, B2))), d[2 * j], d[2 * j + 1]);
+      }
       const int64_t hot = y - first - v * N;
       if (hot >= 0 && hot < N) {     // the target's term belongs inside the sum that is rounded
 #pragma unroll

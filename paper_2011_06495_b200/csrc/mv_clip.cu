@@ -6,12 +6,16 @@
 
 namespace {
 
-// The list is cut into chunks, one CTA each.  A group's factor is known only when all its chunks have been summed, so every
-// element is read twice; to read it from memory only once, the list is worked off in stages of whole groups that fit L2: one
-// launch scales stage s and sums stage s + 1, mixing the reads of the one with the writes of the other.
+// The list is cut into chunks.  A group's factor is known only when all its chunks have been summed, so every element is
+// read twice; to read it from memory only once, the list is worked off in stages of whole groups that fit L2.  One kernel does
+// all of it, one CTA per item (sum this chunk, scale that chunk), in the order: the sums of stage 0, then the scalings
+// of stage s mixed with the sums of stage s + 1.  CTAs take their items by a counter, so an item's predecessors are with CTAs
+// that run or have run; an item that scales waits for its group's factor, and the sums that it waits for wait for nothing.
 constexpr int TPB = 256;
-constexpr int CHUNK = 8192;          // elements per chunk: 16 or 32 KB
+constexpr int CHUNK = 8192;          // elements per chunk: 16 or 32 KB, all on their way at once, six chunks a multiprocessor
 constexpr int64_t STAGE = int64_t(40) << 20;      // bytes of a stage, or one group
+constexpr int LEAD = 148 * 6;        // sums of the next stage taken before the first scaling: its factors are there by then
+constexpr int SPIN_LIMIT = 1 << 22;  // polls of a factor (a second or more) before an item is given up
 
 struct Chunk {
   void* ptr;                         // first element
@@ -19,10 +23,10 @@ struct Chunk {
   int32_t n;
   int32_t type;
   int32_t group;
-  int32_t pad;
+  int32_t what;                      // 2 x the chunk's number; + 1: to be scaled
 };
 
-struct Layout { size_t chunks, first, partial, ticket, coef, total; int64_t n; };
+struct Layout { size_t sums, items, first, ticket, done, taken, partial, total; int64_t n; };
 
 inline bool clip_layout(const int64_t* numel, int n_tensors, int n_groups, Layout* L) {
   if (n_tensors < 0 || (n_tensors > 0 && !numel) || n_groups < 1 || n_groups >= (1 << 20)) return false;
@@ -33,27 +37,31 @@ inline bool clip_layout(const int64_t* numel, int n_tensors, int n_groups, Layou
   }
   if (L->n >= (int64_t(1) << 30)) return false;
   size_t o = 0;
-  L->chunks = o;  o = align_up(o + size_t(L->n) * sizeof(Chunk), 256);
+  L->sums = o;    o = align_up(o + size_t(L->n + 1) * sizeof(Chunk), 256);      // (an empty one more, for a list without elements)
+  L->items = o;   o = align_up(o + size_t(L->n + 1) * 2 * sizeof(Chunk), 256);
   L->first = o;   o = align_up(o + size_t(n_groups + 1) * 4, 256);
-  L->ticket = o;  o = align_up(o + size_t(n_groups) * 4, 256);      // what the host fills ends here
+  L->ticket = o;  o = align_up(o + size_t(n_groups) * 4, 256);
+  L->done = o;    o = align_up(o + size_t(n_groups) * 8, 256);
+  L->taken = o;   o += 256;          // what the host fills ends here
   L->partial = o; o = align_up(o + size_t(L->n) * 8, 256);
-  L->coef = o;    o = align_up(o + size_t(n_groups) * 4, 256);
   L->total = o;
   return true;
 }
 
 struct ClipArgs {
-  const Chunk* chunks;
+  const Chunk* items;
+  unsigned long long* taken;         // items taken so far, by all calls of this kind
   const int32_t* first;              // [groups + 1] first chunk of each group
   uint32_t* ticket;                  // [groups] chunks summed so far; back to 0 with the last one
+  unsigned long long* done;          // [groups] number of the scaling call (from 1) and the factor's bits, once it is known
   double* partial;
-  float *coef, *norms;
+  float* norms;
   float max_norm;
   float* rows;                       // pack: the rows; null: in place
   int64_t ld;
   int n_groups;
-  int apply0, n_apply, sum0, n_sum;  // chunks to scale and chunks to sum in this launch
-  int empty;                         // the first launch also deals with groups that have no chunk
+  int empty;                         // some group has no chunk
+  int scales;                        // 0: a call for the norms alone
 };
 
 // 16 bytes of a chunk as numbers.
@@ -70,158 +78,158 @@ template <typename X> __device__ __forceinline__ int head_of(const X* x, int n) 
   return min(n, int((16 - (reinterpret_cast<uintptr_t>(x) & 15)) & 15) / int(sizeof(X)));
 }
 
-// Sum of squares of a chunk, this thread's part.  64 bits: a square of 32 bits has no room below 1e-19 or above 1e19.
-template <typename X> __device__ double chunk_sum(const X* x, int n) {
-  constexpr int V = CHUNK / PER<X> / TPB;           // vectors per thread, all on their way at once
-  const int head = head_of(x, n), nv = (n - head) / PER<X>, tail = head + nv * PER<X>;
-  const uint4* p = reinterpret_cast<const uint4*>(x + head);
-  uint4 u[V];
+// The chunk's whole vectors on their way to shared memory, vector i * TPB + thread at that place.
+template <typename X> __device__ __forceinline__ void fetch(const X* x, int nv, uint4* buf) {
+  constexpr int V = CHUNK / PER<X> / TPB;
+  const uint4* p = reinterpret_cast<const uint4*>(x) + threadIdx.x;
+  const uint32_t to = uint32_t(__cvta_generic_to_shared(buf + threadIdx.x));
 #pragma unroll
-  for (int i = 0; i < V; ++i) u[i] = i * TPB + int(threadIdx.x) < nv ? __ldg(p + i * TPB + threadIdx.x) : make_uint4(0, 0, 0, 0);
+  for (int i = 0; i < V; ++i)
+    if (i * TPB + int(threadIdx.x) < nv)
+      asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to + i * TPB * 16), "l"(p + i * TPB) : "memory");
+}
+
+// Sum of squares of a chunk, this thread's part.  64 bits: a square of 32 bits has no room below 1e-19 or above 1e19.
+template <typename X> __device__ __forceinline__ double chunk_sum(const X* x, int n, uint4* buf) {
+  constexpr int V = CHUNK / PER<X> / TPB;
+  const int head = head_of(x, n), nv = (n - head) / PER<X>, tail = head + nv * PER<X>, tid = threadIdx.x;
+  fetch(x + head, nv, buf);
   double s = 0.0;
-  if (int(threadIdx.x) < head + n - tail) {
-    const double v = to_f(x[int(threadIdx.x) < head ? int(threadIdx.x) : tail + int(threadIdx.x) - head]);
+  if (tid < head + n - tail) {
+    const double v = to_f(x[tid < head ? tid : tail + tid - head]);
     s = v * v;
   }
-#pragma unroll
+  asm volatile("cp.async.wait_all;" ::: "memory");
+#pragma unroll 2
   for (int i = 0; i < V; ++i) {
+    if (i * TPB + tid >= nv) break;
     float f[PER<X>];
-    widen<X>(u[i], f);
+    widen<X>(buf[i * TPB + tid], f);
 #pragma unroll
     for (int j = 0; j < PER<X>; ++j) { const double v = f[j]; s = fma(v, v, s); }
   }
   return s;
 }
 
-__device__ double block_sum(double x, double* sh) {
-  for (int o = 16; o; o >>= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
-  __syncthreads();
-  if ((threadIdx.x & 31) == 0) sh[threadIdx.x >> 5] = x;
-  __syncthreads();
-  x = sh[0];
-  for (int i = 1; i < TPB / 32; ++i) x += sh[i];
-  return x;
-}
-
-__device__ __forceinline__ void put_norm(const ClipArgs& a, int g, double s) {
+// The norm and the factor of a group from its sum of squares.
+__device__ __forceinline__ void put_norm(const ClipArgs& a, int g, double s, uint32_t call) {
   const double n = sqrt(s);
   if (a.norms) a.norms[g] = float(n);
-  a.coef[g] = n > double(a.max_norm) && !isinf(n) ? float(double(a.max_norm) / n) : 1.0f;
+  const float f = n > double(a.max_norm) && !isinf(n) ? float(double(a.max_norm) / n) : 1.0f;
+  const unsigned long long w = (unsigned long long)call << 32 | __float_as_uint(f);
+  asm volatile("st.release.gpu.u64 [%0], %1;" ::"l"(a.done + g), "l"(w) : "memory");
 }
 
-__device__ void sum_chunk(const ClipArgs& a, int i) {
-  __shared__ double sh[TPB / 32];
-  __shared__ int s_last;
-  const Chunk c = a.chunks[i];
-  double s = c.type == MV_F32 ? chunk_sum(static_cast<const float*>(c.ptr), c.n)
-           : c.type == MV_BF16 ? chunk_sum(static_cast<const __nv_bfloat16*>(c.ptr), c.n)
-                               : chunk_sum(static_cast<const __half*>(c.ptr), c.n);
-  s = block_sum(s, sh);
-  const int c0 = a.first[c.group], c1 = a.first[c.group + 1];
-  if (threadIdx.x == 0) {
-    __stcg(a.partial + i, s);
+// The first warp: a chunk's sum goes to its place, and the CTA that brings a group's last one adds them up, always in the
+// same order.
+__device__ __forceinline__ void finish_sum(const ClipArgs& a, const Chunk& c, double s, uint32_t call) {
+  const int lane = threadIdx.x, c0 = a.first[c.group], c1 = a.first[c.group + 1];
+  uint32_t arrived = 0;
+  if (lane == 0) {
+    __stcg(a.partial + (c.what >> 1), s);
     __threadfence();
-    s_last = atomicAdd(a.ticket + c.group, 1u) == uint32_t(c1 - c0 - 1);
+    arrived = atomicAdd(a.ticket + c.group, 1u);
   }
-  __syncthreads();
-  if (!s_last) return;
-  // the CTA that finishes the group adds its chunks up, always in the same order
+  if (__shfl_sync(0xffffffffu, arrived, 0) != uint32_t(c1 - c0 - 1)) return;
   __threadfence();
   s = 0.0;
-  for (int k = c0 + threadIdx.x; k < c1; k += TPB) s += __ldcg(a.partial + k);
-  s = block_sum(s, sh);
-  if (threadIdx.x == 0) {
-    put_norm(a, c.group, s);
+#pragma unroll 8
+  for (int k = c0 + lane; k < c1; k += 32) s += __ldcg(a.partial + k);
+  for (int o = 16; o; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+  if (lane == 0) {
     a.ticket[c.group] = 0;
+    put_norm(a, c.group, s, call);
   }
 }
 
-// Out of place, to 32 bits.  Source and destination lie alike within 16 bytes: groups of four elements; else one by one, which
-// still moves whole lines per warp.
-template <typename X> __device__ void chunk_pack(const X* x, int n, float c, float* dst) {
-  struct alignas(4 * sizeof(X)) Four { X v[4]; };
-  const int to16 = int((16 - (reinterpret_cast<uintptr_t>(dst) & 15)) & 15) / 4;
-  if ((reinterpret_cast<uintptr_t>(x + to16) & (sizeof(Four) - 1)) == 0) {
-    constexpr int V = CHUNK / 4 / TPB;
-    const int head = min(n, to16), nv = (n - head) / 4, tail = head + nv * 4;
-    const Four* p = reinterpret_cast<const Four*>(x + head);
-    float4* q = reinterpret_cast<float4*>(dst + head);
-    Four f[V];
-#pragma unroll
-    for (int i = 0; i < V; ++i)
-      if (i * TPB + int(threadIdx.x) < nv) f[i] = p[i * TPB + threadIdx.x];
-    if (int(threadIdx.x) < head + n - tail) {
-      const int e = int(threadIdx.x) < head ? int(threadIdx.x) : tail + int(threadIdx.x) - head;
-      dst[e] = to_f(x[e]) * c;
+// The group's factor, when it is there.  A NaN if it does not come in time (never expected): what the item writes is NaN.
+__device__ __forceinline__ float wait_factor(const ClipArgs& a, int g, uint32_t call) {
+  unsigned long long d = 0;
+  for (int i = 0; i < SPIN_LIMIT; ++i) {
+    asm volatile("ld.acquire.gpu.u64 %0, [%1];" : "=l"(d) : "l"(a.done + g) : "memory");
+    if (uint32_t(d >> 32) == call) return __uint_as_float(uint32_t(d));
+    __nanosleep(50);
+  }
+  return __int_as_float(0x7fffffff);
+}
+
+// A chunk times its group's factor: in place, or to 32 bits at dst.
+template <typename X> __device__ __forceinline__ void chunk_scale(const ClipArgs& a, X* x, int n, float* dst, int group, uint32_t call, uint4* buf) {
+  __shared__ float s_factor;
+  const int head = head_of(x, n), nv = (n - head) / PER<X>, tail = head + nv * PER<X>, tid = threadIdx.x;
+  fetch(x + head, nv, buf);
+  const bool single = tid < head + n - tail;
+  const int e = tid < head ? tid : tail + tid - head;
+  const float v = single ? to_f(x[e]) : 0.0f;
+  if (tid == TPB - 1) s_factor = wait_factor(a, group, call);
+  asm volatile("cp.async.wait_all;" ::: "memory");
+  __syncthreads();
+  const float c = s_factor;
+  if (dst) {
+    if (single) dst[e] = v * c;
+    dst += head;
+    const int m = nv * PER<X>;
+    if ((reinterpret_cast<uintptr_t>(dst) & 15) == 0) {
+      struct alignas(4 * sizeof(X)) Four { X v[4]; };
+      const Four* from = reinterpret_cast<const Four*>(buf);
+#pragma unroll 4
+      for (int i = tid; i < m / 4; i += TPB) {
+        const Four f = from[i];
+        __stcs(reinterpret_cast<float4*>(dst) + i, make_float4(to_f(f.v[0]) * c, to_f(f.v[1]) * c, to_f(f.v[2]) * c, to_f(f.v[3]) * c));
+      }
+    } else {                         // word by word, whole lines per warp
+      const X* from = reinterpret_cast<const X*>(buf);
+#pragma unroll 8
+      for (int i = tid; i < m; i += TPB) __stcs(dst + i, to_f(from[i]) * c);
     }
+  } else if (c != 1.0f) {
+    if (single) x[e] = from_f<X>(v * c);
+    uint4* p = reinterpret_cast<uint4*>(x + head);
+#pragma unroll 2
+    for (int i = tid; i < nv; i += TPB) {
+      float f[PER<X>];
+      X y[PER<X>];
+      widen<X>(buf[i], f);
 #pragma unroll
-    for (int i = 0; i < V; ++i)
-      if (i * TPB + int(threadIdx.x) < nv)
-        __stcs(q + i * TPB + threadIdx.x, make_float4(to_f(f[i].v[0]) * c, to_f(f[i].v[1]) * c, to_f(f[i].v[2]) * c, to_f(f[i].v[3]) * c));
-  } else {
-    constexpr int V = CHUNK / TPB;
-    X f[V];
-#pragma unroll
-    for (int i = 0; i < V; ++i)
-      if (i * TPB + int(threadIdx.x) < n) f[i] = x[i * TPB + threadIdx.x];
-#pragma unroll
-    for (int i = 0; i < V; ++i)
-      if (i * TPB + int(threadIdx.x) < n) __stcs(dst + i * TPB + threadIdx.x, to_f(f[i]) * c);
+      for (int j = 0; j < PER<X>; ++j) y[j] = from_f<X>(f[j] * c);
+      uint4 o;
+      memcpy(&o, y, 16);
+      __stcs(p + i, o);
+    }
   }
 }
 
-template <typename X> __device__ void chunk_scale(X* x, int n, float c) {
-  constexpr int V = CHUNK / PER<X> / TPB;
-  const int head = head_of(x, n), nv = (n - head) / PER<X>, tail = head + nv * PER<X>;
-  uint4* p = reinterpret_cast<uint4*>(x + head);
-  uint4 u[V];
-#pragma unroll
-  for (int i = 0; i < V; ++i)
-    if (i * TPB + int(threadIdx.x) < nv) u[i] = p[i * TPB + threadIdx.x];
-  if (int(threadIdx.x) < head + n - tail) {
-    const int e = int(threadIdx.x) < head ? int(threadIdx.x) : tail + int(threadIdx.x) - head;
-    x[e] = from_f<X>(to_f(x[e]) * c);
-  }
-#pragma unroll
-  for (int i = 0; i < V; ++i) {
-    float f[PER<X>];
-    X y[PER<X>];
-    widen<X>(u[i], f);
-#pragma unroll
-    for (int j = 0; j < PER<X>; ++j) y[j] = from_f<X>(f[j] * c);
-    memcpy(&u[i], y, 16);
-    if (i * TPB + int(threadIdx.x) < nv) __stcs(p + i * TPB + threadIdx.x, u[i]);
-  }
-}
-
-__device__ void apply_chunk(const ClipArgs& a, int i) {
-  const Chunk c = a.chunks[i];
-  const float f = __ldcg(a.coef + c.group);
-  if (a.rows) {
-    float* dst = a.rows + c.group * a.ld + c.dst;
-    if (c.type == MV_F32) chunk_pack(static_cast<const float*>(c.ptr), c.n, f, dst);
-    else if (c.type == MV_BF16) chunk_pack(static_cast<const __nv_bfloat16*>(c.ptr), c.n, f, dst);
-    else chunk_pack(static_cast<const __half*>(c.ptr), c.n, f, dst);
-  } else if (f != 1.0f) {
-    if (c.type == MV_F32) chunk_scale(static_cast<float*>(c.ptr), c.n, f);
-    else if (c.type == MV_BF16) chunk_scale(static_cast<__nv_bfloat16*>(c.ptr), c.n, f);
-    else chunk_scale(static_cast<__half*>(c.ptr), c.n, f);
-  }
-}
-
-__global__ void __launch_bounds__(TPB) k_clip(const __grid_constant__ ClipArgs a) {
-  asm volatile("griddepcontrol.launch_dependents;");
-  asm volatile("griddepcontrol.wait;" ::: "memory");      // the launch before this one: the factors, and the tensors' other users
-  const int n = a.n_apply + a.n_sum;
-  if (int(blockIdx.x) >= n) {        // groups without a chunk
+__global__ void __launch_bounds__(TPB, 6) k_clip(const __grid_constant__ ClipArgs a) {
+  __shared__ uint4 s_buf[CHUNK * 4 / 16];
+  __shared__ double s_sum[TPB / 32];
+  __shared__ unsigned long long s_at;
+  const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
+  if (threadIdx.x == 0) s_at = atomicAdd(a.taken, 1ull);
+  __syncthreads();
+  // every call takes as many items as it has CTAs: the remainder is the item, the quotient the call
+  const uint32_t at = uint32_t(s_at % gridDim.x), call = a.scales ? uint32_t(s_at / gridDim.x) + 1u : 0u;
+  if (a.empty && at == 0)
     for (int g = threadIdx.x; g < a.n_groups; g += TPB)
-      if (a.first[g] == a.first[g + 1]) put_norm(a, g, 0.0);
+      if (a.first[g] == a.first[g + 1]) put_norm(a, g, 0.0, call);
+  const Chunk c = a.items[at];
+  if (c.what & 1) {
+    float* dst = a.rows ? a.rows + c.group * a.ld + c.dst : nullptr;
+    if (c.type == MV_F32) chunk_scale(a, static_cast<float*>(c.ptr), c.n, dst, c.group, call, s_buf);
+    else if (c.type == MV_BF16) chunk_scale(a, static_cast<__nv_bfloat16*>(c.ptr), c.n, dst, c.group, call, s_buf);
+    else chunk_scale(a, static_cast<__half*>(c.ptr), c.n, dst, c.group, call, s_buf);
     return;
   }
-  // chunks to scale and chunks to sum, evenly mixed
-  const int applied = int(int64_t(blockIdx.x) * a.n_apply / n);
-  if (int(int64_t(blockIdx.x + 1) * a.n_apply / n) != applied) apply_chunk(a, a.apply0 + applied);
-  else sum_chunk(a, a.sum0 + int(blockIdx.x) - applied);
+  double s = c.type == MV_F32 ? chunk_sum(static_cast<const float*>(c.ptr), c.n, s_buf)
+           : c.type == MV_BF16 ? chunk_sum(static_cast<const __nv_bfloat16*>(c.ptr), c.n, s_buf)
+                               : chunk_sum(static_cast<const __half*>(c.ptr), c.n, s_buf);
+  if (c.n == 0) return;              // the item of a list without elements
+  for (int o = 16; o; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+  if (lane == 0) s_sum[w] = s;
+  __syncthreads();
+  if (w != 0) return;
+  s = lane < TPB / 32 ? s_sum[lane] : 0.0;
+  for (int o = TPB / 64; o; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+  finish_sum(a, c, s, call);
 }
 
 }  // namespace
@@ -233,9 +241,7 @@ struct mv_clip {
   uintptr_t lo, hi;                  // addresses that the tensors span
   int n_tensors;
   struct Span { uintptr_t lo, hi; }* spans;      // host: the bytes of each tensor
-  int empty;                         // some group has no chunk
-  int n_stages;
-  int32_t* stage;                    // host: [n_stages + 1] first chunk of each stage
+  const Chunk *sums, *items;         // the sums alone, and sums and scalings in their order
   ClipArgs args;
 };
 
@@ -250,36 +256,15 @@ bool overlaps(const mv_clip* p, const float* rows, int64_t ld) {
   return false;
 }
 
-int clip_launch(const ClipArgs& a, cudaStream_t st) {
-  const unsigned grid = unsigned(a.n_apply + a.n_sum + a.empty);
-  if (grid == 0) return MV_OK;
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(grid);
-  cfg.blockDim = dim3(TPB);
-  cfg.stream = st;
-  cudaLaunchAttribute early = {};
-  early.id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  early.val.programmaticStreamSerializationAllowed = 1;
-  cfg.attrs = &early;
-  cfg.numAttrs = 1;
-  const bool ok = cudaLaunchKernelEx(&cfg, k_clip, a) == cudaSuccess;
-  return cuda_ok() == MV_OK && ok ? MV_OK : MV_ERR_CUDA;
-}
-
-// The norms only, or stage by stage: sum the first, then scale one while summing the next, then scale the last.
 int clip_run(mv_clip* p, cudaStream_t st, float max_norm, float* rows, int64_t ld, float* norms, bool apply) {
   ClipArgs a = p->args;
   a.max_norm = max_norm; a.rows = rows; a.ld = ld; a.norms = norms;
-  const int last = apply ? p->n_stages : 0;
-  for (int s = 0; s <= last; ++s) {
-    a.apply0 = s > 0 ? p->stage[s - 1] : 0;
-    a.n_apply = s > 0 ? p->stage[s] - p->stage[s - 1] : 0;
-    a.sum0 = s < p->n_stages ? p->stage[s] : 0;
-    a.n_sum = s < p->n_stages ? p->stage[apply ? s + 1 : p->n_stages] - p->stage[s] : 0;
-    a.empty = s == 0 && p->empty;
-    if (int rc = clip_launch(a, st)) return rc;
-  }
-  return MV_OK;
+  a.items = apply ? p->items : p->sums;
+  a.scales = apply;
+  a.taken += apply ? 1 : 0;          // the two kinds of call count their items apart
+  const int64_t n = apply ? 2 * p->n : p->n;
+  k_clip<<<unsigned(n > 0 ? n : 1), TPB, 0, st>>>(a);
+  return cuda_ok();
 }
 
 }  // namespace
@@ -306,22 +291,22 @@ int mv_clip_create(mv_clip** out, void* stream, void* const* tensors, const int*
   mv_clip* p = static_cast<mv_clip*>(calloc(1, sizeof(mv_clip)));
   mv_clip::Span* spans = static_cast<mv_clip::Span*>(calloc(n_tensors ? n_tensors : 1, sizeof(mv_clip::Span)));
   char* host = static_cast<char*>(calloc(1, L.partial));
-  int32_t* stage = static_cast<int32_t*>(calloc(size_t(n_groups) + 1, 4));
-  if (!p || !spans || !host || !stage) { free(p); free(spans); free(host); free(stage); return MV_ERR_WORKSPACE; }
+  if (!p || !spans || !host) { free(p); free(spans); free(host); return MV_ERR_WORKSPACE; }
   char* base = static_cast<char*>(workspace);
   p->n = L.n;
   p->n_groups = n_groups;
   p->n_tensors = n_tensors;
   p->spans = spans;
   p->lo = UINTPTR_MAX;
-  p->stage = stage;
-  p->args.chunks = reinterpret_cast<Chunk*>(base + L.chunks);
+  p->sums = reinterpret_cast<Chunk*>(base + L.sums);
+  p->items = reinterpret_cast<Chunk*>(base + L.items);
   p->args.first = reinterpret_cast<int32_t*>(base + L.first);
   p->args.ticket = reinterpret_cast<uint32_t*>(base + L.ticket);
+  p->args.done = reinterpret_cast<unsigned long long*>(base + L.done);
+  p->args.taken = reinterpret_cast<unsigned long long*>(base + L.taken);
   p->args.partial = reinterpret_cast<double*>(base + L.partial);
-  p->args.coef = reinterpret_cast<float*>(base + L.coef);
   p->args.n_groups = n_groups;
-  Chunk* c = reinterpret_cast<Chunk*>(host + L.chunks);
+  Chunk* c = reinterpret_cast<Chunk*>(host + L.sums);
   int32_t* first = reinterpret_cast<int32_t*>(host + L.first);
   int64_t nc = 0, dst = 0;
   int g = 0;
@@ -335,6 +320,7 @@ int mv_clip_create(mv_clip** out, void* stream, void* const* tensors, const int*
       c[nc].n = int32_t(numel[i] - o < CHUNK ? numel[i] - o : CHUNK);
       c[nc].type = types[i];
       c[nc].group = gi;
+      c[nc].what = int32_t(2 * nc);
     }
     spans[i].lo = reinterpret_cast<uintptr_t>(tensors[i]);
     spans[i].hi = spans[i].lo + size_t(numel[i]) * type_size(types[i]);
@@ -344,19 +330,29 @@ int mv_clip_create(mv_clip** out, void* stream, void* const* tensors, const int*
     if (dst > p->longest) p->longest = dst;
   }
   while (g < n_groups) first[++g] = int32_t(nc);
-  // stages: whole groups, as many as STAGE holds
-  int64_t held = 0;
+  // stages: whole groups, as many as STAGE holds; a stage's sums stand between the scalings of the one before
+  Chunk* item = reinterpret_cast<Chunk*>(host + L.items);
+  int64_t held = 0, s0 = 0, s1 = 0, z0 = 0;          // sums of the stage: [s0, s1); scalings of the one before: [z0, s0)
+  auto stage = [&] {
+    const int64_t ns = s1 - s0, nz = s0 - z0, lead = ns < LEAD ? ns : LEAD;
+    for (int64_t i = 0, si = 0, zi = 0; i < ns + nz; ++i) {
+      if (i < lead || (i + 1 - lead) * nz / (ns + nz - lead) <= zi) *item++ = c[s0 + si++];
+      else { *item = c[z0 + zi++]; item++->what |= 1; }
+    }
+    z0 = s0;
+    s0 = s1;
+    held = 0;
+  };
   for (g = 0; g < n_groups; ++g) {
     int64_t bytes = 0;
     for (int32_t k = first[g]; k < first[g + 1]; ++k) bytes += int64_t(c[k].n) * type_size(c[k].type);
-    p->empty |= first[g] == first[g + 1];
-    if (p->n_stages == 0 || (held > 0 && bytes > 0 && held + bytes > STAGE)) {
-      stage[p->n_stages++] = first[g];
-      held = 0;
-    }
+    p->args.empty |= first[g] == first[g + 1];
+    if (held > 0 && held + bytes > STAGE) stage();
     held += bytes;
-    stage[p->n_stages] = first[g + 1];
+    s1 = first[g + 1];
   }
+  stage();
+  stage();                           // nothing left to sum: the scalings of the last stage
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   const bool ok = cudaMemcpyAsync(base, host, L.partial, cudaMemcpyHostToDevice, st) == cudaSuccess && cudaStreamSynchronize(st) == cudaSuccess;
   free(host);
@@ -368,7 +364,6 @@ int mv_clip_create(mv_clip** out, void* stream, void* const* tensors, const int*
 int mv_clip_destroy(mv_clip* plan) {
   if (!plan) return MV_ERR_INVALID_ARG;
   free(plan->spans);
-  free(plan->stage);
   free(plan);
   return MV_OK;
 }

@@ -602,6 +602,7 @@ def test_the_same_bytes_every_time_and_on_another_stream():
     torch.cuda.synchronize()
     st = torch.cuda.Stream()
     for _ in range(3):
+        plan.mv_clip_norm(nb, stream=st)                    # calls of both kinds on one plan
         plan.mv_clip_pack(1.0, b, nb, stream=st)
         st.synchronize()
         assert torch.equal(a, b) and torch.equal(na, nb)

@@ -11,10 +11,15 @@ namespace {
 // all of it, one CTA per item (sum this chunk, scale that chunk), in the order: the sums of stage 0, then the scalings
 // of stage s mixed with the sums of stage s + 1.  CTAs take their items by a counter, so an item's predecessors are with CTAs
 // that run or have run; an item that scales waits for its group's factor, and the sums that it waits for wait for nothing.
+// The last HOLD chunks of a group (all of a small group) are read only once: their CTAs sum them, keep them in shared memory
+// until the factor is there, and scale them.  Half of the device's CTAs are enough for that, so they cannot wait in vain.
 constexpr int TPB = 256;
 constexpr int CHUNK = 8192;          // elements per chunk: 16 or 32 KB, all on their way at once, six chunks a multiprocessor
-constexpr int64_t STAGE = int64_t(40) << 20;      // bytes of a stage, or one group
 constexpr int LEAD = 148 * 6;        // sums of the next stage taken before the first scaling: its factors are there by then
+#ifndef HOLDN
+#define HOLDN 3
+#endif
+constexpr int HOLD = 148 * HOLDN;
 constexpr int SPIN_LIMIT = 1 << 22;  // polls of a factor (a second or more) before an item is given up
 
 struct Chunk {
@@ -23,8 +28,10 @@ struct Chunk {
   int32_t n;
   int32_t type;
   int32_t group;
-  int32_t what;                      // 2 x the chunk's number; + 1: to be scaled
+  int32_t what;                      // 4 x the chunk's number + SUM, SCALE or both
 };
+
+enum { SUM = 1, SCALE = 2 };
 
 struct Layout { size_t sums, items, first, ticket, done, taken, partial, total; int64_t n; };
 
@@ -35,7 +42,7 @@ inline bool clip_layout(const int64_t* numel, int n_tensors, int n_groups, Layou
     if (numel[i] < 0 || numel[i] >= (int64_t(1) << 40)) return false;
     L->n += (numel[i] + CHUNK - 1) / CHUNK;
   }
-  if (L->n >= (int64_t(1) << 30)) return false;
+  if (L->n >= (int64_t(1) << 29)) return false;
   size_t o = 0;
   L->sums = o;    o = align_up(o + size_t(L->n + 1) * sizeof(Chunk), 256);      // (an empty one more, for a list without elements)
   L->items = o;   o = align_up(o + size_t(L->n + 1) * 2 * sizeof(Chunk), 256);
@@ -89,22 +96,14 @@ template <typename X> __device__ __forceinline__ void fetch(const X* x, int nv, 
       asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to + i * TPB * 16), "l"(p + i * TPB) : "memory");
 }
 
-// Sum of squares of a chunk, this thread's part.  64 bits: a square of 32 bits has no room below 1e-19 or above 1e19.
-template <typename X> __device__ __forceinline__ double chunk_sum(const X* x, int n, uint4* buf) {
-  constexpr int V = CHUNK / PER<X> / TPB;
-  const int head = head_of(x, n), nv = (n - head) / PER<X>, tail = head + nv * PER<X>, tid = threadIdx.x;
-  fetch(x + head, nv, buf);
-  double s = 0.0;
-  if (tid < head + n - tail) {
-    const double v = to_f(x[tid < head ? tid : tail + tid - head]);
-    s = v * v;
-  }
-  asm volatile("cp.async.wait_all;" ::: "memory");
+// Sum of squares of a chunk in shared memory, this thread's part.  64 bits: a square of 32 bits has no room below 1e-19 or
+// above 1e19.
+template <typename X> __device__ __forceinline__ double chunk_sum(int nv, const uint4* buf, double single) {
+  double s = single * single;
 #pragma unroll 2
-  for (int i = 0; i < V; ++i) {
-    if (i * TPB + tid >= nv) break;
+  for (int i = threadIdx.x; i < nv; i += TPB) {
     float f[PER<X>];
-    widen<X>(buf[i * TPB + tid], f);
+    widen<X>(buf[i], f);
 #pragma unroll
     for (int j = 0; j < PER<X>; ++j) { const double v = f[j]; s = fma(v, v, s); }
   }
@@ -126,7 +125,7 @@ __device__ __forceinline__ void finish_sum(const ClipArgs& a, const Chunk& c, do
   const int lane = threadIdx.x, c0 = a.first[c.group], c1 = a.first[c.group + 1];
   uint32_t arrived = 0;
   if (lane == 0) {
-    __stcg(a.partial + (c.what >> 1), s);
+    __stcg(a.partial + (c.what >> 2), s);
     __threadfence();
     arrived = atomicAdd(a.ticket + c.group, 1u);
   }
@@ -153,20 +152,11 @@ __device__ __forceinline__ float wait_factor(const ClipArgs& a, int g, uint32_t 
   return __int_as_float(0x7fffffff);
 }
 
-// A chunk times its group's factor: in place, or to 32 bits at dst.
-template <typename X> __device__ __forceinline__ void chunk_scale(const ClipArgs& a, X* x, int n, float* dst, int group, uint32_t call, uint4* buf) {
-  __shared__ float s_factor;
-  const int head = head_of(x, n), nv = (n - head) / PER<X>, tail = head + nv * PER<X>, tid = threadIdx.x;
-  fetch(x + head, nv, buf);
-  const bool single = tid < head + n - tail;
-  const int e = tid < head ? tid : tail + tid - head;
-  const float v = single ? to_f(x[e]) : 0.0f;
-  if (tid == TPB - 1) s_factor = wait_factor(a, group, call);
-  asm volatile("cp.async.wait_all;" ::: "memory");
-  __syncthreads();
-  const float c = s_factor;
+// A chunk in shared memory times its group's factor: in place, or to 32 bits at dst.
+template <typename X> __device__ __forceinline__ void chunk_scale(X* x, float* dst, int head, int nv, int e, float v, const uint4* buf, float c) {
+  const int tid = threadIdx.x;
   if (dst) {
-    if (single) dst[e] = v * c;
+    if (e >= 0) dst[e] = v * c;
     dst += head;
     const int m = nv * PER<X>;
     if ((reinterpret_cast<uintptr_t>(dst) & 15) == 0) {
@@ -177,13 +167,15 @@ template <typename X> __device__ __forceinline__ void chunk_scale(const ClipArgs
         const Four f = from[i];
         __stcs(reinterpret_cast<float4*>(dst) + i, make_float4(to_f(f.v[0]) * c, to_f(f.v[1]) * c, to_f(f.v[2]) * c, to_f(f.v[3]) * c));
       }
-    } else {                         // word by word, whole lines per warp
+    } else {                         // word by word, whole aligned lines per warp (sectors written in two halves cost a read each)
       const X* from = reinterpret_cast<const X*>(buf);
+      const int i0 = tid - int(reinterpret_cast<uintptr_t>(dst) / 4 % 32);
+      if (i0 >= 0 && i0 < m) __stcs(dst + i0, to_f(from[i0]) * c);
 #pragma unroll 8
-      for (int i = tid; i < m; i += TPB) __stcs(dst + i, to_f(from[i]) * c);
+      for (int i = i0 + TPB; i < m; i += TPB) __stcs(dst + i, to_f(from[i]) * c);
     }
   } else if (c != 1.0f) {
-    if (single) x[e] = from_f<X>(v * c);
+    if (e >= 0) x[e] = from_f<X>(v * c);
     uint4* p = reinterpret_cast<uint4*>(x + head);
 #pragma unroll 2
     for (int i = tid; i < nv; i += TPB) {
@@ -199,11 +191,38 @@ template <typename X> __device__ __forceinline__ void chunk_scale(const ClipArgs
   }
 }
 
+template <typename X> __device__ __forceinline__ void work_off(const ClipArgs& a, const Chunk& c, uint32_t call, uint4* buf) {
+  __shared__ double s_sum[TPB / 32];
+  __shared__ float s_factor;
+  const int lane = threadIdx.x & 31, w = threadIdx.x >> 5, tid = threadIdx.x, n = c.n;
+  X* x = static_cast<X*>(c.ptr);
+  const int head = head_of(x, n), nv = (n - head) / PER<X>, tail = head + nv * PER<X>;
+  fetch(x + head, nv, buf);
+  // what lies before and behind the whole vectors: an element e for a few threads
+  const int e = tid >= head + n - tail ? -1 : tid < head ? tid : tail + tid - head;
+  const float v = e >= 0 ? to_f(x[e]) : 0.0f;
+  if (c.what & SUM) {
+    asm volatile("cp.async.wait_all;" ::: "memory");      // a thread sums the vectors that it fetched itself
+    double s = chunk_sum<X>(nv, buf, v);
+    for (int o = 16; o; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+    if (lane == 0) s_sum[w] = s;
+    __syncthreads();
+    if (w == 0) {
+      s = lane < TPB / 32 ? s_sum[lane] : 0.0;
+      for (int o = TPB / 64; o; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+      finish_sum(a, c, s, call);
+    }
+  }
+  if (!(c.what & SCALE)) return;
+  if (tid == TPB - 1) s_factor = wait_factor(a, c.group, call);
+  asm volatile("cp.async.wait_all;" ::: "memory");
+  __syncthreads();
+  chunk_scale(x, a.rows ? a.rows + c.group * a.ld + c.dst : nullptr, head, nv, e, v, buf, s_factor);
+}
+
 __global__ void __launch_bounds__(TPB, 6) k_clip(const __grid_constant__ ClipArgs a) {
   __shared__ uint4 s_buf[CHUNK * 4 / 16];
-  __shared__ double s_sum[TPB / 32];
   __shared__ unsigned long long s_at;
-  const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
   if (threadIdx.x == 0) s_at = atomicAdd(a.taken, 1ull);
   __syncthreads();
   // every call takes as many items as it has CTAs: the remainder is the item, the quotient the call
@@ -212,24 +231,9 @@ __global__ void __launch_bounds__(TPB, 6) k_clip(const __grid_constant__ ClipArg
     for (int g = threadIdx.x; g < a.n_groups; g += TPB)
       if (a.first[g] == a.first[g + 1]) put_norm(a, g, 0.0, call);
   const Chunk c = a.items[at];
-  if (c.what & 1) {
-    float* dst = a.rows ? a.rows + c.group * a.ld + c.dst : nullptr;
-    if (c.type == MV_F32) chunk_scale(a, static_cast<float*>(c.ptr), c.n, dst, c.group, call, s_buf);
-    else if (c.type == MV_BF16) chunk_scale(a, static_cast<__nv_bfloat16*>(c.ptr), c.n, dst, c.group, call, s_buf);
-    else chunk_scale(a, static_cast<__half*>(c.ptr), c.n, dst, c.group, call, s_buf);
-    return;
-  }
-  double s = c.type == MV_F32 ? chunk_sum(static_cast<const float*>(c.ptr), c.n, s_buf)
-           : c.type == MV_BF16 ? chunk_sum(static_cast<const __nv_bfloat16*>(c.ptr), c.n, s_buf)
-                               : chunk_sum(static_cast<const __half*>(c.ptr), c.n, s_buf);
-  if (c.n == 0) return;              // the item of a list without elements
-  for (int o = 16; o; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
-  if (lane == 0) s_sum[w] = s;
-  __syncthreads();
-  if (w != 0) return;
-  s = lane < TPB / 32 ? s_sum[lane] : 0.0;
-  for (int o = TPB / 64; o; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
-  finish_sum(a, c, s, call);
+  if (c.type == MV_F32) work_off<float>(a, c, call, s_buf);
+  else if (c.type == MV_BF16) work_off<__nv_bfloat16>(a, c, call, s_buf);
+  else work_off<__half>(a, c, call, s_buf);
 }
 
 }  // namespace
@@ -242,6 +246,7 @@ struct mv_clip {
   int n_tensors;
   struct Span { uintptr_t lo, hi; }* spans;      // host: the bytes of each tensor
   const Chunk *sums, *items;         // the sums alone, and sums and scalings in their order
+  int64_t n_items;
   ClipArgs args;
 };
 
@@ -262,7 +267,7 @@ int clip_run(mv_clip* p, cudaStream_t st, float max_norm, float* rows, int64_t l
   a.items = apply ? p->items : p->sums;
   a.scales = apply;
   a.taken += apply ? 1 : 0;          // the two kinds of call count their items apart
-  const int64_t n = apply ? 2 * p->n : p->n;
+  const int64_t n = apply ? p->n_items : p->n;
   k_clip<<<unsigned(n > 0 ? n : 1), TPB, 0, st>>>(a);
   return cuda_ok();
 }
@@ -320,7 +325,7 @@ int mv_clip_create(mv_clip** out, void* stream, void* const* tensors, const int*
       c[nc].n = int32_t(numel[i] - o < CHUNK ? numel[i] - o : CHUNK);
       c[nc].type = types[i];
       c[nc].group = gi;
-      c[nc].what = int32_t(2 * nc);
+      c[nc].what = int32_t(4 * nc + SUM);
     }
     spans[i].lo = reinterpret_cast<uintptr_t>(tensors[i]);
     spans[i].hi = spans[i].lo + size_t(numel[i]) * type_size(types[i]);
@@ -330,29 +335,29 @@ int mv_clip_create(mv_clip** out, void* stream, void* const* tensors, const int*
     if (dst > p->longest) p->longest = dst;
   }
   while (g < n_groups) first[++g] = int32_t(nc);
-  // stages: whole groups, as many as STAGE holds; a stage's sums stand between the scalings of the one before
+  // Items of a call that scales.  A group's own: the sums of all but its last HOLD chunks, then those in one go.  Then the
+  // scalings of the former, mixed with the next group's own items.
   Chunk* item = reinterpret_cast<Chunk*>(host + L.items);
-  int64_t held = 0, s0 = 0, s1 = 0, z0 = 0;          // sums of the stage: [s0, s1); scalings of the one before: [z0, s0)
-  auto stage = [&] {
-    const int64_t ns = s1 - s0, nz = s0 - z0, lead = ns < LEAD ? ns : LEAD;
-    for (int64_t i = 0, si = 0, zi = 0; i < ns + nz; ++i) {
-      if (i < lead || (i + 1 - lead) * nz / (ns + nz - lead) <= zi) *item++ = c[s0 + si++];
-      else { *item = c[z0 + zi++]; item++->what |= 1; }
+  int64_t z0 = 0, z1 = 0;            // chunks still to be scaled
+  for (g = 0; g <= n_groups; ++g) {
+    const int64_t f0 = g < n_groups ? first[g] : 0, f1 = g < n_groups ? first[g + 1] : 0;
+    if (g < n_groups) p->args.empty |= f0 == f1;
+    if (g < n_groups && f0 == f1) continue;
+    const int64_t own = f1 - f0, held = own < HOLD ? own : HOLD, nz = z1 - z0, lead = own < LEAD ? own : LEAD;
+    for (int64_t i = 0, oi = 0, zi = 0; i < own + nz; ++i) {
+      if (i < lead || (i + 1 - lead) * nz / (own + nz - lead) <= zi) {
+        *item = c[f0 + oi++];
+        if (oi > own - held) item->what |= SCALE;
+      } else {
+        *item = c[z0 + zi++];
+        item->what ^= SUM | SCALE;
+      }
+      ++item;
     }
-    z0 = s0;
-    s0 = s1;
-    held = 0;
-  };
-  for (g = 0; g < n_groups; ++g) {
-    int64_t bytes = 0;
-    for (int32_t k = first[g]; k < first[g + 1]; ++k) bytes += int64_t(c[k].n) * type_size(c[k].type);
-    p->args.empty |= first[g] == first[g + 1];
-    if (held > 0 && held + bytes > STAGE) stage();
-    held += bytes;
-    s1 = first[g + 1];
+    z0 = f0;
+    z1 = f1 - held;
   }
-  stage();
-  stage();                           // nothing left to sum: the scalings of the last stage
+  p->n_items = item - reinterpret_cast<Chunk*>(host + L.items);
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   const bool ok = cudaMemcpyAsync(base, host, L.partial, cudaMemcpyHostToDevice, st) == cudaSuccess && cudaStreamSynchronize(st) == cudaSuccess;
   free(host);

@@ -237,6 +237,8 @@ def mv_dequantize(words, K: int, q: int, out, stream: Optional[torch.cuda.Stream
 
 
 _TYPES = {torch.float32: MV_F32, torch.bfloat16: MV_BF16, torch.float16: MV_F16, torch.int32: MV_I32, torch.int64: MV_I64}
+_VALUES, _IDS, _FLOAT = (MV_F32, MV_BF16, MV_F16), (MV_I32, MV_I64), (MV_F32,)
+_raw_current_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)     # absent from a torch without CUDA
 
 
 def _need(ok: bool, where: str):
@@ -245,42 +247,36 @@ def _need(ok: bool, where: str):
         raise MvError(MV_ERR_INVALID_ARG, where)
 
 
-def _addr(t: Optional[torch.Tensor]):
-    return None if t is None else t.data_ptr()
-
-
-def _raw_stream(t: torch.Tensor, stream: Optional[torch.cuda.Stream]):
-    return (stream if stream is not None else torch.cuda.current_stream(t.device)).cuda_stream
+def _raw_stream(device_index: int, stream: Optional[torch.cuda.Stream]):
+    return stream.cuda_stream if stream is not None else _raw_current_stream(device_index)
 
 
 def _matrix(t: torch.Tensor, kinds, where: str):
-    """(type code, rows, columns, row pitch) of a 2-d tensor whose rows are contiguous."""
-    code = _TYPES.get(t.dtype, -1)
-    _need(t.dim() == 2 and code in kinds and t.is_cuda and (t.stride(1) == 1 or t.shape[1] == 1), where)
-    rows, cols = t.shape
-    return code, rows, cols, t.stride(0) if rows > 1 else cols
+    """(address, type code, rows, columns, row pitch, device) of a 2-d CUDA tensor whose rows are contiguous."""
+    code, shape, stride, dev = _TYPES.get(t.dtype, -1), t.shape, t.stride(), t.get_device()
+    if len(shape) != 2 or code not in kinds or dev < 0 or (stride[1] != 1 and shape[1] != 1):
+        raise MvError(MV_ERR_INVALID_ARG, where)
+    rows, cols = shape
+    return t.data_ptr(), code, rows, cols, stride[0] if rows > 1 else cols, dev
 
 
-_VALUES, _IDS = (MV_F32, MV_BF16, MV_F16), (MV_I32, MV_I64)
-
-
-def _vector(t: Optional[torch.Tensor], n: int, kinds, dev, where: str):
-    """Type code of a contiguous 1-d tensor of n elements (None passes as the first kind)."""
+def _vector(t: Optional[torch.Tensor], n: int, kinds, dev: int, where: str):
+    """(address, type code) of a contiguous 1-d tensor of n elements on that device; (None, first kind) for None."""
     if t is None:
-        return kinds[0]
+        return None, kinds[0]
     code = _TYPES.get(t.dtype, -1)
-    _need(t.dim() == 1 and t.shape[0] == n and code in kinds and t.device == dev and (n <= 1 or t.stride(0) == 1), where)
-    return code
+    if code not in kinds or t.dim() != 1 or t.numel() != n or t.get_device() != dev or not t.is_contiguous():
+        raise MvError(MV_ERR_INVALID_ARG, where)
+    return t.data_ptr(), code
 
 
 def mv_embed(weight, ids, out, scale: float = 1.0, stream: Optional[torch.cuda.Stream] = None):
     """out[t] = scale * weight[ids[t]]; weight [V, D], ids [T], out [T, D]."""
-    w_type, V, D, ldw = _matrix(weight, _VALUES, "mv_embed")
-    o_type, T, Do, ldo = _matrix(out, _VALUES, "mv_embed")
-    i_type = _vector(ids, T, _IDS, weight.device, "mv_embed")
-    _need(Do == D and out.device == weight.device, "mv_embed")
-    _check(load().mv_embed(_raw_stream(out, stream), _addr(weight), w_type, V, D, ldw, _addr(ids), i_type, T, float(scale), _addr(out),
-                           o_type, ldo), "mv_embed")
+    w, w_type, V, D, ldw, dev = _matrix(weight, _VALUES, "mv_embed")
+    o, o_type, T, Do, ldo, dev_o = _matrix(out, _VALUES, "mv_embed")
+    i, i_type = _vector(ids, T, _IDS, dev, "mv_embed")
+    _need(Do == D and dev_o == dev, "mv_embed")
+    _check(load().mv_embed(_raw_stream(dev, stream), w, w_type, V, D, ldw, i, i_type, T, scale, o, o_type, ldo), "mv_embed")
 
 
 def embed_grad_workspace_bytes(T: int, V: int, D: int) -> int:
@@ -290,48 +286,43 @@ def embed_grad_workspace_bytes(T: int, V: int, D: int) -> int:
 def mv_embed_grad(dout, ids, dweight, workspace, scale: float = 1.0, pad_id: int = -1, accumulate: bool = False,
                   stream: Optional[torch.cuda.Stream] = None):
     """dweight[v] (+)= scale * sum of dout over the tokens with id v; dout [T, D], ids [T], dweight float [V, D]."""
-    x_type, T, D, ldd = _matrix(dout, _VALUES, "mv_embed_grad")
-    _, V, Dw, ldw = _matrix(dweight, (MV_F32,), "mv_embed_grad")
-    i_type = _vector(ids, T, _IDS, dout.device, "mv_embed_grad")
-    _need(Dw == D and dweight.device == dout.device and workspace.device == dout.device and workspace.is_contiguous(), "mv_embed_grad")
-    _check(load().mv_embed_grad(_raw_stream(dout, stream), _addr(dout), x_type, ldd, _addr(ids), i_type, T, V, D, float(scale), int(pad_id),
-                                int(accumulate), _addr(dweight), ldw, _addr(workspace), workspace.numel() * workspace.element_size()),
-           "mv_embed_grad")
+    x, x_type, T, D, ldd, dev = _matrix(dout, _VALUES, "mv_embed_grad")
+    d, _, V, Dw, ldw, dev_w = _matrix(dweight, _FLOAT, "mv_embed_grad")
+    i, i_type = _vector(ids, T, _IDS, dev, "mv_embed_grad")
+    _need(Dw == D and dev_w == dev and workspace.get_device() == dev and workspace.is_contiguous(), "mv_embed_grad")
+    _check(load().mv_embed_grad(_raw_stream(dev, stream), x, x_type, ldd, i, i_type, T, V, D, scale, pad_id, bool(accumulate), d, ldw,
+                                workspace.data_ptr(), workspace.numel() * workspace.element_size()), "mv_embed_grad")
 
 
 def mv_token_logprob(logits, targets=None, scale: float = 1.0, logprob=None, entropy=None, lse=None, top_logprob=None, top_id=None,
                      stream: Optional[torch.cuda.Stream] = None):
     """Log probabilities of targets [T] under softmax(scale * logits), logits [T, V]; logprob, entropy, lse: float [T];
     top_logprob float [T, k], top_id int32 [T, k].  An output that is None is not computed."""
-    x_type, T, V, ld = _matrix(logits, _VALUES, "mv_token_logprob")
-    dev = logits.device
-    i_type = _vector(targets, T, _IDS, dev, "mv_token_logprob")
-    for t in (logprob, entropy, lse):
-        _vector(t, T, (MV_F32,), dev, "mv_token_logprob")
-    k = 0
-    for t, kind in ((top_logprob, torch.float32), (top_id, torch.int32)):
+    where = "mv_token_logprob"
+    x, x_type, T, V, ld, dev = _matrix(logits, _VALUES, where)
+    y, i_type = _vector(targets, T, _IDS, dev, where)
+    lp, h, l = _vector(logprob, T, _FLOAT, dev, where)[0], _vector(entropy, T, _FLOAT, dev, where)[0], _vector(lse, T, _FLOAT, dev, where)[0]
+    k, tops = None, [None, None]
+    for j, (t, kind) in enumerate(((top_logprob, torch.float32), (top_id, torch.int32))):
         if t is not None:
-            _need(t.dim() == 2 and t.shape[0] == T and t.is_contiguous() and t.dtype == kind and t.device == dev and k in (0, t.shape[1]),
-                  "mv_token_logprob")
-            k = t.shape[1]
-    _check(load().mv_token_logprob(_raw_stream(logits, stream), _addr(logits), x_type, T, V, ld, _addr(targets), i_type, float(scale), k,
-                                   _addr(logprob), _addr(entropy), _addr(lse), _addr(top_logprob), _addr(top_id)), "mv_token_logprob")
+            n, width = t.shape if t.dim() == 2 else (-1, 0)
+            _need(n == T and t.dtype == kind and t.get_device() == dev and t.is_contiguous() and k in (None, width), where)
+            k, tops[j] = width, t.data_ptr()
+    _check(load().mv_token_logprob(_raw_stream(dev, stream), x, x_type, T, V, ld, y, i_type, scale, k or 0, lp, h, l, tops[0], tops[1]), where)
 
 
 def mv_token_logprob_grad(logits, targets, lse, g_logprob, dlogits, scale: float = 1.0, entropy=None, g_entropy=None,
                           stream: Optional[torch.cuda.Stream] = None):
     """dlogits [T, V] of sum(g_logprob * logprob + g_entropy * entropy); dlogits may be logits.  g_logprob (with targets)
     or g_entropy (with entropy) may be None."""
-    x_type, T, V, ld = _matrix(logits, _VALUES, "mv_token_logprob_grad")
-    d_type, Td, Vd, ldg = _matrix(dlogits, _VALUES, "mv_token_logprob_grad")
-    dev = logits.device
-    i_type = _vector(targets, T, _IDS, dev, "mv_token_logprob_grad")
-    for t in (lse, g_logprob, entropy, g_entropy):
-        _vector(t, T, (MV_F32,), dev, "mv_token_logprob_grad")
-    _need((d_type, Td, Vd) == (x_type, T, V) and dlogits.device == dev, "mv_token_logprob_grad")
-    _check(load().mv_token_logprob_grad(_raw_stream(logits, stream), _addr(logits), x_type, T, V, ld, _addr(targets), i_type, float(scale),
-                                        _addr(lse), _addr(entropy), _addr(g_logprob), _addr(g_entropy), _addr(dlogits), ldg),
-           "mv_token_logprob_grad")
+    where = "mv_token_logprob_grad"
+    x, x_type, T, V, ld, dev = _matrix(logits, _VALUES, where)
+    d, d_type, Td, Vd, ldg, dev_d = _matrix(dlogits, _VALUES, where)
+    y, i_type = _vector(targets, T, _IDS, dev, where)
+    l, h = _vector(lse, T, _FLOAT, dev, where)[0], _vector(entropy, T, _FLOAT, dev, where)[0]
+    g1, g2 = _vector(g_logprob, T, _FLOAT, dev, where)[0], _vector(g_entropy, T, _FLOAT, dev, where)[0]
+    _need(d_type == x_type and Td == T and Vd == V and dev_d == dev, where)
+    _check(load().mv_token_logprob_grad(_raw_stream(dev, stream), x, x_type, T, V, ld, y, i_type, scale, l, h, g1, g2, d, ldg), where)
 
 
 class MvClip:
@@ -360,8 +351,9 @@ class MvClip:
         _need(nbytes > 0, "mv_clip_workspace_bytes")
         self.workspace = torch.empty(nbytes, dtype=torch.uint8, device=dev)
         handle = ctypes.c_void_p()
-        _check(self.lib.mv_clip_create(ctypes.byref(handle), _raw_stream(self.workspace, stream), ptrs, types, numel, group, n, self.n_groups,
-                                       _addr(self.workspace), nbytes), "mv_clip_create")
+        self.dev = self.workspace.get_device()
+        _check(self.lib.mv_clip_create(ctypes.byref(handle), _raw_stream(self.dev, stream), ptrs, types, numel, group, n, self.n_groups,
+                                       self.workspace.data_ptr(), nbytes), "mv_clip_create")
         self.handle = handle
 
     def close(self):
@@ -375,23 +367,19 @@ class MvClip:
         except Exception:
             pass
 
-    def _norms(self, norms, where):
-        _vector(norms, self.n_groups, (MV_F32,), self.workspace.device, where)
-
     def mv_clip_norm(self, norms, stream: Optional[torch.cuda.Stream] = None):
-        self._norms(norms, "mv_clip_norm")
-        _check(self.lib.mv_clip_norm(self.handle, _raw_stream(self.workspace, stream), _addr(norms)), "mv_clip_norm")
+        n, _ = _vector(norms, self.n_groups, _FLOAT, self.dev, "mv_clip_norm")
+        _check(self.lib.mv_clip_norm(self.handle, _raw_stream(self.dev, stream), n), "mv_clip_norm")
 
     def mv_clip_scale(self, max_norm: float, norms=None, stream: Optional[torch.cuda.Stream] = None):
-        self._norms(norms, "mv_clip_scale")
-        _check(self.lib.mv_clip_scale(self.handle, _raw_stream(self.workspace, stream), float(max_norm), _addr(norms)), "mv_clip_scale")
+        n, _ = _vector(norms, self.n_groups, _FLOAT, self.dev, "mv_clip_scale")
+        _check(self.lib.mv_clip_scale(self.handle, _raw_stream(self.dev, stream), max_norm, n), "mv_clip_scale")
 
     def mv_clip_pack(self, max_norm: float, rows, norms=None, stream: Optional[torch.cuda.Stream] = None):
-        self._norms(norms, "mv_clip_pack")
-        _, G, d, ld = _matrix(rows, (MV_F32,), "mv_clip_pack")
-        _need(G == self.n_groups and d >= self.longest and rows.device == self.workspace.device, "mv_clip_pack")
-        _check(self.lib.mv_clip_pack(self.handle, _raw_stream(self.workspace, stream), float(max_norm), _addr(rows), ld, _addr(norms)),
-               "mv_clip_pack")
+        n, _ = _vector(norms, self.n_groups, _FLOAT, self.dev, "mv_clip_pack")
+        r, _, G, d, ld, dev = _matrix(rows, _FLOAT, "mv_clip_pack")
+        _need(G == self.n_groups and d >= self.longest and dev == self.dev, "mv_clip_pack")
+        _check(self.lib.mv_clip_pack(self.handle, _raw_stream(self.dev, stream), max_norm, r, ld, n), "mv_clip_pack")
 
 
 class MvContext:

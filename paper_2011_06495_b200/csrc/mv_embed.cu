@@ -39,22 +39,25 @@ template <typename X, bool VEC> __device__ __forceinline__ void load_raw(const X
 }
 
 // ------------------------------------------------------------------------------------------ lookup
-// A warp takes R tokens and one block of columns: it reads the R ids with one load, then R independent pieces of rows.
+// A warp takes R tokens and one block of columns: it reads the R ids with one load, then R independent pieces of rows.  With
+// many tokens the rows come out of L2 for the most part, and L2 bounds it: 65536 rows of 4 KB in and out move 537 MB in 78 us,
+// 6.9 TB/s.  More rows per warp cost warps (R = 4: 85 us, R = 8: 101), fewer leave it waiting for the ids (R = 1: 101).  The
+// output is written past L2 (evict first), whose room belongs to the table.
 constexpr int EMBED_TPB = 128;
 
 template <typename W, typename O, bool VEC, int R>
 __global__ void __launch_bounds__(EMBED_TPB) k_embed(const W* __restrict__ weight, int64_t V, int64_t D, int64_t ldw, const void* __restrict__ ids,
-                                                      int id_type, int64_t T, float scale, O* __restrict__ out, int64_t ldo, int ncb) {
+                                                      int id_type, int64_t T, float scale, O* __restrict__ out, int64_t ldo, unsigned ncb) {
   const int lane = threadIdx.x & 31;
   const int64_t item = int64_t(blockIdx.x) * (EMBED_TPB / 32) + (threadIdx.x >> 5);
   const int64_t t0 = item / ncb * R, cb = item % ncb;
   if (t0 >= T) return;
   const int n = int(min(int64_t(R), T - t0));
-  const int64_t mine = lane < n ? load_id(ids, id_type, t0 + lane, V) : -1;
+  const int mine = lane < n ? int(load_id(ids, id_type, t0 + lane, V)) : -1;
   uint4 u[R];
 #pragma unroll
   for (int i = 0; i < R; ++i) {
-    const int64_t v = __shfl_sync(0xffffffffu, mine, i);
+    const int v = __shfl_sync(0xffffffffu, mine, i);
     u[i] = make_uint4(0, 0, 0, 0);
     if (v >= 0) load_raw<W, VEC>(weight + v * ldw, D, cb, lane, u[i]);
   }
@@ -70,7 +73,8 @@ __global__ void __launch_bounds__(EMBED_TPB) k_embed(const W* __restrict__ weigh
     O* dst = out + (t0 + i) * ldo;
     const int64_t c0 = column<W, VEC>(cb, lane, 0);
     if (VEC && c0 + LANE<W> <= D) {
-      *reinterpret_cast<Row*>(dst + c0) = o;
+      if constexpr (sizeof(Row) == 16) { float4 q; memcpy(&q, &o, 16); __stcs(reinterpret_cast<float4*>(dst + c0), q); }
+      else *reinterpret_cast<Row*>(dst + c0) = o;
     } else {
 #pragma unroll
       for (int j = 0; j < LANE<W>; ++j) {
@@ -520,12 +524,12 @@ int mv_embed(void* stream, const void* weight, int w_type, int64_t V, int64_t D,
       const int64_t ncb = (D + BLOCK<W> - 1) / BLOCK<W>;
       const int ob = int(sizeof(O)) * LANE<W> < 16 ? int(sizeof(O)) * LANE<W> : 16;
       const bool vec = rows_aligned(weight, ldw, sizeof(W), 16) && rows_aligned(out, ldo, sizeof(O), ob);
-      // eight tokens a warp once that still gives every multiprocessor its warps; below, the latency of one row counts
-      const int R = T * ncb >= 148 * 64 * 8 ? 8 : 1;
+      // two tokens a warp once that still gives every multiprocessor its 64 warps; below, the latency of one row counts
+      const int R = T * ncb >= 148 * 64 * 2 ? 2 : 1;
       const int64_t items = (T + R - 1) / R * ncb, grid = (items + EMBED_TPB / 32 - 1) / (EMBED_TPB / 32);
       if (grid >= lim) return int(MV_ERR_INVALID_ARG);
-      auto* kernel = vec ? (R == 8 ? k_embed<W, O, true, 8> : k_embed<W, O, true, 1>) : (R == 8 ? k_embed<W, O, false, 8> : k_embed<W, O, false, 1>);
-      kernel<<<unsigned(grid), EMBED_TPB, 0, st>>>(static_cast<const W*>(weight), V, D, ldw, ids, id_type, T, scale, static_cast<O*>(out), ldo, int(ncb));
+      auto* kernel = vec ? (R == 2 ? k_embed<W, O, true, 2> : k_embed<W, O, true, 1>) : (R == 2 ? k_embed<W, O, false, 2> : k_embed<W, O, false, 1>);
+      kernel<<<unsigned(grid), EMBED_TPB, 0, st>>>(static_cast<const W*>(weight), V, D, ldw, ids, id_type, T, scale, static_cast<O*>(out), ldo, unsigned(ncb));
       return cuda_ok();
     });
   });
@@ -570,10 +574,8 @@ int mv_embed_grad(void* stream, const void* dout, int dout_type, int64_t ldd, co
   s.n_ticket = items;
   const size_t smem = sizeof(SortSmem) + size_t(SORT_WARPS) * p.bins * 4;
   auto* sort = id_type == MV_I32 ? k_embed_sort<int32_t> : k_embed_sort<int64_t>;
-  if (cudaFuncSetAttribute(sort, cudaFuncAttributeMaxDynamicSharedMemorySize, int(smem)) != cudaSuccess) {
-    cudaGetLastError();
-    return MV_ERR_CUDA;
-  }
+  static SmemLimit sort_limit[2];
+  if (!allow_smem(sort, int(smem), &sort_limit[id_type == MV_I32])) return MV_ERR_CUDA;
   sort<<<1u << p.nb_log, SORT_TPB, smem, st>>>(s);
   a.perm = s.perm; a.row = s.row; a.start = s.start; a.valid = s.valid; a.ticket = s.ticket;
   a.part = reinterpret_cast<float*>(base + p.part);
@@ -587,10 +589,8 @@ int mv_embed_grad(void* stream, const void* dout, int dout_type, int64_t ldd, co
     auto* kernel = p.piece == 32 ? (vec ? k_embed_sum<X, true, 32> : k_embed_sum<X, false, 32>)
                                  : (vec ? k_embed_sum<X, true, 8> : k_embed_sum<X, false, 8>);
     const int ring = (p.piece < RING ? p.piece : RING) * SUM_TPB * 16;
-    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, ring) != cudaSuccess) {
-      cudaGetLastError();
-      return int(MV_ERR_CUDA);
-    }
+    static SmemLimit sum_limit[4];     // (per type of dout)
+    if (!allow_smem(kernel, ring, &sum_limit[2 * vec + (p.piece == 32)])) return int(MV_ERR_CUDA);
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(unsigned(n_sum + a.n_fill));
     cfg.blockDim = dim3(SUM_TPB);

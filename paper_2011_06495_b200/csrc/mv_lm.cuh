@@ -33,6 +33,20 @@ __device__ __forceinline__ int64_t load_id(const void* ids, int id_type, int64_t
   return v >= 0 && v < V ? v : -1;
 }
 
+// Lets a kernel use `bytes` of dynamic shared memory; asked of the driver once per kernel (a static of the caller) and device.
+struct SmemLimit { int bytes[64]; };
+template <typename K> bool allow_smem(K* kernel, int bytes, SmemLimit* have) {
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess) return false;
+  if (dev < 64 && have->bytes[dev] >= bytes) return true;
+  if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes) != cudaSuccess) {
+    cudaGetLastError();
+    return false;
+  }
+  if (dev < 64) have->bytes[dev] = bytes;
+  return true;
+}
+
 // Calls f with a value of the element type that a type code names.
 template <typename F> int with_type(int t, F&& f) {
   switch (t) {

@@ -108,10 +108,10 @@ template <> struct Vec<__half> {
   }
 };
 
-__device__ __forceinline__ uint4 load_stream(const uint4* p) {
-  uint4 u;
-  asm volatile("ld.global.nc.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(u.x), "=r"(u.y), "=r"(u.z), "=r"(u.w) : "l"(p));
-  return u;
+// 32 bytes at a multiple of 32: a whole sector.
+__device__ __forceinline__ void load_stream(const uint4* p, uint4& a, uint4& b) {
+  asm volatile("ld.global.nc.L1::no_allocate.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+               : "=r"(a.x), "=r"(a.y), "=r"(a.z), "=r"(a.w), "=r"(b.x), "=r"(b.y), "=r"(b.z), "=r"(b.w) : "l"(p));
 }
 
 // (value descending, index ascending) as one number, larger is earlier; +0 and -0 are one value.  0 is no key.
@@ -125,7 +125,8 @@ __device__ __forceinline__ float key_value(unsigned long long k) {
 }
 __device__ __forceinline__ uint32_t key_index(unsigned long long k) { return 0xffffffffu - uint32_t(k); }
 
-// One row, or one CTA's part of it: `head` single logits, nv vectors of 16 bytes, `tail` single logits.
+// One row, or one CTA's part of it: `head` single logits, nv vectors of 16 bytes (an even number, from a multiple of 32 bytes
+// on), `tail` single logits.
 template <typename X> struct Part {
   const X* row;
   const uint4* vec;                  // the part's first vector
@@ -138,7 +139,7 @@ template <typename X> struct Part {
 // The k largest logits cost the streaming pass almost nothing: a thread keeps the largest logit of every group (a few
 // vectors) that it reads.  Afterwards a bound B is found that at least k group maxima reach; every logit above B lies in a
 // group whose maximum is above B, and those few groups are read again.
-constexpr int U = 4;                 // vectors per thread and step, all in flight
+constexpr int U = 4;                 // vectors per thread and step, all in flight, two by two from neighbouring places
 constexpr int MAX_GROUPS = 32;       // groups per thread
 constexpr int GROUP_LIST = 256;      // groups read again
 constexpr int KEY_LIST = 1024;       // candidates
@@ -199,7 +200,7 @@ template <typename X, int TPB> __device__ __forceinline__ void gather_groups(con
   const unsigned per = unsigned(steps) * U;                          // vectors per group
 #pragma unroll 1
   for (unsigned i = threadIdx.x; i < listed * per; i += TPB) {
-    const unsigned gi = s.group[i / per], v = gi % TPB + (gi / TPB * per + i % per) * TPB;
+    const unsigned gi = s.group[i / per], j = i % per, v = 2 * (gi % TPB + (gi / TPB * (per / 2) + j / 2) * TPB) + j % 2;
     if (int64_t(v) >= p.nv) continue;
     const uint4 u = __ldg(p.vec + v);
     unsigned hit = 0;
@@ -420,9 +421,9 @@ __global__ void __launch_bounds__(TPB, 1024 / TPB) k_token_logprob(const X* __re
   const int64_t t = blockIdx.x / unsigned(ctas);
   Part<X> p;
   p.row = logits + t * a.ld;
-  // the vectors begin at the row's first 16-byte boundary
-  const int64_t to16 = int64_t((16 - (reinterpret_cast<uintptr_t>(p.row) & 15)) & 15) / int(sizeof(X));
-  const int first = int(min(a.V, to16)), all = (int(a.V) - first) / N, per = (all + ctas - 1) / ctas, v0 = min(all, rank * per);
+  // the vectors begin at the row's first 32-byte boundary
+  const int64_t to32 = int64_t((32 - (reinterpret_cast<uintptr_t>(p.row) & 31)) & 31) / int(sizeof(X));
+  const int first = int(min(a.V, to32)), all = (int(a.V) - first) / (2 * N) * 2, per = (all / 2 + ctas - 1) / ctas * 2, v0 = min(all, rank * per);
   p.nv = min(all - v0, per);
   p.vec = reinterpret_cast<const uint4*>(p.row + first) + v0;
   p.col0 = uint32_t(first) + uint32_t(v0) * N;
@@ -436,15 +437,18 @@ __global__ void __launch_bounds__(TPB, 1024 / TPB) k_token_logprob(const X* __re
     if (y >= 0) xy = to_f(p.row[y]);
   }
   const uint4 none = make_uint4(Vec<X>::NONE, Vec<X>::NONE, Vec<X>::NONE, Vec<X>::NONE);
-  const uint4* ptr = p.vec + threadIdx.x;
+  const uint4* ptr = p.vec + 2 * threadIdx.x;
   const int nv = int(p.nv), n_full = nv / (TPB * U), n_steps = (nv + TPB * U - 1) / (TPB * U);
   auto load = [&](int step, uint4 (&u)[U]) {
     if (step < n_full) {
 #pragma unroll
-      for (int i = 0; i < U; ++i) u[i] = load_stream(ptr + i * TPB);
+      for (int i = 0; i < U; i += 2) load_stream(ptr + i * TPB, u[i], u[i + 1]);
     } else {
 #pragma unroll
-      for (int i = 0; i < U; ++i) u[i] = step * TPB * U + i * TPB + int(threadIdx.x) < nv ? load_stream(ptr + i * TPB) : none;
+      for (int i = 0; i < U; i += 2) {
+        u[i] = u[i + 1] = none;
+        if ((step * U + i) * TPB + 2 * int(threadIdx.x) < nv) load_stream(ptr + i * TPB, u[i], u[i + 1]);
+      }
     }
     ptr += U * TPB;
   };

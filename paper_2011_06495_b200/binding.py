@@ -276,7 +276,7 @@ def mv_embed(weight, ids, out, scale: float = 1.0, stream: Optional[torch.cuda.S
     o, o_type, T, Do, ldo, dev_o = _matrix(out, _VALUES, "mv_embed")
     i, i_type = _vector(ids, T, _IDS, dev, "mv_embed")
     _need(Do == D and dev_o == dev, "mv_embed")
-    _check(load().mv_embed(_raw_stream(dev, stream), w, w_type, V, D, ldw, i, i_type, T, scale, o, o_type, ldo), "mv_embed")
+    _check(load().mv_embed(_raw_stream(dev, stream), w, w_type, V, D, ldw, i, i_type, T, float(scale), o, o_type, ldo), "mv_embed")
 
 
 def embed_grad_workspace_bytes(T: int, V: int, D: int) -> int:
@@ -290,7 +290,7 @@ def mv_embed_grad(dout, ids, dweight, workspace, scale: float = 1.0, pad_id: int
     d, _, V, Dw, ldw, dev_w = _matrix(dweight, _FLOAT, "mv_embed_grad")
     i, i_type = _vector(ids, T, _IDS, dev, "mv_embed_grad")
     _need(Dw == D and dev_w == dev and workspace.get_device() == dev and workspace.is_contiguous(), "mv_embed_grad")
-    _check(load().mv_embed_grad(_raw_stream(dev, stream), x, x_type, ldd, i, i_type, T, V, D, scale, pad_id, bool(accumulate), d, ldw,
+    _check(load().mv_embed_grad(_raw_stream(dev, stream), x, x_type, ldd, i, i_type, T, V, D, float(scale), int(pad_id), bool(accumulate), d, ldw,
                                 workspace.data_ptr(), workspace.numel() * workspace.element_size()), "mv_embed_grad")
 
 
@@ -308,7 +308,7 @@ def mv_token_logprob(logits, targets=None, scale: float = 1.0, logprob=None, ent
             n, width = t.shape if t.dim() == 2 else (-1, 0)
             _need(n == T and t.dtype == kind and t.get_device() == dev and t.is_contiguous() and k in (None, width), where)
             k, tops[j] = width, t.data_ptr()
-    _check(load().mv_token_logprob(_raw_stream(dev, stream), x, x_type, T, V, ld, y, i_type, scale, k or 0, lp, h, l, tops[0], tops[1]), where)
+    _check(load().mv_token_logprob(_raw_stream(dev, stream), x, x_type, T, V, ld, y, i_type, float(scale), k or 0, lp, h, l, tops[0], tops[1]), where)
 
 
 def mv_token_logprob_grad(logits, targets, lse, g_logprob, dlogits, scale: float = 1.0, entropy=None, g_entropy=None,
@@ -322,7 +322,7 @@ def mv_token_logprob_grad(logits, targets, lse, g_logprob, dlogits, scale: float
     l, h = _vector(lse, T, _FLOAT, dev, where)[0], _vector(entropy, T, _FLOAT, dev, where)[0]
     g1, g2 = _vector(g_logprob, T, _FLOAT, dev, where)[0], _vector(g_entropy, T, _FLOAT, dev, where)[0]
     _need(d_type == x_type and Td == T and Vd == V and dev_d == dev, where)
-    _check(load().mv_token_logprob_grad(_raw_stream(dev, stream), x, x_type, T, V, ld, y, i_type, scale, l, h, g1, g2, d, ldg), where)
+    _check(load().mv_token_logprob_grad(_raw_stream(dev, stream), x, x_type, T, V, ld, y, i_type, float(scale), l, h, g1, g2, d, ldg), where)
 
 
 class MvClip:
@@ -373,13 +373,13 @@ class MvClip:
 
     def mv_clip_scale(self, max_norm: float, norms=None, stream: Optional[torch.cuda.Stream] = None):
         n, _ = _vector(norms, self.n_groups, _FLOAT, self.dev, "mv_clip_scale")
-        _check(self.lib.mv_clip_scale(self.handle, _raw_stream(self.dev, stream), max_norm, n), "mv_clip_scale")
+        _check(self.lib.mv_clip_scale(self.handle, _raw_stream(self.dev, stream), float(max_norm), n), "mv_clip_scale")
 
     def mv_clip_pack(self, max_norm: float, rows, norms=None, stream: Optional[torch.cuda.Stream] = None):
         n, _ = _vector(norms, self.n_groups, _FLOAT, self.dev, "mv_clip_pack")
         r, _, G, d, ld, dev = _matrix(rows, _FLOAT, "mv_clip_pack")
         _need(G == self.n_groups and d >= self.longest and dev == self.dev, "mv_clip_pack")
-        _check(self.lib.mv_clip_pack(self.handle, _raw_stream(self.dev, stream), max_norm, r, ld, n), "mv_clip_pack")
+        _check(self.lib.mv_clip_pack(self.handle, _raw_stream(self.dev, stream), float(max_norm), r, ld, n), "mv_clip_pack")
 
 
 class MvContext:

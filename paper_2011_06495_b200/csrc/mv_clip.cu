@@ -337,22 +337,24 @@ int clip_run(mv_clip* p, cudaStream_t st, float max_norm, float* rows, int64_t l
   ClipArgs a = p->args;
   a.max_norm = max_norm; a.rows = rows; a.ld = ld; a.norms = norms;
   const unsigned grid = unsigned(p->n > 0 ? p->n : 1);
-  if (apply && p->n <= HOLD) {
-    k_clip_hold<<<grid, TPB, 0, st>>>(a);
-    return cuda_ok();
-  }
-  k_clip_sum<<<grid, TPB, 0, st>>>(a);
-  if (!apply) return cuda_ok();
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(grid);
   cfg.blockDim = dim3(TPB);
   cfg.stream = st;
-  cudaLaunchAttribute early = {};
-  early.id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  early.val.programmaticStreamSerializationAllowed = 1;
-  cfg.attrs = &early;
+  cudaLaunchAttribute attr = {};
+  cfg.attrs = &attr;
   cfg.numAttrs = 1;
-  const bool ok = cudaLaunchKernelEx(&cfg, k_clip_scale, a) == cudaSuccess;
+  bool ok;
+  if (apply && p->n <= HOLD) {
+    attr.id = cudaLaunchAttributeCooperative;        // all CTAs at once or none: they wait for one another
+    attr.val.cooperative = 1;
+    ok = cudaLaunchKernelEx(&cfg, k_clip_hold, a) == cudaSuccess;
+  } else {
+    k_clip_sum<<<grid, TPB, 0, st>>>(a);
+    attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr.val.programmaticStreamSerializationAllowed = 1;
+    ok = !apply || cudaLaunchKernelEx(&cfg, k_clip_scale, a) == cudaSuccess;
+  }
   return cuda_ok() == MV_OK && ok ? MV_OK : MV_ERR_CUDA;
 }
 

@@ -148,7 +148,7 @@ struct TopSmem {
   unsigned long long key[KEY_LIST];
   unsigned long long best[MV_TOP_MAX];
   uint16_t group[GROUP_LIST];
-  float sorted[16][32];              // of each warp
+  float sorted[8][32];               // of each warp
   float bound;
   int n_key, n_group, found;
 };
@@ -732,13 +732,12 @@ int mv_token_logprob(void* stream, const void* logits, int type, int64_t T, int6
   return with_type(type, [&](auto x) {
     using X = decltype(x);
     const int64_t vecs = V / Vec<X>::N;
-    // Many rows: small CTAs, whose ends overlap with the others' streaming (8192 x 65536 bf16, k = 16: 195 us, with 256 threads 222).
-    // Rows for less than two waves of those: 256 threads (1003 x 50021 fp32: 47 us, with 128 threads 49).  Fewer rows than
-    // multiprocessors: 512 threads, and as many CTAs per row (up to the eight of a portable cluster) as keep a whole step for
-    // each thread and fit the device at once; with more rows than that, clusters only cost (two CTAs per row: 246 us).
-    const int tpb = T < 148 ? 512 : T < 148 * 16 ? 256 : 128;
-    int ctas = 1;
-    while (T < 148 && ctas < 8 && T * ctas * tpb < 148 * 1024 && vecs >= int64_t(ctas) * 2 * tpb * U) ctas *= 2;
+    // A CTA per row: 128 threads for many rows of ordinary length, so that the ends of some (choosing the alternatives) overlap
+    // with the streaming of others (3000 rows of 131 KB: 81 us, with 256 threads 86; of 16 KB: 22 and 36), 256 for fewer rows than
+    // there are places for CTAs or for long ones (3000 rows of 200 KB: 123 us, with 128 threads 136; 100 rows: 11.3 and 14.4).
+    // A few long rows: a cluster of four per row, a step or more for each thread (one row of 200 KB: 8.8 us, with one CTA 10.3).
+    const int tpb = T < 600 || vecs > 10240 ? 256 : 128;
+    const int ctas = T <= 16 && vecs >= 4 * 256 * U ? 4 : 1;
     const int64_t n_steps = ((vecs + ctas - 1) / ctas + tpb * U - 1) / (tpb * U);
     a.steps = int((n_steps + MAX_GROUPS - 1) / MAX_GROUPS);
     if (a.steps < 1) a.steps = 1;
@@ -753,14 +752,9 @@ int mv_token_logprob(void* stream, const void* logits, int type, int64_t T, int6
     attr.val.clusterDim.x = unsigned(ctas);
     attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
     cfg.attrs = &attr;
-    cfg.numAttrs = 1;
+    cfg.numAttrs = ctas > 1;
     auto* kernel = tpb == 128 ? (k ? k_token_logprob<X, true, 128> : k_token_logprob<X, false, 128>)
-                 : tpb == 256 ? (k ? k_token_logprob<X, true, 256> : k_token_logprob<X, false, 256>)
-                              : (k ? k_token_logprob<X, true, 512> : k_token_logprob<X, false, 512>);
-    if (cfg.dynamicSmemBytes > 32 << 10 && cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 64 << 10) != cudaSuccess) {
-      cudaGetLastError();
-      return int(MV_ERR_CUDA);
-    }
+                              : (k ? k_token_logprob<X, true, 256> : k_token_logprob<X, false, 256>);
     const bool ok = cudaLaunchKernelEx(&cfg, kernel, static_cast<const X*>(logits), a) == cudaSuccess;
     return cuda_ok() == MV_OK && ok ? int(MV_OK) : int(MV_ERR_CUDA);
   });

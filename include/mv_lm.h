@@ -91,7 +91,8 @@ typedef struct mv_clip mv_clip;
 size_t mv_clip_workspace_bytes(const int64_t* numel, int n_tensors, int n_groups);
 
 /* Creates a plan.  All arrays are HOST arrays, read before the call returns.
- *   tensors [n_tensors] device pointers, contiguous tensors;  types MV_F32 / MV_BF16 / MV_F16;  numel >= 0, below 2^40
+ *   tensors [n_tensors] device pointers, contiguous tensors that share no bytes;  types MV_F32 / MV_BF16 / MV_F16;
+ *           numel >= 0, below 2^40
  *   groups  [n_tensors] ascending, 0 <= groups[i] < n_groups: the tensors that share a norm (NULL: all in group 0)
  *   workspace  mv_clip_workspace_bytes() bytes, 256-byte aligned, owned by the caller, must outlive the plan
  * The list is copied to the workspace on `stream`, and the call waits for that copy: not inside a stream capture.
@@ -100,7 +101,10 @@ int mv_clip_create(mv_clip** out, void* stream, void* const* tensors, const int*
                    int n_tensors, int n_groups, void* workspace, size_t workspace_bytes);
 int mv_clip_destroy(mv_clip* plan);
 
-/* norms [n_groups] float out: sqrt of the sum of squares, added in 64 bits and rounded once (0 for an empty group). */
+/* The calls on a plan.  A short list (up to 14 MB) is clipped by one cooperative kernel whose CTAs wait, with a limit, for
+ * their group's factor; should a wait ever run out (never expected), what the CTA writes is NaN.
+ *
+ * norms [n_groups] float out: sqrt of the sum of squares, added in 64 bits and rounded once (0 for an empty group). */
 int mv_clip_norm(mv_clip* plan, void* stream, float* norms);
 
 /* In place: every tensor of group g is multiplied by c_g = min(1, max_norm / n_g), max_norm >= 0 (+inf: no clipping).

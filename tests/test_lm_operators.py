@@ -161,6 +161,23 @@ def test_embed_grad_of_text_like_tokens_and_of_one_token_only():
     check_grad(100, 2_500_003, 1, F32, accumulate=True)
 
 
+@pytest.mark.parametrize("it", [torch.int32, torch.int64])
+@pytest.mark.parametrize("T", [255, 256, 257, 8191, 8192, 8193, 40_000])
+def test_embed_grad_of_ids_that_start_anywhere(T, it):
+    """The ids are read 16 bytes at a time where they are aligned; stretches of whole and of broken batches; ids of other
+    words (beyond 32 bits, negative) among them; long stretches of one id, as padding leaves them."""
+    g = gen(T)
+    ids = torch.randint(0, 700, (T + 3,), generator=g, device=DEV).to(it)
+    ids[T // 3: T // 2] = 5
+    ids[::17] = -1
+    if it == torch.int64:
+        ids[::19] = (1 << 32) + 3
+        ids[::23] = -(1 << 40)
+    for off in (0, 1, 3):
+        check_grad(T, 700, 20, F32, it, ids=ids[off:off + T])
+        check_grad(T, 700, 20, BF16, it, ids=ids[off:off + T], pad_id=5, accumulate=True)
+
+
 def test_embed_grad_past_32_bit_offsets():
     V, D, T = 70_000, 32_768, 6
     ids = torch.tensor([V - 1, 65_537, 0, V - 1, 65_536, 9], device=DEV)
@@ -297,6 +314,35 @@ def test_logprob_of_masked_flat_and_extreme_rows(dt, V):
     # the rows one by one: a row's result does not depend on its neighbours
     for r in (0, 2, 6, 11, 13):
         check_logprob(x[r:r + 1], targets[r:r + 1], 1.0, 20)
+
+
+@pytest.mark.parametrize("dt", [F32, BF16, F16])
+@pytest.mark.parametrize("V,copies,pad", [(5000, 50, 1), (12_001, 60, 0), (90_001, 60, 3), (40_960, 1, 0)])
+def test_the_same_rows_in_batches_of_every_kind(dt, V, copies, pad):
+    """Twelve kinds of rows, among them empty, flat, tied and extreme ones, in batches that are cut among CTAs differently."""
+    low, g = torch.finfo(dt).min, gen(V)
+    x = (torch.randn((12, V), generator=g, device=DEV) * 3.0).to(dt)
+    x[0] = -math.inf
+    x[1] = low
+    x[2] = 0.75
+    x[3] = torch.linspace(-9, 9, V, device=DEV).to(dt)
+    x[4, torch.rand(V, generator=g, device=DEV) < 0.999] = -math.inf
+    x[5] = torch.randint(0, 4, (V,), generator=g, device=DEV).to(dt)
+    x[6, : V // 2] = low
+    x[7, V - 1] = 50.0
+    x[8] = torch.finfo(dt).max
+    x[9, ::2] = -math.inf
+    x[10, : V - 70] = low                                  # the part before the last logits is all masked
+    big, _ = strided(12 * copies, V, dt, pad, 0, fill=0.0)
+    big.copy_(x.repeat(copies, 1))
+    y = torch.randint(-1, V, (12,), generator=g, device=DEV)
+    for k in (0, 3, 33):
+        want = logprob_reference(x, y, 1.0, k)
+        got = call_logprob(big, y.repeat(copies), 1.0, k)
+        for n in ("lse", "entropy", "logprob") + (("top",) if k else ()):
+            close(got[n], tuple(w.repeat(copies, *([1] * (w.dim() - 1))) for w in want[n]), n)
+        if k:
+            assert torch.equal(got["ids"].long().cpu(), want["ids"].repeat(copies, 1))
 
 
 @pytest.mark.parametrize("dt", [F32, BF16, F16])
@@ -632,6 +678,49 @@ def test_a_step_from_tokens_to_the_shared_mask():
         losses = [m.step() for _ in range(30)]
         assert losses[-1] < losses[0] - 0.3
     m.check_gradients()
+
+
+def test_the_calls_can_be_captured_and_replayed_on_new_inputs():
+    """Every call enqueues kernels and nothing else: captured once into a graph, replayed after the inputs have changed, it gives
+    what a call on another stream gives."""
+    T, V, D = 300, 5000, 96
+    g = gen(8)
+    w, ids = torch.randn((V, D), generator=g, device=DEV), torch.randint(0, V, (T,), generator=g, device=DEV)
+    lg, gl = torch.randn((T, V), generator=g, device=DEV).to(BF16), torch.randn(T, generator=g, device=DEV)
+    small, large = torch.randn(300_000, generator=g, device=DEV), torch.randn(6_000_000, generator=g, device=DEV)
+    plans = [B.MvClip([small]), B.MvClip([large])]
+    ws = torch.empty(B.embed_grad_workspace_bytes(T, V, D), dtype=torch.uint8, device=DEV)
+
+    def outputs():
+        f = lambda *shape, **k: torch.zeros(*shape, device=DEV, **k)
+        return [f(T, D), f(V, D), f(T), f(T), f(T), f(T, 4), f(T, 4, dtype=torch.int32), f(T, V, dtype=BF16), f(1, 300_000), f(1), f(1, 6_000_000), f(1)]
+
+    def run(o, stream=None):
+        B.mv_embed(w, ids, o[0], scale=2.0, stream=stream)
+        B.mv_embed_grad(o[0], ids, o[1], ws, stream=stream)
+        B.mv_token_logprob(lg, ids, logprob=o[2], entropy=o[3], lse=o[4], top_logprob=o[5], top_id=o[6], stream=stream)
+        B.mv_token_logprob_grad(lg, ids, o[4], gl, o[7], stream=stream)
+        for p, r, n in ((plans[0], o[8], o[9]), (plans[1], o[10], o[11])):
+            p.mv_clip_pack(1.0, r, n, stream=stream)
+
+    a, b = outputs(), outputs()
+    run(a)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        run(a)
+    ids.copy_(torch.randint(0, V, (T,), generator=g, device=DEV))
+    lg.copy_(torch.randn((T, V), generator=g, device=DEV))
+    small.mul_(3.0)
+    large.mul_(0.5)
+    graph.replay()
+    graph.replay()
+    torch.cuda.synchronize()
+    st = torch.cuda.Stream()
+    run(b, st)
+    st.synchronize()
+    for i, (x, y) in enumerate(zip(a, b)):
+        assert torch.equal(x, y), i
 
 
 def test_shapes_and_types_that_do_not_fit_are_refused():

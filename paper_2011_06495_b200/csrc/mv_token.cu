@@ -10,6 +10,7 @@
 
 #include <cooperative_groups.h>
 #include <math.h>
+#include <type_traits>
 
 namespace {
 
@@ -141,14 +142,14 @@ template <typename X> struct Part {
 // group whose maximum is above B, and those few groups are read again.
 constexpr int U = 4;                 // vectors per thread and step, all in flight, two by two from neighbouring places
 constexpr int MAX_GROUPS = 32;       // groups per thread
-constexpr int GROUP_LIST = 256;      // groups read again
-constexpr int KEY_LIST = 1024;       // candidates
 
-struct TopSmem {
+template <int TPB> struct TopSmem {
+  static constexpr int GROUP_LIST = 256;                    // groups read again
+  static constexpr int KEY_LIST = TPB >= 128 ? 1024 : 256;  // candidates
   unsigned long long key[KEY_LIST];
   unsigned long long best[MV_TOP_MAX];
   uint16_t group[GROUP_LIST];
-  float sorted[8][32];               // of each warp
+  float sorted[TPB / 32][32];        // of each warp
   float bound;
   int n_key, n_group, found;
 };
@@ -177,13 +178,13 @@ template <typename X, typename F> __device__ __forceinline__ void each_logit(con
   }
 }
 
-__device__ __forceinline__ void push_key(TopSmem& s, float x, uint32_t col) {
+template <int TPB> __device__ __forceinline__ void push_key(TopSmem<TPB>& s, float x, uint32_t col) {
   const int i = atomicAdd(&s.n_key, 1);
-  if (i < KEY_LIST) s.key[i] = make_key(x, col);
+  if (i < s.KEY_LIST) s.key[i] = make_key(x, col);
 }
 
 // Every candidate's place is the number of candidates before it.
-template <int TPB> __device__ __forceinline__ void rank_keys(TopSmem& s, int n, int k) {
+template <int TPB> __device__ __forceinline__ void rank_keys(TopSmem<TPB>& s, int n, int k) {
 #pragma unroll 1
   for (int i = threadIdx.x; i < n; i += TPB) {
     const unsigned long long mine = s.key[i];
@@ -195,7 +196,7 @@ template <int TPB> __device__ __forceinline__ void rank_keys(TopSmem& s, int n, 
 }
 
 // The elements of the listed groups that reach the bound (or lie above it) become candidates.
-template <typename X, int TPB> __device__ __forceinline__ void gather_groups(const Part<X>& p, int listed, int steps, bool above, TopSmem& s) {
+template <typename X, int TPB> __device__ __forceinline__ void gather_groups(const Part<X>& p, int listed, int steps, bool above, TopSmem<TPB>& s) {
   const float B = s.bound;
   const unsigned per = unsigned(steps) * U;                          // vectors per group
 #pragma unroll 1
@@ -213,7 +214,7 @@ template <typename X, int TPB> __device__ __forceinline__ void gather_groups(con
 }
 
 // The groups whose maximum reaches the bound (or lies above it).
-template <int TPB> __device__ __forceinline__ void list_groups(const float* gmax, int groups, bool above, TopSmem& s) {
+template <int TPB> __device__ __forceinline__ void list_groups(const float* gmax, int groups, bool above, TopSmem<TPB>& s) {
   const float B = s.bound;
 #pragma unroll 1
   for (int g0 = 0; g0 < groups; g0 += 8) {
@@ -226,14 +227,14 @@ template <int TPB> __device__ __forceinline__ void list_groups(const float* gmax
     if (hit == 0) continue;
     int i = atomicAdd(&s.n_group, __popc(hit));
     for (; hit; hit &= hit - 1, ++i)
-      if (i < GROUP_LIST) s.group[i] = uint16_t((g0 + __ffs(int(hit)) - 1) * TPB + threadIdx.x);
+      if (i < s.GROUP_LIST) s.group[i] = uint16_t((g0 + __ffs(int(hit)) - 1) * TPB + threadIdx.x);
   }
 }
 
 // Rows with crowds: many groups at the bound itself (few distinct values; fewer logits than k left by a mask), or large
 // logits crowded in the columns of few threads.  Not inlined: seldom run.
 template <typename X, int TPB>
-__device__ __noinline__ void best_of_crowd(const Part<X>& p, int k, const float* gmax, int groups, int steps, float mine, TopSmem& s) {
+__device__ __noinline__ void best_of_crowd(const Part<X>& p, int k, const float* gmax, int groups, int steps, float mine, TopSmem<TPB>& s) {
   constexpr int WARPS = TPB / 32;
   const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
   const float B = s.bound;
@@ -252,9 +253,9 @@ __device__ __noinline__ void best_of_crowd(const Part<X>& p, int k, const float*
   if (mine > B) list_groups<TPB>(gmax, groups, true, s);
   __syncthreads();
   const int above = s.n_group;
-  gather_groups<X, TPB>(p, min(above, GROUP_LIST), steps, true, s);
+  gather_groups<X, TPB>(p, min(above, s.GROUP_LIST), steps, true, s);
   __syncthreads();
-  bool whole = above <= GROUP_LIST && s.n_key <= KEY_LIST;
+  bool whole = above <= s.GROUP_LIST && s.n_key <= s.KEY_LIST;
   if (whole) {
     // the logits at the bound, in order from the start of the part until k of them are found (they are many)
 #pragma unroll 1
@@ -283,7 +284,7 @@ __device__ __noinline__ void best_of_crowd(const Part<X>& p, int k, const float*
       __syncthreads();
       if (all >= k) break;
     }
-    whole = s.n_key <= KEY_LIST;
+    whole = s.n_key <= s.KEY_LIST;
   }
   if (whole) {
     rank_keys<TPB>(s, s.n_key, k);
@@ -318,12 +319,12 @@ __device__ __noinline__ void best_of_crowd(const Part<X>& p, int k, const float*
 // The k best keys of this part, in order, in s.best (0 where there are fewer).  All threads; ends with a barrier.  The
 // code is kept short: it runs once per row, and with one wave of rows its instructions come from memory.
 template <typename X, int TPB>
-__device__ __forceinline__ void best_of_part(const Part<X>& p, int k, const float* gmax, int groups, int steps, float mine, TopSmem& s) {
+__device__ __forceinline__ void best_of_part(const Part<X>& p, int k, const float* gmax, int groups, int steps, float mine, TopSmem<TPB>& s) {
   constexpr int WARPS = TPB / 32;
   const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
   s.sorted[w][lane] = sort_warp(mine);
   if (threadIdx.x == 0) { s.n_key = 0; s.n_group = 0; }
-  if (threadIdx.x < MV_TOP_MAX) s.best[threadIdx.x] = 0;
+  for (int i = threadIdx.x; i < MV_TOP_MAX; i += TPB) s.best[i] = 0;
   __syncthreads();
   // the single logits at the ends are always candidates
   if (threadIdx.x < p.head + p.tail) {
@@ -353,10 +354,10 @@ __device__ __forceinline__ void best_of_part(const Part<X>& p, int k, const floa
   if (mine >= s.bound) list_groups<TPB>(gmax, groups, false, s);
   __syncthreads();
   const int listed = s.n_group;
-  if (listed <= GROUP_LIST) gather_groups<X, TPB>(p, listed, steps, false, s);
+  if (listed <= s.GROUP_LIST) gather_groups<X, TPB>(p, listed, steps, false, s);
   __syncthreads();
   const int n = s.n_key;
-  if (listed <= GROUP_LIST && n <= KEY_LIST) rank_keys<TPB>(s, n, k);
+  if (listed <= s.GROUP_LIST && n <= s.KEY_LIST) rank_keys<TPB>(s, n, k);
   else best_of_crowd<X, TPB>(p, k, gmax, groups, steps, mine, s);
   __syncthreads();
 }
@@ -414,7 +415,7 @@ __global__ void __launch_bounds__(TPB, 1024 / TPB) k_token_logprob(const X* __re
   extern __shared__ float gmax[];    // [group][thread], with TOP
   __shared__ Sums s_sums[WARPS];
   __shared__ Sums s_part;
-  __shared__ TopSmem s_top[1];
+  __shared__ TopSmem<TPB> s_top[1];
   const cg::cluster_group cluster = cg::this_cluster();
   const int ctas = int(cluster.num_blocks()), rank = int(cluster.block_rank());
   const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
@@ -575,7 +576,7 @@ __global__ void __launch_bounds__(TPB, 1024 / TPB) k_token_logprob(const X* __re
       if (TOP) {
         for (int i = threadIdx.x; i < ctas * a.k; i += TPB) s_top[0].key[i] = cluster.map_shared_rank(&s_top[0], unsigned(i / a.k))->best[i % a.k];
         __syncthreads();
-        if (threadIdx.x < MV_TOP_MAX) s_top[0].best[threadIdx.x] = 0;
+        for (int i = threadIdx.x; i < MV_TOP_MAX; i += TPB) s_top[0].best[i] = 0;
         __syncthreads();
         rank_keys<TPB>(s_top[0], ctas * a.k, a.k);
         __syncthreads();
@@ -591,12 +592,13 @@ __global__ void __launch_bounds__(TPB, 1024 / TPB) k_token_logprob(const X* __re
     if (a.entropy) a.entropy[t] = empty ? 0.0f : ls - LN2 * (x.st / x.s);
     if (a.logprob) a.logprob[t] = y < 0 ? 0.0f : empty ? -INFINITY : (xy - r) * a.scale - ls;
   }
-  if (TOP && int(threadIdx.x) < a.k) {
-    const unsigned long long key = s_top[0].best[threadIdx.x];
-    const float v = key_value(key);
-    if (a.top_id) a.top_id[t * a.k + threadIdx.x] = key ? int32_t(key_index(key)) : -1;
-    if (a.top_logprob) a.top_logprob[t * a.k + threadIdx.x] = isnan(x.s) ? x.s : key == 0 || v == -INFINITY ? -INFINITY : (v - r) * a.scale - ls;
-  }
+  if (TOP)
+    for (int i = threadIdx.x; i < a.k; i += TPB) {
+      const unsigned long long key = s_top[0].best[i];
+      const float v = key_value(key);
+      if (a.top_id) a.top_id[t * a.k + i] = key ? int32_t(key_index(key)) : -1;
+      if (a.top_logprob) a.top_logprob[t * a.k + i] = isnan(x.s) ? x.s : key == 0 || v == -INFINITY ? -INFINITY : (v - r) * a.scale - ls;
+    }
 }
 
 // ------------------------------------------------------------------------------------------ gradient
@@ -732,11 +734,15 @@ int mv_token_logprob(void* stream, const void* logits, int type, int64_t T, int6
   return with_type(type, [&](auto x) {
     using X = decltype(x);
     const int64_t vecs = V / Vec<X>::N;
-    // A CTA per row: 128 threads for many rows of ordinary length, so that the ends of some (choosing the alternatives) overlap
-    // with the streaming of others (3000 rows of 131 KB: 81 us, with 256 threads 86; of 16 KB: 22 and 36), 256 for fewer rows than
-    // there are places for CTAs or for long ones (3000 rows of 200 KB: 123 us, with 128 threads 136; 100 rows: 11.3 and 14.4).
+    // A CTA per row.  Its end (choosing the alternatives) is a chain of short phases, so short rows take few threads and many
+    // CTAs, if there are rows enough to fill the device: 16000 rows of 16 KB, k = 8: 62 us with 32 threads, 73 with 64, 102 with 128;
+    // 9079 rows of 33 KB: 77, 70, 84.  Rows in the hundreds take more threads than that (1003 of 16 KB: 10.4, 9.5, 9.6), long ones
+    // more still (3000 of 131 KB: 81 us with 128, 86 with 256; of 200 KB: 136 and 123; 100 of 200 KB: 14.4 and 11.3).
     // A few long rows: a cluster of four per row, a step or more for each thread (one row of 200 KB: 8.8 us, with one CTA 10.3).
-    const int tpb = T < 600 || vecs > 10240 ? 256 : 128;
+    // 32 threads have too few maxima to bound more than 32 alternatives.
+    const int tpb = T >= 2368 && vecs <= 2047 && k <= 32 ? 32
+                  : T >= 1184 && vecs <= 3072 ? 64
+                  : vecs > 10240 || (T < 600 && vecs > 6000) ? 256 : 128;
     const int ctas = T <= 16 && vecs >= 4 * 256 * U ? 4 : 1;
     const int64_t n_steps = ((vecs + ctas - 1) / ctas + tpb * U - 1) / (tpb * U);
     a.steps = int((n_steps + MAX_GROUPS - 1) / MAX_GROUPS);
@@ -753,8 +759,12 @@ int mv_token_logprob(void* stream, const void* logits, int type, int64_t T, int6
     attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
     cfg.attrs = &attr;
     cfg.numAttrs = ctas > 1;
-    auto* kernel = tpb == 128 ? (k ? k_token_logprob<X, true, 128> : k_token_logprob<X, false, 128>)
-                              : (k ? k_token_logprob<X, true, 256> : k_token_logprob<X, false, 256>);
+    auto pick = [&](auto top) {
+      constexpr bool TOP = decltype(top)::value;
+      return tpb == 32 ? k_token_logprob<X, TOP, 32> : tpb == 64 ? k_token_logprob<X, TOP, 64>
+           : tpb == 128 ? k_token_logprob<X, TOP, 128> : k_token_logprob<X, TOP, 256>;
+    };
+    auto* kernel = k ? pick(std::true_type()) : pick(std::false_type());
     const bool ok = cudaLaunchKernelEx(&cfg, kernel, static_cast<const X*>(logits), a) == cudaSuccess;
     return cuda_ok() == MV_OK && ok ? int(MV_OK) : int(MV_ERR_CUDA);
   });

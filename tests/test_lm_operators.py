@@ -317,7 +317,7 @@ def test_logprob_of_masked_flat_and_extreme_rows(dt, V):
 
 
 @pytest.mark.parametrize("dt", [F32, BF16, F16])
-@pytest.mark.parametrize("V,copies,pad", [(5000, 50, 1), (12_001, 60, 0), (90_001, 60, 3), (40_960, 1, 0)])
+@pytest.mark.parametrize("V,copies,pad", [(5000, 50, 1), (12_001, 60, 0), (90_001, 60, 3), (40_960, 1, 0), (3001, 220, 2), (9000, 220, 0), (12_003, 110, 1), (40, 220, 0)])
 def test_the_same_rows_in_batches_of_every_kind(dt, V, copies, pad):
     """Twelve kinds of rows, among them empty, flat, tied and extreme ones, in batches that are cut among CTAs differently."""
     low, g = torch.finfo(dt).min, gen(V)
@@ -332,7 +332,7 @@ def test_the_same_rows_in_batches_of_every_kind(dt, V, copies, pad):
     x[7, V - 1] = 50.0
     x[8] = torch.finfo(dt).max
     x[9, ::2] = -math.inf
-    x[10, : V - 70] = low                                  # the part before the last logits is all masked
+    x[10, : max(0, V - 70)] = low                                # the part before the last logits is all masked
     big, _ = strided(12 * copies, V, dt, pad, 0, fill=0.0)
     big.copy_(x.repeat(copies, 1))
     y = torch.randint(-1, V, (12,), generator=g, device=DEV)

@@ -201,7 +201,7 @@ template <typename X, int TPB> __device__ __forceinline__ void gather_groups(con
   const unsigned per = unsigned(steps) * U;                          // vectors per group
 #pragma unroll 1
   for (unsigned i = threadIdx.x; i < listed * per; i += TPB) {
-    const unsigned gi = s.group[i / per], j = i % per, v = 2 * (gi % TPB + (gi / TPB * (per / 2) + j / 2) * TPB) + j % 2;
+    const unsigned q = steps == 1 ? i / U : i / per, gi = s.group[q], j = i - q * per, v = 2 * (gi % TPB + (gi / TPB * (per / 2) + j / 2) * TPB) + j % 2;
     if (int64_t(v) >= p.nv) continue;
     const uint4 u = __ldg(p.vec + v);
     unsigned hit = 0;
@@ -316,16 +316,18 @@ __device__ __noinline__ void best_of_crowd(const Part<X>& p, int k, const float*
   }
 }
 
-// The k best keys of this part, in order, in s.best (0 where there are fewer).  All threads; ends with a barrier.  The
-// code is kept short: it runs once per row, and with one wave of rows its instructions come from memory.
+// What the choice of the best needs before the next barrier.
+template <int TPB> __device__ __forceinline__ void begin_best(float mine, TopSmem<TPB>& s) {
+  s.sorted[threadIdx.x >> 5][threadIdx.x & 31] = sort_warp(mine);
+  if (threadIdx.x == 0) { s.n_key = 0; s.n_group = 0; }
+  for (int i = threadIdx.x; i < MV_TOP_MAX; i += TPB) s.best[i] = 0;
+}
+
+// The k best keys of this part, in order, in s.best (0 where there are fewer).  All threads; ends with a barrier.
 template <typename X, int TPB>
 __device__ __forceinline__ void best_of_part(const Part<X>& p, int k, const float* gmax, int groups, int steps, float mine, TopSmem<TPB>& s) {
   constexpr int WARPS = TPB / 32;
   const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
-  s.sorted[w][lane] = sort_warp(mine);
-  if (threadIdx.x == 0) { s.n_key = 0; s.n_group = 0; }
-  for (int i = threadIdx.x; i < MV_TOP_MAX; i += TPB) s.best[i] = 0;
-  __syncthreads();
   // the single logits at the ends are always candidates
   if (threadIdx.x < p.head + p.tail) {
     const uint32_t col = threadIdx.x < p.head ? threadIdx.x : p.tail_col + threadIdx.x - p.head;
@@ -408,7 +410,12 @@ __device__ __noinline__ Sums sums_of_extremes(const Part<X>& p, float c2, float*
   return x;
 }
 
-// A row belongs to a cluster of CTAs (one CTA when there are rows enough), each of which streams a part of it once.
+// A row belongs to a CTA (to a cluster of CTAs when there are few), each of which streams its part once, two steps of 64 bytes a
+// lane on their way.  Per 16 bytes of bf16 a lane spends about 40 instructions, eight of them exponentials, which the
+// multiprocessor does at 16 a cycle against the 11.4 logits a cycle that memory brings: so issue, the exponentials and memory
+// are all within a factor of two of one another, and under the power limit (1.68 GHz in a long run) the instructions count.
+// 8192 x 65536 bf16: 176 us without alternatives (6.1 TB/s), 196 us with 16 of them (213 us at the limit); the
+// alternatives' cost is the end of a row, about 2 us of latency that the other CTAs of the multiprocessor only partly cover.
 template <typename X, bool TOP, int TPB>
 __global__ void __launch_bounds__(TPB, 1024 / TPB) k_token_logprob(const X* __restrict__ logits, const __grid_constant__ LogprobArgs a) {
   constexpr int N = Vec<X>::N, WARPS = TPB / 32;
@@ -419,7 +426,7 @@ __global__ void __launch_bounds__(TPB, 1024 / TPB) k_token_logprob(const X* __re
   const cg::cluster_group cluster = cg::this_cluster();
   const int ctas = int(cluster.num_blocks()), rank = int(cluster.block_rank());
   const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
-  const int64_t t = blockIdx.x / unsigned(ctas);
+  const int64_t t = ctas == 1 ? blockIdx.x : blockIdx.x / unsigned(ctas);
   Part<X> p;
   p.row = logits + t * a.ld;
   // the vectors begin at the row's first 32-byte boundary
@@ -534,31 +541,33 @@ __global__ void __launch_bounds__(TPB, 1024 / TPB) k_token_logprob(const X* __re
     const float d = ref == -INFINITY ? 0.0f : fmaf(ref, c2, -R), f = 1.0f - LN2 * d;      // d: at most half a unit of R; 2^-d
     x = {ref, (p0 + p1) * f, fmaf(-d, p0 + p1, q0 + q1) * f};
   }
-  const float top = fmaxf(mine, extra);
-  // logits that the fused form cannot take: too large ones anywhere, or nothing but too small ones
-  if (__syncthreads_or(top * c2 > R_MAX) || (!__syncthreads_or(ref != -INFINITY) && __syncthreads_or(top > -INFINITY)))
-    x = sums_of_extremes<X, TPB>(p, c2, &s_sums[0].ref);
-  // the threads' sums to one reference, warp by warp and then together
-  float m = x.ref;
+  // the sums of `width` neighbouring lanes to one reference
+  auto fold = [&](int width) {
+    float m = x.ref;
 #pragma unroll
-  for (int o = 16; o; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
-  x = shift(x, m, c2);
+    for (int o = width / 2; o; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+    x = shift(x, m, c2);
 #pragma unroll
-  for (int o = 16; o; o >>= 1) {
-    x.s += __shfl_xor_sync(0xffffffffu, x.s, o);
-    x.st += __shfl_xor_sync(0xffffffffu, x.st, o);
-  }
+    for (int o = width / 2; o; o >>= 1) {
+      x.s += __shfl_xor_sync(0xffffffffu, x.s, o);
+      x.st += __shfl_xor_sync(0xffffffffu, x.st, o);
+    }
+  };
+  fold(32);
   if (lane == 0) s_sums[w] = x;
-  __syncthreads();
+  if (TOP) begin_best(mine, s_top[0]);
+  const float top = fmaxf(mine, extra);
+  const bool large = __syncthreads_or(top * c2 > R_MAX);
   x = s_sums[lane % WARPS];
-  m = x.ref;
-#pragma unroll
-  for (int o = WARPS / 2; o; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
-  x = shift(x, m, c2);
-#pragma unroll
-  for (int o = WARPS / 2; o; o >>= 1) {
-    x.s += __shfl_xor_sync(0xffffffffu, x.s, o);
-    x.st += __shfl_xor_sync(0xffffffffu, x.st, o);
+  fold(WARPS);
+  // logits that the fused form cannot take: too large ones anywhere, or nothing but too small ones
+  if (large || (x.ref == -INFINITY && __syncthreads_or(top > -INFINITY))) {
+    x = sums_of_extremes<X, TPB>(p, c2, &s_sums[0].ref);
+    fold(32);
+    if (lane == 0) s_sums[w] = x;
+    __syncthreads();
+    x = s_sums[lane % WARPS];
+    fold(WARPS);
   }
   if (TOP) best_of_part<X, TPB>(p, a.k, gmax, group, a.steps, mine, s_top[0]);
   if (ctas > 1) {
@@ -566,13 +575,7 @@ __global__ void __launch_bounds__(TPB, 1024 / TPB) k_token_logprob(const X* __re
     cluster.sync();
     if (rank == 0) {
       x = *cluster.map_shared_rank(&s_part, unsigned(lane % ctas));
-      m = x.ref;
-      for (int o = ctas / 2; o; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
-      x = shift(x, m, c2);
-      for (int o = ctas / 2; o; o >>= 1) {
-        x.s += __shfl_xor_sync(0xffffffffu, x.s, o);
-        x.st += __shfl_xor_sync(0xffffffffu, x.st, o);
-      }
+      fold(ctas);
       if (TOP) {
         for (int i = threadIdx.x; i < ctas * a.k; i += TPB) s_top[0].key[i] = cluster.map_shared_rank(&s_top[0], unsigned(i / a.k))->best[i % a.k];
         __syncthreads();
@@ -605,7 +608,8 @@ __global__ void __launch_bounds__(TPB, 1024 / TPB) k_token_logprob(const X* __re
 // dx = c (g1 (1[v = y] - p) - g2 p (log p + H)), log p = c x - lse.  With h = log2(p) / 2 and q = 2^h:
 // dx = q (q (A h + B)) + c g1 1[v = y], A = -2 ln 2 c g2, B = -c (g1 + g2 H): two fused multiply-adds, an exponential and two
 // products per logit.  p is formed as q q because the hardware's exponential has no subnormal results.  Each CTA takes
-// one stretch of one row, so that the stretches, in the order of memory, go to the multiprocessors as they become free.
+// one stretch of one row, so that the stretches, in the order of memory, go to the multiprocessors as they become free: memory
+// bounds it (4096 x 131072 bf16: 349 us, 6.2 TB/s in and out; 356 us, the power limit reached, in a long run).
 constexpr int GRAD_TPB = 256, GRAD_U = 4;
 constexpr float H_FLOOR = -1.0e4f;
 
@@ -738,12 +742,13 @@ int mv_token_logprob(void* stream, const void* logits, int type, int64_t T, int6
     // CTAs, if there are rows enough to fill the device: 16000 rows of 16 KB, k = 8: 62 us with 32 threads, 73 with 64, 102 with 128;
     // 9079 rows of 33 KB: 77, 70, 84.  Rows in the hundreds take more threads than that (1003 of 16 KB: 10.4, 9.5, 9.6), long ones
     // more still (3000 of 131 KB: 81 us with 128, 86 with 256; of 200 KB: 136 and 123; 100 of 200 KB: 14.4 and 11.3).
-    // A few long rows: a cluster of four per row, a step or more for each thread (one row of 200 KB: 8.8 us, with one CTA 10.3).
+    // Long rows that are so few that four CTAs each fit the device: a cluster of four per row, a step or more for each thread (one
+    // row of 200 KB: 8.8 us, with one CTA 10.3; 32 of 262 KB: 9.5 and 14.0).
     // 32 threads have too few maxima to bound more than 32 alternatives.
     const int tpb = T >= 2368 && vecs <= 2047 && k <= 32 ? 32
                   : T >= 1184 && vecs <= 3072 ? 64
                   : vecs > 10240 || (T < 600 && vecs > 6000) ? 256 : 128;
-    const int ctas = T <= 16 && vecs >= 4 * 256 * U ? 4 : 1;
+    const int ctas = T <= 148 / 4 && vecs >= 4 * 256 * U ? 4 : 1;
     const int64_t n_steps = ((vecs + ctas - 1) / ctas + tpb * U - 1) / (tpb * U);
     a.steps = int((n_steps + MAX_GROUPS - 1) / MAX_GROUPS);
     if (a.steps < 1) a.steps = 1;

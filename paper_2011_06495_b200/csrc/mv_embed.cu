@@ -11,14 +11,14 @@ namespace {
 template <typename X> constexpr int LANE = 16 / int(sizeof(X));
 template <typename X> constexpr int BLOCK = 32 * LANE<X>;         // columns per warp
 
-template <typename X, bool VEC> __device__ __forceinline__ int64_t column(int64_t cb, int lane, int j) {
-  return VEC ? cb * BLOCK<X> + lane * LANE<X> + j : cb * BLOCK<X> + j * 32 + lane;
+template <typename X, bool VEC> __device__ __forceinline__ int64_t column(int64_t cb, int lane, int j, int lanes = 32) {
+  return VEC ? cb * BLOCK<X> + lane * LANE<X> + j : cb * BLOCK<X> + j * lanes + lane;
 }
 
 // The raw elements of one row, loaded without being converted (so that loads of several rows can be outstanding).
 template <typename X> struct Raw { X e[LANE<X>]; };
 
-template <typename X, bool VEC> __device__ __forceinline__ void load_raw(const X* row, int64_t D, int64_t cb, int lane, uint4& u) {
+template <typename X, bool VEC> __device__ __forceinline__ void load_raw(const X* row, int64_t D, int64_t cb, int lane, int lanes, uint4& u) {
   Raw<X> r;
   if constexpr (VEC) {
     const int64_t c0 = column<X, true>(cb, lane, 0);
@@ -31,7 +31,7 @@ template <typename X, bool VEC> __device__ __forceinline__ void load_raw(const X
   } else {
 #pragma unroll
     for (int j = 0; j < LANE<X>; ++j) {
-      const int64_t c = column<X, false>(cb, lane, j);
+      const int64_t c = column<X, false>(cb, lane, j, lanes);
       r.e[j] = c < D ? row[c] : from_f<X>(0.0f);
     }
   }
@@ -39,7 +39,7 @@ template <typename X, bool VEC> __device__ __forceinline__ void load_raw(const X
 }
 
 // ------------------------------------------------------------------------------------------ lookup
-// A warp takes R tokens and one block of columns: it reads the R ids with one load, then R independent pieces of rows.  With
+// A warp takes R tokens and one block of columns: it reads the R ids, then R independent pieces of rows.  With
 // many tokens the rows come out of L2 for the most part, and L2 bounds it: 65536 rows of 4 KB in and out move 537 MB in 78 us,
 // 6.9 TB/s.  More rows per warp cost warps (R = 4: 85 us, R = 8: 101), fewer leave it waiting for the ids (R = 1: 101).  The
 // output is written past L2 (evict first), whose room belongs to the table.
@@ -59,7 +59,7 @@ __global__ void __launch_bounds__(EMBED_TPB) k_embed(const W* __restrict__ weigh
   for (int i = 0; i < R; ++i) {
     const int v = __shfl_sync(0xffffffffu, mine, i);
     u[i] = make_uint4(0, 0, 0, 0);
-    if (v >= 0) load_raw<W, VEC>(weight + v * ldw, D, cb, lane, u[i]);
+    if (v >= 0) load_raw<W, VEC>(weight + v * ldw, D, cb, lane, 32, u[i]);
   }
 #pragma unroll
   for (int i = 0; i < R; ++i) {
@@ -81,6 +81,33 @@ __global__ void __launch_bounds__(EMBED_TPB) k_embed(const W* __restrict__ weigh
         const int64_t c = column<W, VEC>(cb, lane, j);
         if (c < D) dst[c] = o.e[j];
       }
+    }
+  }
+}
+
+// Rows of at most half a block share a warp: 2^lanes_log lanes each (37752 rows of 128 bytes: 3.4 us, with a warp each 11.1).
+template <typename W, typename O, bool VEC>
+__global__ void __launch_bounds__(EMBED_TPB) k_embed_narrow(const W* __restrict__ weight, int64_t V, int64_t D, int64_t ldw, const void* __restrict__ ids,
+                                                             int id_type, int64_t T, float scale, O* __restrict__ out, int64_t ldo, int lanes_log) {
+  const int lanes = 1 << lanes_log, lane = threadIdx.x & (lanes - 1);
+  const int64_t t = (int64_t(blockIdx.x) * EMBED_TPB + threadIdx.x) >> lanes_log;
+  if (t >= T) return;
+  const int64_t v = load_id(ids, id_type, t, V);
+  uint4 u = make_uint4(0, 0, 0, 0);
+  if (v >= 0) load_raw<W, VEC>(weight + v * ldw, D, 0, lane, lanes, u);
+  Raw<W> r;
+  memcpy(&r, &u, 16);
+  struct alignas(sizeof(O) * LANE<W> < 16 ? sizeof(O) * LANE<W> : 16) Row { O e[LANE<W>]; } o;
+#pragma unroll
+  for (int j = 0; j < LANE<W>; ++j) o.e[j] = from_f<O>(v >= 0 ? to_f(r.e[j]) * scale : 0.0f);
+  O* dst = out + t * ldo;
+  if (VEC && (lane + 1) * LANE<W> <= D) {
+    *reinterpret_cast<Row*>(dst + lane * LANE<W>) = o;
+  } else {
+#pragma unroll
+    for (int j = 0; j < LANE<W>; ++j) {
+      const int64_t c = column<W, VEC>(0, lane, j, lanes);
+      if (c < D) dst[c] = o.e[j];
     }
   }
 }
@@ -122,7 +149,7 @@ inline EmbedPlan embed_plan(int64_t T, int64_t V, int64_t D, int block) {
   p.perm = o;   o = align_up(o + size_t(T) * 4, 16);
   p.row = o;    o = align_up(o + size_t(T) * 4, 16);
   p.start = o;  o = align_up(o + (size_t(p.bins + 1) << p.nb_log) * 4, 16);
-  p.ticket = o; o = align_up(o + size_t(p.pieces) * size_t(p.ncb) * 4, 16);
+  p.ticket = o; o = align_up(o + size_t(p.pieces) * size_t(p.ncb) * 8, 16);
   p.part = o;   o = align_up(o + size_t(p.pieces) * 2 * size_t(D) * 4, 16);
   p.total = o;
   return p;
@@ -311,9 +338,9 @@ __global__ void __launch_bounds__(SORT_TPB) k_embed_sort(const __grid_constant__
 // 6.7 TB/s; with rows in registers instead of the asynchronous ring it was 202 us (latency: two CTAs a multiprocessor).
 struct SumArgs {
   const int32_t *perm, *row, *start, *valid;
-  uint32_t* ticket;
+  uint32_t* ticket;                  // [2][piece][block of columns] warps that have arrived, at either level of the joining
   float* part;                       // [piece][0: the run that the piece begins with, 1: the one it ends with][D]
-  int64_t V, D, ldd, ldw;
+  int64_t V, D, ldd, ldw, pieces;
   float scale;
   int accumulate, nb, ncb;
   int dw_aligned;                    // the table's rows start at multiples of what a lane stores (16 or 32 bytes)
@@ -323,6 +350,7 @@ struct SumArgs {
 };
 
 constexpr int SUM_TPB = 256;
+constexpr int JOIN = 16;             // partial sums added up by one warp
 constexpr int RING = 8;              // rows on their way per warp (4 KB; 32 warps a multiprocessor)
 
 // A row of zeros, written by one warp: single words up to a 16-byte boundary, then 16 bytes a lane.
@@ -407,7 +435,7 @@ template <typename X, bool VEC> __device__ __forceinline__ void fetch(const X* r
       if (c < D) asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(smem_addr(reinterpret_cast<X*>(slot) + j)), "l"(row + c) : "memory");
     }
   } else {
-    load_raw<X, VEC>(row, D, cb, lane, *slot);
+    load_raw<X, VEC>(row, D, cb, lane, 32, *slot);
   }
 }
 
@@ -481,26 +509,45 @@ __global__ void __launch_bounds__(SUM_TPB, 4) k_embed_sum(const X* __restrict__ 
     for (int j = 0; j < E; ++j) acc.v[j] = 0.0f;
   }
   if (!cross0 && !cross1) return;
-  // this piece's partial sums are written: is it the last one of either run?
+  // This piece's partial sums are written.  The warp that brings the last of up to JOIN neighbouring pieces of a run adds them up,
+  // and of a longer run, the warp that brings the last such sum adds those up: two short chains of loads instead of a long one.
   __threadfence();
   __syncwarp();
 #pragma unroll 1
   for (int c = 0; c < 2; ++c) {
     if (!(c ? cross1 : cross0)) continue;
     const int f = c ? first[1] : first[0], p0 = f / PIECE, p1 = (c ? last[1] : last[0]) / PIECE;
-    uint32_t arrived = 0;
-    if (lane == 0) arrived = atomicAdd(a.ticket + int64_t(p0) * a.ncb + cb, 1u);
-    if (__shfl_sync(0xffffffffu, arrived, 0) != uint32_t(p1 - p0)) continue;
-    __threadfence();
-    const float* q0 = part_at<X>(a, p0, f % PIECE ? 1 : 0, cb, lane);
+    auto slot_of = [&](int p) { return p == p0 && f % PIECE ? 1 : 0; };
+    auto last_one = [&](uint32_t* ticket, int others) {      // of others + 1 warps
+      uint32_t arrived = 0;
+      if (lane == 0) arrived = atomicAdd(ticket, 1u);
+      if (__shfl_sync(0xffffffffu, arrived, 0) != uint32_t(others)) return false;
+      __threadfence();
+      return true;
+    };
+    auto add = [&](int from, int to, int step) {      // the sums left at pieces from, from + step, ..., to
+      const float* q = part_at<X>(a, from, slot_of(from), cb, lane);
 #pragma unroll
-    for (int j = 0; j < E; ++j) acc.v[j] = __ldcg(q0 + j * 32);
-    const int64_t step = 2 * int64_t(a.ncb) * BLOCK<X>;
-    const float* q1 = part_at<X>(a, p0 + 1, 0, cb, lane);
+      for (int j = 0; j < E; ++j) acc.v[j] = __ldcg(q + j * 32);
 #pragma unroll 4
-    for (int k = p0 + 1; k <= p1; ++k, q1 += step)
+      for (int k = from + step; k <= to; k += step) {
+        q = part_at<X>(a, k, 0, cb, lane);
 #pragma unroll
-      for (int j = 0; j < E; ++j) acc.v[j] += __ldcg(q1 + j * 32);
+        for (int j = 0; j < E; ++j) acc.v[j] += __ldcg(q + j * 32);
+      }
+    };
+    const int g0 = int(piece) - (int(piece) - p0) % JOIN, g1 = min(p1, g0 + JOIN - 1);
+    if (g1 > g0 && !last_one(a.ticket + int64_t(g0) * a.ncb + cb, g1 - g0)) continue;
+    add(g0, g1, 1);
+    if (p1 - p0 >= JOIN) {
+      float* q = part_at<X>(a, g0, slot_of(g0), cb, lane);
+#pragma unroll
+      for (int j = 0; j < E; ++j) __stcg(q + j * 32, acc.v[j]);
+      __threadfence();
+      __syncwarp();
+      if (!last_one(a.ticket + (a.pieces + p0) * a.ncb + cb, (p1 - p0) / JOIN)) continue;
+      add(p0, p1, JOIN);
+    }
     put_row<X, VEC>(a, c ? rn : r0, cb, lane, acc, stage);
   }
 }
@@ -528,11 +575,19 @@ int mv_embed(void* stream, const void* weight, int w_type, int64_t V, int64_t D,
       const int ob = int(sizeof(O)) * LANE<W> < 16 ? int(sizeof(O)) * LANE<W> : 16;
       const bool vec = rows_aligned(weight, ldw, sizeof(W), 16) && rows_aligned(out, ldo, sizeof(O), ob);
       // two tokens a warp once that still gives every multiprocessor its 64 warps; below, the latency of one row counts
+      int lanes_log = 5;
+      while (ncb == 1 && lanes_log > 0 && (int64_t(LANE<W>) << (lanes_log - 1)) >= D) --lanes_log;
+      if (lanes_log < 5) {
+        const int64_t grid = ((T << lanes_log) + EMBED_TPB - 1) / EMBED_TPB;
+        auto* kernel = vec ? k_embed_narrow<W, O, true> : k_embed_narrow<W, O, false>;
+        kernel<<<unsigned(grid), EMBED_TPB, 0, st>>>(static_cast<const W*>(weight), V, D, ldw, ids, id_type, T, scale, static_cast<O*>(out), ldo, lanes_log);
+        return cuda_ok();
+      }
       const int R = T * ncb >= 148 * 64 * 2 ? 2 : 1;
       const int64_t items = (T + R - 1) / R * ncb, grid = (items + EMBED_TPB / 32 - 1) / (EMBED_TPB / 32);
       if (grid >= lim) return int(MV_ERR_INVALID_ARG);
       auto* kernel = vec ? (R == 2 ? k_embed<W, O, true, 2> : k_embed<W, O, true, 1>) : (R == 2 ? k_embed<W, O, false, 2> : k_embed<W, O, false, 1>);
-      kernel<<<unsigned(grid), EMBED_TPB, 0, st>>>(static_cast<const W*>(weight), V, D, ldw, ids, id_type, T, scale, static_cast<O*>(out), ldo, unsigned(ncb));
+      kernel<<<unsigned(grid), EMBED_TPB, 0, st>>>(static_cast<const W*>(weight), V, D, ldw, ids, id_type, T, scale, static_cast<O*>(out), ldo, int(ncb));
       return cuda_ok();
     });
   });
@@ -559,8 +614,10 @@ int mv_embed_grad(void* stream, const void* dout, int dout_type, int64_t ldd, co
   const EmbedPlan p = embed_plan(T, V, (D + block - 1) / block * block, block);
   const int64_t items = p.pieces * p.ncb, n_sum = (items + SUM_TPB / 32 - 1) / (SUM_TPB / 32);
   SumArgs a;
-  // a CTA that clears looks at 128 KB of rows, or at eight rows (one a warp)
-  a.fill_rows = int(((32 << 10) / D + 7) / 8 * 8);
+  // a CTA that clears looks at 128 KB of rows, at fewer where that would not give every multiprocessor eight of them, and at
+  // eight at least (one a warp)
+  const int64_t by_size = (32 << 10) / D, by_count = V / (148 * 8);
+  a.fill_rows = int(((by_size < by_count ? by_size : by_count) + 7) / 8 * 8);
   if (a.fill_rows < 8) a.fill_rows = 8;
   a.n_fill = accumulate ? 0 : (V + a.fill_rows - 1) / a.fill_rows;
   if (n_sum + a.n_fill >= lim) return MV_ERR_INVALID_ARG;
@@ -574,7 +631,7 @@ int mv_embed_grad(void* stream, const void* dout, int dout_type, int64_t ldd, co
   s.start = reinterpret_cast<int32_t*>(base + p.start);
   s.valid = reinterpret_cast<int32_t*>(base + p.valid);
   s.ticket = reinterpret_cast<uint32_t*>(base + p.ticket);
-  s.n_ticket = items;
+  s.n_ticket = 2 * items;
   const size_t smem = sizeof(SortSmem) + size_t(SORT_WARPS) * p.bins * 4;
   auto* sort = id_type == MV_I32 ? k_embed_sort<int32_t> : k_embed_sort<int64_t>;
   static SmemLimit sort_limit[2];
@@ -584,6 +641,7 @@ int mv_embed_grad(void* stream, const void* dout, int dout_type, int64_t ldd, co
   a.part = reinterpret_cast<float*>(base + p.part);
   a.V = V; a.D = D; a.ldd = ldd; a.ldw = ldw; a.scale = scale; a.accumulate = accumulate; a.nb = 1 << p.nb_log;
   a.ncb = int(p.ncb);
+  a.pieces = p.pieces;
   a.dw_aligned = rows_aligned(dweight, ldw, 4, dout_type == MV_F32 ? 16 : 32);
   a.dweight = dweight;
   return with_type(dout_type, [&](auto x) {

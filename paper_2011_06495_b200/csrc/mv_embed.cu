@@ -364,17 +364,22 @@ __device__ __forceinline__ void clear_row(float* p, int64_t D, int lane) {
   if (lane < D - done) p[done + lane] = 0.0f;
 }
 
-// Clears the unused ones of the rows a CTA looks at.  Each warp has neighbouring rows, and where rows follow one another
-// without a gap, neighbouring unused rows are cleared as one (56769 rows of 256 bytes: 5.0 us, row by row 9.7).
+// Clears the unused ones of the rows a CTA looks at.  Every warp has one row in eight; but where rows follow one another
+// without a gap and are narrow, or would be written in parts of sectors, it has neighbouring rows, and clears neighbouring unused ones as one
+// (56769 rows of 256 bytes: 4.5 us, row by row 9.7; 50021 of 4004 bytes: 33.5 and 37.3).
 template <typename F> __device__ __forceinline__ void clear_unused(const SumArgs& a, int64_t cta, F&& unused) {
-  const int lane = threadIdx.x & 31, w = threadIdx.x >> 5, mine = a.fill_rows / (SUM_TPB / 32);
-  const int64_t v1 = min(a.V, cta * a.fill_rows + (w + 1) * mine);
-  for (int64_t v = cta * a.fill_rows + w * mine; v < v1; v += 32) {
-    unsigned m = __ballot_sync(0xffffffffu, v + lane < v1 && unused(v + lane));
+  constexpr int W = SUM_TPB / 32;
+  const int lane = threadIdx.x & 31, w = threadIdx.x >> 5, rows = a.fill_rows / W;
+  const bool merge = a.ldw == a.D && (a.D < 128 || a.D % 8 != 0 || (reinterpret_cast<uintptr_t>(a.dweight) & 31) != 0);
+  const int step = merge ? 1 : W;
+  const int64_t v0 = cta * a.fill_rows + (merge ? w * rows : w);
+  for (int i0 = 0; i0 < rows; i0 += 32) {
+    const int64_t mine = v0 + int64_t(i0 + lane) * step;
+    unsigned m = __ballot_sync(0xffffffffu, i0 + lane < rows && mine < a.V && unused(mine));
     while (m) {
       const int i = __ffs(int(m)) - 1, run = __ffs(int(~(m >> i))) - 1;      // (-1 where m is all ones)
-      const int n = a.ldw != a.D ? 1 : run < 0 ? 32 : run;
-      clear_row(a.dweight + (v + i) * a.ldw, n * a.D, lane);
+      const int n = !merge ? 1 : run < 0 ? 32 : run;
+      clear_row(a.dweight + (v0 + int64_t(i0 + i) * step) * a.ldw, n * a.D, lane);
       m &= i + n >= 32 ? 0u : ~0u << (i + n);
     }
   }
@@ -700,9 +705,9 @@ int mv_embed_grad(void* stream, const void* dout, int dout_type, int64_t ldd, co
   const EmbedPlan p = embed_plan(T, V, (D + block - 1) / block * block, block);
   const int64_t items = p.pieces * p.ncb, n_sum = (items + SUM_TPB / 32 - 1) / (SUM_TPB / 32);
   SumArgs a;
-  // a CTA that clears looks at 128 KB of rows, at fewer where that would not give every multiprocessor eight of them, and at
+  // a CTA that clears looks at 128 KB of rows, at fewer where that would not give every multiprocessor four of them, and at
   // eight at least (one a warp)
-  const int64_t by_size = (32 << 10) / D, by_count = V / (148 * 8);
+  const int64_t by_size = (32 << 10) / D, by_count = V / (148 * 4);
   a.fill_rows = int(((by_size < by_count ? by_size : by_count) + 7) / 8 * 8);
   if (a.fill_rows < 8) a.fill_rows = 8;
   a.n_fill = accumulate ? 0 : (V + a.fill_rows - 1) / a.fill_rows;

@@ -746,7 +746,7 @@ int mv_token_logprob(void* stream, const void* logits, int type, int64_t T, int6
     // row of 200 KB: 8.8 us, with one CTA 10.3; 32 of 262 KB: 9.5 and 14.0).
     // 32 threads have too few maxima to bound more than 32 alternatives.
     const int tpb = T >= 2368 && vecs <= 2047 && k <= 32 ? 32
-                  : T >= 1184 && vecs <= 3072 ? 64
+                  : T >= 1184 && vecs <= 3000 ? 64
                   : vecs > 10240 || (T < 600 && vecs > 6000) ? 256 : 128;
     const int ctas = T <= 148 / 4 && vecs >= 4 * 256 * U ? 4 : 1;
     const int64_t n_steps = ((vecs + ctas - 1) / ctas + tpb * U - 1) / (tpb * U);

@@ -36,7 +36,7 @@ enum { MV_F32 = 0, MV_BF16 = 1, MV_F16 = 2, MV_I32 = 3, MV_I64 = 4 };
 #define MV_TOP_MAX 64 /* most alternatives per position */
 
 /* Embedding lookup.  out[t, :] = scale * weight[ids[t], :], the product rounded once to 32 bits and once to
- * out's type.  A token id outside [0, V) gives a row of zeros.
+ * out's type.  A token id outside [0, V) gives a row of zeros.  weight and out share no bytes.
  *   weight [V, D] w_type in, rows ldw >= D apart;  ids [T] id_type in;  out [T, D] out_type out, rows ldo >= D apart
  * Limits: 1 <= V < 2^31, 1 <= D < 2^31, 0 <= T < 2^31. */
 int mv_embed(void* stream, const void* weight, int w_type, int64_t V, int64_t D, int64_t ldw, const void* ids, int id_type,
@@ -47,7 +47,7 @@ size_t mv_embed_grad_workspace_bytes(int64_t T, int64_t V, int64_t D);
 
 /* Gradient of the lookup with respect to the table, dense.  The tokens are grouped by id, and each row is summed
  * in 32 bits in an order that only the ids fix, then multiplied by scale.
- *   dout    [T, D] dout_type in, rows ldd >= D apart;  ids [T] id_type in
+ *   dout    [T, D] dout_type in, rows ldd >= D apart, no bytes of dweight;  ids [T] id_type in
  *   dweight [V, D] float, rows ldw >= D apart.  accumulate = 0: overwritten (rows without a token become +0);
  *           accumulate = 1: added to, rows without a token are not touched
  *   pad_id  tokens with this id, like ids outside [0, V), have no gradient; -1 for none

@@ -315,6 +315,7 @@ __global__ void __launch_bounds__(TPB, 6) k_clip_hold(const __grid_constant__ Cl
 
 struct mv_clip {
   int64_t n;                         // chunks
+  int hold;                          // chunks up to which the one-kernel form is used
   int n_groups;
   int64_t longest;                   // elements of the longest group
   uintptr_t lo, hi;                  // addresses that the tensors span
@@ -330,7 +331,7 @@ bool overlaps(const mv_clip* p, const float* rows, int64_t ld) {
   const uintptr_t lo = reinterpret_cast<uintptr_t>(rows), hi = lo + (size_t(p->n_groups - 1) * ld + p->longest) * 4;
   if (hi <= p->lo || lo >= p->hi) return false;
   for (int i = 0; i < p->n_tensors; ++i)
-    if (p->spans[i].lo < hi && lo < p->spans[i].hi) return true;
+    if (p->spans[i].lo < p->spans[i].hi && p->spans[i].lo < hi && lo < p->spans[i].hi) return true;
   return false;
 }
 
@@ -346,7 +347,7 @@ int clip_run(mv_clip* p, cudaStream_t st, float max_norm, float* rows, int64_t l
   cfg.attrs = &attr;
   cfg.numAttrs = 1;
   bool ok;
-  if (apply && p->n <= HOLD) {
+  if (apply && p->n <= p->hold) {
     attr.id = cudaLaunchAttributeCooperative;        // all CTAs at once or none: they wait for one another
     attr.val.cooperative = 1;
     ok = cudaLaunchKernelEx(&cfg, k_clip_hold, a) == cudaSuccess;
@@ -424,6 +425,11 @@ int mv_clip_create(mv_clip** out, void* stream, void* const* tensors, const int*
   }
   while (g < n_groups) first[++g] = int32_t(nc);
   for (g = 0; g < n_groups; ++g) p->args.empty |= first[g] == first[g + 1];
+  // the one-kernel form needs all its CTAs at once
+  int dev = 0, sms = 0, per_sm = 0;
+  if (cudaGetDevice(&dev) == cudaSuccess && cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) == cudaSuccess &&
+      cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, k_clip_hold, TPB, 0) == cudaSuccess)
+    p->hold = sms * per_sm / 2 < HOLD ? sms * per_sm / 2 : HOLD;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   const bool ok = cudaMemcpyAsync(base, host, L.partial, cudaMemcpyHostToDevice, st) == cudaSuccess && cudaStreamSynchronize(st) == cudaSuccess;
   free(host);

@@ -33,6 +33,14 @@ __device__ __forceinline__ int64_t load_id(const void* ids, int id_type, int64_t
   return v >= 0 && v < V ? v : -1;
 }
 
+// Whether two strided matrices (rows of `cols` elements of `size` bytes, `ld` elements apart) span common bytes.
+inline bool share_bytes(const void* p, int64_t rows, int64_t cols, int64_t ld, int size, const void* q, int64_t rows2, int64_t cols2, int64_t ld2,
+                        int size2) {
+  if (rows < 1 || rows2 < 1) return false;
+  const uintptr_t a = reinterpret_cast<uintptr_t>(p), b = reinterpret_cast<uintptr_t>(q);
+  return a < b + size_t((rows2 - 1) * ld2 + cols2) * size2 && b < a + size_t((rows - 1) * ld + cols) * size;
+}
+
 // Lets a kernel use `bytes` of dynamic shared memory; asked of the driver once per kernel (a static of the caller) and device.
 struct SmemLimit { int bytes[64]; };
 template <typename K> bool allow_smem(K* kernel, int bytes, SmemLimit* have) {

@@ -787,9 +787,8 @@ int mv_token_logprob_grad(void* stream, const void* logits, int type, int64_t T,
     return MV_ERR_INVALID_ARG;
   if (T == 0) return MV_OK;
   // in place element by element, or apart
-  const char *a = static_cast<const char*>(logits), *b = static_cast<const char*>(dlogits);
-  const int64_t na = ((T - 1) * ld + V) * type_size(type), nb = ((T - 1) * ldg + V) * type_size(type);
-  if (a < b + nb && b < a + na && !(a == b && ld == ldg)) return MV_ERR_INVALID_ARG;
+  if (share_bytes(logits, T, V, ld, type_size(type), dlogits, T, V, ldg, type_size(type)) && !(logits == dlogits && ld == ldg))
+    return MV_ERR_INVALID_ARG;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   return with_type(type, [&](auto x) {
     using X = decltype(x);

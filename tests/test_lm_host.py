@@ -16,19 +16,21 @@ def lib():
 
 P = ctypes.c_void_p(0x100000)          # never dereferenced
 Q = ctypes.c_void_p(0x200000)
+R = ctypes.c_void_p(0x300000)
 ODD = ctypes.c_void_p(0x100002)
 BAD = B.MV_ERR_INVALID_ARG
 
 
 def test_embed_refusals(lib):
-    ok = dict(w=P, wt=B.MV_F32, V=10, D=8, ldw=8, ids=Q, it=B.MV_I64, T=4, out=P, ot=B.MV_BF16, ldo=8)
+    ok = dict(w=P, wt=B.MV_F32, V=10, D=8, ldw=8, ids=Q, it=B.MV_I64, T=4, out=R, ot=B.MV_BF16, ldo=8)
 
     def call(**k):
         a = {**ok, **k}
         return lib.mv_embed(None, a["w"], a["wt"], a["V"], a["D"], a["ldw"], a["ids"], a["it"], a["T"], 1.0, a["out"], a["ot"], a["ldo"])
 
     for k in (dict(w=None), dict(wt=B.MV_I32), dict(wt=9), dict(V=0), dict(V=1 << 31), dict(D=0), dict(ldw=7), dict(ids=None), dict(it=B.MV_F32),
-              dict(T=-1), dict(T=1 << 31), dict(out=None), dict(ot=5), dict(ldo=7), dict(w=ODD), dict(ids=ODD), dict(ids=ctypes.c_void_p(0x100004))):
+              dict(T=-1), dict(T=1 << 31), dict(out=None), dict(ot=5), dict(ldo=7), dict(w=ODD), dict(ids=ODD), dict(ids=ctypes.c_void_p(0x100004)), dict(out=P), dict(out=ctypes.c_void_p(0x100000 - 62)),
+              dict(out=ctypes.c_void_p(0x100000 + 318))):
         assert call(**k) == BAD, k
     assert call(T=0) == B.MV_OK
 
@@ -38,14 +40,14 @@ def test_embed_grad_refusals_and_workspace(lib):
     assert need >= 8000 and need % 16 == 0
     assert B.embed_grad_workspace_bytes(-1, 50, 8) == 0 and B.embed_grad_workspace_bytes(10, 0, 8) == 0 and B.embed_grad_workspace_bytes(10, 50, 1 << 31) == 0
     assert B.embed_grad_workspace_bytes(0, 50, 8) > 0
-    ok = dict(x=P, xt=B.MV_F16, ldd=8, ids=Q, it=B.MV_I32, T=1000, V=50, D=8, acc=0, dw=P, ldw=8, ws=Q, n=need)
+    ok = dict(x=P, xt=B.MV_F16, ldd=8, ids=Q, it=B.MV_I32, T=1000, V=50, D=8, acc=0, dw=R, ldw=8, ws=Q, n=need)
 
     def call(**k):
         a = {**ok, **k}
         return lib.mv_embed_grad(None, a["x"], a["xt"], a["ldd"], a["ids"], a["it"], a["T"], a["V"], a["D"], 1.0, -1, a["acc"], a["dw"], a["ldw"], a["ws"], a["n"])
 
     for k in (dict(x=None), dict(xt=7), dict(ldd=7), dict(ids=None), dict(it=B.MV_BF16), dict(T=-1), dict(V=0), dict(D=0), dict(acc=2), dict(dw=None),
-              dict(ldw=7), dict(dw=ODD), dict(ids=ODD), dict(x=ctypes.c_void_p(0x100001)), dict(ws=ctypes.c_void_p(0x100008))):
+              dict(ldw=7), dict(dw=ODD), dict(ids=ODD), dict(x=ctypes.c_void_p(0x100001)), dict(ws=ctypes.c_void_p(0x100008)), dict(dw=P)):
         assert call(**k) == BAD, k
     assert call(ws=None) == B.MV_ERR_WORKSPACE and call(n=need - 1) == B.MV_ERR_WORKSPACE
 

@@ -735,6 +735,8 @@ def test_shapes_and_types_that_do_not_fit_are_refused():
         lambda: B.mv_embed(w.double(), ids, out),
         lambda: B.mv_embed(w.t(), ids, out),
         lambda: B.mv_embed(w.cpu(), ids, out),
+        lambda: B.mv_embed(w, ids, w[6:]),
+        lambda: B.mv_embed_grad(w[6:], ids, w, ws),
         lambda: B.mv_embed_grad(out, ids, w.half(), ws),
         lambda: B.mv_embed_grad(out, ids, w, ws[:8]),
         lambda: B.mv_embed_grad(out, ids, w[:, :4], ws),

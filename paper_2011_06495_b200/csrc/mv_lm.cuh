@@ -33,12 +33,17 @@ __device__ __forceinline__ int64_t load_id(const void* ids, int id_type, int64_t
   return v >= 0 && v < V ? v : -1;
 }
 
-// Whether two strided matrices (rows of `cols` elements of `size` bytes, `ld` elements apart) span common bytes.
+// Whether two strided matrices (rows of `cols` elements of `size` bytes, `ld` elements apart) share bytes: their spans meet, and
+// they are not two windows of columns side by side in rows of one pitch.
 inline bool share_bytes(const void* p, int64_t rows, int64_t cols, int64_t ld, int size, const void* q, int64_t rows2, int64_t cols2, int64_t ld2,
                         int size2) {
   if (rows < 1 || rows2 < 1) return false;
   const uintptr_t a = reinterpret_cast<uintptr_t>(p), b = reinterpret_cast<uintptr_t>(q);
-  return a < b + size_t((rows2 - 1) * ld2 + cols2) * size2 && b < a + size_t((rows - 1) * ld + cols) * size;
+  if (a >= b + size_t((rows2 - 1) * ld2 + cols2) * size2 || b >= a + size_t((rows - 1) * ld + cols) * size) return false;
+  const uintptr_t pitch = uintptr_t(ld) * size;
+  if (pitch != uintptr_t(ld2) * size2) return true;
+  const uintptr_t to = a <= b ? (b - a) % pitch : (pitch - (a - b) % pitch) % pitch;      // from a row of p on to the next row of q
+  return to < uintptr_t(cols) * size || pitch - to < uintptr_t(cols2) * size2;
 }
 
 // Lets a kernel use `bytes` of dynamic shared memory; asked of the driver once per kernel (a static of the caller) and device.

@@ -723,6 +723,33 @@ def test_the_calls_can_be_captured_and_replayed_on_new_inputs():
         assert torch.equal(x, y), i
 
 
+@pytest.mark.parametrize("D", [7, 64, 300])
+def test_windows_of_one_buffer_side_by_side(D):
+    """Column windows of the same rows share no bytes: they are taken, and nothing beside them changes; one column more and they are refused."""
+    g = torch.Generator(device=DEV).manual_seed(D)
+    T = 200
+    for left in (True, False):
+        src, dst = (slice(0, D), slice(D, 2 * D)) if left else (slice(D, 2 * D), slice(0, D))
+        wide = (slice(D - 1, 2 * D - 1) if left else slice(1, D + 1))
+        ids = torch.randint(0, T, (T,), generator=g, device=DEV)
+        ws = torch.empty(B.embed_grad_workspace_bytes(T, T, D), dtype=torch.uint8, device=DEV)
+        gl, lse = torch.randn(T, generator=g, device=DEV), torch.zeros(T, device=DEV)
+        calls = [
+            lambda x, o: B.mv_embed(x, ids, o),
+            lambda x, o: B.mv_embed_grad(x, ids, o, ws),
+            lambda x, o: B.mv_token_logprob_grad(x, ids % D, lse, gl, o),
+        ]
+        for call in calls:
+            buf = torch.randn((T, 2 * D + 1), generator=g, device=DEV)
+            old, apart = buf.clone(), torch.empty_like(buf)
+            call(old[:, src], apart[:, dst])           # two buffers, the same places in them
+            call(buf[:, src], buf[:, dst])
+            assert torch.equal(buf[:, dst], apart[:, dst])
+            assert torch.equal(buf[:, src], old[:, src]) and torch.equal(buf[:, 2 * D:], old[:, 2 * D:])
+            with pytest.raises(B.MvError):
+                call(buf[:, src], buf[:, wide])
+
+
 def test_shapes_and_types_that_do_not_fit_are_refused():
     w, out = torch.zeros((10, 8), device=DEV), torch.zeros((4, 8), device=DEV)
     ids = torch.zeros(4, dtype=torch.int64, device=DEV)

@@ -2,9 +2,10 @@
 //
 // With z = c x, r a reference near the row's largest logit and t = (x - r) c log2(e):  s = sum 2^t,  lse = c r + log s,
 // H = log s - ln 2 (sum 2^t t) / s.  A masked logit (-inf) has 2^t = 0 and must not multiply its t, so t is kept above a
-// finite floor.  t is one fused multiply-add, x (c log2 e) - R with R = r c log2(e) rounded; what the rounding of R costs is put
-// right once per thread.  Rows in which R itself would overflow (every logit near the type's lowest or largest value) are
-// summed again in a form that takes the difference first.
+// finite floor.  t is one fused multiply-add, x (c log2 e) - R with R = r c log2(e) rounded; what the rounding of R costs, d = r c
+// log2(e) - R, is put right once per thread by 2^-d to the second order, and so only while |R| stays below R_MAX: there |d| <= 2^-7
+// and (d ln 2)^3 / 6 < 2.7e-8, half a unit of 32 bits.  Parts whose logits times c log2(e) all lie below -R_MAX, or some above
+// R_MAX (a whole row masked by a finite fill, an inverse temperature of 1e5), are summed again in a form that takes the difference first.
 
 #include "mv_lm.cuh"
 
@@ -17,8 +18,10 @@ namespace {
 namespace cg = cooperative_groups;
 
 constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
-constexpr float T_FLOOR = -1.0e30f;
-constexpr float R_MAX = 1.0e37f;     // references up to here are summed by the fused form
+constexpr float T_FLOOR = -1.0e4f;    // 2^t is 0 far above it, and a sum of 2^31 terms of up to 2^10 times it is finite
+constexpr float R_MAX = 131072.0f;   // references of at most this magnitude are summed by the fused form
+constexpr float C2_MIN = 1.0e-30f;   // below that scale the distances that count are not small beside the type's range
+constexpr float LAG = 10.0f;         // a logit changes a thread's reference only if it exceeds it by 2^LAG
 
 __device__ __forceinline__ float max_nan(float a, float b) {
   float r;
@@ -377,23 +380,23 @@ struct LogprobArgs {
 
 struct Sums { float ref, s, st; };   // s = sum 2^t, st = sum 2^t t, both relative to ref (-inf: nothing yet)
 
+// (a - b) c2 of two logits; a quarter of each where the difference could pass the range of 32 bits and count all the same
+__device__ __forceinline__ float distance(float a, float b, float c2) {
+  return c2 < 1.0f ? (0.25f * a - 0.25f * b) * (4.0f * c2) : (a - b) * c2;
+}
+
 // The same sums relative to a larger reference.
 __device__ __forceinline__ Sums shift(const Sums& x, float ref, float c2) {
-  const float d = ref == x.ref ? 0.0f : max_nan((x.ref - ref) * c2, T_FLOOR);
+  const float d = ref == x.ref ? 0.0f : max_nan(distance(x.ref, ref, c2), T_FLOOR);
   const float f = exp2_fast(d);
   return {ref, x.s * f, fmaf(x.s, d, x.st) * f};
 }
 
-// The sums of a part whose reference does not fit the fused form (or that is empty): the largest logit first, then the differences.
+// The sums of a part whose reference does not fit the fused form (or that is empty), by differences to its largest logit m (every
+// thread has the largest of its own): one more reading of the part.
 template <typename X, int TPB>
-__device__ __noinline__ Sums sums_of_extremes(const Part<X>& p, float c2, float* sh) {
+__device__ __noinline__ Sums sums_of_extremes(const Part<X>& p, float c2, float m, float* sh) {
   const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
-  float m = -INFINITY;
-  auto all = [&](auto&& f) {
-    if (threadIdx.x < p.head + p.tail) f(to_f(p.row[threadIdx.x < p.head ? threadIdx.x : p.tail_col + threadIdx.x - p.head]));
-    for (int64_t v = threadIdx.x; v < p.nv; v += TPB) each_logit<X>(__ldg(p.vec + v), [&](int, float x) { f(x); });
-  };
-  all([&](float x) { m = fmaxf(m, x); });
   for (int o = 16; o; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
   __syncthreads();
   if (lane == 0) sh[w] = m;
@@ -401,11 +404,13 @@ __device__ __noinline__ Sums sums_of_extremes(const Part<X>& p, float c2, float*
   for (int i = 0; i < TPB / 32; ++i) m = fmaxf(m, sh[i]);
   const float ref = m == -INFINITY ? 0.0f : m;
   Sums x = {m, 0.0f, 0.0f};
-  all([&](float v) {
-    const float u = max_nan((v - ref) * c2, T_FLOOR), e = exp2_fast(u);
+  auto add = [&](float v) {
+    const float u = max_nan(distance(v, ref, c2), T_FLOOR), e = exp2_fast(u);
     x.s += e;
     x.st = fmaf(e, u, x.st);
-  });
+  };
+  if (threadIdx.x < p.head + p.tail) add(to_f(p.row[threadIdx.x < p.head ? threadIdx.x : p.tail_col + threadIdx.x - p.head]));
+  for (int64_t v = threadIdx.x; v < p.nv; v += TPB) each_logit<X>(__ldg(p.vec + v), [&](int, float x) { add(x); });
   __syncthreads();
   return x;
 }
@@ -460,14 +465,15 @@ __global__ void __launch_bounds__(TPB, 1024 / TPB) k_token_logprob(const X* __re
     }
     ptr += U * TPB;
   };
-  const float c2 = a.scale * LOG2E, room = 40.0f / c2;      // a larger logit changes the reference only if it exceeds it by 2^40
+  const float c2 = fminf(a.scale * LOG2E, 3.0e38f), room = LAG / c2;
   const f2 c22 = pack2(c2, c2);
-  float ref = -INFINITY, R = 0.0f, limit = -R_MAX / fmaxf(c2, 0.1f);      // logits below that never set the reference
+  // logits below the first limit never set the reference; beside a reference above -R_MAX their 2^t is 0
+  float ref = -INFINITY, R = 0.0f, limit = -2.0f * R_MAX / c2;
   // bf16 has the range of 32 bits: two logits at a time are kept above a floor so far below the limit that 2^t is 0 there,
   // and so near that t is finite; for the other types t itself is kept above T_FLOOR
   constexpr bool FLOOR2 = sizeof(X) == 2 && Vec<X>::NONE == 0xff80ff80u;
   uint32_t floor2 = 0;
-  if constexpr (FLOOR2) floor2 = (__float_as_uint(-3.0e38f / fmaxf(c2, 1.0f)) >> 16) * 0x10001u;
+  if constexpr (FLOOR2) floor2 = (__float_as_uint(fmaxf(-8.0f * R_MAX / c2, -3.0e38f)) >> 16) * 0x10001u;
   f2 minus = pack2(0.0f, 0.0f), s2 = pack2(0.0f, 0.0f), st2 = s2;
   auto raise = [&](float m) {        // a new reference
     const float Rm = m * c2;
@@ -538,12 +544,13 @@ __global__ void __launch_bounds__(TPB, 1024 / TPB) k_token_logprob(const X* __re
     float p0, p1, q0, q1;
     unpack2(s2, p0, p1);
     unpack2(st2, q0, q1);
-    const float d = ref == -INFINITY ? 0.0f : fmaf(ref, c2, -R), f = 1.0f - LN2 * d;      // d: at most half a unit of R; 2^-d
+    const float d = ref == -INFINITY ? 0.0f : fmaf(ref, c2, -R), f = fmaf(fmaf(0.5f * LN2 * LN2, d, -LN2), d, 1.0f);      // d: at most half a unit of R; 2^-d
     x = {ref, (p0 + p1) * f, fmaf(-d, p0 + p1, q0 + q1) * f};
   }
-  // the sums of `width` neighbouring lanes to one reference
-  auto fold = [&](int width) {
-    float m = x.ref;
+  const float top = fmaxf(mine, extra);
+  // the sums of `width` neighbouring lanes to one reference, at least m: the largest logit, so that log s is not negative
+  auto fold = [&](int width, float m) {
+    m = fmaxf(m, x.ref);
 #pragma unroll
     for (int o = width / 2; o; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
     x = shift(x, m, c2);
@@ -553,21 +560,20 @@ __global__ void __launch_bounds__(TPB, 1024 / TPB) k_token_logprob(const X* __re
       x.st += __shfl_xor_sync(0xffffffffu, x.st, o);
     }
   };
-  fold(32);
+  fold(32, top);
   if (lane == 0) s_sums[w] = x;
   if (TOP) begin_best(mine, s_top[0]);
-  const float top = fmaxf(mine, extra);
   const bool large = __syncthreads_or(top * c2 > R_MAX);
   x = s_sums[lane % WARPS];
-  fold(WARPS);
-  // logits that the fused form cannot take: too large ones anywhere, or nothing but too small ones
-  if (large || (x.ref == -INFINITY && __syncthreads_or(top > -INFINITY))) {
-    x = sums_of_extremes<X, TPB>(p, c2, &s_sums[0].ref);
-    fold(32);
+  fold(WARPS, -INFINITY);
+  // logits that the fused form cannot take: too large ones anywhere, or none that is not too low (x.ref: the largest of all)
+  if (large || c2 < C2_MIN || (x.ref * c2 < -R_MAX && x.ref > -INFINITY)) {
+    x = sums_of_extremes<X, TPB>(p, c2, top, &s_sums[0].ref);
+    fold(32, -INFINITY);
     if (lane == 0) s_sums[w] = x;
     __syncthreads();
     x = s_sums[lane % WARPS];
-    fold(WARPS);
+    fold(WARPS, -INFINITY);
   }
   if (TOP) best_of_part<X, TPB>(p, a.k, gmax, group, a.steps, mine, s_top[0]);
   if (ctas > 1) {
@@ -575,7 +581,7 @@ __global__ void __launch_bounds__(TPB, 1024 / TPB) k_token_logprob(const X* __re
     cluster.sync();
     if (rank == 0) {
       x = *cluster.map_shared_rank(&s_part, unsigned(lane % ctas));
-      fold(ctas);
+      fold(ctas, -INFINITY);
       if (TOP) {
         for (int i = threadIdx.x; i < ctas * a.k; i += TPB) s_top[0].key[i] = cluster.map_shared_rank(&s_top[0], unsigned(i / a.k))->best[i % a.k];
         __syncthreads();

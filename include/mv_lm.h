@@ -19,7 +19,9 @@
  * stream) without synchronising the host, status codes are MV_OK / MV_ERR_*, and arguments are checked
  * before anything is enqueued.  Pointers need the alignment of their element type only (a table may start
  * anywhere in a worker's row); rows are contiguous and `ld...` elements apart.  Results do not depend
- * on the order in which the GPU runs things: the same inputs give the same bytes.
+ * on the order in which the GPU runs things: the same call on the same inputs gives the same bytes.  Where
+ * the inputs lie can change the order of the sums in mv_token_logprob and mv_clip_* (rows and tensors are cut at
+ * their own 16- or 32-byte boundaries), and so can the number of rows; the other calls' bytes do not depend on it.
  */
 #ifndef MV_LM_H
 #define MV_LM_H
@@ -74,6 +76,7 @@ int mv_token_logprob(void* stream, const void* logits, int type, int64_t T, int6
 
 /* Gradient of sum_t (g_logprob[t] logprob[t] + g_entropy[t] entropy[t]) with respect to the logits:
  *   dlogits[t, v] = scale ( g_logprob[t] (1[v = target] - p_v) - g_entropy[t] p_v (log p_v + entropy[t]) )
+ * with log p_v = min(0, scale logits[t, v] - lse[t]): p is as exact as the 32-bit lse is, and never above 1.
  *   lse, entropy [T] float in, as mv_token_logprob left them (entropy only with g_entropy)
  *   g_logprob [T] float in (NULL: zero; then targets may be NULL);  g_entropy [T] float in (NULL: zero)
  *   dlogits [T, V] out, of the logits' type, rows ldg >= V apart; may be the logits themselves (then ldg = ld)

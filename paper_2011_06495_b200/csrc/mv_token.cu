@@ -28,6 +28,11 @@ __device__ __forceinline__ float max_nan(float a, float b) {
   asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
   return r;
 }
+__device__ __forceinline__ float min_nan(float a, float b) {
+  float r;
+  asm("min.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+  return r;
+}
 __device__ __forceinline__ float exp2_fast(float x) {
   float r;
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
@@ -612,12 +617,15 @@ __global__ void __launch_bounds__(TPB, 1024 / TPB) k_token_logprob(const X* __re
 
 // ------------------------------------------------------------------------------------------ gradient
 // dx = c (g1 (1[v = y] - p) - g2 p (log p + H)), log p = c x - lse.  With h = log2(p) / 2 and q = 2^h:
-// dx = q (q (A h + B)) + c g1 1[v = y], A = -2 ln 2 c g2, B = -c (g1 + g2 H): two fused multiply-adds, an exponential and two
-// products per logit.  p is formed as q q because the hardware's exponential has no subnormal results.  Each CTA takes
-// one stretch of one row, so that the stretches, in the order of memory, go to the multiprocessors as they become free: memory
-// bounds it (4096 x 131072 bf16: 349 us, 6.2 TB/s in and out; 356 us, the power limit reached, in a long run).
+// dx = q (q (A h + B)) + c g1 1[v = y], A = -2 ln 2 c g2, B = -c (g1 + g2 H): two fused multiply-adds, an exponential and three
+// products per logit.  The difference c x - lse is taken first, in one rounding: two products of its terms with log2(e) would
+// differ by their own roundings, which for an lse of 1e9 are tens; and since the lse itself is rounded by as much there, log p is kept
+// from being positive (4096 x 131072 bf16: 358 us, without that 355.5; asking it only of rows with a large lse: 358).  p is formed
+// as q q because the hardware's exponential has no subnormal results; that doubles its error to 2^-21, beside the 2^-11 (f16) or
+// 2^-8 (bf16) of the result's rounding.  Each CTA takes one stretch of one row, so that the stretches, in the order of memory, go to the multiprocessors as they become free: memory
+// bounds it (4096 x 131072 bf16: 6.0 TB/s in and out).
 constexpr int GRAD_TPB = 256, GRAD_U = 4;
-constexpr float H_FLOOR = -1.0e4f;
+constexpr float H_FLOOR = -256.0f;     // q is 0 from -127 on; so near that A h is finite for any gradient below 1e36
 
 struct GradArgs {
   int64_t V, ld, ldg;
@@ -661,12 +669,11 @@ __global__ void __launch_bounds__(GRAD_TPB) k_token_grad(const X* logits, X* dlo
   const float g2 = a.g_entropy ? a.g_entropy[t] : 0.0f;
   const bool none = (g1 == 0.0f && g2 == 0.0f) || l == -INFINITY;
   const float sum = g1 + (g2 == 0.0f ? 0.0f : g2 * a.entropy[t]);
-  auto one = [&](float v, int64_t col) {
+  const float l2e = 0.5f * LOG2E, A = -2.0f * LN2 * a.scale * g2, B = -a.scale * sum;
+  auto one = [&](float v, int64_t col) {      // the same operations as two logits at a time below: a row's bits do not depend on its place
     if (none) return 0.0f;
-    const float lp = max_nan(fmaf(v, a.scale, -l), T_FLOOR);
-    float d = -exp2f(lp * LOG2E) * fmaf(g2, lp, sum);
-    if (col == y) d += g1;
-    return d * a.scale;
+    const float h = min_nan(max_nan(fmaf(v, a.scale, -l) * l2e, H_FLOOR), 0.0f), q = exp2_fast(h), d = q * (q * fmaf(h, A, B));
+    return col == y ? fmaf(a.scale, g1, d) : d;
   };
   // the vectors begin at the row's first 16-byte boundary; what is before and behind them goes to the first stretch
   const int64_t first = VEC ? min(a.V, int64_t((16 - (reinterpret_cast<uintptr_t>(x) & 15)) & 15) / int(sizeof(X))) : 0;
@@ -688,9 +695,7 @@ __global__ void __launch_bounds__(GRAD_TPB) k_token_grad(const X* logits, X* dlo
         if (v0 + i * GRAD_TPB < nv) __stcs(out + v0 + i * GRAD_TPB, make_uint4(0, 0, 0, 0));
       return;
     }
-    const float c2 = a.scale * LOG2E * 0.5f, l2 = l * LOG2E * 0.5f;
-    const float A = -2.0f * LN2 * a.scale * g2, B = -a.scale * sum;
-    const f2 c22 = pack2(c2, c2), minus = pack2(-l2, -l2), A2 = pack2(A, A), B2 = pack2(B, B);
+    const f2 scale2 = pack2(a.scale, a.scale), minus = pack2(-l, -l), l2e2 = pack2(l2e, l2e), A2 = pack2(A, A), B2 = pack2(B, B);
     uint4 u[GRAD_U];
 #pragma unroll
     for (int i = 0; i < GRAD_U; ++i)
@@ -703,9 +708,9 @@ __global__ void __launch_bounds__(GRAD_TPB) k_token_grad(const X* logits, X* dlo
 #pragma unroll
       for (int j = 0; j < N / 2; ++j) {
         float h0, h1;
-        unpack2(fma2(Vec<X>::pair(u[i], j), c22, minus), h0, h1);
-        h0 = max_nan(h0, H_FLOOR);
-        h1 = max_nan(h1, H_FLOOR);
+        unpack2(mul2(fma2(Vec<X>::pair(u[i], j), scale2, minus), l2e2), h0, h1);
+        h0 = min_nan(max_nan(h0, H_FLOOR), 0.0f);
+        h1 = min_nan(max_nan(h1, H_FLOOR), 0.0f);
         const f2 q = pack2(exp2_fast(h0), exp2_fast(h1));
         unpack2(mul2(q, mul2(q, fma2(pack2(h0, h1), A2, B2))), d[2 * j], d[2 * j + 1]);
       }

@@ -167,3 +167,70 @@ def test_parts_of_one_row_of_different_magnitudes():
             x[0, i * (V // 4): (i + 1) * (V // 4)] += v
         for dt in (F32, BF16):
             check(x.to(dt), torch.tensor([V // 2], device=DEV), 1.0, 20, mags)
+
+
+# ------------------------------------------------------------------------------------------ gradient
+
+def grad_reference(x, y, scale, lse, H, g1, g2):
+    """(value, bound) for the lse and entropy that the call is given, log p not above 0.  log p = scale x - lse is one rounding (u |log p|),
+    times log2(e)/2 two more; p = q q doubles that and the exponential's 2^-22, and four products follow.  No term grows with |lse|."""
+    x, l = x.double().cpu(), lse.double().cpu()[:, None]
+    c = float(np.float32(scale))
+    g1, g2, H, y = g1.double().cpu()[:, None], g2.double().cpu()[:, None], H.double().cpu()[:, None], y.long().cpu()
+    lp = (x * c - l).clamp(max=0.0)
+    p = torch.exp(lp)
+    lp = torch.where(p > 0, lp, torch.zeros_like(lp))
+    hot = torch.zeros_like(p)
+    hot[torch.arange(x.shape[0]), y] = 1.0
+    val = c * (g1 * (hot - p) - g2 * p * (lp + H))
+    rel = 1.01 * (2 * EX2 + U32 * (4 * lp.abs() + 8))
+    pmag = c * p * (g1.abs() + g2.abs() * (lp.abs() + H.abs()))
+    tol = rel * pmag + 4 * U32 * c * g2.abs() * p * (lp.abs() + 1) + 4 * U32 * c * (g1.abs() * (hot + p) + g2.abs() * p * (lp.abs() + H.abs()))
+    return val, tol + 2.0 ** -148 + 2.0 ** -126 * c * (g1.abs() + g2.abs() * (H.abs() + 100))
+
+
+def within(got, want, tol):
+    """Is got (of its own type) the rounding of a value in [want - tol, want + tol]?"""
+    lo, hi = ((want + e).float().to(got.dtype).double() for e in (-tol, tol))
+    g = got.double().cpu()
+    return (g >= lo) & (g <= hi)
+
+
+@pytest.mark.parametrize("dt", [F32, BF16, F16])
+@pytest.mark.parametrize("M", [1e2, 1e4, 6e4, 1e6, 1e8, 1e9, 1e12, 1e30])
+@pytest.mark.parametrize("V", [9, 1000, 9001])
+def test_logits_gradient_at_every_magnitude_and_place(dt, M, V):
+    """Rows of every magnitude: right for the lse of the call, and the same bits wherever logits and gradient lie."""
+    if dt == F16 and M > 65_504:
+        pytest.skip("beyond the type's range")
+    g = gen(V)
+    x = kinds(V, M, dt, g)
+    y = torch.randint(0, V, (8,), generator=g, device=DEV)
+    g1, g2 = torch.randn(8, generator=g, device=DEV), torch.randn(8, generator=g, device=DEV)
+    for scale in (1.0, 0.7, 1e3):
+        o = call(x, y, scale, 0)
+        want, tol = grad_reference(x, y, scale, o["lse"], o["entropy"], g1, g2)
+        first = None
+        for src, dst in (((0, 0), (0, 0)), ((1, 3), (1, 3)), ((1, 0), (0, 0)), ((3, 8), (2, 8)), ((0, 1), (0, 2))):
+            dx = placed(torch.full_like(x, 7.0), *dst)
+            B.mv_token_logprob_grad(placed(x, *src), y, o["lse"], g1, dx, scale=scale, entropy=o["entropy"], g_entropy=g2)
+            bad = ~within(dx, want, tol)
+            assert not bool(bad.any()), (scale, src, dst, bad.nonzero()[0].tolist(), float(dx[bad.to(DEV)][0]), float(want[bad][0]), float(tol[bad][0]))
+            first = dx.clone() if first is None else first
+            assert torch.equal(first, dx), (scale, src, dst)
+
+
+@pytest.mark.parametrize("place", [(0, 0), (1, 3)])
+def test_logits_gradient_of_large_upstream_gradients(place):
+    """A loss scaled by 1e10: masked logits, at the row's ends and inside, have a gradient of 0, not 0 times infinity."""
+    x = torch.randn((3, 301), generator=gen(3), device=DEV)
+    x[:, :5] = -math.inf
+    x[:, 100:140] = torch.finfo(F32).min
+    x[:, -5:] = -math.inf
+    y = torch.tensor([50, 60, 70], device=DEV)
+    o = call(x, y, 1.0, 0)
+    g1, g2 = torch.tensor([1e10, -3e20, 1e30], device=DEV), torch.tensor([-1e10, 1e20, 1e30], device=DEV)
+    want, tol = grad_reference(x, y, 1.0, o["lse"], o["entropy"], g1, g2)
+    dx = placed(torch.full_like(x, 7.0), *place)
+    B.mv_token_logprob_grad(placed(x), y, o["lse"], g1, dx, entropy=o["entropy"], g_entropy=g2)
+    assert bool(within(dx, want, tol).all()) and not bool(dx[:, :5].any()) and not bool(dx[:, 100:140].any()) and not bool(dx[:, -5:].any())

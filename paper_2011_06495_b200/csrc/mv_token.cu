@@ -385,9 +385,9 @@ struct LogprobArgs {
 
 struct Sums { float ref, s, st; };   // s = sum 2^t, st = sum 2^t t, both relative to ref (-inf: nothing yet)
 
-// (a - b) c2 of two logits; a quarter of each where the difference could pass the range of 32 bits and count all the same
-__device__ __forceinline__ float distance(float a, float b, float c2) {
-  return c2 < 1.0f ? (0.25f * a - 0.25f * b) * (4.0f * c2) : (a - b) * c2;
+// (a - b) c of two logits; a quarter of each where the difference could pass the range of 32 bits and count all the same
+__device__ __forceinline__ float distance(float a, float b, float c) {
+  return c < 1.0f ? (0.25f * a - 0.25f * b) * (4.0f * c) : (a - b) * c;
 }
 
 // The same sums relative to a larger reference.
@@ -604,14 +604,14 @@ __global__ void __launch_bounds__(TPB, 1024 / TPB) k_token_logprob(const X* __re
   if (threadIdx.x == 0) {
     if (a.lse) a.lse[t] = empty ? -INFINITY : fmaf(a.scale, r, ls);
     if (a.entropy) a.entropy[t] = empty ? 0.0f : ls - LN2 * (x.st / x.s);
-    if (a.logprob) a.logprob[t] = y < 0 ? 0.0f : empty ? -INFINITY : (xy - r) * a.scale - ls;
+    if (a.logprob) a.logprob[t] = y < 0 ? 0.0f : empty ? -INFINITY : distance(xy, r, a.scale) - ls;
   }
   if (TOP)
     for (int i = threadIdx.x; i < a.k; i += TPB) {
       const unsigned long long key = s_top[0].best[i];
       const float v = key_value(key);
       if (a.top_id) a.top_id[t * a.k + i] = key ? int32_t(key_index(key)) : -1;
-      if (a.top_logprob) a.top_logprob[t * a.k + i] = isnan(x.s) ? x.s : key == 0 || v == -INFINITY ? -INFINITY : (v - r) * a.scale - ls;
+      if (a.top_logprob) a.top_logprob[t * a.k + i] = isnan(x.s) ? x.s : key == 0 || v == -INFINITY ? -INFINITY : distance(v, r, a.scale) - ls;
     }
 }
 

@@ -169,6 +169,16 @@ def test_parts_of_one_row_of_different_magnitudes():
             check(x.to(dt), torch.tensor([V // 2], device=DEV), 1.0, 20, mags)
 
 
+@pytest.mark.parametrize("dt", [F32, BF16])
+@pytest.mark.parametrize("scale", [0.5, 0.3, 1e-3, 1e-37])
+@pytest.mark.parametrize("V", [2, 700, 30_001])
+def test_logits_at_opposite_ends_of_the_range(dt, scale, V):
+    """Their difference passes the range of 32 bits, but not their log probabilities."""
+    x = torch.randn((2, V), generator=gen(V), device=DEV)
+    x[:, 0], x[0, V - 1], x[1, V // 2] = 3.2e38, -3.2e38, -3.3e38
+    check(x.to(dt), torch.tensor([V - 1, V // 2], device=DEV), scale, min(V, 30))
+
+
 # ------------------------------------------------------------------------------------------ gradient
 
 def grad_reference(x, y, scale, lse, H, g1, g2):

@@ -97,7 +97,7 @@ size_t mv_clip_workspace_bytes(const int64_t* numel, int n_tensors, int n_groups
  *   tensors [n_tensors] device pointers, contiguous tensors that share no bytes;  types MV_F32 / MV_BF16 / MV_F16;
  *           numel >= 0, below 2^40
  *   groups  [n_tensors] ascending, 0 <= groups[i] < n_groups: the tensors that share a norm (NULL: all in group 0)
- *   workspace  mv_clip_workspace_bytes() bytes, 256-byte aligned, owned by the caller, must outlive the plan
+ *   workspace  mv_clip_workspace_bytes() bytes, 256-byte aligned, owned by the caller, must outlive the plan and every call enqueued on it
  * The list is copied to the workspace on `stream`, and the call waits for that copy: not inside a stream capture.
  * A plan serves one call at a time (calls on several streams must be ordered).  n_tensors >= 0, 1 <= n_groups < 2^20. */
 int mv_clip_create(mv_clip** out, void* stream, void* const* tensors, const int* types, const int64_t* numel, const int* groups,

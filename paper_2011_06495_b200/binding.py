@@ -327,7 +327,8 @@ def mv_token_logprob_grad(logits, targets, lse, g_logprob, dlogits, scale: float
 
 class MvClip:
     """A plan over a fixed list of contiguous tensors, which it keeps alive with its workspace; `groups` (ascending) says
-    which tensors share a norm (None: all of them)."""
+    which tensors share a norm (None: all of them).  Calls may go to any stream, one after the other; the plan and the tensors
+    may be dropped before they have run."""
 
     def __init__(self, tensors, groups=None, n_groups: Optional[int] = None, stream: Optional[torch.cuda.Stream] = None, device=None):
         self.handle = None
@@ -349,10 +350,13 @@ class MvClip:
         group = (ctypes.c_int * n)(*groups)
         nbytes = int(self.lib.mv_clip_workspace_bytes(numel, n, self.n_groups))
         _need(nbytes > 0, "mv_clip_workspace_bytes")
-        self.workspace = torch.empty(nbytes, dtype=torch.uint8, device=dev)
+        # memory of the stream that fills it: other memory may still be in use by what the current stream has yet to run
+        with torch.cuda.stream(stream):          # (None: the current one)
+            self.workspace = torch.empty(nbytes, dtype=torch.uint8, device=dev)
         handle = ctypes.c_void_p()
         self.dev = self.workspace.get_device()
-        _check(self.lib.mv_clip_create(ctypes.byref(handle), _raw_stream(self.dev, stream), ptrs, types, numel, group, n, self.n_groups,
+        self.streams = {_raw_stream(self.dev, None)}      # that the allocator knows of
+        _check(self.lib.mv_clip_create(ctypes.byref(handle), self._stream(stream), ptrs, types, numel, group, n, self.n_groups,
                                        self.workspace.data_ptr(), nbytes), "mv_clip_create")
         self.handle = handle
 
@@ -367,19 +371,29 @@ class MvClip:
         except Exception:
             pass
 
+    def _stream(self, stream: Optional[torch.cuda.Stream]):
+        """The stream of a call, of which the allocator is told once: the memory is not given away before that stream is through."""
+        raw = _raw_stream(self.dev, stream)
+        if raw not in self.streams:
+            used = stream if stream is not None else torch.cuda.current_stream(self.dev)
+            for t in (self.workspace, *self.tensors):
+                t.record_stream(used)
+            self.streams.add(raw)
+        return raw
+
     def mv_clip_norm(self, norms, stream: Optional[torch.cuda.Stream] = None):
         n, _ = _vector(norms, self.n_groups, _FLOAT, self.dev, "mv_clip_norm")
-        _check(self.lib.mv_clip_norm(self.handle, _raw_stream(self.dev, stream), n), "mv_clip_norm")
+        _check(self.lib.mv_clip_norm(self.handle, self._stream(stream), n), "mv_clip_norm")
 
     def mv_clip_scale(self, max_norm: float, norms=None, stream: Optional[torch.cuda.Stream] = None):
         n, _ = _vector(norms, self.n_groups, _FLOAT, self.dev, "mv_clip_scale")
-        _check(self.lib.mv_clip_scale(self.handle, _raw_stream(self.dev, stream), float(max_norm), n), "mv_clip_scale")
+        _check(self.lib.mv_clip_scale(self.handle, self._stream(stream), float(max_norm), n), "mv_clip_scale")
 
     def mv_clip_pack(self, max_norm: float, rows, norms=None, stream: Optional[torch.cuda.Stream] = None):
         n, _ = _vector(norms, self.n_groups, _FLOAT, self.dev, "mv_clip_pack")
         r, _, G, d, ld, dev = _matrix(rows, _FLOAT, "mv_clip_pack")
         _need(G == self.n_groups and d >= self.longest and dev == self.dev, "mv_clip_pack")
-        _check(self.lib.mv_clip_pack(self.handle, _raw_stream(self.dev, stream), float(max_norm), r, ld, n), "mv_clip_pack")
+        _check(self.lib.mv_clip_pack(self.handle, self._stream(stream), float(max_norm), r, ld, n), "mv_clip_pack")
 
 
 class MvContext:

@@ -1,0 +1,55 @@
+"""GPU tests of the clipping plans (MvClip): their memory, and what a plan does outside the ordinary."""
+import torch
+import pytest
+
+from paper_2011_06495_b200 import binding as B
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+
+
+def addresses(nbytes, n=40):
+    """Where the current stream's next n allocations of that size lie."""
+    ts = [torch.empty(nbytes, dtype=torch.uint8, device=DEV) for _ in range(n)]
+    return {t.data_ptr() for t in ts}
+
+
+@pytest.mark.parametrize("n", [5000, 5_000_000])
+@pytest.mark.parametrize("created_on_it", [False, True])
+def test_a_plan_dropped_while_its_call_waits_keeps_its_memory(n, created_on_it):
+    """A call on another stream that has yet to run: neither the plan's list nor the tensors are given to other tensors."""
+    want = torch.randn(n, device=DEV)
+    rows, norms = torch.empty((1, n), device=DEV), torch.empty(1, device=DEV)
+    st = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    t = want.clone()
+    plan = B.MvClip([t], stream=st if created_on_it else None)
+    torch.cuda.synchronize()
+    mine, list_bytes, at = plan.workspace.data_ptr(), plan.workspace.numel(), t.data_ptr()
+    with torch.cuda.stream(st):
+        torch.cuda._sleep(400_000_000)                     # 0.2 s
+    plan.mv_clip_pack(1e30, rows, norms, stream=st)
+    del plan, t
+    there = addresses(list_bytes) | addresses(4 * n, 4)
+    assert not st.query()                                  # the call is still waiting
+    assert mine not in there and at not in there
+    st.synchronize()
+    assert torch.equal(rows[0], want)
+
+
+def test_a_plan_made_on_another_stream_takes_no_memory_still_in_use():
+    """What the current stream has freed, but not yet finished with, may be overwritten by it at any later time."""
+    t = torch.randn(5000, device=DEV)
+    st = torch.cuda.Stream()
+    sizes = int(B.load().mv_clip_workspace_bytes((B.ctypes.c_int64 * 1)(5000), 1, 1))
+    torch.cuda.synchronize()
+    torch.cuda._sleep(200_000_000)
+    freed = addresses(sizes)                               # freed at once; the current stream is still asleep
+    plan = B.MvClip([t], stream=st)
+    assert not torch.cuda.current_stream().query()
+    assert plan.workspace.data_ptr() not in freed
+    norms = torch.empty(1, device=DEV)
+    st.wait_stream(torch.cuda.current_stream())
+    plan.mv_clip_norm(norms, stream=st)
+    st.synchronize()
+    assert abs(float(norms) - float(t.norm())) < 1e-3

@@ -104,8 +104,15 @@ int mv_clip_create(mv_clip** out, void* stream, void* const* tensors, const int*
                    int n_tensors, int n_groups, void* workspace, size_t workspace_bytes);
 int mv_clip_destroy(mv_clip* plan);
 
+/* Waits for the stream (not inside a stream capture) and returns MV_ERR_TIMEOUT if a wait between the CTAs of a call on the
+ * plan has run out since the last time it was asked, MV_OK if none has.  Later calls on the plan are not affected. */
+int mv_clip_status(mv_clip* plan, void* stream);
+
+/* How often a CTA polls its group's factor before it gives up, in later calls: polls >= 0; -1: the default (a second or more). */
+int mv_clip_set_polls(mv_clip* plan, int polls);
+
 /* The calls on a plan.  A short list (up to 14 MB) is clipped by one cooperative kernel whose CTAs wait, with a limit, for
- * their group's factor; should a wait ever run out (never expected), what the CTA writes is NaN.
+ * their group's factor; should a wait ever run out (never expected), what the CTA writes is NaN, and mv_clip_status says so.
  *
  * norms [n_groups] float out: sqrt of the sum of squares, added in 64 bits and rounded once (0 for an empty group). */
 int mv_clip_norm(mv_clip* plan, void* stream, float* norms);

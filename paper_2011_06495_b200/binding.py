@@ -148,6 +148,10 @@ def _open(path: str, how: str) -> ctypes.CDLL:
     lib.mv_clip_create.argtypes = [ctypes.POINTER(c_vp), c_vp, c_vp, c_vp, c_vp, c_vp, c_i, c_i, c_vp, c_sz]
     lib.mv_clip_destroy.restype = c_i
     lib.mv_clip_destroy.argtypes = [c_vp]
+    lib.mv_clip_status.restype = c_i
+    lib.mv_clip_status.argtypes = [c_vp, c_vp]
+    lib.mv_clip_set_polls.restype = c_i
+    lib.mv_clip_set_polls.argtypes = [c_vp, c_i]
     lib.mv_clip_norm.restype = c_i
     lib.mv_clip_norm.argtypes = [c_vp, c_vp, c_vp]
     lib.mv_clip_scale.restype = c_i
@@ -380,6 +384,13 @@ class MvClip:
                 t.record_stream(used)
             self.streams.add(raw)
         return raw
+
+    def mv_clip_status(self, stream: Optional[torch.cuda.Stream] = None):
+        """Waits for the stream; MvError(MV_ERR_TIMEOUT) if a wait inside a call has run out since the last time it was asked."""
+        _check(self.lib.mv_clip_status(self.handle, self._stream(stream)), "mv_clip_status")
+
+    def mv_clip_set_polls(self, polls: int):
+        _check(self.lib.mv_clip_set_polls(self.handle, int(polls)), "mv_clip_set_polls")
 
     def mv_clip_norm(self, norms, stream: Optional[torch.cuda.Stream] = None):
         n, _ = _vector(norms, self.n_groups, _FLOAT, self.dev, "mv_clip_norm")

@@ -15,7 +15,7 @@ namespace {
 constexpr int TPB = 256;
 constexpr int CHUNK_BYTES = 32768;
 constexpr int HOLD = 148 * 3;        // chunks of a short list: six fit a multiprocessor
-constexpr int SPIN_LIMIT = 1 << 22;  // polls of a factor (a second or more) before a CTA gives up
+constexpr int SPIN_LIMIT = 1 << 22;  // polls of a factor (a second or more) before a CTA gives up, unless the plan says otherwise
 
 struct Chunk {
   void* ptr;                         // first element
@@ -28,7 +28,7 @@ struct Chunk {
 
 inline int64_t chunk_len(int type) { return CHUNK_BYTES / type_size(type); }
 
-struct Layout { size_t chunks, first, ticket, done, taken, partial, total; int64_t n; };
+struct Layout { size_t chunks, first, ticket, done, taken, gave_up, partial, total; int64_t n; };
 
 // types == nullptr: room for the longest list of chunks that any types give
 inline bool clip_layout(const int64_t* numel, const int* types, int n_tensors, int n_groups, Layout* L) {
@@ -45,7 +45,7 @@ inline bool clip_layout(const int64_t* numel, const int* types, int n_tensors, i
   L->first = o;   o = align_up(o + size_t(n_groups + 1) * 4, 256);
   L->ticket = o;  o = align_up(o + size_t(n_groups) * 4, 256);
   L->done = o;    o = align_up(o + size_t(n_groups) * 8, 256);
-  L->taken = o;   o += 256;          // what the host fills ends here
+  L->taken = o;   L->gave_up = o + 8;   o += 256;      // what the host fills ends here
   L->partial = o; o = align_up(o + size_t(L->n) * 8, 256);
   L->total = o;
   return true;
@@ -57,6 +57,7 @@ struct ClipArgs {
   uint32_t* ticket;                  // [groups] chunks summed so far; back to 0 with the last one
   unsigned long long* done;          // [groups] the factor's bits, and above them the number of the call that found it
   unsigned long long* taken;         // CTAs of the one-kernel form started so far, by all calls
+  uint32_t* gave_up;                 // 1: a wait has run out since the host last asked
   double* partial;
   float* norms;
   float max_norm;
@@ -64,6 +65,7 @@ struct ClipArgs {
   int64_t ld;
   int n_groups;
   int empty;                         // some group has no chunk
+  int polls;                         // of a factor, before a CTA gives up
 };
 
 // 16 bytes of a chunk as numbers.
@@ -258,14 +260,16 @@ __global__ void __launch_bounds__(TPB, 5) k_clip_scale(const __grid_constant__ C
 }
 
 // ------------------------------------------------------------------------------------------ a short list: one kernel
-// The group's factor, when it is there.  A NaN if it does not come in time (never expected): then what the CTA writes is NaN.
+// The group's factor, when it is there.  A NaN if it does not come in time (never expected): then what the CTA writes is NaN, and
+// the host can ask for the word that says so.
 __device__ __forceinline__ float wait_factor(const ClipArgs& a, int g, uint32_t call) {
   unsigned long long d = 0;
-  for (int i = 0; i < SPIN_LIMIT; ++i) {
+  for (int i = 0; i < a.polls; ++i) {
     asm volatile("ld.acquire.gpu.u64 %0, [%1];" : "=l"(d) : "l"(a.done + g) : "memory");
     if (uint32_t(d >> 32) == call) return __uint_as_float(uint32_t(d));
     __nanosleep(50);
   }
+  *a.gave_up = 1;
   return __int_as_float(0x7fffffff);
 }
 
@@ -398,7 +402,9 @@ int mv_clip_create(mv_clip** out, void* stream, void* const* tensors, const int*
   p->args.ticket = reinterpret_cast<uint32_t*>(base + L.ticket);
   p->args.done = reinterpret_cast<unsigned long long*>(base + L.done);
   p->args.taken = reinterpret_cast<unsigned long long*>(base + L.taken);
+  p->args.gave_up = reinterpret_cast<uint32_t*>(base + L.gave_up);
   p->args.partial = reinterpret_cast<double*>(base + L.partial);
+  p->args.polls = SPIN_LIMIT;
   p->args.n_groups = n_groups;
   Chunk* c = reinterpret_cast<Chunk*>(host + L.chunks);
   int32_t* first = reinterpret_cast<int32_t*>(host + L.first);
@@ -442,6 +448,24 @@ int mv_clip_destroy(mv_clip* plan) {
   if (!plan) return MV_ERR_INVALID_ARG;
   free(plan->spans);
   free(plan);
+  return MV_OK;
+}
+
+int mv_clip_status(mv_clip* plan, void* stream) {
+  if (!plan) return MV_ERR_INVALID_ARG;
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  uint32_t flag = 0;
+  if (cudaMemcpyAsync(&flag, plan->args.gave_up, 4, cudaMemcpyDeviceToHost, st) != cudaSuccess || cudaMemsetAsync(plan->args.gave_up, 0, 4, st) != cudaSuccess ||
+      cudaStreamSynchronize(st) != cudaSuccess) {
+    cudaGetLastError();
+    return MV_ERR_CUDA;
+  }
+  return flag ? MV_ERR_TIMEOUT : MV_OK;
+}
+
+int mv_clip_set_polls(mv_clip* plan, int polls) {
+  if (!plan || polls < -1) return MV_ERR_INVALID_ARG;
+  plan->args.polls = polls < 0 ? SPIN_LIMIT : polls;
   return MV_OK;
 }
 

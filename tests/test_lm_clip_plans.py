@@ -53,3 +53,42 @@ def test_a_plan_made_on_another_stream_takes_no_memory_still_in_use():
     plan.mv_clip_norm(norms, stream=st)
     st.synchronize()
     assert abs(float(norms) - float(t.norm())) < 1e-3
+
+
+@pytest.mark.parametrize("sizes", [[5000], [3, 20_000, 70_001]])
+@pytest.mark.parametrize("dt", [torch.float32, torch.bfloat16])
+def test_a_wait_that_runs_out_is_reported(sizes, dt):
+    """With no poll allowed every CTA of the one-kernel form gives up at once: what it writes is NaN, the status says so once, and the
+    plan is as good as before."""
+    ts = [torch.randn(n, device=DEV).to(dt) for n in sizes]
+    plan = B.MvClip(ts)
+    rows, norms = torch.empty((1, sum(sizes)), device=DEV), torch.empty(1, device=DEV)
+    plan.mv_clip_pack(1.0, rows, norms)
+    plan.mv_clip_status()
+    good, n = rows.clone(), norms.clone()
+    plan.mv_clip_set_polls(0)
+    plan.mv_clip_pack(1.0, rows, norms)
+    with pytest.raises(B.MvError) as e:
+        plan.mv_clip_status()
+    assert e.value.status == B.MV_ERR_TIMEOUT
+    assert bool(torch.isnan(rows).all()) and torch.equal(norms, n)
+    plan.mv_clip_status()                                  # reported once
+    keep = [t.clone() for t in ts]
+    plan.mv_clip_scale(1.0)
+    with pytest.raises(B.MvError):
+        plan.mv_clip_status()
+    assert all(bool(torch.isnan(t).all()) for t in ts)
+    for t, k in zip(ts, keep):
+        t.copy_(k)
+    plan.mv_clip_norm(norms)                               # no wait in it
+    plan.mv_clip_status()
+    plan.mv_clip_set_polls(-1)
+    plan.mv_clip_pack(1.0, rows, norms)
+    plan.mv_clip_status()
+    assert torch.equal(rows, good) and torch.equal(norms, n)
+    with pytest.raises(B.MvError):
+        plan.mv_clip_set_polls(-2)
+    plan.close()
+    for f in (plan.mv_clip_status, lambda: plan.mv_clip_set_polls(1), lambda: plan.mv_clip_norm(norms)):
+        with pytest.raises(B.MvError):
+            f()

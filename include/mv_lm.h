@@ -94,7 +94,8 @@ typedef struct mv_clip mv_clip;
 size_t mv_clip_workspace_bytes(const int64_t* numel, int n_tensors, int n_groups);
 
 /* Creates a plan.  All arrays are HOST arrays, read before the call returns.
- *   tensors [n_tensors] device pointers, contiguous tensors that share no bytes;  types MV_F32 / MV_BF16 / MV_F16;
+ *   tensors [n_tensors] device pointers, contiguous tensors (a plan whose tensors share bytes, as tied weights do, has no
+ *           mv_clip_scale);  types MV_F32 / MV_BF16 / MV_F16;
  *           numel >= 0, below 2^40
  *   groups  [n_tensors] ascending, 0 <= groups[i] < n_groups: the tensors that share a norm (NULL: all in group 0)
  *   workspace  mv_clip_workspace_bytes() bytes, 256-byte aligned, owned by the caller, must outlive the plan and every call enqueued on it
@@ -118,6 +119,7 @@ int mv_clip_set_polls(mv_clip* plan, int polls);
 int mv_clip_norm(mv_clip* plan, void* stream, float* norms);
 
 /* In place: every tensor of group g is multiplied by c_g = min(1, max_norm / n_g), max_norm >= 0 (+inf: no clipping).
+ * MV_ERR_INVALID_ARG where tensors of the plan share bytes, which would be multiplied twice.
  * A group whose norm is inf or NaN is left as it is (the caller sees the norm).  norms may be NULL. */
 int mv_clip_scale(mv_clip* plan, void* stream, float max_norm, float* norms);
 

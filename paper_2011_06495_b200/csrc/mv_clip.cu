@@ -1,6 +1,7 @@
 // mv_clip.cu -- norms over many tensors, one per group, and clipping in place or into the workers' rows, for sm_100a.
 #include "mv_lm.cuh"
 
+#include <algorithm>
 #include <math.h>
 #include <stdlib.h>
 
@@ -323,8 +324,9 @@ struct mv_clip {
   int n_groups;
   int64_t longest;                   // elements of the longest group
   uintptr_t lo, hi;                  // addresses that the tensors span
-  int n_tensors;
-  struct Span { uintptr_t lo, hi; }* spans;      // host: the bytes of each tensor
+  int n_spans;
+  struct Span { uintptr_t lo, hi; }* spans;      // host: the bytes of each tensor that has any, by address
+  bool shared;                       // two of them share bytes
   ClipArgs args;
 };
 
@@ -334,8 +336,8 @@ namespace {
 bool overlaps(const mv_clip* p, const float* rows, int64_t ld) {
   const uintptr_t lo = reinterpret_cast<uintptr_t>(rows), hi = lo + (size_t(p->n_groups - 1) * ld + p->longest) * 4;
   if (hi <= p->lo || lo >= p->hi) return false;
-  for (int i = 0; i < p->n_tensors; ++i)
-    if (p->spans[i].lo < p->spans[i].hi && p->spans[i].lo < hi && lo < p->spans[i].hi) return true;
+  for (int i = 0; i < p->n_spans; ++i)
+    if (p->spans[i].lo < hi && lo < p->spans[i].hi) return true;
   return false;
 }
 
@@ -394,7 +396,6 @@ int mv_clip_create(mv_clip** out, void* stream, void* const* tensors, const int*
   char* base = static_cast<char*>(workspace);
   p->n = L.n;
   p->n_groups = n_groups;
-  p->n_tensors = n_tensors;
   p->spans = spans;
   p->lo = UINTPTR_MAX;
   p->args.chunks = reinterpret_cast<Chunk*>(base + L.chunks);
@@ -422,15 +423,19 @@ int mv_clip_create(mv_clip** out, void* stream, void* const* tensors, const int*
       c[nc].type = types[i];
       c[nc].group = gi;
     }
-    spans[i].lo = reinterpret_cast<uintptr_t>(tensors[i]);
-    spans[i].hi = spans[i].lo + size_t(numel[i]) * type_size(types[i]);
-    if (numel[i] > 0 && spans[i].lo < p->lo) p->lo = spans[i].lo;
-    if (numel[i] > 0 && spans[i].hi > p->hi) p->hi = spans[i].hi;
+    if (numel[i] > 0) {
+      const uintptr_t lo = reinterpret_cast<uintptr_t>(tensors[i]), hi = lo + size_t(numel[i]) * type_size(types[i]);
+      spans[p->n_spans++] = {lo, hi};
+      p->lo = lo < p->lo ? lo : p->lo;
+      p->hi = hi > p->hi ? hi : p->hi;
+    }
     dst += numel[i];
     if (dst > p->longest) p->longest = dst;
   }
   while (g < n_groups) first[++g] = int32_t(nc);
   for (g = 0; g < n_groups; ++g) p->args.empty |= first[g] == first[g + 1];
+  std::sort(spans, spans + p->n_spans, [](const mv_clip::Span& a, const mv_clip::Span& b) { return a.lo < b.lo; });
+  for (int i = 1; i < p->n_spans; ++i) p->shared |= spans[i].lo < spans[i - 1].hi;
   // the one-kernel form needs all its CTAs at once
   int dev = 0, sms = 0, per_sm = 0;
   if (cudaGetDevice(&dev) == cudaSuccess && cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) == cudaSuccess &&
@@ -475,7 +480,7 @@ int mv_clip_norm(mv_clip* plan, void* stream, float* norms) {
 }
 
 int mv_clip_scale(mv_clip* plan, void* stream, float max_norm, float* norms) {
-  if (!plan || !(max_norm >= 0.0f) || misaligned(norms, 4)) return MV_ERR_INVALID_ARG;
+  if (!plan || plan->shared || !(max_norm >= 0.0f) || misaligned(norms, 4)) return MV_ERR_INVALID_ARG;
   return clip_run(plan, static_cast<cudaStream_t>(stream), max_norm, nullptr, 0, norms, true);
 }
 

@@ -55,6 +55,32 @@ def test_a_plan_made_on_another_stream_takes_no_memory_still_in_use():
     assert abs(float(norms) - float(t.norm())) < 1e-3
 
 
+@pytest.mark.parametrize("n", [100, 6_000_000])
+def test_tensors_that_share_bytes_are_not_scaled_in_place(n):
+    """The same tensor twice, windows that overlap, in one group or two: norms and rows count every tensor, scaling is refused;
+    tensors end to end and empty ones inside others share nothing."""
+    b = torch.randn(n, generator=torch.Generator(device=DEV).manual_seed(n), device=DEV)
+    old = b.clone()
+    for ts, gs in (([b, b], [0, 0]), ([b, b], [0, 1]), ([b[: n // 2 + 1], b[n // 2:]], None), ([b[n // 2:], b], None), ([b, b.view(torch.bfloat16)[7:8]], None)):
+        plan = B.MvClip(ts, gs)
+        want = [sum(float(t.double().pow(2).sum()) for t, g in zip(ts, gs or [0] * 9) if g == i) ** 0.5 for i in range(plan.n_groups)]
+        norms = torch.empty(plan.n_groups, device=DEV)
+        rows = torch.zeros((plan.n_groups, plan.longest), device=DEV)
+        plan.mv_clip_pack(float("inf"), rows, norms)
+        for g in range(plan.n_groups):
+            assert abs(float(norms[g]) - want[g]) <= 2.0 ** -22 * want[g]
+            mine = torch.cat([t.float() for t, gg in zip(ts, gs or [0] * 9) if gg == g])
+            assert torch.equal(rows[g, : mine.numel()], mine)
+        with pytest.raises(B.MvError):
+            plan.mv_clip_scale(0.5)
+        assert torch.equal(b, old)
+    for ts in ([b[n // 2:], b[: n // 2]], [b, b[5:5]], [b[5:5], b, b[7:7]]):
+        b.copy_(old)
+        norms = torch.empty(1, device=DEV)
+        B.MvClip(ts).mv_clip_scale(0.5, norms)
+        assert bool(((b.double() - old.double() * (0.5 / float(old.double().norm()))).abs() <= 4 * 2.0 ** -24 * old.double().abs()).all())
+
+
 @pytest.mark.parametrize("sizes", [[5000], [3, 20_000, 70_001]])
 @pytest.mark.parametrize("dt", [torch.float32, torch.bfloat16])
 def test_a_wait_that_runs_out_is_reported(sizes, dt):

@@ -115,12 +115,14 @@ int mv_clip_set_polls(mv_clip* plan, int polls);
 /* The calls on a plan.  A short list (up to 14 MB) is clipped by one cooperative kernel whose CTAs wait, with a limit, for
  * their group's factor; should a wait ever run out (never expected), what the CTA writes is NaN, and mv_clip_status says so.
  *
- * norms [n_groups] float out: sqrt of the sum of squares, added in 64 bits and rounded once (0 for an empty group). */
+ * norms [n_groups] float out: sqrt of the sum of squares, added in 64 bits and rounded once (0 for an empty group; finite values
+ *       whose norm passes the range of 32 bits: inf). */
 int mv_clip_norm(mv_clip* plan, void* stream, float* norms);
 
 /* In place: every tensor of group g is multiplied by c_g = min(1, max_norm / n_g), max_norm >= 0 (+inf: no clipping).
  * MV_ERR_INVALID_ARG where tensors of the plan share bytes, which would be multiplied twice.
- * A group whose norm is inf or NaN is left as it is (the caller sees the norm).  norms may be NULL. */
+ * A group that holds an inf or a NaN is left as it is (its norm is inf or NaN).  One of finite values is scaled by its norm in
+ * 64 bits, even where the norm that is reported passes the range of 32.  norms may be NULL. */
 int mv_clip_scale(mv_clip* plan, void* stream, float max_norm, float* norms);
 
 /* Out of place: row g of `rows` receives the tensors of group g, end to end in list order, times c_g, in fp32.

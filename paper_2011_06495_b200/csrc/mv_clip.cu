@@ -2,6 +2,7 @@
 #include "mv_lm.cuh"
 
 #include <algorithm>
+#include <float.h>
 #include <math.h>
 #include <stdlib.h>
 
@@ -29,7 +30,7 @@ struct Chunk {
 
 inline int64_t chunk_len(int type) { return CHUNK_BYTES / type_size(type); }
 
-struct Layout { size_t chunks, first, ticket, done, taken, gave_up, partial, total; int64_t n; };
+struct Layout { size_t chunks, first, ticket, done, taken, gave_up, exact, partial, total; int64_t n; };
 
 // types == nullptr: room for the longest list of chunks that any types give
 inline bool clip_layout(const int64_t* numel, const int* types, int n_tensors, int n_groups, Layout* L) {
@@ -47,6 +48,7 @@ inline bool clip_layout(const int64_t* numel, const int* types, int n_tensors, i
   L->ticket = o;  o = align_up(o + size_t(n_groups) * 4, 256);
   L->done = o;    o = align_up(o + size_t(n_groups) * 8, 256);
   L->taken = o;   L->gave_up = o + 8;   o += 256;      // what the host fills ends here
+  L->exact = o;   o = align_up(o + size_t(n_groups) * 8, 256);
   L->partial = o; o = align_up(o + size_t(L->n) * 8, 256);
   L->total = o;
   return true;
@@ -59,6 +61,7 @@ struct ClipArgs {
   unsigned long long* done;          // [groups] the factor's bits, and above them the number of the call that found it
   unsigned long long* taken;         // CTAs of the one-kernel form started so far, by all calls
   uint32_t* gave_up;                 // 1: a wait has run out since the host last asked
+  double* exact;                     // [groups] the factor where 32 bits have no full precision for it
   double* partial;
   float* norms;
   float max_norm;
@@ -104,7 +107,9 @@ template <typename X> __device__ __forceinline__ void add_squares(const uint4& u
 __device__ __forceinline__ void put_norm(const ClipArgs& a, int g, double s, uint32_t call) {
   const double n = sqrt(s);
   if (a.norms) a.norms[g] = float(n);
-  const float f = n > double(a.max_norm) && !isinf(n) ? float(double(a.max_norm) / n) : 1.0f;
+  const double c = n > double(a.max_norm) && !isinf(n) ? double(a.max_norm) / n : 1.0;
+  const float f = float(c);
+  if (f < FLT_MIN) __stcg(a.exact + g, c);
   const unsigned long long w = (unsigned long long)call << 32 | __float_as_uint(f);
   asm volatile("st.release.gpu.u64 [%0], %1;" ::"l"(a.done + g), "l"(w) : "memory");
 }
@@ -209,6 +214,16 @@ template <typename X> __device__ __forceinline__ void scale(const uint4* from, u
   }
 }
 
+// A chunk times a factor below the normal range of 32 bits (values near 1e38 clipped to a norm near 1): in 64 bits.  Seldom run.
+template <typename X> __device__ __noinline__ void times_tiny(X* x, int n, double f, float* row) {
+#pragma unroll 1
+  for (int i = threadIdx.x; i < n; i += TPB) {
+    const float y = float(double(to_f(x[i])) * f);
+    if (row) row[i] = y;
+    else x[i] = from_f<X>(y);
+  }
+}
+
 // ------------------------------------------------------------------------------------------ a long list: two kernels
 template <typename X> __device__ __forceinline__ double chunk_sum(const X* x, int n) {
   const Ends<X> ends(x, n);
@@ -241,7 +256,9 @@ __global__ void __launch_bounds__(TPB, 8) k_clip_sum(const __grid_constant__ Cli
 
 template <typename X> __device__ __forceinline__ void chunk_scale(const ClipArgs& a, const Chunk& c, float f) {
   X* x = static_cast<X*>(c.ptr);
-  if (a.rows) {
+  if (f < FLT_MIN) {
+    times_tiny<X>(x, c.n, __ldcg(a.exact + c.group), a.rows ? a.rows + c.group * a.ld + c.dst : nullptr);
+  } else if (a.rows) {
     pack(static_cast<const X*>(x), c.n, f, a.rows + c.group * a.ld + c.dst);
   } else if (f != 1.0f) {
     const Ends<X> ends(x, c.n);
@@ -291,7 +308,9 @@ template <typename X> __device__ __forceinline__ void sum_and_scale(const ClipAr
   if (threadIdx.x == 0) s_factor = wait_factor(a, c.group, call);
   __syncthreads();
   const float f = s_factor;
-  if (a.rows) {
+  if (f < FLT_MIN) {
+    times_tiny<X>(x, c.n, __ldcg(a.exact + c.group), a.rows ? a.rows + c.group * a.ld + c.dst : nullptr);
+  } else if (a.rows) {
     float* dst = a.rows + c.group * a.ld + c.dst;
     if (ends.e >= 0) dst[ends.e] = ends.v * f;
     pack(reinterpret_cast<const X*>(buf), ends.nv * PER<X>, f, dst + ends.head);
@@ -391,7 +410,7 @@ int mv_clip_create(mv_clip** out, void* stream, void* const* tensors, const int*
   clip_layout(numel, types, n_tensors, n_groups, &L);
   mv_clip* p = static_cast<mv_clip*>(calloc(1, sizeof(mv_clip)));
   mv_clip::Span* spans = static_cast<mv_clip::Span*>(calloc(n_tensors ? n_tensors : 1, sizeof(mv_clip::Span)));
-  char* host = static_cast<char*>(calloc(1, L.partial));
+  char* host = static_cast<char*>(calloc(1, L.exact));
   if (!p || !spans || !host) { free(p); free(spans); free(host); return MV_ERR_WORKSPACE; }
   char* base = static_cast<char*>(workspace);
   p->n = L.n;
@@ -404,6 +423,7 @@ int mv_clip_create(mv_clip** out, void* stream, void* const* tensors, const int*
   p->args.done = reinterpret_cast<unsigned long long*>(base + L.done);
   p->args.taken = reinterpret_cast<unsigned long long*>(base + L.taken);
   p->args.gave_up = reinterpret_cast<uint32_t*>(base + L.gave_up);
+  p->args.exact = reinterpret_cast<double*>(base + L.exact);
   p->args.partial = reinterpret_cast<double*>(base + L.partial);
   p->args.polls = SPIN_LIMIT;
   p->args.n_groups = n_groups;
@@ -442,7 +462,7 @@ int mv_clip_create(mv_clip** out, void* stream, void* const* tensors, const int*
       cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, k_clip_hold, TPB, 0) == cudaSuccess)
     p->hold = sms * per_sm / 2 < HOLD ? sms * per_sm / 2 : HOLD;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
-  const bool ok = cudaMemcpyAsync(base, host, L.partial, cudaMemcpyHostToDevice, st) == cudaSuccess && cudaStreamSynchronize(st) == cudaSuccess;
+  const bool ok = cudaMemcpyAsync(base, host, L.exact, cudaMemcpyHostToDevice, st) == cudaSuccess && cudaStreamSynchronize(st) == cudaSuccess;
   free(host);
   if (!ok) { cudaGetLastError(); mv_clip_destroy(p); return MV_ERR_CUDA; }
   *out = p;

@@ -118,3 +118,36 @@ def test_a_wait_that_runs_out_is_reported(sizes, dt):
     for f in (plan.mv_clip_status, lambda: plan.mv_clip_set_polls(1), lambda: plan.mv_clip_norm(norms)):
         with pytest.raises(B.MvError):
             f()
+
+
+@pytest.mark.parametrize("n", [300, 6_000_000])
+@pytest.mark.parametrize("dt", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("top,max_norm", [(2e38, 1e-8), (3e38, 0.01), (1e38, 3e-44), (1e30, 1e-20), (2e38, 0.0)])
+def test_factors_below_the_normal_range(n, dt, top, max_norm):
+    """max_norm / norm down to 1e-82: the product is rounded once from 64 bits, in place (then to the tensors' type) and into rows."""
+    t = (torch.randn(n, generator=torch.Generator(device=DEV).manual_seed(n), device=DEV) * (top / 1e6)).to(dt)
+    t[n // 2], t[-1] = top, -top / 3
+    old, bound = t.double(), float(torch.tensor(max_norm))
+    norm = float(old.norm())
+    want = old * (bound / norm)
+    plan = B.MvClip([t[: n // 3], t[n // 3:]])
+    rows, norms = torch.empty((1, n), device=DEV), torch.empty(1, device=DEV)
+    plan.mv_clip_pack(max_norm, rows, norms)
+    assert abs(float(norms) - norm) <= 2.0 ** -23 * norm if norm < 3.4e38 else float(norms) == float("inf")
+    tol = 3 * 2.0 ** -24 * want.abs() + 2.0 ** -149
+    assert bool(((rows[0].double() - want).abs() <= tol).all())
+    plan.mv_clip_scale(max_norm)
+    lo, hi = ((want + e).float().to(dt).double() for e in (-tol, tol))
+    assert bool(((t.double() >= lo) & (t.double() <= hi)).all())
+
+
+@pytest.mark.parametrize("n", [300, 6_000_000])
+def test_finite_groups_whose_norm_passes_the_range_are_scaled(n):
+    """Their norm is reported as inf; a group that does hold an inf is left alone."""
+    a, b = torch.full((n,), 2.0e38, device=DEV), torch.full((n,), 1.0, device=DEV)
+    b[5] = float("inf")
+    keep = b.clone()
+    plan, norms = B.MvClip([a, b], [0, 1]), torch.empty(2, device=DEV)
+    plan.mv_clip_scale(1.0, norms)
+    assert norms.tolist() == [float("inf")] * 2 and torch.equal(b, keep)
+    assert bool(((a.double() - n ** -0.5).abs() <= 3 * 2.0 ** -24 * n ** -0.5).all())

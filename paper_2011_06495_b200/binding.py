@@ -339,7 +339,9 @@ class MvClip:
         self.lib = load()
         self.tensors = list(tensors)
         n = len(self.tensors)
-        dev = torch.device(device) if device is not None else self.tensors[0].device if n else torch.device("cuda", torch.cuda.current_device())
+        dev = torch.device(device) if device is not None else self.tensors[0].device if n else torch.device("cuda")
+        if dev.type == "cuda" and dev.index is None:
+            dev = torch.device("cuda", torch.cuda.current_device())
         groups = [0] * n if groups is None else [int(g) for g in groups]
         self.n_groups = int(n_groups) if n_groups is not None else (max(groups) + 1 if n else 1)
         lengths = [0] * max(self.n_groups, 1)

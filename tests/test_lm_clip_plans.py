@@ -55,6 +55,18 @@ def test_a_plan_made_on_another_stream_takes_no_memory_still_in_use():
     assert abs(float(norms) - float(t.norm())) < 1e-3
 
 
+def test_the_device_may_be_named_without_its_number():
+    t = torch.ones(16, device=DEV)
+    norms = torch.empty(1, device=DEV)
+    for dev in ("cuda", "cuda:0", torch.device("cuda"), torch.device(DEV), None):
+        B.MvClip([t], device=dev).mv_clip_norm(norms)
+        assert float(norms) == 4.0
+        B.MvClip([], device=dev).mv_clip_norm(norms)
+        assert float(norms) == 0.0
+    with pytest.raises(B.MvError):
+        B.MvClip([t], device="cpu")
+
+
 @pytest.mark.parametrize("n", [100, 6_000_000])
 def test_tensors_that_share_bytes_are_not_scaled_in_place(n):
     """The same tensor twice, windows that overlap, in one group or two: norms and rows count every tensor, scaling is refused;

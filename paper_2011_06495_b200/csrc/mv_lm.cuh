@@ -34,14 +34,14 @@ __device__ __forceinline__ int64_t load_id(const void* ids, int id_type, int64_t
 }
 
 // Whether two strided matrices (rows of `cols` elements of `size` bytes, `ld` elements apart) share bytes: their spans meet, and
-// they are not two windows of columns side by side in rows of one pitch.
+// they are not two windows of columns side by side in rows of one pitch (a single row has the other's).
 inline bool share_bytes(const void* p, int64_t rows, int64_t cols, int64_t ld, int size, const void* q, int64_t rows2, int64_t cols2, int64_t ld2,
                         int size2) {
   if (rows < 1 || rows2 < 1) return false;
   const uintptr_t a = reinterpret_cast<uintptr_t>(p), b = reinterpret_cast<uintptr_t>(q);
   if (a >= b + size_t((rows2 - 1) * ld2 + cols2) * size2 || b >= a + size_t((rows - 1) * ld + cols) * size) return false;
-  const uintptr_t pitch = uintptr_t(ld) * size;
-  if (pitch != uintptr_t(ld2) * size2) return true;
+  const uintptr_t pitch = rows > 1 ? uintptr_t(ld) * size : uintptr_t(ld2) * size2;
+  if ((rows2 > 1 && pitch != uintptr_t(ld2) * size2) || (rows < 2 && rows2 < 2)) return true;
   const uintptr_t to = a <= b ? (b - a) % pitch : (pitch - (a - b) % pitch) % pitch;      // from a row of p on to the next row of q
   return to < uintptr_t(cols) * size || pitch - to < uintptr_t(cols2) * size2;
 }

@@ -351,12 +351,18 @@ struct mv_clip {
 
 namespace {
 
-// Whether the rows and one of the tensors share bytes.
+// Whether the rows (of the longest group's length each) and one of the tensors share bytes.
 bool overlaps(const mv_clip* p, const float* rows, int64_t ld) {
   const uintptr_t lo = reinterpret_cast<uintptr_t>(rows), hi = lo + (size_t(p->n_groups - 1) * ld + p->longest) * 4;
   if (hi <= p->lo || lo >= p->hi) return false;
-  for (int i = 0; i < p->n_spans; ++i)
-    if (p->spans[i].lo < hi && lo < p->spans[i].hi) return true;
+  const uintptr_t pitch = uintptr_t(ld) * 4, len = uintptr_t(p->longest) * 4;
+  for (int i = 0; i < p->n_spans; ++i) {
+    const uintptr_t a = p->spans[i].lo, b = p->spans[i].hi;
+    if (a >= hi || b <= lo) continue;
+    if (a <= lo) return true;
+    const uintptr_t row = lo + (a - lo) / pitch * pitch;      // the last one that begins at the tensor or before it
+    if (a < row + len || b > row + pitch) return true;        // (in a gap, so another row follows)
+  }
   return false;
 }
 

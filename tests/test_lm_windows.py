@@ -35,3 +35,26 @@ def test_one_row_beside_a_matrix(D, row, left):
         assert torch.equal(buf[rest][:, one], apart_r[rest][:, one])
         with pytest.raises(B.MvError):
             call(buf[:, many], buf[row:row + 1, inside])
+
+
+@pytest.mark.parametrize("d", [64, 1000, 200_003])
+@pytest.mark.parametrize("left", [True, False])
+def test_rows_beside_the_tensors_packed_into_them(d, left):
+    """Every worker's tensors behind (or before) its row in one buffer; one element more and the rows are refused."""
+    G, a = 5, 17
+    buf = torch.randn((G, 2 * d + 2), generator=torch.Generator(device=DEV).manual_seed(d), device=DEV)
+    old = buf.clone()
+    at, to = (0, d + 1) if left else (d + 1, 0)                       # the tensors' columns, the rows' columns
+    ts = [t for g in range(G) for t in (buf[g, at:at + a], buf[g, at + a:at + d])]
+    plan = B.MvClip(ts, [g for g in range(G) for _ in range(2)])
+    norms = torch.empty(G, device=DEV)
+    plan.mv_clip_pack(float("inf"), buf[:, to:to + d], norms)
+    want = old.clone()
+    want[:, to:to + d] = old[:, at:at + d]
+    assert torch.equal(buf, want)
+    assert bool(((norms.double() - old[:, at:at + d].double().norm(dim=1)).abs() <= 2.0 ** -22 * norms.double()).all())
+    for off in (to - 2, to - 1 if left else to + 2, at, at + 1):
+        if 0 <= off and off + d <= 2 * d + 2 and (off + d > at and off < at + d):
+            with pytest.raises(B.MvError):
+                plan.mv_clip_pack(1.0, buf[:, off:off + d], norms)
+    assert torch.equal(buf, want)

@@ -11,7 +11,7 @@ namespace {
 // The list is cut into chunks of 32 KB, one CTA each.  A group's factor is known only when all its chunks have been summed.
 // A short list, whose chunks all fit the shared memory of half the device, is read once: one kernel whose CTAs sum their
 // chunk, keep it until the factor is there, and scale it.  A long one is read twice, by a kernel that sums and one that scales.
-// Memory bounds both: ten groups of 11,173,962 fp32 are summed in 71 us (6.3 TB/s) and scaled into rows in 136 us (6.6 TB/s).
+// Memory bounds both: ten groups of 11,173,962 fp32 are summed in 71 us (6.3 TB/s) and scaled into rows in 136 us (6.6 TB/s), or in place in 138.
 // (Working a long list off group by group, so that the second reading finds its data in L2, gains nothing: L2 delivers hardly
 // more than memory does, 8 to 9 TB/s against 7, and the stages' ends cost more: 232 to 274 us for the whole in four forms of it.)
 constexpr int TPB = 256;

@@ -424,8 +424,9 @@ __device__ __noinline__ Sums sums_of_extremes(const Part<X>& p, float c2, float 
 // lane on their way.  Per 16 bytes of bf16 a lane spends about 40 instructions, eight of them exponentials, which the
 // multiprocessor does at 16 a cycle against the 11.4 logits a cycle that memory brings: so issue, the exponentials and memory
 // are all within a factor of two of one another, and under the power limit (1.68 GHz in a long run) the instructions count.
-// 8192 x 65536 bf16: 176 us without alternatives (6.1 TB/s), 196 us with 16 of them (213 us at the limit); the
+// 8192 x 65536 bf16: 176 us without alternatives (6.1 TB/s), 191 us with 16 of them (207 us at the limit); the
 // alternatives' cost is the end of a row, about 2 us of latency that the other CTAs of the multiprocessor only partly cover.
+// Rows that are summed again by differences cost a second, plainer reading: 450 us without alternatives, 485 us with them.
 template <typename X, bool TOP, int TPB>
 __global__ void __launch_bounds__(TPB, 1024 / TPB) k_token_logprob(const X* __restrict__ logits, const __grid_constant__ LogprobArgs a) {
   constexpr int N = Vec<X>::N, WARPS = TPB / 32;
@@ -622,8 +623,9 @@ __global__ void __launch_bounds__(TPB, 1024 / TPB) k_token_logprob(const X* __re
 // differ by their own roundings, which for an lse of 1e9 are tens; and since the lse itself is rounded by as much there, log p is kept
 // from being positive (4096 x 131072 bf16: 358 us, without that 355.5; asking it only of rows with a large lse: 358).  p is formed
 // as q q because the hardware's exponential has no subnormal results; that doubles its error to 2^-21, beside the 2^-11 (f16) or
-// 2^-8 (bf16) of the result's rounding.  Each CTA takes one stretch of one row, so that the stretches, in the order of memory, go to the multiprocessors as they become free: memory
-// bounds it (4096 x 131072 bf16: 6.0 TB/s in and out).
+// 2^-8 (bf16) of the result's rounding.  Each CTA takes one stretch of one row, so that the stretches, in the order of memory, go
+// to the multiprocessors as they become free: memory bounds it (6.0 TB/s in and out; 365 us with the power limit reached, in a
+// long run).  Where logits and gradient lie differently within 16 bytes, single elements are read and written: 1041 us.
 constexpr int GRAD_TPB = 256, GRAD_U = 4;
 constexpr float H_FLOOR = -256.0f;     // q is 0 from -127 on; so near that A h is finite for any gradient below 1e36
 
@@ -751,7 +753,7 @@ int mv_token_logprob(void* stream, const void* logits, int type, int64_t T, int6
     const int64_t vecs = V / Vec<X>::N;
     // A CTA per row.  Its end (choosing the alternatives) is a chain of short phases, so short rows take few threads and many
     // CTAs, if there are rows enough to fill the device: 16000 rows of 16 KB, k = 8: 62 us with 32 threads, 73 with 64, 102 with 128;
-    // 9079 rows of 33 KB: 77, 70, 84.  Rows in the hundreds take more threads than that (1003 of 16 KB: 10.4, 9.5, 9.6), long ones
+    // 9079 rows of 33 KB: 77, 70, 84; with 64 and 128, 8000 of 48 KB: 79 and 84, of 64 KB: 103 and 103 to 105.  Rows in the hundreds take more threads than that (1003 of 16 KB: 10.4, 9.5, 9.6), long ones
     // more still (3000 of 131 KB: 81 us with 128, 86 with 256; of 200 KB: 136 and 123; 100 of 200 KB: 14.4 and 11.3).
     // Long rows that are so few that four CTAs each fit the device: a cluster of four per row, a step or more for each thread (one
     // row of 200 KB: 8.8 us, with one CTA 10.3; 32 of 262 KB: 9.5 and 14.0).

@@ -27,7 +27,7 @@ def test_a_plan_dropped_while_its_call_waits_keeps_its_memory(n, created_on_it):
     torch.cuda.synchronize()
     mine, list_bytes, at = plan.workspace.data_ptr(), plan.workspace.numel(), t.data_ptr()
     with torch.cuda.stream(st):
-        torch.cuda._sleep(400_000_000)                     # 0.2 s
+        torch.cuda._sleep(1_000_000_000)                   # half a second
     plan.mv_clip_pack(1e30, rows, norms, stream=st)
     del plan, t
     there = addresses(list_bytes) | addresses(4 * n, 4)
@@ -43,7 +43,7 @@ def test_a_plan_made_on_another_stream_takes_no_memory_still_in_use():
     st = torch.cuda.Stream()
     sizes = int(B.load().mv_clip_workspace_bytes((B.ctypes.c_int64 * 1)(5000), 1, 1))
     torch.cuda.synchronize()
-    torch.cuda._sleep(200_000_000)
+    torch.cuda._sleep(1_000_000_000)
     freed = addresses(sizes)                               # freed at once; the current stream is still asleep
     plan = B.MvClip([t], stream=st)
     assert not torch.cuda.current_stream().query()

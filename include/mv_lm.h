@@ -80,8 +80,9 @@ int mv_token_logprob(void* stream, const void* logits, int type, int64_t T, int6
  *   lse, entropy [T] float in, as mv_token_logprob left them (entropy only with g_entropy)
  *   g_logprob [T] float in (NULL: zero; then targets may be NULL);  g_entropy [T] float in (NULL: zero)
  *   dlogits [T, V] out, of the logits' type, rows ldg >= V apart; may be the logits themselves (then ldg = ld)
- * (Logits beyond the range of 32 bits once scaled, lse +inf: p = 0.)  A position without a target has no logprob term.  Where neither term is left (no target or g_logprob 0, and
- * g_entropy 0) the row is +0 whatever its logits hold; so is a row whose lse is -inf. */
+ * A position without a target has no logprob term.  Where neither term is left (no target or g_logprob 0, and
+ * g_entropy 0) the row is +0 whatever its logits hold; so is a row whose lse is -inf.  In a row of finite logits whose
+ * lse is +inf (beyond the range of 32 bits once scaled) every p is 0. */
 int mv_token_logprob_grad(void* stream, const void* logits, int type, int64_t T, int64_t V, int64_t ld, const void* targets,
                           int id_type, float scale, const float* lse, const float* entropy, const float* g_logprob,
                           const float* g_entropy, void* dlogits, int64_t ldg);

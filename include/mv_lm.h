@@ -4,8 +4,11 @@
  * a worker's gradient before error feedback.
  *
  *   embedding    out_t = s W[id_t]                  and its gradient  dW_v = s sum_{t: id_t = v} dout_t
+ *   layer norm   y = (x - mean) / sqrt(variance + eps) w + b row by row, and its gradients
  *   token loss   z = c x, lse = log sum_v exp z_v, log p = z - lse:  log p of given tokens, the entropy
  *                H = -sum_v p_v log p_v, the k largest log p, and the gradient with respect to x
+ *   distillation the divergence of softmax(c x) from a teacher that is known by its largest log probabilities, and its gradient
+ *   sampling     one token per row from softmax(c x), cut to the top k, the top p and the min p, by given random numbers
  *   clipping     n_g = sqrt(sum of squares over the tensors of group g), every tensor of the group times
  *                min(1, max_norm / n_g): in place, or laid end to end as the fp32 rows that
  *                mv_sparse_step takes (one group per worker)
@@ -35,7 +38,8 @@ extern "C" {
 
 enum { MV_F32 = 0, MV_BF16 = 1, MV_F16 = 2, MV_I32 = 3, MV_I64 = 4 };
 
-#define MV_TOP_MAX 64 /* most alternatives per position */
+#define MV_TOP_MAX 64        /* most alternatives per position that mv_token_logprob finds */
+#define MV_TEACHER_MAX 1024  /* most alternatives per position that mv_distill takes */
 
 /* Embedding lookup.  out[t, :] = scale * weight[ids[t], :], the product rounded once to 32 bits and once to
  * out's type.  A token id outside [0, V) gives a row of zeros.  weight and out share no bytes.
@@ -58,6 +62,30 @@ size_t mv_embed_grad_workspace_bytes(int64_t T, int64_t V, int64_t D);
 int mv_embed_grad(void* stream, const void* dout, int dout_type, int64_t ldd, const void* ids, int id_type, int64_t T, int64_t V,
                   int64_t D, float scale, int64_t pad_id, int accumulate, float* dweight, int64_t ldw, void* workspace,
                   size_t workspace_bytes);
+
+/* Layer norm of rows.  mu = mean of x[t, :], v = mean of (x - mu)^2, r = 1 / sqrt(v + eps), y[t, i] = (x[t, i] - mu) r w[i] + b[i],
+ * in 32 bits (sums of D terms, the squares' after the mean is known), rounded once to y's type.
+ *   x [T, D] type in, rows ldx >= D apart;  y [T, D] out, of the same type, rows ldy >= D apart; may be x itself (then ldy = ldx)
+ *   weight, bias [D] w_type in: MV_F32 or x's type; each may be NULL (1 and 0)
+ *   mean, rstd [T] float out (mu and r), what the gradient needs; each may be NULL
+ * eps >= 0, finite.  A row that holds an inf or a NaN, or whose sums pass the range of 32 bits, has no other meaning than the
+ * formula's in 32 bits.  Limits: 0 <= T < 2^31, 1 <= D < 2^31. */
+int mv_layer_norm(void* stream, const void* x, int type, int64_t T, int64_t D, int64_t ldx, const void* weight, const void* bias, int w_type,
+                  float eps, void* y, int64_t ldy, float* mean, float* rstd);
+
+/* Bytes of scratch mv_layer_norm_grad needs (host arithmetic only); 0 if out of range. */
+size_t mv_layer_norm_grad_workspace_bytes(int64_t T, int64_t D);
+
+/* Its gradients, given dy.  With n = (x - mu) r and h = dy w:
+ *   dx[t, i] = r (h_i - mean(h) - n_i mean(h n)),  dweight[i] = sum_t dy[t, i] n[t, i],  dbias[i] = sum_t dy[t, i]
+ *   dy, x [T, D] type in, rows lddy and ldx apart;  weight as in mv_layer_norm;  mean, rstd [T] float in, as mv_layer_norm left them
+ *   dx [T, D] out, of the same type, rows lddx apart; may be dy or x itself (of the same pitch); NULL: not wanted
+ *   dweight, dbias [D] float out, each may be NULL.  accumulate = 0: overwritten (T = 0: zeros); accumulate = 1: added to
+ *   workspace  mv_layer_norm_grad_workspace_bytes(T, D) bytes, 16-byte aligned (unused, and may be NULL, without dweight and dbias)
+ * The sums over rows are in 32 bits, in an order that T, D and the device's number of multiprocessors fix. */
+int mv_layer_norm_grad(void* stream, const void* dy, int64_t lddy, const void* x, int64_t ldx, int type, int64_t T, int64_t D,
+                       const void* weight, int w_type, const float* mean, const float* rstd, void* dx, int64_t lddx, float* dweight,
+                       float* dbias, int accumulate, void* workspace, size_t workspace_bytes);
 
 /* Log probabilities of given tokens under softmax(scale * logits), row by row, with entropy and alternatives.
  *   logits  [T, V] type in, rows ld >= V apart;  scale > 0 (an inverse temperature)
@@ -86,6 +114,45 @@ int mv_token_logprob(void* stream, const void* logits, int type, int64_t T, int6
 int mv_token_logprob_grad(void* stream, const void* logits, int type, int64_t T, int64_t V, int64_t ld, const void* targets,
                           int id_type, float scale, const float* lse, const float* entropy, const float* g_logprob,
                           const float* g_entropy, void* dlogits, int64_t ldg);
+
+/* Divergence of the student p = softmax(scale * logits) from a teacher that is known by k alternatives per row, a_j = top_logprob[t, j]
+ * of token top_id[t, j] (what mv_token_logprob leaves for the teacher's logits, at the same scale).
+ *   rest = 0: the alternatives stand for the whole teacher, q = softmax(a) over them:  kl = sum_j q_j (log q_j - log p_j)
+ *   rest = 1: q_j = exp(a_j) are the teacher's probabilities; what is missing to one, r = max(0, 1 - sum_j q_j), is one more class, beside
+ *             the student's mass outside the list P = 1 - sum of p over the listed tokens:  kl = ... + r (log r - log P)
+ *   logits [T, V] type in, rows ld >= V apart;  top_logprob, top_id [T, k] float / id_type in, contiguous, 1 <= k <= MV_TEACHER_MAX
+ *   kl, lse, log_rest [T] float out, each may be NULL: the divergence, log sum exp of the scaled logits, and log P (rest = 1 only)
+ * An id outside [0, V) is no alternative.  A row without one has no teacher: kl 0 (log_rest 0, or NaN as below).  The same id twice is two terms of the sums,
+ * but one token.  q_j = 0 adds nothing; q_j > 0 where p_j = 0 (a masked logit, a row that is all -inf) makes kl +inf.  P is summed
+ * without the listed tokens, not taken as a difference.  A row of logits with a NaN or +inf has NaN in all three; a NaN or +inf among a row's a_j makes kl NaN.
+ * Limits as mv_token_logprob. */
+int mv_distill(void* stream, const void* logits, int type, int64_t T, int64_t V, int64_t ld, const float* top_logprob, const void* top_id,
+               int id_type, int k, int rest, float scale, float* kl, float* lse, float* log_rest);
+
+/* Gradient of sum_t g[t] kl[t] with respect to the logits, M = sum_j q_j + r (1 without rest):
+ *   dlogits[t, v] = scale g[t] (M p_v - sum_{j: id_j = v} q_j) for a listed token v,  scale g[t] p_v (M - r / P) for the others
+ * with log p_v = min(0, scale logits[t, v] - lse[t]).
+ *   lse, log_rest [T] float in, as mv_distill left them (log_rest NULL: rest = 0);  g [T] float in
+ *   dlogits [T, V] out, of the logits' type, rows ldg >= V apart; may be the logits themselves (then ldg = ld)
+ * A row without a teacher, with g[t] = 0 or with lse = -inf is +0 whatever its logits hold; where log_rest is -inf, the others are 0. */
+int mv_distill_grad(void* stream, const void* logits, int type, int64_t T, int64_t V, int64_t ld, const float* top_logprob,
+                    const void* top_id, int id_type, int k, float scale, const float* lse, const float* log_rest, const float* g,
+                    void* dlogits, int64_t ldg);
+
+/* Draws a token per row.  w_v = exp(scale (x_v - max x)); the tokens in descending order of x, equal ones (+0 and -0 are equal) by
+ * ascending index, are cut to the first top_k, those to the shortest start whose sum is at least top_p times theirs, those to w_v >=
+ * min_p; the first always stays.  token[t] is the first index at which the sum of the kept w, in ascending order of the index, exceeds u[t] times their
+ * sum, and logprob[t] the log of its share of that sum.  Weights are formed in 64 bits and added as whole multiples of n / 2^61 of the largest,
+ * n the smallest power of two that is not below V: a token with less than half of that (3e-14 for V = 10^5) is never drawn.
+ *   logits [T, V] type in, rows ld >= V apart;  u [T] float in, in [0, 1) (below: 0; from 1 on: the last kept token that has a weight)
+ *   scale, top_p, min_p [T] float in, top_k [T] int32 in, on the device, each may be NULL: 1, 1 (all), 0 (all), 0 (all).
+ *           scale > 0, an inverse temperature; top_k <= 0 or >= V, top_p >= 1, min_p <= 0: nothing is cut
+ *   token [T] id_type out;  logprob [T] float out, may be NULL
+ * -inf marks a masked logit, which is never drawn.  A row with nothing else has token -1 and logprob -inf.  A row with a NaN or
+ * +inf, with a NaN among its settings, or whose scale is not positive and finite, has token -1 and logprob NaN.
+ * Limits as mv_token_logprob. */
+int mv_sample(void* stream, const void* logits, int type, int64_t T, int64_t V, int64_t ld, const float* u, const float* scale,
+              const int32_t* top_k, const float* top_p, const float* min_p, void* token, int id_type, float* logprob);
 
 /* Norms and clipping over a fixed list of tensors.  The plan holds the list (the tensors' addresses, types and
  * sizes), not their values; it stays valid as long as the tensors stay where they are. */

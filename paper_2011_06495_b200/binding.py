@@ -29,6 +29,7 @@ MV_MODE_GENERAL = 1
 MV_MODE_TRACK = 2
 MV_F32, MV_BF16, MV_F16, MV_I32, MV_I64 = 0, 1, 2, 3, 4
 MV_TOP_MAX = 64
+MV_TEACHER_MAX = 1024
 MV_DBG_CAND_OVERFLOW, MV_DBG_WINDOW_OVERFLOW, MV_DBG_FALLBACK, MV_DBG_LIST_OVERFLOW = 1, 2, 4, 8
 MV_DBG_PICK_RANGE, MV_DBG_LIST_RANGE, MV_DBG_OUT_RANGE, MV_DBG_GATHER_RANGE, MV_DBG_INTERNAL = 16, 32, 64, 128, 256
 
@@ -142,6 +143,18 @@ def _open(path: str, how: str) -> ctypes.CDLL:
     lib.mv_token_logprob.argtypes = [c_vp, c_vp, c_i, c_i64, c_i64, c_i64, c_vp, c_i, c_f, c_i, c_vp, c_vp, c_vp, c_vp, c_vp]
     lib.mv_token_logprob_grad.restype = c_i
     lib.mv_token_logprob_grad.argtypes = [c_vp, c_vp, c_i, c_i64, c_i64, c_i64, c_vp, c_i, c_f, c_vp, c_vp, c_vp, c_vp, c_vp, c_i64]
+    lib.mv_layer_norm.restype = c_i
+    lib.mv_layer_norm.argtypes = [c_vp, c_vp, c_i, c_i64, c_i64, c_i64, c_vp, c_vp, c_i, c_f, c_vp, c_i64, c_vp, c_vp]
+    lib.mv_layer_norm_grad_workspace_bytes.restype = c_sz
+    lib.mv_layer_norm_grad_workspace_bytes.argtypes = [c_i64, c_i64]
+    lib.mv_layer_norm_grad.restype = c_i
+    lib.mv_layer_norm_grad.argtypes = [c_vp, c_vp, c_i64, c_vp, c_i64, c_i, c_i64, c_i64, c_vp, c_i, c_vp, c_vp, c_vp, c_i64, c_vp, c_vp, c_i, c_vp, c_sz]
+    lib.mv_distill.restype = c_i
+    lib.mv_distill.argtypes = [c_vp, c_vp, c_i, c_i64, c_i64, c_i64, c_vp, c_vp, c_i, c_i, c_i, c_f, c_vp, c_vp, c_vp]
+    lib.mv_distill_grad.restype = c_i
+    lib.mv_distill_grad.argtypes = [c_vp, c_vp, c_i, c_i64, c_i64, c_i64, c_vp, c_vp, c_i, c_i, c_f, c_vp, c_vp, c_vp, c_vp, c_i64]
+    lib.mv_sample.restype = c_i
+    lib.mv_sample.argtypes = [c_vp, c_vp, c_i, c_i64, c_i64, c_i64, c_vp, c_vp, c_vp, c_vp, c_vp, c_vp, c_i, c_vp]
     lib.mv_clip_workspace_bytes.restype = c_sz
     lib.mv_clip_workspace_bytes.argtypes = [c_vp, c_i, c_i]
     lib.mv_clip_create.restype = c_i
@@ -241,7 +254,7 @@ def mv_dequantize(words, K: int, q: int, out, stream: Optional[torch.cuda.Stream
 
 
 _TYPES = {torch.float32: MV_F32, torch.bfloat16: MV_BF16, torch.float16: MV_F16, torch.int32: MV_I32, torch.int64: MV_I64}
-_VALUES, _IDS, _FLOAT = (MV_F32, MV_BF16, MV_F16), (MV_I32, MV_I64), (MV_F32,)
+_VALUES, _IDS, _FLOAT, _INT32 = (MV_F32, MV_BF16, MV_F16), (MV_I32, MV_I64), (MV_F32,), (MV_I32,)
 _raw_current_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)     # absent from a torch without CUDA
 
 
@@ -298,6 +311,53 @@ def mv_embed_grad(dout, ids, dweight, workspace, scale: float = 1.0, pad_id: int
                                 workspace.data_ptr(), workspace.numel() * workspace.element_size()), "mv_embed_grad")
 
 
+def mv_layer_norm(x, weight, bias, y, eps: float = 1e-5, mean=None, rstd=None, stream: Optional[torch.cuda.Stream] = None):
+    """y = (x - mean) / sqrt(variance + eps) * weight + bias row by row; x, y [T, D] of one type (y may be x), weight, bias [D]
+    float or of x's type, both of one type, each may be None; mean, rstd: float [T] or None."""
+    where = "mv_layer_norm"
+    p, x_type, T, D, ldx, dev = _matrix(x, _VALUES, where)
+    o, y_type, Ty, Dy, ldy, dev_y = _matrix(y, _VALUES, where)
+    w, b, w_type = _parameters(weight, bias, D, x_type, dev, where)
+    m, r = _vector(mean, T, _FLOAT, dev, where)[0], _vector(rstd, T, _FLOAT, dev, where)[0]
+    _need(y_type == x_type and Ty == T and Dy == D and dev_y == dev, where)
+    _check(load().mv_layer_norm(_raw_stream(dev, stream), p, x_type, T, D, ldx, w, b, w_type, float(eps), o, ldy, m, r), where)
+
+
+def _parameters(weight, bias, D: int, x_type: int, dev: int, where: str):
+    """(address, address, type code) of two vectors of D parameters of one type, each of which may be None."""
+    kinds = (MV_F32, x_type)
+    w, w_type = _vector(weight, D, kinds, dev, where)
+    b, b_type = _vector(bias, D, kinds, dev, where)
+    _need(w is None or b is None or w_type == b_type, where)
+    return w, b, w_type if w is not None else b_type
+
+
+def layer_norm_grad_workspace_bytes(T: int, D: int) -> int:
+    return int(load().mv_layer_norm_grad_workspace_bytes(int(T), int(D)))
+
+
+def mv_layer_norm_grad(dy, x, weight, mean, rstd, dx, dweight, dbias, workspace, accumulate: bool = False,
+                       stream: Optional[torch.cuda.Stream] = None):
+    """dx [T, D], dweight and dbias (float [D]) of mv_layer_norm for dy [T, D]; dx may be dy or x; dx, dweight, dbias and, without the
+    latter two, workspace may be None."""
+    where = "mv_layer_norm_grad"
+    p, x_type, T, D, ldx, dev = _matrix(x, _VALUES, where)
+    q, dy_type, Ty, Dy, lddy, dev_y = _matrix(dy, _VALUES, where)
+    _need(dy_type == x_type and Ty == T and Dy == D and dev_y == dev, where)
+    w, _, w_type = _parameters(weight, None, D, x_type, dev, where)
+    m, r = _vector(mean, T, _FLOAT, dev, where)[0], _vector(rstd, T, _FLOAT, dev, where)[0]
+    o, lddx = None, D
+    if dx is not None:
+        o, dx_type, To, Do, lddx, dev_o = _matrix(dx, _VALUES, where)
+        _need(dx_type == x_type and To == T and Do == D and dev_o == dev, where)
+    dw, db = _vector(dweight, D, _FLOAT, dev, where)[0], _vector(dbias, D, _FLOAT, dev, where)[0]
+    ws, n = None, 0
+    if workspace is not None:
+        _need(workspace.get_device() == dev and workspace.is_contiguous(), where)
+        ws, n = workspace.data_ptr(), workspace.numel() * workspace.element_size()
+    _check(load().mv_layer_norm_grad(_raw_stream(dev, stream), q, lddy, p, ldx, x_type, T, D, w, w_type, m, r, o, lddx, dw, db, bool(accumulate), ws, n), where)
+
+
 def mv_token_logprob(logits, targets=None, scale: float = 1.0, logprob=None, entropy=None, lse=None, top_logprob=None, top_id=None,
                      stream: Optional[torch.cuda.Stream] = None):
     """Log probabilities of targets [T] under softmax(scale * logits), logits [T, V]; logprob, entropy, lse: float [T];
@@ -327,6 +387,49 @@ def mv_token_logprob_grad(logits, targets, lse, g_logprob, dlogits, scale: float
     g1, g2 = _vector(g_logprob, T, _FLOAT, dev, where)[0], _vector(g_entropy, T, _FLOAT, dev, where)[0]
     _need(d_type == x_type and Td == T and Vd == V and dev_d == dev, where)
     _check(load().mv_token_logprob_grad(_raw_stream(dev, stream), x, x_type, T, V, ld, y, i_type, float(scale), l, h, g1, g2, d, ldg), where)
+
+
+def _list(top_logprob, top_id, T: int, dev: int, where: str):
+    """(address, address, type code of the ids, k) of a teacher's alternatives: float [T, k] and ids [T, k], contiguous."""
+    code = _TYPES.get(top_id.dtype, -1)
+    _need(top_logprob.dim() == 2 and top_logprob.shape == top_id.shape and top_logprob.shape[0] == T and top_logprob.dtype == torch.float32 and code in _IDS and
+          top_logprob.get_device() == dev and top_id.get_device() == dev and top_logprob.is_contiguous() and top_id.is_contiguous(), where)
+    return top_logprob.data_ptr(), top_id.data_ptr(), code, top_logprob.shape[1]
+
+
+def mv_distill(logits, top_logprob, top_id, scale: float = 1.0, kl=None, lse=None, log_rest=None, rest: Optional[bool] = None,
+               stream: Optional[torch.cuda.Stream] = None):
+    """Divergence of softmax(scale * logits), logits [T, V], from a teacher's alternatives top_logprob, top_id [T, k]; kl, lse, log_rest:
+    float [T] or None.  rest: the teacher's remaining mass is one more class (None: if log_rest is asked for)."""
+    where = "mv_distill"
+    x, x_type, T, V, ld, dev = _matrix(logits, _VALUES, where)
+    a, i, i_type, k = _list(top_logprob, top_id, T, dev, where)
+    o = [_vector(t, T, _FLOAT, dev, where)[0] for t in (kl, lse, log_rest)]
+    rest = log_rest is not None if rest is None else bool(rest)
+    _check(load().mv_distill(_raw_stream(dev, stream), x, x_type, T, V, ld, a, i, i_type, k, rest, float(scale), *o), where)
+
+
+def mv_distill_grad(logits, top_logprob, top_id, lse, g, dlogits, scale: float = 1.0, log_rest=None,
+                    stream: Optional[torch.cuda.Stream] = None):
+    """dlogits [T, V] of sum(g * kl), with the rest as a class if log_rest is given; dlogits may be logits."""
+    where = "mv_distill_grad"
+    x, x_type, T, V, ld, dev = _matrix(logits, _VALUES, where)
+    d, d_type, Td, Vd, ldg, dev_d = _matrix(dlogits, _VALUES, where)
+    a, i, i_type, k = _list(top_logprob, top_id, T, dev, where)
+    l, r, w = (_vector(t, T, _FLOAT, dev, where)[0] for t in (lse, log_rest, g))
+    _need(d_type == x_type and Td == T and Vd == V and dev_d == dev, where)
+    _check(load().mv_distill_grad(_raw_stream(dev, stream), x, x_type, T, V, ld, a, i, i_type, k, float(scale), l, r, w, d, ldg), where)
+
+
+def mv_sample(logits, u, token, scale=None, top_k=None, top_p=None, min_p=None, logprob=None, stream: Optional[torch.cuda.Stream] = None):
+    """A token per row of logits [T, V] by u [T] in [0, 1), from softmax(scale * logits) cut to top_k, top_p and min_p (each [T] or
+    None: float, top_k int32); token: int32 or int64 [T]; logprob: float [T] or None."""
+    where = "mv_sample"
+    x, x_type, T, V, ld, dev = _matrix(logits, _VALUES, where)
+    r, c, p, m, l = (_vector(t, T, _FLOAT, dev, where)[0] for t in (u, scale, top_p, min_p, logprob))
+    k = _vector(top_k, T, _INT32, dev, where)[0]
+    o, o_type = _vector(token, T, _IDS, dev, where)
+    _check(load().mv_sample(_raw_stream(dev, stream), x, x_type, T, V, ld, r, c, k, p, m, o, o_type, l), where)
 
 
 class MvClip:

@@ -1,0 +1,93 @@
+"""CPU checks of layer norm, distillation and sampling (include/mv_lm.h): the refusals that happen before anything is enqueued."""
+import ctypes
+import math
+
+import pytest
+
+from paper_2011_06495_b200 import binding as B
+from paper_2011_06495_b200 import build as BUILD
+
+
+@pytest.fixture(scope="module")
+def lib():
+    BUILD.build()
+    return B.load()
+
+
+at = ctypes.c_void_p
+P, Q, R, S, ODD = at(0x100000), at(0x200000), at(0x300000), at(0x400000), at(0x100001)      # never dereferenced
+BAD = B.MV_ERR_INVALID_ARG
+
+
+def test_layer_norm_refusals(lib):
+    ok = dict(x=P, xt=B.MV_BF16, T=4, D=8, ldx=8, w=Q, b=Q, wt=B.MV_F32, eps=1e-5, y=R, ldy=8, m=None, r=None)
+
+    def call(**k):
+        a = {**ok, **k}
+        return lib.mv_layer_norm(None, a["x"], a["xt"], a["T"], a["D"], a["ldx"], a["w"], a["b"], a["wt"], a["eps"], a["y"], a["ldy"], a["m"], a["r"])
+
+    for k in (dict(x=None), dict(xt=B.MV_I32), dict(T=-1), dict(T=1 << 31), dict(D=0), dict(D=1 << 31), dict(ldx=7), dict(wt=B.MV_F16), dict(wt=B.MV_I64), dict(eps=-1e-9),
+              dict(eps=math.nan), dict(eps=math.inf), dict(y=None), dict(ldy=7), dict(x=ODD), dict(y=ODD), dict(w=at(0x200002)), dict(b=ODD), dict(m=at(0x400002)), dict(r=ODD),
+              dict(y=at(0x100002)), dict(y=at(0x100000 - 2)), dict(y=P, ldy=9), dict(y=Q), dict(w=at(0x300020))):
+        assert call(**k) == BAD, k
+    assert call(T=0) == B.MV_OK and call(T=0, x=None, y=None) == B.MV_OK
+
+
+def test_layer_norm_grad_refusals_and_workspace(lib):
+    need = B.layer_norm_grad_workspace_bytes(100, 8)
+    assert need >= 64 and need % 16 == 0
+    assert all(B.layer_norm_grad_workspace_bytes(*a) == 0 for a in ((-1, 8), (1 << 31, 8), (4, 0), (4, 1 << 31)))
+    assert B.layer_norm_grad_workspace_bytes(0, 8) > 0
+    ok = dict(dy=P, lddy=8, x=Q, ldx=8, xt=B.MV_F32, T=100, D=8, w=R, wt=B.MV_F32, m=R, r=R, dx=S, lddx=8, dw=at(0x500000), db=at(0x500020), acc=0, ws=R, n=need)
+
+    def call(**k):
+        a = {**ok, **k}
+        return lib.mv_layer_norm_grad(None, a["dy"], a["lddy"], a["x"], a["ldx"], a["xt"], a["T"], a["D"], a["w"], a["wt"], a["m"], a["r"], a["dx"], a["lddx"], a["dw"], a["db"],
+                                      a["acc"], a["ws"], a["n"])
+
+    for k in (dict(dy=None), dict(x=None), dict(lddy=7), dict(ldx=7), dict(lddx=7), dict(xt=9), dict(T=-1), dict(D=0), dict(wt=B.MV_BF16), dict(m=None), dict(r=None), dict(m=ODD),
+              dict(dx=None, dw=None, db=None), dict(acc=2), dict(ws=at(0x300008)), dict(dw=ODD), dict(db=at(0x500022)), dict(dx=ODD), dict(dx=at(0x100020)), dict(dx=P, lddx=9),
+              dict(dx=at(0x200004)), dict(dw=P), dict(dw=Q), dict(dw=S), dict(db=at(0x300010)), dict(db=at(0x500010)), dict(w=at(0x400000))):
+        assert call(**k) == BAD, k
+    assert call(ws=None) == B.MV_ERR_WORKSPACE and call(n=need - 1) == B.MV_ERR_WORKSPACE
+
+
+def test_distill_refusals(lib):
+    ok = dict(x=P, xt=B.MV_BF16, T=4, V=30, ld=30, a=Q, i=R, it=B.MV_I64, k=3, rest=1, c=1.0, kl=S, lse=None, lr=None)
+
+    def call(**k):
+        a = {**ok, **k}
+        return lib.mv_distill(None, a["x"], a["xt"], a["T"], a["V"], a["ld"], a["a"], a["i"], a["it"], a["k"], a["rest"], a["c"], a["kl"], a["lse"], a["lr"])
+
+    for k in (dict(x=None), dict(xt=B.MV_I32), dict(T=-1), dict(T=1 << 31), dict(V=0), dict(V=1 << 31), dict(ld=29), dict(a=None), dict(i=None), dict(it=B.MV_F32), dict(k=0),
+              dict(k=B.MV_TEACHER_MAX + 1), dict(rest=2), dict(rest=0, lr=S), dict(c=0.0), dict(c=-1.0), dict(c=math.nan), dict(c=math.inf), dict(x=ODD), dict(a=at(0x200002)),
+              dict(i=at(0x300004)), dict(kl=ODD), dict(lse=ODD), dict(lr=ODD)):
+        assert call(**k) == BAD, k
+    assert call(T=0) == B.MV_OK and call(T=0, x=None, a=None, i=None) == B.MV_OK
+
+
+def test_distill_grad_refusals(lib):
+    ok = dict(x=P, xt=B.MV_F32, T=4, V=30, ld=30, a=Q, i=R, it=B.MV_I32, k=3, c=1.0, lse=S, lr=None, g=S, dx=at(0x500000), ldg=30)
+
+    def call(**k):
+        a = {**ok, **k}
+        return lib.mv_distill_grad(None, a["x"], a["xt"], a["T"], a["V"], a["ld"], a["a"], a["i"], a["it"], a["k"], a["c"], a["lse"], a["lr"], a["g"], a["dx"], a["ldg"])
+
+    for k in (dict(x=None), dict(xt=7), dict(T=-1), dict(V=0), dict(ld=29), dict(ldg=29), dict(a=None), dict(i=None), dict(it=B.MV_F16), dict(k=0), dict(k=1025), dict(c=0.0), dict(c=math.nan),
+              dict(lse=None), dict(g=None), dict(dx=None), dict(x=ODD), dict(dx=ODD), dict(lse=ODD), dict(lr=ODD), dict(g=ODD), dict(dx=at(0x100004)), dict(dx=P, ldg=31), dict(dx=Q),
+              dict(dx=at(0x300000 - 4))):
+        assert call(**k) == BAD, k
+    assert call(T=0) == B.MV_OK
+
+
+def test_sample_refusals(lib):
+    ok = dict(x=P, xt=B.MV_F16, T=4, V=30, ld=30, u=Q, c=None, k=None, p=None, m=None, y=R, it=B.MV_I64, lp=None)
+
+    def call(**k):
+        a = {**ok, **k}
+        return lib.mv_sample(None, a["x"], a["xt"], a["T"], a["V"], a["ld"], a["u"], a["c"], a["k"], a["p"], a["m"], a["y"], a["it"], a["lp"])
+
+    for k in (dict(x=None), dict(xt=B.MV_I64), dict(T=-1), dict(T=1 << 31), dict(V=0), dict(V=1 << 31), dict(ld=29), dict(u=None), dict(y=None), dict(it=B.MV_BF16), dict(x=ODD), dict(u=ODD),
+              dict(c=ODD), dict(k=ODD), dict(p=ODD), dict(m=ODD), dict(y=at(0x300004)), dict(lp=ODD)):
+        assert call(**k) == BAD, k
+    assert call(T=0) == B.MV_OK

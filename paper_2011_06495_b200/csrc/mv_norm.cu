@@ -4,28 +4,73 @@
 
 namespace {
 
-// A row is read once, into registers, by L lanes (L = 32: of one warp or of all warps of a CTA), each with NV units: vectors of 16 bytes where rows
-// lie on their boundaries, single elements elsewhere.
+// A row is read once, into registers, by L lanes (of a part of a warp, or of several), each with up to NV units: vectors of 16 bytes where
+// rows lie on their boundaries, single elements elsewhere.  Arithmetic is on two elements at a time.
 template <typename X, bool VEC> struct Unit;
 template <typename X> struct Unit<X, true> {
   static constexpr int N = Vec<X>::N;
   uint4 u;
-  __device__ __forceinline__ void load(const X* row, int i) { u = __ldcs(reinterpret_cast<const uint4*>(row) + i); }
-  __device__ __forceinline__ void clear() { u = make_uint4(0, 0, 0, 0); }
-  __device__ __forceinline__ void get(float (&f)[N]) const {
-#pragma unroll
-    for (int j = 0; j < N / 2; ++j) unpack2(Vec<X>::pair(u, j), f[2 * j], f[2 * j + 1]);
-  }
-  __device__ __forceinline__ static void store(X* row, int i, const float (&f)[N]) { __stcs(reinterpret_cast<uint4*>(row) + i, pack_vec<X>(f)); }
+  __device__ __forceinline__ void load(const X* p) { u = __ldcs(reinterpret_cast<const uint4*>(p)); }
 };
 template <typename X> struct Unit<X, false> {
   static constexpr int N = 1;
   X u;
-  __device__ __forceinline__ void load(const X* row, int i) { u = row[i]; }
-  __device__ __forceinline__ void clear() { u = from_f<X>(0.0f); }
-  __device__ __forceinline__ void get(float (&f)[1]) const { f[0] = to_f(u); }
-  __device__ __forceinline__ static void store(X* row, int i, const float (&f)[1]) { row[i] = from_f<X>(f[0]); }
+  __device__ __forceinline__ void load(const X* p) { u = *p; }
 };
+
+// The pairs of a thread's units, of which `n` hold something: f(unit, pair in it, pair's number, whether the second element counts).
+template <typename X, bool VEC, int NV, typename F> __device__ __forceinline__ void each_pair(int n, F&& f) {
+  if constexpr (VEC) {
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      if (i >= n) break;
+#pragma unroll
+      for (int j = 0; j < Vec<X>::N / 2; ++j) f(i, j, i * (Vec<X>::N / 2) + j, true);
+    }
+  } else {
+#pragma unroll
+    for (int j = 0; j < NV / 2; ++j) {
+      if (2 * j >= n) break;
+      f(2 * j, 0, j, 2 * j + 1 < n);
+    }
+  }
+}
+
+// Writes f of every pair, its arguments as above, to a row from p on.
+template <typename X, bool VEC, int NV, int L, typename F> __device__ __forceinline__ void put_pairs(int n, X* p, F&& f) {
+  if constexpr (VEC) {
+    constexpr int N = Vec<X>::N;
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      if (i >= n) break;
+      float o[N];
+#pragma unroll
+      for (int j = 0; j < N / 2; ++j) unpack2(f(i, j, i * (N / 2) + j, true), o[2 * j], o[2 * j + 1]);
+      __stcs(reinterpret_cast<uint4*>(p + i * L * N), pack_vec<X>(o));
+    }
+  } else {
+#pragma unroll
+    for (int j = 0; j < NV / 2; ++j) {
+      if (2 * j >= n) break;
+      const bool second = 2 * j + 1 < n;
+      float a, b;
+      unpack2(f(2 * j, 0, j, second), a, b);
+      p[2 * j * L] = from_f<X>(a);
+      if (second) p[(2 * j + 1) * L] = from_f<X>(b);
+    }
+  }
+}
+// The pair j of a vector, or the pair that begins with element i.
+template <typename X, bool VEC, typename G> __device__ __forceinline__ f2 pair_of(G&& get, int i, int j, bool second) {
+  if constexpr (VEC) return Vec<X>::pair(get(i).u, j);
+  else return pack2(to_f(get(i).u), second ? to_f(get(i + 1).u) : 0.0f);
+}
+__device__ __forceinline__ float add_up(f2 v) {
+  float a, b;
+  unpack2(v, a, b);
+  return a + b;
+}
+__device__ __forceinline__ f2 both(float v) { return pack2(v, v); }
 
 // The sum over L neighbouring lanes, for each of them.
 template <int L> __device__ __forceinline__ float lanes_sum(float v) {
@@ -42,16 +87,36 @@ __device__ __forceinline__ float parameter(const void* p, int type, int64_t i, f
 // Parameters in shared memory, unit by unit; of units of eight the first fours, then the second fours, so that neighbouring lanes read
 // neighbouring 16 bytes.
 template <int N> __device__ __forceinline__ int place(int i, int units) { return N == 8 ? (((i >> 2) & 1) * units + (i >> 3)) * 4 + (i & 3) : i; }
-template <int N> __device__ __forceinline__ void get_params(const float* p, int unit, int units, float (&f)[N]) {
+// The parameters of pair k (as in each_pair) of the lane `at`.
+template <int N, int L> __device__ __forceinline__ f2 param_pair(const float* p, int at, int units, int k, bool second) {
   if constexpr (N == 1) {
-    f[0] = p[unit];
+    const float* q = p + at + 2 * k * L;
+    return pack2(q[0], second ? q[L] : 0.0f);
   } else {
-#pragma unroll
-    for (int h = 0; h < N / 4; ++h) {
-      const float4 v = reinterpret_cast<const float4*>(p)[h * units + unit];
-      f[4 * h] = v.x; f[4 * h + 1] = v.y; f[4 * h + 2] = v.z; f[4 * h + 3] = v.w;
-    }
+    const int i = k / (N / 2), j = k % (N / 2);
+    const ulonglong2 q = reinterpret_cast<const ulonglong2*>(p)[(j / 2) * units + at + i * L];
+    return j % 2 ? q.y : q.x;
   }
+}
+
+// D parameters to their places, eight loads of a thread on their way at once.
+template <int N, typename W> __device__ __forceinline__ void put_typed(float* to, const W* from, int D, int units) {
+  for (int i0 = threadIdx.x; i0 < D; i0 += 8 * blockDim.x) {
+    W v[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+      if (i0 + j * int(blockDim.x) < D) v[j] = from[i0 + j * blockDim.x];
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+      if (i0 + j * int(blockDim.x) < D) to[place<N>(i0 + j * blockDim.x, units)] = to_f(v[j]);
+  }
+}
+template <int N> __device__ __forceinline__ void put_params(float* to, const void* p, int type, float none, int D, int units) {
+  if (!p)
+    for (int i = threadIdx.x; i < D; i += blockDim.x) to[i] = none;
+  else if (type == MV_F32) put_typed<N>(to, static_cast<const float*>(p), D, units);
+  else if (type == MV_BF16) put_typed<N>(to, static_cast<const __nv_bfloat16*>(p), D, units);
+  else put_typed<N>(to, static_cast<const __half*>(p), D, units);
 }
 
 struct NormArgs {
@@ -63,84 +128,77 @@ struct NormArgs {
   int64_t per;                       // rows per CTA
 };
 
-constexpr int NORM_TPB = 256;
+constexpr int NORM_TPB = 256, WIDE_TPB = 512;
 
-// WIDE: all warps of the CTA share a row, else L lanes have one each.
-template <typename X, bool VEC, int L, int NV, bool WIDE>
-__global__ void __launch_bounds__(WIDE ? 512 : NORM_TPB) k_norm(const X* x, X* y, const __grid_constant__ NormArgs a) {
+// Waits for the `lanes` threads (whole warps) of one group.
+__device__ __forceinline__ void group_sync(int group, int lanes) { asm volatile("bar.sync %0, %1;" ::"r"(group + 1), "r"(lanes) : "memory"); }
+
+// Threads at work at once decide how many bytes are on their way: CTAs per multiprocessor that the registers allow.
+constexpr int norm_resident(int elements, bool wide) { return elements > 16 ? (wide ? 1 : 2) : wide ? 2 : elements > 8 ? 4 : 6; }
+
+template <typename X, bool VEC, int L, int NV>
+__global__ void __launch_bounds__(L > 32 ? WIDE_TPB : NORM_TPB, norm_resident(NV * Unit<X, VEC>::N, L > 32)) k_norm(const X* x, X* y, const __grid_constant__ NormArgs a) {
   using Un = Unit<X, VEC>;
-  constexpr int N = Un::N;
+  constexpr int N = Un::N, GROUPS = (L > 32 ? WIDE_TPB : NORM_TPB) / L, WARPS = L / 32;
   extern __shared__ float4 params[];         // weights, then biases
-  __shared__ float part[2][16];
-  const int D = int(a.D), units = D / N;
+  __shared__ float part[2][WIDE_TPB / 32];
+  const int D = int(a.D), units = D / N, mine = threadIdx.x / L, at = threadIdx.x % L;
+  const int n = units > at ? (units - at - 1) / L + 1 : 0;
   float* pw = reinterpret_cast<float*>(params);
   float* pb = pw + (D + 3) / 4 * 4;
-  for (int i = threadIdx.x; i < D; i += blockDim.x) {
-    pw[place<N>(i, units)] = parameter(a.weight, a.w_type, i, 1.0f);
-    pb[place<N>(i, units)] = parameter(a.bias, a.w_type, i, 0.0f);
-  }
-  const int groups = WIDE ? 1 : NORM_TPB / L, mine = WIDE ? 0 : threadIdx.x / L;
-  const int at = WIDE ? threadIdx.x : threadIdx.x % L, span = WIDE ? blockDim.x : L;
   const int64_t t0 = blockIdx.x * a.per, t1 = min(a.T, t0 + a.per);
   Un next[NV], u[NV];
   auto load = [&](int64_t t) {
+    const X* p = x + t * a.ldx + at * N;
+    const int any = t < t1 ? n : 0;
 #pragma unroll
-    for (int i = 0; i < NV; ++i) {
-      if (t < t1 && at + i * span < units) next[i].load(x + t * a.ldx, at + i * span);
-      else next[i].clear();
-    }
+    for (int i = 0; i < NV; ++i)
+      if (i < any) next[i].load(p + i * L * N);
   };
+#pragma unroll
+  for (int i = 0; i < NV; ++i) next[i] = Un();
   load(t0 + mine);
+  put_params<N>(pw, a.weight, a.w_type, 1.0f, D, units);
+  put_params<N>(pb, a.bias, a.w_type, 0.0f, D, units);
   __syncthreads();
   auto sum = [&](float v, int k) {
-    v = lanes_sum<L>(v);
-    if (WIDE) {
+    v = lanes_sum<(L < 32 ? L : 32)>(v);
+    if constexpr (WARPS > 1) {
       if ((threadIdx.x & 31) == 0) part[k][threadIdx.x >> 5] = v;
-      __syncthreads();
+      group_sync(mine, L);
       v = 0.0f;
-      for (int i = 0; i < blockDim.x / 32; ++i) v += part[k][i];
+#pragma unroll
+      for (int i = 0; i < WARPS; ++i) v += part[k][mine * WARPS + i];
     }
     return v;
   };
-  const float size = float(D);
-  for (int64_t r = t0; r < t1; r += groups) {
+  auto get = [&](int i) -> const Un& { return u[i]; };
+  const float share = 1.0f / float(D);
+  for (int64_t r = t0; r < t1; r += GROUPS) {
     const int64_t t = r + mine;
 #pragma unroll
     for (int i = 0; i < NV; ++i) u[i] = next[i];
-    load(t + groups);
-    float s = 0.0f, f[N];
-#pragma unroll
-    for (int i = 0; i < NV; ++i) {
-      u[i].get(f);
-      float q = f[0];
-#pragma unroll
-      for (int e = 1; e < N; ++e) q += f[e];
-      s += q;
-    }
-    const float mu = sum(s, 0) / size;
-    s = 0.0f;
-#pragma unroll
-    for (int i = 0; i < NV; ++i) {
-      if (at + i * span >= units) break;
-      u[i].get(f);
-#pragma unroll
-      for (int e = 0; e < N; ++e) s = fmaf(f[e] - mu, f[e] - mu, s);
-    }
-    const float rs = rsqrtf(sum(s, 1) / size + a.eps);
+    load(t + GROUPS);
+    f2 s = both(0.0f);
+    each_pair<X, VEC, NV>(n, [&](int i, int j, int, bool second) { s = add2(s, pair_of<X, VEC>(get, i, j, second)); });
+    const float mu = sum(add_up(s), 0) * share;
+    const f2 minus = both(-mu);
+    s = both(0.0f);
+    each_pair<X, VEC, NV>(n, [&](int i, int j, int, bool second) {
+      f2 d = add2(pair_of<X, VEC>(get, i, j, second), minus);
+      if (!second) {
+        float d0, d1;
+        unpack2(d, d0, d1);
+        d = pack2(d0, 0.0f);
+      }
+      s = fma2(d, d, s);
+    });
+    const float rs = rsqrtf(fmaf(sum(add_up(s), 1), share, a.eps));
     if (t >= t1) continue;
-    X* out = y + t * a.ldy;
-#pragma unroll
-    for (int i = 0; i < NV; ++i) {
-      const int v = at + i * span;
-      if (v >= units) break;
-      u[i].get(f);
-      float w[N], b[N];
-      get_params<N>(pw, v, units, w);
-      get_params<N>(pb, v, units, b);
-#pragma unroll
-      for (int e = 0; e < N; ++e) f[e] = fmaf((f[e] - mu) * rs, w[e], b[e]);
-      Un::store(out, v, f);
-    }
+    const f2 rs2 = both(rs);
+    put_pairs<X, VEC, NV, L>(n, y + t * a.ldy + at * N, [&](int i, int j, int k, bool second) {
+      return fma2(mul2(add2(pair_of<X, VEC>(get, i, j, second), minus), rs2), param_pair<N, L>(pw, at, units, k, second), param_pair<N, L>(pb, at, units, k, second));
+    });
     if (at == 0) {
       if (a.mean) a.mean[t] = mu;
       if (a.rstd) a.rstd[t] = rs;
@@ -192,122 +250,177 @@ struct NormGradArgs {
   float *dweight, *dbias, *part;      // part: [CTAs][2][D]
   int accumulate, parts;
   int64_t per;                       // rows per CTA
+  int stages;
 };
 
-// R rows at a time; a thread owns its columns' weights and sums over rows.
-template <typename X, bool VEC, int L, int NV, int R, int THREADS>
-__global__ void __launch_bounds__(THREADS) k_norm_grad(const X* dy, const X* x, X* dx, const __grid_constant__ NormGradArgs a) {
+// Bytes to a thread's own place in shared memory, `n` of them (the rest of 16 or 4 is zero).
+template <int BYTES> __device__ __forceinline__ void fetch(void* to, const void* from, bool any) {
+  const uint32_t s = uint32_t(__cvta_generic_to_shared(to));
+  const int n = any ? BYTES : 0;
+  if constexpr (BYTES == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(s), "l"(from), "r"(n) : "memory");
+  else asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(s), "l"(from), "r"(n) : "memory");
+}
+__device__ __forceinline__ void fetched(int behind) {        // all but the last `behind` groups of copies have come
+  if (behind == 2) asm volatile("cp.async.wait_group 2;" ::: "memory");
+  else if (behind == 1) asm volatile("cp.async.wait_group 1;" ::: "memory");
+  else asm volatile("cp.async.wait_group 0;" ::: "memory");
+}
+
+// R rows at a time; a thread owns its columns' sums over rows.  The units of x and dy travel through a thread's own places in
+// shared memory, a.stages deep, so that nothing waits for them but the thread itself (elements of 2 bytes, which cannot be copied like that,
+// go through registers).
+template <int L> constexpr int GRAD_THREADS = L > NORM_TPB ? L : NORM_TPB;
+
+template <typename X, bool VEC, int L, int NV, int R>
+__global__ void __launch_bounds__(GRAD_THREADS<L>, L > NORM_TPB ? 1 : 2) k_norm_grad(const X* dy, const X* x, X* dx, const __grid_constant__ NormGradArgs a) {
   using Un = Unit<X, VEC>;
-  constexpr int N = Un::N;
-  constexpr bool WIDE = THREADS > NORM_TPB;
-  extern __shared__ float4 params[];         // weights, laid out as above; at the end the groups' sums, not WIDE
-  __shared__ float part[2][2 * R][32];
-  const int D = int(a.D), units = D / N;
-  float* pw = reinterpret_cast<float*>(params);
-  for (int i = threadIdx.x; i < D; i += blockDim.x) pw[place<N>(i, units)] = parameter(a.weight, a.w_type, i, 1.0f);
-  const int groups = WIDE ? 1 : NORM_TPB / L, mine = WIDE ? 0 : threadIdx.x / L;
-  const int at = WIDE ? threadIdx.x : threadIdx.x % L, span = WIDE ? blockDim.x : L;
+  constexpr int N = Un::N, BYTES = N * int(sizeof(X)), PAIRS = NV * N / 2, THREADS = GRAD_THREADS<L>, GROUPS = THREADS / L, WARPS = L / 32, STAGE = R * NV * 2 * THREADS;
+  constexpr bool RING = BYTES >= 4;
+  extern __shared__ float4 shared[];         // the ring, weights, laid out as above; at the end the groups' sums
+  __shared__ float part[2][2 * R][THREADS / 32];
+  const int D = int(a.D), units = D / N, tid = threadIdx.x, mine = tid / L, at = tid % L;
+  const int n = units > at ? (units - at - 1) / L + 1 : 0;
+  Un* ring = reinterpret_cast<Un*>(shared);
+  float* pw = RING ? reinterpret_cast<float*>(ring + a.stages * STAGE) : reinterpret_cast<float*>(shared);
   const int64_t t0 = blockIdx.x * a.per, t1 = min(a.T, t0 + a.per);
-  float dw[NV][N] = {}, db[NV][N] = {};
-  __syncthreads();
-  const float size = float(D);
-  int flip = 0;
-  for (int64_t r0 = t0; r0 < t1; r0 += groups * R) {
-    Un ux[R][NV], uy[R][NV];
-    float mu[R], rs[R], s[2 * R];
+  constexpr int STEP = GROUPS * R;
+  auto row = [&](int64_t r0, int r) { return r0 + r * GROUPS + mine; };
+  auto issue = [&](int64_t r0, int slot) {
+    if constexpr (RING) {
 #pragma unroll
-    for (int r = 0; r < R; ++r) {
-      const int64_t t = r0 + r * groups + mine;
+      for (int r = 0; r < R; ++r) {
+        const int64_t t = row(r0, r);
+        const int any = t < t1 ? n : 0;
+        const X *px = x + t * a.ldx + at * N, *py = dy + t * a.lddy + at * N;
+        Un* to = ring + slot * STAGE + r * NV * 2 * THREADS + tid;
 #pragma unroll
-      for (int i = 0; i < NV; ++i) {
-        if (t < t1 && at + i * span < units) {
-          ux[r][i].load(x + t * a.ldx, at + i * span);
-          uy[r][i].load(dy + t * a.lddy, at + i * span);
-        } else {
-          ux[r][i].clear();
-          uy[r][i].clear();
+        for (int i = 0; i < NV; ++i) {
+          fetch<BYTES>(to + i * 2 * THREADS, i < any ? px + i * L * N : x, i < any);
+          fetch<BYTES>(to + (i * 2 + 1) * THREADS, i < any ? py + i * L * N : dy, i < any);
         }
       }
+      asm volatile("cp.async.commit_group;" ::: "memory");
+    }
+  };
+  float mu[R], rs[R];
+  auto statistics = [&](int64_t r0) {
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+      const int64_t t = row(r0, r);
       mu[r] = t < t1 ? a.mean[t] : 0.0f;
       rs[r] = t < t1 ? a.rstd[t] : 0.0f;
     }
+  };
+  for (int s = 0; s + 1 < a.stages; ++s) issue(t0 + s * STEP, s);
+  statistics(t0);
+  put_params<N>(pw, a.weight, a.w_type, 1.0f, D, units);
+  f2 dw[PAIRS], db[PAIRS];
 #pragma unroll
-    for (int r = 0; r < R; ++r) {
-      float s0 = 0.0f, s1 = 0.0f;
+  for (int k = 0; k < PAIRS; ++k) dw[k] = db[k] = both(0.0f);
+  __syncthreads();
+  const float share = 1.0f / float(D);
+  int flip = 0, slot = 0;
+  for (int64_t r0 = t0; r0 < t1; r0 += STEP) {
+    Un regs[RING ? 1 : R][RING ? 1 : NV][2];
+    if constexpr (RING) {
+      issue(r0 + (a.stages - 1) * STEP, slot == 0 ? a.stages - 1 : slot - 1);
+      fetched(a.stages - 1);
+    } else {
 #pragma unroll
-      for (int i = 0; i < NV; ++i) {
-        if (at + i * span >= units) break;
-        float fx[N], fy[N], w[N];
-        ux[r][i].get(fx);
-        uy[r][i].get(fy);
-        get_params<N>(pw, at + i * span, units, w);
+      for (int r = 0; r < R; ++r) {
+        const int64_t t = row(r0, r);
+        const int any = t < t1 ? n : 0;
+        const X *px = x + t * a.ldx + at, *py = dy + t * a.lddy + at;
 #pragma unroll
-        for (int e = 0; e < N; ++e) {
-          const float n = (fx[e] - mu[r]) * rs[r], h = fy[e] * w[e];
-          s0 += h;
-          s1 = fmaf(h, n, s1);
-          dw[i][e] = fmaf(fy[e], n, dw[i][e]);
-          db[i][e] += fy[e];
+        for (int i = 0; i < NV; ++i) {
+          regs[r][i][0] = regs[r][i][1] = Un();
+          if (i < any) {
+            regs[r][i][0].load(px + i * L);
+            regs[r][i][1].load(py + i * L);
+          }
         }
       }
-      s[2 * r] = s0;
-      s[2 * r + 1] = s1;
     }
-    if (!dx) continue;
-#pragma unroll
-    for (int j = 0; j < 2 * R; ++j) s[j] = lanes_sum<L>(s[j]);
-    if (WIDE) {
-      if ((threadIdx.x & 31) == 0)
-#pragma unroll
-        for (int j = 0; j < 2 * R; ++j) part[flip][j][threadIdx.x >> 5] = s[j];
-      __syncthreads();
-#pragma unroll
-      for (int j = 0; j < 2 * R; ++j) {
-        s[j] = 0.0f;
-        for (int i = 0; i < blockDim.x / 32; ++i) s[j] += part[flip][j][i];
-      }
-      flip ^= 1;
-    }
+    // x (0) or dy (1) of row r
+    auto of = [&](int r, int which) {
+      const Un* from = ring + slot * STAGE + (r * NV * 2 + which) * THREADS + tid;
+      return [&, from, r, which](int i) -> const Un& {
+        if constexpr (RING) return from[i * 2 * THREADS];
+        else return regs[r][i][which];
+      };
+    };
+    float s[2 * R];
 #pragma unroll
     for (int r = 0; r < R; ++r) {
-      const int64_t t = r0 + r * groups + mine;
-      if (t >= t1) continue;
-      const float s0 = s[2 * r] / size, s1 = s[2 * r + 1] / size;
+      f2 s0 = both(0.0f), s1 = s0;
+      const f2 minus = both(-mu[r]), rs2 = both(rs[r]);
+      auto gx = of(r, 0), gy = of(r, 1);
+      each_pair<X, VEC, NV>(n, [&](int i, int j, int k, bool second) {
+        const f2 vx = pair_of<X, VEC>(gx, i, j, second), vy = pair_of<X, VEC>(gy, i, j, second);
+        const f2 nn = mul2(add2(vx, minus), rs2), h = mul2(vy, param_pair<N, L>(pw, at, units, k, second));
+        s0 = add2(s0, h);
+        s1 = fma2(h, nn, s1);
+        dw[k] = fma2(vy, nn, dw[k]);
+        db[k] = add2(db[k], vy);
+      });
+      s[2 * r] = add_up(s0);
+      s[2 * r + 1] = add_up(s1);
+    }
+    if (dx) {
 #pragma unroll
-      for (int i = 0; i < NV; ++i) {
-        if (at + i * span >= units) break;
-        float fx[N], fy[N], w[N];
-        ux[r][i].get(fx);
-        uy[r][i].get(fy);
-        get_params<N>(pw, at + i * span, units, w);
+      for (int j = 0; j < 2 * R; ++j) s[j] = lanes_sum<(L < 32 ? L : 32)>(s[j]);
+      if constexpr (WARPS > 1) {
+        if ((tid & 31) == 0)
 #pragma unroll
-        for (int e = 0; e < N; ++e) {
-          const float n = (fx[e] - mu[r]) * rs[r];
-          fx[e] = rs[r] * (fmaf(fy[e], w[e], -s0) - n * s1);
+          for (int j = 0; j < 2 * R; ++j) part[flip][j][tid >> 5] = s[j];
+        group_sync(mine, L);
+#pragma unroll
+        for (int j = 0; j < 2 * R; ++j) {
+          s[j] = 0.0f;
+#pragma unroll
+          for (int i = 0; i < WARPS; ++i) s[j] += part[flip][j][mine * WARPS + i];
         }
-        Un::store(dx + t * a.lddx, at + i * span, fx);
+        flip ^= 1;
+      }
+#pragma unroll
+      for (int r = 0; r < R; ++r) {
+        const int64_t t = row(r0, r);
+        if (t >= t1) continue;
+        const f2 minus = both(-mu[r]), rs2 = both(rs[r]), m0 = both(-s[2 * r] * share), m1 = both(-s[2 * r + 1] * share);
+        auto gx = of(r, 0), gy = of(r, 1);
+        put_pairs<X, VEC, NV, L>(n, dx + t * a.lddx + at * N, [&](int i, int j, int k, bool second) {
+          const f2 nn = mul2(add2(pair_of<X, VEC>(gx, i, j, second), minus), rs2);
+          return mul2(fma2(nn, m1, fma2(pair_of<X, VEC>(gy, i, j, second), param_pair<N, L>(pw, at, units, k, second), m0)), rs2);
+        });
       }
     }
+    statistics(r0 + STEP);
+    slot = slot + 1 == a.stages ? 0 : slot + 1;
   }
   if (!a.part) return;
   float* out = a.part + int64_t(blockIdx.x) * 2 * D;
-  float* sums = WIDE ? out : pw + mine * 2 * D;
+  float* sums = GROUPS == 1 ? out : reinterpret_cast<float*>(shared) + mine * 2 * D;
+  asm volatile("cp.async.wait_all;" ::: "memory");
   __syncthreads();
 #pragma unroll
-  for (int i = 0; i < NV; ++i)
+  for (int k = 0; k < PAIRS; ++k) {
+    float w[2], b[2];
+    unpack2(dw[k], w[0], w[1]);
+    unpack2(db[k], b[0], b[1]);
 #pragma unroll
-    for (int e = 0; e < N; ++e) {
-      const int c = (at + i * span) * N + e;
+    for (int e = 0; e < 2; ++e) {
+      const int c = N == 1 ? at + (2 * k + e) * L : (at + k / (N / 2) * L) * N + k % (N / 2) * 2 + e;
       if (c < D) {
-        sums[c] = dw[i][e];
-        sums[D + c] = db[i][e];
+        sums[c] = w[e];
+        sums[D + c] = b[e];
       }
     }
-  if (WIDE) return;
+  }
+  if (GROUPS == 1) return;
   __syncthreads();
-  for (int c = threadIdx.x; c < 2 * D; c += NORM_TPB) {
+  for (int c = tid; c < 2 * D; c += THREADS) {
     float v = 0.0f;
-    for (int g = 0; g < groups; ++g) v += pw[g * 2 * D + c];
+    for (int g = 0; g < GROUPS; ++g) v += reinterpret_cast<const float*>(shared)[g * 2 * D + c];
     out[c] = v;
   }
 }
@@ -341,8 +454,8 @@ __global__ void __launch_bounds__(LONG_TPB) k_norm_grad_long(const X* dy, const 
   }
 }
 
-// The CTAs' sums, 32 columns (of 2 D) per CTA, each by eight threads in turn.
-constexpr int JOIN = 8;
+// The CTAs' sums, 32 columns (of 2 D) per CTA, each by 32 threads in turn.
+constexpr int JOIN = 32;
 __global__ void __launch_bounds__(32 * JOIN) k_norm_join(const __grid_constant__ NormGradArgs a) {
   __shared__ float sh[JOIN][32];
   const int64_t c = int64_t(blockIdx.x) * 32 + threadIdx.x % 32;
@@ -364,13 +477,9 @@ __global__ void __launch_bounds__(32 * JOIN) k_norm_join(const __grid_constant__
 }
 
 // How rows of `units` are shared: by few lanes with many units each where there are many rows, by many lanes where there are few.
-struct Shape {
-  int lanes, nv, threads;            // lanes per row, units of each, threads per CTA; more than 32 lanes: a CTA per row
-  bool wide() const { return lanes > 32; }
-  int groups() const { return wide() ? 1 : threads / lanes; }
-};
+struct Shape { int lanes, nv; };
 
-constexpr int MANY_ROWS = 148 * 8;
+constexpr int MANY_ROWS = 148 * 8, WAVES = 3;
 
 inline int pow2_at_least(int64_t n) {
   int p = 1;
@@ -378,28 +487,29 @@ inline int pow2_at_least(int64_t n) {
   return p;
 }
 
-// least and most units per lane: powers of two
-inline bool norm_shape(int64_t units, int64_t T, int least_lanes, int most_lanes, int least, int most, Shape* s) {
+// All of them powers of two; `liked`: units per lane where there are many rows.
+inline bool norm_shape(int64_t units, int64_t T, int least_lanes, int most_lanes, int least, int liked, int most, Shape* s) {
   if (units > int64_t(most_lanes) * most) return false;
-  int64_t lanes = pow2_at_least((units + (T >= MANY_ROWS ? most : least) - 1) / (T >= MANY_ROWS ? most : least));
-  if (lanes < least_lanes) lanes = least_lanes;
-  if (lanes > most_lanes) lanes = most_lanes;
+  const int want = T >= MANY_ROWS ? liked : least;
+  int64_t lanes = pow2_at_least((units + want - 1) / want);
+  lanes = lanes < least_lanes ? least_lanes : lanes > most_lanes ? most_lanes : lanes;
   s->nv = pow2_at_least((units + lanes - 1) / lanes);
   if (s->nv < least) s->nv = least;
-  if (lanes > 32) lanes = (((units + s->nv - 1) / s->nv) + 31) / 32 * 32;
   s->lanes = int(lanes);
-  s->threads = s->wide() ? s->lanes : NORM_TPB;
   return true;
 }
 
+// Calls f with the lanes and units as constants; only the pairs that norm_shape can give.
 template <int I> using Int = std::integral_constant<int, I>;
-// Calls f with the lanes (0: more than 32) and the units per lane as constants.
-template <typename F> int with_lanes(const Shape& s, F&& f) {
-  return s.lanes == 8 ? f(Int<8>()) : s.lanes == 16 ? f(Int<16>()) : s.wide() ? f(Int<0>()) : f(Int<32>());
+template <int LANES, bool ALL, int NV, int LIKED, int MOST, typename F> int with_units(int nv, F&& f) {
+  if constexpr (NV >= MOST) return f(Int<LANES>(), Int<MOST>());
+  else return nv <= NV ? f(Int<LANES>(), Int<NV>()) : with_units<LANES, ALL, ALL ? NV * 2 : LIKED, LIKED, MOST>(nv, f);
 }
-template <int LEAST, int MOST, typename F> int with_units(int nv, F&& f) {
-  if constexpr (LEAST >= MOST) return f(Int<MOST>());
-  else return nv <= LEAST ? f(Int<LEAST>()) : with_units<LEAST * 2, MOST>(nv, f);
+template <int LANES, int MOST_LANES, int LEAST, int LIKED, int MOST, int FEWEST, typename F> int with_shape(const Shape& s, F&& f) {
+  if constexpr (LANES < MOST_LANES) {
+    if (s.lanes != LANES) return with_shape<LANES * 2, MOST_LANES, LEAST, LIKED, MOST, FEWEST>(s, f);
+  }
+  return with_units<LANES, LANES == FEWEST || LANES == MOST_LANES, LEAST, LIKED, LANES == MOST_LANES ? MOST : LIKED>(s.nv, f);
 }
 
 constexpr int64_t MOST_PARTS = 1184;
@@ -439,21 +549,21 @@ int mv_layer_norm(void* stream, const void* x, int type, int64_t T, int64_t D, i
     X* yp = static_cast<X*>(y);
     auto launch = [&](auto vec) {
       constexpr bool VEC = decltype(vec)::value;
-      constexpr int N = Unit<X, VEC>::N, LEAST = VEC ? 1 : 4, MOST = VEC ? 8 : 32;
+      constexpr int N = Unit<X, VEC>::N, FEWEST = VEC ? 8 : 32, LEAST = VEC ? 1 : 4, LIKED = 8, MOST = VEC ? 8 : 32;
       Shape s;
       const size_t smem = size_t((D + 3) / 4 * 4) * 8;
-      if (smem > 200 * 1024 || !norm_shape(D / N, T, VEC ? 8 : 32, 512, LEAST, MOST, &s)) return -1;
-      const int64_t waves = int64_t(148) * (2048 / s.threads) * 2, groups = s.groups();
-      a.per = ((T + waves - 1) / waves + groups - 1) / groups * groups;
-      return with_lanes(s, [&](auto lanes) {
-        return with_units<LEAST, MOST>(s.nv, [&](auto nv) {
-          constexpr int L = decltype(lanes)::value, NV = decltype(nv)::value;
-          auto* kernel = k_norm<X, VEC, L ? L : 32, NV, L == 0>;
-          static SmemLimit limit;
-          if (smem > 48 * 1024 && !allow_smem(kernel, int(smem), &limit)) return int(MV_ERR_CUDA);
-          kernel<<<unsigned((T + a.per - 1) / a.per), s.threads, smem, st>>>(xp, yp, a);
-          return cuda_ok();
-        });
+      if (smem > 200 * 1024 || !norm_shape(D / N, T, FEWEST, WIDE_TPB, LEAST, LIKED, MOST, &s)) return -1;
+      return with_shape<FEWEST, WIDE_TPB, LEAST, LIKED, MOST, FEWEST>(s, [&](auto lanes, auto nv) {
+        constexpr int L = decltype(lanes)::value, NV = decltype(nv)::value, THREADS = L > 32 ? WIDE_TPB : NORM_TPB, GROUPS = THREADS / L;
+        int64_t ctas = norm_resident(NV * N, L > 32);
+        if (ctas * int64_t(smem + 1024) > 227 * 1024) ctas = 227 * 1024 / int64_t(smem + 1024);
+        ctas *= 148 * WAVES;
+        a.per = ((T + ctas - 1) / ctas + GROUPS - 1) / GROUPS * GROUPS;
+        auto* kernel = k_norm<X, VEC, L, NV>;
+        static SmemLimit limit;
+        if (smem > 48 * 1024 && !allow_smem(kernel, int(smem), &limit)) return int(MV_ERR_CUDA);
+        kernel<<<unsigned((T + a.per - 1) / a.per), THREADS, smem, st>>>(xp, yp, a);
+        return cuda_ok();
       });
     };
     const bool vec = D % Vec<X>::N == 0 && !unaligned(x, T, ldx, size) && !unaligned(y, T, ldy, size);
@@ -506,24 +616,30 @@ int mv_layer_norm_grad(void* stream, const void* dy, int64_t lddy, const void* x
     X* dxp = static_cast<X*>(dx);
     auto launch = [&](auto vec) {
       constexpr bool VEC = decltype(vec)::value;
-      constexpr int N = Unit<X, VEC>::N, LEAST = VEC ? 1 : 4, MOST = 16 / N;
+      constexpr int N = Unit<X, VEC>::N, BYTES = N * int(sizeof(X)), FEWEST = VEC ? 8 : 32, LEAST = VEC ? 1 : 4, LIKED = 16 / N, MOST = 32 / N;
       Shape s;
-      if (!norm_shape(D / N, T, VEC ? 8 : 32, 1024, LEAST, MOST, &s)) return -1;
-      const int64_t groups = s.groups();
-      int64_t parts = int64_t(148) * (s.threads > 512 ? 1 : s.threads >= 256 ? 768 / s.threads : 6);
-      if (parts > most_parts) parts = most_parts;
-      a.per = ((T + parts - 1) / parts + groups - 1) / groups * groups;
-      a.parts = int((T + a.per - 1) / a.per);
-      const size_t smem = size_t(s.wide() || !a.part ? 1 : groups * 2) * D * 4;
-      return with_lanes(s, [&](auto lanes) {
-        return with_units<LEAST, MOST>(s.nv, [&](auto nv) {
-          constexpr int L = decltype(lanes)::value, NV = decltype(nv)::value, R = VEC ? (NV < 4 ? 4 / NV : 1) : (NV < 16 ? 2 : 1);
-          auto* kernel = L ? k_norm_grad<X, VEC, L ? L : 32, NV, R, NORM_TPB> : s.threads <= 512 ? k_norm_grad<X, VEC, 32, NV, R, 512> : k_norm_grad<X, VEC, 32, NV, 1, 1024>;
-          static SmemLimit limit;
-          if (smem > 48 * 1024 && !allow_smem(kernel, int(smem), &limit)) return int(MV_ERR_CUDA);
-          kernel<<<unsigned(a.parts), s.threads, smem, st>>>(yp, xp, dxp, a);
-          return cuda_ok();
-        });
+      if (!norm_shape(D / N, T, FEWEST, 512, LEAST, LIKED, MOST, &s)) return -1;
+      return with_shape<FEWEST, 512, LEAST, LIKED, MOST, FEWEST>(s, [&](auto lanes, auto nv) {
+        constexpr int L = decltype(lanes)::value, NV = decltype(nv)::value, THREADS = GRAD_THREADS<L>, GROUPS = THREADS / L;
+        constexpr int R = NV * N > 16 ? 1 : VEC ? (NV < 4 ? 4 / NV : 1) : (NV < 16 ? 2 : 1);
+        const int64_t stage = BYTES < 4 ? 0 : int64_t(R) * NV * 2 * THREADS * BYTES;
+        // two CTAs of 256 threads with two stages each come before three stages
+        int64_t parts = L > NORM_TPB ? 1 : 2;
+        const int64_t least_smem = 2 * stage + 4 * D > GROUPS * 8 * D ? 2 * stage + 4 * D : GROUPS * 8 * D;
+        if (parts * (least_smem + 2048) > 227 * 1024) parts = 1;
+        for (a.stages = 3; a.stages && parts * (a.stages * stage + 4 * D + 2048) > 227 * 1024; --a.stages) {}
+        if (!a.stages) return -1;
+        size_t smem = size_t(a.stages * stage + 4 * D);
+        if (GROUPS > 1 && smem < size_t(GROUPS * 8 * D)) smem = size_t(GROUPS * 8 * D);
+        parts *= 148;
+        if (parts > most_parts) parts = most_parts;
+        a.per = ((T + parts - 1) / parts + GROUPS - 1) / GROUPS * GROUPS;
+        a.parts = int((T + a.per - 1) / a.per);
+        auto* kernel = k_norm_grad<X, VEC, L, NV, R>;
+        static SmemLimit limit;
+        if (smem > 48 * 1024 && !allow_smem(kernel, int(smem), &limit)) return int(MV_ERR_CUDA);
+        kernel<<<unsigned(a.parts), THREADS, smem, st>>>(yp, xp, dxp, a);
+        return cuda_ok();
       });
     };
     const bool vec = D % Vec<X>::N == 0 && !unaligned(x, T, ldx, size) && !unaligned(dy, T, lddy, size) && (!dx || !unaligned(dx, T, lddx, size));

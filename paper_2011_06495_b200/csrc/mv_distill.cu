@@ -12,6 +12,24 @@ struct Teacher {
   int id_type, k, rest;
 };
 
+// A row's alternatives in shared memory: columns (-1: none), log probabilities (-inf there), and one more number each.
+struct List {
+  int* col;
+  float *a, *x;
+  __device__ __forceinline__ List(void* smem, int k) : col(static_cast<int*>(smem)), a(reinterpret_cast<float*>(col + k)), x(a + k) {}
+};
+constexpr int LIST_BYTES = 12;
+
+// want(column): whether its logit is asked for.
+template <typename X, typename F> __device__ __forceinline__ void load_list(const Teacher& h, int64_t t, int64_t V, const X* row, const List& s, F&& want) {
+  for (int j = threadIdx.x; j < h.k; j += blockDim.x) {
+    const int c = int(load_id(h.id, h.id_type, t * h.k + j, V));
+    s.col[j] = c;
+    s.a[j] = c < 0 ? -INFINITY : h.top[t * h.k + j];
+    s.x[j] = c >= 0 && want(c) ? to_f(row[c]) : -INFINITY;
+  }
+}
+
 // What a row's alternatives add up to, in 64 bits (1 - sum q is a small difference).
 struct Mass {
   double scale, rest, all;           // q = scale exp(a - shift), r, M = sum q + r
@@ -19,21 +37,14 @@ struct Mass {
   bool any, bad;                     // an alternative; a NaN or +inf
 };
 
-// The alternative j of row t: its log probability, -inf and column -1 where there is none.
-__device__ __forceinline__ float alternative(const Teacher& h, int64_t t, int j, int64_t V, int64_t& col) {
-  col = load_id(h.id, h.id_type, t * h.k + j, V);
-  return col < 0 ? -INFINITY : h.top[t * h.k + j];
-}
-
 // For every lane of a warp.
-__device__ __forceinline__ Mass mass_of_row(const Teacher& h, int64_t t, int64_t V) {
+__device__ __forceinline__ Mass mass_of_list(const List& l, int k, bool rest) {
   const int lane = threadIdx.x & 31;
   float m = -INFINITY;
   bool any = false, bad = false;
-  for (int j = lane; j < h.k; j += 32) {
-    int64_t c;
-    const float a = alternative(h, t, j, V, c);
-    any |= c >= 0 && (h.rest || a != -INFINITY);
+  for (int j = lane; j < k; j += 32) {
+    const float a = l.a[j];
+    any |= l.col[j] >= 0 && (rest || a != -INFINITY);
     bad |= !(a < INFINITY);
     m = fmaxf(m, a);
   }
@@ -41,17 +52,13 @@ __device__ __forceinline__ Mass mass_of_row(const Teacher& h, int64_t t, int64_t
   s.any = __any_sync(0xffffffffu, any);
   s.bad = __any_sync(0xffffffffu, bad);
   for (int o = 16; o; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
-  s.shift = h.rest || m == -INFINITY ? 0.0f : m;
+  s.shift = rest || m == -INFINITY ? 0.0f : m;
   double q = 0.0;
-  for (int j = lane; j < h.k; j += 32) {
-    int64_t c;
-    const float a = alternative(h, t, j, V, c);
-    if (a != -INFINITY) q += exp(double(a) - double(s.shift));
-  }
+  for (int j = lane; j < k; j += 32) q += exp(double(l.a[j]) - double(s.shift));
   for (int o = 16; o; o >>= 1) q += __shfl_xor_sync(0xffffffffu, q, o);
-  s.scale = h.rest ? 1.0 : 1.0 / q;
-  s.rest = h.rest ? fmax(0.0, 1.0 - q) : 0.0;
-  s.all = h.rest ? q + s.rest : 1.0;
+  s.scale = rest ? 1.0 : 1.0 / q;
+  s.rest = rest ? fmax(0.0, 1.0 - q) : 0.0;
+  s.all = rest ? q + s.rest : 1.0;
   return s;
 }
 
@@ -62,124 +69,305 @@ struct DistillArgs {
   float *kl, *lse, *log_rest;
 };
 
-constexpr int WINDOW = 65536;        // columns whose listed tokens are marked at a time
+constexpr int U = 4;                 // vectors per thread and step, all in flight, two by two from neighbouring places
+constexpr int MARKS = 4096;          // words of marks: one for each thread and step, a bit for each of its logits
 
-template <typename X, int TPB>
-__global__ void __launch_bounds__(TPB) k_distill(const X* __restrict__ logits, const __grid_constant__ DistillArgs a) {
-  __shared__ uint32_t mark[WINDOW / 32];
-  __shared__ float sh[TPB / 32];
-  __shared__ double shd[2][TPB / 32];
+// A CTA per row, streamed once.  With the rest as a class the listed tokens are kept out of the sum (taking them off it would leave nothing of
+// a small rest): a bit for every logit of the next steps, set for the listed ones, which a thread asks one word at a time; their
+// own terms are added at the end.
+template <typename X, bool REST, int TPB>
+__global__ void __launch_bounds__(TPB, 1024 / TPB) k_distill(const X* __restrict__ logits, const __grid_constant__ DistillArgs a) {
+  constexpr int N = Vec<X>::N, WARPS = TPB / 32, WINDOW = MARKS / TPB;
+  extern __shared__ uint32_t dynamic[];
+  __shared__ float s_max[WARPS], s_ref[WARPS], s_sum[WARPS];
+  __shared__ uint32_t s_ends;
+  __shared__ int s_twice;
+  uint32_t* mark = dynamic;          // [step of the window][thread], with REST
+  const List list(dynamic + (REST ? MARKS : 0), a.h.k);
   const int64_t t = blockIdx.x;
+  const int tid = threadIdx.x, lane = tid & 31, w = tid >> 5;
   const X* row = logits + t * a.ld;
-  const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
-  float m = -INFINITY;
-  for (int64_t c = threadIdx.x; c < a.V; c += TPB) m = max_nan(m, to_f(row[c]));
-  for (int o = 16; o; o >>= 1) m = max_nan(m, __shfl_xor_sync(0xffffffffu, m, o));
-  if (lane == 0) sh[w] = m;
+  // the vectors begin at the row's first 32-byte boundary
+  const int64_t to32 = int64_t((32 - (reinterpret_cast<uintptr_t>(row) & 31)) & 31) / int(sizeof(X));
+  const int first = int(min(a.V, to32)), nv = (int(a.V) - first) / (2 * N) * 2, tail_col = first + nv * N, ends = first + int(a.V) - tail_col;
+  const uint4* vec = reinterpret_cast<const uint4*>(row + first);
+  const uint4 none = make_uint4(Vec<X>::NONE, Vec<X>::NONE, Vec<X>::NONE, Vec<X>::NONE);
+  const int n_full = nv / (TPB * U), n_steps = (nv + TPB * U - 1) / (TPB * U);
+  auto load = [&](int step, uint4 (&u)[U]) {
+    const uint4* ptr = vec + step * (U * TPB) + 2 * tid;
+    if (step < n_full) {
+#pragma unroll
+      for (int i = 0; i < U; i += 2) load_stream(ptr + i * TPB, u[i], u[i + 1]);
+    } else {
+#pragma unroll
+      for (int i = 0; i < U; i += 2) {
+        u[i] = u[i + 1] = none;
+        if ((step * U + i) * TPB + 2 * tid < nv) load_stream(ptr + i * TPB, u[i], u[i + 1]);
+      }
+    }
+  };
+  uint4 even[U], odd[U];
+  if (n_steps > 0) load(0, even);
+  if (tid == 0) { s_ends = 0; s_twice = 0; }
+  load_list(a.h, t, a.V, row, list, [](int) { return true; });
+  // marks the listed tokens of the steps [step, step + WINDOW); the ends with the first ones
+  auto set_marks = [&](int step) {
+    __syncthreads();                 // the marks before have been read
+    for (int i = tid; i < min(MARKS, (n_steps - step) * TPB); i += TPB) mark[i] = 0;
+    __syncthreads();
+    for (int j = tid; j < a.h.k; j += TPB) {
+      const int c = list.col[j];
+      uint32_t bit, old = 0;
+      if (c < 0) continue;
+      if (c < first || c >= tail_col) {
+        bit = 1u << (c < first ? c : first + c - tail_col);
+        if (step == 0) old = atomicOr(&s_ends, bit);
+      } else {
+        const unsigned v = unsigned(c - first) / N, s = v / (U * TPB), at = v % (U * TPB), in = at % (2 * TPB);
+        bit = 1u << ((at / (2 * TPB) * 2 + (in & 1)) * N + unsigned(c - first) % N);
+        if (int(s) >= step && int(s) < step + WINDOW) old = atomicOr(mark + (s - step) * TPB + in / 2, bit);
+      }
+      if (old & bit) s_twice = 1;
+    }
+    __syncthreads();
+  };
+  if constexpr (REST) set_marks(0);
+  const bool my_end = tid < ends, end_listed = REST && my_end && (s_ends >> tid & 1u);
+  const float end = my_end ? to_f(row[tid < first ? tid : tail_col + tid - first]) : -INFINITY;
+  const float c2 = fminf(a.scale * LOG2E, 3.0e38f), room = LAG / c2;
+  const f2 c22 = pack2(c2, c2);
+  // logits below the first limit never set the reference; beside a reference above -R_MAX their 2^t is 0
+  float ref = -INFINITY, R = 0.0f, limit = -2.0f * R_MAX / c2, largest = end;
+  f2 minus = pack2(0.0f, 0.0f), s2 = pack2(0.0f, 0.0f);
+  auto raise = [&](float m) {        // a new reference
+    const float Rm = m * c2;
+    if (ref != -INFINITY) {
+      float p0, p1;
+      unpack2(s2, p0, p1);
+      s2 = pack2((p0 + p1) * exp2_fast(max_nan(R - Rm, T_FLOOR)), 0.0f);
+    }
+    ref = m;
+    R = Rm;
+    limit = m + room;
+    minus = pack2(-Rm, -Rm);
+  };
+  auto add_pair = [&](f2 v) {
+    float u0, u1;
+    unpack2(fma2(v, c22, minus), u0, u1);
+    s2 = add2(s2, pack2(exp2_fast(u0), exp2_fast(u1)));
+  };
+  auto hide = [&](int step, uint4 (&u)[U]) {          // the listed logits of a step become masked ones
+    const uint32_t word = mark[step % WINDOW * TPB + tid];
+    if (word == 0) return;
+#pragma unroll
+    for (int i = 0; i < U; ++i) {
+      uint32_t q[4] = {u[i].x, u[i].y, u[i].z, u[i].w};
+#pragma unroll
+      for (int e = 0; e < N; ++e)
+        if (word >> (i * N + e) & 1u) {
+          if constexpr (N == 4) q[e] = Vec<X>::NONE;
+          else q[e / 2] = e % 2 ? (q[e / 2] & 0xffffu) | (Vec<X>::NONE & 0xffff0000u) : (q[e / 2] & 0xffff0000u) | (Vec<X>::NONE & 0xffffu);
+        }
+      u[i] = make_uint4(q[0], q[1], q[2], q[3]);
+    }
+  };
+  auto take = [&](int step, uint4 (&u)[U]) {
+    uint32_t m2 = Vec<X>::max2(Vec<X>::max2(u[0].x, u[0].y), Vec<X>::max2(u[0].z, u[0].w));
+#pragma unroll
+    for (int i = 1; i < U; ++i) m2 = Vec<X>::max2(m2, Vec<X>::max2(Vec<X>::max2(u[i].x, u[i].y), Vec<X>::max2(u[i].z, u[i].w)));
+    const float m = Vec<X>::widen(m2);
+    if (m > limit) raise(m);
+    largest = fmaxf(largest, m);
+    if constexpr (REST) hide(step, u);
+#pragma unroll
+    for (int i = 0; i < U; ++i)
+#pragma unroll
+      for (int j = 0; j < N / 2; ++j) add_pair(Vec<X>::pair(u[i], j));
+  };
+  if (my_end) {
+    if (end > limit) raise(end);
+    add_pair(pack2(end_listed ? -INFINITY : end, -INFINITY));
+  }
+  for (int step = 0; step < n_steps; step += 2) {
+    if (step + 1 < n_steps) load(step + 1, odd);
+    if (REST && step && step % WINDOW == 0) set_marks(step);
+    take(step, even);
+    if (step + 1 >= n_steps) break;
+    if (step + 2 < n_steps) load(step + 2, even);
+    take(step + 1, odd);
+  }
+  float sum;
+  {
+    float p0, p1;
+    unpack2(s2, p0, p1);
+    const float d = ref == -INFINITY ? 0.0f : fmaf(ref, c2, -R);      // at most half a unit of R; 2^-d
+    sum = (p0 + p1) * fmaf(fmaf(0.5f * LN2 * LN2, d, -LN2), d, 1.0f);
+  }
+  // the largest logit, and the sums relative to it
+  for (int o = 16; o; o >>= 1) largest = fmaxf(largest, __shfl_xor_sync(0xffffffffu, largest, o));
+  if (lane == 0) s_max[w] = largest;
   __syncthreads();
-  for (int i = 0; i < TPB / 32; ++i) m = max_nan(m, sh[i]);
-  const float ref = m == -INFINITY ? 0.0f : m;
-  double rest = 0.0, listed = 0.0;
-  for (int64_t c0 = 0; c0 < a.V; c0 += WINDOW) {
-    const int64_t c1 = min(a.V, c0 + WINDOW);
-    __syncthreads();
-    for (int i = threadIdx.x; i < WINDOW / 32; i += TPB) mark[i] = 0;
-    __syncthreads();
-    for (int j = threadIdx.x; j < a.h.k; j += TPB) {
-      int64_t c;
-      alternative(a.h, t, j, a.V, c);
-      if (c >= c0 && c < c1) atomicOr(&mark[(c - c0) / 32], 1u << ((c - c0) & 31));
+  for (int i = 0; i < WARPS; ++i) largest = fmaxf(largest, s_max[i]);
+  const float top = largest, zero = top == -INFINITY ? 0.0f : top;
+  if (top * c2 > R_MAX || c2 < C2_MIN || (top * c2 < -R_MAX && top > -INFINITY)) {
+    // logits that the fused form cannot take: summed again by differences to the largest one
+    sum = 0.0f;
+    auto add = [&](float v) { sum += exp2_fast(distance(v, zero, c2)); };
+    if (my_end && !end_listed) add(end);
+    for (int step = 0; step < n_steps; ++step) {
+      if (REST && step % WINDOW == 0) set_marks(step);
+      load(step, even);
+      if constexpr (REST) hide(step, even);
+#pragma unroll
+      for (int i = 0; i < U; ++i) each_logit<X>(even[i], [&](int, float v) { add(v); });
     }
-    __syncthreads();
-    for (int64_t c = c0 + threadIdx.x; c < c1; c += TPB) {
-      const double e = exp2_fast(distance(to_f(row[c]), ref, a.scale) * LOG2E);
-      (mark[(c - c0) / 32] >> ((c - c0) & 31) & 1u ? listed : rest) += e;
-    }
+  } else if (ref != top) {
+    sum = ref == -INFINITY ? sum : sum * exp2_fast(max_nan(distance(ref, zero, c2), T_FLOOR));
   }
-  for (int o = 16; o; o >>= 1) {
-    rest += __shfl_xor_sync(0xffffffffu, rest, o);
-    listed += __shfl_xor_sync(0xffffffffu, listed, o);
-  }
-  if (lane == 0) { shd[0][w] = rest; shd[1][w] = listed; }
+  for (int o = 16; o; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+  if (lane == 0) s_sum[w] = sum;
   __syncthreads();
   if (w) return;
-  rest = listed = 0.0;
-  for (int i = 0; i < TPB / 32; ++i) { rest += shd[0][i]; listed += shd[1][i]; }
-  const bool nan = !(m < INFINITY);
-  const double ls = log(rest + listed), lr = log(rest) - ls;
-  const Mass s = mass_of_row(a.h, t, a.V);
-  double kl = 0.0;
-  if (s.any)
+  sum = 0.0f;
+  for (int i = 0; i < WARPS; ++i) sum += s_sum[i];
+  // the listed tokens' own terms, each token once
+  double all = sum;
+  if constexpr (REST) {
+    double own = 0.0;
     for (int j = lane; j < a.h.k; j += 32) {
-      int64_t c;
-      const float l = alternative(a.h, t, j, a.V, c);
-      if (l == -INFINITY) continue;
-      const double logq = double(l) - double(s.shift) + log(s.scale), q = exp(logq);
-      if (q > 0.0) kl += q * (logq - (double(distance(to_f(row[c]), ref, a.scale)) - ls));
+      const int c = list.col[j];
+      bool again = c < 0;
+      if (s_twice)
+        for (int i = 0; i < j && !again; ++i) again = list.col[i] == c;
+      if (!again) own += double(exp2_fast(distance(list.x[j], zero, c2)));
     }
+    for (int o = 16; o; o >>= 1) own += __shfl_xor_sync(0xffffffffu, own, o);
+    all += own;
+  }
+  const Mass s = mass_of_list(list, a.h.k, REST);
+  const double ls = log(all), lr = log(double(sum)) - ls;
+  double kl = 0.0;
+  for (int j = lane; j < a.h.k; j += 32) {
+    if (list.a[j] == -INFINITY) continue;
+    const double d = double(list.a[j]) - double(s.shift), q = exp(d) * s.scale;
+    if (q > 0.0) kl += q * (d + log(s.scale) - (double(distance(list.x[j], zero, a.scale)) - ls));
+  }
   for (int o = 16; o; o >>= 1) kl += __shfl_xor_sync(0xffffffffu, kl, o);
   if (lane == 0) {
-    if (s.any && s.rest > 0.0) kl += s.rest * (log(s.rest) - lr);
-    const bool empty = m == -INFINITY;
-    if (a.kl) a.kl[t] = nan || s.bad ? NAN : !s.any ? 0.0f : empty ? INFINITY : float(kl);
-    if (a.lse) a.lse[t] = nan ? NAN : empty ? -INFINITY : fmaf(a.scale, ref, float(ls));
+    const bool nan = isnan(all), empty = all == 0.0;
+    if (REST && s.any && s.rest > 0.0) kl += s.rest * (log(s.rest) - lr);
+    if (a.kl) a.kl[t] = !s.any ? 0.0f : nan || s.bad ? NAN : empty ? INFINITY : float(kl);
+    if (a.lse) a.lse[t] = nan ? NAN : empty ? -INFINITY : fmaf(a.scale, zero, float(ls));
     if (a.log_rest) a.log_rest[t] = nan ? NAN : empty ? -INFINITY : float(lr);
   }
 }
+
+// ------------------------------------------------------------------------------------------ gradient
+// dx = f (M p - q) for a listed token, f M' p for the others, f = c g, M' = M - r / P.  p = q q with q = 2^h, h = log2(p) / 2: the
+// hardware's exponential has no subnormal results.  Each CTA takes one stretch of one row, and all of the row's list: the others' value is
+// written everywhere, and then the listed tokens of the stretch over it.
+constexpr int GRAD_TPB = 256, GRAD_U = 4;
 
 struct DistillGradArgs {
   int64_t V, ld, ldg;
   Teacher h;
   float scale;
+  unsigned stretches;                // CTAs per row
   const float *lse, *log_rest, *g;
 };
 
-template <typename X, int TPB>
-__global__ void __launch_bounds__(TPB) k_distill_grad(const X* logits, X* dlogits, const __grid_constant__ DistillGradArgs a) {
-  __shared__ float sh[4];
-  __shared__ int64_t s_id[MV_TEACHER_MAX];
-  __shared__ float s_q[MV_TEACHER_MAX], s_x[MV_TEACHER_MAX];
-  const int64_t t = blockIdx.x;
+// VEC: logits and gradient start at the same place within 16 bytes in every row.
+template <typename X, bool VEC>
+__global__ void __launch_bounds__(GRAD_TPB) k_distill_grad(const X* logits, X* dlogits, const __grid_constant__ DistillGradArgs a) {
+  constexpr int N = Vec<X>::N;
+  extern __shared__ uint32_t dynamic[];
+  __shared__ float s_f[3];
+  const List list(dynamic, a.h.k);
+  const int64_t t = blockIdx.x / a.stretches;
+  const unsigned stretch = blockIdx.x % a.stretches;
+  const int tid = threadIdx.x;
   const X* x = logits + t * a.ld;
   X* dx = dlogits + t * a.ldg;
-  if (threadIdx.x < 32) {
-    const Mass s = mass_of_row(a.h, t, a.V);
-    const float l = a.lse[t], g = a.g[t];
-    for (int j = threadIdx.x; j < a.h.k; j += 32) {
-      int64_t c;
-      const float v = alternative(a.h, t, j, a.V, c);
-      s_id[j] = c;
-      s_q[j] = float(exp(double(v) - double(s.shift)) * s.scale);
-      s_x[j] = c >= 0 ? to_f(x[c]) : 0.0f;
+  // the vectors begin at the row's first 16-byte boundary; what is before and behind them goes to the first stretch
+  const int64_t first = VEC ? min(a.V, int64_t((16 - (reinterpret_cast<uintptr_t>(x) & 15)) & 15) / int(sizeof(X))) : 0;
+  const int64_t nv = VEC ? (a.V - first) / N : 0, behind = VEC ? first + nv * N : a.V, ends = VEC ? first + a.V - behind : 0;
+  const int64_t v0 = int64_t(stretch) * GRAD_TPB * GRAD_U;                               // of its vectors
+  const int64_t c0 = VEC ? first + v0 * N : v0 * N, c1 = VEC ? min(behind, c0 + GRAD_TPB * GRAD_U * N) : min(a.V, c0 + GRAD_TPB * GRAD_U * N);
+  const uint4* in = reinterpret_cast<const uint4*>(x + first);
+  uint4* out = reinterpret_cast<uint4*>(dx + first);
+  const bool my_end = VEC && stretch == 0 && tid < ends;
+  const int64_t end_col = tid < first ? tid : behind + tid - first;
+  uint4 u[GRAD_U];
+  float end = 0.0f;
+  if constexpr (VEC) {
+#pragma unroll
+    for (int i = 0; i < GRAD_U; ++i)
+      if (v0 + i * GRAD_TPB + tid < nv) u[i] = __ldcs(in + v0 + i * GRAD_TPB + tid);
+    if (my_end) end = to_f(x[end_col]);
+  }
+  auto here = [&](int64_t c) { return (c >= c0 && c < c1) || (VEC && stretch == 0 && c >= 0 && (c < first || c >= behind)); };      // columns of this stretch
+  load_list(a.h, t, a.V, x, list, here);
+  const float l = a.lse[t];
+  __syncthreads();
+  if (tid < 32) {
+    const Mass s = mass_of_list(list, a.h.k, a.h.rest);
+    const float g = a.g[t];
+    if (tid == 0) {
+      double ratio = 0.0;
+      if (a.h.rest && s.rest > 0.0) ratio = a.log_rest[t] == -INFINITY ? s.all : exp(log(s.rest) - double(a.log_rest[t]));
+      s_f[0] = !s.any || g == 0.0f || l == -INFINITY ? 0.0f : a.scale * g;
+      s_f[1] = s.bad ? NAN : float(s.all);
+      s_f[2] = s.bad ? NAN : float(s.all - ratio);
     }
-    if (threadIdx.x == 0) {
-      const bool none = !s.any || g == 0.0f || l == -INFINITY;
-      float ratio = 0.0f;
-      if (a.h.rest && s.rest > 0.0) ratio = a.log_rest[t] == -INFINITY ? float(s.all) : float(exp(log(s.rest) - double(a.log_rest[t])));
-      sh[0] = none ? 0.0f : a.scale * g;
-      sh[1] = s.bad ? NAN : float(s.all);
-      sh[2] = s.bad ? NAN : float(s.all - double(ratio));
-      sh[3] = l;
-    }
+    for (int j = tid; j < a.h.k; j += 32) list.a[j] = float(exp(double(list.a[j]) - double(s.shift)) * s.scale);          // q
   }
   __syncthreads();
-  const float f = sh[0], all = sh[1], other = sh[2], l = sh[3];
-  for (int64_t c = threadIdx.x; c < a.V; c += TPB) {
-    bool listed = false;
-    for (int j = 0; j < a.h.k && !listed; ++j) listed = s_id[j] == c;
-    if (!listed) dx[c] = from_f<X>(f == 0.0f ? 0.0f : f * other * expf(min_nan(fmaf(to_f(x[c]), a.scale, -l), 0.0f)));
-  }
-  for (int j = threadIdx.x; j < a.h.k; j += TPB) {
-    const int64_t c = s_id[j];
-    if (c < 0) continue;
-    float q = 0.0f;
-    bool first = true;
-    for (int i = 0; i < a.h.k; ++i)
-      if (s_id[i] == c) {
-        first &= i >= j;
-        q += s_q[i];
+  const float f = s_f[0], other = f * s_f[2], l2e = 0.5f * LOG2E;
+  const bool none = f == 0.0f;
+  auto share = [&](float v) {                  // p / q; the same operations as two logits at a time below
+    return exp2_fast(min_nan(fmaf(v, a.scale, -l) * l2e, 0.0f));
+  };
+  auto one = [&](float v) {
+    const float q = share(v);
+    return none ? 0.0f : q * (q * other);
+  };
+  if constexpr (VEC) {
+    const f2 scale2 = pack2(a.scale, a.scale), minus = pack2(-l, -l), l2e2 = pack2(l2e, l2e), other2 = pack2(other, other);
+#pragma unroll
+    for (int i = 0; i < GRAD_U; ++i) {
+      const int64_t v = v0 + i * GRAD_TPB + tid;
+      if (v >= nv) break;
+      float d[N];
+#pragma unroll
+      for (int j = 0; j < N / 2; ++j) {
+        float h0, h1;
+        unpack2(mul2(fma2(Vec<X>::pair(u[i], j), scale2, minus), l2e2), h0, h1);
+        const f2 q = pack2(exp2_fast(min_nan(h0, 0.0f)), exp2_fast(min_nan(h1, 0.0f)));
+        unpack2(mul2(q, mul2(q, other2)), d[2 * j], d[2 * j + 1]);
       }
-    if (first) dx[c] = from_f<X>(f == 0.0f ? 0.0f : f * (all * expf(min_nan(fmaf(s_x[j], a.scale, -l), 0.0f)) - q));
+      __stcs(out + v, none ? make_uint4(0, 0, 0, 0) : pack_vec<X>(d));
+    }
+    if (my_end) dx[end_col] = from_f<X>(one(end));
+  } else {
+    for (int64_t c = c0 + tid; c < c1; c += GRAD_TPB) dx[c] = from_f<X>(one(to_f(x[c])));
+  }
+  if (none) return;
+  // the listed tokens of this stretch, each by the thread of its first entry
+  bool mine = false;
+  for (int j = tid; j < a.h.k; j += GRAD_TPB) mine |= here(list.col[j]);
+  if (!__syncthreads_or(mine)) return;
+  for (int j = tid; j < a.h.k; j += GRAD_TPB) {
+    const int c = list.col[j];
+    if (!here(c)) continue;
+    float q = 0.0f;
+    bool head = true;
+    for (int i = 0; i < a.h.k; ++i)
+      if (list.col[i] == c) {
+        head &= i >= j;
+        q += list.a[i];
+      }
+    const float p = share(list.x[j]);
+    if (head) dx[c] = from_f<X>(f * fmaf(s_f[1] * p, p, -q));
   }
 }
 
@@ -203,8 +391,17 @@ int mv_distill(void* stream, const void* logits, int type, int64_t T, int64_t V,
   a.V = V; a.ld = ld; a.h = {top_logprob, top_id, id_type, k, rest}; a.scale = scale; a.kl = kl; a.lse = lse; a.log_rest = log_rest;
   return with_type(type, [&](auto x) {
     using X = decltype(x);
-    k_distill<X, 256><<<unsigned(T), 256, 0, static_cast<cudaStream_t>(stream)>>>(static_cast<const X*>(logits), a);
-    return cuda_ok();
+    const int64_t vecs = V / Vec<X>::N;
+    // short rows take few threads and many CTAs, if there are rows enough to fill the device; long or few rows many threads
+    const int tpb = T >= 1184 && vecs <= 3000 ? 64 : vecs > 10240 || (T < 600 && vecs > 6000) ? 256 : 128;
+    const size_t smem = size_t(k) * LIST_BYTES + (rest ? MARKS * 4 : 0);
+    auto launch = [&](auto r) {
+      constexpr bool REST = decltype(r)::value;
+      auto* kernel = tpb == 64 ? k_distill<X, REST, 64> : tpb == 128 ? k_distill<X, REST, 128> : k_distill<X, REST, 256>;
+      kernel<<<unsigned(T), unsigned(tpb), smem, static_cast<cudaStream_t>(stream)>>>(static_cast<const X*>(logits), a);
+      return cuda_ok();
+    };
+    return rest ? launch(std::true_type()) : launch(std::false_type());
   });
 }
 
@@ -225,7 +422,13 @@ int mv_distill_grad(void* stream, const void* logits, int type, int64_t T, int64
   a.V = V; a.ld = ld; a.ldg = ldg; a.h = {top_logprob, top_id, id_type, k, log_rest ? 1 : 0}; a.scale = scale; a.lse = lse; a.log_rest = log_rest; a.g = g;
   return with_type(type, [&](auto x) {
     using X = decltype(x);
-    k_distill_grad<X, 256><<<unsigned(T), 256, 0, static_cast<cudaStream_t>(stream)>>>(static_cast<const X*>(logits), static_cast<X*>(dlogits), a);
+    const int64_t per = int64_t(GRAD_TPB) * GRAD_U * Vec<X>::N, stretches = (V + per - 1) / per;
+    if (T * stretches >= lim) return int(MV_ERR_INVALID_ARG);
+    a.stretches = unsigned(stretches);
+    // a gradient that lies otherwise within 16 bytes than the logits, in some row, is written one by one
+    const bool vec = ((reinterpret_cast<uintptr_t>(logits) ^ reinterpret_cast<uintptr_t>(dlogits)) & 15) == 0 && (T == 1 || (ld - ldg) * int64_t(sizeof(X)) % 16 == 0);
+    auto* kernel = vec ? k_distill_grad<X, true> : k_distill_grad<X, false>;
+    kernel<<<unsigned(T * stretches), GRAD_TPB, size_t(k) * LIST_BYTES, static_cast<cudaStream_t>(stream)>>>(static_cast<const X*>(logits), static_cast<X*>(dlogits), a);
     return cuda_ok();
   });
 }

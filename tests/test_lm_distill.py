@@ -235,10 +235,10 @@ def test_positions_without_a_teacher_are_zero_whatever_their_logits_hold():
     x, top, ids = case(6, 9001, 4, BF16)
     ids = ids.clamp(min=0)
     g = torch.ones(6, device=DEV)
-    x[0], x[1], x[2] = math.nan, math.nan, math.inf
+    x[0], x[1], x[2], x[4] = math.nan, math.nan, math.inf, math.nan
     ids[0], g[1], ids[2] = -1, 0.0, 9001
     o = call(x, top, ids, 1.0, True)
-    assert float(o["kl"][3]) > 0 and bool(torch.isnan(o["kl"][0])) and bool(torch.isnan(o["log_rest"][0]))
+    assert float(o["kl"][3]) > 0 and float(o["kl"][0]) == 0 and bool(torch.isnan(o["kl"][4])) and bool(torch.isnan(o["log_rest"][0]))
     dx = torch.full_like(x, 7.0)
     B.mv_distill_grad(x, top, ids, o["lse"], g, dx, log_rest=o["log_rest"])
     assert bool((dx[:3] == 0).all()) and bool((dx[3:] != 0).any(1).all())

@@ -264,15 +264,16 @@ __global__ void __launch_bounds__(TPB, 1024 / TPB) k_distill(const X* __restrict
 
 // ------------------------------------------------------------------------------------------ gradient
 // dx = f (M p - q) for a listed token, f M' p for the others, f = c g, M' = M - r / P.  p = q q with q = 2^h, h = log2(p) / 2: the
-// hardware's exponential has no subnormal results.  Each CTA takes one stretch of one row, and all of the row's list: the others' value is
-// written everywhere, and then the listed tokens of the stretch over it.
-constexpr int GRAD_TPB = 256, GRAD_U = 4;
+// hardware's exponential has no subnormal results.  Each CTA takes some stretches of one row, and all of the row's list: the others' value is
+// written everywhere, and then its listed tokens' over it.
+constexpr int GRAD_TPB = 256, GRAD_U = 4, GRAD_MOST = 16, GRAD_CTAS = 148 * 8;
 
 struct DistillGradArgs {
   int64_t V, ld, ldg;
   Teacher h;
   float scale;
-  unsigned stretches;                // CTAs per row
+  unsigned ctas;                     // per row
+  int stretches;                     // per CTA
   const float *lse, *log_rest, *g;
 };
 
@@ -283,29 +284,32 @@ __global__ void __launch_bounds__(GRAD_TPB) k_distill_grad(const X* logits, X* d
   extern __shared__ uint32_t dynamic[];
   __shared__ float s_f[3];
   const List list(dynamic, a.h.k);
-  const int64_t t = blockIdx.x / a.stretches;
-  const unsigned stretch = blockIdx.x % a.stretches;
+  const int64_t t = blockIdx.x / a.ctas;
+  const unsigned part = blockIdx.x % a.ctas;
   const int tid = threadIdx.x;
   const X* x = logits + t * a.ld;
   X* dx = dlogits + t * a.ldg;
   // the vectors begin at the row's first 16-byte boundary; what is before and behind them goes to the first stretch
   const int64_t first = VEC ? min(a.V, int64_t((16 - (reinterpret_cast<uintptr_t>(x) & 15)) & 15) / int(sizeof(X))) : 0;
   const int64_t nv = VEC ? (a.V - first) / N : 0, behind = VEC ? first + nv * N : a.V, ends = VEC ? first + a.V - behind : 0;
-  const int64_t v0 = int64_t(stretch) * GRAD_TPB * GRAD_U;                               // of its vectors
-  const int64_t c0 = VEC ? first + v0 * N : v0 * N, c1 = VEC ? min(behind, c0 + GRAD_TPB * GRAD_U * N) : min(a.V, c0 + GRAD_TPB * GRAD_U * N);
+  const int64_t v0 = int64_t(part) * a.stretches * (GRAD_TPB * GRAD_U), v1 = VEC ? min(nv, v0 + a.stretches * (GRAD_TPB * GRAD_U)) : 0;      // its vectors
+  const int64_t c0 = first + v0 * N, c1 = min(behind, c0 + a.stretches * (GRAD_TPB * GRAD_U * N));                                            // and columns
   const uint4* in = reinterpret_cast<const uint4*>(x + first);
   uint4* out = reinterpret_cast<uint4*>(dx + first);
-  const bool my_end = VEC && stretch == 0 && tid < ends;
+  const bool my_end = VEC && part == 0 && tid < ends;
   const int64_t end_col = tid < first ? tid : behind + tid - first;
-  uint4 u[GRAD_U];
-  float end = 0.0f;
-  if constexpr (VEC) {
+  uint4 u[GRAD_U], next[GRAD_U];
+  auto load = [&](int64_t v) {
 #pragma unroll
     for (int i = 0; i < GRAD_U; ++i)
-      if (v0 + i * GRAD_TPB + tid < nv) u[i] = __ldcs(in + v0 + i * GRAD_TPB + tid);
+      if (v + i * GRAD_TPB < v1) next[i] = __ldcs(in + v + i * GRAD_TPB);
+  };
+  float end = 0.0f;
+  if constexpr (VEC) {
+    load(v0 + tid);
     if (my_end) end = to_f(x[end_col]);
   }
-  auto here = [&](int64_t c) { return (c >= c0 && c < c1) || (VEC && stretch == 0 && c >= 0 && (c < first || c >= behind)); };      // columns of this stretch
+  auto here = [&](int64_t c) { return (c >= c0 && c < c1) || (VEC && part == 0 && c >= 0 && (c < first || c >= behind)); };      // the CTA's columns
   load_list(a.h, t, a.V, x, list, here);
   const float l = a.lse[t];
   __syncthreads();
@@ -333,26 +337,31 @@ __global__ void __launch_bounds__(GRAD_TPB) k_distill_grad(const X* logits, X* d
   };
   if constexpr (VEC) {
     const f2 scale2 = pack2(a.scale, a.scale), minus = pack2(-l, -l), l2e2 = pack2(l2e, l2e), other2 = pack2(other, other);
+    for (int64_t vs = v0 + tid; vs < v1; vs += GRAD_TPB * GRAD_U) {
 #pragma unroll
-    for (int i = 0; i < GRAD_U; ++i) {
-      const int64_t v = v0 + i * GRAD_TPB + tid;
-      if (v >= nv) break;
-      float d[N];
+      for (int i = 0; i < GRAD_U; ++i) u[i] = next[i];
+      load(vs + GRAD_TPB * GRAD_U);
 #pragma unroll
-      for (int j = 0; j < N / 2; ++j) {
-        float h0, h1;
-        unpack2(mul2(fma2(Vec<X>::pair(u[i], j), scale2, minus), l2e2), h0, h1);
-        const f2 q = pack2(exp2_fast(min_nan(h0, 0.0f)), exp2_fast(min_nan(h1, 0.0f)));
-        unpack2(mul2(q, mul2(q, other2)), d[2 * j], d[2 * j + 1]);
+      for (int i = 0; i < GRAD_U; ++i) {
+        const int64_t v = vs + i * GRAD_TPB;
+        if (v >= v1) break;
+        float d[N];
+#pragma unroll
+        for (int j = 0; j < N / 2; ++j) {
+          float h0, h1;
+          unpack2(mul2(fma2(Vec<X>::pair(u[i], j), scale2, minus), l2e2), h0, h1);
+          const f2 q = pack2(exp2_fast(min_nan(h0, 0.0f)), exp2_fast(min_nan(h1, 0.0f)));
+          unpack2(mul2(q, mul2(q, other2)), d[2 * j], d[2 * j + 1]);
+        }
+        __stcs(out + v, none ? make_uint4(0, 0, 0, 0) : pack_vec<X>(d));
       }
-      __stcs(out + v, none ? make_uint4(0, 0, 0, 0) : pack_vec<X>(d));
     }
     if (my_end) dx[end_col] = from_f<X>(one(end));
   } else {
     for (int64_t c = c0 + tid; c < c1; c += GRAD_TPB) dx[c] = from_f<X>(one(to_f(x[c])));
   }
   if (none) return;
-  // the listed tokens of this stretch, each by the thread of its first entry
+  // the CTA's listed tokens, each by the thread of its first entry
   bool mine = false;
   for (int j = tid; j < a.h.k; j += GRAD_TPB) mine |= here(list.col[j]);
   if (!__syncthreads_or(mine)) return;
@@ -422,13 +431,17 @@ int mv_distill_grad(void* stream, const void* logits, int type, int64_t T, int64
   a.V = V; a.ld = ld; a.ldg = ldg; a.h = {top_logprob, top_id, id_type, k, log_rest ? 1 : 0}; a.scale = scale; a.lse = lse; a.log_rest = log_rest; a.g = g;
   return with_type(type, [&](auto x) {
     using X = decltype(x);
+    // The list costs a CTA a few microseconds of latency: as many stretches for each as leave enough CTAs to fill the device.
     const int64_t per = int64_t(GRAD_TPB) * GRAD_U * Vec<X>::N, stretches = (V + per - 1) / per;
-    if (T * stretches >= lim) return int(MV_ERR_INVALID_ARG);
-    a.stretches = unsigned(stretches);
+    int64_t each = T * stretches / GRAD_CTAS;
+    each = each < 1 ? 1 : each > GRAD_MOST ? GRAD_MOST : each;
+    a.stretches = int(each);
+    a.ctas = unsigned((stretches + each - 1) / each);
+    if (T * a.ctas >= lim) return int(MV_ERR_INVALID_ARG);
     // a gradient that lies otherwise within 16 bytes than the logits, in some row, is written one by one
     const bool vec = ((reinterpret_cast<uintptr_t>(logits) ^ reinterpret_cast<uintptr_t>(dlogits)) & 15) == 0 && (T == 1 || (ld - ldg) * int64_t(sizeof(X)) % 16 == 0);
     auto* kernel = vec ? k_distill_grad<X, true> : k_distill_grad<X, false>;
-    kernel<<<unsigned(T * stretches), GRAD_TPB, size_t(k) * LIST_BYTES, static_cast<cudaStream_t>(stream)>>>(static_cast<const X*>(logits), static_cast<X*>(dlogits), a);
+    kernel<<<unsigned(T * a.ctas), GRAD_TPB, size_t(k) * LIST_BYTES, static_cast<cudaStream_t>(stream)>>>(static_cast<const X*>(logits), static_cast<X*>(dlogits), a);
     return cuda_ok();
   });
 }

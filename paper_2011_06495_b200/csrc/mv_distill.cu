@@ -30,38 +30,6 @@ template <typename X, typename F> __device__ __forceinline__ void load_list(cons
   }
 }
 
-// What a row's alternatives add up to, in 64 bits (1 - sum q is a small difference).
-struct Mass {
-  double scale, rest, all;           // q = scale exp(a - shift), r, M = sum q + r
-  float shift;
-  bool any, bad;                     // an alternative; a NaN or +inf
-};
-
-// For every lane of a warp.
-__device__ __forceinline__ Mass mass_of_list(const List& l, int k, bool rest) {
-  const int lane = threadIdx.x & 31;
-  float m = -INFINITY;
-  bool any = false, bad = false;
-  for (int j = lane; j < k; j += 32) {
-    const float a = l.a[j];
-    any |= l.col[j] >= 0 && (rest || a != -INFINITY);
-    bad |= !(a < INFINITY);
-    m = fmaxf(m, a);
-  }
-  Mass s;
-  s.any = __any_sync(0xffffffffu, any);
-  s.bad = __any_sync(0xffffffffu, bad);
-  for (int o = 16; o; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
-  s.shift = rest || m == -INFINITY ? 0.0f : m;
-  double q = 0.0;
-  for (int j = lane; j < k; j += 32) q += exp(double(l.a[j]) - double(s.shift));
-  for (int o = 16; o; o >>= 1) q += __shfl_xor_sync(0xffffffffu, q, o);
-  s.scale = rest ? 1.0 : 1.0 / q;
-  s.rest = rest ? fmax(0.0, 1.0 - q) : 0.0;
-  s.all = rest ? q + s.rest : 1.0;
-  return s;
-}
-
 struct DistillArgs {
   int64_t V, ld;
   Teacher h;
@@ -244,21 +212,42 @@ __global__ void __launch_bounds__(TPB, 1024 / TPB) k_distill(const X* __restrict
     for (int o = 16; o; o >>= 1) own += __shfl_xor_sync(0xffffffffu, own, o);
     all += own;
   }
-  const Mass s = mass_of_list(list, a.h.k, REST);
-  const double ls = log(all), lr = log(double(sum)) - ls;
-  double kl = 0.0;
+  // With e_j = exp(a_j - shift): q_j = e_j / sum e without the rest (shift: the largest a_j), e_j with it (shift 0).  1 - sum q is a small
+  // difference, so these are in 64 bits.
+  const float ls = logf(float(all)), lr = logf(sum) - ls;
+  float m = -INFINITY;
+  bool any = false, bad = false;
   for (int j = lane; j < a.h.k; j += 32) {
-    if (list.a[j] == -INFINITY) continue;
-    const double d = double(list.a[j]) - double(s.shift), q = exp(d) * s.scale;
-    if (q > 0.0) kl += q * (d + log(s.scale) - (double(distance(list.x[j], zero, a.scale)) - ls));
+    const float v = list.a[j];
+    any |= list.col[j] >= 0 && (REST || v != -INFINITY);
+    bad |= !(v < INFINITY);
+    m = fmaxf(m, v);
   }
-  for (int o = 16; o; o >>= 1) kl += __shfl_xor_sync(0xffffffffu, kl, o);
+  for (int o = 16; o; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+  any = __any_sync(0xffffffffu, any);
+  bad = __any_sync(0xffffffffu, bad);
+  const double shift = REST || m == -INFINITY ? 0.0 : double(m);
+  double q = 0.0, kl = 0.0;
+  for (int j = lane; j < a.h.k; j += 32) {
+    const double d = double(list.a[j]) - shift, e = exp(d);
+    q += e;
+    if (e > 0.0) kl = fma(e, d - (double(distance(list.x[j], zero, a.scale)) - double(ls)), kl);
+  }
+  for (int o = 16; o; o >>= 1) {
+    q += __shfl_xor_sync(0xffffffffu, q, o);
+    kl += __shfl_xor_sync(0xffffffffu, kl, o);
+  }
   if (lane == 0) {
     const bool nan = isnan(all), empty = all == 0.0;
-    if (REST && s.any && s.rest > 0.0) kl += s.rest * (log(s.rest) - lr);
-    if (a.kl) a.kl[t] = !s.any ? 0.0f : nan || s.bad ? NAN : empty ? INFINITY : float(kl);
-    if (a.lse) a.lse[t] = nan ? NAN : empty ? -INFINITY : fmaf(a.scale, zero, float(ls));
-    if (a.log_rest) a.log_rest[t] = nan ? NAN : empty ? -INFINITY : float(lr);
+    if (!REST) {
+      kl = kl / q - log(q);
+    } else if (any && q < 1.0) {
+      const double rest = 1.0 - q;
+      kl += rest * (log(rest) - double(lr));
+    }
+    if (a.kl) a.kl[t] = !any ? 0.0f : nan || bad ? NAN : empty ? INFINITY : float(kl);
+    if (a.lse) a.lse[t] = nan ? NAN : empty ? -INFINITY : fmaf(a.scale, zero, ls);
+    if (a.log_rest) a.log_rest[t] = nan ? NAN : empty ? -INFINITY : lr;
   }
 }
 
@@ -266,7 +255,7 @@ __global__ void __launch_bounds__(TPB, 1024 / TPB) k_distill(const X* __restrict
 // dx = f (M p - q) for a listed token, f M' p for the others, f = c g, M' = M - r / P.  p = q q with q = 2^h, h = log2(p) / 2: the
 // hardware's exponential has no subnormal results.  Each CTA takes some stretches of one row, and all of the row's list: the others' value is
 // written everywhere, and then its listed tokens' over it.
-constexpr int GRAD_TPB = 256, GRAD_U = 4, GRAD_MOST = 16, GRAD_CTAS = 148 * 8;
+constexpr int GRAD_U = 4, GRAD_MOST = 16;
 
 struct DistillGradArgs {
   int64_t V, ld, ldg;
@@ -278,22 +267,24 @@ struct DistillGradArgs {
 };
 
 // VEC: logits and gradient start at the same place within 16 bytes in every row.
-template <typename X, bool VEC>
-__global__ void __launch_bounds__(GRAD_TPB) k_distill_grad(const X* logits, X* dlogits, const __grid_constant__ DistillGradArgs a) {
-  constexpr int N = Vec<X>::N;
+template <typename X, bool VEC, int TPB>
+__global__ void __launch_bounds__(TPB) k_distill_grad(const X* logits, X* dlogits, const __grid_constant__ DistillGradArgs a) {
+  constexpr int N = Vec<X>::N, WARPS = TPB / 32, SEEN = 128;
   extern __shared__ uint32_t dynamic[];
-  __shared__ float s_f[3];
+  __shared__ float s_max[WARPS];
+  __shared__ double s_sum[WARPS];
+  __shared__ uint32_t s_seen[2][SEEN];
   const List list(dynamic, a.h.k);
   const int64_t t = blockIdx.x / a.ctas;
   const unsigned part = blockIdx.x % a.ctas;
-  const int tid = threadIdx.x;
+  const int tid = threadIdx.x, lane = tid & 31, w = tid >> 5;
   const X* x = logits + t * a.ld;
   X* dx = dlogits + t * a.ldg;
   // the vectors begin at the row's first 16-byte boundary; what is before and behind them goes to the first stretch
   const int64_t first = VEC ? min(a.V, int64_t((16 - (reinterpret_cast<uintptr_t>(x) & 15)) & 15) / int(sizeof(X))) : 0;
   const int64_t nv = VEC ? (a.V - first) / N : 0, behind = VEC ? first + nv * N : a.V, ends = VEC ? first + a.V - behind : 0;
-  const int64_t v0 = int64_t(part) * a.stretches * (GRAD_TPB * GRAD_U), v1 = VEC ? min(nv, v0 + a.stretches * (GRAD_TPB * GRAD_U)) : 0;      // its vectors
-  const int64_t c0 = first + v0 * N, c1 = min(behind, c0 + a.stretches * (GRAD_TPB * GRAD_U * N));                                            // and columns
+  const int64_t v0 = int64_t(part) * a.stretches * (TPB * GRAD_U), v1 = VEC ? min(nv, v0 + a.stretches * (TPB * GRAD_U)) : 0;      // its vectors
+  const int64_t c0 = first + v0 * N, c1 = min(behind, c0 + a.stretches * (TPB * GRAD_U * N));                                            // and columns
   const uint4* in = reinterpret_cast<const uint4*>(x + first);
   uint4* out = reinterpret_cast<uint4*>(dx + first);
   const bool my_end = VEC && part == 0 && tid < ends;
@@ -302,7 +293,7 @@ __global__ void __launch_bounds__(GRAD_TPB) k_distill_grad(const X* logits, X* d
   auto load = [&](int64_t v) {
 #pragma unroll
     for (int i = 0; i < GRAD_U; ++i)
-      if (v + i * GRAD_TPB < v1) next[i] = __ldcs(in + v + i * GRAD_TPB);
+      if (v + i * TPB < v1) next[i] = __ldcs(in + v + i * TPB);
   };
   float end = 0.0f;
   if constexpr (VEC) {
@@ -310,24 +301,48 @@ __global__ void __launch_bounds__(GRAD_TPB) k_distill_grad(const X* logits, X* d
     if (my_end) end = to_f(x[end_col]);
   }
   auto here = [&](int64_t c) { return (c >= c0 && c < c1) || (VEC && part == 0 && c >= 0 && (c < first || c >= behind)); };      // the CTA's columns
+  for (int i = tid; i < 2 * SEEN; i += TPB) s_seen[i / SEEN][i % SEEN] = 0;
   load_list(a.h, t, a.V, x, list, here);
-  const float l = a.lse[t];
-  __syncthreads();
-  if (tid < 32) {
-    const Mass s = mass_of_list(list, a.h.k, a.h.rest);
-    const float g = a.g[t];
-    if (tid == 0) {
-      double ratio = 0.0;
-      if (a.h.rest && s.rest > 0.0) ratio = a.log_rest[t] == -INFINITY ? s.all : exp(log(s.rest) - double(a.log_rest[t]));
-      s_f[0] = !s.any || g == 0.0f || l == -INFINITY ? 0.0f : a.scale * g;
-      s_f[1] = s.bad ? NAN : float(s.all);
-      s_f[2] = s.bad ? NAN : float(s.all - ratio);
-    }
-    for (int j = tid; j < a.h.k; j += 32) list.a[j] = float(exp(double(list.a[j]) - double(s.shift)) * s.scale);          // q
+  const float l = a.lse[t], g = a.g[t], lr = a.h.rest ? a.log_rest[t] : 0.0f;
+  // e_j as in the forward pass, in the place of a_j; their sum in 64 bits
+  float m = -INFINITY;
+  bool any = false, bad = false;
+  for (int j = tid; j < a.h.k; j += TPB) {
+    const float v = list.a[j];
+    any |= list.col[j] >= 0 && (a.h.rest || v != -INFINITY);
+    bad |= !(v < INFINITY);
+    m = fmaxf(m, v);
   }
+  any = __syncthreads_or(any);
+  bad = __syncthreads_or(bad);
+  if (!a.h.rest) {
+    for (int o = 16; o; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+    if (lane == 0) s_max[w] = m;
+    __syncthreads();
+    for (int i = 0; i < WARPS; ++i) m = fmaxf(m, s_max[i]);
+  }
+  const double shift = a.h.rest || m == -INFINITY ? 0.0 : double(m);
+  double sum = 0.0;
+  for (int j = tid; j < a.h.k; j += TPB) {
+    const double e = exp(double(list.a[j]) - shift);
+    sum += e;
+    list.a[j] = float(e);
+    const int c = list.col[j];
+    if (here(c)) {                   // its place among SEEN * 32: taken once, or more than once
+      const uint32_t bit = 1u << (c & 31);
+      if (atomicOr(&s_seen[0][c / 32 % SEEN], bit) & bit) atomicOr(&s_seen[1][c / 32 % SEEN], bit);
+    }
+  }
+  for (int o = 16; o; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+  if (lane == 0) s_sum[w] = sum;
   __syncthreads();
-  const float f = s_f[0], other = f * s_f[2], l2e = 0.5f * LOG2E;
-  const bool none = f == 0.0f;
+  sum = 0.0;
+  for (int i = 0; i < WARPS; ++i) sum += s_sum[i];
+  const double r = a.h.rest ? fmax(0.0, 1.0 - sum) : 0.0;
+  const float all = bad ? NAN : a.h.rest ? float(sum + r) : 1.0f, unit = a.h.rest ? 1.0f : float(1.0 / sum);
+  const float ratio = r == 0.0 ? 0.0f : lr == -INFINITY ? all : expf(logf(float(r)) - lr);
+  const bool none = !any || g == 0.0f || l == -INFINITY || a.scale * g == 0.0f;
+  const float f = none ? 0.0f : a.scale * g, other = f * (all - ratio), l2e = 0.5f * LOG2E;
   auto share = [&](float v) {                  // p / q; the same operations as two logits at a time below
     return exp2_fast(min_nan(fmaf(v, a.scale, -l) * l2e, 0.0f));
   };
@@ -337,13 +352,13 @@ __global__ void __launch_bounds__(GRAD_TPB) k_distill_grad(const X* logits, X* d
   };
   if constexpr (VEC) {
     const f2 scale2 = pack2(a.scale, a.scale), minus = pack2(-l, -l), l2e2 = pack2(l2e, l2e), other2 = pack2(other, other);
-    for (int64_t vs = v0 + tid; vs < v1; vs += GRAD_TPB * GRAD_U) {
+    for (int64_t vs = v0 + tid; vs < v1; vs += TPB * GRAD_U) {
 #pragma unroll
       for (int i = 0; i < GRAD_U; ++i) u[i] = next[i];
-      load(vs + GRAD_TPB * GRAD_U);
+      load(vs + TPB * GRAD_U);
 #pragma unroll
       for (int i = 0; i < GRAD_U; ++i) {
-        const int64_t v = vs + i * GRAD_TPB;
+        const int64_t v = vs + i * TPB;
         if (v >= v1) break;
         float d[N];
 #pragma unroll
@@ -358,25 +373,28 @@ __global__ void __launch_bounds__(GRAD_TPB) k_distill_grad(const X* logits, X* d
     }
     if (my_end) dx[end_col] = from_f<X>(one(end));
   } else {
-    for (int64_t c = c0 + tid; c < c1; c += GRAD_TPB) dx[c] = from_f<X>(one(to_f(x[c])));
+    for (int64_t c = c0 + tid; c < c1; c += TPB) dx[c] = from_f<X>(one(to_f(x[c])));
   }
   if (none) return;
   // the CTA's listed tokens, each by the thread of its first entry
   bool mine = false;
-  for (int j = tid; j < a.h.k; j += GRAD_TPB) mine |= here(list.col[j]);
+  for (int j = tid; j < a.h.k; j += TPB) mine |= here(list.col[j]);
   if (!__syncthreads_or(mine)) return;
-  for (int j = tid; j < a.h.k; j += GRAD_TPB) {
+  for (int j = tid; j < a.h.k; j += TPB) {
     const int c = list.col[j];
     if (!here(c)) continue;
-    float q = 0.0f;
+    float q = list.a[j];
     bool head = true;
-    for (int i = 0; i < a.h.k; ++i)
-      if (list.col[i] == c) {
-        head &= i >= j;
-        q += list.a[i];
-      }
+    if (s_seen[1][c / 32 % SEEN] >> (c & 31) & 1u) {
+      q = 0.0f;
+      for (int i = 0; i < a.h.k; ++i)
+        if (list.col[i] == c) {
+          head &= i >= j;
+          q += list.a[i];
+        }
+    }
     const float p = share(list.x[j]);
-    if (head) dx[c] = from_f<X>(f * fmaf(s_f[1] * p, p, -q));
+    if (head) dx[c] = from_f<X>(f * fmaf(all * p, p, -q * unit));
   }
 }
 
@@ -432,16 +450,17 @@ int mv_distill_grad(void* stream, const void* logits, int type, int64_t T, int64
   return with_type(type, [&](auto x) {
     using X = decltype(x);
     // The list costs a CTA a few microseconds of latency: as many stretches for each as leave enough CTAs to fill the device.
-    const int64_t per = int64_t(GRAD_TPB) * GRAD_U * Vec<X>::N, stretches = (V + per - 1) / per;
-    int64_t each = T * stretches / GRAD_CTAS;
+    const int tpb = V * size <= 16384 ? 64 : 256;
+    const int64_t per = int64_t(tpb) * GRAD_U * Vec<X>::N, stretches = (V + per - 1) / per;
+    int64_t each = T * stretches / (148 * 2048 / tpb);
     each = each < 1 ? 1 : each > GRAD_MOST ? GRAD_MOST : each;
     a.stretches = int(each);
     a.ctas = unsigned((stretches + each - 1) / each);
     if (T * a.ctas >= lim) return int(MV_ERR_INVALID_ARG);
     // a gradient that lies otherwise within 16 bytes than the logits, in some row, is written one by one
     const bool vec = ((reinterpret_cast<uintptr_t>(logits) ^ reinterpret_cast<uintptr_t>(dlogits)) & 15) == 0 && (T == 1 || (ld - ldg) * int64_t(sizeof(X)) % 16 == 0);
-    auto* kernel = vec ? k_distill_grad<X, true> : k_distill_grad<X, false>;
-    kernel<<<unsigned(T * a.ctas), GRAD_TPB, size_t(k) * LIST_BYTES, static_cast<cudaStream_t>(stream)>>>(static_cast<const X*>(logits), static_cast<X*>(dlogits), a);
+    auto* kernel = tpb == 64 ? (vec ? k_distill_grad<X, true, 64> : k_distill_grad<X, false, 64>) : vec ? k_distill_grad<X, true, 256> : k_distill_grad<X, false, 256>;
+    kernel<<<unsigned(T * a.ctas), unsigned(tpb), size_t(k) * LIST_BYTES, static_cast<cudaStream_t>(stream)>>>(static_cast<const X*>(logits), static_cast<X*>(dlogits), a);
     return cuda_ok();
   });
 }

@@ -266,8 +266,9 @@ struct DistillGradArgs {
   const float *lse, *log_rest, *g;
 };
 
-// VEC: logits and gradient start at the same place within 16 bytes in every row.
-template <typename X, bool VEC, int TPB>
+// APART: logits and gradient do not start at the same place within 16 bytes in every row; then the vectors are the gradient's, and the logits
+// come from between two of theirs.
+template <typename X, bool APART, int TPB>
 __global__ void __launch_bounds__(TPB) k_distill_grad(const X* logits, X* dlogits, const __grid_constant__ DistillGradArgs a) {
   constexpr int N = Vec<X>::N, WARPS = TPB / 32, SEEN = 128;
   extern __shared__ uint32_t dynamic[];
@@ -280,27 +281,33 @@ __global__ void __launch_bounds__(TPB) k_distill_grad(const X* logits, X* dlogit
   const int tid = threadIdx.x, lane = tid & 31, w = tid >> 5;
   const X* x = logits + t * a.ld;
   X* dx = dlogits + t * a.ldg;
-  // the vectors begin at the row's first 16-byte boundary; what is before and behind them goes to the first stretch
-  const int64_t first = VEC ? min(a.V, int64_t((16 - (reinterpret_cast<uintptr_t>(x) & 15)) & 15) / int(sizeof(X))) : 0;
-  const int64_t nv = VEC ? (a.V - first) / N : 0, behind = VEC ? first + nv * N : a.V, ends = VEC ? first + a.V - behind : 0;
-  const int64_t v0 = int64_t(part) * a.stretches * (TPB * GRAD_U), v1 = VEC ? min(nv, v0 + a.stretches * (TPB * GRAD_U)) : 0;      // its vectors
+  // the vectors begin at a 16-byte boundary of the gradient's row; what is before and behind them goes to the first stretch
+  int64_t first = min(a.V, int64_t((16 - (reinterpret_cast<uintptr_t>(dx) & 15)) & 15) / int(sizeof(X)));
+  const int shift = APART ? int(reinterpret_cast<uintptr_t>(x + first) & 15) : 0;       // where in a vector of the logits
+  if (shift > first * int(sizeof(X))) first = min(a.V, first + N);                       // all of the two vectors' bytes are the row's
+  const int64_t nv = max(int64_t(0), (a.V - first - (APART ? N - shift / int(sizeof(X)) : 0)) / N), behind = first + nv * N, ends = first + a.V - behind;
+  const int64_t v0 = int64_t(part) * a.stretches * (TPB * GRAD_U), v1 = min(nv, v0 + a.stretches * (TPB * GRAD_U));      // its vectors
   const int64_t c0 = first + v0 * N, c1 = min(behind, c0 + a.stretches * (TPB * GRAD_U * N));                                            // and columns
-  const uint4* in = reinterpret_cast<const uint4*>(x + first);
+  const uint4* in = reinterpret_cast<const uint4*>(reinterpret_cast<uintptr_t>(x + first) - shift);
   uint4* out = reinterpret_cast<uint4*>(dx + first);
-  const bool my_end = VEC && part == 0 && tid < ends;
+  const bool my_end = part == 0 && tid < ends;
   const int64_t end_col = tid < first ? tid : behind + tid - first;
-  uint4 u[GRAD_U], next[GRAD_U];
+  uint4 u[GRAD_U], next[GRAD_U], more[APART ? GRAD_U : 1];
   auto load = [&](int64_t v) {
 #pragma unroll
     for (int i = 0; i < GRAD_U; ++i)
-      if (v + i * TPB < v1) next[i] = __ldcs(in + v + i * TPB);
+      if (v + i * TPB < v1) {
+        if constexpr (APART) {
+          next[i] = __ldg(in + v + i * TPB);
+          more[i] = __ldg(in + v + i * TPB + 1);
+        } else {
+          next[i] = __ldcs(in + v + i * TPB);
+        }
+      }
   };
-  float end = 0.0f;
-  if constexpr (VEC) {
-    load(v0 + tid);
-    if (my_end) end = to_f(x[end_col]);
-  }
-  auto here = [&](int64_t c) { return (c >= c0 && c < c1) || (VEC && part == 0 && c >= 0 && (c < first || c >= behind)); };      // the CTA's columns
+  load(v0 + tid);
+  const float end = my_end ? to_f(x[end_col]) : 0.0f;
+  auto here = [&](int64_t c) { return (c >= c0 && c < c1) || (part == 0 && c >= 0 && (c < first || c >= behind)); };      // the CTA's columns
   for (int i = tid; i < 2 * SEEN; i += TPB) s_seen[i / SEEN][i % SEEN] = 0;
   load_list(a.h, t, a.V, x, list, here);
   const float l = a.lse[t], g = a.g[t], lr = a.h.rest ? a.log_rest[t] : 0.0f;
@@ -321,10 +328,10 @@ __global__ void __launch_bounds__(TPB) k_distill_grad(const X* logits, X* dlogit
     __syncthreads();
     for (int i = 0; i < WARPS; ++i) m = fmaxf(m, s_max[i]);
   }
-  const double shift = a.h.rest || m == -INFINITY ? 0.0 : double(m);
+  const double base = a.h.rest || m == -INFINITY ? 0.0 : double(m);
   double sum = 0.0;
   for (int j = tid; j < a.h.k; j += TPB) {
-    const double e = exp(double(list.a[j]) - shift);
+    const double e = exp(double(list.a[j]) - base);
     sum += e;
     list.a[j] = float(e);
     const int c = list.col[j];
@@ -350,31 +357,30 @@ __global__ void __launch_bounds__(TPB) k_distill_grad(const X* logits, X* dlogit
     const float q = share(v);
     return none ? 0.0f : q * (q * other);
   };
-  if constexpr (VEC) {
-    const f2 scale2 = pack2(a.scale, a.scale), minus = pack2(-l, -l), l2e2 = pack2(l2e, l2e), other2 = pack2(other, other);
-    for (int64_t vs = v0 + tid; vs < v1; vs += TPB * GRAD_U) {
+  const f2 scale2 = pack2(a.scale, a.scale), minus = pack2(-l, -l), l2e2 = pack2(l2e, l2e), other2 = pack2(other, other);
+  for (int64_t vs = v0 + tid; vs < v1; vs += TPB * GRAD_U) {
 #pragma unroll
-      for (int i = 0; i < GRAD_U; ++i) u[i] = next[i];
-      load(vs + TPB * GRAD_U);
-#pragma unroll
-      for (int i = 0; i < GRAD_U; ++i) {
-        const int64_t v = vs + i * TPB;
-        if (v >= v1) break;
-        float d[N];
-#pragma unroll
-        for (int j = 0; j < N / 2; ++j) {
-          float h0, h1;
-          unpack2(mul2(fma2(Vec<X>::pair(u[i], j), scale2, minus), l2e2), h0, h1);
-          const f2 q = pack2(exp2_fast(min_nan(h0, 0.0f)), exp2_fast(min_nan(h1, 0.0f)));
-          unpack2(mul2(q, mul2(q, other2)), d[2 * j], d[2 * j + 1]);
-        }
-        __stcs(out + v, none ? make_uint4(0, 0, 0, 0) : pack_vec<X>(d));
-      }
+    for (int i = 0; i < GRAD_U; ++i) {
+      if constexpr (APART) u[i] = between(next[i], more[i], shift);
+      else u[i] = next[i];
     }
-    if (my_end) dx[end_col] = from_f<X>(one(end));
-  } else {
-    for (int64_t c = c0 + tid; c < c1; c += TPB) dx[c] = from_f<X>(one(to_f(x[c])));
+    load(vs + TPB * GRAD_U);
+#pragma unroll
+    for (int i = 0; i < GRAD_U; ++i) {
+      const int64_t v = vs + i * TPB;
+      if (v >= v1) break;
+      float d[N];
+#pragma unroll
+      for (int j = 0; j < N / 2; ++j) {
+        float h0, h1;
+        unpack2(mul2(fma2(Vec<X>::pair(u[i], j), scale2, minus), l2e2), h0, h1);
+        const f2 q = pack2(exp2_fast(min_nan(h0, 0.0f)), exp2_fast(min_nan(h1, 0.0f)));
+        unpack2(mul2(q, mul2(q, other2)), d[2 * j], d[2 * j + 1]);
+      }
+      __stcs(out + v, none ? make_uint4(0, 0, 0, 0) : pack_vec<X>(d));
+    }
   }
+  if (my_end) dx[end_col] = from_f<X>(one(end));
   if (none) return;
   // the CTA's listed tokens, each by the thread of its first entry
   bool mine = false;
@@ -457,9 +463,8 @@ int mv_distill_grad(void* stream, const void* logits, int type, int64_t T, int64
     a.stretches = int(each);
     a.ctas = unsigned((stretches + each - 1) / each);
     if (T * a.ctas >= lim) return int(MV_ERR_INVALID_ARG);
-    // a gradient that lies otherwise within 16 bytes than the logits, in some row, is written one by one
     const bool vec = ((reinterpret_cast<uintptr_t>(logits) ^ reinterpret_cast<uintptr_t>(dlogits)) & 15) == 0 && (T == 1 || (ld - ldg) * int64_t(sizeof(X)) % 16 == 0);
-    auto* kernel = tpb == 64 ? (vec ? k_distill_grad<X, true, 64> : k_distill_grad<X, false, 64>) : vec ? k_distill_grad<X, true, 256> : k_distill_grad<X, false, 256>;
+    auto* kernel = tpb == 64 ? (vec ? k_distill_grad<X, false, 64> : k_distill_grad<X, true, 64>) : vec ? k_distill_grad<X, false, 256> : k_distill_grad<X, true, 256>;
     kernel<<<unsigned(T * a.ctas), unsigned(tpb), size_t(k) * LIST_BYTES, static_cast<cudaStream_t>(stream)>>>(static_cast<const X*>(logits), static_cast<X*>(dlogits), a);
     return cuda_ok();
   });

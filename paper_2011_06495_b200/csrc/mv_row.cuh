@@ -119,6 +119,15 @@ template <> struct Vec<__half> {
   }
 };
 
+// 16 bytes that begin `shift` bytes (even, below 16) into two neighbouring vectors.
+__device__ __forceinline__ uint4 between(const uint4& lo, const uint4& hi, int shift) {
+  const bool two = shift & 8, one = shift & 4;
+  const int bits = shift % 4 * 8;
+  const uint32_t a0 = two ? lo.z : lo.x, a1 = two ? lo.w : lo.y, a2 = two ? hi.x : lo.z, a3 = two ? hi.y : lo.w, a4 = two ? hi.z : hi.x, a5 = two ? hi.w : hi.y;
+  const uint32_t b0 = one ? a1 : a0, b1 = one ? a2 : a1, b2 = one ? a3 : a2, b3 = one ? a4 : a3, b4 = one ? a5 : a4;
+  return make_uint4(__funnelshift_r(b0, b1, bits), __funnelshift_r(b1, b2, bits), __funnelshift_r(b2, b3, bits), __funnelshift_r(b3, b4, bits));
+}
+
 // 32 bytes at a multiple of 32: a whole sector.
 __device__ __forceinline__ void load_stream(const uint4* p, uint4& a, uint4& b) {
   asm volatile("ld.global.nc.L1::no_allocate.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"

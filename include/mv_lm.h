@@ -145,7 +145,8 @@ int mv_distill_grad(void* stream, const void* logits, int type, int64_t T, int64
  * ascending index, are cut to the first top_k, those to the shortest start whose sum is at least top_p times theirs, those to w_v >=
  * min_p; the first always stays.  token[t] is the first index at which the sum of the kept w, in ascending order of the index, exceeds u[t] times their
  * sum, and logprob[t] the log of its share of that sum.  Weights are formed in 64 bits and added as whole multiples of n / 2^61 of the largest,
- * n the smallest power of two that is not below V: a token with less than half of that (3e-14 for V = 10^5) is never drawn.
+ * n the smallest power of two that is not below V and at least 1024: a token with less than half of that (3e-14 for V = 10^5) is
+ * never drawn.
  *   logits [T, V] type in, rows ld >= V apart;  u [T] float in, in [0, 1) (below: 0; from 1 on: the last kept token that has a weight)
  *   scale, top_p, min_p [T] float in, top_k [T] int32 in, on the device, each may be NULL: 1, 1 (all), 0 (all), 0 (all).
  *           scale > 0, an inverse temperature; top_k <= 0 or >= V, top_p >= 1, min_p <= 0: nothing is cut

@@ -18,22 +18,66 @@ struct SampleArgs {
   void* token;
   int id_type;
   float* logprob;
+  int steps;                         // steps of U vectors per group
+  int chunks;                        // chunks of the row, its ends included; 0: too many for the fast paths
 };
 
-// The order of the logits as that of 32-bit numbers: larger is earlier; +0 and -0 are one value.
-__device__ __forceinline__ uint32_t order_of(float x) {
-  const uint32_t b = __float_as_uint(x + 0.0f);
-  return b & 0x80000000u ? ~b : b | 0x80000000u;
-}
-__device__ __forceinline__ float value_of(uint32_t h) { return __uint_as_float(h & 0x80000000u ? h & 0x7fffffffu : ~h); }
+// The order of the logits as that of 32-bit numbers: larger is earlier; +0 and -0 are one value.  A key is an order and, below it, the
+// index, lower ones first.
+__device__ __forceinline__ uint32_t order_of(float x) { return uint32_t(make_key(x, 0) >> 32); }
+__device__ __forceinline__ float value_of(uint32_t h) { return key_value(u64(h) << 32); }
 
-constexpr int TPB = 256, WARPS = TPB / 32, BINS = 2048, CHUNKS = 2048;
+constexpr int TPB = 256, WARPS = TPB / 32, U = 4;
+constexpr int LIST = 1024;           // candidates
+constexpr int CHUNKS = 2048;         // sums over neighbouring tokens
+constexpr int CHUNK_VECS = 64;       // vectors of each, one warp's
+constexpr int GROUPS = 32;           // groups per thread whose maxima are kept
+constexpr int COARSE = 512, FINE = 4096;       // bins over 2^-32 .. 1 of the largest weight: 1/16 and 1/128 of a power of two wide
+constexpr int SLOW_BINS = 2048;
 
-// A row's weights: of a logit, in 64 bits and as a whole number.
+// What one path or the other keeps in shared memory.
+struct Smem {
+  union {
+    float gmax[GROUPS][TPB];         // the groups' maxima
+    struct {
+      uint32_t bin[FINE];
+      u64 chunk[CHUNKS];
+    } fast;
+    struct {
+      u64 bin[SLOW_BINS];
+      u64 chunk[CHUNKS];
+    } slow;
+  };
+  uint32_t coarse[COARSE];
+  u64 key[LIST], sorted[LIST], sum[LIST];
+  uint16_t group[LIST];
+  double table[32];                  // 2^(j/32)
+  u64 warp[WARPS];
+  double warp_d[WARPS];
+  float max[WARPS], part_max;
+  int n_key, n_group, first_bin, last_bin;
+  u64 found, before, total, certain;
+};
+
+// A row's weights 2^t, t = (x - m) c log2(e) <= 0, in 64 bits and as whole numbers.  2^t = 2^(i/32) 2^f with |f| <= 1/64: a table and the
+// exponential series to the fifth power (the sixth is below 2.3e-15).
 struct Weights {
-  double c, m, unit;
-  __device__ double of(float x) const { return exp((double(x) - m) * c); }
-  __device__ u64 whole(float x) const { return u64(of(x) * unit + 0.5); }
+  double m, c2, unit;
+  const double* table;
+  int lift;                          // log2(unit), in the place of a double's exponent
+  // 2^52 and the whole number, as a double
+  __device__ __forceinline__ double lifted(float x) const {
+    const double t0 = (double(x) - m) * c2;
+    // below 2^-80: as 2^-80, which is nothing
+    const double t = __hiloint2double(int(min(uint32_t(__double2hiint(t0)), 0xC0540000u)), __double2loint(t0));
+    constexpr double MAGIC = 6755399441055744.0 / 32.0;                                  // 1.5 2^52 / 32: its last bit is 1/32
+    const double r = t + MAGIC, f = t - (r - MAGIC);
+    const int i = __double2loint(r);
+    constexpr double L = 0.6931471805599453;
+    const double p = fma(fma(fma(fma(fma(L * L * L * L * L / 120, f, L * L * L * L / 24), f, L * L * L / 6), f, L * L / 2), f, L), f, 1.0) * table[i & 31];
+    return fma(p, __hiloint2double(((i >> 5) << 20) + lift, 0), 4503599627370496.0);
+  }
+  __device__ __forceinline__ u64 whole(float x) const { return u64(__double_as_longlong(lifted(x))) - 0x4330000000000000ull; }
 };
 
 // The largest whole number not above u all, u in [0, 1), exactly.
@@ -46,17 +90,7 @@ __device__ __forceinline__ u64 share_of(float u, u64 all) {
   return down < 64 ? hi << (64 - down) | lo >> down : down < 128 ? hi >> (down - 64) : 0;
 }
 
-struct Cut { uint32_t order; int64_t ties, all; };       // kept: larger orders, and the first `ties` of the `all` tokens of this order
-
-struct Smem {
-  u64 bin[BINS];
-  u64 warp[WARPS];
-  u64 found, before;
-  int bin_found;
-  float max[WARPS];
-};
-
-// The sum of v over the threads before this one (after: of all threads in `all`).
+// The sum of v over the threads before this one, and over all of them.
 __device__ __forceinline__ u64 scan_before(u64 v, Smem& s, u64& all) {
   const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
   u64 incl = v;
@@ -75,46 +109,99 @@ __device__ __forceinline__ u64 scan_before(u64 v, Smem& s, u64& all) {
   }
   return at;
 }
+__device__ __forceinline__ double scan_before(double v, Smem& s, double& all) {
+  const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
+  double incl = v;
+  for (int o = 1; o < 32; o <<= 1) {
+    const double y = __shfl_up_sync(0xffffffffu, incl, o);
+    if (lane >= o) incl += y;
+  }
+  __syncthreads();
+  if (lane == 31) s.warp_d[w] = incl;
+  __syncthreads();
+  double at = incl - v;
+  all = 0.0;
+  for (int i = 0; i < WARPS; ++i) {
+    at += i < w ? s.warp_d[i] : 0.0;
+    all += s.warp_d[i];
+  }
+  return at;
+}
+
+// What a row's request asks for.
+struct Request {
+  float u, scale, p, mp;
+  int64_t k;
+  bool valid;
+};
+__device__ __forceinline__ Request request_of(const SampleArgs& a, int64_t t) {
+  Request q;
+  q.u = a.u[t];
+  q.scale = a.scale ? a.scale[t] : 1.0f;
+  q.p = a.top_p ? a.top_p[t] : 1.0f;
+  q.mp = a.min_p ? a.min_p[t] : 0.0f;
+  q.k = a.top_k ? a.top_k[t] : 0;
+  q.valid = q.scale > 0.0f && q.scale < INFINITY && !isnan(q.p) && !isnan(q.mp) && !isnan(q.u);
+  if (q.p <= 0.0f || q.mp > 1.0f) q.k = 1;
+  q.mp = fminf(q.mp, 1.0f);
+  if (q.k <= 0 || q.k > a.V) q.k = a.V;
+  if (q.k == 1) q.p = 1.0f;
+  return q;
+}
+
+__device__ __forceinline__ void put_token(const SampleArgs& a, int64_t t, int64_t token, float logprob) {
+  if (a.id_type == MV_I32) static_cast<int32_t*>(a.token)[t] = int32_t(token);
+  else static_cast<int64_t*>(a.token)[t] = token;
+  if (a.logprob) a.logprob[t] = logprob;
+}
+__device__ __forceinline__ void put_drawn(const SampleArgs& a, int64_t t, int64_t token, float x, const Weights& wt, u64 all) {
+  put_token(a, t, token, float((double(x) - wt.m) * (wt.c2 * 0.6931471805599453) - log(double(all) / wt.unit)));
+}
+__device__ __forceinline__ u64 limit_of(float u, u64 all) { return u >= 1.0f ? all - 1 : u > 0.0f ? share_of(u, all) : 0; }      // the first token at which the sum is larger is drawn
+
+// ------------------------------------------------------------------------------------------ any row
+// Rows that the fast paths do not take: cuts by three readings each, over 11, 11 and 10 bits of the order.
+struct Cut { uint32_t order; int64_t ties, all; };       // kept: larger orders, and the first `ties` of the `all` tokens of this order
 
 // Cuts the tokens that `floor` keeps (all of them: null) to the shortest start, in descending order, that holds at least `target` (> 0)
-// of what `amount` gives to each; there is one.  Three steps over 11, 11 and 10 bits of the order.
+// of what `amount` gives to each; there is one.
 template <typename X, typename F>
-__device__ Cut cut_row(const X* row, int64_t V, u64 target, const Cut* floor, F&& amount, Smem& s) {
+__device__ __noinline__ Cut cut_row(const X* row, int64_t V, u64 target, const Cut* floor, F&& amount, Smem& s) {
   uint32_t prefix = 0;
   u64 before = 0;
   int shift = 32;
   for (int step = 0; step < 3; ++step) {
     const int bits = step < 2 ? 11 : 10, next = shift - bits;
     __syncthreads();
-    for (int i = threadIdx.x; i < BINS; i += TPB) s.bin[i] = 0;
+    for (int i = threadIdx.x; i < SLOW_BINS; i += TPB) s.slow.bin[i] = 0;
     __syncthreads();
     for (int64_t i = threadIdx.x; i < V; i += TPB) {
       const float x = to_f(row[i]);
       const uint32_t h = order_of(x);
       if ((shift == 32 || h >> shift == prefix) && (!floor || h >= floor->order)) {
         const u64 v = amount(x);
-        if (v) atomicAdd(&s.bin[(h >> next) & ((1u << bits) - 1)], v);
+        if (v) atomicAdd(&s.slow.bin[(h >> next) & ((1u << bits) - 1)], v);
       }
     }
     __syncthreads();
     if (floor && threadIdx.x == 0 && (shift == 32 || floor->order >> shift == prefix))   // the tokens of the floor's own order that it drops
-      s.bin[(floor->order >> next) & ((1u << bits) - 1)] -= amount(value_of(floor->order)) * u64(floor->all - floor->ties);
+      s.slow.bin[(floor->order >> next) & ((1u << bits) - 1)] -= amount(value_of(floor->order)) * u64(floor->all - floor->ties);
     __syncthreads();
     // bins in descending order, eight per thread
-    constexpr int PER = BINS / TPB;
+    constexpr int PER = SLOW_BINS / TPB;
     u64 mine = 0, all;
-    for (int j = 0; j < PER; ++j) mine += s.bin[BINS - 1 - (threadIdx.x * PER + j)];
+    for (int j = 0; j < PER; ++j) mine += s.slow.bin[SLOW_BINS - 1 - (threadIdx.x * PER + j)];
     u64 at = before + scan_before(mine, s, all);
     for (int j = 0; j < PER; ++j) {
-      const int b = BINS - 1 - (threadIdx.x * PER + j);
-      if (at < target && target <= at + s.bin[b]) {
-        s.bin_found = b;
+      const int b = SLOW_BINS - 1 - (threadIdx.x * PER + j);
+      if (at < target && target <= at + s.slow.bin[b]) {
+        s.first_bin = b;
         s.before = at;
       }
-      at += s.bin[b];
+      at += s.slow.bin[b];
     }
     __syncthreads();
-    prefix = prefix << bits | uint32_t(s.bin_found);
+    prefix = prefix << bits | uint32_t(s.first_bin);
     before = s.before;
     shift = next;
   }
@@ -128,42 +215,15 @@ __device__ Cut cut_row(const X* row, int64_t V, u64 target, const Cut* floor, F&
 }
 
 template <typename X>
-__global__ void __launch_bounds__(TPB) k_sample(const X* __restrict__ logits, const __grid_constant__ SampleArgs a) {
-  __shared__ Smem s;
-  __shared__ u64 s_chunk[CHUNKS];
-  __shared__ int64_t s_last;
-  const int64_t t = blockIdx.x;
-  const X* row = logits + t * a.ld;
+__device__ __noinline__ void sample_any(const X* row, const SampleArgs& a, int64_t t, const Request& q, const Weights& wt, Smem& s) {
   const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
-  auto finish = [&](int64_t token, float logprob) {
-    if (a.id_type == MV_I32) static_cast<int32_t*>(a.token)[t] = int32_t(token);
-    else static_cast<int64_t*>(a.token)[t] = token;
-    if (a.logprob) a.logprob[t] = logprob;
-  };
-  const float scale = a.scale ? a.scale[t] : 1.0f, u = a.u[t];
-  float p = a.top_p ? a.top_p[t] : 1.0f, mp = a.min_p ? a.min_p[t] : 0.0f;
-  int64_t k = a.top_k ? a.top_k[t] : 0;
-  float m = -INFINITY;
-  for (int64_t i = threadIdx.x; i < a.V; i += TPB) m = max_nan(m, to_f(row[i]));
-  for (int o = 16; o; o >>= 1) m = max_nan(m, __shfl_xor_sync(0xffffffffu, m, o));
-  if (lane == 0) s.max[w] = m;
-  __syncthreads();
-  for (int i = 0; i < WARPS; ++i) m = max_nan(m, s.max[i]);
-  if (!(m < INFINITY) || !(scale > 0.0f && scale < INFINITY) || isnan(p) || isnan(mp) || isnan(u) || m == -INFINITY) {
-    if (threadIdx.x == 0) finish(-1, m == -INFINITY && scale > 0.0f && scale < INFINITY && !isnan(p) && !isnan(mp) && !isnan(u) ? -INFINITY : NAN);
-    return;
-  }
-  if (p <= 0.0f || mp > 1.0f) k = 1;
-  mp = fminf(mp, 1.0f);
-  if (k <= 0 || k > a.V) k = a.V;
-  const Weights wt = {double(scale), double(m), a.unit};
   Cut cut = {0, 0, 0};               // all
   bool cuts = false;
-  if (k < a.V) {
-    cut = cut_row(row, a.V, u64(k), nullptr, [](float) { return u64(1); }, s);
+  if (q.k < a.V) {
+    cut = cut_row(row, a.V, u64(q.k), nullptr, [](float) { return u64(1); }, s);
     cuts = true;
   }
-  if (p < 1.0f && p > 0.0f) {
+  if (q.p < 1.0f) {
     u64 mine = 0, all;
     for (int64_t i = threadIdx.x; i < a.V; i += TPB) {
       const float x = to_f(row[i]);
@@ -171,7 +231,7 @@ __global__ void __launch_bounds__(TPB) k_sample(const X* __restrict__ logits, co
     }
     scan_before(mine, s, all);
     if (cuts) all += u64(cut.ties) * wt.whole(value_of(cut.order));
-    const u64 target = max(u64(1), u64(ceil(double(p) * double(all))));
+    const u64 target = max(u64(1), u64(ceil(double(q.p) * double(all))));
     cut = cut_row(row, a.V, target, cuts ? &cut : nullptr, [&](float x) { return wt.whole(x); }, s);
     cuts = true;
   }
@@ -184,19 +244,18 @@ __global__ void __launch_bounds__(TPB) k_sample(const X* __restrict__ logits, co
       const bool tie = i < a.V && order_of(to_f(row[i])) == cut.order;
       u64 all;
       const u64 at = found + scan_before(tie, s, all);
-      if (tie && at + 1 == u64(cut.ties)) s_last = i;
+      if (tie && at + 1 == u64(cut.ties)) s.found = u64(i);
       found += all;
       if (found >= u64(cut.ties)) break;
     }
     __syncthreads();
-    last = s_last;
+    last = int64_t(s.found);
   }
   auto kept = [&](int64_t i) {       // the weight of token i, 0 if it is cut
     const float x = to_f(row[i]);
     const uint32_t h = order_of(x);
     if (cuts && !(h > cut.order || (h == cut.order && i <= last))) return u64(0);
-    const double v = wt.of(x);
-    return v >= double(mp) ? u64(v * wt.unit + 0.5) : u64(0);
+    return exp((double(x) - wt.m) * double(q.scale)) >= double(q.mp) ? wt.whole(x) : u64(0);
   };
   const int64_t per = ((a.V + CHUNKS - 1) / CHUNKS + 31) / 32 * 32;
   __syncthreads();
@@ -204,18 +263,18 @@ __global__ void __launch_bounds__(TPB) k_sample(const X* __restrict__ logits, co
     u64 n = 0;
     for (int64_t i = c * per + lane; i < min(a.V, (c + 1) * per); i += 32) n += kept(i);
     for (int o = 16; o; o >>= 1) n += __shfl_xor_sync(0xffffffffu, n, o);
-    if (lane == 0) s_chunk[c] = n;
+    if (lane == 0) s.slow.chunk[c] = n;
   }
   __syncthreads();
   constexpr int PER = CHUNKS / TPB;
   u64 mine = 0, all;
-  for (int j = 0; j < PER; ++j) mine += s_chunk[threadIdx.x * PER + j];
+  for (int j = 0; j < PER; ++j) mine += s.slow.chunk[threadIdx.x * PER + j];
   u64 at = scan_before(mine, s, all);
-  const u64 limit = u >= 1.0f ? all - 1 : u > 0.0f ? share_of(u, all) : 0;       // the first token at which the sum is larger is drawn
+  const u64 limit = limit_of(q.u, all);
   for (int j = 0; j < PER; ++j) {
-    const u64 n = s_chunk[threadIdx.x * PER + j];
+    const u64 n = s.slow.chunk[threadIdx.x * PER + j];
     if (at <= limit && limit < at + n) {
-      s.bin_found = threadIdx.x * PER + j;
+      s.first_bin = threadIdx.x * PER + j;
       s.before = at;
     }
     at += n;
@@ -223,7 +282,7 @@ __global__ void __launch_bounds__(TPB) k_sample(const X* __restrict__ logits, co
   __syncthreads();
   if (w) return;
   u64 before = s.before;
-  for (int64_t i0 = s.bin_found * per; i0 < a.V; i0 += 32) {
+  for (int64_t i0 = int64_t(s.first_bin) * per; i0 < a.V; i0 += 32) {
     const int64_t i = i0 + lane;
     const u64 n = i < a.V ? kept(i) : 0;
     u64 incl = n;
@@ -233,7 +292,464 @@ __global__ void __launch_bounds__(TPB) k_sample(const X* __restrict__ logits, co
     }
     const unsigned hit = __ballot_sync(0xffffffffu, before + incl > limit);
     if (hit) {
-      if (lane == __ffs(int(hit)) - 1) finish(i, float((double(to_f(row[i])) - wt.m) * wt.c - log(double(all) / wt.unit)));
+      if (lane == __ffs(int(hit)) - 1) put_drawn(a, t, i, to_f(row[i]), wt, all);
+      return;
+    }
+    before += __shfl_sync(0xffffffffu, incl, 31);
+  }
+}
+
+// ------------------------------------------------------------------------------------------ fast paths
+template <typename X> __device__ __forceinline__ uint32_t max2_nan(uint32_t a, uint32_t b);
+template <> __device__ __forceinline__ uint32_t max2_nan<float>(uint32_t a, uint32_t b) { return __float_as_uint(max_nan(__uint_as_float(a), __uint_as_float(b))); }
+template <> __device__ __forceinline__ uint32_t max2_nan<__nv_bfloat16>(uint32_t a, uint32_t b) { return Vec<__nv_bfloat16>::max2_nan(a, b); }
+template <> __device__ __forceinline__ uint32_t max2_nan<__half>(uint32_t a, uint32_t b) {
+  uint32_t r;
+  asm("max.NaN.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+  return r;
+}
+template <typename X> __device__ __forceinline__ float widen_nan(uint32_t m) {
+  if constexpr (sizeof(X) == 4) {
+    return __uint_as_float(m);
+  } else {
+    float a, b;
+    unpack2(Vec<X>::pair(make_uint4(m, 0, 0, 0), 0), a, b);
+    return max_nan(a, b);
+  }
+}
+
+// The bin of a logit among `n`: 0 at the largest one, the last one for all that is 2^-32 of its weight or less.  Never falls as x falls.
+__device__ __forceinline__ int bin_of(float x, float m, float c, int n) { return int(fminf(distance(m, x, c), float(n - 1))); }
+
+template <typename X>
+__global__ void __launch_bounds__(TPB, 3) k_sample(const X* __restrict__ logits, const __grid_constant__ SampleArgs a) {
+  constexpr int N = Vec<X>::N;
+  extern __shared__ u64 dynamic[];
+  Smem& s = *reinterpret_cast<Smem*>(dynamic);
+  const cg::cluster_group cluster = cg::this_cluster();
+  const int ctas = int(cluster.num_blocks()), rank = int(cluster.block_rank());
+  const int tid = threadIdx.x, lane = tid & 31, w = tid >> 5;
+  const int64_t t = ctas == 1 ? blockIdx.x : blockIdx.x / unsigned(ctas);
+  const X* row = logits + t * a.ld;
+  const Request q = request_of(a, t);
+  // the vectors begin at the row's first 32-byte boundary; `per` of them for each CTA of the cluster
+  const int64_t to32 = int64_t((32 - (reinterpret_cast<uintptr_t>(row) & 31)) & 31) / int(sizeof(X));
+  const int first = int(min(a.V, to32)), all_v = (int(a.V) - first) / (2 * N) * 2;
+  const int per = ((all_v + ctas - 1) / ctas + CHUNK_VECS - 1) / CHUNK_VECS * CHUNK_VECS, v0 = min(all_v, rank * per), nv = min(all_v - v0, per);
+  const int tail_col = first + all_v * N, head = rank == 0 ? first : 0, tail = rank == ctas - 1 ? int(a.V) - tail_col : 0;
+  const uint4* vec = reinterpret_cast<const uint4*>(row + first) + v0;
+  const int col0 = first + v0 * N;
+  const int end_col = tid < head ? tid : tid - head < tail ? tail_col + tid - head : -1;      // a single logit of this thread
+  const float end = end_col >= 0 ? to_f(row[end_col]) : -INFINITY;
+  const uint4 none = make_uint4(Vec<X>::NONE, Vec<X>::NONE, Vec<X>::NONE, Vec<X>::NONE);
+  const int n_full = nv / (TPB * U), n_steps = (nv + TPB * U - 1) / (TPB * U);
+  auto load = [&](int step, uint4 (&u)[U]) {
+    const uint4* ptr = vec + step * (U * TPB) + 2 * tid;
+    if (step < n_full) {
+#pragma unroll
+      for (int i = 0; i < U; i += 2) load_stream(ptr + i * TPB, u[i], u[i + 1]);
+    } else {
+#pragma unroll
+      for (int i = 0; i < U; i += 2) {
+        u[i] = u[i + 1] = none;
+        if ((step * U + i) * TPB + 2 * tid < nv) load_stream(ptr + i * TPB, u[i], u[i + 1]);
+      }
+    }
+  };
+  auto stream = [&](auto&& f) {      // f(step, vectors), the next step's on their way
+    uint4 even[U], odd[U];
+    if (n_steps > 0) load(0, even);
+    for (int step = 0; step < n_steps; step += 2) {
+      if (step + 1 < n_steps) load(step + 1, odd);
+      f(step, even);
+      if (step + 1 >= n_steps) break;
+      if (step + 2 < n_steps) load(step + 2, even);
+      f(step + 1, odd);
+    }
+  };
+  auto column = [&](int step, int i) { return col0 + ((step * U + (i & ~1)) * TPB + 2 * tid + (i & 1)) * N; };      // of vector i of a step
+  auto all_sync = [&]() {
+    if (ctas > 1) cluster.sync();
+    else __syncthreads();
+  };
+  auto of_rank = [&](int r) -> const Smem& { return ctas > 1 ? *cluster.map_shared_rank(&s, unsigned(r)) : s; };
+  if (tid < 32) s.table[tid] = exp2(double(tid) / 32.0);
+
+  // the largest logit, and those of the groups where the top k are asked for
+  bool by_list = q.k <= LIST && q.k < a.V;
+  float m = end;
+  {
+    float g = -INFINITY;
+    int left = a.steps, group = 0;
+    stream([&](int, const uint4 (&u)[U]) {
+      uint32_t m2 = max2_nan<X>(max2_nan<X>(u[0].x, u[0].y), max2_nan<X>(u[0].z, u[0].w));
+#pragma unroll
+      for (int i = 1; i < U; ++i) m2 = max2_nan<X>(m2, max2_nan<X>(max2_nan<X>(u[i].x, u[i].y), max2_nan<X>(u[i].z, u[i].w)));
+      const float v = widen_nan<X>(m2);
+      m = max_nan(m, v);
+      if (by_list) {
+        g = max_nan(g, v);
+        if (--left == 0) {
+          s.gmax[group++][tid] = g;
+          g = -INFINITY;
+          left = a.steps;
+        }
+      }
+    });
+    if (by_list && left != a.steps) s.gmax[group][tid] = g;
+  }
+  const int groups = (n_steps + a.steps - 1) / a.steps;
+  for (int o = 16; o; o >>= 1) m = max_nan(m, __shfl_xor_sync(0xffffffffu, m, o));
+  if (lane == 0) s.max[w] = m;
+  for (int i = tid; i < COARSE; i += TPB) s.coarse[i] = 0;
+  if (tid == 0) { s.n_key = s.n_group = 0; }
+  __syncthreads();
+  for (int i = 0; i < WARPS; ++i) m = max_nan(m, s.max[i]);
+  if (ctas > 1) {
+    if (tid == 0) s.part_max = m;
+    cluster.sync();
+    for (int r = 0; r < ctas; ++r) m = max_nan(m, of_rank(r).part_max);
+  }
+  if (!(m < INFINITY) || !q.valid || m == -INFINITY) {
+    if (ctas > 1) cluster.sync();    // the parts' maxima have been read
+    if (rank == 0 && tid == 0) put_token(a, t, -1, q.valid && m == -INFINITY ? -INFINITY : NAN);
+    return;
+  }
+  Weights wt;
+  wt.m = double(m);
+  wt.c2 = double(q.scale) * 1.4426950408889634;
+  wt.unit = a.unit;
+  wt.table = s.table;
+  wt.lift = __double2hiint(a.unit);
+  const float c_coarse = fminf(q.scale * (LOG2E * 16.0f), 3.0e38f), c_fine = fminf(q.scale * (LOG2E * 128.0f), 3.0e38f);
+  auto push = [&](float x, int col) {
+    const int i = atomicAdd(&s.n_key, 1);
+    if (i < LIST) s.key[i] = make_key(x, uint32_t(col));
+  };
+
+  if (by_list) {
+    // the coarse bin b up to which k groups' maxima lie: so do k logits, and all of the top k
+    for (int g = 0; g < groups; ++g) atomicAdd(&s.coarse[bin_of(s.gmax[g][tid], m, c_coarse, COARSE)], 1u);
+    if (end_col >= 0) atomicAdd(&s.coarse[bin_of(end, m, c_coarse, COARSE)], 1u);
+    all_sync();
+    u64 c[2] = {0, 0}, all;
+    for (int r = 0; r < ctas; ++r) {
+      const Smem& o = of_rank(r);
+      c[0] += o.coarse[2 * tid];
+      c[1] += o.coarse[2 * tid + 1];
+    }
+    if (tid == 0) s.first_bin = COARSE;
+    const u64 at = scan_before(c[0] + c[1], s, all);
+    if (at < u64(q.k) && u64(q.k) <= at + c[0] + c[1]) s.first_bin = 2 * tid + (at + c[0] < u64(q.k));
+    __syncthreads();
+    int b = s.first_bin;
+    if (q.p >= 1.0f && q.mp > 0.0f) b = min(b, int(fminf(-log2f(q.mp) * 16.0f, 1.0e4f)) + 1);      // nothing beyond it is kept
+    by_list = b < COARSE - 1;
+    if (by_list) {
+      for (int g = 0; g < groups; ++g)
+        if (bin_of(s.gmax[g][tid], m, c_coarse, COARSE) <= b) {
+          const int i = atomicAdd(&s.n_group, 1);
+          if (i < LIST) s.group[i] = uint16_t(g * TPB + tid);
+        }
+      if (end_col >= 0 && bin_of(end, m, c_coarse, COARSE) <= b) push(end, end_col);
+      __syncthreads();
+      const int listed = s.n_group, vecs = a.steps * U;
+      if (listed <= LIST) {
+        for (int i = tid; i < listed * vecs; i += TPB) {
+          const int g = s.group[i / vecs], j = i % vecs, v = (g / TPB * vecs + (j & ~1)) * TPB + 2 * (g % TPB) + (j & 1);
+          if (v >= nv) continue;
+          const uint4 x = __ldg(vec + v);
+          each_logit<X>(x, [&](int e, float y) {
+            if (bin_of(y, m, c_coarse, COARSE) <= b) push(y, col0 + v * N + e);
+          });
+        }
+      } else if (tid == 0) {
+        s.n_key = LIST + 1;
+      }
+    }
+    all_sync();
+    int n = 0;
+    if (by_list)
+      for (int r = 0; r < ctas; ++r) n += of_rank(r).n_key;
+    by_list = by_list && n <= LIST;
+    if (by_list) {
+      if (rank == 0)
+        for (int r = 1, base = s.n_key; r < ctas; ++r) {
+          const Smem& o = of_rank(r);
+          for (int i = tid; i < o.n_key; i += TPB) s.key[base + i] = o.key[i];
+          base += o.n_key;
+        }
+      all_sync();
+      if (rank) return;
+      // sorted, summed up in descending order, cut, summed up by index
+      for (int i = tid; i < n; i += TPB) {
+        const u64 mine = s.key[i];
+        int place = 0;
+        for (int j = 0; j < n; ++j) place += s.key[j] > mine;
+        s.sorted[place] = mine;
+      }
+      __syncthreads();
+      constexpr int PER = LIST / TPB;
+      u64 v[PER], mine = 0, total;
+      const int kept_k = int(min(q.k, int64_t(n)));
+      for (int j = 0; j < PER; ++j) {
+        const int i = tid * PER + j;
+        v[j] = i < kept_k ? wt.whole(key_value(s.sorted[i])) : 0;
+        mine += v[j];
+      }
+      u64 before = scan_before(mine, s, total);
+      const u64 target = q.p < 1.0f ? max(u64(1), u64(ceil(double(q.p) * double(total)))) : ~0ull;
+      for (int j = 0; j < PER; ++j) {
+        const int i = tid * PER + j;
+        const bool in = i < kept_k && (i == 0 || before < target) && (i == 0 || q.mp <= 0.0f || exp((double(key_value(s.sorted[i])) - wt.m) * double(q.scale)) >= double(q.mp));
+        before += v[j];
+        if (!in) v[j] = 0;
+        if (i < n) s.sum[i] = v[j];
+      }
+      // places by index among all of the list; the cut ones weigh nothing
+      __syncthreads();
+      for (int i = tid; i < n; i += TPB) {
+        const uint32_t low = uint32_t(s.sorted[i]);          // larger: earlier
+        int place = 0;
+        for (int j = 0; j < n; ++j) place += uint32_t(s.sorted[j]) > low;
+        s.key[place] = u64(i);
+      }
+      __syncthreads();
+      mine = 0;
+      for (int j = 0; j < PER; ++j) {
+        const int i = tid * PER + j;
+        v[j] = i < n ? s.sum[s.key[i]] : 0;
+        mine += v[j];
+      }
+      before = scan_before(mine, s, total);
+      const u64 limit = limit_of(q.u, total);
+      for (int j = 0; j < PER; ++j) {
+        if (before <= limit && limit < before + v[j]) {
+          const u64 key = s.sorted[s.key[tid * PER + j]];
+          put_drawn(a, t, key_index(key), key_value(key), wt, total);
+        }
+        before += v[j];
+      }
+      return;
+    }
+    all_sync();                      // the lists' lengths have been read
+    if (tid == 0) s.n_key = 0;
+  }
+
+  // bins of all logits, where a cut is asked for: the bins [lo, hi] in which the last token of the start may lie
+  int lo = FINE, hi = FINE;          // nothing is cut
+  bool slow = a.chunks == 0;
+  const bool by_count = q.k < a.V, by_mass = q.p < 1.0f;
+  u64 count_before = 0;
+  if (by_count && by_mass) slow = true;
+  if (!slow && (by_count || by_mass)) {
+    __syncthreads();
+    for (int i = tid; i < FINE; i += TPB) s.fast.bin[i] = 0;
+    __syncthreads();
+    if (end_col >= 0) atomicAdd(&s.fast.bin[bin_of(end, m, c_fine, FINE)], 1u);
+    stream([&](int step, const uint4 (&u)[U]) {
+#pragma unroll
+      for (int i = 0; i < U; ++i)
+        if (step < n_full || (step * U + (i & ~1)) * TPB + 2 * tid < nv) each_logit<X>(u[i], [&](int, float y) { atomicAdd(&s.fast.bin[bin_of(y, m, c_fine, FINE)], 1u); });
+    });
+    all_sync();
+    constexpr int PER = FINE / TPB;
+    uint32_t c[PER] = {};
+    for (int r = 0; r < ctas; ++r) {
+      const Smem& o = of_rank(r);
+#pragma unroll
+      for (int j = 0; j < PER; ++j) c[j] += o.fast.bin[tid * PER + j];
+    }
+    if (tid == 0) { s.first_bin = s.last_bin = FINE - 1; s.before = 0; }
+    if (by_count) {
+      u64 mine = 0, all;
+      for (int j = 0; j < PER; ++j) mine += c[j];
+      u64 at = scan_before(mine, s, all);
+      for (int j = 0; j < PER; ++j) {
+        if (at < u64(q.k) && u64(q.k) <= at + c[j]) {
+          s.first_bin = s.last_bin = tid * PER + j;
+          s.before = at;
+        }
+        at += c[j];
+      }
+    } else {
+      // a bin's weights lie within 2^(-1/128) of one another; what 32 bits round is a hundredth of the slack
+      const double step = exp2(-1.0 / 128.0), top = exp2(-double(tid * PER) / 128.0) * (1.0 + 1e-4);
+      double most = 0.0, all_most, all_least, v = top;
+      for (int j = 0; j < PER; ++j, v *= step) most += c[j] * v;
+      const double last = tid == TPB - 1 ? c[PER - 1] * top : 0.0;       // the last bin's may be nothing
+      double at_most = scan_before(most, s, all_most);
+      const double least = (most - last) * (step * (1.0 - 2e-4));
+      double at_least = scan_before(least, s, all_least);
+      const double goal_least = double(q.p) * all_least, goal_most = double(q.p) * all_most;
+      v = top;
+      for (int j = 0; j < PER; ++j, v *= step) {
+        const double n_most = at_most + c[j] * v, n_least = at_least + c[j] * v * (step * (1.0 - 2e-4));
+        if (at_most < goal_least && goal_least <= n_most) s.first_bin = tid * PER + j;
+        if (at_least < goal_most && goal_most <= n_least) s.last_bin = tid * PER + j;
+        at_most = n_most;
+        at_least = n_least;
+      }
+    }
+    __syncthreads();
+    lo = s.first_bin;
+    hi = s.last_bin;
+    count_before = s.before;
+    slow = hi >= FINE - 1 || lo > hi;
+    all_sync();                      // the bins have been read
+  }
+  if (slow) {
+    all_sync();                      // what the others read of this CTA has been read
+    if (rank == 0) sample_any<X>(row, a, t, q, wt, s);
+    return;
+  }
+
+  __syncthreads();
+  // every token's weight once: sums of neighbours among those before the bins [lo, hi], a list of those in them, and the sum of all
+  const double least = q.mp > 0.0f ? double(q.mp) : 0.0;
+  {
+    u64 total = 0, certain = 0;
+    auto one = [&](float x, int col, bool in) -> u64 {
+      if (!in) return 0;
+      const int b = lo < FINE ? bin_of(x, m, c_fine, FINE) : 0;
+      const u64 v = wt.whole(x);
+      total += v;
+      if (b < lo) {
+        certain += v;
+        return least == 0.0 || exp((double(x) - wt.m) * double(q.scale)) >= least ? v : 0;
+      }
+      if (b <= hi) push(x, col);
+      return 0;
+    };
+    stream([&](int step, const uint4 (&u)[U]) {
+#pragma unroll
+      for (int half = 0; half < 2; ++half) {
+        u64 v = 0;
+        const bool in = step < n_full || (step * U + 2 * half) * TPB + 2 * tid < nv;
+#pragma unroll
+        for (int i = 2 * half; i < 2 * half + 2; ++i) each_logit<X>(u[i], [&](int e, float y) { v += one(y, column(step, i) + e, in); });
+        for (int o = 16; o; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+        if (lane == 0 && ((step * U + 2 * half) * TPB + 64 * w) < nv) s.fast.chunk[1 + (step * 2 + half) * WARPS + w] = v;
+      }
+    });
+    // the ends: chunk 0 is the head, the one behind the last is the tail
+    u64 v = one(end, end_col, end_col >= 0), h = end_col >= 0 && end_col < first ? v : 0;
+    v -= h;
+    for (int o = 16; o; o >>= 1) {
+      v += __shfl_xor_sync(0xffffffffu, v, o);
+      h += __shfl_xor_sync(0xffffffffu, h, o);
+    }
+    if (tid == 0) {
+      if (rank == 0) s.fast.chunk[0] = h;
+      if (rank == ctas - 1) s.fast.chunk[1 + (nv + CHUNK_VECS - 1) / CHUNK_VECS] = v;
+    }
+    u64 all;
+    scan_before(total, s, all);
+    if (tid == 0) s.total = all;
+    scan_before(certain, s, all);
+    if (tid == 0) s.certain = all;
+  }
+  all_sync();
+  u64 total = 0, certain = 0;
+  int n = 0;
+  if (rank == 0) {
+    for (int r = 0; r < ctas; ++r) {
+      const Smem& o = of_rank(r);
+      total += o.total;
+      certain += o.certain;
+      const int more = o.n_key;
+      if (r && n + more <= LIST)
+        for (int i = tid; i < more; i += TPB) s.key[n + i] = o.key[i];
+      n += more;
+      if (r) {
+        const int64_t from = min(all_v, r * per), to = min(int64_t(all_v), from + per);
+        const int chunks = int((to - from + CHUNK_VECS - 1) / CHUNK_VECS) + (r == ctas - 1);
+        for (int i = tid; i < chunks; i += TPB) s.fast.chunk[1 + (from + CHUNK_VECS - 1) / CHUNK_VECS + i] = o.fast.chunk[1 + i];
+      }
+    }
+  }
+  all_sync();
+  if (rank) return;
+  if (n > LIST) {
+    __syncthreads();
+    sample_any<X>(row, a, t, q, wt, s);
+    return;
+  }
+  u64 last = 0;                      // the last kept token's key
+  if (lo < FINE) {
+    for (int i = tid; i < n; i += TPB) {
+      const u64 mine = s.key[i];
+      int place = 0;
+      for (int j = 0; j < n; ++j) place += s.key[j] > mine;
+      s.sorted[place] = mine;
+    }
+    if (tid == 0) s.found = 0;
+    __syncthreads();
+    constexpr int PER = LIST / TPB;
+    u64 v[PER], mine = 0, all;
+    for (int j = 0; j < PER; ++j) {
+      const int i = tid * PER + j;
+      v[j] = i >= n ? 0 : by_count ? 1 : wt.whole(key_value(s.sorted[i]));
+      mine += v[j];
+    }
+    u64 at = (by_count ? count_before : certain) + scan_before(mine, s, all);
+    const u64 target = by_count ? u64(q.k) : max(u64(1), u64(ceil(double(q.p) * double(total))));
+    for (int j = 0; j < PER; ++j) {
+      if (at < target && target <= at + v[j]) s.found = s.sorted[tid * PER + j];
+      at += v[j];
+    }
+    __syncthreads();
+    last = s.found;
+    if (last == 0) {                 // not where the bins said: never expected
+      sample_any<X>(row, a, t, q, wt, s);
+      return;
+    }
+    // the listed ones that stay, to their chunks
+    for (int i = tid; i < n; i += TPB) {
+      const u64 key = s.sorted[i];
+      const float x = key_value(key);
+      if (key < last || (least > 0.0 && exp((double(x) - wt.m) * double(q.scale)) < least)) continue;
+      const int col = int(key_index(key));
+      atomicAdd(&s.fast.chunk[col < first ? 0 : col >= tail_col ? 1 + (all_v + CHUNK_VECS - 1) / CHUNK_VECS : 1 + (col - first) / N / CHUNK_VECS], wt.whole(x));
+    }
+    __syncthreads();
+  }
+  // the chunk, and the token in it
+  constexpr int PER = CHUNKS / TPB;
+  const int chunks = 2 + (all_v + CHUNK_VECS - 1) / CHUNK_VECS;
+  u64 mine = 0, all;
+  for (int j = 0; j < PER; ++j) {
+    const int i = tid * PER + j;
+    mine += i < chunks ? s.fast.chunk[i] : 0;
+  }
+  u64 at = scan_before(mine, s, all);
+  const u64 limit = limit_of(q.u, all);
+  for (int j = 0; j < PER; ++j) {
+    const int i = tid * PER + j;
+    const u64 v = i < chunks ? s.fast.chunk[i] : 0;
+    if (at <= limit && limit < at + v) {
+      s.first_bin = i;
+      s.before = at;
+    }
+    at += v;
+  }
+  __syncthreads();
+  if (w) return;
+  const int c = s.first_bin;
+  const int from = c == 0 ? 0 : c == chunks - 1 ? tail_col : first + (c - 1) * CHUNK_VECS * N, to = c == 0 ? first : c == chunks - 1 ? int(a.V) : min(tail_col, from + CHUNK_VECS * N);
+  u64 before = s.before;
+  for (int i0 = from; i0 < to; i0 += 32) {
+    const int i = i0 + lane;
+    const float x = i < to ? to_f(row[i]) : -INFINITY;
+    const bool in = i < to && make_key(x, uint32_t(i)) >= last && (least == 0.0 || exp((double(x) - wt.m) * double(q.scale)) >= least);
+    u64 incl = in ? wt.whole(x) : 0;
+    for (int o = 1; o < 32; o <<= 1) {
+      const u64 y = __shfl_up_sync(0xffffffffu, incl, o);
+      if (lane >= o) incl += y;
+    }
+    const unsigned hit = __ballot_sync(0xffffffffu, before + incl > limit);
+    if (hit) {
+      if (lane == __ffs(int(hit)) - 1) put_drawn(a, t, i, x, wt, all);
       return;
     }
     before += __shfl_sync(0xffffffffu, incl, 31);
@@ -253,12 +769,36 @@ int mv_sample(void* stream, const void* logits, int type, int64_t T, int64_t V, 
     return MV_ERR_INVALID_ARG;
   if (T == 0) return MV_OK;
   SampleArgs a;
-  a.V = V; a.ld = ld; a.unit = ldexp(1.0, 61); a.u = u;
-  for (int64_t n = 1; n < V; n *= 2) a.unit *= 0.5; a.scale = scale; a.top_k = top_k; a.top_p = top_p; a.min_p = min_p; a.token = token; a.id_type = id_type; a.logprob = logprob;
+  a.V = V; a.ld = ld; a.u = u; a.scale = scale; a.top_k = top_k; a.top_p = top_p; a.min_p = min_p; a.token = token; a.id_type = id_type; a.logprob = logprob;
+  a.unit = 0x1p51;                   // one of 2^52 has to fit the lower bits of a double
+  for (int64_t n = 1024; n < V; n *= 2) a.unit *= 0.5;
   return with_type(type, [&](auto x) {
     using X = decltype(x);
-    k_sample<X><<<unsigned(T), TPB, 0, static_cast<cudaStream_t>(stream)>>>(static_cast<const X*>(logits), a);
-    return cuda_ok();
+    const int64_t vecs = V / Vec<X>::N;
+    a.chunks = vecs / CHUNK_VECS + 10 <= CHUNKS;
+    // as many CTAs per row as fill the device, a step or more for each
+    int ctas = T >= 296 ? 1 : T >= 148 ? 2 : T >= 37 ? 4 : 8;
+    while (ctas > 1 && vecs < int64_t(ctas) * TPB * U) ctas /= 2;
+    if (T * ctas >= lim) return int(MV_ERR_INVALID_ARG);
+    const int64_t n_steps = ((vecs + ctas - 1) / ctas + CHUNK_VECS + TPB * U - 1) / (TPB * U);
+    a.steps = int((n_steps + GROUPS - 1) / GROUPS);
+    if (a.steps < 1) a.steps = 1;
+    auto* kernel = k_sample<X>;
+    static SmemLimit limit;
+    if (!allow_smem(kernel, int(sizeof(Smem)), &limit)) return int(MV_ERR_CUDA);
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(unsigned(T * ctas));
+    cfg.blockDim = dim3(TPB);
+    cfg.dynamicSmemBytes = sizeof(Smem);
+    cfg.stream = static_cast<cudaStream_t>(stream);
+    cudaLaunchAttribute attr = {};
+    attr.id = cudaLaunchAttributeClusterDimension;
+    attr.val.clusterDim.x = unsigned(ctas);
+    attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
+    cfg.attrs = &attr;
+    cfg.numAttrs = ctas > 1;
+    const bool ok = cudaLaunchKernelEx(&cfg, kernel, static_cast<const X*>(logits), a) == cudaSuccess;
+    return cuda_ok() == MV_OK && ok ? int(MV_OK) : int(MV_ERR_CUDA);
   });
 }
 

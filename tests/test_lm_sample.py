@@ -3,7 +3,7 @@
 Tokens have to be equal.  Sums in 64 bits are off by at most 1e-11 of the row's sum on either side, so that a random u meets a border between two
 of 10^5 tokens that the two place differently once in 10^6 rows or less; the seeds are fixed.  Where borders are met on purpose the weights are
 powers of two or equal, and every sum is exact.  logprob: scale (x - max) less the log of a sum of V weights, each off by at most half of
-2^-(61 - log2 V) of the largest one; in 64 bits, rounded to 32 at the end."""
+2^-(61 - log2 V) of the largest one (V at least 1024); in 64 bits, rounded to 32 at the end."""
 import math
 
 import numpy as np
@@ -36,7 +36,7 @@ def reference(x, u, scale, top_k, top_p, min_p):
     keep &= (w >= min_p) | (np.arange(V) == 0)
     chosen = np.sort(order[keep])
     weight = np.zeros(V)
-    weight[order] = np.where(w * 2.0 ** (62 - (V - 1).bit_length()) >= 1.0, w, 0.0)       # too light to be drawn
+    weight[order] = np.where(w * 2.0 ** (62 - max(10, (V - 1).bit_length())) >= 1.0, w, 0.0)       # too light to be drawn
     run = np.cumsum(weight[chosen])
     goal = min(max(u, 0.0), 1.0) * run[-1]
     j = int(np.searchsorted(run, goal, side="right"))
@@ -64,7 +64,7 @@ def check(x, u, scale=None, top_k=None, top_p=None, min_p=None, it=torch.int64):
         if math.isnan(wlp) or math.isinf(wlp):
             assert (math.isnan(lp[t]) and math.isnan(wlp)) or lp[t] == wlp, at
         else:
-            assert abs(lp[t] - wlp) <= 1.01 * U32 * abs(wlp) + 2.0 ** -61 * x.shape[1] ** 2 + 1e-12, (at, lp[t], wlp)
+            assert abs(lp[t] - wlp) <= 1.01 * U32 * abs(wlp) + 2.0 ** -61 * max(1024, x.shape[1]) ** 2 + 1e-12, (at, lp[t], wlp)
     return token
 
 

@@ -9,6 +9,7 @@
 namespace {
 
 typedef unsigned long long u64;
+template <int I> using Int = std::integral_constant<int, I>;
 
 struct SampleArgs {
   int64_t V, ld;
@@ -56,8 +57,10 @@ struct Smem {
   double warp_d[WARPS];
   float max[WARPS], part_max;
   int n_key, n_group, first_bin, last_bin;
-  u64 found, before, total, certain;
+  u64 found, before, total;
 };
+
+constexpr u64 NOTHING = 0x4330000000000000ull;      // 2^52 as a double
 
 // A row's weights 2^t, t = (x - m) c log2(e) <= 0, in 64 bits and as whole numbers.  2^t = 2^(i/32) 2^f with |f| <= 1/64: a table and the
 // exponential series to the fifth power (the sixth is below 2.3e-15).
@@ -77,7 +80,8 @@ struct Weights {
     const double p = fma(fma(fma(fma(fma(L * L * L * L * L / 120, f, L * L * L * L / 24), f, L * L * L / 6), f, L * L / 2), f, L), f, 1.0) * table[i & 31];
     return fma(p, __hiloint2double(((i >> 5) << 20) + lift, 0), 4503599627370496.0);
   }
-  __device__ __forceinline__ u64 whole(float x) const { return u64(__double_as_longlong(lifted(x))) - 0x4330000000000000ull; }
+  __device__ __forceinline__ u64 raw(float x) const { return u64(__double_as_longlong(lifted(x))); }      // NOTHING and the whole number
+  __device__ __forceinline__ u64 whole(float x) const { return raw(x) - NOTHING; }
 };
 
 // The largest whole number not above u all, u in [0, 1), exactly.
@@ -158,6 +162,26 @@ __device__ __forceinline__ void put_drawn(const SampleArgs& a, int64_t t, int64_
   put_token(a, t, token, float((double(x) - wt.m) * (wt.c2 * 0.6931471805599453) - log(double(all) / wt.unit)));
 }
 __device__ __forceinline__ u64 limit_of(float u, u64 all) { return u >= 1.0f ? all - 1 : u > 0.0f ? share_of(u, all) : 0; }      // the first token at which the sum is larger is drawn
+
+// The smallest logit for which f holds, f false below it and true from it on; +inf: none.  By all lanes of a warp, five bits of the
+// order at a time.
+template <typename F> __device__ __forceinline__ float smallest(F&& f) {
+  const uint32_t lane = threadIdx.x & 31;
+  constexpr uint32_t LOW = 0x00800000u, HIGH = 0xff7fffffu;          // the orders of the finite numbers
+  uint32_t base = 0;                 // f is false below it
+  for (int shift = 27; ; shift = shift > 5 ? shift - 5 : 0) {
+    const uint32_t h = base + (lane << shift);
+    const bool over = h < base;      // past 2^32
+    const unsigned hit = __ballot_sync(0xffffffffu, over || h > HIGH || (h >= LOW && f(value_of(h))));
+    const int n = hit ? __ffs(int(hit)) - 1 : 32;      // the first place where it holds
+    if (shift == 0) {
+      base += uint32_t(n);
+      break;
+    }
+    base += n ? uint32_t(n - 1) << shift : 0;
+  }
+  return base > HIGH ? INFINITY : value_of(base);
+}
 
 // ------------------------------------------------------------------------------------------ any row
 // Rows that the fast paths do not take: cuts by three readings each, over 11, 11 and 10 bits of the order.
@@ -367,7 +391,23 @@ __global__ void __launch_bounds__(TPB, 3) k_sample(const X* __restrict__ logits,
       f(step + 1, odd);
     }
   };
-  auto column = [&](int step, int i) { return col0 + ((step * U + (i & ~1)) * TPB + 2 * tid + (i & 1)) * N; };      // of vector i of a step
+  // f(chunk of the CTA's, two vectors of a lane, whether they are of the row), the next ones on their way
+  auto pass = [&](auto&& f) {
+    const int turns = (nv + 2 * TPB - 1) / (2 * TPB);
+    uint4 u[2], next[2];
+    auto fetch = [&](int i) {
+      next[0] = next[1] = none;
+      if (i * (2 * TPB) + 2 * tid < nv) load_stream(vec + i * (2 * TPB) + 2 * tid, next[0], next[1]);
+    };
+    fetch(0);
+#pragma unroll 1
+    for (int i = 0; i < turns; ++i) {
+      u[0] = next[0];
+      u[1] = next[1];
+      fetch(i + 1);
+      f(i * WARPS + w, u, i * (2 * TPB) + 2 * tid < nv);
+    }
+  };
   auto all_sync = [&]() {
     if (ctas > 1) cluster.sync();
     else __syncthreads();
@@ -422,6 +462,7 @@ __global__ void __launch_bounds__(TPB, 3) k_sample(const X* __restrict__ logits,
   wt.table = s.table;
   wt.lift = __double2hiint(a.unit);
   const float c_coarse = fminf(q.scale * (LOG2E * 16.0f), 3.0e38f), c_fine = fminf(q.scale * (LOG2E * 128.0f), 3.0e38f);
+  const float t_mp = q.mp <= 0.0f ? -INFINITY : smallest([&](float x) { return exp((double(x) - wt.m) * double(q.scale)) >= double(q.mp); });      // min p as a logit
   auto push = [&](float x, int col) {
     const int i = atomicAdd(&s.n_key, 1);
     if (i < LIST) s.key[i] = make_key(x, uint32_t(col));
@@ -443,7 +484,7 @@ __global__ void __launch_bounds__(TPB, 3) k_sample(const X* __restrict__ logits,
     if (at < u64(q.k) && u64(q.k) <= at + c[0] + c[1]) s.first_bin = 2 * tid + (at + c[0] < u64(q.k));
     __syncthreads();
     int b = s.first_bin;
-    if (q.p >= 1.0f && q.mp > 0.0f) b = min(b, int(fminf(-log2f(q.mp) * 16.0f, 1.0e4f)) + 1);      // nothing beyond it is kept
+    if (q.p >= 1.0f && q.mp > 0.0f) b = min(b, bin_of(t_mp, m, c_coarse, COARSE));      // nothing beyond it is kept
     by_list = b < COARSE - 1;
     if (by_list) {
       for (int g = 0; g < groups; ++g)
@@ -501,7 +542,7 @@ __global__ void __launch_bounds__(TPB, 3) k_sample(const X* __restrict__ logits,
       const u64 target = q.p < 1.0f ? max(u64(1), u64(ceil(double(q.p) * double(total)))) : ~0ull;
       for (int j = 0; j < PER; ++j) {
         const int i = tid * PER + j;
-        const bool in = i < kept_k && (i == 0 || before < target) && (i == 0 || q.mp <= 0.0f || exp((double(key_value(s.sorted[i])) - wt.m) * double(q.scale)) >= double(q.mp));
+        const bool in = i < kept_k && (i == 0 || (before < target && key_value(s.sorted[i]) >= t_mp));
         before += v[j];
         if (!in) v[j] = 0;
         if (i < n) s.sum[i] = v[j];
@@ -536,9 +577,9 @@ __global__ void __launch_bounds__(TPB, 3) k_sample(const X* __restrict__ logits,
     if (tid == 0) s.n_key = 0;
   }
 
-  // bins of all logits, where a cut is asked for: the bins [lo, hi] in which the last token of the start may lie
-  int lo = FINE, hi = FINE;          // nothing is cut
-  bool slow = a.chunks == 0;
+  // bins of all logits, where a cut is asked for: the bins [lo, hi] in which the last token of the start may lie, and their logits [t2, t1)
+  float t1 = -INFINITY, t2 = -INFINITY;
+  bool slow = a.chunks == 0, cut = false;
   const bool by_count = q.k < a.V, by_mass = q.p < 1.0f;
   u64 count_before = 0;
   if (by_count && by_mass) slow = true;
@@ -547,10 +588,10 @@ __global__ void __launch_bounds__(TPB, 3) k_sample(const X* __restrict__ logits,
     for (int i = tid; i < FINE; i += TPB) s.fast.bin[i] = 0;
     __syncthreads();
     if (end_col >= 0) atomicAdd(&s.fast.bin[bin_of(end, m, c_fine, FINE)], 1u);
-    stream([&](int step, const uint4 (&u)[U]) {
+    pass([&](int, const uint4 (&u)[2], bool in) {
+      if (in)
 #pragma unroll
-      for (int i = 0; i < U; ++i)
-        if (step < n_full || (step * U + (i & ~1)) * TPB + 2 * tid < nv) each_logit<X>(u[i], [&](int, float y) { atomicAdd(&s.fast.bin[bin_of(y, m, c_fine, FINE)], 1u); });
+        for (int i = 0; i < 2; ++i) each_logit<X>(u[i], [&](int, float y) { atomicAdd(&s.fast.bin[bin_of(y, m, c_fine, FINE)], 1u); });
     });
     all_sync();
     constexpr int PER = FINE / TPB;
@@ -573,30 +614,36 @@ __global__ void __launch_bounds__(TPB, 3) k_sample(const X* __restrict__ logits,
         at += c[j];
       }
     } else {
-      // a bin's weights lie within 2^(-1/128) of one another; what 32 bits round is a hundredth of the slack
-      const double step = exp2(-1.0 / 128.0), top = exp2(-double(tid * PER) / 128.0) * (1.0 + 1e-4);
+      // A bin's weights lie within 2^(-1/128) of one another; what 32 bits round is a hundredth of the slack.  The start ends in the first bin
+      // at whose end (1 - p) times the sum up to it is no less than p times the rest.
+      const double step = exp2(-1.0 / 128.0), low = step * (1.0 - 2e-4), top = exp2(-double(tid * PER) / 128.0) * (1.0 + 1e-4), p = double(q.p);
       double most = 0.0, all_most, all_least, v = top;
       for (int j = 0; j < PER; ++j, v *= step) most += c[j] * v;
-      const double last = tid == TPB - 1 ? c[PER - 1] * top : 0.0;       // the last bin's may be nothing
-      double at_most = scan_before(most, s, all_most);
-      const double least = (most - last) * (step * (1.0 - 2e-4));
-      double at_least = scan_before(least, s, all_least);
-      const double goal_least = double(q.p) * all_least, goal_most = double(q.p) * all_most;
+      double last = tid == TPB - 1 ? c[PER - 1] * exp2(-double(FINE - 1) / 128.0) * (1.0 + 1e-4) : 0.0;      // the last bin's may be nothing
+      double at_most = scan_before(most, s, all_most), at_least = scan_before((most - last) * low, s, all_least);
       v = top;
+      bool lo_done = (1.0 - p) * at_most >= p * (all_least - at_least), hi_done = (1.0 - p) * at_least >= p * (all_most - at_most);
+      if (tid == 0) lo_done = hi_done = false;
       for (int j = 0; j < PER; ++j, v *= step) {
-        const double n_most = at_most + c[j] * v, n_least = at_least + c[j] * v * (step * (1.0 - 2e-4));
-        if (at_most < goal_least && goal_least <= n_most) s.first_bin = tid * PER + j;
-        if (at_least < goal_most && goal_most <= n_least) s.last_bin = tid * PER + j;
-        at_most = n_most;
-        at_least = n_least;
+        at_most += c[j] * v;
+        at_least += c[j] * v * low;
+        const bool lo_now = (1.0 - p) * at_most >= p * (all_least - at_least), hi_now = (1.0 - p) * at_least >= p * (all_most - at_most);
+        if (lo_now && !lo_done) s.first_bin = tid * PER + j;
+        if (hi_now && !hi_done) s.last_bin = tid * PER + j;
+        lo_done |= lo_now;
+        hi_done |= hi_now;
       }
     }
     __syncthreads();
-    lo = s.first_bin;
-    hi = s.last_bin;
+    const int lo = s.first_bin, hi = s.last_bin;
     count_before = s.before;
-    slow = hi >= FINE - 1 || lo > hi;
     all_sync();                      // the bins have been read
+    slow = hi >= FINE - 1 || lo > hi;
+    if (!slow) {
+      t1 = lo == 0 ? INFINITY : smallest([&](float x) { return bin_of(x, m, c_fine, FINE) < lo; });
+      t2 = smallest([&](float x) { return bin_of(x, m, c_fine, FINE) <= hi; });
+      cut = t_mp < t1;               // else min p leaves nothing of them
+    }
   }
   if (slow) {
     all_sync();                      // what the others read of this CTA has been read
@@ -604,59 +651,59 @@ __global__ void __launch_bounds__(TPB, 3) k_sample(const X* __restrict__ logits,
     return;
   }
 
+  if (!cut) t1 = t2 = t_mp;
   __syncthreads();
-  // every token's weight once: sums of neighbours among those before the bins [lo, hi], a list of those in them, and the sum of all
-  const double least = q.mp > 0.0f ? double(q.mp) : 0.0;
+  // Weights: sums of neighbours among the logits from t1 on, a list of those in [t2, t1), and, for a cut by mass, the sum of all.
   {
-    u64 total = 0, certain = 0;
-    auto one = [&](float x, int col, bool in) -> u64 {
-      if (!in) return 0;
-      const int b = lo < FINE ? bin_of(x, m, c_fine, FINE) : 0;
-      const u64 v = wt.whole(x);
-      total += v;
-      if (b < lo) {
-        certain += v;
-        return least == 0.0 || exp((double(x) - wt.m) * double(q.scale)) >= least ? v : 0;
-      }
-      if (b <= hi) push(x, col);
-      return 0;
-    };
-    stream([&](int step, const uint4 (&u)[U]) {
-#pragma unroll
-      for (int half = 0; half < 2; ++half) {
+    u64 total = 0;
+    auto sums = [&](auto kind) {
+      constexpr int KIND = decltype(kind)::value;      // 0: of all; 1: of those from t2 on; 2: of all, with the sum of all
+      auto one = [&](float x, int col) -> u64 {
+        if constexpr (KIND == 0) return wt.raw(x);
+        if (KIND == 1 && !(x >= t2)) return NOTHING;
+        const u64 v = KIND == 1 && x < t1 ? NOTHING : wt.raw(x);
+        if constexpr (KIND == 2) total += v - NOTHING;
+        if (x >= t1) return v;
+        if (x >= t2) push(x, col);
+        return NOTHING;
+      };
+      pass([&](int chunk, const uint4 (&u)[2], bool) {
         u64 v = 0;
-        const bool in = step < n_full || (step * U + 2 * half) * TPB + 2 * tid < nv;
+        const int col = col0 + (chunk * CHUNK_VECS + 2 * lane) * N;
 #pragma unroll
-        for (int i = 2 * half; i < 2 * half + 2; ++i) each_logit<X>(u[i], [&](int e, float y) { v += one(y, column(step, i) + e, in); });
+        for (int i = 0; i < 2; ++i) each_logit<X>(u[i], [&](int e, float y) { v += one(y, col + i * N + e); });
+        v -= 2 * N * NOTHING;
         for (int o = 16; o; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
-        if (lane == 0 && ((step * U + 2 * half) * TPB + 64 * w) < nv) s.fast.chunk[1 + (step * 2 + half) * WARPS + w] = v;
+        if (lane == 0 && chunk * CHUNK_VECS < nv) s.fast.chunk[1 + chunk] = v;
+      });
+      // the ends: chunk 0 is the head, the one behind the last is the tail
+      if (w == 0) {
+        u64 v = one(end, end_col) - NOTHING, h = end_col >= 0 && end_col < first ? v : 0;
+        v -= h;
+        for (int o = 16; o; o >>= 1) {
+          v += __shfl_xor_sync(0xffffffffu, v, o);
+          h += __shfl_xor_sync(0xffffffffu, h, o);
+        }
+        if (lane == 0) {
+          if (rank == 0) s.fast.chunk[0] = h;
+          if (rank == ctas - 1) s.fast.chunk[1 + (nv + CHUNK_VECS - 1) / CHUNK_VECS] = v;
+        }
       }
-    });
-    // the ends: chunk 0 is the head, the one behind the last is the tail
-    u64 v = one(end, end_col, end_col >= 0), h = end_col >= 0 && end_col < first ? v : 0;
-    v -= h;
-    for (int o = 16; o; o >>= 1) {
-      v += __shfl_xor_sync(0xffffffffu, v, o);
-      h += __shfl_xor_sync(0xffffffffu, h, o);
-    }
-    if (tid == 0) {
-      if (rank == 0) s.fast.chunk[0] = h;
-      if (rank == ctas - 1) s.fast.chunk[1 + (nv + CHUNK_VECS - 1) / CHUNK_VECS] = v;
-    }
+    };
+    if (cut && by_mass) sums(Int<2>());
+    else if (t2 > -INFINITY) sums(Int<1>());
+    else sums(Int<0>());
     u64 all;
     scan_before(total, s, all);
     if (tid == 0) s.total = all;
-    scan_before(certain, s, all);
-    if (tid == 0) s.certain = all;
   }
   all_sync();
-  u64 total = 0, certain = 0;
+  u64 total = 0;
   int n = 0;
   if (rank == 0) {
     for (int r = 0; r < ctas; ++r) {
       const Smem& o = of_rank(r);
       total += o.total;
-      certain += o.certain;
       const int more = o.n_key;
       if (r && n + more <= LIST)
         for (int i = tid; i < more; i += TPB) s.key[n + i] = o.key[i];
@@ -676,7 +723,8 @@ __global__ void __launch_bounds__(TPB, 3) k_sample(const X* __restrict__ logits,
     return;
   }
   u64 last = 0;                      // the last kept token's key
-  if (lo < FINE) {
+  const int chunks = 2 + (all_v + CHUNK_VECS - 1) / CHUNK_VECS;
+  if (cut) {
     for (int i = tid; i < n; i += TPB) {
       const u64 mine = s.key[i];
       int place = 0;
@@ -686,7 +734,9 @@ __global__ void __launch_bounds__(TPB, 3) k_sample(const X* __restrict__ logits,
     if (tid == 0) s.found = 0;
     __syncthreads();
     constexpr int PER = LIST / TPB;
-    u64 v[PER], mine = 0, all;
+    u64 v[PER], mine = 0, all, certain = 0;
+    for (int i = tid; i < chunks; i += TPB) certain += s.fast.chunk[i];
+    scan_before(certain, s, certain);
     for (int j = 0; j < PER; ++j) {
       const int i = tid * PER + j;
       v[j] = i >= n ? 0 : by_count ? 1 : wt.whole(key_value(s.sorted[i]));
@@ -708,7 +758,7 @@ __global__ void __launch_bounds__(TPB, 3) k_sample(const X* __restrict__ logits,
     for (int i = tid; i < n; i += TPB) {
       const u64 key = s.sorted[i];
       const float x = key_value(key);
-      if (key < last || (least > 0.0 && exp((double(x) - wt.m) * double(q.scale)) < least)) continue;
+      if (key < last || x < t_mp) continue;
       const int col = int(key_index(key));
       atomicAdd(&s.fast.chunk[col < first ? 0 : col >= tail_col ? 1 + (all_v + CHUNK_VECS - 1) / CHUNK_VECS : 1 + (col - first) / N / CHUNK_VECS], wt.whole(x));
     }
@@ -716,7 +766,6 @@ __global__ void __launch_bounds__(TPB, 3) k_sample(const X* __restrict__ logits,
   }
   // the chunk, and the token in it
   constexpr int PER = CHUNKS / TPB;
-  const int chunks = 2 + (all_v + CHUNK_VECS - 1) / CHUNK_VECS;
   u64 mine = 0, all;
   for (int j = 0; j < PER; ++j) {
     const int i = tid * PER + j;
@@ -737,23 +786,32 @@ __global__ void __launch_bounds__(TPB, 3) k_sample(const X* __restrict__ logits,
   if (w) return;
   const int c = s.first_bin;
   const int from = c == 0 ? 0 : c == chunks - 1 ? tail_col : first + (c - 1) * CHUNK_VECS * N, to = c == 0 ? first : c == chunks - 1 ? int(a.V) : min(tail_col, from + CHUNK_VECS * N);
-  u64 before = s.before;
-  for (int i0 = from; i0 < to; i0 += 32) {
-    const int i = i0 + lane;
-    const float x = i < to ? to_f(row[i]) : -INFINITY;
-    const bool in = i < to && make_key(x, uint32_t(i)) >= last && (least == 0.0 || exp((double(x) - wt.m) * double(q.scale)) >= least);
-    u64 incl = in ? wt.whole(x) : 0;
-    for (int o = 1; o < 32; o <<= 1) {
-      const u64 y = __shfl_up_sync(0xffffffffu, incl, o);
-      if (lane >= o) incl += y;
+  // up to 16 neighbouring tokens per lane
+  constexpr int MOST = CHUNK_VECS * N / 32;
+  const int share = (to - from + 31) / 32, i0 = from + lane * share;
+  u64 v[MOST], incl = 0;
+#pragma unroll
+  for (int j = 0; j < MOST; ++j) {
+    v[j] = 0;
+    if (j < share && i0 + j < to) {
+      const float x = to_f(row[i0 + j]);
+      if (make_key(x, uint32_t(i0 + j)) >= last && x >= t_mp) v[j] = wt.whole(x);
     }
-    const unsigned hit = __ballot_sync(0xffffffffu, before + incl > limit);
-    if (hit) {
-      if (lane == __ffs(int(hit)) - 1) put_drawn(a, t, i, x, wt, all);
-      return;
-    }
-    before += __shfl_sync(0xffffffffu, incl, 31);
+    incl += v[j];
   }
+  u64 before = incl;
+  for (int o = 1; o < 32; o <<= 1) {
+    const u64 y = __shfl_up_sync(0xffffffffu, incl, o);
+    if (lane >= o) incl += y;
+  }
+  before = s.before + incl - before;
+  incl += s.before;
+  if (before <= limit && limit < incl)
+#pragma unroll
+    for (int j = 0; j < MOST; ++j) {
+      if (before <= limit && limit < before + v[j]) put_drawn(a, t, i0 + j, to_f(row[i0 + j]), wt, all);
+      before += v[j];
+    }
 }
 
 }  // namespace

@@ -35,13 +35,17 @@ constexpr int CHUNK_VECS = 64;       // vectors of each, one warp's
 constexpr int GROUPS = 32;           // groups per thread whose maxima are kept
 constexpr int COARSE = 512, FINE = 4096;       // bins over 2^-32 .. 1 of the largest weight: 1/16 and 1/128 of a power of two wide
 constexpr int SLOW_BINS = 2048;
+constexpr int RESIDENT = 4;          // CTAs per multiprocessor
 
 // What one path or the other keeps in shared memory.
 struct Smem {
   union {
     float gmax[GROUPS][TPB];         // the groups' maxima
     struct {
-      uint32_t bin[FINE];
+      union {
+        uint32_t bin[FINE];
+        struct { u64 sorted[LIST], sum[LIST]; };
+      };
       u64 chunk[CHUNKS];
     } fast;
     struct {
@@ -50,7 +54,7 @@ struct Smem {
     } slow;
   };
   uint32_t coarse[COARSE];
-  u64 key[LIST], sorted[LIST], sum[LIST];
+  u64 key[LIST];
   uint16_t group[LIST];
   double table[32];                  // 2^(j/32)
   u64 warp[WARPS];
@@ -130,6 +134,30 @@ __device__ __forceinline__ double scan_before(double v, Smem& s, double& all) {
     all += s.warp_d[i];
   }
   return at;
+}
+
+// Sorts n keys in descending order; those behind them, up to a power of two, are overwritten.  Pairs up to 32 apart belong to one warp.
+__device__ __forceinline__ void sort_keys(u64* key, int n) {
+  int size = 64;
+  while (size < n) size *= 2;
+  for (int i = n + threadIdx.x; i < size; i += TPB) key[i] = 0;
+  __syncthreads();
+#pragma unroll 1
+  for (int k = 2; k <= size; k *= 2)
+#pragma unroll 1
+    for (int j = k / 2; j; j /= 2) {
+      for (int p = threadIdx.x; p < size / 2; p += TPB) {
+        const int i = 2 * p - (p & (j - 1));
+        const u64 a = key[i], b = key[i + j];
+        if (((i & k) == 0) == (a < b)) {
+          key[i] = b;
+          key[i + j] = a;
+        }
+      }
+      if (j > 32 || (j == 1 && k >= 64)) __syncthreads();
+      else __syncwarp();
+    }
+  __syncthreads();
 }
 
 // What a row's request asks for.
@@ -346,7 +374,7 @@ template <typename X> __device__ __forceinline__ float widen_nan(uint32_t m) {
 __device__ __forceinline__ int bin_of(float x, float m, float c, int n) { return int(fminf(distance(m, x, c), float(n - 1))); }
 
 template <typename X>
-__global__ void __launch_bounds__(TPB, 3) k_sample(const X* __restrict__ logits, const __grid_constant__ SampleArgs a) {
+__global__ void __launch_bounds__(TPB, RESIDENT) k_sample(const X* __restrict__ logits, const __grid_constant__ SampleArgs a) {
   constexpr int N = Vec<X>::N;
   extern __shared__ u64 dynamic[];
   Smem& s = *reinterpret_cast<Smem*>(dynamic);
@@ -523,50 +551,39 @@ __global__ void __launch_bounds__(TPB, 3) k_sample(const X* __restrict__ logits,
       all_sync();
       if (rank) return;
       // sorted, summed up in descending order, cut, summed up by index
-      for (int i = tid; i < n; i += TPB) {
-        const u64 mine = s.key[i];
-        int place = 0;
-        for (int j = 0; j < n; ++j) place += s.key[j] > mine;
-        s.sorted[place] = mine;
-      }
-      __syncthreads();
+      sort_keys(s.key, n);
       constexpr int PER = LIST / TPB;
       u64 v[PER], mine = 0, total;
       const int kept_k = int(min(q.k, int64_t(n)));
       for (int j = 0; j < PER; ++j) {
         const int i = tid * PER + j;
-        v[j] = i < kept_k ? wt.whole(key_value(s.sorted[i])) : 0;
+        v[j] = i < kept_k ? wt.whole(key_value(s.key[i])) : 0;
         mine += v[j];
       }
       u64 before = scan_before(mine, s, total);
       const u64 target = q.p < 1.0f ? max(u64(1), u64(ceil(double(q.p) * double(total)))) : ~0ull;
       for (int j = 0; j < PER; ++j) {
         const int i = tid * PER + j;
-        const bool in = i < kept_k && (i == 0 || (before < target && key_value(s.sorted[i]) >= t_mp));
+        const bool in = i < kept_k && (i == 0 || (before < target && key_value(s.key[i]) >= t_mp));
         before += v[j];
         if (!in) v[j] = 0;
-        if (i < n) s.sum[i] = v[j];
+        if (i < n) {
+          s.fast.sum[i] = v[j];
+          s.fast.sorted[i] = u64(uint32_t(s.key[i])) << 32 | unsigned(i);       // by index, and the place among the keys
+        }
       }
-      // places by index among all of the list; the cut ones weigh nothing
-      __syncthreads();
-      for (int i = tid; i < n; i += TPB) {
-        const uint32_t low = uint32_t(s.sorted[i]);          // larger: earlier
-        int place = 0;
-        for (int j = 0; j < n; ++j) place += uint32_t(s.sorted[j]) > low;
-        s.key[place] = u64(i);
-      }
-      __syncthreads();
+      sort_keys(s.fast.sorted, n);
       mine = 0;
       for (int j = 0; j < PER; ++j) {
         const int i = tid * PER + j;
-        v[j] = i < n ? s.sum[s.key[i]] : 0;
+        v[j] = i < n ? s.fast.sum[uint32_t(s.fast.sorted[i])] : 0;
         mine += v[j];
       }
       before = scan_before(mine, s, total);
       const u64 limit = limit_of(q.u, total);
       for (int j = 0; j < PER; ++j) {
         if (before <= limit && limit < before + v[j]) {
-          const u64 key = s.sorted[s.key[tid * PER + j]];
+          const u64 key = s.key[uint32_t(s.fast.sorted[tid * PER + j])];
           put_drawn(a, t, key_index(key), key_value(key), wt, total);
         }
         before += v[j];
@@ -596,10 +613,21 @@ __global__ void __launch_bounds__(TPB, 3) k_sample(const X* __restrict__ logits,
     all_sync();
     constexpr int PER = FINE / TPB;
     uint32_t c[PER] = {};
-    for (int r = 0; r < ctas; ++r) {
-      const Smem& o = of_rank(r);
+    if (ctas > 1) {                  // neighbouring threads take neighbouring bins from the others; the sums go where the chunks will be
+      uint32_t* sums = reinterpret_cast<uint32_t*>(s.fast.chunk);
+      for (int r = 0; r < ctas; ++r) {
+        const Smem& o = of_rank((rank + r) % ctas);
 #pragma unroll
-      for (int j = 0; j < PER; ++j) c[j] += o.fast.bin[tid * PER + j];
+        for (int j = 0; j < PER; ++j) c[j] += o.fast.bin[j * TPB + tid];
+      }
+#pragma unroll
+      for (int j = 0; j < PER; ++j) sums[j * TPB + tid] = c[j];
+      __syncthreads();
+#pragma unroll
+      for (int j = 0; j < PER; ++j) c[j] = sums[tid * PER + j];
+    } else {
+#pragma unroll
+      for (int j = 0; j < PER; ++j) c[j] = s.fast.bin[tid * PER + j];
     }
     if (tid == 0) { s.first_bin = s.last_bin = FINE - 1; s.before = 0; }
     if (by_count) {
@@ -658,28 +686,44 @@ __global__ void __launch_bounds__(TPB, 3) k_sample(const X* __restrict__ logits,
     u64 total = 0;
     auto sums = [&](auto kind) {
       constexpr int KIND = decltype(kind)::value;      // 0: of all; 1: of those from t2 on; 2: of all, with the sum of all
-      auto one = [&](float x, int col) -> u64 {
-        if constexpr (KIND == 0) return wt.raw(x);
-        if (KIND == 1 && !(x >= t2)) return NOTHING;
-        const u64 v = KIND == 1 && x < t1 ? NOTHING : wt.raw(x);
+      auto one = [&](float x, bool& listed) -> u64 {
+        const u64 v = wt.raw(x);
+        if constexpr (KIND == 0) return v;
         if constexpr (KIND == 2) total += v - NOTHING;
-        if (x >= t1) return v;
-        if (x >= t2) push(x, col);
-        return NOTHING;
+        listed = x >= t2 && !(x >= t1);
+        return x >= t1 ? v : NOTHING;
       };
       pass([&](int chunk, const uint4 (&u)[2], bool) {
         u64 v = 0;
-        const int col = col0 + (chunk * CHUNK_VECS + 2 * lane) * N;
+        unsigned hit = 0;
+        if constexpr (KIND == 1) {   // few of them
 #pragma unroll
-        for (int i = 0; i < 2; ++i) each_logit<X>(u[i], [&](int e, float y) { v += one(y, col + i * N + e); });
-        v -= 2 * N * NOTHING;
+          for (int i = 0; i < 2; ++i) each_logit<X>(u[i], [&](int e, float y) { hit |= y >= t2 ? 1u << (i * N + e) : 0u; });
+        } else {
+#pragma unroll
+          for (int i = 0; i < 2; ++i)
+            each_logit<X>(u[i], [&](int e, float y) {
+              bool listed = false;
+              v += one(y, listed);
+              hit |= listed ? 1u << (i * N + e) : 0u;
+            });
+          v -= 2 * N * NOTHING;
+        }
+        for (; hit; hit &= hit - 1) {
+          const int col = col0 + (chunk * CHUNK_VECS + 2 * lane) * N + __ffs(int(hit)) - 1;
+          const float x = to_f(row[col]);
+          if (x < t1) push(x, col);
+          else v += wt.whole(x);     // KIND 1 alone
+        }
         for (int o = 16; o; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
         if (lane == 0 && chunk * CHUNK_VECS < nv) s.fast.chunk[1 + chunk] = v;
       });
       // the ends: chunk 0 is the head, the one behind the last is the tail
       if (w == 0) {
-        u64 v = one(end, end_col) - NOTHING, h = end_col >= 0 && end_col < first ? v : 0;
+        bool listed = false;
+        u64 v = one(end, listed) - NOTHING, h = end_col >= 0 && end_col < first ? v : 0;
         v -= h;
+        if (listed) push(end, end_col);
         for (int o = 16; o; o >>= 1) {
           v += __shfl_xor_sync(0xffffffffu, v, o);
           h += __shfl_xor_sync(0xffffffffu, h, o);
@@ -698,6 +742,7 @@ __global__ void __launch_bounds__(TPB, 3) k_sample(const X* __restrict__ logits,
     if (tid == 0) s.total = all;
   }
   all_sync();
+  const int chunks = 2 + (all_v + CHUNK_VECS - 1) / CHUNK_VECS;
   u64 total = 0;
   int n = 0;
   if (rank == 0) {
@@ -708,11 +753,10 @@ __global__ void __launch_bounds__(TPB, 3) k_sample(const X* __restrict__ logits,
       if (r && n + more <= LIST)
         for (int i = tid; i < more; i += TPB) s.key[n + i] = o.key[i];
       n += more;
-      if (r) {
-        const int64_t from = min(all_v, r * per), to = min(int64_t(all_v), from + per);
-        const int chunks = int((to - from + CHUNK_VECS - 1) / CHUNK_VECS) + (r == ctas - 1);
-        for (int i = tid; i < chunks; i += TPB) s.fast.chunk[1 + (from + CHUNK_VECS - 1) / CHUNK_VECS + i] = o.fast.chunk[1 + i];
-      }
+    }
+    for (int i = tid; ctas > 1 && i < chunks; i += TPB) {
+      const int r = min(ctas - 1, max(0, i - 1) / (per / CHUNK_VECS));
+      if (r) s.fast.chunk[i] = of_rank(r).fast.chunk[i - r * (per / CHUNK_VECS)];
     }
   }
   all_sync();
@@ -723,14 +767,8 @@ __global__ void __launch_bounds__(TPB, 3) k_sample(const X* __restrict__ logits,
     return;
   }
   u64 last = 0;                      // the last kept token's key
-  const int chunks = 2 + (all_v + CHUNK_VECS - 1) / CHUNK_VECS;
   if (cut) {
-    for (int i = tid; i < n; i += TPB) {
-      const u64 mine = s.key[i];
-      int place = 0;
-      for (int j = 0; j < n; ++j) place += s.key[j] > mine;
-      s.sorted[place] = mine;
-    }
+    sort_keys(s.key, n);
     if (tid == 0) s.found = 0;
     __syncthreads();
     constexpr int PER = LIST / TPB;
@@ -739,13 +777,13 @@ __global__ void __launch_bounds__(TPB, 3) k_sample(const X* __restrict__ logits,
     scan_before(certain, s, certain);
     for (int j = 0; j < PER; ++j) {
       const int i = tid * PER + j;
-      v[j] = i >= n ? 0 : by_count ? 1 : wt.whole(key_value(s.sorted[i]));
+      v[j] = i >= n ? 0 : by_count ? 1 : wt.whole(key_value(s.key[i]));
       mine += v[j];
     }
     u64 at = (by_count ? count_before : certain) + scan_before(mine, s, all);
     const u64 target = by_count ? u64(q.k) : max(u64(1), u64(ceil(double(q.p) * double(total))));
     for (int j = 0; j < PER; ++j) {
-      if (at < target && target <= at + v[j]) s.found = s.sorted[tid * PER + j];
+      if (at < target && target <= at + v[j]) s.found = s.key[tid * PER + j];
       at += v[j];
     }
     __syncthreads();
@@ -756,7 +794,7 @@ __global__ void __launch_bounds__(TPB, 3) k_sample(const X* __restrict__ logits,
     }
     // the listed ones that stay, to their chunks
     for (int i = tid; i < n; i += TPB) {
-      const u64 key = s.sorted[i];
+      const u64 key = s.key[i];
       const float x = key_value(key);
       if (key < last || x < t_mp) continue;
       const int col = int(key_index(key));
@@ -783,35 +821,29 @@ __global__ void __launch_bounds__(TPB, 3) k_sample(const X* __restrict__ logits,
     at += v;
   }
   __syncthreads();
-  if (w) return;
   const int c = s.first_bin;
   const int from = c == 0 ? 0 : c == chunks - 1 ? tail_col : first + (c - 1) * CHUNK_VECS * N, to = c == 0 ? first : c == chunks - 1 ? int(a.V) : min(tail_col, from + CHUNK_VECS * N);
-  // up to 16 neighbouring tokens per lane
-  constexpr int MOST = CHUNK_VECS * N / 32;
-  const int share = (to - from + 31) / 32, i0 = from + lane * share;
-  u64 v[MOST], incl = 0;
+  constexpr int SHARE = (CHUNK_VECS * N + TPB - 1) / TPB;      // neighbouring tokens per thread
+  u64 v[SHARE], before = s.before;
+  mine = 0;
 #pragma unroll
-  for (int j = 0; j < MOST; ++j) {
+  for (int j = 0; j < SHARE; ++j) {
+    const int i = from + tid * SHARE + j;
     v[j] = 0;
-    if (j < share && i0 + j < to) {
-      const float x = to_f(row[i0 + j]);
-      if (make_key(x, uint32_t(i0 + j)) >= last && x >= t_mp) v[j] = wt.whole(x);
+    if (i < to) {
+      const float x = to_f(row[i]);
+      if (make_key(x, uint32_t(i)) >= last && x >= t_mp) v[j] = wt.whole(x);
     }
-    incl += v[j];
+    mine += v[j];
   }
-  u64 before = incl;
-  for (int o = 1; o < 32; o <<= 1) {
-    const u64 y = __shfl_up_sync(0xffffffffu, incl, o);
-    if (lane >= o) incl += y;
-  }
-  before = s.before + incl - before;
-  incl += s.before;
-  if (before <= limit && limit < incl)
+  u64 in_chunk;
+  before += scan_before(mine, s, in_chunk);
 #pragma unroll
-    for (int j = 0; j < MOST; ++j) {
-      if (before <= limit && limit < before + v[j]) put_drawn(a, t, i0 + j, to_f(row[i0 + j]), wt, all);
-      before += v[j];
-    }
+  for (int j = 0; j < SHARE; ++j) {
+    const int i = from + tid * SHARE + j;
+    if (before <= limit && limit < before + v[j]) put_drawn(a, t, i, to_f(row[i]), wt, all);
+    before += v[j];
+  }
 }
 
 }  // namespace
@@ -834,9 +866,9 @@ int mv_sample(void* stream, const void* logits, int type, int64_t T, int64_t V, 
     using X = decltype(x);
     const int64_t vecs = V / Vec<X>::N;
     a.chunks = vecs / CHUNK_VECS + 10 <= CHUNKS;
-    // as many CTAs per row as fill the device, a step or more for each
-    int ctas = T >= 296 ? 1 : T >= 148 ? 2 : T >= 37 ? 4 : 8;
-    while (ctas > 1 && vecs < int64_t(ctas) * TPB * U) ctas /= 2;
+    // as many CTAs per row as the device holds at once, a step or more for each
+    int ctas = 8;
+    while (ctas > 1 && (T * ctas > 148 * RESIDENT || vecs < int64_t(ctas) * TPB * U)) ctas /= 2;
     if (T * ctas >= lim) return int(MV_ERR_INVALID_ARG);
     const int64_t n_steps = ((vecs + ctas - 1) / ctas + CHUNK_VECS + TPB * U - 1) / (TPB * U);
     a.steps = int((n_steps + GROUPS - 1) / GROUPS);

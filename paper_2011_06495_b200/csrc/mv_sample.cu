@@ -35,7 +35,9 @@ constexpr int CHUNK_VECS = 64;       // vectors of each, one warp's
 constexpr int GROUPS = 32;           // groups per thread whose maxima are kept
 constexpr int COARSE = 512, FINE = 4096;       // bins over 2^-32 .. 1 of the largest weight: 1/16 and 1/128 of a power of two wide
 constexpr int SLOW_BINS = 2048;
+constexpr int TABLE = 256;           // as many as threads
 constexpr int RESIDENT = 4;          // CTAs per multiprocessor
+constexpr int MOST_CTAS = 8;         // per row
 
 // What one path or the other keeps in shared memory.
 struct Smem {
@@ -53,10 +55,10 @@ struct Smem {
       u64 chunk[CHUNKS];
     } slow;
   };
-  uint32_t coarse[COARSE];
+  alignas(8) uint32_t coarse[COARSE];
   u64 key[LIST];
   uint16_t group[LIST];
-  double table[32];                  // 2^(j/32)
+  double table[TABLE];               // 2^(j/256)
   u64 warp[WARPS];
   double warp_d[WARPS];
   float max[WARPS], part_max;
@@ -66,23 +68,23 @@ struct Smem {
 
 constexpr u64 NOTHING = 0x4330000000000000ull;      // 2^52 as a double
 
-// A row's weights 2^t, t = (x - m) c log2(e) <= 0, in 64 bits and as whole numbers.  2^t = 2^(i/32) 2^f with |f| <= 1/64: a table and the
-// exponential series to the fifth power (the sixth is below 2.3e-15).
+// A row's weights 2^t, t = (x - m) c log2(e) <= 0, in 64 bits and as whole numbers.  2^t = 2^n 2^(i/256) 2^f with |f| <= 1/512: a table
+// and the exponential series to the third power (the fourth is below 1.4e-13).  64-bit arithmetic bounds the passes that weigh every
+// token: eight operations (with a table of 32 and the fifth power: ten, and two more in the reduction before).
 struct Weights {
-  double m, c2, unit;
+  double m, c2, unit, least;         // least: the difference of a logit from m below which a weight is nothing, 80 / c2
   const double* table;
   int lift;                          // log2(unit), in the place of a double's exponent
   // 2^52 and the whole number, as a double
   __device__ __forceinline__ double lifted(float x) const {
-    const double t0 = (double(x) - m) * c2;
-    // below 2^-80: as 2^-80, which is nothing
-    const double t = __hiloint2double(int(min(uint32_t(__double2hiint(t0)), 0xC0540000u)), __double2loint(t0));
-    constexpr double MAGIC = 6755399441055744.0 / 32.0;                                  // 1.5 2^52 / 32: its last bit is 1/32
-    const double r = t + MAGIC, f = t - (r - MAGIC);
+    const double d0 = double(x) - m;
+    const double d = __hiloint2double(int(min(uint32_t(__double2hiint(d0)), uint32_t(__double2hiint(least)))), __double2loint(d0));       // negative numbers: the larger word is the smaller one
+    constexpr double MAGIC = 6755399441055744.0 / TABLE;                                 // 1.5 2^52 / 256: its last bit is 1/256
+    const double r = fma(d, c2, MAGIC), f = fma(d, c2, MAGIC - r);
     const int i = __double2loint(r);
     constexpr double L = 0.6931471805599453;
-    const double p = fma(fma(fma(fma(fma(L * L * L * L * L / 120, f, L * L * L * L / 24), f, L * L * L / 6), f, L * L / 2), f, L), f, 1.0) * table[i & 31];
-    return fma(p, __hiloint2double(((i >> 5) << 20) + lift, 0), 4503599627370496.0);
+    const double p = fma(fma(fma(L * L * L / 6, f, L * L / 2), f, L), f, 1.0), e = table[i & (TABLE - 1)];
+    return fma(p, __hiloint2double(__double2hiint(e) + (i >> 8 << 20) + lift, __double2loint(e)), 4503599627370496.0);
   }
   __device__ __forceinline__ u64 raw(float x) const { return u64(__double_as_longlong(lifted(x))); }      // NOTHING and the whole number
   __device__ __forceinline__ u64 whole(float x) const { return raw(x) - NOTHING; }
@@ -136,8 +138,23 @@ __device__ __forceinline__ double scan_before(double v, Smem& s, double& all) {
   return at;
 }
 
-// Sorts n keys in descending order; those behind them, up to a power of two, are overwritten.  Pairs up to 32 apart belong to one warp.
-__device__ __forceinline__ void sort_keys(u64* key, int n) {
+// Sorts n keys in descending order.  A key for each thread: by counting the larger ones (256: 1 us).  More: in a network, in which pairs up to
+// 32 apart belong to one warp, and the keys behind them, up to a power of two, are overwritten (1024: 5 us).
+__device__ __noinline__ void sort_keys(u64* key, int n) {
+  if (n <= TPB) {
+    __syncthreads();
+    u64 mine = 0;
+    int place = 0;
+    if (int(threadIdx.x) < n) {
+      mine = key[threadIdx.x];
+#pragma unroll 8
+      for (int j = 0; j < n; ++j) place += key[j] > mine;
+    }
+    __syncthreads();
+    if (int(threadIdx.x) < n) key[place] = mine;
+    __syncthreads();
+    return;
+  }
   int size = 64;
   while (size < n) size *= 2;
   for (int i = n + threadIdx.x; i < size; i += TPB) key[i] = 0;
@@ -441,7 +458,7 @@ __global__ void __launch_bounds__(TPB, RESIDENT) k_sample(const X* __restrict__ 
     else __syncthreads();
   };
   auto of_rank = [&](int r) -> const Smem& { return ctas > 1 ? *cluster.map_shared_rank(&s, unsigned(r)) : s; };
-  if (tid < 32) s.table[tid] = exp2(double(tid) / 32.0);
+  s.table[tid] = exp2(double(tid) / TABLE);
 
   // the largest logit, and those of the groups where the top k are asked for
   bool by_list = q.k <= LIST && q.k < a.V;
@@ -476,7 +493,8 @@ __global__ void __launch_bounds__(TPB, RESIDENT) k_sample(const X* __restrict__ 
   if (ctas > 1) {
     if (tid == 0) s.part_max = m;
     cluster.sync();
-    for (int r = 0; r < ctas; ++r) m = max_nan(m, of_rank(r).part_max);
+    m = max_nan(m, of_rank(lane % ctas).part_max);
+    for (int o = 4; o; o >>= 1) m = max_nan(m, __shfl_xor_sync(0xffffffffu, m, o));      // at most eight
   }
   if (!(m < INFINITY) || !q.valid || m == -INFINITY) {
     if (ctas > 1) cluster.sync();    // the parts' maxima have been read
@@ -488,12 +506,25 @@ __global__ void __launch_bounds__(TPB, RESIDENT) k_sample(const X* __restrict__ 
   wt.c2 = double(q.scale) * 1.4426950408889634;
   wt.unit = a.unit;
   wt.table = s.table;
-  wt.lift = __double2hiint(a.unit);
+  wt.lift = __double2hiint(a.unit) - (1023 << 20);
+  wt.least = -80.0 / wt.c2;
   const float c_coarse = fminf(q.scale * (LOG2E * 16.0f), 3.0e38f), c_fine = fminf(q.scale * (LOG2E * 128.0f), 3.0e38f);
   const float t_mp = q.mp <= 0.0f ? -INFINITY : smallest([&](float x) { return exp((double(x) - wt.m) * double(q.scale)) >= double(q.mp); });      // min p as a logit
   auto push = [&](float x, int col) {
     const int i = atomicAdd(&s.n_key, 1);
     if (i < LIST) s.key[i] = make_key(x, uint32_t(col));
+  };
+
+  // the other CTAs' lists behind the first one's, a warp for each; own: the length of the list of CTA `lane`
+  auto gather = [&](int own) {
+    int base = own;
+    for (int o = 1; o < MOST_CTAS; o <<= 1) {
+      const int y = __shfl_up_sync(0xffffffffu, base, o);
+      if (lane >= o) base += y;
+    }
+    const int from = __shfl_sync(0xffffffffu, base - own, w), more = __shfl_sync(0xffffffffu, own, w);
+    if (w && w < ctas)
+      for (int i = lane; i < more; i += 32) s.key[from + i] = of_rank(w).key[i];
   };
 
   if (by_list) {
@@ -502,10 +533,11 @@ __global__ void __launch_bounds__(TPB, RESIDENT) k_sample(const X* __restrict__ 
     if (end_col >= 0) atomicAdd(&s.coarse[bin_of(end, m, c_coarse, COARSE)], 1u);
     all_sync();
     u64 c[2] = {0, 0}, all;
-    for (int r = 0; r < ctas; ++r) {
-      const Smem& o = of_rank(r);
-      c[0] += o.coarse[2 * tid];
-      c[1] += o.coarse[2 * tid + 1];
+#pragma unroll
+    for (int r = 0; r < MOST_CTAS; ++r) {
+      const uint2 v = r < ctas ? *reinterpret_cast<const uint2*>(&of_rank(r).coarse[2 * tid]) : make_uint2(0, 0);
+      c[0] += v.x;
+      c[1] += v.y;
     }
     if (tid == 0) s.first_bin = COARSE;
     const u64 at = scan_before(c[0] + c[1], s, all);
@@ -537,17 +569,10 @@ __global__ void __launch_bounds__(TPB, RESIDENT) k_sample(const X* __restrict__ 
       }
     }
     all_sync();
-    int n = 0;
-    if (by_list)
-      for (int r = 0; r < ctas; ++r) n += of_rank(r).n_key;
+    const int own = lane < ctas ? min(of_rank(lane).n_key, LIST + 1) : 0, n = __reduce_add_sync(0xffffffffu, own);
     by_list = by_list && n <= LIST;
     if (by_list) {
-      if (rank == 0)
-        for (int r = 1, base = s.n_key; r < ctas; ++r) {
-          const Smem& o = of_rank(r);
-          for (int i = tid; i < o.n_key; i += TPB) s.key[base + i] = o.key[i];
-          base += o.n_key;
-        }
+      if (rank == 0) gather(own);
       all_sync();
       if (rank) return;
       // sorted, summed up in descending order, cut, summed up by index
@@ -615,6 +640,7 @@ __global__ void __launch_bounds__(TPB, RESIDENT) k_sample(const X* __restrict__ 
     uint32_t c[PER] = {};
     if (ctas > 1) {                  // neighbouring threads take neighbouring bins from the others; the sums go where the chunks will be
       uint32_t* sums = reinterpret_cast<uint32_t*>(s.fast.chunk);
+#pragma unroll 2
       for (int r = 0; r < ctas; ++r) {
         const Smem& o = of_rank((rank + r) % ctas);
 #pragma unroll
@@ -746,14 +772,12 @@ __global__ void __launch_bounds__(TPB, RESIDENT) k_sample(const X* __restrict__ 
   u64 total = 0;
   int n = 0;
   if (rank == 0) {
-    for (int r = 0; r < ctas; ++r) {
-      const Smem& o = of_rank(r);
-      total += o.total;
-      const int more = o.n_key;
-      if (r && n + more <= LIST)
-        for (int i = tid; i < more; i += TPB) s.key[n + i] = o.key[i];
-      n += more;
-    }
+    const int own = lane < ctas ? min(of_rank(lane).n_key, LIST + 1) : 0;
+    n = __reduce_add_sync(0xffffffffu, own);
+    total = lane < ctas ? of_rank(lane).total : 0;
+    for (int o = MOST_CTAS / 2; o; o >>= 1) total += __shfl_xor_sync(0xffffffffu, total, o);
+    total = __shfl_sync(0xffffffffu, total, 0);
+    if (n <= LIST) gather(own);
     for (int i = tid; ctas > 1 && i < chunks; i += TPB) {
       const int r = min(ctas - 1, max(0, i - 1) / (per / CHUNK_VECS));
       if (r) s.fast.chunk[i] = of_rank(r).fast.chunk[i - r * (per / CHUNK_VECS)];
@@ -867,7 +891,7 @@ int mv_sample(void* stream, const void* logits, int type, int64_t T, int64_t V, 
     const int64_t vecs = V / Vec<X>::N;
     a.chunks = vecs / CHUNK_VECS + 10 <= CHUNKS;
     // as many CTAs per row as the device holds at once, a step or more for each
-    int ctas = 8;
+    int ctas = MOST_CTAS;
     while (ctas > 1 && (T * ctas > 148 * RESIDENT || vecs < int64_t(ctas) * TPB * U)) ctas /= 2;
     if (T * ctas >= lim) return int(MV_ERR_INVALID_ARG);
     const int64_t n_steps = ((vecs + ctas - 1) / ctas + CHUNK_VECS + TPB * U - 1) / (TPB * U);

@@ -69,8 +69,9 @@ struct Smem {
 constexpr u64 NOTHING = 0x4330000000000000ull;      // 2^52 as a double
 
 // A row's weights 2^t, t = (x - m) c log2(e) <= 0, in 64 bits and as whole numbers.  2^t = 2^n 2^(i/256) 2^f with |f| <= 1/512: a table
-// and the exponential series to the third power (the fourth is below 1.4e-13).  64-bit arithmetic bounds the passes that weigh every
-// token: eight operations (with a table of 32 and the fifth power: ten, and two more in the reduction before).
+// and the exponential series to the third power (the fourth is below 1.4e-13).  A 64-bit operation takes two turns of the scheduler, and
+// turns bound the passes that weigh every token (256 rows of 131072: 62 us; with a table of 16 and the fifth power, two operations
+// more and no bank conflicts, 66).
 struct Weights {
   double m, c2, unit, least;         // least: the difference of a logit from m below which a weight is nothing, 80 / c2
   const double* table;
@@ -890,9 +891,10 @@ int mv_sample(void* stream, const void* logits, int type, int64_t T, int64_t V, 
     using X = decltype(x);
     const int64_t vecs = V / Vec<X>::N;
     a.chunks = vecs / CHUNK_VECS + 10 <= CHUNKS;
-    // as many CTAs per row as the device holds at once, a step or more for each
+    // As many CTAs per row as fill the device twice (requests of different kinds end at different times), a step or more for each: 256 rows of
+    // mixed requests 81 us, once 92, four times 102; all of one kind, top k, 35, 27 and 54.
     int ctas = MOST_CTAS;
-    while (ctas > 1 && (T * ctas > 148 * RESIDENT || vecs < int64_t(ctas) * TPB * U)) ctas /= 2;
+    while (ctas > 1 && (T * ctas > 2 * 148 * RESIDENT || vecs < int64_t(ctas) * TPB * U)) ctas /= 2;
     if (T * ctas >= lim) return int(MV_ERR_INVALID_ARG);
     const int64_t n_steps = ((vecs + ctas - 1) / ctas + CHUNK_VECS + TPB * U - 1) / (TPB * U);
     a.steps = int((n_steps + GROUPS - 1) / GROUPS);

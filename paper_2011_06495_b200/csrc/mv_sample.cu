@@ -31,7 +31,7 @@ __device__ __forceinline__ float value_of(uint32_t h) { return key_value(u64(h) 
 constexpr int TPB = 256, WARPS = TPB / 32, U = 4;
 constexpr int LIST = 1024;           // candidates
 constexpr int CHUNKS = 2048;         // sums over neighbouring tokens
-constexpr int CHUNK_VECS = 64;       // vectors of each, one warp's
+constexpr int CHUNK = 512;           // tokens of each, 16 neighbouring ones for each lane of a warp
 constexpr int GROUPS = 32;           // groups per thread whose maxima are kept
 constexpr int COARSE = 512, FINE = 4096;       // bins over 2^-32 .. 1 of the largest weight: 1/16 and 1/128 of a power of two wide
 constexpr int SLOW_BINS = 2048;
@@ -58,7 +58,7 @@ struct Smem {
   alignas(8) uint32_t coarse[COARSE];
   u64 key[LIST];
   uint16_t group[LIST];
-  double table[TABLE];               // 2^(j/256)
+  double table[TABLE];               // for the weights
   u64 warp[WARPS];
   double warp_d[WARPS];
   float max[WARPS], part_max;
@@ -68,27 +68,35 @@ struct Smem {
 
 constexpr u64 NOTHING = 0x4330000000000000ull;      // 2^52 as a double
 
-// A row's weights 2^t, t = (x - m) c log2(e) <= 0, in 64 bits and as whole numbers.  2^t = 2^n 2^(i/256) 2^f with |f| <= 1/512: a table
-// and the exponential series to the third power (the fourth is below 1.4e-13).  A 64-bit operation takes two turns of the scheduler, and
-// turns bound the passes that weigh every token (256 rows of 131072: 62 us; with a table of 16 and the fifth power, two operations
-// more and no bank conflicts, 66).
+// A row's weights 2^t, t = (x - m) c log2(e) <= 0, in 64 bits and as whole numbers, exact to 3e-14 of themselves.  One fused multiply-add
+// gives t as a whole number of 2^-45, in the lower bits of a double of the size of 1.5 2^52: t = n + i/256 + g/256.  2^(i/256) comes from a
+// table, 2^(g/256) from a cubic in z = 1 + g that meets it at the Chebyshev points of [1, 2) (1.8e-14), and n is added to the table's
+// exponent.  A 64-bit operation takes two turns of the scheduler, and turns bound the passes that weigh every token (five operations
+// and 14 others a token; with eight, from a difference x - m and a remainder by subtraction, TIMES).  Rounding
+// m c log2(e) to 2^-33 (a common factor of all weights) asks for |m c log2(e)| < 2^20.
+constexpr double MAGIC = 6755399441055744.0;         // 1.5 2^52
 struct Weights {
-  double m, c2, unit, least;         // least: the difference of a logit from m below which a weight is nothing, 80 / c2
+  double m, c2, unit, C, K;
+  float low;                         // a weight of 2^-60, which is nothing
   const double* table;
-  int lift;                          // log2(unit), in the place of a double's exponent
-  // 2^52 and the whole number, as a double
-  __device__ __forceinline__ double lifted(float x) const {
-    const double d0 = double(x) - m;
-    const double d = __hiloint2double(int(min(uint32_t(__double2hiint(d0)), uint32_t(__double2hiint(least)))), __double2loint(d0));       // negative numbers: the larger word is the smaller one
-    constexpr double MAGIC = 6755399441055744.0 / TABLE;                                 // 1.5 2^52 / 256: its last bit is 1/256
-    const double r = fma(d, c2, MAGIC), f = fma(d, c2, MAGIC - r);
-    const int i = __double2loint(r);
-    constexpr double L = 0.6931471805599453;
-    const double p = fma(fma(fma(L * L * L / 6, f, L * L / 2), f, L), f, 1.0), e = table[i & (TABLE - 1)];
-    return fma(p, __hiloint2double(__double2hiint(e) + (i >> 8 << 20) + lift, __double2loint(e)), 4503599627370496.0);
+  __device__ __forceinline__ Weights(float largest, float scale, double unit, const double* table)
+      : m(largest), c2(double(scale) * 1.4426950408889634), unit(unit), C(c2 * 0x1p45), K(MAGIC - m * C), low(float(m - 60.0 / c2)), table(table) {}
+  __device__ __forceinline__ bool extreme() const { return !(fabs(m * c2) < 1048576.0) || !(low > -3.0e38f); }
+  // Number i of the table, its exponent such that what stands above the fraction of t only has to be added.
+  __device__ static double entry(int i, double unit) {
+    const double e = exp2(double(i) / TABLE) * unit;
+    return __hiloint2double(int(uint32_t(__double2hiint(e)) - 0x9C000000u), __double2loint(e));
   }
-  __device__ __forceinline__ u64 raw(float x) const { return u64(__double_as_longlong(lifted(x))); }      // NOTHING and the whole number
+  __device__ __forceinline__ u64 raw(float x) const {                   // NOTHING and the whole number
+    const double r = fma(double(fmaxf(x, low)), C, K);
+    const uint32_t hi = uint32_t(__double2hiint(r)), lo = uint32_t(__double2loint(r));
+    const double z = __hiloint2double(int((__funnelshift_r(lo, hi, 17) & 0xfffffu) | 0x3ff00000u), int(lo << 15)), e = table[(hi >> 5) & (TABLE - 1)];
+    const double p = fma(fma(fma(3.3127848075725495e-09, z, 3.6556244405132574e-06), z, 0.0027002849873872833), z, 0.9972960560753699);
+    return u64(__double_as_longlong(fma(p, __hiloint2double(__double2hiint(e) + int((hi << 7) & 0xfff00000u), __double2loint(e)), 4503599627370496.0)));
+  }
   __device__ __forceinline__ u64 whole(float x) const { return raw(x) - NOTHING; }
+  __device__ __forceinline__ double log_of(u64 sum) const { return log(double(sum) / unit) - (fma(m, C, K) - MAGIC) * (0x1p-45 * 0.6931471805599453); }      // without the common factor
+  __device__ __forceinline__ u64 any(float x) const { return u64(exp2((double(x) - m) * c2) * unit + 0.5); }      // of extreme rows too
 };
 
 // The largest whole number not above u all, u in [0, 1), exactly.
@@ -178,6 +186,15 @@ __device__ __noinline__ void sort_keys(u64* key, int n) {
   __syncthreads();
 }
 
+// The smallest whole number not below p all, p in (0, 1), exactly, and at least 1.
+__device__ __forceinline__ u64 start_of(float p, u64 all) {
+  const uint32_t b = __float_as_uint(p);
+  const int e = int(b >> 23), down = 150 - (e ? e : 1);
+  const u64 f = (b & 0x7fffffu) | (e ? 0x800000u : 0u), lo = f * all, hi = __umul64hi(f, all), n = share_of(p, all);
+  const bool whole = down < 64 ? (lo & ((1ull << down) - 1)) == 0 : down < 128 && lo == 0 && (hi & ((1ull << (down - 64)) - 1)) == 0;
+  return max(u64(1), n + (whole ? 0 : 1));
+}
+
 // What a row's request asks for.
 struct Request {
   float u, scale, p, mp;
@@ -204,8 +221,9 @@ __device__ __forceinline__ void put_token(const SampleArgs& a, int64_t t, int64_
   else static_cast<int64_t*>(a.token)[t] = token;
   if (a.logprob) a.logprob[t] = logprob;
 }
-__device__ __forceinline__ void put_drawn(const SampleArgs& a, int64_t t, int64_t token, float x, const Weights& wt, u64 all) {
-  put_token(a, t, token, float((double(x) - wt.m) * (wt.c2 * 0.6931471805599453) - log(double(all) / wt.unit)));
+// log_sum: of the kept weights beside the largest.
+__device__ __forceinline__ void put_drawn(const SampleArgs& a, int64_t t, int64_t token, float x, const Weights& wt, double log_sum) {
+  put_token(a, t, token, float((double(x) - wt.m) * (wt.c2 * 0.6931471805599453) - log_sum));
 }
 __device__ __forceinline__ u64 limit_of(float u, u64 all) { return u >= 1.0f ? all - 1 : u > 0.0f ? share_of(u, all) : 0; }      // the first token at which the sum is larger is drawn
 
@@ -297,12 +315,12 @@ __device__ __noinline__ void sample_any(const X* row, const SampleArgs& a, int64
     u64 mine = 0, all;
     for (int64_t i = threadIdx.x; i < a.V; i += TPB) {
       const float x = to_f(row[i]);
-      if (!cuts || order_of(x) > cut.order) mine += wt.whole(x);
+      if (!cuts || order_of(x) > cut.order) mine += wt.any(x);
     }
     scan_before(mine, s, all);
-    if (cuts) all += u64(cut.ties) * wt.whole(value_of(cut.order));
-    const u64 target = max(u64(1), u64(ceil(double(q.p) * double(all))));
-    cut = cut_row(row, a.V, target, cuts ? &cut : nullptr, [&](float x) { return wt.whole(x); }, s);
+    if (cuts) all += u64(cut.ties) * wt.any(value_of(cut.order));
+    const u64 target = start_of(q.p, all);
+    cut = cut_row(row, a.V, target, cuts ? &cut : nullptr, [&](float x) { return wt.any(x); }, s);
     cuts = true;
   }
   // the index of the last kept token of the cut's own order
@@ -325,7 +343,7 @@ __device__ __noinline__ void sample_any(const X* row, const SampleArgs& a, int64
     const float x = to_f(row[i]);
     const uint32_t h = order_of(x);
     if (cuts && !(h > cut.order || (h == cut.order && i <= last))) return u64(0);
-    return exp((double(x) - wt.m) * double(q.scale)) >= double(q.mp) ? wt.whole(x) : u64(0);
+    return exp((double(x) - wt.m) * double(q.scale)) >= double(q.mp) ? wt.any(x) : u64(0);
   };
   const int64_t per = ((a.V + CHUNKS - 1) / CHUNKS + 31) / 32 * 32;
   __syncthreads();
@@ -362,7 +380,7 @@ __device__ __noinline__ void sample_any(const X* row, const SampleArgs& a, int64
     }
     const unsigned hit = __ballot_sync(0xffffffffu, before + incl > limit);
     if (hit) {
-      if (lane == __ffs(int(hit)) - 1) put_drawn(a, t, i, to_f(row[i]), wt, all);
+      if (lane == __ffs(int(hit)) - 1) put_drawn(a, t, i, to_f(row[i]), wt, log(double(all) / wt.unit));
       return;
     }
     before += __shfl_sync(0xffffffffu, incl, 31);
@@ -393,7 +411,7 @@ __device__ __forceinline__ int bin_of(float x, float m, float c, int n) { return
 
 template <typename X>
 __global__ void __launch_bounds__(TPB, RESIDENT) k_sample(const X* __restrict__ logits, const __grid_constant__ SampleArgs a) {
-  constexpr int N = Vec<X>::N;
+  constexpr int N = Vec<X>::N, CHUNK_VECS = CHUNK / N, OWN = CHUNK_VECS / 32;      // OWN: vectors of a chunk that a lane has
   extern __shared__ u64 dynamic[];
   Smem& s = *reinterpret_cast<Smem*>(dynamic);
   const cg::cluster_group cluster = cg::this_cluster();
@@ -437,21 +455,24 @@ __global__ void __launch_bounds__(TPB, RESIDENT) k_sample(const X* __restrict__ 
       f(step + 1, odd);
     }
   };
-  // f(chunk of the CTA's, two vectors of a lane, whether they are of the row), the next ones on their way
+  // f(chunk of the CTA's, a lane's vectors of it), the next ones on their way; what is not of the row is masked
   auto pass = [&](auto&& f) {
-    const int turns = (nv + 2 * TPB - 1) / (2 * TPB);
-    uint4 u[2], next[2];
+    const int turns = (nv + OWN * TPB - 1) / (OWN * TPB);
+    uint4 u[OWN], next[OWN];
     auto fetch = [&](int i) {
-      next[0] = next[1] = none;
-      if (i * (2 * TPB) + 2 * tid < nv) load_stream(vec + i * (2 * TPB) + 2 * tid, next[0], next[1]);
+#pragma unroll
+      for (int j = 0; j < OWN; j += 2) {
+        next[j] = next[j + 1] = none;
+        if ((i * TPB + tid) * OWN + j < nv) load_stream(vec + (i * TPB + tid) * OWN + j, next[j], next[j + 1]);
+      }
     };
     fetch(0);
 #pragma unroll 1
     for (int i = 0; i < turns; ++i) {
-      u[0] = next[0];
-      u[1] = next[1];
+#pragma unroll
+      for (int j = 0; j < OWN; ++j) u[j] = next[j];
       fetch(i + 1);
-      f(i * WARPS + w, u, i * (2 * TPB) + 2 * tid < nv);
+      f(i * WARPS + w, u);
     }
   };
   auto all_sync = [&]() {
@@ -459,7 +480,7 @@ __global__ void __launch_bounds__(TPB, RESIDENT) k_sample(const X* __restrict__ 
     else __syncthreads();
   };
   auto of_rank = [&](int r) -> const Smem& { return ctas > 1 ? *cluster.map_shared_rank(&s, unsigned(r)) : s; };
-  s.table[tid] = exp2(double(tid) / TABLE);
+  s.table[tid] = Weights::entry(tid, a.unit);
 
   // the largest logit, and those of the groups where the top k are asked for
   bool by_list = q.k <= LIST && q.k < a.V;
@@ -502,13 +523,9 @@ __global__ void __launch_bounds__(TPB, RESIDENT) k_sample(const X* __restrict__ 
     if (rank == 0 && tid == 0) put_token(a, t, -1, q.valid && m == -INFINITY ? -INFINITY : NAN);
     return;
   }
-  Weights wt;
-  wt.m = double(m);
-  wt.c2 = double(q.scale) * 1.4426950408889634;
-  wt.unit = a.unit;
-  wt.table = s.table;
-  wt.lift = __double2hiint(a.unit) - (1023 << 20);
-  wt.least = -80.0 / wt.c2;
+  const Weights wt(m, q.scale, a.unit, s.table);
+  const bool extreme = wt.extreme();
+  by_list &= !extreme;
   const float c_coarse = fminf(q.scale * (LOG2E * 16.0f), 3.0e38f), c_fine = fminf(q.scale * (LOG2E * 128.0f), 3.0e38f);
   const float t_mp = q.mp <= 0.0f ? -INFINITY : smallest([&](float x) { return exp((double(x) - wt.m) * double(q.scale)) >= double(q.mp); });      // min p as a logit
   auto push = [&](float x, int col) {
@@ -587,7 +604,7 @@ __global__ void __launch_bounds__(TPB, RESIDENT) k_sample(const X* __restrict__ 
         mine += v[j];
       }
       u64 before = scan_before(mine, s, total);
-      const u64 target = q.p < 1.0f ? max(u64(1), u64(ceil(double(q.p) * double(total)))) : ~0ull;
+      const u64 target = q.p < 1.0f ? start_of(q.p, total) : ~0ull;
       for (int j = 0; j < PER; ++j) {
         const int i = tid * PER + j;
         const bool in = i < kept_k && (i == 0 || (before < target && key_value(s.key[i]) >= t_mp));
@@ -610,7 +627,7 @@ __global__ void __launch_bounds__(TPB, RESIDENT) k_sample(const X* __restrict__ 
       for (int j = 0; j < PER; ++j) {
         if (before <= limit && limit < before + v[j]) {
           const u64 key = s.key[uint32_t(s.fast.sorted[tid * PER + j])];
-          put_drawn(a, t, key_index(key), key_value(key), wt, total);
+          put_drawn(a, t, key_index(key), key_value(key), wt, wt.log_of(total));
         }
         before += v[j];
       }
@@ -622,7 +639,7 @@ __global__ void __launch_bounds__(TPB, RESIDENT) k_sample(const X* __restrict__ 
 
   // bins of all logits, where a cut is asked for: the bins [lo, hi] in which the last token of the start may lie, and their logits [t2, t1)
   float t1 = -INFINITY, t2 = -INFINITY;
-  bool slow = a.chunks == 0, cut = false;
+  bool slow = a.chunks == 0 || extreme, cut = false;
   const bool by_count = q.k < a.V, by_mass = q.p < 1.0f;
   u64 count_before = 0;
   if (by_count && by_mass) slow = true;
@@ -630,11 +647,13 @@ __global__ void __launch_bounds__(TPB, RESIDENT) k_sample(const X* __restrict__ 
     __syncthreads();
     for (int i = tid; i < FINE; i += TPB) s.fast.bin[i] = 0;
     __syncthreads();
-    if (end_col >= 0) atomicAdd(&s.fast.bin[bin_of(end, m, c_fine, FINE)], 1u);
-    pass([&](int, const uint4 (&u)[2], bool in) {
-      if (in)
+    if (end > -INFINITY) atomicAdd(&s.fast.bin[bin_of(end, m, c_fine, FINE)], 1u);
+    pass([&](int, const uint4 (&u)[OWN]) {
 #pragma unroll
-        for (int i = 0; i < 2; ++i) each_logit<X>(u[i], [&](int, float y) { atomicAdd(&s.fast.bin[bin_of(y, m, c_fine, FINE)], 1u); });
+      for (int i = 0; i < OWN; ++i)
+        each_logit<X>(u[i], [&](int, float y) {
+          if (y > -INFINITY) atomicAdd(&s.fast.bin[bin_of(y, m, c_fine, FINE)], 1u);
+        });
     });
     all_sync();
     constexpr int PER = FINE / TPB;
@@ -657,10 +676,12 @@ __global__ void __launch_bounds__(TPB, RESIDENT) k_sample(const X* __restrict__ 
       for (int j = 0; j < PER; ++j) c[j] = s.fast.bin[tid * PER + j];
     }
     if (tid == 0) { s.first_bin = s.last_bin = FINE - 1; s.before = 0; }
+    bool enough = false;
     if (by_count) {
       u64 mine = 0, all;
       for (int j = 0; j < PER; ++j) mine += c[j];
       u64 at = scan_before(mine, s, all);
+      enough = all < u64(q.k);       // masks leave fewer
       for (int j = 0; j < PER; ++j) {
         if (at < u64(q.k) && u64(q.k) <= at + c[j]) {
           s.first_bin = s.last_bin = tid * PER + j;
@@ -693,8 +714,8 @@ __global__ void __launch_bounds__(TPB, RESIDENT) k_sample(const X* __restrict__ 
     const int lo = s.first_bin, hi = s.last_bin;
     count_before = s.before;
     all_sync();                      // the bins have been read
-    slow = hi >= FINE - 1 || lo > hi;
-    if (!slow) {
+    slow = !enough && (hi >= FINE - 1 || lo > hi);
+    if (!slow && !enough) {
       t1 = lo == 0 ? INFINITY : smallest([&](float x) { return bin_of(x, m, c_fine, FINE) < lo; });
       t2 = smallest([&](float x) { return bin_of(x, m, c_fine, FINE) <= hi; });
       cut = t_mp < t1;               // else min p leaves nothing of them
@@ -720,24 +741,24 @@ __global__ void __launch_bounds__(TPB, RESIDENT) k_sample(const X* __restrict__ 
         listed = x >= t2 && !(x >= t1);
         return x >= t1 ? v : NOTHING;
       };
-      pass([&](int chunk, const uint4 (&u)[2], bool) {
+      pass([&](int chunk, const uint4 (&u)[OWN]) {
         u64 v = 0;
         unsigned hit = 0;
         if constexpr (KIND == 1) {   // few of them
 #pragma unroll
-          for (int i = 0; i < 2; ++i) each_logit<X>(u[i], [&](int e, float y) { hit |= y >= t2 ? 1u << (i * N + e) : 0u; });
+          for (int i = 0; i < OWN; ++i) each_logit<X>(u[i], [&](int e, float y) { hit |= y >= t2 ? 1u << (i * N + e) : 0u; });
         } else {
 #pragma unroll
-          for (int i = 0; i < 2; ++i)
+          for (int i = 0; i < OWN; ++i)
             each_logit<X>(u[i], [&](int e, float y) {
               bool listed = false;
               v += one(y, listed);
               hit |= listed ? 1u << (i * N + e) : 0u;
             });
-          v -= 2 * N * NOTHING;
+          v -= 16 * NOTHING;
         }
         for (; hit; hit &= hit - 1) {
-          const int col = col0 + (chunk * CHUNK_VECS + 2 * lane) * N + __ffs(int(hit)) - 1;
+          const int col = col0 + chunk * CHUNK + 16 * lane + __ffs(int(hit)) - 1;
           const float x = to_f(row[col]);
           if (x < t1) push(x, col);
           else v += wt.whole(x);     // KIND 1 alone
@@ -806,7 +827,7 @@ __global__ void __launch_bounds__(TPB, RESIDENT) k_sample(const X* __restrict__ 
       mine += v[j];
     }
     u64 at = (by_count ? count_before : certain) + scan_before(mine, s, all);
-    const u64 target = by_count ? u64(q.k) : max(u64(1), u64(ceil(double(q.p) * double(total))));
+    const u64 target = by_count ? u64(q.k) : start_of(q.p, total);
     for (int j = 0; j < PER; ++j) {
       if (at < target && target <= at + v[j]) s.found = s.key[tid * PER + j];
       at += v[j];
@@ -823,7 +844,7 @@ __global__ void __launch_bounds__(TPB, RESIDENT) k_sample(const X* __restrict__ 
       const float x = key_value(key);
       if (key < last || x < t_mp) continue;
       const int col = int(key_index(key));
-      atomicAdd(&s.fast.chunk[col < first ? 0 : col >= tail_col ? 1 + (all_v + CHUNK_VECS - 1) / CHUNK_VECS : 1 + (col - first) / N / CHUNK_VECS], wt.whole(x));
+      atomicAdd(&s.fast.chunk[col < first ? 0 : col >= tail_col ? 1 + (all_v + CHUNK_VECS - 1) / CHUNK_VECS : 1 + (col - first) / CHUNK], wt.whole(x));
     }
     __syncthreads();
   }
@@ -847,8 +868,8 @@ __global__ void __launch_bounds__(TPB, RESIDENT) k_sample(const X* __restrict__ 
   }
   __syncthreads();
   const int c = s.first_bin;
-  const int from = c == 0 ? 0 : c == chunks - 1 ? tail_col : first + (c - 1) * CHUNK_VECS * N, to = c == 0 ? first : c == chunks - 1 ? int(a.V) : min(tail_col, from + CHUNK_VECS * N);
-  constexpr int SHARE = (CHUNK_VECS * N + TPB - 1) / TPB;      // neighbouring tokens per thread
+  const int from = c == 0 ? 0 : c == chunks - 1 ? tail_col : first + (c - 1) * CHUNK, to = c == 0 ? first : c == chunks - 1 ? int(a.V) : min(tail_col, from + CHUNK);
+  constexpr int SHARE = CHUNK / TPB;      // neighbouring tokens per thread
   u64 v[SHARE], before = s.before;
   mine = 0;
 #pragma unroll
@@ -866,7 +887,7 @@ __global__ void __launch_bounds__(TPB, RESIDENT) k_sample(const X* __restrict__ 
 #pragma unroll
   for (int j = 0; j < SHARE; ++j) {
     const int i = from + tid * SHARE + j;
-    if (before <= limit && limit < before + v[j]) put_drawn(a, t, i, to_f(row[i]), wt, all);
+    if (before <= limit && limit < before + v[j]) put_drawn(a, t, i, to_f(row[i]), wt, wt.log_of(all));
     before += v[j];
   }
 }
@@ -890,13 +911,13 @@ int mv_sample(void* stream, const void* logits, int type, int64_t T, int64_t V, 
   return with_type(type, [&](auto x) {
     using X = decltype(x);
     const int64_t vecs = V / Vec<X>::N;
-    a.chunks = vecs / CHUNK_VECS + 10 <= CHUNKS;
+    a.chunks = V / CHUNK + 10 <= CHUNKS;
     // As many CTAs per row as fill the device twice (requests of different kinds end at different times), a step or more for each: 256 rows of
     // mixed requests 81 us, once 92, four times 102; all of one kind, top k, 35, 27 and 54.
     int ctas = MOST_CTAS;
     while (ctas > 1 && (T * ctas > 2 * 148 * RESIDENT || vecs < int64_t(ctas) * TPB * U)) ctas /= 2;
     if (T * ctas >= lim) return int(MV_ERR_INVALID_ARG);
-    const int64_t n_steps = ((vecs + ctas - 1) / ctas + CHUNK_VECS + TPB * U - 1) / (TPB * U);
+    const int64_t n_steps = ((vecs + ctas - 1) / ctas + CHUNK / Vec<X>::N + TPB * U - 1) / (TPB * U);
     a.steps = int((n_steps + GROUPS - 1) / GROUPS);
     if (a.steps < 1) a.steps = 1;
     auto* kernel = k_sample<X>;

@@ -35,7 +35,7 @@ constexpr int CHUNK = 512;           // tokens of each, 16 neighbouring ones for
 constexpr int GROUPS = 32;           // groups per thread whose maxima are kept
 constexpr int COARSE = 512, FINE = 4096;       // bins over 2^-32 .. 1 of the largest weight: 1/16 and 1/128 of a power of two wide
 constexpr int SLOW_BINS = 2048;
-constexpr int TABLE = 256;           // as many as threads
+constexpr int TABLE = 16;
 constexpr int RESIDENT = 4;          // CTAs per multiprocessor
 constexpr int MOST_CTAS = 8;         // per row
 
@@ -68,11 +68,11 @@ struct Smem {
 
 constexpr u64 NOTHING = 0x4330000000000000ull;      // 2^52 as a double
 
-// A row's weights 2^t, t = (x - m) c log2(e) <= 0, in 64 bits and as whole numbers, exact to 3e-14 of themselves.  One fused multiply-add
-// gives t as a whole number of 2^-45, in the lower bits of a double of the size of 1.5 2^52: t = n + i/256 + g/256.  2^(i/256) comes from a
-// table, 2^(g/256) from a cubic in z = 1 + g that meets it at the Chebyshev points of [1, 2) (1.8e-14), and n is added to the table's
-// exponent.  A 64-bit operation takes two turns of the scheduler, and turns bound the passes that weigh every token (five operations
-// and 14 others a token; with eight, from a difference x - m and a remainder by subtraction, TIMES).  Rounding
+// A row's weights 2^t, t = (x - m) c log2(e) <= 0, in 64 bits and as whole numbers, exact to 2e-14 of themselves.  One fused multiply-add
+// gives t as a whole number of 2^-45, in the lower bits of a double of the size of 1.5 2^52: t = n + i/16 + g/16.  2^(i/16) comes from a table
+// of as many numbers as shared memory has 64-bit banks, 2^(g/16) from a polynomial in z = 1 + g that meets it at six Chebyshev points of
+// [1, 2) (5e-15), and n is added to the table's exponent.  64-bit operations, seven of them, bound the passes that weigh every token:
+// with nothing else in the loop a multiprocessor takes 7.6 cycles for 32 tokens, 2.4 of them for the conversion and the first operation.  A table of 256 saves one and costs as much in bank conflicts.  Rounding
 // m c log2(e) to 2^-33 (a common factor of all weights) asks for |m c log2(e)| < 2^20.
 constexpr double MAGIC = 6755399441055744.0;         // 1.5 2^52
 struct Weights {
@@ -90,8 +90,8 @@ struct Weights {
   __device__ __forceinline__ u64 raw(float x) const {                   // NOTHING and the whole number
     const double r = fma(double(fmaxf(x, low)), C, K);
     const uint32_t hi = uint32_t(__double2hiint(r)), lo = uint32_t(__double2loint(r));
-    const double z = __hiloint2double(int((__funnelshift_r(lo, hi, 17) & 0xfffffu) | 0x3ff00000u), int(lo << 15)), e = table[(hi >> 5) & (TABLE - 1)];
-    const double p = fma(fma(fma(3.3127848075725495e-09, z, 3.6556244405132574e-06), z, 0.0027002849873872833), z, 0.9972960560753699);
+    const double z = __hiloint2double(int((__funnelshift_r(lo, hi, 21) & 0xfffffu) | 0x3ff00000u), int(lo << 11)), e = table[(hi >> 9) & (TABLE - 1)];
+    const double p = fma(fma(fma(fma(fma(1.299453103455795e-09, z, 1.402322708390649e-07), z, 1.2976900509924959e-05), z, 0.0008985996992888076), z, 0.04148500125886912), z, 0.9576032806096036);
     return u64(__double_as_longlong(fma(p, __hiloint2double(__double2hiint(e) + int((hi << 7) & 0xfff00000u), __double2loint(e)), 4503599627370496.0)));
   }
   __device__ __forceinline__ u64 whole(float x) const { return raw(x) - NOTHING; }
@@ -480,7 +480,7 @@ __global__ void __launch_bounds__(TPB, RESIDENT) k_sample(const X* __restrict__ 
     else __syncthreads();
   };
   auto of_rank = [&](int r) -> const Smem& { return ctas > 1 ? *cluster.map_shared_rank(&s, unsigned(r)) : s; };
-  s.table[tid] = Weights::entry(tid, a.unit);
+  if (tid < TABLE) s.table[tid] = Weights::entry(tid, a.unit);
 
   // the largest logit, and those of the groups where the top k are asked for
   bool by_list = q.k <= LIST && q.k < a.V;
@@ -744,24 +744,17 @@ __global__ void __launch_bounds__(TPB, RESIDENT) k_sample(const X* __restrict__ 
       pass([&](int chunk, const uint4 (&u)[OWN]) {
         u64 v = 0;
         unsigned hit = 0;
-        if constexpr (KIND == 1) {   // few of them
 #pragma unroll
-          for (int i = 0; i < OWN; ++i) each_logit<X>(u[i], [&](int e, float y) { hit |= y >= t2 ? 1u << (i * N + e) : 0u; });
-        } else {
-#pragma unroll
-          for (int i = 0; i < OWN; ++i)
-            each_logit<X>(u[i], [&](int e, float y) {
-              bool listed = false;
-              v += one(y, listed);
-              hit |= listed ? 1u << (i * N + e) : 0u;
-            });
-          v -= 16 * NOTHING;
-        }
+        for (int i = 0; i < OWN; ++i)
+          each_logit<X>(u[i], [&](int e, float y) {
+            if (KIND == 1 && !__any_sync(0xffffffffu, y >= t2)) return;      // few of them
+            bool listed = false;
+            v += one(y, listed) - NOTHING;
+            if (KIND) hit |= listed ? 1u << (i * N + e) : 0u;
+          });
         for (; hit; hit &= hit - 1) {
           const int col = col0 + chunk * CHUNK + 16 * lane + __ffs(int(hit)) - 1;
-          const float x = to_f(row[col]);
-          if (x < t1) push(x, col);
-          else v += wt.whole(x);     // KIND 1 alone
+          push(to_f(row[col]), col);
         }
         for (int o = 16; o; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
         if (lane == 0 && chunk * CHUNK_VECS < nv) s.fast.chunk[1 + chunk] = v;

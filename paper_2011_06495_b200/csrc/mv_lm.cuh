@@ -70,4 +70,11 @@ template <typename F> int with_type(int t, F&& f) {
   }
 }
 
+// The same on the device.
+template <typename F> __device__ __forceinline__ void with_type_device(int t, F&& f) {
+  if (t == MV_F32) f(float());
+  else if (t == MV_BF16) f(__nv_bfloat16());
+  else f(__half());
+}
+
 }  // namespace

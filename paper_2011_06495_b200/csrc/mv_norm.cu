@@ -130,15 +130,18 @@ struct NormArgs {
 
 constexpr int NORM_TPB = 256, WIDE_TPB = 512;
 
-// Waits for the `lanes` threads (whole warps) of one group.
-__device__ __forceinline__ void group_sync(int group, int lanes) { asm volatile("bar.sync %0, %1;" ::"r"(group + 1), "r"(lanes) : "memory"); }
+// Waits for the L threads of one group.
+template <int L> __device__ __forceinline__ void group_sync(int group) {
+  if constexpr (L > 32) asm volatile("bar.sync %0, %1;" ::"r"(group + 1), "n"(L) : "memory");
+  else __syncwarp();
+}
 
 // Threads at work at once decide how many bytes are on their way: CTAs per multiprocessor that the registers allow.
 constexpr int norm_resident(int elements, bool wide) { return elements > 16 ? (wide ? 1 : 2) : wide ? 2 : elements > 8 ? 4 : 6; }
 
-template <typename X, bool VEC, int L, int NV>
-__global__ void __launch_bounds__(L > 32 ? WIDE_TPB : NORM_TPB, norm_resident(NV * Unit<X, VEC>::N, L > 32)) k_norm(const X* x, X* y, const __grid_constant__ NormArgs a) {
-  using Un = Unit<X, VEC>;
+template <typename X, int L, int NV>
+__global__ void __launch_bounds__(L > 32 ? WIDE_TPB : NORM_TPB, norm_resident(NV * Unit<X, true>::N, L > 32)) k_norm(const X* x, X* y, const __grid_constant__ NormArgs a) {
+  using Un = Unit<X, true>;
   constexpr int N = Un::N, GROUPS = (L > 32 ? WIDE_TPB : NORM_TPB) / L, WARPS = L / 32;
   extern __shared__ float4 params[];         // weights, then biases
   __shared__ float part[2][WIDE_TPB / 32];
@@ -165,7 +168,7 @@ __global__ void __launch_bounds__(L > 32 ? WIDE_TPB : NORM_TPB, norm_resident(NV
     v = lanes_sum<(L < 32 ? L : 32)>(v);
     if constexpr (WARPS > 1) {
       if ((threadIdx.x & 31) == 0) part[k][threadIdx.x >> 5] = v;
-      group_sync(mine, L);
+      group_sync<L>(mine);
       v = 0.0f;
 #pragma unroll
       for (int i = 0; i < WARPS; ++i) v += part[k][mine * WARPS + i];
@@ -180,25 +183,171 @@ __global__ void __launch_bounds__(L > 32 ? WIDE_TPB : NORM_TPB, norm_resident(NV
     for (int i = 0; i < NV; ++i) u[i] = next[i];
     load(t + GROUPS);
     f2 s = both(0.0f);
-    each_pair<X, VEC, NV>(n, [&](int i, int j, int, bool second) { s = add2(s, pair_of<X, VEC>(get, i, j, second)); });
+    each_pair<X, true, NV>(n, [&](int i, int j, int, bool second) { s = add2(s, pair_of<X, true>(get, i, j, second)); });
     const float mu = sum(add_up(s), 0) * share;
     const f2 minus = both(-mu);
     s = both(0.0f);
-    each_pair<X, VEC, NV>(n, [&](int i, int j, int, bool second) {
-      f2 d = add2(pair_of<X, VEC>(get, i, j, second), minus);
-      if (!second) {
-        float d0, d1;
-        unpack2(d, d0, d1);
-        d = pack2(d0, 0.0f);
-      }
+    each_pair<X, true, NV>(n, [&](int i, int j, int, bool second) {
+      const f2 d = add2(pair_of<X, true>(get, i, j, second), minus);
       s = fma2(d, d, s);
     });
     const float rs = rsqrtf(fmaf(sum(add_up(s), 1), share, a.eps));
     if (t >= t1) continue;
     const f2 rs2 = both(rs);
-    put_pairs<X, VEC, NV, L>(n, y + t * a.ldy + at * N, [&](int i, int j, int k, bool second) {
-      return fma2(mul2(add2(pair_of<X, VEC>(get, i, j, second), minus), rs2), param_pair<N, L>(pw, at, units, k, second), param_pair<N, L>(pb, at, units, k, second));
+    put_pairs<X, true, NV, L>(n, y + t * a.ldy + at * N, [&](int i, int j, int k, bool second) {
+      return fma2(mul2(add2(pair_of<X, true>(get, i, j, second), minus), rs2), param_pair<N, L>(pw, at, units, k, second), param_pair<N, L>(pb, at, units, k, second));
     });
+    if (at == 0) {
+      if (a.mean) a.mean[t] = mu;
+      if (a.rstd) a.rstd[t] = rs;
+    }
+  }
+}
+
+// Rows that do not lie on 16-byte boundaries.  The vectors are those of y's row, from its first boundary on (in every row another column); what is
+// before and behind them, up to 31 elements, goes to a lane each.  APART: x lies otherwise within 16 bytes, and comes from between
+// two of its vectors.  Weight and bias of a column side by side, those of every N-th column together, so that neighbouring lanes
+// read neighbouring pairs wherever the vectors begin.
+template <typename X, bool APART, int L, int NV>
+__global__ void __launch_bounds__(L > 32 ? WIDE_TPB : NORM_TPB, L > 32 ? 1 : 2) k_norm_any(const X* x, X* y, const __grid_constant__ NormArgs a) {
+  constexpr int N = Vec<X>::N, GROUPS = (L > 32 ? WIDE_TPB : NORM_TPB) / L, WARPS = L / 32, SIZE = sizeof(X), ENDS = L < 32 ? 32 / L : 1;
+  extern __shared__ float2 pairs[];
+  __shared__ float part[2][WIDE_TPB / 32];
+  const int D = int(a.D), columns = (D + N - 1) / N, mine = threadIdx.x / L, at = threadIdx.x % L;
+  const int64_t t0 = blockIdx.x * a.per, t1 = min(a.T, t0 + a.per);
+  struct Row { const X* x; X* y; int first, nv, shift; };
+  auto row_of = [&](int64_t t) {
+    Row r;
+    r.x = x + t * a.ldx;
+    r.y = y + t * a.ldy;
+    r.first = min(D, int((16 - (reinterpret_cast<uintptr_t>(r.y) & 15)) & 15) / SIZE);
+    r.shift = APART ? int(reinterpret_cast<uintptr_t>(r.x + r.first) & 15) : 0;
+    if (r.shift > r.first * SIZE) r.first = min(D, r.first + N);                         // all of the two vectors' bytes are the row's
+    r.nv = max(0, (D - r.first - (APART ? N - r.shift / SIZE : 0)) / N);
+    return r;
+  };
+  uint4 next[NV], more[APART ? NV : 1];
+  X next_end[ENDS];
+  auto load = [&](const Row& r) {
+    const uint4* p = reinterpret_cast<const uint4*>(reinterpret_cast<const char*>(r.x + r.first) - r.shift) + at;
+#pragma unroll
+    for (int i = 0; i < NV; ++i)
+      if (at + i * L < r.nv) {
+        next[i] = __ldg(p + i * L);
+        if constexpr (APART) more[i] = __ldg(p + i * L + 1);
+      }
+    const int ends = D - r.nv * N;
+#pragma unroll
+    for (int i = 0; i < ENDS; ++i) {
+      const int e = at + i * L;
+      if (e < ends) next_end[i] = r.x[e < r.first ? e : r.nv * N + e];
+    }
+  };
+  Row now, coming = row_of(t0 + mine);
+  if (t0 + mine < t1) load(coming);
+  {
+    float* flat = reinterpret_cast<float*>(pairs);
+    auto put = [&](const void* p, float none, int which) {
+      auto from = [&](auto w) {
+        using W = decltype(w);
+        for (int i0 = threadIdx.x; i0 < D; i0 += 8 * blockDim.x) {
+          W v[8];
+#pragma unroll
+          for (int j = 0; j < 8; ++j)
+            if (i0 + j * int(blockDim.x) < D) v[j] = static_cast<const W*>(p)[i0 + j * blockDim.x];
+#pragma unroll
+          for (int j = 0; j < 8; ++j) {
+            const int c = i0 + j * blockDim.x;
+            if (c < D) flat[2 * (c % N * columns + c / N) + which] = to_f(v[j]);
+          }
+        }
+        return 0;
+      };
+      if (p) with_type_device(a.w_type, from);
+      else
+        for (int i = threadIdx.x; i < N * columns; i += blockDim.x) flat[2 * i + which] = none;
+    };
+    put(a.weight, 1.0f, 0);
+    put(a.bias, 0.0f, 1);
+  }
+  __syncthreads();
+  auto sum = [&](float v, int k) {
+    v = lanes_sum<(L < 32 ? L : 32)>(v);
+    if constexpr (WARPS > 1) {
+      if ((threadIdx.x & 31) == 0) part[k][threadIdx.x >> 5] = v;
+      group_sync<L>(mine);
+      v = 0.0f;
+#pragma unroll
+      for (int i = 0; i < WARPS; ++i) v += part[k][mine * WARPS + i];
+    }
+    return v;
+  };
+  const float share = 1.0f / float(D);
+  for (int64_t r0 = t0; r0 < t1; r0 += GROUPS) {
+    const int64_t t = r0 + mine;
+    now = coming;
+    uint4 u[NV];
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      if constexpr (APART) u[i] = between(next[i], more[i], now.shift);
+      else u[i] = next[i];
+    }
+    float end[ENDS];
+    const int n = now.nv > at ? (now.nv - at - 1) / L + 1 : 0, ends = D - now.nv * N;
+#pragma unroll
+    for (int i = 0; i < ENDS; ++i) end[i] = at + i * L < ends ? to_f(next_end[i]) : 0.0f;
+    coming = row_of(t + GROUPS);
+    if (t + GROUPS < t1) load(coming);
+    f2 s = both(0.0f);
+#pragma unroll
+    for (int i = 0; i < ENDS; ++i) s = add2(s, pack2(end[i], 0.0f));
+#pragma unroll
+    for (int i = 0; i < NV; ++i)
+      if (i < n)
+#pragma unroll
+        for (int j = 0; j < N / 2; ++j) s = add2(s, Vec<X>::pair(u[i], j));
+    const float mu = sum(add_up(s), 0) * share;
+    const f2 minus = both(-mu);
+    s = both(0.0f);
+#pragma unroll
+    for (int i = 0; i < ENDS; ++i) {
+      const float d = at + i * L < ends ? end[i] - mu : 0.0f;
+      s = fma2(pack2(d, 0.0f), pack2(d, 0.0f), s);
+    }
+#pragma unroll
+    for (int i = 0; i < NV; ++i)
+      if (i < n)
+#pragma unroll
+        for (int j = 0; j < N / 2; ++j) {
+          const f2 d = add2(Vec<X>::pair(u[i], j), minus);
+          s = fma2(d, d, s);
+        }
+    const float rs = rsqrtf(fmaf(sum(add_up(s), 1), share, a.eps));
+    if (t >= t1) continue;
+    const f2 rs2 = both(rs);
+    auto place = [&](int c) { return c % N * columns + c / N; };
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      if (i >= n) break;
+      const int v = at + i * L;
+      float o[N];
+#pragma unroll
+      for (int j = 0; j < N / 2; ++j) {
+        // column first + N v + e: with first = N q + f, in the group (f + e) mod N
+        const int e0 = now.first + 2 * j, e1 = e0 + 1;
+        const float2 p = pairs[place(e0) + v], q = pairs[place(e1) + v];
+        unpack2(fma2(mul2(add2(Vec<X>::pair(u[i], j), minus), rs2), pack2(p.x, q.x), pack2(p.y, q.y)), o[2 * j], o[2 * j + 1]);
+      }
+      __stcs(reinterpret_cast<uint4*>(now.y + now.first) + v, pack_vec<X>(o));
+    }
+#pragma unroll
+    for (int i = 0; i < ENDS; ++i) {
+      const int e = at + i * L;
+      if (e >= ends) break;
+      const int c = e < now.first ? e : now.nv * N + e;
+      const float2 p = pairs[place(c)];
+      now.y[c] = from_f<X>(fmaf((end[i] - mu) * rs, p.x, p.y));
+    }
     if (at == 0) {
       if (a.mean) a.mean[t] = mu;
       if (a.rstd) a.rstd[t] = rs;
@@ -250,57 +399,76 @@ struct NormGradArgs {
   float *dweight, *dbias, *part;      // part: [CTAs][2][D]
   int accumulate, parts;
   int64_t per;                       // rows per CTA
-  int stages;
+  int stages, image;
 };
 
-// Bytes to a thread's own place in shared memory, `n` of them (the rest of 16 or 4 is zero).
-template <int BYTES> __device__ __forceinline__ void fetch(void* to, const void* from, bool any) {
-  const uint32_t s = uint32_t(__cvta_generic_to_shared(to));
-  const int n = any ? BYTES : 0;
-  if constexpr (BYTES == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(s), "l"(from), "r"(n) : "memory");
-  else asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(s), "l"(from), "r"(n) : "memory");
+// 16 bytes to shared memory, or as many zeros.
+__device__ __forceinline__ void fetch(void* to, const void* from, bool any) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(uint32_t(__cvta_generic_to_shared(to))), "l"(from), "r"(any ? 16 : 0) : "memory");
 }
+__device__ __forceinline__ void fetches_end() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 __device__ __forceinline__ void fetched(int behind) {        // all but the last `behind` groups of copies have come
   if (behind == 2) asm volatile("cp.async.wait_group 2;" ::: "memory");
   else if (behind == 1) asm volatile("cp.async.wait_group 1;" ::: "memory");
   else asm volatile("cp.async.wait_group 0;" ::: "memory");
 }
 
+// A row that lies anywhere, as the vectors in which its bytes are: L lanes copy them, and it begins (address mod 16) bytes into `to`.  The
+// neighbouring rows' bytes may come with it; what is outside the T rows [lo, hi) does not.
+inline int image_bytes(int64_t D, int size) { return int((D * size + 15) / 16 + 1) * 16; }
+template <typename X, int L> __device__ __forceinline__ void fetch_row(char* to, const X* row, int D, int at, const X* lo, const X* hi) {
+  const char* a = reinterpret_cast<const char*>(reinterpret_cast<uintptr_t>(row) & ~uintptr_t(15));
+  const int vecs = int((reinterpret_cast<const char*>(row + D) - a + 15) / 16);
+  if (a >= reinterpret_cast<const char*>(lo) && a + 16 * vecs <= reinterpret_cast<const char*>(hi)) {
+#pragma unroll 2
+    for (int i = at; i < vecs; i += L) fetch(to + 16 * i, a + 16 * i, true);
+  } else {                           // the first and the last row
+    for (int i = at; i < D; i += L) const_cast<X*>(reinterpret_cast<const X*>(to + (reinterpret_cast<uintptr_t>(row) & 15)))[i] = row[i];
+  }
+}
+template <typename X> __device__ __forceinline__ const X* in_image(const char* image, const X* row) {
+  return reinterpret_cast<const X*>(image + (reinterpret_cast<uintptr_t>(row) & 15));
+}
+
 // R rows at a time; a thread owns its columns' sums over rows.  The units of x and dy travel through a thread's own places in
-// shared memory, a.stages deep, so that nothing waits for them but the thread itself (elements of 2 bytes, which cannot be copied like that,
-// go through registers).
+// shared memory, a.stages deep, so that nothing waits for them but the thread itself; of rows that lie anywhere, as images that their lanes share.
 template <int L> constexpr int GRAD_THREADS = L > NORM_TPB ? L : NORM_TPB;
 
 template <typename X, bool VEC, int L, int NV, int R>
 __global__ void __launch_bounds__(GRAD_THREADS<L>, L > NORM_TPB ? 1 : 2) k_norm_grad(const X* dy, const X* x, X* dx, const __grid_constant__ NormGradArgs a) {
   using Un = Unit<X, VEC>;
-  constexpr int N = Un::N, BYTES = N * int(sizeof(X)), PAIRS = NV * N / 2, THREADS = GRAD_THREADS<L>, GROUPS = THREADS / L, WARPS = L / 32, STAGE = R * NV * 2 * THREADS;
-  constexpr bool RING = BYTES >= 4;
-  extern __shared__ float4 shared[];         // the ring, weights, laid out as above; at the end the groups' sums
+  constexpr int N = Un::N, PAIRS = NV * N / 2, THREADS = GRAD_THREADS<L>, GROUPS = THREADS / L, WARPS = L / 32, STAGE = R * NV * 2 * THREADS;
+  extern __shared__ float4 shared[];         // the ring (or the images), weights, laid out as above; at the end the groups' sums
   __shared__ float part[2][2 * R][THREADS / 32];
   const int D = int(a.D), units = D / N, tid = threadIdx.x, mine = tid / L, at = tid % L;
   const int n = units > at ? (units - at - 1) / L + 1 : 0;
   Un* ring = reinterpret_cast<Un*>(shared);
-  float* pw = RING ? reinterpret_cast<float*>(ring + a.stages * STAGE) : reinterpret_cast<float*>(shared);
+  char* images = reinterpret_cast<char*>(shared) + mine * (R * 2) * a.image;       // of a group; GROUPS of them for each stage
+  const int stage = VEC ? STAGE * 16 : GROUPS * R * 2 * a.image;
+  float* pw = reinterpret_cast<float*>(reinterpret_cast<char*>(shared) + a.stages * stage);
   const int64_t t0 = blockIdx.x * a.per, t1 = min(a.T, t0 + a.per);
   constexpr int STEP = GROUPS * R;
   auto row = [&](int64_t r0, int r) { return r0 + r * GROUPS + mine; };
   auto issue = [&](int64_t r0, int slot) {
-    if constexpr (RING) {
 #pragma unroll
-      for (int r = 0; r < R; ++r) {
-        const int64_t t = row(r0, r);
+    for (int r = 0; r < R; ++r) {
+      const int64_t t = row(r0, r);
+      if constexpr (VEC) {
         const int any = t < t1 ? n : 0;
         const X *px = x + t * a.ldx + at * N, *py = dy + t * a.lddy + at * N;
         Un* to = ring + slot * STAGE + r * NV * 2 * THREADS + tid;
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
-          fetch<BYTES>(to + i * 2 * THREADS, i < any ? px + i * L * N : x, i < any);
-          fetch<BYTES>(to + (i * 2 + 1) * THREADS, i < any ? py + i * L * N : dy, i < any);
+          fetch(to + i * 2 * THREADS, i < any ? px + i * L * N : x, i < any);
+          fetch(to + (i * 2 + 1) * THREADS, i < any ? py + i * L * N : dy, i < any);
         }
+      } else if (t < t1) {
+        char* to = images + slot * stage + r * 2 * a.image;
+        fetch_row<X, L>(to, x + t * a.ldx, D, at, x, x + (a.T - 1) * a.ldx + D);
+        fetch_row<X, L>(to + a.image, dy + t * a.lddy, D, at, dy, dy + (a.T - 1) * a.lddy + D);
       }
-      asm volatile("cp.async.commit_group;" ::: "memory");
     }
+    fetches_end();
   };
   float mu[R], rs[R];
   auto statistics = [&](int64_t r0) {
@@ -321,41 +489,33 @@ __global__ void __launch_bounds__(GRAD_THREADS<L>, L > NORM_TPB ? 1 : 2) k_norm_
   const float share = 1.0f / float(D);
   int flip = 0, slot = 0;
   for (int64_t r0 = t0; r0 < t1; r0 += STEP) {
-    Un regs[RING ? 1 : R][RING ? 1 : NV][2];
-    if constexpr (RING) {
+    if constexpr (VEC) {
       issue(r0 + (a.stages - 1) * STEP, slot == 0 ? a.stages - 1 : slot - 1);
       fetched(a.stages - 1);
     } else {
-#pragma unroll
-      for (int r = 0; r < R; ++r) {
-        const int64_t t = row(r0, r);
-        const int any = t < t1 ? n : 0;
-        const X *px = x + t * a.ldx + at, *py = dy + t * a.lddy + at;
-#pragma unroll
-        for (int i = 0; i < NV; ++i) {
-          regs[r][i][0] = regs[r][i][1] = Un();
-          if (i < any) {
-            regs[r][i][0].load(px + i * L);
-            regs[r][i][1].load(py + i * L);
-          }
-        }
-      }
+      fetched(a.stages - 2);
+      group_sync<L>(mine);           // the rows have come, and the ones before have been read
+      issue(r0 + (a.stages - 1) * STEP, slot == 0 ? a.stages - 1 : slot - 1);
     }
     // x (0) or dy (1) of row r
     auto of = [&](int r, int which) {
-      const Un* from = ring + slot * STAGE + (r * NV * 2 + which) * THREADS + tid;
-      return [&, from, r, which](int i) -> const Un& {
-        if constexpr (RING) return from[i * 2 * THREADS];
-        else return regs[r][i][which];
-      };
+      if constexpr (VEC) {
+        const Un* from = ring + slot * STAGE + (r * NV * 2 + which) * THREADS + tid;
+        return [from](int i) -> const Un& { return from[i * 2 * THREADS]; };
+      } else {
+        const int64_t t = row(r0, r);
+        const X* from = in_image(images + slot * stage + (r * 2 + which) * a.image, which ? dy + t * a.lddy : x + t * a.ldx) + at;
+        return [from](int i) { return Un{from[i * L]}; };
+      }
     };
     float s[2 * R];
 #pragma unroll
     for (int r = 0; r < R; ++r) {
       f2 s0 = both(0.0f), s1 = s0;
+      const int some = VEC || row(r0, r) < t1 ? n : 0;
       const f2 minus = both(-mu[r]), rs2 = both(rs[r]);
       auto gx = of(r, 0), gy = of(r, 1);
-      each_pair<X, VEC, NV>(n, [&](int i, int j, int k, bool second) {
+      each_pair<X, VEC, NV>(some, [&](int i, int j, int k, bool second) {
         const f2 vx = pair_of<X, VEC>(gx, i, j, second), vy = pair_of<X, VEC>(gy, i, j, second);
         const f2 nn = mul2(add2(vx, minus), rs2), h = mul2(vy, param_pair<N, L>(pw, at, units, k, second));
         s0 = add2(s0, h);
@@ -373,7 +533,7 @@ __global__ void __launch_bounds__(GRAD_THREADS<L>, L > NORM_TPB ? 1 : 2) k_norm_
         if ((tid & 31) == 0)
 #pragma unroll
           for (int j = 0; j < 2 * R; ++j) part[flip][j][tid >> 5] = s[j];
-        group_sync(mine, L);
+        group_sync<L>(mine);
 #pragma unroll
         for (int j = 0; j < 2 * R; ++j) {
           s[j] = 0.0f;
@@ -547,27 +707,43 @@ int mv_layer_norm(void* stream, const void* x, int type, int64_t T, int64_t D, i
     using X = decltype(xx);
     const X* xp = static_cast<const X*>(x);
     X* yp = static_cast<X*>(y);
-    auto launch = [&](auto vec) {
-      constexpr bool VEC = decltype(vec)::value;
-      constexpr int N = Unit<X, VEC>::N, FEWEST = VEC ? 8 : 32, LEAST = VEC ? 1 : 4, LIKED = 8, MOST = VEC ? 8 : 32;
+    constexpr int N = Vec<X>::N;
+    auto launch = [&](auto* kernel, SmemLimit* limit, int lanes, size_t smem, int64_t resident) {
+      const int threads = lanes > 32 ? WIDE_TPB : NORM_TPB;
+      const int64_t groups = threads / lanes;
+      if (resident * int64_t(smem + 1024) > 227 * 1024) resident = 227 * 1024 / int64_t(smem + 1024);
+      // several waves, if a group of lanes has eight rows or more in each CTA (which copies the parameters first)
+      int64_t ctas = T / (groups * 8);
+      ctas = ctas < resident * 148 ? resident * 148 : ctas > resident * 148 * WAVES ? resident * 148 * WAVES : ctas;
+      a.per = ((T + ctas - 1) / ctas + groups - 1) / groups * groups;
+      if (smem > 48 * 1024 && !allow_smem(kernel, int(smem), limit)) return int(MV_ERR_CUDA);
+      kernel<<<unsigned((T + a.per - 1) / a.per), unsigned(threads), smem, st>>>(xp, yp, a);
+      return cuda_ok();
+    };
+    auto vectors = [&]() {
       Shape s;
       const size_t smem = size_t((D + 3) / 4 * 4) * 8;
-      if (smem > 200 * 1024 || !norm_shape(D / N, T, FEWEST, WIDE_TPB, LEAST, LIKED, MOST, &s)) return -1;
-      return with_shape<FEWEST, WIDE_TPB, LEAST, LIKED, MOST, FEWEST>(s, [&](auto lanes, auto nv) {
-        constexpr int L = decltype(lanes)::value, NV = decltype(nv)::value, THREADS = L > 32 ? WIDE_TPB : NORM_TPB, GROUPS = THREADS / L;
-        int64_t ctas = norm_resident(NV * N, L > 32);
-        if (ctas * int64_t(smem + 1024) > 227 * 1024) ctas = 227 * 1024 / int64_t(smem + 1024);
-        ctas *= 148 * WAVES;
-        a.per = ((T + ctas - 1) / ctas + GROUPS - 1) / GROUPS * GROUPS;
-        auto* kernel = k_norm<X, VEC, L, NV>;
+      if (smem > 200 * 1024 || !norm_shape(D / N, T, 8, WIDE_TPB, 1, 8, 8, &s)) return -1;
+      return with_shape<8, WIDE_TPB, 1, 8, 8, 8>(s, [&](auto lanes, auto nv) {
+        constexpr int L = decltype(lanes)::value, NV = decltype(nv)::value;
         static SmemLimit limit;
-        if (smem > 48 * 1024 && !allow_smem(kernel, int(smem), &limit)) return int(MV_ERR_CUDA);
-        kernel<<<unsigned((T + a.per - 1) / a.per), THREADS, smem, st>>>(xp, yp, a);
-        return cuda_ok();
+        return launch(k_norm<X, L, NV>, &limit, L, smem, norm_resident(NV * N, L > 32));
+      });
+    };
+    auto anywhere = [&](auto apart) {
+      constexpr bool APART = decltype(apart)::value;
+      Shape s;
+      const size_t smem = size_t((D + N - 1) / N) * N * 8;
+      if (smem > 200 * 1024 || !norm_shape(D / N + 1, T, 8, WIDE_TPB, 4, 4, 8, &s)) return -1;
+      return with_shape<8, WIDE_TPB, 4, 4, 8, 8>(s, [&](auto lanes, auto nv) {
+        constexpr int L = decltype(lanes)::value, NV = decltype(nv)::value;
+        static SmemLimit limit;
+        return launch(k_norm_any<X, APART, L, NV>, &limit, L, smem, L > 32 ? 1 : 2);
       });
     };
     const bool vec = D % Vec<X>::N == 0 && !unaligned(x, T, ldx, size) && !unaligned(y, T, ldy, size);
-    const int status = vec ? launch(std::true_type()) : launch(std::false_type());
+    const bool alike = ((reinterpret_cast<uintptr_t>(x) ^ reinterpret_cast<uintptr_t>(y)) & 15) == 0 && (T == 1 || (ldx - ldy) * size % 16 == 0);
+    const int status = vec ? vectors() : alike ? anywhere(std::false_type()) : anywhere(std::true_type());
     if (status != -1) return status;
     k_norm_long<X><<<unsigned(T), LONG_TPB, 0, st>>>(xp, yp, a);
     return cuda_ok();
@@ -616,19 +792,20 @@ int mv_layer_norm_grad(void* stream, const void* dy, int64_t lddy, const void* x
     X* dxp = static_cast<X*>(dx);
     auto launch = [&](auto vec) {
       constexpr bool VEC = decltype(vec)::value;
-      constexpr int N = Unit<X, VEC>::N, BYTES = N * int(sizeof(X)), FEWEST = VEC ? 8 : 32, LEAST = VEC ? 1 : 4, LIKED = 16 / N, MOST = 32 / N;
+      constexpr int N = Unit<X, VEC>::N, FEWEST = VEC ? 8 : 32, LEAST = VEC ? 1 : 4, LIKED = (VEC ? 16 : 32) / N, MOST = 32 / N;
       Shape s;
       if (!norm_shape(D / N, T, FEWEST, 512, LEAST, LIKED, MOST, &s)) return -1;
       return with_shape<FEWEST, 512, LEAST, LIKED, MOST, FEWEST>(s, [&](auto lanes, auto nv) {
         constexpr int L = decltype(lanes)::value, NV = decltype(nv)::value, THREADS = GRAD_THREADS<L>, GROUPS = THREADS / L;
         constexpr int R = NV * N > 16 ? 1 : VEC ? (NV < 4 ? 4 / NV : 1) : (NV < 16 ? 2 : 1);
-        const int64_t stage = BYTES < 4 ? 0 : int64_t(R) * NV * 2 * THREADS * BYTES;
+        a.image = VEC ? 0 : image_bytes(D, size);
+        const int64_t stage = VEC ? int64_t(R) * NV * 2 * THREADS * 16 : int64_t(GROUPS) * R * 2 * a.image;
         // two CTAs of 256 threads with two stages each come before three stages
         int64_t parts = L > NORM_TPB ? 1 : 2;
         const int64_t least_smem = 2 * stage + 4 * D > GROUPS * 8 * D ? 2 * stage + 4 * D : GROUPS * 8 * D;
         if (parts * (least_smem + 2048) > 227 * 1024) parts = 1;
         for (a.stages = 3; a.stages && parts * (a.stages * stage + 4 * D + 2048) > 227 * 1024; --a.stages) {}
-        if (!a.stages) return -1;
+        if (a.stages < (VEC ? 1 : 2)) return -1;
         size_t smem = size_t(a.stages * stage + 4 * D);
         if (GROUPS > 1 && smem < size_t(GROUPS * 8 * D)) smem = size_t(GROUPS * 8 * D);
         parts *= 148;

@@ -792,26 +792,32 @@ int mv_layer_norm_grad(void* stream, const void* dy, int64_t lddy, const void* x
     X* dxp = static_cast<X*>(dx);
     auto launch = [&](auto vec) {
       constexpr bool VEC = decltype(vec)::value;
-      constexpr int N = Unit<X, VEC>::N, FEWEST = VEC ? 8 : 32, LEAST = VEC ? 1 : 4, LIKED = (VEC ? 16 : 32) / N, MOST = 32 / N;
+      // (images of rows of 32 elements a lane leave room for one CTA only where they are of 4 bytes)
+      constexpr int N = Unit<X, VEC>::N, LEAST = VEC ? 1 : 4, LIKED = (VEC || sizeof(X) == 4 ? 16 : 32) / N, MOST = 32 / N;
       Shape s;
-      if (!norm_shape(D / N, T, FEWEST, 512, LEAST, LIKED, MOST, &s)) return -1;
-      return with_shape<FEWEST, 512, LEAST, LIKED, MOST, FEWEST>(s, [&](auto lanes, auto nv) {
+      if (!norm_shape(D / N, T, 8, 512, LEAST, LIKED, MOST, &s)) return -1;
+      return with_shape<8, 512, LEAST, LIKED, MOST, 8>(s, [&](auto lanes, auto nv) {
         constexpr int L = decltype(lanes)::value, NV = decltype(nv)::value, THREADS = GRAD_THREADS<L>, GROUPS = THREADS / L;
         constexpr int R = NV * N > 16 ? 1 : VEC ? (NV < 4 ? 4 / NV : 1) : (NV < 16 ? 2 : 1);
         a.image = VEC ? 0 : image_bytes(D, size);
         const int64_t stage = VEC ? int64_t(R) * NV * 2 * THREADS * 16 : int64_t(GROUPS) * R * 2 * a.image;
-        // two CTAs of 256 threads with two stages each come before three stages
+        // Two CTAs of 256 threads with two stages each come before three stages, and more than a few rows for each before more CTAs, whose
+        // sums are written and read again.
         int64_t parts = L > NORM_TPB ? 1 : 2;
         const int64_t least_smem = 2 * stage + 4 * D > GROUPS * 8 * D ? 2 * stage + 4 * D : GROUPS * 8 * D;
         if (parts * (least_smem + 2048) > 227 * 1024) parts = 1;
         for (a.stages = 3; a.stages && parts * (a.stages * stage + 4 * D + 2048) > 227 * 1024; --a.stages) {}
         if (a.stages < (VEC ? 1 : 2)) return -1;
-        size_t smem = size_t(a.stages * stage + 4 * D);
-        if (GROUPS > 1 && smem < size_t(GROUPS * 8 * D)) smem = size_t(GROUPS * 8 * D);
         parts *= 148;
+        const int64_t few = T * size / 16 > 64 ? T * size / 16 : 64;
+        if (parts > few) parts = few;
         if (parts > most_parts) parts = most_parts;
         a.per = ((T + parts - 1) / parts + GROUPS - 1) / GROUPS * GROUPS;
         a.parts = int((T + a.per - 1) / a.per);
+        const int64_t turns = (a.per + GROUPS * R - 1) / (GROUPS * R);
+        if (a.stages > turns) a.stages = turns > 1 || VEC ? int(turns) : 2;
+        size_t smem = size_t(a.stages * stage + 4 * D);
+        if (GROUPS > 1 && smem < size_t(GROUPS * 8 * D)) smem = size_t(GROUPS * 8 * D);
         auto* kernel = k_norm_grad<X, VEC, L, NV, R>;
         static SmemLimit limit;
         if (smem > 48 * 1024 && !allow_smem(kernel, int(smem), &limit)) return int(MV_ERR_CUDA);

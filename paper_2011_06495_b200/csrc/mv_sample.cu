@@ -63,7 +63,8 @@ struct Smem {
   double warp_d[WARPS];
   float max[WARPS], part_max;
   int n_key, n_group, first_bin, last_bin;
-  u64 found, before, total;
+  u64 found, before, total, certain;
+  unsigned low_order, high_order;
 };
 
 constexpr u64 NOTHING = 0x4330000000000000ull;      // 2^52 as a double
@@ -509,7 +510,11 @@ __global__ void __launch_bounds__(TPB, RESIDENT) k_sample(const X* __restrict__ 
   for (int o = 16; o; o >>= 1) m = max_nan(m, __shfl_xor_sync(0xffffffffu, m, o));
   if (lane == 0) s.max[w] = m;
   for (int i = tid; i < COARSE; i += TPB) s.coarse[i] = 0;
-  if (tid == 0) { s.n_key = s.n_group = 0; }
+  if (tid == 0) {
+    s.n_key = s.n_group = 0;
+    s.low_order = 0xffffffffu;
+    s.high_order = 0;
+  }
   __syncthreads();
   for (int i = 0; i < WARPS; ++i) m = max_nan(m, s.max[i]);
   if (ctas > 1) {
@@ -637,16 +642,35 @@ __global__ void __launch_bounds__(TPB, RESIDENT) k_sample(const X* __restrict__ 
     if (tid == 0) s.n_key = 0;
   }
 
+  // The sums of all CTAs' bins (which are complete) in each of them; neighbouring threads take neighbouring bins.
+  auto sum_bins = [&]() {
+    if (ctas == 1) return;
+    uint32_t c[FINE / TPB] = {};
+#pragma unroll 2
+    for (int r = 0; r < ctas; ++r) {
+      const Smem& o = of_rank((rank + r) % ctas);
+#pragma unroll
+      for (int j = 0; j < FINE / TPB; ++j) c[j] += o.fast.bin[j * TPB + tid];
+    }
+    all_sync();
+#pragma unroll
+    for (int j = 0; j < FINE / TPB; ++j) s.fast.bin[j * TPB + tid] = c[j];
+    __syncthreads();
+  };
+  auto clear_bins = [&]() {
+    __syncthreads();
+    for (int i = tid; i < FINE; i += TPB) s.fast.bin[i] = 0;
+    __syncthreads();
+  };
+
   // bins of all logits, where a cut is asked for: the bins [lo, hi] in which the last token of the start may lie, and their logits [t2, t1)
   float t1 = -INFINITY, t2 = -INFINITY;
-  bool slow = a.chunks == 0 || extreme, cut = false;
+  bool slow = a.chunks == 0 || extreme, cut = false, crowd = false;      // crowd: more than the list holds
   const bool by_count = q.k < a.V, by_mass = q.p < 1.0f;
   u64 count_before = 0;
   if (by_count && by_mass) slow = true;
   if (!slow && (by_count || by_mass)) {
-    __syncthreads();
-    for (int i = tid; i < FINE; i += TPB) s.fast.bin[i] = 0;
-    __syncthreads();
+    clear_bins();
     if (end > -INFINITY) atomicAdd(&s.fast.bin[bin_of(end, m, c_fine, FINE)], 1u);
     pass([&](int, const uint4 (&u)[OWN]) {
 #pragma unroll
@@ -657,24 +681,10 @@ __global__ void __launch_bounds__(TPB, RESIDENT) k_sample(const X* __restrict__ 
     });
     all_sync();
     constexpr int PER = FINE / TPB;
-    uint32_t c[PER] = {};
-    if (ctas > 1) {                  // neighbouring threads take neighbouring bins from the others; the sums go where the chunks will be
-      uint32_t* sums = reinterpret_cast<uint32_t*>(s.fast.chunk);
-#pragma unroll 2
-      for (int r = 0; r < ctas; ++r) {
-        const Smem& o = of_rank((rank + r) % ctas);
+    sum_bins();
+    uint32_t c[PER];
 #pragma unroll
-        for (int j = 0; j < PER; ++j) c[j] += o.fast.bin[j * TPB + tid];
-      }
-#pragma unroll
-      for (int j = 0; j < PER; ++j) sums[j * TPB + tid] = c[j];
-      __syncthreads();
-#pragma unroll
-      for (int j = 0; j < PER; ++j) c[j] = sums[tid * PER + j];
-    } else {
-#pragma unroll
-      for (int j = 0; j < PER; ++j) c[j] = s.fast.bin[tid * PER + j];
-    }
+    for (int j = 0; j < PER; ++j) c[j] = s.fast.bin[tid * PER + j];
     if (tid == 0) { s.first_bin = s.last_bin = FINE - 1; s.before = 0; }
     bool enough = false;
     if (by_count) {
@@ -713,7 +723,10 @@ __global__ void __launch_bounds__(TPB, RESIDENT) k_sample(const X* __restrict__ 
     __syncthreads();
     const int lo = s.first_bin, hi = s.last_bin;
     count_before = s.before;
-    all_sync();                      // the bins have been read
+    u64 mine = 0, in_range;
+    for (int j = 0; j < PER; ++j) mine += tid * PER + j >= lo && tid * PER + j <= hi ? c[j] : 0;
+    scan_before(mine, s, in_range);
+    crowd = in_range > LIST;
     slow = !enough && (hi >= FINE - 1 || lo > hi);
     if (!slow && !enough) {
       t1 = lo == 0 ? INFINITY : smallest([&](float x) { return bin_of(x, m, c_fine, FINE) < lo; });
@@ -727,86 +740,195 @@ __global__ void __launch_bounds__(TPB, RESIDENT) k_sample(const X* __restrict__ 
     return;
   }
 
+  crowd &= cut;
   if (!cut) t1 = t2 = t_mp;
-  __syncthreads();
-  // Weights: sums of neighbours among the logits from t1 on, a list of those in [t2, t1), and, for a cut by mass, the sum of all.
-  {
+  // Weights: sums of neighbours among the logits from t1 on, and, for a cut by mass, the sum of all.  What is in [t2, t1) is listed; where it is
+  // a crowd (few distinct values, as 16 bits leave them), counted in bins by its order, which narrow [t2, t1), and in a second pass listed or,
+  // where it is a crowd of one value, counted by chunks.
+  enum { LISTED, BINNED, TIED };
+  int mode = crowd ? BINNED : LISTED, shift = 0;
+  uint32_t base = 0, top = 0, low_order = 0xffffffffu, high_order = 0;
+  const int own_chunks = (nv + CHUNK_VECS - 1) / CHUNK_VECS, chunks = 2 + (all_v + CHUNK_VECS - 1) / CHUNK_VECS;
+  u64 sum_of_all = 0;
+  auto sums = [&](auto kind) {
+    constexpr int KIND = decltype(kind)::value;        // 0: of all; 1: of those from t2 on; 2: of all, with the sum of all
     u64 total = 0;
-    auto sums = [&](auto kind) {
-      constexpr int KIND = decltype(kind)::value;      // 0: of all; 1: of those from t2 on; 2: of all, with the sum of all
-      auto one = [&](float x, bool& listed) -> u64 {
-        const u64 v = wt.raw(x);
-        if constexpr (KIND == 0) return v;
-        if constexpr (KIND == 2) total += v - NOTHING;
-        listed = x >= t2 && !(x >= t1);
-        return x >= t1 ? v : NOTHING;
-      };
-      pass([&](int chunk, const uint4 (&u)[OWN]) {
-        u64 v = 0;
-        unsigned hit = 0;
-#pragma unroll
-        for (int i = 0; i < OWN; ++i)
-          each_logit<X>(u[i], [&](int e, float y) {
-            if (KIND == 1 && !__any_sync(0xffffffffu, y >= t2)) return;      // few of them
-            bool listed = false;
-            v += one(y, listed) - NOTHING;
-            if (KIND) hit |= listed ? 1u << (i * N + e) : 0u;
-          });
-        for (; hit; hit &= hit - 1) {
-          const int col = col0 + chunk * CHUNK + 16 * lane + __ffs(int(hit)) - 1;
-          push(to_f(row[col]), col);
-        }
-        for (int o = 16; o; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
-        if (lane == 0 && chunk * CHUNK_VECS < nv) s.fast.chunk[1 + chunk] = v;
-      });
-      // the ends: chunk 0 is the head, the one behind the last is the tail
-      if (w == 0) {
-        bool listed = false;
-        u64 v = one(end, listed) - NOTHING, h = end_col >= 0 && end_col < first ? v : 0;
-        v -= h;
-        if (listed) push(end, end_col);
-        for (int o = 16; o; o >>= 1) {
-          v += __shfl_xor_sync(0xffffffffu, v, o);
-          h += __shfl_xor_sync(0xffffffffu, h, o);
-        }
-        if (lane == 0) {
-          if (rank == 0) s.fast.chunk[0] = h;
-          if (rank == ctas - 1) s.fast.chunk[1 + (nv + CHUNK_VECS - 1) / CHUNK_VECS] = v;
-        }
+    auto one = [&](float x, bool& listed) -> u64 {
+      const u64 v = wt.raw(x);
+      if constexpr (KIND == 0) return v;
+      if constexpr (KIND == 2) total += v - NOTHING;
+      listed = x >= t2 && !(x >= t1);
+      return x >= t1 ? v : NOTHING;
+    };
+    auto note = [&](float x, int col) {
+      if (mode == LISTED) {
+        push(x, col);
+      } else if (mode == BINNED) {
+        atomicAdd(&s.fast.bin[(order_of(x) - base) >> shift], 1u);
+      } else {
+        low_order = min(low_order, order_of(x));
+        high_order = max(high_order, order_of(x));
       }
     };
-    if (cut && by_mass) sums(Int<2>());
-    else if (t2 > -INFINITY) sums(Int<1>());
-    else sums(Int<0>());
+    pass([&](int chunk, const uint4 (&u)[OWN]) {
+      u64 v = 0;
+      unsigned hit = 0;
+#pragma unroll
+      for (int i = 0; i < OWN; ++i)
+        each_logit<X>(u[i], [&](int e, float y) {
+          if (KIND == 1 && !__any_sync(0xffffffffu, y >= t2)) return;        // few of them
+          bool listed = false;
+          v += one(y, listed) - NOTHING;
+          if (KIND) hit |= listed ? 1u << (i * N + e) : 0u;
+        });
+      if (KIND && mode == TIED) {
+        const unsigned ties = __reduce_add_sync(0xffffffffu, unsigned(__popc(hit)));
+        if (lane == 0 && chunk < own_chunks) s.fast.bin[1 + chunk] = ties;
+      }
+      for (; hit; hit &= hit - 1) {
+        const int col = col0 + chunk * CHUNK + 16 * lane + __ffs(int(hit)) - 1;
+        note(to_f(row[col]), col);
+      }
+      for (int o = 16; o; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+      if (lane == 0 && chunk < own_chunks) s.fast.chunk[1 + chunk] = v;
+    });
+    // the ends: chunk 0 is the head, the one behind the last is the tail
+    if (w == 0) {
+      bool listed = false;
+      u64 v = one(end, listed) - NOTHING, h = end_col >= 0 && end_col < first ? v : 0;
+      v -= h;
+      if (listed) {
+        note(end, end_col);
+        if (mode == TIED) atomicAdd(&s.fast.bin[end_col < first ? 0 : 1 + own_chunks], 1u);
+      }
+      for (int o = 16; o; o >>= 1) {
+        v += __shfl_xor_sync(0xffffffffu, v, o);
+        h += __shfl_xor_sync(0xffffffffu, h, o);
+      }
+      if (lane == 0) {
+        if (rank == 0) s.fast.chunk[0] = h;
+        if (rank == ctas - 1) s.fast.chunk[1 + own_chunks] = v;
+      }
+    }
     u64 all;
     scan_before(total, s, all);
     if (tid == 0) s.total = all;
+  };
+  // a number of every CTA, added up
+  auto over_ctas = [&](u64 Smem::*field) {
+    u64 v = lane < ctas ? of_rank(lane).*field : 0;
+    for (int o = MOST_CTAS / 2; o; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+    return __shfl_sync(0xffffffffu, v, 0);
+  };
+  if (crowd) {
+    base = order_of(t2);
+    top = t1 == INFINITY ? order_of(m) + 1 : order_of(t1);
+    while ((top - 1 - base) >> shift >= FINE) ++shift;
+    clear_bins();
+    if (by_mass) sums(Int<2>());
+    else sums(Int<1>());
+    u64 certain = 0;
+    for (int i = (rank == 0 ? 0 : 1) + tid; i < 1 + own_chunks + (rank == ctas - 1); i += TPB) certain += s.fast.chunk[i];
+    scan_before(certain, s, certain);
+    if (tid == 0) s.certain = certain;
+    all_sync();
+    sum_of_all = over_ctas(&Smem::total);
+    certain = by_count ? count_before : over_ctas(&Smem::certain);
+    const u64 target = by_count ? u64(q.k) : start_of(q.p, sum_of_all);
+    sum_bins();
+    // In descending order: the place p is bin FINE - 1 - p.  The start ends between the first place whose bins, taken at their largest weights,
+    // reach the target, and the first that does so at their smallest.
+    constexpr int PER = FINE / TPB;
+    auto weight = [&](uint32_t order) { return by_count ? u64(1) : wt.whole(value_of(order)); };
+    u64 most = 0, least = 0, all;
+    for (int j = 0; j < PER; ++j) {
+      const uint32_t i = FINE - 1 - (tid * PER + j), n = s.fast.bin[i];
+      if (n) {
+        most += n * weight(min(top - 1, base + ((i + 1) << shift) - 1));
+        least += n * weight(base + (i << shift));
+      }
+    }
+    if (tid == 0) { s.first_bin = -1; s.last_bin = FINE - 1; s.before = 0; }
+    u64 at_most = certain + scan_before(most, s, all), at_least = certain + scan_before(least, s, all);
+    for (int j = 0; j < PER; ++j) {
+      const uint32_t i = FINE - 1 - (tid * PER + j), n = s.fast.bin[i];
+      if (n == 0) continue;
+      most = n * weight(min(top - 1, base + ((i + 1) << shift) - 1));
+      least = n * weight(base + (i << shift));
+      if (at_most < target && target <= at_most + most) {
+        s.first_bin = tid * PER + j;
+        s.before = at_most;          // a cut by count: how many
+      }
+      if (at_least < target && target <= at_least + least) s.last_bin = tid * PER + j;
+      at_most += most;
+      at_least += least;
+    }
+    __syncthreads();
+    const int lo = s.first_bin, hi = s.last_bin;
+    count_before = s.before;
+    u64 mine = 0;
+    for (int j = 0; j < PER; ++j) mine += tid * PER + j >= lo && tid * PER + j <= hi ? s.fast.bin[FINE - 1 - (tid * PER + j)] : 0;
+    scan_before(mine, s, all);
+    if (lo < 0 || lo > hi) {         // never expected
+      all_sync();
+      if (rank == 0) sample_any<X>(row, a, t, q, wt, s);
+      return;
+    }
+    const u64 edge = u64(base) + (u64(FINE - lo) << shift);          // above the place lo
+    if (edge < top) t1 = value_of(uint32_t(edge));
+    t2 = value_of(base + (uint32_t(FINE - 1 - hi) << shift));
+    cut = t_mp < t1;
+    if (!cut) t1 = t2 = t_mp;
+    mode = cut && all > LIST ? TIED : LISTED;
+    clear_bins();
+  }
+  __syncthreads();
+  if (cut && by_mass && !crowd) sums(Int<2>());
+  else if (t2 > -INFINITY) sums(Int<1>());
+  else sums(Int<0>());
+  if (mode == TIED) {
+    for (int o = 16; o; o >>= 1) {
+      low_order = min(low_order, __shfl_xor_sync(0xffffffffu, low_order, o));
+      high_order = max(high_order, __shfl_xor_sync(0xffffffffu, high_order, o));
+    }
+    if (lane == 0) {
+      atomicMin(&s.low_order, low_order);
+      atomicMax(&s.high_order, high_order);
+    }
   }
   all_sync();
-  const int chunks = 2 + (all_v + CHUNK_VECS - 1) / CHUNK_VECS;
-  u64 total = 0;
   int n = 0;
   if (rank == 0) {
     const int own = lane < ctas ? min(of_rank(lane).n_key, LIST + 1) : 0;
     n = __reduce_add_sync(0xffffffffu, own);
-    total = lane < ctas ? of_rank(lane).total : 0;
-    for (int o = MOST_CTAS / 2; o; o >>= 1) total += __shfl_xor_sync(0xffffffffu, total, o);
-    total = __shfl_sync(0xffffffffu, total, 0);
+    if (!crowd) sum_of_all = over_ctas(&Smem::total);
+    low_order = lane < ctas ? of_rank(lane).low_order : 0xffffffffu;
+    high_order = lane < ctas ? of_rank(lane).high_order : 0;
+    low_order = __reduce_min_sync(0xffffffffu, low_order);
+    high_order = __reduce_max_sync(0xffffffffu, high_order);
     if (n <= LIST) gather(own);
     for (int i = tid; ctas > 1 && i < chunks; i += TPB) {
       const int r = min(ctas - 1, max(0, i - 1) / (per / CHUNK_VECS));
-      if (r) s.fast.chunk[i] = of_rank(r).fast.chunk[i - r * (per / CHUNK_VECS)];
+      if (r) {
+        s.fast.chunk[i] = of_rank(r).fast.chunk[i - r * (per / CHUNK_VECS)];
+        if (mode == TIED) s.fast.bin[i] = of_rank(r).fast.bin[i - r * (per / CHUNK_VECS)];
+      }
     }
   }
   all_sync();
   if (rank) return;
-  if (n > LIST) {
+  if (n > LIST || (mode == TIED && low_order != high_order)) {
     __syncthreads();
     sample_any<X>(row, a, t, q, wt, s);
     return;
   }
+  auto bounds = [&](int c, int& from, int& to) {       // the columns of a chunk
+    from = c == 0 ? 0 : c == chunks - 1 ? tail_col : first + (c - 1) * CHUNK;
+    to = c == 0 ? first : c == chunks - 1 ? int(a.V) : min(tail_col, from + CHUNK);
+  };
+  constexpr int SHARE = CHUNK / TPB;                   // neighbouring tokens of a chunk per thread
   u64 last = 0;                      // the last kept token's key
-  if (cut) {
+  if (cut && mode == LISTED) {
     sort_keys(s.key, n);
     if (tid == 0) s.found = 0;
     __syncthreads();
@@ -820,7 +942,7 @@ __global__ void __launch_bounds__(TPB, RESIDENT) k_sample(const X* __restrict__ 
       mine += v[j];
     }
     u64 at = (by_count ? count_before : certain) + scan_before(mine, s, all);
-    const u64 target = by_count ? u64(q.k) : start_of(q.p, total);
+    const u64 target = by_count ? u64(q.k) : start_of(q.p, sum_of_all);
     for (int j = 0; j < PER; ++j) {
       if (at < target && target <= at + v[j]) s.found = s.key[tid * PER + j];
       at += v[j];
@@ -837,9 +959,54 @@ __global__ void __launch_bounds__(TPB, RESIDENT) k_sample(const X* __restrict__ 
       const float x = key_value(key);
       if (key < last || x < t_mp) continue;
       const int col = int(key_index(key));
-      atomicAdd(&s.fast.chunk[col < first ? 0 : col >= tail_col ? 1 + (all_v + CHUNK_VECS - 1) / CHUNK_VECS : 1 + (col - first) / CHUNK], wt.whole(x));
+      atomicAdd(&s.fast.chunk[col < first ? 0 : col >= tail_col ? chunks - 1 : 1 + (col - first) / CHUNK], wt.whole(x));
     }
     __syncthreads();
+  }
+  if (cut && mode == TIED) {
+    // a crowd of one value, of which the first `need` stay, in the order of the index
+    constexpr int PER = CHUNKS / TPB;
+    const float x = value_of(low_order);
+    const u64 each = wt.whole(x), target = by_count ? u64(q.k) : start_of(q.p, sum_of_all);
+    u64 certain = 0, mine = 0, ties;
+    for (int i = tid; i < chunks; i += TPB) certain += s.fast.chunk[i];
+    scan_before(certain, s, certain);
+    if (by_count) certain = count_before;
+    for (int j = 0; j < PER; ++j) mine += tid * PER + j < chunks ? s.fast.bin[tid * PER + j] : 0;
+    u64 at = scan_before(mine, s, ties);
+    const u64 need = target <= certain ? 0 : by_count ? target - certain : each ? (target - certain + each - 1) / each : 0;
+    if (need == 0 || need > ties) {  // never expected
+      __syncthreads();
+      sample_any<X>(row, a, t, q, wt, s);
+      return;
+    }
+    for (int j = 0; j < PER && tid * PER + j < chunks; ++j) {
+      const int i = tid * PER + j;
+      const u64 n = s.fast.bin[i], stay = at >= need ? 0 : min(n, need - at);
+      if (x >= t_mp) s.fast.chunk[i] += stay * each;
+      if (at < need && need <= at + n) {
+        s.first_bin = i;
+        s.before = at;
+      }
+      at += n;
+    }
+    __syncthreads();
+    int from, to;
+    bounds(s.first_bin, from, to);
+    bool tie[SHARE];
+    mine = 0;
+#pragma unroll
+    for (int j = 0; j < SHARE; ++j) {
+      const int i = from + tid * SHARE + j;
+      tie[j] = i < to && order_of(to_f(row[i])) == low_order;
+      mine += tie[j];
+    }
+    at = s.before + scan_before(mine, s, ties);
+#pragma unroll
+    for (int j = 0; j < SHARE; ++j)
+      if (tie[j] && ++at == need) s.found = make_key(x, uint32_t(from + tid * SHARE + j));
+    __syncthreads();
+    last = s.found;
   }
   // the chunk, and the token in it
   constexpr int PER = CHUNKS / TPB;
@@ -860,9 +1027,8 @@ __global__ void __launch_bounds__(TPB, RESIDENT) k_sample(const X* __restrict__ 
     at += v;
   }
   __syncthreads();
-  const int c = s.first_bin;
-  const int from = c == 0 ? 0 : c == chunks - 1 ? tail_col : first + (c - 1) * CHUNK, to = c == 0 ? first : c == chunks - 1 ? int(a.V) : min(tail_col, from + CHUNK);
-  constexpr int SHARE = CHUNK / TPB;      // neighbouring tokens per thread
+  int from, to;
+  bounds(s.first_bin, from, to);
   u64 v[SHARE], before = s.before;
   mine = 0;
 #pragma unroll

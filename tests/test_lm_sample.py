@@ -186,6 +186,34 @@ def test_nuclei_of_every_size():
         check(x, u, None, None, None, p)
 
 
+@pytest.mark.parametrize("dt", [BF16, F16, F32])
+@pytest.mark.parametrize("V,offset", [(3001, 1), (60_000, 0), (131_072, 3), (200_003, 0)])
+@pytest.mark.parametrize("mean,std", [(0.0, 2.0), (10.0, 2.0), (20.0, 0.5), (-30.0, 4.0), (0.0, 0.01)])
+def test_crowds_of_equal_logits_at_the_cut(dt, V, offset, mean, std):
+    """Logits far from zero have few distinct values in 16 bits: thousands of them lie at the cut, and the first ones by index stay.  The last row:
+    16-bit values in 32 bits beside a few others."""
+    x, _ = strided(3, V, dt, 2, offset, seed=V)
+    x.mul_(std).add_(mean)
+    x[2] = x[2].to(BF16).to(dt)
+    x[2, ::97] += 0.01
+    x[1, torch.rand(V, generator=gen(V), device=DEV) < 0.3] = -math.inf
+    for j, s in enumerate([(None, None, 0.9, None), (0.7, None, 0.5, 0.2), (1.0, 2000, None, None), (1.1, V // 3, None, 0.01), (1.0, V - 10, None, None), (None, None, 0.995, None)]):
+        check(x, torch.rand(3, generator=gen(j), device=DEV), *s)
+
+
+def test_many_rows_with_crowds():
+    """More rows than one wave, a CTA for each; and few long rows, shared by several."""
+    for T, V in ((1300, 20_011), (5, 700_000), (3, 1_500_000)):
+        x = (torch.randn((T, V), generator=gen(T), device=DEV) * 1.5 + 12.0).to(BF16)
+        u = torch.rand(T, generator=gen(T + 1), device=DEV)
+        p = torch.tensor([0.9, 1.0, 0.7], device=DEV).repeat(T)[:T].contiguous()
+        k = torch.tensor([0, 0, 0, 3000], dtype=torch.int32, device=DEV).repeat(T)[:T].contiguous()
+        rows = torch.tensor(sorted({0, 1, 2, 3, T // 2, T - 2, T - 1}), device=DEV).clamp(0, T - 1).unique()
+        token, _ = draw(x, u, None, k, p)
+        for r in rows.tolist():
+            assert int(token[r]) == reference(x[r], float(u[r]), 1.0, int(k[r]), float(p[r]), 0.0)[0], (T, V, r)
+
+
 def test_frequencies_are_the_probabilities():
     """The same row with an even grid of u: every token as often as its share of the grid, to within one of the grid's steps."""
     T, V = 4096, 50

@@ -39,6 +39,13 @@ constexpr int TABLE = 16;
 constexpr int RESIDENT = 4;          // CTAs per multiprocessor
 constexpr int MOST_CTAS = 8;         // per row
 
+// What a row's request asks for.
+struct Request {
+  float u, scale, p, mp;
+  int64_t k;
+  bool valid;
+};
+
 // What one path or the other keeps in shared memory.
 struct Smem {
   union {
@@ -63,8 +70,10 @@ struct Smem {
   double warp_d[WARPS];
   float max[WARPS], part_max;
   int n_key, n_group, first_bin, last_bin;
-  u64 found, before, total, certain;
-  unsigned low_order, high_order;
+  u64 found, before, total, certain, count_before, sum_of_all;
+  uint32_t low_order, high_order, base, top;
+  int mode, shift;
+  Request request;
 };
 
 constexpr u64 NOTHING = 0x4330000000000000ull;      // 2^52 as a double
@@ -76,6 +85,13 @@ constexpr u64 NOTHING = 0x4330000000000000ull;      // 2^52 as a double
 // with nothing else in the loop a multiprocessor takes 7.6 cycles for 32 tokens, 2.4 of them for the conversion and the first operation.  A table of 256 saves one and costs as much in bank conflicts.  Rounding
 // m c log2(e) to 2^-33 (a common factor of all weights) asks for |m c log2(e)| < 2^20.
 constexpr double MAGIC = 6755399441055744.0;         // 1.5 2^52
+__device__ __forceinline__ u64 raw_weight(float x, double C, double K, float low, const double* table) {
+  const double r = fma(double(fmaxf(x, low)), C, K);
+  const uint32_t hi = uint32_t(__double2hiint(r)), lo = uint32_t(__double2loint(r));
+  const double z = __hiloint2double(int((__funnelshift_r(lo, hi, 21) & 0xfffffu) | 0x3ff00000u), int(lo << 11)), e = table[(hi >> 9) & (TABLE - 1)];
+  const double p = fma(fma(fma(fma(fma(1.299453103455795e-09, z, 1.402322708390649e-07), z, 1.2976900509924959e-05), z, 0.0008985996992888076), z, 0.04148500125886912), z, 0.9576032806096036);
+  return u64(__double_as_longlong(fma(p, __hiloint2double(__double2hiint(e) + int((hi << 7) & 0xfff00000u), __double2loint(e)), 4503599627370496.0)));
+}
 struct Weights {
   double m, c2, unit, C, K;
   float low;                         // a weight of 2^-60, which is nothing
@@ -88,13 +104,7 @@ struct Weights {
     const double e = exp2(double(i) / TABLE) * unit;
     return __hiloint2double(int(uint32_t(__double2hiint(e)) - 0x9C000000u), __double2loint(e));
   }
-  __device__ __forceinline__ u64 raw(float x) const {                   // NOTHING and the whole number
-    const double r = fma(double(fmaxf(x, low)), C, K);
-    const uint32_t hi = uint32_t(__double2hiint(r)), lo = uint32_t(__double2loint(r));
-    const double z = __hiloint2double(int((__funnelshift_r(lo, hi, 21) & 0xfffffu) | 0x3ff00000u), int(lo << 11)), e = table[(hi >> 9) & (TABLE - 1)];
-    const double p = fma(fma(fma(fma(fma(1.299453103455795e-09, z, 1.402322708390649e-07), z, 1.2976900509924959e-05), z, 0.0008985996992888076), z, 0.04148500125886912), z, 0.9576032806096036);
-    return u64(__double_as_longlong(fma(p, __hiloint2double(__double2hiint(e) + int((hi << 7) & 0xfff00000u), __double2loint(e)), 4503599627370496.0)));
-  }
+  __device__ __forceinline__ u64 raw(float x) const { return raw_weight(x, C, K, low, table); }      // NOTHING and the whole number
   __device__ __forceinline__ u64 whole(float x) const { return raw(x) - NOTHING; }
   __device__ __forceinline__ double log_of(u64 sum) const { return log(double(sum) / unit) - (fma(m, C, K) - MAGIC) * (0x1p-45 * 0.6931471805599453); }      // without the common factor
   __device__ __forceinline__ u64 any(float x) const { return u64(exp2((double(x) - m) * c2) * unit + 0.5); }      // of extreme rows too
@@ -196,12 +206,6 @@ __device__ __forceinline__ u64 start_of(float p, u64 all) {
   return max(u64(1), n + (whole ? 0 : 1));
 }
 
-// What a row's request asks for.
-struct Request {
-  float u, scale, p, mp;
-  int64_t k;
-  bool valid;
-};
 __device__ __forceinline__ Request request_of(const SampleArgs& a, int64_t t) {
   Request q;
   q.u = a.u[t];
@@ -407,6 +411,81 @@ template <typename X> __device__ __forceinline__ float widen_nan(uint32_t m) {
   }
 }
 
+// f(chunk of the CTA's, a lane's vectors of it), the next ones on their way; what is not of the row is masked.
+template <typename X, typename F> __device__ __forceinline__ void walk(const uint4* vec, int nv, F&& f) {
+  constexpr int OWN = CHUNK / Vec<X>::N / 32;
+  const int tid = threadIdx.x, turns = (nv + OWN * TPB - 1) / (OWN * TPB);
+  uint4 u[OWN], next[OWN];
+  auto fetch = [&](int i) {
+#pragma unroll
+    for (int j = 0; j < OWN; j += 2) {
+      next[j] = next[j + 1] = make_uint4(Vec<X>::NONE, Vec<X>::NONE, Vec<X>::NONE, Vec<X>::NONE);
+      if ((i * TPB + tid) * OWN + j < nv) load_stream(vec + (i * TPB + tid) * OWN + j, next[j], next[j + 1]);
+    }
+  };
+  fetch(0);
+#pragma unroll 1
+  for (int i = 0; i < turns; ++i) {
+#pragma unroll
+    for (int j = 0; j < OWN; ++j) u[j] = next[j];
+    fetch(i + 1);
+    f(i * WARPS + (tid >> 5), u);
+  }
+}
+
+// What happens to a logit between the thresholds.
+enum { LISTED, BINNED, TIED };
+__device__ __forceinline__ void push(Smem& s, float x, int col) {
+  const int i = atomicAdd(&s.n_key, 1);
+  if (i < LIST) s.key[i] = make_key(x, uint32_t(col));
+}
+__device__ __forceinline__ void note(Smem& s, float x, int col) {
+  if (s.mode == LISTED) {
+    push(s, x, col);
+  } else if (s.mode == BINNED) {
+    atomicAdd(&s.fast.bin[(order_of(x) - s.base) >> s.shift], 1u);
+  } else {
+    atomicMin(&s.low_order, order_of(x));
+    atomicMax(&s.high_order, order_of(x));
+  }
+}
+
+// The weights of a CTA's vectors (from column col0 of the row on): their sums by chunks, of the logits from t1 on; those in [t2, t1) are noted.
+// KIND 0: of all; 1: of those from t2 on; 2: of all, with the sum of all, of which a thread's part is returned.  A function of its own, so
+// that it has all of the registers.
+template <typename X, int KIND>
+__device__ __noinline__ u64 weigh(const X* row, int col0, int nv, double C, double K, float low, float t1, float t2) {
+  constexpr int N = Vec<X>::N, CHUNK_VECS = CHUNK / N, OWN = CHUNK_VECS / 32;
+  extern __shared__ u64 dynamic[];
+  Smem& s = *reinterpret_cast<Smem*>(dynamic);
+  const int lane = threadIdx.x & 31;
+  u64 total = 0;
+  walk<X>(reinterpret_cast<const uint4*>(row + col0), nv, [&](int chunk, const uint4 (&u)[OWN]) {
+    u64 v = 0;
+    unsigned hit = 0;
+#pragma unroll
+    for (int i = 0; i < OWN; ++i)
+      each_logit<X>(u[i], [&](int e, float y) {
+        if (KIND == 1 && !__any_sync(0xffffffffu, y >= t2)) return;            // few of them
+        const u64 weight = raw_weight(y, C, K, low, s.table) - NOTHING;
+        if (KIND == 2) total += weight;
+        v += KIND == 0 || y >= t1 ? weight : 0;
+        if (KIND) hit |= y >= t2 && y < t1 ? 1u << (i * N + e) : 0u;
+      });
+    if (KIND == 1 && s.mode == TIED) {
+      const unsigned ties = __reduce_add_sync(0xffffffffu, unsigned(__popc(hit)));
+      if (lane == 0 && chunk * CHUNK_VECS < nv) s.fast.bin[1 + chunk] = ties;
+    }
+    for (; hit; hit &= hit - 1) {
+      const int col = col0 + chunk * CHUNK + 16 * lane + __ffs(int(hit)) - 1;
+      note(s, to_f(row[col]), col);
+    }
+    for (int o = 16; o; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+    if (lane == 0 && chunk * CHUNK_VECS < nv) s.fast.chunk[1 + chunk] = v;
+  });
+  return total;
+}
+
 // The bin of a logit among `n`: 0 at the largest one, the last one for all that is 2^-32 of its weight or less.  Never falls as x falls.
 __device__ __forceinline__ int bin_of(float x, float m, float c, int n) { return int(fminf(distance(m, x, c), float(n - 1))); }
 
@@ -456,26 +535,6 @@ __global__ void __launch_bounds__(TPB, RESIDENT) k_sample(const X* __restrict__ 
       f(step + 1, odd);
     }
   };
-  // f(chunk of the CTA's, a lane's vectors of it), the next ones on their way; what is not of the row is masked
-  auto pass = [&](auto&& f) {
-    const int turns = (nv + OWN * TPB - 1) / (OWN * TPB);
-    uint4 u[OWN], next[OWN];
-    auto fetch = [&](int i) {
-#pragma unroll
-      for (int j = 0; j < OWN; j += 2) {
-        next[j] = next[j + 1] = none;
-        if ((i * TPB + tid) * OWN + j < nv) load_stream(vec + (i * TPB + tid) * OWN + j, next[j], next[j + 1]);
-      }
-    };
-    fetch(0);
-#pragma unroll 1
-    for (int i = 0; i < turns; ++i) {
-#pragma unroll
-      for (int j = 0; j < OWN; ++j) u[j] = next[j];
-      fetch(i + 1);
-      f(i * WARPS + w, u);
-    }
-  };
   auto all_sync = [&]() {
     if (ctas > 1) cluster.sync();
     else __syncthreads();
@@ -514,6 +573,7 @@ __global__ void __launch_bounds__(TPB, RESIDENT) k_sample(const X* __restrict__ 
     s.n_key = s.n_group = 0;
     s.low_order = 0xffffffffu;
     s.high_order = 0;
+    s.request = q;
   }
   __syncthreads();
   for (int i = 0; i < WARPS; ++i) m = max_nan(m, s.max[i]);
@@ -533,10 +593,6 @@ __global__ void __launch_bounds__(TPB, RESIDENT) k_sample(const X* __restrict__ 
   by_list &= !extreme;
   const float c_coarse = fminf(q.scale * (LOG2E * 16.0f), 3.0e38f), c_fine = fminf(q.scale * (LOG2E * 128.0f), 3.0e38f);
   const float t_mp = q.mp <= 0.0f ? -INFINITY : smallest([&](float x) { return exp((double(x) - wt.m) * double(q.scale)) >= double(q.mp); });      // min p as a logit
-  auto push = [&](float x, int col) {
-    const int i = atomicAdd(&s.n_key, 1);
-    if (i < LIST) s.key[i] = make_key(x, uint32_t(col));
-  };
 
   // the other CTAs' lists behind the first one's, a warp for each; own: the length of the list of CTA `lane`
   auto gather = [&](int own) {
@@ -575,7 +631,7 @@ __global__ void __launch_bounds__(TPB, RESIDENT) k_sample(const X* __restrict__ 
           const int i = atomicAdd(&s.n_group, 1);
           if (i < LIST) s.group[i] = uint16_t(g * TPB + tid);
         }
-      if (end_col >= 0 && bin_of(end, m, c_coarse, COARSE) <= b) push(end, end_col);
+      if (end_col >= 0 && bin_of(end, m, c_coarse, COARSE) <= b) push(s, end, end_col);
       __syncthreads();
       const int listed = s.n_group, vecs = a.steps * U;
       if (listed <= LIST) {
@@ -584,7 +640,7 @@ __global__ void __launch_bounds__(TPB, RESIDENT) k_sample(const X* __restrict__ 
           if (v >= nv) continue;
           const uint4 x = __ldg(vec + v);
           each_logit<X>(x, [&](int e, float y) {
-            if (bin_of(y, m, c_coarse, COARSE) <= b) push(y, col0 + v * N + e);
+            if (bin_of(y, m, c_coarse, COARSE) <= b) push(s, y, col0 + v * N + e);
           });
         }
       } else if (tid == 0) {
@@ -672,7 +728,7 @@ __global__ void __launch_bounds__(TPB, RESIDENT) k_sample(const X* __restrict__ 
   if (!slow && (by_count || by_mass)) {
     clear_bins();
     if (end > -INFINITY) atomicAdd(&s.fast.bin[bin_of(end, m, c_fine, FINE)], 1u);
-    pass([&](int, const uint4 (&u)[OWN]) {
+    walk<X>(vec, nv, [&](int, const uint4 (&u)[OWN]) {
 #pragma unroll
       for (int i = 0; i < OWN; ++i)
         each_logit<X>(u[i], [&](int, float y) {
@@ -745,61 +801,30 @@ __global__ void __launch_bounds__(TPB, RESIDENT) k_sample(const X* __restrict__ 
   // Weights: sums of neighbours among the logits from t1 on, and, for a cut by mass, the sum of all.  What is in [t2, t1) is listed; where it is
   // a crowd (few distinct values, as 16 bits leave them), counted in bins by its order, which narrow [t2, t1), and in a second pass listed or,
   // where it is a crowd of one value, counted by chunks.
-  enum { LISTED, BINNED, TIED };
-  int mode = crowd ? BINNED : LISTED, shift = 0;
-  uint32_t base = 0, top = 0, low_order = 0xffffffffu, high_order = 0;
+  // (What only the seldom parts need waits in shared memory: the passes' registers are few.)
+  if (tid == 0) {
+    s.mode = crowd ? BINNED : LISTED;
+    s.count_before = count_before;
+    if (crowd) {
+      s.base = order_of(t2);
+      s.top = t1 == INFINITY ? order_of(m) + 1 : order_of(t1);
+      s.shift = 0;
+      while ((s.top - 1 - s.base) >> s.shift >= FINE) ++s.shift;
+    }
+  }
   const int own_chunks = (nv + CHUNK_VECS - 1) / CHUNK_VECS, chunks = 2 + (all_v + CHUNK_VECS - 1) / CHUNK_VECS;
-  u64 sum_of_all = 0;
   auto sums = [&](auto kind) {
-    constexpr int KIND = decltype(kind)::value;        // 0: of all; 1: of those from t2 on; 2: of all, with the sum of all
-    u64 total = 0;
-    auto one = [&](float x, bool& listed) -> u64 {
-      const u64 v = wt.raw(x);
-      if constexpr (KIND == 0) return v;
-      if constexpr (KIND == 2) total += v - NOTHING;
-      listed = x >= t2 && !(x >= t1);
-      return x >= t1 ? v : NOTHING;
-    };
-    auto note = [&](float x, int col) {
-      if (mode == LISTED) {
-        push(x, col);
-      } else if (mode == BINNED) {
-        atomicAdd(&s.fast.bin[(order_of(x) - base) >> shift], 1u);
-      } else {
-        low_order = min(low_order, order_of(x));
-        high_order = max(high_order, order_of(x));
-      }
-    };
-    pass([&](int chunk, const uint4 (&u)[OWN]) {
-      u64 v = 0;
-      unsigned hit = 0;
-#pragma unroll
-      for (int i = 0; i < OWN; ++i)
-        each_logit<X>(u[i], [&](int e, float y) {
-          if (KIND == 1 && !__any_sync(0xffffffffu, y >= t2)) return;        // few of them
-          bool listed = false;
-          v += one(y, listed) - NOTHING;
-          if (KIND) hit |= listed ? 1u << (i * N + e) : 0u;
-        });
-      if (KIND && mode == TIED) {
-        const unsigned ties = __reduce_add_sync(0xffffffffu, unsigned(__popc(hit)));
-        if (lane == 0 && chunk < own_chunks) s.fast.bin[1 + chunk] = ties;
-      }
-      for (; hit; hit &= hit - 1) {
-        const int col = col0 + chunk * CHUNK + 16 * lane + __ffs(int(hit)) - 1;
-        note(to_f(row[col]), col);
-      }
-      for (int o = 16; o; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
-      if (lane == 0 && chunk < own_chunks) s.fast.chunk[1 + chunk] = v;
-    });
+    constexpr int KIND = decltype(kind)::value;
+    u64 total = weigh<X, KIND>(row, col0, nv, wt.C, wt.K, wt.low, t1, t2), all;
     // the ends: chunk 0 is the head, the one behind the last is the tail
     if (w == 0) {
-      bool listed = false;
-      u64 v = one(end, listed) - NOTHING, h = end_col >= 0 && end_col < first ? v : 0;
+      const u64 weight = wt.whole(end);
+      u64 v = end >= t1 ? weight : 0, h = end_col >= 0 && end_col < first ? v : 0;
       v -= h;
-      if (listed) {
-        note(end, end_col);
-        if (mode == TIED) atomicAdd(&s.fast.bin[end_col < first ? 0 : 1 + own_chunks], 1u);
+      total += weight;
+      if (end >= t2 && end < t1) {
+        note(s, end, end_col);
+        if (s.mode == TIED) atomicAdd(&s.fast.bin[end_col < first ? 0 : 1 + own_chunks], 1u);
       }
       for (int o = 16; o; o >>= 1) {
         v += __shfl_xor_sync(0xffffffffu, v, o);
@@ -810,7 +835,6 @@ __global__ void __launch_bounds__(TPB, RESIDENT) k_sample(const X* __restrict__ 
         if (rank == ctas - 1) s.fast.chunk[1 + own_chunks] = v;
       }
     }
-    u64 all;
     scan_before(total, s, all);
     if (tid == 0) s.total = all;
   };
@@ -820,21 +844,23 @@ __global__ void __launch_bounds__(TPB, RESIDENT) k_sample(const X* __restrict__ 
     for (int o = MOST_CTAS / 2; o; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
     return __shfl_sync(0xffffffffu, v, 0);
   };
-  if (crowd) {
-    base = order_of(t2);
-    top = t1 == INFINITY ? order_of(m) + 1 : order_of(t1);
-    while ((top - 1 - base) >> shift >= FINE) ++shift;
-    clear_bins();
-    if (by_mass) sums(Int<2>());
-    else sums(Int<1>());
+  if (crowd) clear_bins();
+  for (;;) {
+    __syncthreads();
+    if (cut && by_mass && (!crowd || s.mode == BINNED)) sums(Int<2>());
+    else if (t2 > -INFINITY) sums(Int<1>());
+    else sums(Int<0>());
+    if (s.mode != BINNED) break;
     u64 certain = 0;
     for (int i = (rank == 0 ? 0 : 1) + tid; i < 1 + own_chunks + (rank == ctas - 1); i += TPB) certain += s.fast.chunk[i];
     scan_before(certain, s, certain);
     if (tid == 0) s.certain = certain;
     all_sync();
-    sum_of_all = over_ctas(&Smem::total);
-    certain = by_count ? count_before : over_ctas(&Smem::certain);
-    const u64 target = by_count ? u64(q.k) : start_of(q.p, sum_of_all);
+    const u64 sum_of_all = over_ctas(&Smem::total);
+    certain = by_count ? s.count_before : over_ctas(&Smem::certain);
+    const u64 target = by_count ? u64(s.request.k) : start_of(s.request.p, sum_of_all);
+    const uint32_t base = s.base, top = s.top;
+    const int shift = s.shift;
     sum_bins();
     // In descending order: the place p is bin FINE - 1 - p.  The start ends between the first place whose bins, taken at their largest weights,
     // reach the target, and the first that does so at their smallest.
@@ -865,13 +891,12 @@ __global__ void __launch_bounds__(TPB, RESIDENT) k_sample(const X* __restrict__ 
     }
     __syncthreads();
     const int lo = s.first_bin, hi = s.last_bin;
-    count_before = s.before;
     u64 mine = 0;
     for (int j = 0; j < PER; ++j) mine += tid * PER + j >= lo && tid * PER + j <= hi ? s.fast.bin[FINE - 1 - (tid * PER + j)] : 0;
     scan_before(mine, s, all);
     if (lo < 0 || lo > hi) {         // never expected
       all_sync();
-      if (rank == 0) sample_any<X>(row, a, t, q, wt, s);
+      if (rank == 0) sample_any<X>(row, a, t, s.request, wt, s);
       return;
     }
     const u64 edge = u64(base) + (u64(FINE - lo) << shift);          // above the place lo
@@ -879,33 +904,24 @@ __global__ void __launch_bounds__(TPB, RESIDENT) k_sample(const X* __restrict__ 
     t2 = value_of(base + (uint32_t(FINE - 1 - hi) << shift));
     cut = t_mp < t1;
     if (!cut) t1 = t2 = t_mp;
-    mode = cut && all > LIST ? TIED : LISTED;
+    if (tid == 0) {
+      s.mode = cut && all > LIST ? TIED : LISTED;
+      s.count_before = s.before;
+      s.sum_of_all = sum_of_all;
+    }
     clear_bins();
-  }
-  __syncthreads();
-  if (cut && by_mass && !crowd) sums(Int<2>());
-  else if (t2 > -INFINITY) sums(Int<1>());
-  else sums(Int<0>());
-  if (mode == TIED) {
-    for (int o = 16; o; o >>= 1) {
-      low_order = min(low_order, __shfl_xor_sync(0xffffffffu, low_order, o));
-      high_order = max(high_order, __shfl_xor_sync(0xffffffffu, high_order, o));
-    }
-    if (lane == 0) {
-      atomicMin(&s.low_order, low_order);
-      atomicMax(&s.high_order, high_order);
-    }
   }
   all_sync();
   int n = 0;
+  u64 sum_of_all = 0;
+  uint32_t low_order = 0, high_order = 0;
+  const int mode = s.mode;
   if (rank == 0) {
     const int own = lane < ctas ? min(of_rank(lane).n_key, LIST + 1) : 0;
     n = __reduce_add_sync(0xffffffffu, own);
-    if (!crowd) sum_of_all = over_ctas(&Smem::total);
-    low_order = lane < ctas ? of_rank(lane).low_order : 0xffffffffu;
-    high_order = lane < ctas ? of_rank(lane).high_order : 0;
-    low_order = __reduce_min_sync(0xffffffffu, low_order);
-    high_order = __reduce_max_sync(0xffffffffu, high_order);
+    sum_of_all = crowd ? s.sum_of_all : over_ctas(&Smem::total);
+    low_order = __reduce_min_sync(0xffffffffu, lane < ctas ? of_rank(lane).low_order : 0xffffffffu);
+    high_order = __reduce_max_sync(0xffffffffu, lane < ctas ? of_rank(lane).high_order : 0);
     if (n <= LIST) gather(own);
     for (int i = tid; ctas > 1 && i < chunks; i += TPB) {
       const int r = min(ctas - 1, max(0, i - 1) / (per / CHUNK_VECS));
@@ -919,7 +935,7 @@ __global__ void __launch_bounds__(TPB, RESIDENT) k_sample(const X* __restrict__ 
   if (rank) return;
   if (n > LIST || (mode == TIED && low_order != high_order)) {
     __syncthreads();
-    sample_any<X>(row, a, t, q, wt, s);
+    sample_any<X>(row, a, t, s.request, wt, s);
     return;
   }
   auto bounds = [&](int c, int& from, int& to) {       // the columns of a chunk
@@ -941,8 +957,8 @@ __global__ void __launch_bounds__(TPB, RESIDENT) k_sample(const X* __restrict__ 
       v[j] = i >= n ? 0 : by_count ? 1 : wt.whole(key_value(s.key[i]));
       mine += v[j];
     }
-    u64 at = (by_count ? count_before : certain) + scan_before(mine, s, all);
-    const u64 target = by_count ? u64(q.k) : start_of(q.p, sum_of_all);
+    u64 at = (by_count ? s.count_before : certain) + scan_before(mine, s, all);
+    const u64 target = by_count ? u64(s.request.k) : start_of(s.request.p, sum_of_all);
     for (int j = 0; j < PER; ++j) {
       if (at < target && target <= at + v[j]) s.found = s.key[tid * PER + j];
       at += v[j];
@@ -950,7 +966,7 @@ __global__ void __launch_bounds__(TPB, RESIDENT) k_sample(const X* __restrict__ 
     __syncthreads();
     last = s.found;
     if (last == 0) {                 // not where the bins said: never expected
-      sample_any<X>(row, a, t, q, wt, s);
+      sample_any<X>(row, a, t, s.request, wt, s);
       return;
     }
     // the listed ones that stay, to their chunks
@@ -967,17 +983,17 @@ __global__ void __launch_bounds__(TPB, RESIDENT) k_sample(const X* __restrict__ 
     // a crowd of one value, of which the first `need` stay, in the order of the index
     constexpr int PER = CHUNKS / TPB;
     const float x = value_of(low_order);
-    const u64 each = wt.whole(x), target = by_count ? u64(q.k) : start_of(q.p, sum_of_all);
+    const u64 each = wt.whole(x), target = by_count ? u64(s.request.k) : start_of(s.request.p, sum_of_all);
     u64 certain = 0, mine = 0, ties;
     for (int i = tid; i < chunks; i += TPB) certain += s.fast.chunk[i];
     scan_before(certain, s, certain);
-    if (by_count) certain = count_before;
+    if (by_count) certain = s.count_before;
     for (int j = 0; j < PER; ++j) mine += tid * PER + j < chunks ? s.fast.bin[tid * PER + j] : 0;
     u64 at = scan_before(mine, s, ties);
     const u64 need = target <= certain ? 0 : by_count ? target - certain : each ? (target - certain + each - 1) / each : 0;
     if (need == 0 || need > ties) {  // never expected
       __syncthreads();
-      sample_any<X>(row, a, t, q, wt, s);
+      sample_any<X>(row, a, t, s.request, wt, s);
       return;
     }
     for (int j = 0; j < PER && tid * PER + j < chunks; ++j) {
@@ -1016,7 +1032,7 @@ __global__ void __launch_bounds__(TPB, RESIDENT) k_sample(const X* __restrict__ 
     mine += i < chunks ? s.fast.chunk[i] : 0;
   }
   u64 at = scan_before(mine, s, all);
-  const u64 limit = limit_of(q.u, all);
+  const u64 limit = limit_of(s.request.u, all);
   for (int j = 0; j < PER; ++j) {
     const int i = tid * PER + j;
     const u64 v = i < chunks ? s.fast.chunk[i] : 0;

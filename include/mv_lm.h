@@ -23,8 +23,8 @@
  * before anything is enqueued.  Pointers need the alignment of their element type only (a table may start
  * anywhere in a worker's row); rows are contiguous and `ld...` elements apart.  Results do not depend
  * on the order in which the GPU runs things: the same call on the same inputs gives the same bytes.  Where
- * the inputs lie can change the order of the sums in mv_token_logprob and mv_clip_* (rows and tensors are cut at
- * their own 16- or 32-byte boundaries), and so can the number of rows; the other calls' bytes do not depend on it.
+ * the inputs lie can change the order of the sums in mv_token_logprob, mv_layer_norm*, mv_distill and mv_clip_* (rows and tensors are
+ * cut at their own 16- or 32-byte boundaries), and so can the number of rows; the other calls' bytes do not depend on it.
  */
 #ifndef MV_LM_H
 #define MV_LM_H
@@ -82,7 +82,7 @@ size_t mv_layer_norm_grad_workspace_bytes(int64_t T, int64_t D);
  *   dx [T, D] out, of the same type, rows lddx apart; may be dy or x itself (of the same pitch); NULL: not wanted
  *   dweight, dbias [D] float out, each may be NULL.  accumulate = 0: overwritten (T = 0: zeros); accumulate = 1: added to
  *   workspace  mv_layer_norm_grad_workspace_bytes(T, D) bytes, 16-byte aligned (unused, and may be NULL, without dweight and dbias)
- * The sums over rows are in 32 bits, in an order that T, D and the device's number of multiprocessors fix. */
+ * The sums over rows are in 32 bits, in an order that the sizes, the type and the rows' places within 16 bytes fix. */
 int mv_layer_norm_grad(void* stream, const void* dy, int64_t lddy, const void* x, int64_t ldx, int type, int64_t T, int64_t D,
                        const void* weight, int w_type, const float* mean, const float* rstd, void* dx, int64_t lddx, float* dweight,
                        float* dbias, int accumulate, void* workspace, size_t workspace_bytes);

@@ -7,9 +7,9 @@ import sys
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 SRC = os.path.join(HERE, "csrc", "mv_sparse.cu")
-SRCS = [SRC, *(os.path.join(HERE, "csrc", f) for f in ("mv_wire.cu", "mv_embed.cu", "mv_norm.cu", "mv_token.cu", "mv_distill.cu", "mv_sample.cu", "mv_clip.cu"))]
+SRCS = [SRC, *(os.path.join(HERE, "csrc", f) for f in ("mv_wire.cu", "mv_embed.cu", "mv_norm.cu", "mv_norm_grad.cu", "mv_token.cu", "mv_distill.cu", "mv_sample.cu", "mv_clip.cu"))]
 HDRS = [*(os.path.join(os.path.dirname(HERE), "include", h) for h in ("mv_sparse.h", "mv_wire.h", "mv_lm.h")),
-        os.path.join(HERE, "csrc", "mv_lm.cuh"), os.path.join(HERE, "csrc", "mv_row.cuh")]
+        *(os.path.join(HERE, "csrc", h) for h in ("mv_lm.cuh", "mv_row.cuh", "mv_norm.cuh"))]
 LIB = os.path.join(HERE, "libmvsparse.so")
 LIB_DEBUG = os.path.join(HERE, "libmvsparse_debug.so")      # the checked build (-DMV_DEBUG), see mv_debug_status
 
@@ -42,7 +42,7 @@ def build(force: bool = False, verbose: bool = False, debug: bool = False) -> st
     lib = LIB_DEBUG if debug else LIB
     if not force and not needs_build(lib):
         return lib
-    cmd = [nvcc_path(), *NVCC_FLAGS, *(["-DMV_DEBUG"] if debug else []), "-o", lib, *SRCS]
+    cmd = [nvcc_path(), "-t", "0", *NVCC_FLAGS, *(["-DMV_DEBUG"] if debug else []), "-o", lib, *SRCS]
     if verbose:
         cmd.insert(1, "-Xptxas")
         cmd.insert(2, "-v")

@@ -40,9 +40,11 @@ struct DistillArgs {
 constexpr int U = 4;                 // vectors per thread and step, all in flight, two by two from neighbouring places
 constexpr int MARKS = 4096;          // words of marks: one for each thread and step, a bit for each of its logits
 
-// A CTA per row, streamed once.  With the rest as a class the listed tokens are kept out of the sum (taking them off it would leave nothing of
-// a small rest): a bit for every logit of the next steps, set for the listed ones, which a thread asks one word at a time; their
-// own terms are added at the end.
+// A CTA per row, streamed once with a running reference.  With the rest as a class the listed tokens are kept out of the sum (taking them
+// off it would leave nothing of a small rest): a bit for every logit of the next steps, set for the listed ones, which a thread asks
+// one word at a time; their own terms are added at the end.  Memory bounds it: 8192 x 65536 bf16 162 us (6.6 TB/s), with 32 alternatives
+// and the rest 169.  The end of a row, some microseconds of latency for its list, is covered by the other CTAs unless rows are short
+// (16000 x 8000: 71 us of 39) or few (64 x 131072: 19 us).
 template <typename X, bool REST, int TPB>
 __global__ void __launch_bounds__(TPB, 1024 / TPB) k_distill(const X* __restrict__ logits, const __grid_constant__ DistillArgs a) {
   constexpr int N = Vec<X>::N, WARPS = TPB / 32, WINDOW = MARKS / TPB;
@@ -254,8 +256,10 @@ __global__ void __launch_bounds__(TPB, 1024 / TPB) k_distill(const X* __restrict
 // ------------------------------------------------------------------------------------------ gradient
 // dx = f (M p - q) for a listed token, f M' p for the others, f = c g, M' = M - r / P.  p = q q with q = 2^h, h = log2(p) / 2: the
 // hardware's exponential has no subnormal results.  Each CTA takes some stretches of one row, and all of the row's list: the others' value is
-// written everywhere, and then its listed tokens' over it.
-constexpr int GRAD_U = 4, GRAD_MOST = 16;
+// written everywhere, and then its listed tokens' over it.  Memory bounds it: 8192 x 65536 bf16 345 us (6.2 TB/s in and out), 4096 x
+// 131072 with 64 alternatives 361 (one stretch of 8192 logits per CTA: 570); rows that lie differently within 16 bytes 9000 x 33001 f16
+// 219 us (element by element 877).
+constexpr int GRAD_U = 4, GRAD_MOST = 4;
 
 struct DistillGradArgs {
   int64_t V, ld, ldg;
@@ -425,7 +429,8 @@ int mv_distill(void* stream, const void* logits, int type, int64_t T, int64_t V,
   return with_type(type, [&](auto x) {
     using X = decltype(x);
     const int64_t vecs = V / Vec<X>::N;
-    // short rows take few threads and many CTAs, if there are rows enough to fill the device; long or few rows many threads
+    // short rows take few threads and many CTAs, if there are rows enough to fill the device; long or few rows many threads (the sides of
+    // this rule as measured for the log probabilities, whose stream is the same)
     const int tpb = T >= 1184 && vecs <= 3000 ? 64 : vecs > 10240 || (T < 600 && vecs > 6000) ? 256 : 128;
     const size_t smem = size_t(k) * LIST_BYTES + (rest ? MARKS * 4 : 0);
     auto launch = [&](auto r) {
@@ -455,7 +460,8 @@ int mv_distill_grad(void* stream, const void* logits, int type, int64_t T, int64
   a.V = V; a.ld = ld; a.ldg = ldg; a.h = {top_logprob, top_id, id_type, k, log_rest ? 1 : 0}; a.scale = scale; a.lse = lse; a.log_rest = log_rest; a.g = g;
   return with_type(type, [&](auto x) {
     using X = decltype(x);
-    // The list costs a CTA a few microseconds of latency: as many stretches for each as leave enough CTAs to fill the device.
+    // The list costs a CTA a few microseconds of latency: as many stretches for each as leave enough CTAs to fill the device, up to four
+    // (4096 x 131072 bf16 with 64 alternatives: one 476 us, two 383, four 338, eight 346, sixteen 361).  Rows of up to 16 KB take small CTAs (16000 x 8000 bf16: 90 us, with 256 threads 138).
     const int tpb = V * size <= 16384 ? 64 : 256;
     const int64_t per = int64_t(tpb) * GRAD_U * Vec<X>::N, stretches = (V + per - 1) / per;
     int64_t each = T * stretches / (148 * 2048 / tpb);

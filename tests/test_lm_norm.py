@@ -1,7 +1,7 @@
 """GPU tests of layer norm and its gradients (include/mv_lm.h) against plain statements in 64 bits.
 
-Tolerances, with u = 2^-24 the rounding of 32 bits.  At least 32 lanes share a row, so that no term of a sum over D passes more than
-n = D / 32 + 16 additions: a sum is off by at most 1.01 n u sum|terms|.  Sums over rows are taken as in any order, 1.01 (T + 2) u sum|terms|.
+Tolerances, with u = 2^-24 the rounding of 32 bits.  At least eight lanes share a row and each keeps two sums, so that no term of a sum over D
+passes more than n = D / 16 + 16 additions: a sum is off by at most 1.01 n u sum|terms|.  Sums over rows are taken as in any order, 1.01 (T + 2) u sum|terms|.
 mean: n u mean|x| and a division.  variance: its squares are exact to 3 u of themselves, the sum to n u, and a mean that is off by e adds
 e^2.  rstd = 1 / sqrt(v + eps): half the relative error of v + eps, and 4 u for sum, root (an approximation of 2^-22 counts as 4 u) and
 division.  A result of 16 bits has to be what some value inside the 32-bit tolerance rounds to."""
@@ -21,7 +21,7 @@ def forward_reference(x, w, b, eps):
     """((y, tol), (mean, tol), (rstd, tol)) in 64 bits."""
     x = x.double().cpu()
     D = x.shape[1]
-    n = D / 32 + 16
+    n = D / 16 + 16
     w = w.double().cpu() if w is not None else torch.ones(D, dtype=torch.float64)
     b = b.double().cpu() if b is not None else torch.zeros(D, dtype=torch.float64)
     eps = float(torch.tensor(eps, dtype=torch.float32))
@@ -115,7 +115,7 @@ def grad_reference(dy, x, w, mean, rstd, old=None):
     """((dx, tol), (dweight, tol), (dbias, tol)) in 64 bits for the mean and rstd that the call is given."""
     dy, x, mean, rstd = (t.double().cpu() for t in (dy, x, mean, rstd))
     T, D = x.shape
-    n = D / 32 + 16
+    n = D / 16 + 16
     w = w.double().cpu() if w is not None else torch.ones(D, dtype=torch.float64)
     d = x - mean[:, None]
     z = d * rstd[:, None]

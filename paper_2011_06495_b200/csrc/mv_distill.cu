@@ -256,10 +256,10 @@ __global__ void __launch_bounds__(TPB, 1024 / TPB) k_distill(const X* __restrict
 // ------------------------------------------------------------------------------------------ gradient
 // dx = f (M p - q) for a listed token, f M' p for the others, f = c g, M' = M - r / P.  p = q q with q = 2^h, h = log2(p) / 2: the
 // hardware's exponential has no subnormal results.  Each CTA takes some stretches of one row, and all of the row's list: the others' value is
-// written everywhere, and then its listed tokens' over it.  Memory bounds it: 8192 x 65536 bf16 345 us (6.2 TB/s in and out), 4096 x
-// 131072 with 64 alternatives 361 (one stretch of 8192 logits per CTA: 570); rows that lie differently within 16 bytes 9000 x 33001 f16
-// 219 us (element by element 877).
-constexpr int GRAD_U = 4, GRAD_MOST = 4;
+// written everywhere, and then its listed tokens' over it.  Memory bounds it: 8192 x 65536 bf16 340 us (6.3 TB/s in and out), 4096 x
+// 131072 with 64 alternatives the same; rows that lie differently within 16 bytes 9000 x 33001 f16 222 us (element by element 877).
+// Short rows wait for their lists: 16384 x 1000 f16 with 50 alternatives 47 us.
+constexpr int GRAD_U = 4, GRAD_EACH = 4;
 
 struct DistillGradArgs {
   int64_t V, ld, ldg;
@@ -460,12 +460,15 @@ int mv_distill_grad(void* stream, const void* logits, int type, int64_t T, int64
   a.V = V; a.ld = ld; a.ldg = ldg; a.h = {top_logprob, top_id, id_type, k, log_rest ? 1 : 0}; a.scale = scale; a.lse = lse; a.log_rest = log_rest; a.g = g;
   return with_type(type, [&](auto x) {
     using X = decltype(x);
-    // The list costs a CTA a few microseconds of latency: as many stretches for each as leave enough CTAs to fill the device, up to four
-    // (4096 x 131072 bf16 with 64 alternatives: one 476 us, two 383, four 338, eight 346, sixteen 361).  Rows of up to 16 KB take small CTAs (16000 x 8000 bf16: 90 us, with 256 threads 138).
+    // The list costs a CTA a few microseconds of latency: as many stretches for each as leave enough CTAs to fill the device, up to a CTA for
+    // four, and none for fewer behind them (4096 x 131072 bf16 with 64 alternatives, 16 stretches: one each 476 us, two 383, four 338,
+    // eight 346, sixteen 361; 9000 x 33001, five: four and one 219, together 194).  Rows of up to 16 KB take small CTAs (16000 x
+    // 8000 bf16: 90 us, with 256 threads 138).
     const int tpb = V * size <= 16384 ? 64 : 256;
     const int64_t per = int64_t(tpb) * GRAD_U * Vec<X>::N, stretches = (V + per - 1) / per;
+    const int64_t least = stretches < 2 * GRAD_EACH ? 1 : stretches / GRAD_EACH, most = (stretches + least - 1) / least;
     int64_t each = T * stretches / (148 * 2048 / tpb);
-    each = each < 1 ? 1 : each > GRAD_MOST ? GRAD_MOST : each;
+    each = each < 1 ? 1 : each > most ? most : each;
     a.stretches = int(each);
     a.ctas = unsigned((stretches + each - 1) / each);
     if (T * a.ctas >= lim) return int(MV_ERR_INVALID_ARG);

@@ -201,9 +201,8 @@ __global__ void __launch_bounds__(TPB, 1024 / TPB) k_distill(const X* __restrict
   sum = 0.0f;
   for (int i = 0; i < WARPS; ++i) sum += s_sum[i];
   // the listed tokens' own terms, each token once
-  double all = sum;
+  double all = sum, own = 0.0;
   if constexpr (REST) {
-    double own = 0.0;
     for (int j = lane; j < a.h.k; j += 32) {
       const int c = list.col[j];
       bool again = c < 0;
@@ -216,7 +215,8 @@ __global__ void __launch_bounds__(TPB, 1024 / TPB) k_distill(const X* __restrict
   }
   // With e_j = exp(a_j - shift): q_j = e_j / sum e without the rest (shift: the largest a_j), e_j with it (shift 0).  1 - sum q is a small
   // difference, so these are in 64 bits.
-  const float ls = logf(float(all)), lr = logf(sum) - ls;
+  // log P by what is missing to one where that is the smaller part: the difference of two logarithms would lose it.
+  const float ls = logf(float(all)), lr = own > 0.0 && own < sum ? log1pf(-float(own / all)) : logf(sum) - ls;
   float m = -INFINITY;
   bool any = false, bad = false;
   for (int j = lane; j < a.h.k; j += 32) {

@@ -244,6 +244,24 @@ def test_positions_without_a_teacher_are_zero_whatever_their_logits_hold():
     assert bool((dx[:3] == 0).all()) and bool((dx[3:] != 0).any(1).all())
 
 
+@pytest.mark.parametrize("T,V,k,dt", [(40, 2000, 1, F32), (33, 30011, 8, BF16), (5, 131072, 64, F16)])
+def test_log_rest_beside_a_light_list_is_as_exact_as_the_list_is(T, V, k, dt):
+    """log P = log1p(-o / s), o the listed tokens' sum and s all: off by what o and s are off, 1.45 times as much of itself up to
+    o = s / 2, and the function's own two units; nothing is lost where P is close to one."""
+    x = (torch.randn((T, V), generator=gen(V), device=DEV) * 2).to(dt)
+    ids = torch.stack([torch.randperm(V, generator=gen(i), device=DEV)[:k] for i in range(T)]).int()
+    x.scatter_(1, ids.long(), -torch.linspace(0, 14, T, device=DEV)[:, None].expand(T, k).to(dt))
+    got = call(x, torch.full((T, k), -9.0, device=DEV), ids, 1.0, True)["log_rest"]
+    z = x.double().cpu()
+    e = torch.exp(z - z.amax(1, keepdim=True))
+    at = (z - z.amax(1, keepdim=True)).abs()
+    own, s = torch.gather(e, 1, ids.long().cpu()).sum(1), e.sum(1)
+    assert float((own / s).max()) < 0.5 and float((own / s).min()) < 1e-5
+    rho = lambda v, d: EX2 + 4 * U32 * (v * d).sum(1) / v.sum(1)
+    off = rho(torch.gather(e, 1, ids.long().cpu()), torch.gather(at, 1, ids.long().cpu())) + rho(e, at) + (V / 32 + 64) * U32 + 6 * U32
+    assert bool(within(got, torch.log1p(-own / s), 1.5 * off * torch.log1p(-own / s).abs()).all())
+
+
 def test_divergence_of_a_student_that_agrees_is_zero_and_so_is_its_gradient():
     """The teacher's own logits: kl is 0 up to its bound, and the alternatives are those that mv_token_logprob leaves."""
     T, V, k = 40, 6007, 32

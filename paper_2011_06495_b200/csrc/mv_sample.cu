@@ -118,7 +118,7 @@ struct Weights {
   }
   __device__ __forceinline__ u64 raw(float x) const { return raw_weight(x, C, K, low, table); }      // NOTHING and the whole number
   __device__ __forceinline__ u64 whole(float x) const { return raw(x) - NOTHING; }
-  __device__ __forceinline__ double log_of(u64 sum) const { return log(double(sum) / unit) - (fma(m, C, K) - MAGIC) * (0x1p-45 * 0.6931471805599453); }      // without the common factor
+  __device__ __forceinline__ double log_factor() const { return (fma(m, C, K) - MAGIC) * (0x1p-45 * 0.6931471805599453); }      // of the common factor
   __device__ __forceinline__ u64 any(float x) const { return u64(exp2((double(x) - m) * c2) * unit + 0.5); }      // of extreme rows too
 };
 
@@ -238,9 +238,13 @@ __device__ __forceinline__ void put_token(const SampleArgs& a, int64_t t, int64_
   else static_cast<int64_t*>(a.token)[t] = token;
   if (a.logprob) a.logprob[t] = logprob;
 }
-// log_sum: of the kept weights beside the largest.
-__device__ __forceinline__ void put_drawn(const SampleArgs& a, int64_t t, int64_t token, float x, const Weights& wt, double log_sum) {
-  put_token(a, t, token, float((double(x) - wt.m) * (wt.c2 * 0.6931471805599453) - log_sum));
+// The log of a token's share: of one half and more by what is missing to one, a whole number (0 where nothing is), of less by its logit,
+// since a light weight is a rounded one.
+__device__ __forceinline__ void put_drawn(const SampleArgs& a, int64_t t, int64_t token, float x, const Weights& wt, u64 weight, u64 all, double log_factor) {
+  const u64 rest = all - weight;
+  const double share = rest < weight ? 0.0 - log1p(double(rest) / double(weight))
+                                     : (double(x) - wt.m) * (wt.c2 * 0.6931471805599453) - log(double(all) / wt.unit) + log_factor;
+  put_token(a, t, token, float(share));
 }
 __device__ __forceinline__ u64 limit_of(float u, u64 all) { return u >= 1.0f ? all - 1 : u > 0.0f ? share_of(u, all) : 0; }      // the first token at which the sum is larger is drawn
 
@@ -397,7 +401,7 @@ __device__ __noinline__ void sample_any(const X* row, const SampleArgs& a, int64
     }
     const unsigned hit = __ballot_sync(0xffffffffu, before + incl > limit);
     if (hit) {
-      if (lane == __ffs(int(hit)) - 1) put_drawn(a, t, i, to_f(row[i]), wt, log(double(all) / wt.unit));
+      if (lane == __ffs(int(hit)) - 1) put_drawn(a, t, i, to_f(row[i]), wt, n, all, 0.0);
       return;
     }
     before += __shfl_sync(0xffffffffu, incl, 31);
@@ -700,7 +704,7 @@ __global__ void __launch_bounds__(TPB, RESIDENT) k_sample(const X* __restrict__ 
       for (int j = 0; j < PER; ++j) {
         if (before <= limit && limit < before + v[j]) {
           const u64 key = s.key[uint32_t(s.fast.sorted[tid * PER + j])];
-          put_drawn(a, t, key_index(key), key_value(key), wt, wt.log_of(total));
+          put_drawn(a, t, key_index(key), key_value(key), wt, v[j], total, wt.log_factor());
         }
         before += v[j];
       }
@@ -1074,7 +1078,7 @@ __global__ void __launch_bounds__(TPB, RESIDENT) k_sample(const X* __restrict__ 
 #pragma unroll
   for (int j = 0; j < SHARE; ++j) {
     const int i = from + tid * SHARE + j;
-    if (before <= limit && limit < before + v[j]) put_drawn(a, t, i, to_f(row[i]), wt, wt.log_of(all));
+    if (before <= limit && limit < before + v[j]) put_drawn(a, t, i, to_f(row[i]), wt, v[j], all, wt.log_factor());
     before += v[j];
   }
 }

@@ -214,6 +214,32 @@ def test_many_rows_with_crowds():
             assert int(token[r]) == reference(x[r], float(u[r]), 1.0, int(k[r]), float(p[r]), 0.0)[0], (T, V, r)
 
 
+@pytest.mark.parametrize("dt", [F32, BF16, F16])
+@pytest.mark.parametrize("V", [2, 3000, 40_000, 131_072])
+def test_logprob_of_a_nearly_sure_token_keeps_its_digits(dt, V):
+    """A token that is ahead by 0.5 to 30: the rest beside it is a sum of whole numbers, each weight exact to 2e-14 and half of n / 2^61."""
+    T = 48
+    x = torch.randn((T, V), generator=gen(V), device=DEV)
+    at = torch.randint(0, V, (T, 1), generator=gen(1), device=DEV)
+    x.scatter_(1, at, x.amax(1, keepdim=True) + 0.5 + torch.arange(T, device=DEV)[:, None] * 0.625)
+    x = (x - 4.37).to(dt)
+    for scale, k in ((1.0, 0), (1.3, 0), (1.0, 40), (0.9, 1)):
+        u = torch.full((T,), 0.5, device=DEV)
+        token, lp = draw(x, u, scale, k)
+        w = torch.sort(torch.exp((x.double() - x.double().amax(1, keepdim=True)) * float(np.float32(scale))), dim=1, descending=True)[0]
+        w = w[:, :k] if k else w
+        rest = w[:, 1:].sum(1).cpu()
+        sure = (rest < 1) & (w[:, 0].cpu() == 1)
+        n = 2.0 ** max(10, (V - 1).bit_length())
+        want, got = -torch.log1p(rest), lp.double().cpu()
+        assert int(sure.sum()) > T // 2
+        off = 1.01 * U32 * want.abs() + 1e-13 * rest + w.shape[1] * n * 2.0 ** -62
+        assert bool((((got - want).abs() <= off) | ~sure).all()) and bool((got <= 0).all())
+        assert torch.equal(token.cpu()[sure], x.float().argmax(1).cpu()[sure])
+        if k == 1:
+            assert bool((got == 0).all()) and not bool(torch.signbit(got).any())
+
+
 def test_frequencies_are_the_probabilities():
     """The same row with an even grid of u: every token as often as its share of the grid, to within one of the grid's steps."""
     T, V = 4096, 50

@@ -623,31 +623,55 @@ __global__ void __launch_bounds__(TPB, RESIDENT) k_sample(const X* __restrict__ 
   };
 
   if (by_list) {
-    // the coarse bin b up to which k groups' maxima lie: so do k logits, and all of the top k
+    // the coarse bin up to which k of what the CTAs have counted lie (COARSE: none), and how much they have counted
+    u64 counted;
+    auto bin_of_k = [&]() {
+      all_sync();
+      u64 c[2] = {0, 0};
+#pragma unroll
+      for (int r = 0; r < MOST_CTAS; ++r) {
+        const uint2 v = r < ctas ? *reinterpret_cast<const uint2*>(&of_rank(r).coarse[2 * tid]) : make_uint2(0, 0);
+        c[0] += v.x;
+        c[1] += v.y;
+      }
+      if (tid == 0) s.first_bin = COARSE;
+      const u64 at = scan_before(c[0] + c[1], s, counted);
+      if (at < u64(q.k) && u64(q.k) <= at + c[0] + c[1]) s.first_bin = 2 * tid + (at + c[0] < u64(q.k));
+      __syncthreads();
+      return s.first_bin;
+    };
+    // k groups' maxima lie up to bin b: so do k logits, and all of the top k
     for (int g = 0; g < groups; ++g) atomicAdd(&s.coarse[bin_of(s.gmax[g][tid], m, c_coarse, COARSE)], 1u);
     if (end_col >= 0) atomicAdd(&s.coarse[bin_of(end, m, c_coarse, COARSE)], 1u);
-    all_sync();
-    u64 c[2] = {0, 0}, all;
-#pragma unroll
-    for (int r = 0; r < MOST_CTAS; ++r) {
-      const uint2 v = r < ctas ? *reinterpret_cast<const uint2*>(&of_rank(r).coarse[2 * tid]) : make_uint2(0, 0);
-      c[0] += v.x;
-      c[1] += v.y;
+    int b = bin_of_k();
+    if (b >= COARSE - 1) {
+      // too few groups (a short row, or one that is masked but for a few tokens): the logits are counted, those of the last bin, which has the
+      // masked ones too, by each thread (2 rows of 3200 f16, 97 % masked, k 50, p 0.9: 78 us without this)
+      all_sync();
+      for (int i = tid; i < COARSE; i += TPB) s.coarse[i] = 0;
+      __syncthreads();
+      uint32_t last = 0;
+      auto count = [&](float y) {
+        const int i = bin_of(y, m, c_coarse, COARSE);
+        if (i < COARSE - 1) atomicAdd(&s.coarse[i], 1u);
+        else last += y > -INFINITY;
+      };
+#pragma unroll 2
+      for (int v = tid; v < nv; v += TPB) each_logit<X>(__ldg(vec + v), [&](int, float y) { count(y); });
+      if (end_col >= 0) count(end);
+      last = __reduce_add_sync(0xffffffffu, last);
+      if (lane == 0 && last) atomicAdd(&s.coarse[COARSE - 1], last);
+      b = min(bin_of_k(), COARSE - 1);
+      by_list = b < COARSE - 1 || counted <= LIST;
     }
-    if (tid == 0) s.first_bin = COARSE;
-    const u64 at = scan_before(c[0] + c[1], s, all);
-    if (at < u64(q.k) && u64(q.k) <= at + c[0] + c[1]) s.first_bin = 2 * tid + (at + c[0] < u64(q.k));
-    __syncthreads();
-    int b = s.first_bin;
     if (q.p >= 1.0f && q.mp > 0.0f) b = min(b, bin_of(t_mp, m, c_coarse, COARSE));      // nothing beyond it is kept
-    by_list = b < COARSE - 1;
     if (by_list) {
       for (int g = 0; g < groups; ++g)
-        if (bin_of(s.gmax[g][tid], m, c_coarse, COARSE) <= b) {
+        if (s.gmax[g][tid] > -INFINITY && bin_of(s.gmax[g][tid], m, c_coarse, COARSE) <= b) {
           const int i = atomicAdd(&s.n_group, 1);
           if (i < LIST) s.group[i] = uint16_t(g * TPB + tid);
         }
-      if (end_col >= 0 && bin_of(end, m, c_coarse, COARSE) <= b) push(s, end, end_col);
+      if (end > -INFINITY && bin_of(end, m, c_coarse, COARSE) <= b) push(s, end, end_col);
       __syncthreads();
       const int listed = s.n_group, vecs = a.steps * U;
       if (listed <= LIST) {
@@ -656,7 +680,7 @@ __global__ void __launch_bounds__(TPB, RESIDENT) k_sample(const X* __restrict__ 
           if (v >= nv) continue;
           const uint4 x = __ldg(vec + v);
           each_logit<X>(x, [&](int e, float y) {
-            if (bin_of(y, m, c_coarse, COARSE) <= b) push(s, y, col0 + v * N + e);
+            if (y > -INFINITY && bin_of(y, m, c_coarse, COARSE) <= b) push(s, y, col0 + v * N + e);
           });
         }
       } else if (tid == 0) {

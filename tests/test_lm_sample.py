@@ -240,6 +240,19 @@ def test_logprob_of_a_nearly_sure_token_keeps_its_digits(dt, V):
             assert bool((got == 0).all()) and not bool(torch.signbit(got).any())
 
 
+@pytest.mark.parametrize("dt,V,offset", [(F32, 1408, 1), (F16, 3200, 0), (BF16, 1152, 3), (BF16, 60_000, 0), (F16, 131_072, 1)])
+def test_fewer_candidates_than_the_top_k_asks_for(dt, V, offset):
+    """Short rows, and rows that are masked but for some tokens: fewer, as many and more than k, within the weights' range and outside it."""
+    g = gen(V)
+    T = 24
+    x = strided(T, V, dt, 1, offset, seed=V)[0].mul_(2.5)
+    for t, left in enumerate([1, 2, 49, 50, 51, 64, 120, 700, 1024, 1025, 1100, V] * 2):
+        x[t].masked_fill_(torch.rand(V, generator=g, device=DEV).argsort().argsort() >= left, -math.inf)
+    u = torch.rand(T, generator=g, device=DEV)
+    for scale, k, p, mp in ((1.25, 50, 0.9, None), (1.0, 50, None, None), (1.0, 50, 0.95, 0.01), (9.0, 50, 0.999, None), (1.0, 1000, 0.9, None), (0.9, 1024, 0.97, None)):
+        check(x, u, scale, k, p, mp)
+
+
 def test_frequencies_are_the_probabilities():
     """The same row with an even grid of u: every token as often as its share of the grid, to within one of the grid's steps."""
     T, V = 4096, 50

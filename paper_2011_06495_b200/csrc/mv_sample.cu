@@ -1128,9 +1128,12 @@ int mv_sample(void* stream, const void* logits, int type, int64_t T, int64_t V, 
     const int64_t vecs = V / Vec<X>::N;
     a.chunks = V / CHUNK + 10 <= CHUNKS;
     // As many CTAs per row as fill the device twice (requests of different kinds end at different times), a step or more for each: 256 rows of
-    // mixed requests 81 us, once 92, four times 102; all of one kind, top k, 35, 27 and 54.
+    // 131072 bf16, mixed requests: 81 us, once 92, four times 102; all of one kind, top k, 35, 27 and 54.  Rows of 256 KB and more
+    // are shared by two at least, as mixed requests end unevenly (1024 rows: 230 us, by one CTA each 266; 600 of one kind 128 and 139;
+    // rows of 200 KB 113 and 103).
+    const int least = vecs >= 16 * TPB * U ? 2 : 1;
     int ctas = MOST_CTAS;
-    while (ctas > 1 && (T * ctas > 2 * 148 * RESIDENT || vecs < int64_t(ctas) * TPB * U)) ctas /= 2;
+    while (ctas > least && (T * ctas > 2 * 148 * RESIDENT || vecs < int64_t(ctas) * TPB * U)) ctas /= 2;
     if (T * ctas >= lim) return int(MV_ERR_INVALID_ARG);
     const int64_t n_steps = ((vecs + ctas - 1) / ctas + CHUNK / Vec<X>::N + TPB * U - 1) / (TPB * U);
     a.steps = int((n_steps + GROUPS - 1) / GROUPS);

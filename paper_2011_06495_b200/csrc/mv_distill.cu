@@ -34,6 +34,7 @@ struct DistillArgs {
   int64_t V, ld;
   Teacher h;
   float scale;
+  int marks;                         // words of marks that a row needs, at most MARKS
   float *kl, *lse, *log_rest;
 };
 
@@ -44,7 +45,7 @@ constexpr int MARKS = 4096;          // words of marks: one for each thread and 
 // off it would leave nothing of a small rest): a bit for every logit of the next steps, set for the listed ones, which a thread asks
 // one word at a time; their own terms are added at the end.  Memory bounds it: 8192 x 65536 bf16 162 us (6.6 TB/s), with 32 alternatives
 // and the rest 169.  The end of a row, some microseconds of latency for its list, is covered by the other CTAs unless rows are short
-// (16000 x 8000: 71 us of 39) or few (64 x 131072: 19 us).
+// (16000 x 8000: 68 us of 39) or few (64 x 131072: 19 us).
 template <typename X, bool REST, int TPB>
 __global__ void __launch_bounds__(TPB, 1024 / TPB) k_distill(const X* __restrict__ logits, const __grid_constant__ DistillArgs a) {
   constexpr int N = Vec<X>::N, WARPS = TPB / 32, WINDOW = MARKS / TPB;
@@ -53,7 +54,7 @@ __global__ void __launch_bounds__(TPB, 1024 / TPB) k_distill(const X* __restrict
   __shared__ uint32_t s_ends;
   __shared__ int s_twice;
   uint32_t* mark = dynamic;          // [step of the window][thread], with REST
-  const List list(dynamic + (REST ? MARKS : 0), a.h.k);
+  const List list(dynamic + (REST ? a.marks : 0), a.h.k);
   const int64_t t = blockIdx.x;
   const int tid = threadIdx.x, lane = tid & 31, w = tid >> 5;
   const X* row = logits + t * a.ld;
@@ -432,7 +433,9 @@ int mv_distill(void* stream, const void* logits, int type, int64_t T, int64_t V,
     // short rows take few threads and many CTAs, if there are rows enough to fill the device; long or few rows many threads (the sides of
     // this rule as measured for the log probabilities, whose stream is the same)
     const int tpb = T >= 1184 && vecs <= 3000 ? 64 : vecs > 10240 || (T < 600 && vecs > 6000) ? 256 : 128;
-    const size_t smem = size_t(k) * LIST_BYTES + (rest ? MARKS * 4 : 0);
+    const int64_t words = (vecs + tpb * U - 1) / (tpb * U) * tpb;
+    a.marks = !rest ? 0 : words > MARKS ? MARKS : int(words);        // short rows leave room for more CTAs
+    const size_t smem = size_t(k) * LIST_BYTES + size_t(a.marks) * 4;
     auto launch = [&](auto r) {
       constexpr bool REST = decltype(r)::value;
       auto* kernel = tpb == 64 ? k_distill<X, REST, 64> : tpb == 128 ? k_distill<X, REST, 128> : k_distill<X, REST, 256>;

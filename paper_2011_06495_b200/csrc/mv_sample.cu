@@ -804,16 +804,20 @@ __global__ void __launch_bounds__(TPB, RESIDENT) k_sample(const X* __restrict__ 
       double last = tid == TPB - 1 ? c[PER - 1] * exp2(-double(FINE - 1) / 128.0) * (1.0 + 1e-4) : 0.0;      // the last bin's may be nothing
       double at_most = scan_before(most, s, all_most), at_least = scan_before((most - last) * low, s, all_least);
       v = top;
-      bool lo_done = (1.0 - p) * at_most >= p * (all_least - at_least), hi_done = (1.0 - p) * at_least >= p * (all_most - at_most);
-      if (tid == 0) lo_done = hi_done = false;
+      // Two threads may each see their first one at their border, where the scan and the running sum round differently: the lower one counts, in
+      // every CTA of the cluster alike.
+      unsigned lo_at = FINE - 1, hi_at = FINE - 1;
       for (int j = 0; j < PER; ++j, v *= step) {
         at_most += c[j] * v;
         at_least += c[j] * v * low;
-        const bool lo_now = (1.0 - p) * at_most >= p * (all_least - at_least), hi_now = (1.0 - p) * at_least >= p * (all_most - at_most);
-        if (lo_now && !lo_done) s.first_bin = tid * PER + j;
-        if (hi_now && !hi_done) s.last_bin = tid * PER + j;
-        lo_done |= lo_now;
-        hi_done |= hi_now;
+        if ((1.0 - p) * at_most >= p * (all_least - at_least)) lo_at = min(lo_at, unsigned(tid * PER + j));
+        if ((1.0 - p) * at_least >= p * (all_most - at_most)) hi_at = min(hi_at, unsigned(tid * PER + j));
+      }
+      lo_at = __reduce_min_sync(0xffffffffu, lo_at);
+      hi_at = __reduce_min_sync(0xffffffffu, hi_at);
+      if (lane == 0) {
+        atomicMin(&s.first_bin, int(lo_at));
+        atomicMin(&s.last_bin, int(hi_at));
       }
     }
     __syncthreads();

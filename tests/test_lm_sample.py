@@ -186,6 +186,30 @@ def test_nuclei_of_every_size():
         check(x, u, None, None, None, p)
 
 
+def test_top_p_that_ends_where_two_threads_bins_meet():
+    """The count by bins of 1/128 of a power of two, 16 bins a thread, bounds the start from above and below: p as near as 32 bits come to each
+    bound at every thread's border, in rows of one CTA and in rows that a cluster shares."""
+    V, per, n = 40_960, 16, 120
+    bins = np.random.default_rng(5).integers(0, 4000, V)
+    step = 2.0 ** (-1 / 128)
+    weight = np.bincount(bins, minlength=4096) * step ** np.arange(4096)
+    most, least = np.cumsum(weight * (1 + 1e-4)), np.cumsum(weight * (1 + 1e-4) * step * (1 - 2e-4))
+    at = np.arange(1, n + 1) * per - 1
+    low, high = most[at] / (most[at] + least[-1] - least[at]), least[at] / (least[at] + most[-1] - most[at])
+    p = torch.from_numpy(np.concatenate([low, high])).float().to(DEV)
+    row = torch.from_numpy(-(bins + 0.5) * math.log(2) / 128).float().to(DEV)
+    many = p.repeat(3)                                       # 720 rows: one CTA each
+    u = torch.rand(len(p), generator=gen(8), device=DEV)
+    token, lp = draw(row.repeat(len(many), 1), u.repeat(3), None, None, many)
+    for j in range(0, len(p), 40):                           # 40 rows: eight CTAs each
+        few = draw(row.repeat(40, 1), u[j:j + 40].contiguous(), None, None, p[j:j + 40].contiguous())
+        for part in range(3):
+            here = slice(part * len(p) + j, part * len(p) + j + 40)
+            assert torch.equal(few[0], token[here]) and torch.equal(few[1], lp[here])
+    some = slice(0, len(p), 17)
+    check(row.repeat(len(p[some]), 1), u[some].contiguous(), None, None, p[some].contiguous())
+
+
 @pytest.mark.parametrize("dt", [BF16, F16, F32])
 @pytest.mark.parametrize("V,offset", [(3001, 1), (60_000, 0), (131_072, 3), (200_003, 0)])
 @pytest.mark.parametrize("mean,std", [(0.0, 2.0), (10.0, 2.0), (20.0, 0.5), (-30.0, 4.0), (0.0, 0.01)])

@@ -120,8 +120,13 @@ __global__ void __launch_bounds__(L > 32 ? WIDE_TPB : NORM_TPB, L > 32 ? 1 : 2) 
 #pragma unroll
     for (int i = 0; i < NV; ++i)
       if (at + i * L < r.nv) {
-        next[i] = __ldg(p + i * L);
-        if constexpr (APART) more[i] = __ldg(p + i * L + 1);
+        // in place (never APART) the rows are written by this kernel, which the non-coherent path does not allow for
+        if constexpr (APART) {
+          next[i] = __ldg(p + i * L);
+          more[i] = __ldg(p + i * L + 1);
+        } else {
+          next[i] = __ldcs(p + i * L);
+        }
       }
     const int ends = D - r.nv * N;
 #pragma unroll

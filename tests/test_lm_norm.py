@@ -99,6 +99,19 @@ def test_rows_without_parameters_in_place_and_far_from_zero(dt, D):
         assert torch.equal(run_forward(x[r:r + 1], w, b, 1e-3)[0], y[r:r + 1])
 
 
+@pytest.mark.parametrize("dt", [F32, BF16])
+@pytest.mark.parametrize("T,D", [(9000, 1001), (20_000, 77), (4000, 4099)])
+def test_many_rows_in_place_off_the_boundaries(dt, T, D):
+    """Neighbouring rows share sectors of memory, one of which is read while the other is written: the bytes are those of a call out of place."""
+    x = torch.randn((T, D), generator=gen(D), device=DEV).to(dt)
+    w, b = parameters(D, F32, 1)
+    want = run_forward(x, w, b)
+    for _ in range(3):
+        z = x.clone()
+        got = run_forward(z, w, b, y=z)
+        assert all(torch.equal(p, q) for p, q in zip(got, want))
+
+
 def test_rows_with_nan_and_inf_leave_the_others_alone():
     for D in (5, 1024, 1001):
         x = torch.randn((40, D), generator=gen(D), device=DEV).to(BF16)

@@ -46,6 +46,9 @@ inline bool share_bytes(const void* p, int64_t rows, int64_t cols, int64_t ld, i
   return to < uintptr_t(cols) * size || pitch - to < uintptr_t(cols2) * size2;
 }
 
+// Dynamic shared memory that a kernel may use without asking: the limit of 48 KB counts its static shared memory (up to 1 KB here) too.
+constexpr size_t SMEM_UNASKED = 47 * 1024;
+
 // Lets a kernel use `bytes` of dynamic shared memory; asked of the driver once per kernel (a static of the caller) and device.
 struct SmemLimit { int bytes[64]; };
 template <typename K> bool allow_smem(K* kernel, int bytes, SmemLimit* have) {

@@ -304,7 +304,7 @@ int mv_layer_norm(void* stream, const void* x, int type, int64_t T, int64_t D, i
       int64_t ctas = T / (groups * 8);
       ctas = ctas < resident * 148 ? resident * 148 : ctas > resident * 148 * WAVES ? resident * 148 * WAVES : ctas;
       a.per = ((T + ctas - 1) / ctas + groups - 1) / groups * groups;
-      if (smem > 48 * 1024 && !allow_smem(kernel, int(smem), limit)) return int(MV_ERR_CUDA);
+      if (smem > SMEM_UNASKED && !allow_smem(kernel, int(smem), limit)) return int(MV_ERR_CUDA);
       kernel<<<unsigned((T + a.per - 1) / a.per), unsigned(threads), smem, st>>>(xp, yp, a);
       return cuda_ok();
     };

@@ -333,7 +333,7 @@ int mv_layer_norm_grad(void* stream, const void* dy, int64_t lddy, const void* x
         if (GROUPS > 1 && smem < size_t(GROUPS * 8 * D)) smem = size_t(GROUPS * 8 * D);
         auto* kernel = k_norm_grad<X, VEC, L, NV, R>;
         static SmemLimit limit;
-        if (smem > 48 * 1024 && !allow_smem(kernel, int(smem), &limit)) return int(MV_ERR_CUDA);
+        if (smem > SMEM_UNASKED && !allow_smem(kernel, int(smem), &limit)) return int(MV_ERR_CUDA);
         kernel<<<unsigned(a.parts), THREADS, smem, st>>>(yp, xp, dxp, a);
         return cuda_ok();
       });

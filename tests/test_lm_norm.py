@@ -112,6 +112,27 @@ def test_many_rows_in_place_off_the_boundaries(dt, T, D):
         assert all(torch.equal(p, q) for p, q in zip(got, want))
 
 
+@pytest.mark.parametrize("dt", [F32, BF16, F16])
+def test_widths_at_the_limits_of_shared_memory(dt):
+    """6129 to 6144 columns need just 48 KB for their parameters, beside a little static shared memory; the gradient gets there at widths that
+    hang on the type and the alignment, so that every width up to 6200 has to be taken at least."""
+    for T in (2, 1300):
+        for D in (6128, 6129, 6136, 6143, 6144, 6145):
+            x = torch.randn((T, D), generator=gen(D), device=DEV).to(dt)
+            w, b = parameters(D, F32)
+            check_forward(x[:20], w, b)
+            y = run_forward(x, w, b)[0]
+            assert torch.isfinite(y).all()
+    stats, dw, db = torch.ones(1300, device=DEV), torch.empty(6200, device=DEV), torch.empty(6200, device=DEV)
+    ws = torch.empty(max(B.layer_norm_grad_workspace_bytes(1300, D) for D in range(1, 6200)), dtype=torch.uint8, device=DEV)
+    x = torch.zeros((1300, 6200), dtype=dt, device=DEV)
+    for D in range(1, 6200):                                 # refused by the launch, if at all
+        for T in (2, 1300) if D % 16 == 0 else (2,):
+            B.mv_layer_norm_grad(x[:T, :D], x[:T, :D], None, stats[:T], stats[:T], None, dw[:D], db[:D], ws)
+            B.mv_layer_norm(x[:T, :D], None, None, x[:T, :D])
+    torch.cuda.synchronize()
+
+
 def test_rows_with_nan_and_inf_leave_the_others_alone():
     for D in (5, 1024, 1001):
         x = torch.randn((40, D), generator=gen(D), device=DEV).to(BF16)

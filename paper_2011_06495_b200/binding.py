@@ -256,6 +256,7 @@ def mv_dequantize(words, K: int, q: int, out, stream: Optional[torch.cuda.Stream
 _TYPES = {torch.float32: MV_F32, torch.bfloat16: MV_BF16, torch.float16: MV_F16, torch.int32: MV_I32, torch.int64: MV_I64}
 _VALUES, _IDS, _FLOAT, _INT32 = (MV_F32, MV_BF16, MV_F16), (MV_I32, MV_I64), (MV_F32,), (MV_I32,)
 _raw_current_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)     # absent from a torch without CUDA
+_current_device = getattr(torch._C, "_cuda_getDevice", None)
 
 
 def _need(ok: bool, where: str):
@@ -265,6 +266,9 @@ def _need(ok: bool, where: str):
 
 
 def _raw_stream(device_index: int, stream: Optional[torch.cuda.Stream]):
+    """The stream of a call on tensors of that device, which has to be the current one: kernels are launched there, whatever their
+    pointers' device, and the default stream's handle is the same on all of them."""
+    _need(_current_device() == device_index and (stream is None or stream.device_index == device_index), "device")
     return stream.cuda_stream if stream is not None else _raw_current_stream(device_index)
 
 

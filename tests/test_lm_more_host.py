@@ -91,3 +91,16 @@ def test_sample_refusals(lib):
               dict(c=ODD), dict(k=ODD), dict(p=ODD), dict(m=ODD), dict(y=at(0x300004)), dict(lp=ODD)):
         assert call(**k) == BAD, k
     assert call(T=0) == B.MV_OK
+
+
+def test_tensors_and_streams_of_another_device_than_the_current_one(monkeypatch):
+    class Stream:
+        def __init__(self, device):
+            self.device_index, self.cuda_stream = device, 0x1234
+
+    monkeypatch.setattr(B, "_current_device", lambda: 1)
+    monkeypatch.setattr(B, "_raw_current_stream", lambda device: 0x5678)
+    assert B._raw_stream(1, None) == 0x5678 and B._raw_stream(1, Stream(1)) == 0x1234
+    for device, stream in ((0, None), (0, Stream(0)), (1, Stream(0))):
+        with pytest.raises(B.MvError):
+            B._raw_stream(device, stream)

@@ -135,7 +135,7 @@ int mv_distill(void* stream, const void* logits, int type, int64_t T, int64_t V,
  *   dlogits[t, v] = scale g[t] (M p_v - sum_{j: id_j = v} q_j) for a listed token v,  scale g[t] p_v (M - r / P) for the others
  * with log p_v = min(0, scale logits[t, v] - lse[t]).
  *   lse, log_rest [T] float in, as mv_distill left them (log_rest NULL: rest = 0);  g [T] float in
- *   dlogits [T, V] out, of the logits' type, rows ldg >= V apart; may be the logits themselves (then ldg = ld)
+ *   dlogits [T, V] out, of the logits' type, rows ldg >= V apart; may be the logits themselves (then ldg = ld), else no bytes of any input
  * A row without a teacher, with g[t] = 0 or with lse = -inf is +0 whatever its logits hold; where log_rest is -inf, the others are 0. */
 int mv_distill_grad(void* stream, const void* logits, int type, int64_t T, int64_t V, int64_t ld, const float* top_logprob,
                     const void* top_id, int id_type, int k, float scale, const float* lse, const float* log_rest, const float* g,

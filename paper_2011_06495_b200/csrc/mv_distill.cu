@@ -459,6 +459,8 @@ int mv_distill_grad(void* stream, const void* logits, int type, int64_t T, int64
   if ((share_bytes(logits, T, V, ld, size, dlogits, T, V, ldg, size) && !(logits == dlogits && ld == ldg)) ||
       share_bytes(dlogits, T, V, ldg, size, top_logprob, T, k, k, 4) || share_bytes(dlogits, T, V, ldg, size, top_id, T, k, k, type_size(id_type)))
     return MV_ERR_INVALID_ARG;
+  for (const float* p : {lse, log_rest, g})            // which a row's other CTAs may have yet to read
+    if (share_vector(p, T, 4, dlogits, T, V, ldg, size)) return MV_ERR_INVALID_ARG;
   DistillGradArgs a;
   a.V = V; a.ld = ld; a.ldg = ldg; a.h = {top_logprob, top_id, id_type, k, log_rest ? 1 : 0}; a.scale = scale; a.lse = lse; a.log_rest = log_rest; a.g = g;
   return with_type(type, [&](auto x) {

@@ -46,6 +46,11 @@ inline bool share_bytes(const void* p, int64_t rows, int64_t cols, int64_t ld, i
   return to < uintptr_t(cols) * size || pitch - to < uintptr_t(cols2) * size2;
 }
 
+// The same for a vector of n elements beside a matrix; an empty or absent one shares nothing.
+inline bool share_vector(const void* v, int64_t n, int size, const void* p, int64_t rows, int64_t cols, int64_t ld, int size2) {
+  return v && p && n > 0 && share_bytes(p, rows, cols, ld, size2, v, 1, n, n, size);
+}
+
 // Dynamic shared memory that a kernel may use without asking: the limit of 48 KB counts its static shared memory (up to 1 KB here) too.
 constexpr size_t SMEM_UNASKED = 47 * 1024;
 

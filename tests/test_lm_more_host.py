@@ -104,3 +104,14 @@ def test_tensors_and_streams_of_another_device_than_the_current_one(monkeypatch)
     for device, stream in ((0, None), (0, Stream(0)), (1, Stream(0))):
         with pytest.raises(B.MvError):
             B._raw_stream(device, stream)
+
+
+def test_a_gradient_of_the_distillation_that_shares_bytes_with_what_its_rows_are_weighed_by(lib):
+    """dlogits: 4 rows of 30 floats from 0x500000 on, 480 bytes; with a pitch of 40, gaps of 40 bytes behind each row."""
+    def call(ldg=30, lse=S, lr=S, g=S):
+        return lib.mv_distill_grad(None, P, B.MV_F32, 4, 30, 30, Q, R, B.MV_I32, 3, 1.0, lse, lr, g, at(0x500000), ldg)
+
+    for where in ("lse", "lr", "g"):
+        for inside in (0x500000, 0x500000 + 476, 0x500000 - 12):
+            assert call(**{where: at(inside)}) == BAD, (where, inside)
+        assert call(ldg=40, **{where: at(0x500000 + 108)}) == BAD and call(ldg=40, **{where: at(0x500000 + 148)}) == BAD

@@ -68,6 +68,7 @@ int mv_embed_grad(void* stream, const void* dout, int dout_type, int64_t ldd, co
  *   x [T, D] type in, rows ldx >= D apart;  y [T, D] out, of the same type, rows ldy >= D apart; may be x itself (then ldy = ldx)
  *   weight, bias [D] w_type in: MV_F32 or x's type; each may be NULL (1 and 0)
  *   mean, rstd [T] float out (mu and r), what the gradient needs; each may be NULL
+ * What is written shares no bytes with anything else, y with x excepted.
  * eps >= 0, finite.  A row that holds an inf or a NaN, or whose sums pass the range of 32 bits, has no other meaning than the
  * formula's in 32 bits.  Limits: 0 <= T < 2^31, 1 <= D < 2^31. */
 int mv_layer_norm(void* stream, const void* x, int type, int64_t T, int64_t D, int64_t ldx, const void* weight, const void* bias, int w_type,

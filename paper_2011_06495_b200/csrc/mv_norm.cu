@@ -287,6 +287,12 @@ int mv_layer_norm(void* stream, const void* x, int type, int64_t T, int64_t D, i
   if ((share_bytes(x, T, D, ldx, size, y, T, D, ldy, size) && !(x == y && ldx == ldy)) || (weight && share_bytes(y, T, D, ldy, size, weight, 1, D, D, wsize)) ||
       (bias && share_bytes(y, T, D, ldy, size, bias, 1, D, D, wsize)))
     return MV_ERR_INVALID_ARG;
+  // the statistics of a row are written while others are read and written
+  for (const float* p : {mean, rstd})
+    if (share_vector(p, T, 4, x, T, D, ldx, size) || share_vector(p, T, 4, y, T, D, ldy, size) || share_vector(p, T, 4, weight, 1, D, D, wsize) ||
+        share_vector(p, T, 4, bias, 1, D, D, wsize))
+      return MV_ERR_INVALID_ARG;
+  if (share_vector(mean, T, 4, rstd, 1, T, T, 4)) return MV_ERR_INVALID_ARG;
   if (T == 0) return MV_OK;
   NormArgs a;
   a.T = T; a.D = D; a.ldx = ldx; a.ldy = ldy; a.weight = weight; a.bias = bias; a.w_type = w_type; a.eps = eps; a.mean = mean; a.rstd = rstd;

@@ -115,3 +115,14 @@ def test_a_gradient_of_the_distillation_that_shares_bytes_with_what_its_rows_are
         for inside in (0x500000, 0x500000 + 476, 0x500000 - 12):
             assert call(**{where: at(inside)}) == BAD, (where, inside)
         assert call(ldg=40, **{where: at(0x500000 + 108)}) == BAD and call(ldg=40, **{where: at(0x500000 + 148)}) == BAD
+
+
+def test_statistics_of_the_layer_norm_that_share_bytes_with_anything(lib):
+    """x: 4 rows of 8 bf16 in a pitch of 8, 64 bytes from 0x100000 on; weight and bias: 32 bytes from 0x200000 and 0x200100 on; y from 0x300000 on."""
+    def call(m=S, r=at(0x500000), ldy=8, y=R):
+        return lib.mv_layer_norm(None, P, B.MV_BF16, 4, 8, 8, Q, at(0x200100), B.MV_F32, 1e-5, y, ldy, m, r)
+
+    for inside in (0x100000, 0x10003c, 0x100000 - 12, 0x200000, 0x20001c, 0x200100 - 4, 0x300000, 0x30003c):
+        assert call(m=at(inside)) == BAD and call(r=at(inside)) == BAD, hex(inside)
+    assert call(r=S) == BAD and call(r=at(0x400000 + 12)) == BAD
+    assert call(ldy=16, m=at(0x300000 + 8)) == BAD and call(y=P, m=at(0x100020)) == BAD

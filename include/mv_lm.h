@@ -83,6 +83,7 @@ size_t mv_layer_norm_grad_workspace_bytes(int64_t T, int64_t D);
  *   dx [T, D] out, of the same type, rows lddx apart; may be dy or x itself (of the same pitch); NULL: not wanted
  *   dweight, dbias [D] float out, each may be NULL.  accumulate = 0: overwritten (T = 0: zeros); accumulate = 1: added to
  *   workspace  mv_layer_norm_grad_workspace_bytes(T, D) bytes, 16-byte aligned (unused, and may be NULL, without dweight and dbias)
+ * dx, dweight, dbias and the workspace share no bytes with one another or with an input, dx with dy or x excepted.
  * The sums over rows are in 32 bits, in an order that the sizes, the type and the rows' places within 16 bytes fix. */
 int mv_layer_norm_grad(void* stream, const void* dy, int64_t lddy, const void* x, int64_t ldx, int type, int64_t T, int64_t D,
                        const void* weight, int w_type, const float* mean, const float* rstd, void* dx, int64_t lddx, float* dweight,

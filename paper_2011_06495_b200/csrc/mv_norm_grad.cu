@@ -287,7 +287,20 @@ int mv_layer_norm_grad(void* stream, const void* dy, int64_t lddy, const void* x
               (weight && share_bytes(weight, 1, D, D, wsize, p, 1, D, D, 4))))
       return MV_ERR_INVALID_ARG;
   if (dweight && dbias && share_bytes(dweight, 1, D, D, 4, dbias, 1, D, D, 4)) return MV_ERR_INVALID_ARG;
-  if ((dweight || dbias) && (!workspace || workspace_bytes < mv_layer_norm_grad_workspace_bytes(T, D))) return MV_ERR_WORKSPACE;
+  for (const float* p : {mean, rstd})
+    if (share_vector(p, T, 4, dx, T, D, lddx, size)) return MV_ERR_INVALID_ARG;
+  if (dweight || dbias) {
+    const size_t need = mv_layer_norm_grad_workspace_bytes(T, D);
+    if (!workspace || workspace_bytes < need) return MV_ERR_WORKSPACE;
+    const int64_t words = int64_t(need / 4);
+    if (share_vector(workspace, words, 4, x, T, D, ldx, size) || share_vector(workspace, words, 4, dy, T, D, lddy, size) ||
+        share_vector(workspace, words, 4, dx, T, D, lddx, size) || share_vector(workspace, words, 4, weight, 1, D, D, wsize))
+      return MV_ERR_INVALID_ARG;
+    for (const float* p : {mean, rstd})
+      if (share_vector(p, T, 4, workspace, 1, words, words, 4)) return MV_ERR_INVALID_ARG;
+    for (const float* p : {dweight, dbias})
+      if (share_vector(p, D, 4, workspace, 1, words, words, 4)) return MV_ERR_INVALID_ARG;
+  }
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   if (T == 0) {
     if (accumulate) return MV_OK;

@@ -126,3 +126,19 @@ def test_statistics_of_the_layer_norm_that_share_bytes_with_anything(lib):
         assert call(m=at(inside)) == BAD and call(r=at(inside)) == BAD, hex(inside)
     assert call(r=S) == BAD and call(r=at(0x400000 + 12)) == BAD
     assert call(ldy=16, m=at(0x300000 + 8)) == BAD and call(y=P, m=at(0x100020)) == BAD
+
+
+def test_gradients_of_the_layer_norm_that_share_bytes_with_statistics_or_workspace(lib):
+    """x, dy, dx: 100 rows of 8 floats, 3200 bytes from 0x100000, 0x200000 and 0x300000 on; vectors and the workspace behind them."""
+    need = B.layer_norm_grad_workspace_bytes(100, 8)
+
+    def call(dx=R, m=S, r=at(0x500000), dw=at(0x600000), ws=at(0x700000), w=at(0x600100)):
+        return lib.mv_layer_norm_grad(None, P, 8, Q, 8, B.MV_F32, 100, 8, w, B.MV_F32, m, r, dx, 8, dw, None, 0, ws, need)
+
+    for inside in (0x300000, 0x300c7c, 0x300000 - 396):
+        assert call(m=at(inside)) == BAD and call(r=at(inside)) == BAD
+    for other in (0x100000, 0x200000, 0x300000, 0x400000, 0x500000, 0x600000, 0x600100):
+        for ws in (other, other - need + 16, other + 16):
+            assert call(ws=at(ws)) == BAD, hex(ws)
+    assert lib.mv_layer_norm_grad(None, P, 8, Q, 8, B.MV_F32, 100, 8, None, B.MV_F32, S, S, R, 8, None, at(0x700010), 0, at(0x700000), need) == BAD
+    assert lib.mv_layer_norm_grad(None, P, 8, Q, 8, B.MV_F32, 100, 8, None, B.MV_F32, S, S, R, 8, at(0x700000 - 16), None, 0, at(0x700000), need) == BAD

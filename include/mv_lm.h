@@ -124,6 +124,7 @@ int mv_token_logprob_grad(void* stream, const void* logits, int type, int64_t T,
  *             the student's mass outside the list P = 1 - sum of p over the listed tokens:  kl = ... + r (log r - log P)
  *   logits [T, V] type in, rows ld >= V apart;  top_logprob, top_id [T, k] float / id_type in, contiguous, 1 <= k <= MV_TEACHER_MAX
  *   kl, lse, log_rest [T] float out, each may be NULL: the divergence, log sum exp of the scaled logits, and log P (rest = 1 only)
+ *           They share no bytes with the inputs or one another.
  * An id outside [0, V) is no alternative, nor is a_j = -inf with rest = 0.  A row without one has no teacher: kl 0 whatever its
  * logits hold, log_rest as if the list were empty.  The same id twice is two terms of the sums, but one token.  q_j = 0 adds
  * nothing; q_j > 0 where p_j = 0 (a masked logit, a row that is all -inf) makes kl +inf.  P is summed without the listed tokens,

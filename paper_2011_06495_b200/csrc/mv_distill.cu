@@ -425,6 +425,13 @@ int mv_distill(void* stream, const void* logits, int type, int64_t T, int64_t V,
       misaligned(kl, 4) || misaligned(lse, 4) || misaligned(log_rest, 4))
     return MV_ERR_INVALID_ARG;
   if (T == 0) return MV_OK;
+  // a row's results are written while other rows are read
+  for (const float* p : {kl, lse, log_rest})
+    if (share_vector(p, T, 4, logits, T, V, ld, type_size(type)) || share_vector(p, T, 4, top_logprob, T, k, k, 4) ||
+        share_vector(p, T, 4, top_id, T, k, k, type_size(id_type)))
+      return MV_ERR_INVALID_ARG;
+  if (share_vector(kl, T, 4, lse, 1, T, T, 4) || share_vector(kl, T, 4, log_rest, 1, T, T, 4) || share_vector(lse, T, 4, log_rest, 1, T, T, 4))
+    return MV_ERR_INVALID_ARG;
   DistillArgs a;
   a.V = V; a.ld = ld; a.h = {top_logprob, top_id, id_type, k, rest}; a.scale = scale; a.kl = kl; a.lse = lse; a.log_rest = log_rest;
   return with_type(type, [&](auto x) {

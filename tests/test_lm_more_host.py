@@ -142,3 +142,14 @@ def test_gradients_of_the_layer_norm_that_share_bytes_with_statistics_or_workspa
             assert call(ws=at(ws)) == BAD, hex(ws)
     assert lib.mv_layer_norm_grad(None, P, 8, Q, 8, B.MV_F32, 100, 8, None, B.MV_F32, S, S, R, 8, None, at(0x700010), 0, at(0x700000), need) == BAD
     assert lib.mv_layer_norm_grad(None, P, 8, Q, 8, B.MV_F32, 100, 8, None, B.MV_F32, S, S, R, 8, at(0x700000 - 16), None, 0, at(0x700000), need) == BAD
+
+
+def test_results_of_the_distillation_that_share_bytes_with_its_inputs(lib):
+    """logits: 4 rows of 30 bf16, 240 bytes from 0x100000 on; alternatives and ids: 48 and 96 bytes from 0x200000 and 0x300000 on."""
+    def call(kl=S, lse=at(0x500000), lr=at(0x600000)):
+        return lib.mv_distill(None, P, B.MV_BF16, 4, 30, 30, Q, R, B.MV_I64, 3, 1, 1.0, kl, lse, lr)
+
+    for name in ("kl", "lse", "lr"):
+        for inside in (0x100000, 0x1000ec, 0x100000 - 12, 0x200000, 0x20002c, 0x300000, 0x30005c):
+            assert call(**{name: at(inside)}) == BAD, (name, hex(inside))
+    assert call(lse=S) == BAD and call(lr=S) == BAD and call(lr=at(0x500000 + 12)) == BAD

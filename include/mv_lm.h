@@ -153,7 +153,8 @@ int mv_distill_grad(void* stream, const void* logits, int type, int64_t T, int64
  *   logits [T, V] type in, rows ld >= V apart;  u [T] float in, in [0, 1) (below: 0; from 1 on: the last kept token that has a weight)
  *   scale, top_p, min_p [T] float in, top_k [T] int32 in, on the device, each may be NULL: 1, 1 (all), 0 (all), 0 (all).
  *           scale > 0, an inverse temperature; top_k <= 0 or >= V, top_p >= 1, min_p <= 0: nothing is cut
- *   token [T] id_type out;  logprob [T] float out, may be NULL
+ *   token [T] id_type out;  logprob [T] float out, may be NULL.  They share no bytes with the inputs or one another, but each may
+ *           take the very place of u or a setting, element for element of 4 bytes
  * -inf marks a masked logit, which is never drawn.  A row with nothing else has token -1 and logprob -inf.  A row with a NaN or
  * +inf, with a NaN among its settings, or whose scale is not positive and finite, has token -1 and logprob NaN.
  * Limits as mv_token_logprob. */

@@ -1123,6 +1123,16 @@ int mv_sample(void* stream, const void* logits, int type, int64_t T, int64_t V, 
       misaligned(min_p, 4) || misaligned(logprob, 4))
     return MV_ERR_INVALID_ARG;
   if (T == 0) return MV_OK;
+  // a row's results are written while other rows are read; in the very place of its random number or of a setting they are not in the way
+  const int token_size = type_size(id_type);
+  const void *results[] = {token, logprob}, *inputs[] = {u, scale, top_k, top_p, min_p};
+  for (int i = 0; i < 2; ++i) {
+    const int size = i ? 4 : token_size;
+    if (share_vector(results[i], T, size, logits, T, V, ld, type_size(type))) return MV_ERR_INVALID_ARG;
+    for (const void* p : inputs)
+      if (share_vector(results[i], T, size, p, 1, T, T, 4) && !(p == results[i] && size == 4)) return MV_ERR_INVALID_ARG;
+  }
+  if (share_vector(token, T, token_size, logprob, 1, T, T, 4)) return MV_ERR_INVALID_ARG;
   SampleArgs a;
   a.V = V; a.ld = ld; a.u = u; a.scale = scale; a.top_k = top_k; a.top_p = top_p; a.min_p = min_p; a.token = token; a.id_type = id_type; a.logprob = logprob;
   a.unit = 0x1p51;                   // one of 2^52 has to fit the lower bits of a double

@@ -153,3 +153,15 @@ def test_results_of_the_distillation_that_share_bytes_with_its_inputs(lib):
         for inside in (0x100000, 0x1000ec, 0x100000 - 12, 0x200000, 0x20002c, 0x300000, 0x30005c):
             assert call(**{name: at(inside)}) == BAD, (name, hex(inside))
     assert call(lse=S) == BAD and call(lr=S) == BAD and call(lr=at(0x500000 + 12)) == BAD
+
+
+def test_tokens_and_log_probabilities_that_share_bytes_with_what_other_rows_read(lib):
+    """logits: 4 rows of 30 f16, 240 bytes from 0x100000 on; u from 0x200000, settings behind it."""
+    def call(y=R, it=B.MV_I64, lp=S, c=at(0x200100), k=at(0x200200), p=at(0x200300), m=at(0x200400)):
+        return lib.mv_sample(None, P, B.MV_F16, 4, 30, 30, Q, c, k, p, m, y, it, lp)
+
+    for inside in (0x100000, 0x1000e8, 0x100000 - 8):
+        assert call(y=at(inside)) == BAD and call(lp=at(inside)) == BAD and call(y=at(inside), it=B.MV_I32) == BAD
+    for other in (0x200000, 0x200100, 0x200200, 0x200300, 0x200400):
+        assert call(y=at(other)) == BAD and call(y=at(other + 4), it=B.MV_I32) == BAD and call(lp=at(other + 12)) == BAD and call(lp=at(other - 4)) == BAD
+    assert call(lp=R) == BAD and call(lp=R, it=B.MV_I32) == BAD and call(lp=at(0x300000 + 28)) == BAD

@@ -277,6 +277,18 @@ def test_fewer_candidates_than_the_top_k_asks_for(dt, V, offset):
         check(x, u, scale, k, p, mp)
 
 
+@pytest.mark.parametrize("T,V", [(3, 131_072), (700, 5001)])
+def test_results_in_the_place_of_u_and_of_settings(T, V):
+    x = head(T, V, BF16, 9)
+    u, k = torch.rand(T, generator=gen(10), device=DEV), torch.full((T,), 40, dtype=torch.int32, device=DEV)
+    p = torch.full((T,), 0.95, device=DEV)
+    for kk, pp in ((k, p), (None, p), (k, None), (None, None)):
+        token, lp = draw(x, u, None, kk, pp, it=torch.int32)
+        u2, k2 = u.clone(), k.clone()
+        B.mv_sample(x, u2, k2, top_k=k2 if kk is not None else None, top_p=pp, logprob=u2)
+        assert torch.equal(k2, token) and torch.equal(u2, lp)
+
+
 def test_frequencies_are_the_probabilities():
     """The same row with an even grid of u: every token as often as its share of the grid, to within one of the grid's steps."""
     T, V = 4096, 50

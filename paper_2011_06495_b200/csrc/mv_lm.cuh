@@ -5,6 +5,8 @@
 #include <cuda_fp16.h>
 #include <stdint.h>
 
+#include <mutex>
+
 #include "../../include/mv_sparse.h"
 #include "../../include/mv_lm.h"
 
@@ -54,11 +56,16 @@ inline bool share_vector(const void* v, int64_t n, int size, const void* p, int6
 // Dynamic shared memory that a kernel may use without asking: the limit of 48 KB counts its static shared memory (up to 1 KB here) too.
 constexpr size_t SMEM_UNASKED = 47 * 1024;
 
-// Lets a kernel use `bytes` of dynamic shared memory; asked of the driver once per kernel (a static of the caller) and device.
-struct SmemLimit { int bytes[64]; };
+// Lets a kernel use `bytes` of dynamic shared memory; asked of the driver once per kernel (a static of the caller) and device, by one host
+// thread at a time, so that what one was granted is not taken back by another's smaller request.
+struct SmemLimit {
+  int bytes[64] = {};
+  std::mutex asking;
+};
 template <typename K> bool allow_smem(K* kernel, int bytes, SmemLimit* have) {
   int dev = 0;
   if (cudaGetDevice(&dev) != cudaSuccess) return false;
+  const std::lock_guard<std::mutex> lock(have->asking);
   if (dev < 64 && have->bytes[dev] >= bytes) return true;
   if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes) != cudaSuccess) {
     cudaGetLastError();

@@ -1,6 +1,8 @@
 """CPU checks of layer norm, distillation and sampling (include/mv_lm.h): the refusals that happen before anything is enqueued."""
 import ctypes
 import math
+import os
+import subprocess
 
 import pytest
 
@@ -165,3 +167,56 @@ def test_tokens_and_log_probabilities_that_share_bytes_with_what_other_rows_read
     for other in (0x200000, 0x200100, 0x200200, 0x200300, 0x200400):
         assert call(y=at(other)) == BAD and call(y=at(other + 4), it=B.MV_I32) == BAD and call(lp=at(other + 12)) == BAD and call(lp=at(other - 4)) == BAD
     assert call(lp=R) == BAD and call(lp=R, it=B.MV_I32) == BAD and call(lp=at(0x300000 + 28)) == BAD
+
+
+TWO_THREADS = r"""
+#include <chrono>
+#include <condition_variable>
+#include <cstdio>
+#include <mutex>
+#include <thread>
+#include "mv_lm.cuh"
+
+std::mutex m;
+std::condition_variable cv;
+bool slow_inside = false;
+int granted = 0;                     // what the driver last heard
+
+extern "C" cudaError_t cudaGetDevice(int* d) { *d = 0; return cudaSuccess; }
+extern "C" cudaError_t cudaGetLastError() { return cudaSuccess; }
+extern "C" cudaError_t cudaFuncSetAttribute(const void*, cudaFuncAttribute, int bytes) {
+  if (bytes == 50000) {
+    { std::lock_guard<std::mutex> l(m); slow_inside = true; }
+    cv.notify_all();
+    std::this_thread::sleep_for(std::chrono::milliseconds(200));
+  }
+  std::lock_guard<std::mutex> l(m);
+  granted = bytes;
+  return cudaSuccess;
+}
+static char kernel;                  // stands for one
+
+int main() {
+  static SmemLimit limit;
+  bool ok[2];
+  std::thread small([&] { ok[0] = allow_smem(&kernel, 50000, &limit); });
+  std::thread large([&] {
+    { std::unique_lock<std::mutex> l(m); cv.wait(l, [] { return slow_inside; }); }
+    ok[1] = allow_smem(&kernel, 60000, &limit);
+  });
+  small.join();
+  large.join();
+  std::printf("%d\n", granted);
+  return ok[0] && ok[1] && granted == 60000 && allow_smem(&kernel, 55000, &limit) && granted == 60000 ? 0 : 1;
+}
+"""
+
+
+def test_two_threads_that_ask_for_shared_memory_of_one_kernel_at_once(tmp_path):
+    """The smaller request, begun first and answered last, must not take back what the larger one was granted."""
+    csrc = os.path.join(os.path.dirname(BUILD.__file__), "csrc")
+    cuda = os.path.dirname(os.path.dirname(BUILD.nvcc_path()))
+    (tmp_path / "two.cpp").write_text(TWO_THREADS)
+    exe = str(tmp_path / "two")
+    subprocess.run(["g++", "-std=c++17", "-w", "-I", csrc, "-I", os.path.join(cuda, "include"), str(tmp_path / "two.cpp"), "-o", exe, "-pthread"], check=True, timeout=300)
+    assert subprocess.run([exe], timeout=60, capture_output=True).returncode == 0

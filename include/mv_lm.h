@@ -64,7 +64,8 @@ int mv_embed_grad(void* stream, const void* dout, int dout_type, int64_t ldd, co
                   size_t workspace_bytes);
 
 /* Layer norm of rows.  mu = mean of x[t, :], v = mean of (x - mu)^2, r = 1 / sqrt(v + eps), y[t, i] = (x[t, i] - mu) r w[i] + b[i],
- * in 32 bits (sums of D terms, the squares' after the mean is known), rounded once to y's type.
+ * in 32 bits (sums of D terms, the squares' after the mean is known, and what that is off by taken out of mu, v and y again, so that rows
+ * far from zero keep their digits), rounded once to y's type.
  *   x [T, D] type in, rows ldx >= D apart;  y [T, D] out, of the same type, rows ldy >= D apart; may be x itself (then ldy = ldx)
  *   weight, bias [D] w_type in: MV_F32 or x's type; each may be NULL (1 and 0)
  *   mean, rstd [T] float out (mu and r), what the gradient needs; each may be NULL

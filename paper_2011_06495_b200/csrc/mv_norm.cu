@@ -1,7 +1,7 @@
 // mv_norm.cu -- layer norm of rows, for sm_100a.
 //
-// Forward: mu = mean x, then v = mean (x - mu)^2 of the same registers (one reading of memory; no difference of large sums), r = 1 /
-// sqrt(v + eps), y = (x - mu) r w + b.  Backward, with n = (x - mu) r and h = dy w: the two sums of h and h n in one reduction, dx = r (h -
+// Forward: mu = mean x, then v = mean (x - mu)^2 of the same registers (one reading of memory; no difference of large sums; what mu is
+// off is put right by the same pass), r = 1 / sqrt(v + eps), y = (x - mu) r w + b.  Backward, with n = (x - mu) r and h = dy w: the two sums of h and h n in one reduction, dx = r (h -
 // mean h - n mean(h n)); the sums over rows of dy n and dy stay in the registers of the thread that owns the columns, CTA by CTA, and
 // a second kernel adds the CTAs' sums up in their order.  Memory bounds both where rows are many and lie on 16-byte boundaries: 65536 x
 // 2048 bf16 89 us (6.0 TB/s in and out), its gradient 140 us (5.8 TB/s; 137 us without the second kernel); 32768 x 4096 94 and 146.  A few
@@ -30,7 +30,7 @@ __global__ void __launch_bounds__(L > 32 ? WIDE_TPB : NORM_TPB, norm_resident(NV
   using Un = Unit<X, true>;
   constexpr int N = Un::N, GROUPS = (L > 32 ? WIDE_TPB : NORM_TPB) / L, WARPS = L / 32;
   extern __shared__ float4 params[];         // weights, then biases
-  __shared__ float part[2][WIDE_TPB / 32];
+  __shared__ float part[3][WIDE_TPB / 32];
   const int D = int(a.D), units = D / N, mine = threadIdx.x / L, at = threadIdx.x % L;
   const int n = units > at ? (units - at - 1) / L + 1 : 0;
   float* pw = reinterpret_cast<float*>(params);
@@ -50,16 +50,33 @@ __global__ void __launch_bounds__(L > 32 ? WIDE_TPB : NORM_TPB, norm_resident(NV
   put_params<N>(pw, a.weight, a.w_type, 1.0f, D, units);
   put_params<N>(pb, a.bias, a.w_type, 0.0f, D, units);
   __syncthreads();
-  auto sum = [&](float v, int k) {
+  auto sum = [&](float v) {
     v = lanes_sum<(L < 32 ? L : 32)>(v);
     if constexpr (WARPS > 1) {
-      if ((threadIdx.x & 31) == 0) part[k][threadIdx.x >> 5] = v;
+      if ((threadIdx.x & 31) == 0) part[0][threadIdx.x >> 5] = v;
       group_sync<L>(mine);
       v = 0.0f;
 #pragma unroll
-      for (int i = 0; i < WARPS; ++i) v += part[k][mine * WARPS + i];
+      for (int i = 0; i < WARPS; ++i) v += part[0][mine * WARPS + i];
     }
     return v;
+  };
+  auto sum_both = [&](float& v, float& w) {
+    v = lanes_sum<(L < 32 ? L : 32)>(v);
+    w = lanes_sum<(L < 32 ? L : 32)>(w);
+    if constexpr (WARPS > 1) {
+      if ((threadIdx.x & 31) == 0) {
+        part[1][threadIdx.x >> 5] = v;
+        part[2][threadIdx.x >> 5] = w;
+      }
+      group_sync<L>(mine);
+      v = w = 0.0f;
+#pragma unroll
+      for (int i = 0; i < WARPS; ++i) {
+        v += part[1][mine * WARPS + i];
+        w += part[2][mine * WARPS + i];
+      }
+    }
   };
   auto get = [&](int i) -> const Un& { return u[i]; };
   const float share = 1.0f / float(D);
@@ -70,22 +87,26 @@ __global__ void __launch_bounds__(L > 32 ? WIDE_TPB : NORM_TPB, norm_resident(NV
     load(t + GROUPS);
     f2 s = both(0.0f);
     each_pair<X, true, NV>(n, [&](int i, int j, int, bool second) { s = add2(s, pair_of<X, true>(get, i, j, second)); });
-    const float mu = sum(add_up(s), 0) * share;
-    const f2 minus = both(-mu);
-    s = both(0.0f);
+    const float m = sum(add_up(s)) * share;
+    const f2 minus = both(-m);
+    f2 off = both(0.0f);
+    s = off;
     each_pair<X, true, NV>(n, [&](int i, int j, int, bool second) {
       const f2 d = add2(pair_of<X, true>(get, i, j, second), minus);
+      off = add2(off, d);
       s = fma2(d, d, s);
     });
-    const float rs = rsqrtf(fmaf(sum(add_up(s), 1), share, a.eps));
+    float sum_d = add_up(off), sum_d2 = add_up(s);
+    sum_both(sum_d, sum_d2);
+    const Centre c = centre(m, sum_d, sum_d2, share, a.eps);
     if (t >= t1) continue;
-    const f2 rs2 = both(rs);
+    const f2 rs2 = both(c.rstd), shift2 = both(c.shift);
     put_pairs<X, true, NV, L>(n, y + t * a.ldy + at * N, [&](int i, int j, int k, bool second) {
-      return fma2(mul2(add2(pair_of<X, true>(get, i, j, second), minus), rs2), param_pair<N, L>(pw, at, units, k, second), param_pair<N, L>(pb, at, units, k, second));
+      return fma2(fma2(add2(pair_of<X, true>(get, i, j, second), minus), rs2, shift2), param_pair<N, L>(pw, at, units, k, second), param_pair<N, L>(pb, at, units, k, second));
     });
     if (at == 0) {
-      if (a.mean) a.mean[t] = mu;
-      if (a.rstd) a.rstd[t] = rs;
+      if (a.mean) a.mean[t] = c.mean;
+      if (a.rstd) a.rstd[t] = c.rstd;
     }
   }
 }
@@ -99,7 +120,7 @@ template <typename X, bool APART, int L, int NV>
 __global__ void __launch_bounds__(L > 32 ? WIDE_TPB : NORM_TPB, L > 32 ? 1 : 2) k_norm_any(const X* x, X* y, const __grid_constant__ NormArgs a) {
   constexpr int N = Vec<X>::N, GROUPS = (L > 32 ? WIDE_TPB : NORM_TPB) / L, WARPS = L / 32, SIZE = sizeof(X), ENDS = L < 32 ? 32 / L : 1;
   extern __shared__ float2 pairs[];
-  __shared__ float part[2][WIDE_TPB / 32];
+  __shared__ float part[3][WIDE_TPB / 32];
   const int D = int(a.D), columns = (D + N - 1) / N, mine = threadIdx.x / L, at = threadIdx.x % L;
   const int64_t t0 = blockIdx.x * a.per, t1 = min(a.T, t0 + a.per);
   struct Row { const X* x; X* y; int first, nv, shift; };
@@ -163,16 +184,33 @@ __global__ void __launch_bounds__(L > 32 ? WIDE_TPB : NORM_TPB, L > 32 ? 1 : 2) 
     put(a.bias, 0.0f, 1);
   }
   __syncthreads();
-  auto sum = [&](float v, int k) {
+  auto sum = [&](float v) {
     v = lanes_sum<(L < 32 ? L : 32)>(v);
     if constexpr (WARPS > 1) {
-      if ((threadIdx.x & 31) == 0) part[k][threadIdx.x >> 5] = v;
+      if ((threadIdx.x & 31) == 0) part[0][threadIdx.x >> 5] = v;
       group_sync<L>(mine);
       v = 0.0f;
 #pragma unroll
-      for (int i = 0; i < WARPS; ++i) v += part[k][mine * WARPS + i];
+      for (int i = 0; i < WARPS; ++i) v += part[0][mine * WARPS + i];
     }
     return v;
+  };
+  auto sum_both = [&](float& v, float& w) {
+    v = lanes_sum<(L < 32 ? L : 32)>(v);
+    w = lanes_sum<(L < 32 ? L : 32)>(w);
+    if constexpr (WARPS > 1) {
+      if ((threadIdx.x & 31) == 0) {
+        part[1][threadIdx.x >> 5] = v;
+        part[2][threadIdx.x >> 5] = w;
+      }
+      group_sync<L>(mine);
+      v = w = 0.0f;
+#pragma unroll
+      for (int i = 0; i < WARPS; ++i) {
+        v += part[1][mine * WARPS + i];
+        w += part[2][mine * WARPS + i];
+      }
+    }
   };
   const float share = 1.0f / float(D);
   for (int64_t r0 = t0; r0 < t1; r0 += GROUPS) {
@@ -198,13 +236,15 @@ __global__ void __launch_bounds__(L > 32 ? WIDE_TPB : NORM_TPB, L > 32 ? 1 : 2) 
       if (i < n)
 #pragma unroll
         for (int j = 0; j < N / 2; ++j) s = add2(s, Vec<X>::pair(u[i], j));
-    const float mu = sum(add_up(s), 0) * share;
-    const f2 minus = both(-mu);
-    s = both(0.0f);
+    const float m = sum(add_up(s)) * share;
+    const f2 minus = both(-m);
+    f2 off = both(0.0f);
+    s = off;
 #pragma unroll
     for (int i = 0; i < ENDS; ++i) {
-      const float d = at + i * L < ends ? end[i] - mu : 0.0f;
-      s = fma2(pack2(d, 0.0f), pack2(d, 0.0f), s);
+      const f2 d = pack2(at + i * L < ends ? end[i] - m : 0.0f, 0.0f);
+      off = add2(off, d);
+      s = fma2(d, d, s);
     }
 #pragma unroll
     for (int i = 0; i < NV; ++i)
@@ -212,12 +252,15 @@ __global__ void __launch_bounds__(L > 32 ? WIDE_TPB : NORM_TPB, L > 32 ? 1 : 2) 
 #pragma unroll
         for (int j = 0; j < N / 2; ++j) {
           const f2 d = add2(Vec<X>::pair(u[i], j), minus);
+          off = add2(off, d);
           s = fma2(d, d, s);
         }
-    const float rs = rsqrtf(fmaf(sum(add_up(s), 1), share, a.eps));
+    float sum_d = add_up(off), sum_d2 = add_up(s);
+    sum_both(sum_d, sum_d2);
+    const Centre c = centre(m, sum_d, sum_d2, share, a.eps);
     if (t >= t1) continue;
-    const f2 rs2 = both(rs);
-    auto place = [&](int c) { return c % N * columns + c / N; };
+    const f2 rs2 = both(c.rstd), shift2 = both(c.shift);
+    auto place = [&](int column) { return column % N * columns + column / N; };
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
       if (i >= n) break;
@@ -228,7 +271,7 @@ __global__ void __launch_bounds__(L > 32 ? WIDE_TPB : NORM_TPB, L > 32 ? 1 : 2) 
         // column first + N v + e: with first = N q + f, in the group (f + e) mod N
         const int e0 = now.first + 2 * j, e1 = e0 + 1;
         const float2 p = pairs[place(e0) + v], q = pairs[place(e1) + v];
-        unpack2(fma2(mul2(add2(Vec<X>::pair(u[i], j), minus), rs2), pack2(p.x, q.x), pack2(p.y, q.y)), o[2 * j], o[2 * j + 1]);
+        unpack2(fma2(fma2(add2(Vec<X>::pair(u[i], j), minus), rs2, shift2), pack2(p.x, q.x), pack2(p.y, q.y)), o[2 * j], o[2 * j + 1]);
       }
       __stcs(reinterpret_cast<uint4*>(now.y + now.first) + v, pack_vec<X>(o));
     }
@@ -236,13 +279,13 @@ __global__ void __launch_bounds__(L > 32 ? WIDE_TPB : NORM_TPB, L > 32 ? 1 : 2) 
     for (int i = 0; i < ENDS; ++i) {
       const int e = at + i * L;
       if (e >= ends) break;
-      const int c = e < now.first ? e : now.nv * N + e;
-      const float2 p = pairs[place(c)];
-      now.y[c] = from_f<X>(fmaf((end[i] - mu) * rs, p.x, p.y));
+      const int column = e < now.first ? e : now.nv * N + e;
+      const float2 p = pairs[place(column)];
+      now.y[column] = from_f<X>(fmaf(fmaf(end[i] - m, c.rstd, c.shift), p.x, p.y));
     }
     if (at == 0) {
-      if (a.mean) a.mean[t] = mu;
-      if (a.rstd) a.rstd[t] = rs;
+      if (a.mean) a.mean[t] = c.mean;
+      if (a.rstd) a.rstd[t] = c.rstd;
     }
   }
 }
@@ -255,18 +298,21 @@ __global__ void __launch_bounds__(LONG_TPB) k_norm_long(const X* x, X* y, const 
   X* out = y + t * a.ldy;
   float s = 0.0f;
   for (int64_t i = threadIdx.x; i < a.D; i += LONG_TPB) s += to_f(row[i]);
-  const float mu = cta_sum(s, sh) / float(a.D);
+  const float share = 1.0f / float(a.D), m = cta_sum(s, sh) * share;
+  float off = 0.0f;
   s = 0.0f;
   for (int64_t i = threadIdx.x; i < a.D; i += LONG_TPB) {
-    const float d = to_f(row[i]) - mu;
+    const float d = to_f(row[i]) - m;
+    off += d;
     s = fmaf(d, d, s);
   }
-  const float r = rsqrtf(cta_sum(s, sh) / float(a.D) + a.eps);
+  off = cta_sum(off, sh);
+  const Centre c = centre(m, off, cta_sum(s, sh), share, a.eps);
   for (int64_t i = threadIdx.x; i < a.D; i += LONG_TPB)
-    out[i] = from_f<X>(fmaf((to_f(row[i]) - mu) * r, parameter(a.weight, a.w_type, i, 1.0f), parameter(a.bias, a.w_type, i, 0.0f)));
+    out[i] = from_f<X>(fmaf(fmaf(to_f(row[i]) - m, c.rstd, c.shift), parameter(a.weight, a.w_type, i, 1.0f), parameter(a.bias, a.w_type, i, 0.0f)));
   if (threadIdx.x == 0) {
-    if (a.mean) a.mean[t] = mu;
-    if (a.rstd) a.rstd[t] = r;
+    if (a.mean) a.mean[t] = c.mean;
+    if (a.rstd) a.rstd[t] = c.rstd;
   }
 }
 

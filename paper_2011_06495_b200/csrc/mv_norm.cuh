@@ -84,6 +84,14 @@ __device__ __forceinline__ float parameter(const void* p, int type, int64_t i, f
   return type == MV_F32 ? static_cast<const float*>(p)[i] : type == MV_BF16 ? to_f(static_cast<const __nv_bfloat16*>(p)[i]) : to_f(static_cast<const __half*>(p)[i]);
 }
 
+// A sum over D, times a rounded 1 / D, leaves the mean m off by e, which beside a small spread is not little (1000 columns of 1000.0: 6e-5; y 0.02
+// instead of 0).  The pass over d = x - m adds up d beside d^2: e = mean d, v = mean d^2 - e^2, and y's (d - e) r is d r + shift.
+struct Centre { float mean, rstd, shift; };
+__device__ __forceinline__ Centre centre(float m, float sum_d, float sum_d2, float share, float eps) {
+  const float e = fabsf(sum_d) < INFINITY ? sum_d * share : 0.0f, r = rsqrtf(max_nan(fmaf(-e, e, sum_d2 * share), 0.0f) + eps);
+  return {m + e, r, -e * r};
+}
+
 // Parameters in shared memory, unit by unit; of units of eight the first fours, then the second fours, so that neighbouring lanes read
 // neighbouring 16 bytes.
 template <int N> __device__ __forceinline__ int place(int i, int units) { return N == 8 ? (((i >> 2) & 1) * units + (i >> 3)) * 4 + (i & 3) : i; }

@@ -113,6 +113,48 @@ def test_many_rows_in_place_off_the_boundaries(dt, T, D):
 
 
 @pytest.mark.parametrize("dt", [F32, BF16, F16])
+@pytest.mark.parametrize("T,D", [(40, 1), (40, 7), (40, 64), (40, 1000), (40, 1001), (40, 2048), (40, 5000), (40, 16_383), (40, 30_000), (1300, 96), (1300, 1000), (1300, 1003)])
+def test_means_that_are_large_beside_the_spread(dt, T, D):
+    """Constant rows and a spread of 1e-4 of the mean.  A sum of D terms passes n additions at most: of few rows a lane holds D / 1024 pairs, or up to 32
+    elements, and a warp's and a CTA's sums add 21 more; of many rows as above.  The first mean m is off by e0 = (n + 2) u mean|x|.
+    What the second pass finds of that is off by e1 = (n + 4) u mean|x - m|, and so is the mean, beside its own rounding; the variance by
+    (n + 7) u (v + e0^2) + 2 e0 e1 + e1^2; y by that of rstd, by e1 rstd, and by the roundings of x - m, of its product's sum and of e rstd."""
+    g = gen(T + D)
+    x = torch.randn((T, D), generator=g, device=DEV)
+    x = torch.cat([x[::4] * 0 + 1000.0, x[1::4] * 0 + 3000.33, x[2::4] * 0.1 + 1000.0, x[3::4] * 0.01 + 100.0]).to(dt)
+    w, b = parameters(D, F32)
+    y, mean, rstd = run_forward(x, w, b)
+    x, w, b = x.double().cpu(), w.double().cpu(), b.double().cpu()
+    n = D / 16 + 16 if T > 1000 else min(D + 8, D / 256 + 48)
+    mu, eps = x.mean(1), float(torch.tensor(EPS, dtype=torch.float32))
+    d = x - mu[:, None]
+    v, spread = (d * d).mean(1), d.abs().mean(1)
+    e0 = 1.01 * (n + 2) * U32 * x.abs().mean(1)
+    e1 = 1.01 * (n + 4) * U32 * (spread + e0)
+    ev = 1.01 * ((n + 7) * U32 * (v + e0 ** 2) + 2 * e0 * e1 + e1 ** 2)
+    r = 1 / torch.sqrt(v + eps)
+    rel = 1.01 * (0.5 * ev / (v + eps) + 4 * U32) + (ev / (v + eps)) ** 2
+    z = d * r[:, None]
+    ez = 1.01 * (1 + rel[:, None]) * (z.abs() * (rel[:, None] + U32) + r[:, None] * (e1[:, None] + U32 * (d.abs() + 2 * e0[:, None])))
+    want = z * w + b
+    for got, value, off in ((y, want, ez * w.abs() + 2 * U32 * want.abs() + 2.0 ** -149), (mean, mu, e1 + 1.01 * U32 * mu.abs()), (rstd, r, rel * r)):
+        assert bool(within(got, value, off).all()), float((got.double().cpu() - value).abs().max())
+
+
+def test_rows_whose_squares_pass_the_range_of_32_bits():
+    """rstd is 0 then, and y the bias, where sums of some of the terms, in any order, cannot pass the range too: that is where the magnitudes' sum does
+    not (of +-1e38 in turn, four or more of either sign are inf together, and a row whose sums pass the range is nothing but the formula's)."""
+    for D in (2, 64, 1001, 2048, 40_000):
+        x = torch.randn((6, D), generator=gen(D), device=DEV) * 1e25
+        x[0] = torch.where(torch.arange(D, device=DEV) % 2 == 0, 1e38, -1e38)
+        b = torch.randn(D, generator=gen(1), device=DEV)
+        y, mean, rstd = run_forward(x, None, b)
+        fits = x.double().abs().sum(1) < 3e38
+        assert bool(fits[1:].all()) and bool(fits[0]) == (D == 2)
+        assert bool((rstd[fits] == 0).all()) and torch.equal(y[fits], b.expand_as(y)[fits]) and bool(torch.isfinite(mean[fits]).all())
+
+
+@pytest.mark.parametrize("dt", [F32, BF16, F16])
 def test_widths_at_the_limits_of_shared_memory(dt):
     """6129 to 6144 columns need just 48 KB for their parameters, beside a little static shared memory; the gradient gets there at widths that
     hang on the type and the alignment, so that every width up to 6200 has to be taken at least."""

@@ -119,7 +119,7 @@ struct Weights {
   __device__ __forceinline__ u64 raw(float x) const { return raw_weight(x, C, K, low, table); }      // NOTHING and the whole number
   __device__ __forceinline__ u64 whole(float x) const { return raw(x) - NOTHING; }
   __device__ __forceinline__ double log_factor() const { return (fma(m, C, K) - MAGIC) * (0x1p-45 * 0.6931471805599453); }      // of the common factor
-  __device__ __forceinline__ u64 any(float x) const { return u64(exp2((double(x) - m) * c2) * unit + 0.5); }      // of extreme rows too
+  __device__ __forceinline__ u64 any(float x) const { return u64(exp2((double(x) - m) * c2) * unit + 0.5); }      // of extreme rows
 };
 
 // The largest whole number not above u all, u in [0, 1), exactly.
@@ -326,6 +326,9 @@ __device__ __noinline__ Cut cut_row(const X* row, int64_t V, u64 target, const C
 template <typename X>
 __device__ __noinline__ void sample_any(const X* row, const SampleArgs& a, int64_t t, const Request& q, const Weights& wt, Smem& s) {
   const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
+  const bool extreme = wt.extreme();
+  // the fast paths' weights to the bit, so that a row's token does not hang on the path that it takes
+  auto weight = [&](float x) { return extreme ? wt.any(x) : wt.whole(x); };
   Cut cut = {0, 0, 0};               // all
   bool cuts = false;
   if (q.k < a.V) {
@@ -336,12 +339,12 @@ __device__ __noinline__ void sample_any(const X* row, const SampleArgs& a, int64
     u64 mine = 0, all;
     for (int64_t i = threadIdx.x; i < a.V; i += TPB) {
       const float x = to_f(row[i]);
-      if (!cuts || order_of(x) > cut.order) mine += wt.any(x);
+      if (!cuts || order_of(x) > cut.order) mine += weight(x);
     }
     scan_before(mine, s, all);
-    if (cuts) all += u64(cut.ties) * wt.any(value_of(cut.order));
+    if (cuts) all += u64(cut.ties) * weight(value_of(cut.order));
     const u64 target = start_of(q.p, all);
-    cut = cut_row(row, a.V, target, cuts ? &cut : nullptr, [&](float x) { return wt.any(x); }, s);
+    cut = cut_row(row, a.V, target, cuts ? &cut : nullptr, weight, s);
     cuts = true;
   }
   // the index of the last kept token of the cut's own order
@@ -364,7 +367,7 @@ __device__ __noinline__ void sample_any(const X* row, const SampleArgs& a, int64
     const float x = to_f(row[i]);
     const uint32_t h = order_of(x);
     if (cuts && !(h > cut.order || (h == cut.order && i <= last))) return u64(0);
-    return exp((double(x) - wt.m) * double(q.scale)) >= double(q.mp) ? wt.any(x) : u64(0);
+    return exp((double(x) - wt.m) * double(q.scale)) >= double(q.mp) ? weight(x) : u64(0);
   };
   const int64_t per = ((a.V + CHUNKS - 1) / CHUNKS + 31) / 32 * 32;
   __syncthreads();
@@ -401,7 +404,7 @@ __device__ __noinline__ void sample_any(const X* row, const SampleArgs& a, int64
     }
     const unsigned hit = __ballot_sync(0xffffffffu, before + incl > limit);
     if (hit) {
-      if (lane == __ffs(int(hit)) - 1) put_drawn(a, t, i, to_f(row[i]), wt, n, all, 0.0);
+      if (lane == __ffs(int(hit)) - 1) put_drawn(a, t, i, to_f(row[i]), wt, n, all, extreme ? 0.0 : wt.log_factor());
       return;
     }
     before += __shfl_sync(0xffffffffu, incl, 31);

@@ -289,6 +289,52 @@ def test_results_in_the_place_of_u_and_of_settings(T, V):
         assert torch.equal(k2, token) and torch.equal(u2, lp)
 
 
+def test_a_row_has_the_same_token_however_many_rows_there_are():
+    """Two tokens, the lighter one behind the heavier, and u within 2e-14 of their border: the weights' last bits decide.  The two lie in one group of
+    logits when four CTAs share the row, so that too many others come into the list and the row is sampled without it; in two groups when a CTA
+    has the row for itself, and the list holds just these two."""
+    V, first, second, far = 20_480, 1580 * 4, 2092 * 4, -6.0
+    g = gen(12)
+    found = []
+    for _ in range(24):                                      # pairs whose border is as near to a u of 32 bits
+        scale = torch.empty(1 << 24, device=DEV).uniform_(1.0, 2.0, generator=g)
+        x = torch.empty(1 << 24, device=DEV).uniform_(-2.0, -0.1, generator=g)
+        border = 1 / (1 + torch.exp(x.double() * scale.double()))
+        u = border.float()
+        near = (u.double() - border).abs() < 2e-14
+        found.append(torch.stack([scale[near], x[near], u[near]]))
+    scale, x, u = (t.contiguous() for t in torch.cat(found, 1))
+    n = len(u)
+    assert n >= 50
+    rows = torch.full((n, V), far, device=DEV)
+    rows[:, first], rows[:, second] = 0.0, x
+    p = 1 - 2.0 ** -24
+    times = 600 // n + 1                                     # more than 592 rows: one CTA each
+    many = draw(rows.repeat(times, 1), u.repeat(times), scale.repeat(times), 2, p)
+    assert bool(((many[0] == first) | (many[0] == second)).all())
+    for t in range(n):
+        one = draw(rows[t:t + 1], u[t:t + 1], scale[t:t + 1], 2, p)
+        assert torch.equal(one[0], many[0][t:t + 1]) and torch.equal(one[1], many[1][t:t + 1]), (t, float(scale[t]), float(x[t]), float(u[t]))
+
+
+def test_rows_alone_and_in_a_batch_at_other_places():
+    """The same bytes for every setting, whichever path a row takes: heads, crowds of 16 bits, masks."""
+    V = 33_000
+    x = torch.cat([head(12, V, BF16, 77), (torch.randn((12, V), generator=gen(78), device=DEV) * 1.5 + 12.0).to(BF16)])
+    x[::5, V // 3:] = -math.inf
+    u = torch.rand(len(x), generator=gen(79), device=DEV)
+    for s in SETTINGS + [(1.0, 50, 0.9, None), (1.0, 2000, 0.9, 0.05), (1.25, 50, None, None)]:
+        many = draw(x.repeat(50, 1), u.repeat(50), *s)      # 1200 rows
+        few = draw(x, u, *s)
+        assert torch.equal(many[0][:len(x)], few[0]) and torch.equal(many[1][:len(x)], few[1])
+        assert torch.equal(many[0][-len(x):], few[0]) and torch.equal(many[1][-len(x):], few[1])
+        for t in range(0, len(x), 3):
+            apart, _ = strided(1, V, BF16, 0, 3 + t, fill=0.0)
+            apart.copy_(x[t:t + 1])
+            one = draw(apart, u[t:t + 1], *s)
+            assert torch.equal(one[0], few[0][t:t + 1]) and torch.equal(one[1], few[1][t:t + 1])
+
+
 def test_frequencies_are_the_probabilities():
     """The same row with an even grid of u: every token as often as its share of the grid, to within one of the grid's steps."""
     T, V = 4096, 50

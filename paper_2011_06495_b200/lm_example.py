@@ -148,7 +148,8 @@ def train(m, steps):
     for i in range(steps):
         loss = m.step()
         if i % 10 == 0 or i == steps - 1:
-            print(f"step {i:4d}  loss {loss:.4f}  norms {', '.join('%.3f' % v for v in m.norms.tolist())}  K = {m.K} of {m.d}")
+            entropy = f"entropy {float(m.ent.mean()):.3f}  " if m.teacher is None else ""
+            print(f"step {i:4d}  loss {loss:.4f}  norms {', '.join('%.3f' % v for v in m.norms.tolist())}  {entropy}K = {m.K} of {m.d}")
 
 
 def main():

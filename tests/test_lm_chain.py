@@ -1,9 +1,11 @@
 """GPU tests of the language-model operators strung together: embedding, layer norm, logits, distillation or log probabilities, their gradients,
 clipping, the sparse step, and tokens drawn from the trained model."""
+import re
+
 import pytest
 import torch
 
-from paper_2011_06495_b200.lm_example import BigramWorkers
+from paper_2011_06495_b200.lm_example import BigramWorkers, train
 
 pytestmark = pytest.mark.gpu
 DEV = "cuda:0"
@@ -34,3 +36,15 @@ def test_tokens_drawn_one_after_another():
     for row in greedy:
         assert torch.equal(row, m.logits(x).float().argmax(1))
         x = row
+
+
+def test_what_training_prints(capsys):
+    """Loss, norms and the entropy of the predictions; a student of a teacher's alternatives has no entropy."""
+    m = BigramWorkers(N=2, V=300, D=32, T=400, device=DEV)
+    train(m, 2)
+    train(BigramWorkers(N=2, V=300, D=32, T=400, device=DEV, teacher=m), 1)
+    lines = capsys.readouterr().out.splitlines()
+    number = r"-?\d+\.\d+"
+    for line in lines[:2]:
+        assert re.fullmatch(rf"step +\d+  loss {number}  norms {number}, {number}  entropy {number}  K = {m.K} of {m.d}", line), line
+    assert re.fullmatch(rf"step +0  loss {number}  norms {number}, {number}  K = {m.K} of {m.d}", lines[2]) and len(lines) == 3

@@ -351,7 +351,8 @@ __global__ void __launch_bounds__(TPB) k_distill_grad(const X* logits, X* dlogit
   sum = 0.0;
   for (int i = 0; i < WARPS; ++i) sum += s_sum[i];
   const double r = a.h.rest ? fmax(0.0, 1.0 - sum) : 0.0;
-  const float all = bad ? NAN : a.h.rest ? float(sum + r) : 1.0f, unit = a.h.rest ? 1.0f : float(1.0 / sum);
+  const float all = bad ? NAN : a.h.rest ? float(sum + r) : 1.0f;
+  const double unit = a.h.rest ? 1.0 : 1.0 / sum;
   const float ratio = r == 0.0 ? 0.0f : lr == -INFINITY ? all : expf(logf(float(r)) - lr);
   const bool none = !any || g == 0.0f || l == -INFINITY || a.scale * g == 0.0f;
   const float f = none ? 0.0f : a.scale * g, other = f * (all - ratio), l2e = 0.5f * LOG2E;
@@ -394,18 +395,18 @@ __global__ void __launch_bounds__(TPB) k_distill_grad(const X* logits, X* dlogit
   for (int j = tid; j < a.h.k; j += TPB) {
     const int c = list.col[j];
     if (!here(c)) continue;
-    float q = list.a[j];
+    double q = list.a[j];            // (its terms are of 32 bits, their sum is not: a token may have all k of them)
     bool head = true;
     if (s_seen[1][c / 32 % SEEN] >> (c & 31) & 1u) {
-      q = 0.0f;
+      q = 0.0;
       for (int i = 0; i < a.h.k; ++i)
         if (list.col[i] == c) {
           head &= i >= j;
-          q += list.a[i];
+          q += double(list.a[i]);
         }
     }
     const float p = share(list.x[j]);
-    if (head) dx[c] = from_f<X>(f * fmaf(all * p, p, -q * unit));
+    if (head) dx[c] = from_f<X>(f * fmaf(all * p, p, -float(q * unit)));
   }
 }
 

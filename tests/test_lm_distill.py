@@ -202,6 +202,15 @@ def test_the_same_token_more_than_once(rest):
         check_gradient(x, top, ids, 0.7, rest, forward=check_forward(x, top, ids, 0.7, rest))
 
 
+@pytest.mark.parametrize("rest", [True, False])
+@pytest.mark.parametrize("V,k", [(1, 1024), (2, 500), (12, 1024), (60, 1024), (7, 129)])
+def test_long_lists_of_few_tokens(V, k, rest):
+    """Hundreds of terms of one token: their sum is as exact as one term is, which is what the bound allows for."""
+    for seed in range(3):
+        x, top, ids = case(800, V, k, F32, duplicates=True, seed=seed)
+        check_gradient(x, top, ids, 0.5, rest, seed=seed)
+
+
 @pytest.mark.parametrize("magnitude,scale", [(1e2, 1.0), (1e4, 1.0), (1e9, 1.0), (1e30, 1.0), (1.0, 1e6), (1.0, 1e-6), (1e30, 1e-30), (1e38, 0.5)])
 @pytest.mark.parametrize("rest", [True, False])
 def test_magnitudes(magnitude, scale, rest):

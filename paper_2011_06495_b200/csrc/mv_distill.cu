@@ -234,7 +234,7 @@ __global__ void __launch_bounds__(TPB, 1024 / TPB) k_distill(const X* __restrict
   for (int j = lane; j < a.h.k; j += 32) {
     const double d = double(list.a[j]) - shift, e = exp(d);
     q += e;
-    if (e > 0.0) kl = fma(e, d - (double(distance(list.x[j], zero, a.scale)) - double(ls)), kl);
+    if (e > 0.0) kl = fma(e, d - ((double(list.x[j]) - double(zero)) * double(a.scale) - double(ls)), kl);      // (in 32 bits a finite mask may pass the range)
   }
   for (int o = 16; o; o >>= 1) {
     q += __shfl_xor_sync(0xffffffffu, q, o);

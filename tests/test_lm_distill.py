@@ -227,6 +227,26 @@ def test_magnitudes(magnitude, scale, rest):
         check_gradient(x, top, ids, scale, rest, forward=got)
 
 
+@pytest.mark.parametrize("dt", [F32, BF16])
+@pytest.mark.parametrize("rest", [True, False])
+def test_listed_tokens_that_are_masked_by_the_lowest_value(dt, rest):
+    """scale x passes the range of 32 bits, q_j log p_j does not."""
+    x, top, ids = case(6, 700, 5, dt, seed=11)
+    ids = torch.arange(5, device=DEV, dtype=torch.int32).repeat(6, 1) * 97
+    top = torch.log(torch.tensor([0.5, 0.2, 0.1, 0.05, 0.01], device=DEV)).repeat(6, 1)
+    x[:, 291] = torch.finfo(dt).min                         # the fourth
+    x[3, 388] = torch.finfo(dt).min                         # and the fifth
+    x[4, 500] = torch.finfo(dt).max                         # everything else is as far away
+    x[5, 0] = torch.finfo(dt).max
+    for scale in (1.0, 4.0):
+        want, got = forward_reference(x[:4], top[:4], ids[:4], scale, rest), call(x, top, ids, scale, rest)
+        close(got["kl"][:4], want["kl"], "kl")
+        assert float(got["kl"][:4].min()) > 1e37 * scale / 4
+    if not rest:                                             # (with it, log P is -inf in the last rows)
+        want = forward_reference(x[5:], top[5:], ids[5:], 1.0, rest)
+        close(call(x[5:], top[5:], ids[5:], 1.0, rest)["kl"], want["kl"], "kl")
+
+
 def test_rows_with_nan_and_inf():
     for dt in (F32, BF16):
         for V in (5, 3000, 40_001):

@@ -355,15 +355,18 @@ __global__ void __launch_bounds__(TPB) k_distill_grad(const X* logits, X* dlogit
   const double unit = a.h.rest ? 1.0 : 1.0 / sum;
   const float ratio = r == 0.0 ? 0.0f : lr == -INFINITY ? all : expf(logf(float(r)) - lr);
   const bool none = !any || g == 0.0f || l == -INFINITY || a.scale * g == 0.0f;
-  const float f = none ? 0.0f : a.scale * g, other = f * (all - ratio), l2e = 0.5f * LOG2E;
-  auto share = [&](float v) {                  // p / q; the same operations as two logits at a time below
-    return exp2_fast(min_nan(fmaf(v, a.scale, -l) * l2e, 0.0f));
+  // r / P may pass the range of 32 bits where P is small; p_v r / P does not.  Then the others are f (p_v / P) (M P - r).
+  const bool far = r > 0.0 && lr > -INFINITY && lr < -40.0f;
+  const float f = none ? 0.0f : a.scale * g, other = f * (far ? all * expf(lr) - float(r) : all - ratio), l2e = 0.5f * LOG2E;
+  const float lo = far ? l + lr : l, most = far ? -lr * l2e : 0.0f;            // of p_v / P, or of p_v: its log, and at most how much (p_v: 1)
+  auto share = [&](float v, float base, float most) {       // p / q, or p / P / q; the same operations as two logits at a time below
+    return exp2_fast(min_nan(fmaf(v, a.scale, -base) * l2e, most));
   };
   auto one = [&](float v) {
-    const float q = share(v);
+    const float q = share(v, lo, most);
     return none ? 0.0f : q * (q * other);
   };
-  const f2 scale2 = pack2(a.scale, a.scale), minus = pack2(-l, -l), l2e2 = pack2(l2e, l2e), other2 = pack2(other, other);
+  const f2 scale2 = pack2(a.scale, a.scale), minus = pack2(-lo, -lo), l2e2 = pack2(l2e, l2e), other2 = pack2(other, other);
   for (int64_t vs = v0 + tid; vs < v1; vs += TPB * GRAD_U) {
 #pragma unroll
     for (int i = 0; i < GRAD_U; ++i) {
@@ -380,7 +383,7 @@ __global__ void __launch_bounds__(TPB) k_distill_grad(const X* logits, X* dlogit
       for (int j = 0; j < N / 2; ++j) {
         float h0, h1;
         unpack2(mul2(fma2(Vec<X>::pair(u[i], j), scale2, minus), l2e2), h0, h1);
-        const f2 q = pack2(exp2_fast(min_nan(h0, 0.0f)), exp2_fast(min_nan(h1, 0.0f)));
+        const f2 q = pack2(exp2_fast(min_nan(h0, most)), exp2_fast(min_nan(h1, most)));
         unpack2(mul2(q, mul2(q, other2)), d[2 * j], d[2 * j + 1]);
       }
       __stcs(out + v, none ? make_uint4(0, 0, 0, 0) : pack_vec<X>(d));
@@ -405,7 +408,7 @@ __global__ void __launch_bounds__(TPB) k_distill_grad(const X* logits, X* dlogit
           q += double(list.a[i]);
         }
     }
-    const float p = share(list.x[j]);
+    const float p = share(list.x[j], l, 0.0f);
     if (head) dx[c] = from_f<X>(f * fmaf(all * p, p, -float(q * unit)));
   }
 }

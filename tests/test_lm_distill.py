@@ -247,6 +247,38 @@ def test_listed_tokens_that_are_masked_by_the_lowest_value(dt, rest):
         close(call(x[5:], top[5:], ids[5:], 1.0, rest)["kl"], want["kl"], "kl")
 
 
+@pytest.mark.parametrize("dt", [F32, BF16, F16])
+@pytest.mark.parametrize("V,pad", [(40, 0), (9001, 1)])
+@pytest.mark.parametrize("weight", [1.0, 1e4])
+def test_students_that_leave_hardly_anything_to_the_rest(dt, V, pad, weight):
+    """g r / P passes the range of 32 bits where log P is low, g p_v r / P does not: the gradient of the tokens outside the list, c g p (M - r / P), is
+    at most c g r.  Its relative error: the exponential, the roundings of its argument log p - log P, and those of r / P."""
+    T, k = 60, 4
+    x = torch.randn((T, V), generator=gen(V), device=DEV)
+    ids = (torch.arange(k, device=DEV, dtype=torch.int32) * 7).repeat(T, 1)
+    ahead = torch.linspace(0.0, 86.0, T, device=DEV)[:, None]
+    x.scatter_(1, ids.long(), ahead + 3.5 + torch.randn((T, k), generator=gen(1), device=DEV).abs())
+    x = x.to(dt)
+    top = torch.log(torch.tensor([0.5, 0.2, 0.1, 0.05], device=DEV)).repeat(T, 1)
+    top[::3] += 0.1                                          # r a sixth, a sixteenth and 1e-7
+    top[1::3] += math.log(0.9999999 / 0.85)
+    o = call(x, top, ids, 1.0, True)
+    assert float(o["log_rest"].min()) < -84                  # (-inf, where nothing of the rest is above 2^-126 of the largest: then the others are 0)
+    g = torch.randn(T, generator=gen(2), device=DEV) * weight
+    dx, _ = strided(T, V, dt, pad, pad, fill=7.0)
+    B.mv_distill_grad(x, top, ids, o["lse"], g, dx, log_rest=o["log_rest"])
+    q, r, M, valid, _ = teacher(top, ids, V, True)
+    z, l, lr = x.double().cpu(), o["lse"].double().cpu()[:, None], o["log_rest"].double().cpu()[:, None]
+    M, r, f = M[:, None], r[:, None], g.double().cpu()[:, None]
+    r, lr = torch.where(torch.isinf(lr), 0.0, r), torch.where(torch.isinf(lr), 0.0, lr)
+    M = torch.where(o["log_rest"].cpu()[:, None] == -math.inf, 0.0, M)
+    want = f * (M * torch.exp(z - l) - r * torch.exp(z - l - lr))
+    off = f.abs() * (M * torch.exp(z - l) + r * torch.exp(z - l - lr)) * (1.01 * EX2 + U32 * (2 * z.abs() + l.abs() + 8 * (z - l).abs() + 4 * torch.log(r.clamp(min=1e-300)).abs() + 8 * lr.abs() + 16))
+    outside = ~listed_columns(ids, valid, V)
+    assert bool(torch.isfinite(dx).all())
+    assert bool((within(dx, want, off + 2.0 ** -125 * f.abs()) | ~outside).all())
+
+
 def test_rows_with_nan_and_inf():
     for dt in (F32, BF16):
         for V in (5, 3000, 40_001):

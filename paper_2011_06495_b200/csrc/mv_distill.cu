@@ -43,9 +43,12 @@ constexpr int MARKS = 4096;          // words of marks: one for each thread and 
 
 // A CTA per row, streamed once with a running reference.  With the rest as a class the listed tokens are kept out of the sum (taking them
 // off it would leave nothing of a small rest): a bit for every logit of the next steps, set for the listed ones, which a thread asks
-// one word at a time; their own terms are added at the end.  Memory bounds it: 8192 x 65536 bf16 162 us (6.6 TB/s), with 32 alternatives
-// and the rest 169.  The end of a row, some microseconds of latency for its list, is covered by the other CTAs unless rows are short
-// (16000 x 8000: 68 us of 39) or few (64 x 131072: 19 us).
+// one word at a time; their own terms are added at the end.  Memory bounds it: 8192 x 65536 bf16 with 32 alternatives 173 us (6.2 TB/s), with
+// the rest 183 (5.9).  The end of a row, some microseconds of latency for its list, is covered by the other CTAs unless rows are short
+// (16000 x 8000 68 us, floor 39; 16384 x 1000 f16 with 50 alternatives 50, floor 6) or few (64 x 131072: 19 us, floor 2.6: a CTA a row).  Times
+// here and below are those of calls that follow one another for half a second, at the power limit; in short runs those that memory
+// bounds take up to a tenth less (161 and 169 us), and the two sides of a rule were compared like that.
+// (Its sums are in 32 bits: lse, log P and so each log p are; the list's sums and the divergence in 64.)
 template <typename X, bool REST, int TPB>
 __global__ void __launch_bounds__(TPB, 1024 / TPB) k_distill(const X* __restrict__ logits, const __grid_constant__ DistillArgs a) {
   constexpr int N = Vec<X>::N, WARPS = TPB / 32, WINDOW = MARKS / TPB;
@@ -257,9 +260,10 @@ __global__ void __launch_bounds__(TPB, 1024 / TPB) k_distill(const X* __restrict
 // ------------------------------------------------------------------------------------------ gradient
 // dx = f (M p - q) for a listed token, f M' p for the others, f = c g, M' = M - r / P.  p = q q with q = 2^h, h = log2(p) / 2: the
 // hardware's exponential has no subnormal results.  Each CTA takes some stretches of one row, and all of the row's list: the others' value is
-// written everywhere, and then its listed tokens' over it.  Memory bounds it: 8192 x 65536 bf16 340 us (6.3 TB/s in and out), 4096 x
-// 131072 with 64 alternatives the same; rows that lie differently within 16 bytes 9000 x 33001 f16 222 us (element by element 877).
-// Short rows wait for their lists: 16384 x 1000 f16 with 50 alternatives 47 us.
+// written everywhere, and then its listed tokens' over it.  Memory bounds it: 8192 x 65536 bf16 354 us (6.1 TB/s in and out), 4096 x
+// 131072 with 64 alternatives 353; 9000 x 33001 f16 196 us, with rows that lie differently within 16 bytes 219 (element by element 877).
+// Short rows wait for their lists: 16384 x 1000 f16 with 50 alternatives 47 us (floor 11); so do long lists, all of which every CTA works out:
+// 2000 x 151936 bf16 with 1024 alternatives 364 us (floor 188).  The shares e_j are kept in 32 bits, half a unit of a result of 32 bits.
 constexpr int GRAD_U = 4, GRAD_EACH = 4;
 
 struct DistillGradArgs {
@@ -477,9 +481,10 @@ int mv_distill_grad(void* stream, const void* logits, int type, int64_t T, int64
   return with_type(type, [&](auto x) {
     using X = decltype(x);
     // The list costs a CTA a few microseconds of latency: as many stretches for each as leave enough CTAs to fill the device, up to a CTA for
-    // four, and none for fewer behind them (4096 x 131072 bf16 with 64 alternatives, 16 stretches: one each 476 us, two 383, four 338,
-    // eight 346, sixteen 361; 9000 x 33001, five: four and one 219, together 194).  Rows of up to 16 KB take small CTAs (16000 x
-    // 8000 bf16: 90 us, with 256 threads 138).
+    // four, or for a few more than to leave a row's last CTA with fewer (4096 x 131072 bf16 with 64 alternatives, 16 stretches: one each
+    // 476 us, two 383, four 338, eight 346, sixteen 361; 9000 x 33001, five: four and one 219, together 194).  Where the device's fill
+    // decides, a row's last CTA has what is left (five as four and one from 948 to 1183 rows: 1003 x 33001 31 us).  Rows of up to 16 KB
+    // take small CTAs (16000 x 8000 bf16: 90 us, with 256 threads 138).
     const int tpb = V * size <= 16384 ? 64 : 256;
     const int64_t per = int64_t(tpb) * GRAD_U * Vec<X>::N, stretches = (V + per - 1) / per;
     const int64_t least = stretches < 2 * GRAD_EACH ? 1 : stretches / GRAD_EACH, most = (stretches + least - 1) / least;

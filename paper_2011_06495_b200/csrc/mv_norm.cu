@@ -4,8 +4,14 @@
 // off is put right by the same pass), r = 1 / sqrt(v + eps), y = (x - mu) r w + b.  Backward, with n = (x - mu) r and h = dy w: the two sums of h and h n in one reduction, dx = r (h -
 // mean h - n mean(h n)); the sums over rows of dy n and dy stay in the registers of the thread that owns the columns, CTA by CTA, and
 // a second kernel adds the CTAs' sums up in their order.  Memory bounds both where rows are many and lie on 16-byte boundaries: 65536 x
-// 2048 bf16 89 us (6.0 TB/s in and out), its gradient 140 us (5.8 TB/s; 137 us without the second kernel); 32768 x 4096 94 and 146.  A few
-// thousand short rows are bound by latency: 2048 x 512 6 and 11 us.
+// 2048 bf16 94 us (5.7 TB/s in and out), its gradient 155 us (5.2 TB/s, 6 us of it the second kernel); 32768 x 4096 99 and 163, 32768 x 2048
+// f32 90 and 148.  A few thousand short rows are bound by latency: 2048 x 512 6 (8 from call to call) and 12.6 us.  Times are those of calls that follow one another for
+// half a second, at the power limit; in short runs memory-bound ones take up to a tenth less (90 and 141 us), and where a comment compares two
+// forms, both were timed like that.
+//
+// Edges: forward, rows of more than 25600 columns (parameters do not fit shared memory), of f32 more than 16384, off the boundaries from 16384
+// on, take k_norm_long, three readings: 4096 x 28000 bf16 236 us (floor 70), 4096 x 16384 f32 off the boundaries 162 (16381 columns: 133,
+// floor 82).  Gradient: see k_norm_grad.
 
 #include "mv_norm.cuh"
 
@@ -114,7 +120,7 @@ __global__ void __launch_bounds__(L > 32 ? WIDE_TPB : NORM_TPB, norm_resident(NV
 // Rows that do not lie on 16-byte boundaries.  The vectors are those of y's row, from its first boundary on (in every row another column); what is
 // before and behind them, up to 31 elements, goes to a lane each.  APART: x lies otherwise within 16 bytes, and comes from between
 // two of its vectors.  Weight and bias of a column side by side, those of every N-th column together, so that neighbouring lanes
-// read neighbouring pairs wherever the vectors begin.  30000 x 1001 bf16: 39 us (element by element 45 to 80); bound by instructions, 25 an
+// read neighbouring pairs wherever the vectors begin.  30000 x 1001 bf16: 39 us (element by element 45 to 80, floor 18); bound by instructions, 25 an
 // element, half of them for the parameters and the shift.
 template <typename X, bool APART, int L, int NV>
 __global__ void __launch_bounds__(L > 32 ? WIDE_TPB : NORM_TPB, L > 32 ? 1 : 2) k_norm_any(const X* x, X* y, const __grid_constant__ NormArgs a) {

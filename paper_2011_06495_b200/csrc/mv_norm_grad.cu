@@ -47,6 +47,10 @@ template <typename X> __device__ __forceinline__ const X* in_image(const char* i
 // shared memory, a.stages deep, so that nothing waits for them but the thread itself; of rows that lie anywhere, as images that their lanes
 // share.  One barrier for R rows.  8191 x 1001 f32 with pitches of 1003 and 1001: 27 us for 98 MB, half of it start, end and the second
 // kernel; 30000 x 1001 bf16 55 us, bound by instructions (an element at a time is read, weighed twice and written).
+// Edges: f32 from 8200 columns on has room for one stage, so that a row's loads are not covered by another's work (8192 x 8192 140 us, 8200 columns
+// 181, floor 123); f32 off the boundaries has no room for two images from 11517 columns on and takes k_norm_grad_long, as everything
+// above 16384 columns does: single elements, sums over rows in memory (4096 x 11500 f32 121 us, 11520 columns 476, floor 86; 4096 x
+// 20480 bf16 998, floor 77).
 template <int L> constexpr int GRAD_THREADS = L > NORM_TPB ? L : NORM_TPB;
 
 template <typename X, bool VEC, int L, int NV, int R>

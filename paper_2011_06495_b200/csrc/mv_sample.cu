@@ -6,15 +6,21 @@
 //
 // A CTA, or a cluster of two to eight where there are few rows, reads its row once for the largest logit, and then, by request:
 //   top k up to 1024           the maxima of groups of tokens give a bound that the top k reach; the tokens beyond it (some more than k)
-//                              are listed, sorted, summed up, cut, and drawn from.  One row of 131072: 12 us, 256 rows 36 (27 with half as
-//                              many CTAs); what is not the reading is a chain of short phases, about 8 us.
+//                              are listed, sorted, summed up, cut, and drawn from.  One row of 131072 bf16: 12 us, 256 rows 34 (greedy) to
+//                              38; what is not the reading is a chain of short phases, about 8 us.
 //   nothing, min p             one more reading (out of L2), 64-bit weights summed by chunks of 512 tokens; the chunk where the limit is
-//                              passed is read again.  256 rows of 131072 bf16 67 us, 1024 of 50021 f32 103: 64-bit arithmetic.
+//                              passed is read again.  256 rows of 131072 bf16 67 us, 1024 of 50021 f32 102: 28 and 43 us of it 64-bit
+//                              arithmetic, the rest the two readings, one after the other in every CTA.
 //   top p, or a larger top k   a count by 4096 bins of the logits first, which bounds where the cut lies, then the same reading with a list of
 //                              the tokens there.  One row 38 us, 256 rows 156.  Where too many lie there (16-bit logits far from zero: a few
-//                              values), a third reading; 64 rows of 131072 bf16 around 10: 125 us.
-// What none of these takes (top p of more than the top 1024, logits beyond 10^6 times a unit of the softmax, lists that overflow twice, more
-// than 10^6 tokens) goes to a plain form with exact cuts by radix, one CTA a row, about ten times as long.
+//                              values), a third reading; 64 rows of 131072 bf16 around 10: 127 us.
+// What none of these takes goes to a plain form with exact cuts by radix, ten readings or more by one CTA, the others of its row gone:
+//   top k and top p together where the list overflows or k is above 1024: one row of 131072 f32, top k 2000 and top p 0.9, 1.5 ms, 64 rows 1.9; equal
+//                              logits meet in one bin, 131072 of them (a constant row, top k 50 and top p 0.9) 34 ms, 64 such rows 40
+//   logits beyond 2^20 times a unit of the softmax (inverse temperatures of 10^5 and more; or below 10^-36): one row 0.34 ms, 64 rows 0.57, greedy 1.0
+//   more than 1 043 000 tokens, unless the top k are listed: 4 rows of 1 500 000 bf16 3.0 ms, with top p 15 (of 1 000 000: 43 us and 0.2 ms)
+//   any other crowd that two passes of narrowing leave of more than one value
+// Times are those of calls that follow one another for half a second.
 
 #include "mv_row.cuh"
 
@@ -1145,9 +1151,9 @@ int mv_sample(void* stream, const void* logits, int type, int64_t T, int64_t V, 
     const int64_t vecs = V / Vec<X>::N;
     a.chunks = V / CHUNK + 10 <= CHUNKS;
     // As many CTAs per row as fill the device twice (requests of different kinds end at different times), a step or more for each: 256 rows of
-    // 131072 bf16, mixed requests: 81 us, once 92, four times 102; all of one kind, top k, 35, 27 and 54.  Rows of 256 KB and more
-    // are shared by two at least, as mixed requests end unevenly (1024 rows: 230 us, by one CTA each 266; 600 of one kind 128 and 139;
-    // rows of 200 KB 113 and 103).
+    // 131072 bf16, mixed requests: 94 us, once 102, four times 119; all of one kind, top k 50 and top p 0.9, 38, 29 and 60, top p alone
+    // 156, 157 and 224.  Rows of 256 KB and more are shared by two at least, as mixed requests end unevenly (1024 rows: 230 us, by one
+    // CTA each 271; 600 with nothing cut 129 and 140; of 200 KB, 1024 of f32 112 and 102, 600 of bf16 108 and 115).
     const int least = vecs >= 16 * TPB * U ? 2 : 1;
     int ctas = MOST_CTAS;
     while (ctas > least && (T * ctas > 2 * 148 * RESIDENT || vecs < int64_t(ctas) * TPB * U)) ctas /= 2;

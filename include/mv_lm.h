@@ -19,9 +19,10 @@
  *
  * Memory and errors follow mv_sparse.h: DEVICE pointers owned by the caller unless said otherwise,
  * nothing is allocated on the device, work is enqueued on `stream` (a cudaStream_t, NULL = default
- * stream) without synchronising the host, on the current device, which is the one of the pointers and of the stream;
- * status codes are MV_OK / MV_ERR_*, and arguments are checked before anything is enqueued.  Pointers need the alignment of their element type only (a table may start
- * anywhere in a worker's row); rows are contiguous and `ld...` elements apart.  Results do not depend
+ * stream) without synchronising the host, on the current device, which is the one of the pointers and of
+ * the stream; status codes are MV_OK / MV_ERR_*, and arguments are checked before anything is enqueued.
+ * Pointers need the alignment of their element type only (a table may start anywhere in a worker's row);
+ * rows are contiguous and `ld...` elements apart.  Results do not depend
  * on the order in which the GPU runs things: the same call on the same inputs gives the same bytes.  Where
  * the inputs lie can change the order of the sums in mv_token_logprob, mv_layer_norm*, mv_distill and mv_clip_* (rows and tensors are
  * cut at their own 16- or 32-byte boundaries), and so can the number of rows; the other calls' bytes do not depend on it.
